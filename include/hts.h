@@ -246,6 +246,101 @@ int32_t     hts_stream_create_cu_range(int32_t first_cu, int32_t n_cus, void **h
 /* Waits for the stream's work and destroys it (streams made by hts_stream_create_cu_range only). */
 int32_t     hts_stream_destroy(void *hip_stream);
 
+/* ---- Sequence memory ---------------------------------------------------------------------------------------------
+ * Operators of a recurrent core between a trunk's features and the heads, for policies that have to remember: matrix products with
+ * bias, activation and residual, a short causal convolution along time, and a selective state space scan, each with its gradients.
+ * A learner runs them over a whole storage, an actor one step at a time (T = 1, the state handed from call to call), a server over
+ * prompts of any length.
+ *
+ * Operand type: binary32 (HTS_PRECISION_FP32) or bfloat16 (HTS_PRECISION_BF16) for activations, their gradients and the matrix
+ * product's weights.  Everything else is binary32: the other parameters, all parameter gradients, the states.  Sums, states and
+ * exponentials are formed in binary32 and an output is rounded once.
+ *
+ * Layout: a row or step is contiguous in its last index and starts anywhere, the distance between rows is the caller's: parts of a
+ * wider array (one projection that holds several operands) are read and written in place.  Strides count elements.  Strides of
+ * inputs may be 0 (one row for all); rows of an output must not overlap each other or any input, except where a comment allows it.
+ *
+ * Sequences: `starts` u8 [T,N] or NULL: 1 = step t begins an episode, nothing from before it is seen.  Rows 1..T of a [T+1,N]
+ * array of starts are the `dones` of hts_returns_gae.  `lengths` i32 [N] or NULL: sequence n has steps 0..lengths[n]-1 (less than
+ * 0 counts as 0, more than T as T); beyond them nothing is read, outputs are 0, and states stay what they were.
+ *
+ * Conventions are those above; the context is of its own type, since these calls need no network: */
+typedef struct hts_seq_ctx hts_seq_ctx;
+
+/* workspace_bytes >= 0: device memory for the calls' intermediate results (partial sums of split reductions and the like).  A call
+ * that needs more than the context has returns HTS_ESHAPE; the hts_*_workspace functions say how much a shape needs. */
+int32_t hts_seq_create(int64_t workspace_bytes, void *hip_stream, hts_seq_ctx **out);
+int32_t hts_seq_destroy(hts_seq_ctx *ctx);
+
+#define HTS_ACT_NONE 0
+#define HTS_ACT_RELU 1
+#define HTS_ACT_SILU 2   /* v / (1 + exp(-v))                 */
+#define HTS_ACT_GELU 3   /* v (1 + erf(v / sqrt(2))) / 2      */
+
+/* Rows of K entries: row m starts at p + m * ld. */
+typedef struct { void *p; int64_t ld; } hts_rows;
+/* Steps of K entries: step t of sequence n starts at p + t * st + n * sn. */
+typedef struct { void *p; int64_t st, sn; } hts_steps;
+
+/* ---- y = act(x W^T + bias) + residual ----
+ *   x [M,K]   w [N,K]   bias f32 [N] or NULL   residual [M,N], p NULL: none; y may take its place
+ *   pre [M,N], p NULL: not wanted; receives x W^T + bias, which the backward call of an activation reads
+ * M, N, K 1 .. 2^24. */
+typedef struct { int32_t M, N, K; int32_t precision, act; } hts_linear_desc;
+/* Bytes of workspace of the call and its backward call; negative error code for an unsupported shape.  Host only. */
+int64_t hts_linear_workspace(const hts_linear_desc *desc);
+int32_t hts_linear(hts_seq_ctx *ctx, const hts_linear_desc *desc, hts_rows x, hts_rows w, const float *bias, hts_rows residual,
+                   hts_rows y, hts_rows pre);
+/* With g = dy act'(pre):  dx = g W + add [M,K],  dw = g^T x f32 [N,K] contiguous,  db = column sums of g f32 [N].
+ * dx.p, dw, db: any may be NULL, not all.  add [M,K], p NULL: none; dx may take its place.  (A residual's own gradient is dy: a
+ * block with a skip hands it over as `add`.)  pre is read for an activation only.  In bfloat16 an activation's g goes to dw and db
+ * unrounded (as the sum of two bfloat16 numbers), and rounded once to dx. */
+int32_t hts_linear_backward(hts_seq_ctx *ctx, const hts_linear_desc *desc, hts_rows x, hts_rows w, hts_rows pre, hts_rows dy,
+                            hts_rows add, hts_rows dx, float *dw, float *db);
+
+/* ---- short causal convolution along time, a filter for each channel ----
+ *   v_t = bias + sum_j w[d,j] x_{t-W+1+j},  j = 0..W-1, over the steps of t's episode;  y = act(v), act NONE or SILU
+ *   x, y [T,N,D]   w f32 [D,W], W 2..4   bias f32 [D] or NULL
+ *   state_in f32 [N,W-1,D] or NULL (zeros): the last W-1 inputs before step 0, oldest first; state_out or NULL: those after the
+ *   last step, with zeros for what lies before its episode.  state_out may be state_in. */
+typedef struct { int32_t T, N, D, W; int32_t precision, act; } hts_short_conv_desc;
+int64_t hts_short_conv_workspace(const hts_short_conv_desc *desc);
+int32_t hts_short_conv(hts_seq_ctx *ctx, const hts_short_conv_desc *desc, hts_steps x, const float *w, const float *bias,
+                       const uint8_t *starts, const int32_t *lengths, const float *state_in, hts_steps y, float *state_out);
+/* Gradients of dy and dstate_out (f32 [N,W-1,D], NULL: zeros): dx [T,N,D], dw f32 [D,W], db f32 [D] or NULL, dstate_in f32
+ * [N,W-1,D] or NULL. */
+int32_t hts_short_conv_backward(hts_seq_ctx *ctx, const hts_short_conv_desc *desc, hts_steps x, const float *w, const float *bias,
+                                const uint8_t *starts, const int32_t *lengths, const float *state_in, hts_steps dy,
+                                const float *dstate_out, hts_steps dx, float *dw, float *db, float *dstate_in);
+
+/* ---- selective state space scan ----
+ *   delta = softplus(dt + dt_bias) (softplus = 1) or dt + dt_bias (0);  for every channel d, of group k = d / (D / G), and state s:
+ *   h_t[d,s] = exp(delta A[d,s]) h_{t-1}[d,s] + delta x B_t[k,s];   y = (sum_s C_t[k,s] h_t[d,s] + skip[d] x) * z / (1 + exp(-z))
+ *   x, dt, z, y [T,N,D] (z.p NULL: no gate)   B, C [T,N,G*S], S 1..64, G divides D
+ *   A f32 [D,S]   skip, dt_bias f32 [D] or NULL (zeros)
+ *   h_in f32 [N,D,S] or NULL (zeros); h_out or NULL: the state after the last step.  h_out may be h_in.
+ *   states f32 or NULL: receives what the backward call needs of the states, hts_selective_scan_states(desc) floats. */
+typedef struct { int32_t T, N, D, S, G; int32_t precision, softplus; } hts_scan_desc;
+typedef struct {
+    hts_steps x, dt, B, C, z;
+    const float *A, *skip, *dt_bias;
+    const uint8_t *starts;
+    const int32_t *lengths;
+    const float *h_in;
+} hts_scan_inputs;
+int64_t hts_selective_scan_workspace(const hts_scan_desc *desc);
+int64_t hts_selective_scan_states(const hts_scan_desc *desc);
+int32_t hts_selective_scan(hts_seq_ctx *ctx, const hts_scan_desc *desc, const hts_scan_inputs *in, hts_steps y, float *h_out,
+                           float *states);
+/* Gradients of dy and dh_out (f32 [N,D,S], NULL: zeros), `states` as the forward call on the same inputs left it.  dz.p is NULL
+ * where there is no gate; dskip, ddt_bias and dh_in may be NULL. */
+typedef struct {
+    hts_steps dx, ddt, dB, dC, dz;
+    float *dA, *dskip, *ddt_bias, *dh_in;
+} hts_scan_grads;
+int32_t hts_selective_scan_backward(hts_seq_ctx *ctx, const hts_scan_desc *desc, const hts_scan_inputs *in, hts_steps dy,
+                                    const float *dh_out, const float *states, const hts_scan_grads *grads);
+
 int32_t     hts_last_hip_error(void);
 const char *hts_strerror(int32_t code);
 

@@ -12,12 +12,15 @@ LIB_PATH = os.path.join(_HERE, "libhts.so")
 PRECISION_FP32, PRECISION_BF16 = 0, 1
 ALGO_A2C, ALGO_PPO, ALGO_A2C_TIS = 0, 1, 2
 OPT_ADAM, OPT_RMSPROP = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 EXPORTS = ["hts_param_count", "hts_create", "hts_destroy", "hts_act", "hts_sync_params", "hts_sample_from_logits", "hts_returns_gae",
            "hts_normalize_advantages", "hts_learner_step", "hts_learner_step_delayed", "hts_loss_and_grads", "hts_adam_apply", "hts_test_gemm",
            "hts_last_hip_error", "hts_strerror", "hts_profile_site_count", "hts_profile_site_name", "hts_profile_begin",
            "hts_profile_end", "hts_profile_overhead", "hts_profile_begin_sampled", "hts_adam_apply_static", "hts_track_params",
-           "hts_stream_create_cu_range", "hts_stream_destroy"]
+           "hts_stream_create_cu_range", "hts_stream_destroy", "hts_seq_create", "hts_seq_destroy", "hts_linear_workspace", "hts_linear",
+           "hts_linear_backward", "hts_short_conv_workspace", "hts_short_conv", "hts_short_conv_backward", "hts_selective_scan_workspace",
+           "hts_selective_scan_states", "hts_selective_scan", "hts_selective_scan_backward"]
 
 
 class HtsError(RuntimeError):
@@ -56,6 +59,36 @@ class OptState:
 
     def __init__(self, m: torch.Tensor, v: torch.Tensor, step: int = 0):
         self.m, self.v, self.step = m, v, step
+
+
+class _Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64)]
+
+
+class _Steps(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("st", C.c_int64), ("sn", C.c_int64)]
+
+
+class _LinearDesc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("M", "N", "K", "precision", "act")]
+
+
+class _ConvDesc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("T", "N", "D", "W", "precision", "act")]
+
+
+class _ScanDesc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("T", "N", "D", "S", "G", "precision", "softplus")]
+
+
+class _ScanInputs(C.Structure):
+    _fields_ = [("x", _Steps), ("dt", _Steps), ("B", _Steps), ("C", _Steps), ("z", _Steps), ("A", C.c_void_p), ("skip", C.c_void_p),
+                ("dt_bias", C.c_void_p), ("starts", C.c_void_p), ("lengths", C.c_void_p), ("h_in", C.c_void_p)]
+
+
+class _ScanGrads(C.Structure):
+    _fields_ = [("dx", _Steps), ("ddt", _Steps), ("dB", _Steps), ("dC", _Steps), ("dz", _Steps), ("dA", C.c_void_p), ("dskip", C.c_void_p),
+                ("ddt_bias", C.c_void_p), ("dh_in", C.c_void_p)]
 
 
 STATS_FIELDS = ("policy_loss", "value_loss", "entropy", "grad_norm", "clip_frac", "approx_kl", "nonfinite")
@@ -105,6 +138,19 @@ def load_library():
         lib.hts_profile_overhead.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_double)]
         lib.hts_stream_create_cu_range.argtypes = [C.c_int32, C.c_int32, C.POINTER(C.c_void_p)]
         lib.hts_stream_destroy.argtypes = [C.c_void_p]
+        vp, rows, steps = C.c_void_p, _Rows, _Steps
+        lib.hts_seq_create.argtypes = [C.c_int64, vp, C.POINTER(vp)]
+        lib.hts_seq_destroy.argtypes = [vp]
+        for f, desc in (("hts_linear_workspace", _LinearDesc), ("hts_short_conv_workspace", _ConvDesc), ("hts_selective_scan_workspace", _ScanDesc),
+                        ("hts_selective_scan_states", _ScanDesc)):
+            getattr(lib, f).restype = C.c_int64
+            getattr(lib, f).argtypes = [C.POINTER(desc)]
+        lib.hts_linear.argtypes = [vp, C.POINTER(_LinearDesc), rows, rows, vp, rows, rows, rows]
+        lib.hts_linear_backward.argtypes = [vp, C.POINTER(_LinearDesc), rows, rows, rows, rows, rows, rows, vp, vp]
+        lib.hts_short_conv.argtypes = [vp, C.POINTER(_ConvDesc), steps, vp, vp, vp, vp, vp, steps, vp]
+        lib.hts_short_conv_backward.argtypes = [vp, C.POINTER(_ConvDesc), steps, vp, vp, vp, vp, vp, steps, vp, steps, vp, vp, vp]
+        lib.hts_selective_scan.argtypes = [vp, C.POINTER(_ScanDesc), C.POINTER(_ScanInputs), steps, vp, vp]
+        lib.hts_selective_scan_backward.argtypes = [vp, C.POINTER(_ScanDesc), C.POINTER(_ScanInputs), steps, vp, vp, C.POINTER(_ScanGrads)]
         _lib = lib
     return _lib
 
@@ -332,3 +378,170 @@ class Context:
         d = {k: float(h[i]) for i, k in enumerate(STATS_FIELDS[:6])}
         d["nonfinite"] = int(h[6:7].view(torch.int32)[0])
         return d
+
+
+# ---- sequence memory --------------------------------------------------------------------------------------------------
+_DTYPE = {PRECISION_FP32: torch.float32, PRECISION_BF16: torch.bfloat16}
+_NO_ROWS, _NO_STEPS = _Rows(None, 0), _Steps(None, 0, 0)
+
+
+def _size(what: str, rc: int) -> int:
+    if rc < 0:
+        _check(rc, what)
+    return rc
+
+
+def linear_workspace(M: int, N: int, K: int, precision: int = PRECISION_FP32, act: int = ACT_NONE) -> int:
+    """Bytes of workspace that hts_linear and hts_linear_backward need for M rows, N outputs and K inputs."""
+    return _size("hts_linear_workspace", load_library().hts_linear_workspace(C.byref(_LinearDesc(M, N, K, precision, act))))
+
+
+def short_conv_workspace(T: int, N: int, D: int, W: int, precision: int = PRECISION_FP32) -> int:
+    return _size("hts_short_conv_workspace", load_library().hts_short_conv_workspace(C.byref(_ConvDesc(T, N, D, W, precision, ACT_NONE))))
+
+
+def selective_scan_workspace(T: int, N: int, D: int, S: int, G: int = 1, precision: int = PRECISION_FP32) -> int:
+    return _size("hts_selective_scan_workspace", load_library().hts_selective_scan_workspace(C.byref(_ScanDesc(T, N, D, S, G, precision, 1))))
+
+
+def selective_scan_states(T: int, N: int, D: int, S: int, G: int = 1) -> int:
+    """Floats of the `states` that a training forward call hands to its backward call."""
+    return _size("hts_selective_scan_states", load_library().hts_selective_scan_states(C.byref(_ScanDesc(T, N, D, S, G, PRECISION_FP32, 1))))
+
+
+def _precision(t, name):
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16):
+        raise HtsError(f"{name}: expected a float32 or bfloat16 device tensor")
+    return PRECISION_BF16 if t.dtype == torch.bfloat16 else PRECISION_FP32
+
+
+def _rows(t, dtype, shape, name):
+    """A [M, K] operand whose rows are contiguous, at any distance."""
+    if t is None:
+        return _NO_ROWS
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape:
+        raise HtsError(f"{name}: expected a {dtype} device tensor of shape {shape}")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise HtsError(f"{name}: rows must be contiguous")
+    return _Rows(t.data_ptr(), ld)
+
+
+def _steps(t, dtype, shape, name):
+    """A [T, N, ...] operand whose steps are contiguous, at any distance."""
+    if t is None:
+        return _NO_STEPS
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape:
+        raise HtsError(f"{name}: expected a {dtype} device tensor of shape {shape}")
+    st = t.stride()
+    inner = 1
+    for size, stride in zip(shape[:1:-1], st[:1:-1]):
+        if stride != inner and size > 1:
+            raise HtsError(f"{name}: steps must be contiguous")
+        inner *= size
+    return _Steps(t.data_ptr(), st[0], st[1])
+
+
+def _array(t, dtype, shape, name):
+    """A contiguous array of that shape, or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise HtsError(f"{name}: expected a contiguous {dtype} device tensor of shape {shape}")
+    return t.data_ptr()
+
+
+class SeqContext:
+    """Owns an hts_seq_ctx bound to a torch stream (default: the current stream at construction): the operators of a sequence memory.
+    workspace_bytes: the most that any of its calls needs (linear_workspace, short_conv_workspace, selective_scan_workspace)."""
+
+    def __init__(self, workspace_bytes=0, stream=None):
+        self.lib = load_library()
+        if not torch.cuda.is_available():
+            raise HtsError("no GPU visible: the library has no CPU path")
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self._h = C.c_void_p()
+        _check(self.lib.hts_seq_create(workspace_bytes, C.c_void_p(self.stream.cuda_stream), C.byref(self._h)), "hts_seq_create")
+
+    def close(self):
+        if getattr(self, "_h", None) and self._h.value:
+            self.stream.synchronize()
+            self.lib.hts_seq_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def hts_linear(self, x, w, y, bias=None, residual=None, pre=None, act=ACT_NONE):
+        """y = act(x w^T + bias) + residual; pre receives x w^T + bias."""
+        prec = _precision(x, "x")
+        dt, (M, K), N = _DTYPE[prec], x.shape, w.shape[0]
+        _check(self.lib.hts_linear(self._h, C.byref(_LinearDesc(M, N, K, prec, act)), _rows(x, dt, (M, K), "x"), _rows(w, dt, (N, K), "w"),
+                                   _array(bias, torch.float32, (N,), "bias"), _rows(residual, dt, (M, N), "residual"), _rows(y, dt, (M, N), "y"),
+                                   _rows(pre, dt, (M, N), "pre")), "hts_linear")
+
+    def hts_linear_backward(self, x, w, dy, pre=None, act=ACT_NONE, add=None, dx=None, dw=None, db=None):
+        """With g = dy act'(pre): dx = g w + add, dw = g^T x, db = column sums of g; each of the three only where it is given."""
+        prec = _precision(dy, "dy")
+        dt, (M, N), K = _DTYPE[prec], dy.shape, w.shape[1]
+        _check(self.lib.hts_linear_backward(self._h, C.byref(_LinearDesc(M, N, K, prec, act)), _rows(x, dt, (M, K), "x"), _rows(w, dt, (N, K), "w"),
+                                            _rows(pre, dt, (M, N), "pre"), _rows(dy, dt, (M, N), "dy"), _rows(add, dt, (M, K), "add"),
+                                            _rows(dx, dt, (M, K), "dx"), _array(dw, torch.float32, (N, K), "dw"),
+                                            _array(db, torch.float32, (N,), "db")), "hts_linear_backward")
+
+    @staticmethod
+    def _sequences(starts, lengths, T, N):
+        return _array(starts, torch.uint8, (T, N), "starts"), _array(lengths, torch.int32, (N,), "lengths")
+
+    def hts_short_conv(self, x, w, y, bias=None, act=ACT_NONE, starts=None, lengths=None, state_in=None, state_out=None):
+        prec, (T, N, D), W, f = _precision(x, "x"), x.shape, w.shape[-1], torch.float32
+        dt, state = _DTYPE[prec], (N, W - 1, D)
+        _check(self.lib.hts_short_conv(self._h, C.byref(_ConvDesc(T, N, D, W, prec, act)), _steps(x, dt, (T, N, D), "x"), _array(w, f, (D, W), "w"),
+                                       _array(bias, f, (D,), "bias"), *self._sequences(starts, lengths, T, N),
+                                       _array(state_in, f, state, "state_in"), _steps(y, dt, (T, N, D), "y"),
+                                       _array(state_out, f, state, "state_out")), "hts_short_conv")
+
+    def hts_short_conv_backward(self, x, w, dy, dx, dw, db=None, bias=None, act=ACT_NONE, starts=None, lengths=None, state_in=None, dstate_out=None,
+                                dstate_in=None):
+        prec, (T, N, D), W, f = _precision(x, "x"), x.shape, w.shape[-1], torch.float32
+        dt, state = _DTYPE[prec], (N, W - 1, D)
+        _check(self.lib.hts_short_conv_backward(self._h, C.byref(_ConvDesc(T, N, D, W, prec, act)), _steps(x, dt, (T, N, D), "x"),
+                                                _array(w, f, (D, W), "w"), _array(bias, f, (D,), "bias"), *self._sequences(starts, lengths, T, N),
+                                                _array(state_in, f, state, "state_in"), _steps(dy, dt, (T, N, D), "dy"),
+                                                _array(dstate_out, f, state, "dstate_out"), _steps(dx, dt, (T, N, D), "dx"),
+                                                _array(dw, f, (D, W), "dw"), _array(db, f, (D,), "db"), _array(dstate_in, f, state, "dstate_in")),
+               "hts_short_conv_backward")
+
+    def _scan(self, x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in):
+        prec, (T, N, D), f = _precision(x, "x"), x.shape, torch.float32
+        S, G, ty = A.shape[-1], B.shape[2] if B.dim() == 4 else 1, _DTYPE[prec]
+        pair = (T, N, G, S) if B.dim() == 4 else (T, N, S)
+        st, le = self._sequences(starts, lengths, T, N)
+        inputs = _ScanInputs(_steps(x, ty, (T, N, D), "x"), _steps(dt, ty, (T, N, D), "dt"), _steps(B, ty, pair, "B"), _steps(C_, ty, pair, "C"),
+                             _steps(z, ty, (T, N, D), "z"), _array(A, f, (D, S), "A"), _array(skip, f, (D,), "skip"),
+                             _array(dt_bias, f, (D,), "dt_bias"), st, le, _array(h_in, f, (N, D, S), "h_in"))
+        return _ScanDesc(T, N, D, S, G, prec, 1 if softplus else 0), inputs, ty, (T, N, D), pair, (N, D, S)
+
+    def hts_selective_scan(self, x, dt, A, B, C_, y, z=None, skip=None, dt_bias=None, softplus=True, starts=None, lengths=None, h_in=None, h_out=None,
+                           states=None):
+        desc, inputs, ty, cells, _, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
+        if states is not None and states.numel() < selective_scan_states(desc.T, desc.N, desc.D, desc.S, desc.G):
+            raise HtsError("states: too few entries (selective_scan_states)")
+        _check(self.lib.hts_selective_scan(self._h, C.byref(desc), C.byref(inputs), _steps(y, ty, cells, "y"),
+                                           _array(h_out, torch.float32, held, "h_out"), _ptr(states, torch.float32, "states")), "hts_selective_scan")
+
+    def hts_selective_scan_backward(self, x, dt, A, B, C_, dy, states, dx, ddt, dB, dC, dA, z=None, dz=None, skip=None, dskip=None, dt_bias=None,
+                                    ddt_bias=None, softplus=True, starts=None, lengths=None, h_in=None, dh_out=None, dh_in=None):
+        desc, inputs, ty, cells, pair, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
+        if states is None or states.numel() < selective_scan_states(desc.T, desc.N, desc.D, desc.S, desc.G):
+            raise HtsError("states: too few entries (selective_scan_states)")
+        f, D = torch.float32, desc.D
+        grads = _ScanGrads(_steps(dx, ty, cells, "dx"), _steps(ddt, ty, cells, "ddt"), _steps(dB, ty, pair, "dB"), _steps(dC, ty, pair, "dC"),
+                           _steps(dz, ty, cells, "dz"), _array(dA, f, (D, desc.S), "dA"), _array(dskip, f, (D,), "dskip"),
+                           _array(ddt_bias, f, (D,), "ddt_bias"), _array(dh_in, f, held, "dh_in"))
+        _check(self.lib.hts_selective_scan_backward(self._h, C.byref(desc), C.byref(inputs), _steps(dy, ty, cells, "dy"),
+                                                    _array(dh_out, f, held, "dh_out"), _ptr(states, f, "states"), C.byref(grads)),
+               "hts_selective_scan_backward")

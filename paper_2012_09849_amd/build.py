@@ -8,7 +8,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhts.so")
-SOURCES = ["api.hip", "fwd.hip", "bwd.hip", "misc.hip"]
+SOURCES = ["api.hip", "fwd.hip", "bwd.hip", "misc.hip", "seqapi.hip", "linear.hip", "shortconv.hip", "scan.hip"]
 COMMON = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 PER_FILE = {"misc.hip": ["-ffp-contract=off"]}
@@ -24,7 +24,7 @@ def _compile(src: str) -> str:
 
 
 def build(verbose: bool = False) -> str:
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, SOURCES))
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,--no-undefined", "-o", LIB] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -108,7 +108,7 @@ void carve(Ctx &c, Carver &cv)
 }  // namespace
 
 // compute units that a stream's kernels run on: the device's, or those of its range (see hts_stream_create_cu_range)
-static int stream_cus(hipStream_t stream)
+int hts::stream_cus(hipStream_t stream)
 {
     int dev = 0, cus = 0;
     if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1 || cus > 1024) {

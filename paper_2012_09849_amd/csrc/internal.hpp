@@ -136,6 +136,7 @@ struct LossArgs {
     float rho_bar, value_clip;        // truncation level of the importance weight; radius of the clipped value loss (<= 0: off)
 };
 
+int stream_cus(hipStream_t stream);          // api.hip: compute units that its kernels run on
 // api.hip: remembers a HIP error code for hts_last_hip_error()
 void note_hip_error(hipError_t e);
 // fwd.hip

@@ -1,0 +1,121 @@
+// Sequence memory: declarations and device helpers shared by linear.hip, shortconv.hip, scan.hip and seqapi.hip (not part of the C ABI).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/hts.h"
+#include "gemm.hpp"
+
+struct hts_seq_ctx {
+    hipStream_t stream;
+    int cus;                  // compute units that the stream's kernels run on
+    char *ws;
+    int64_t bytes;
+};
+
+namespace hts {
+
+int stream_cus(hipStream_t stream);       // api.hip
+
+struct LinearOp {
+    int M, N, K, act;
+    hts_rows x, w, residual, y, pre, dy, add, dx;
+    const float *bias;
+    float *dw, *db;
+};
+struct ConvOp {
+    int T, N, D, W, act;
+    hts_steps x, y, dy, dx;
+    const float *w, *bias, *state_in, *dstate_out;
+    float *state_out, *dw, *db, *dstate_in;
+    const uint8_t *starts;
+    const int32_t *lengths;
+};
+struct ScanOp {
+    hts_scan_desc d;
+    hts_scan_inputs in;
+    hts_steps y, dy;
+    float *h_out, *states_out;
+    const float *dh_out, *states;
+    hts_scan_grads g;
+};
+
+int64_t linear_workspace(int precision, int act, int64_t M, int64_t N, int64_t K);
+int64_t conv_workspace(int64_t T, int64_t N, int64_t D, int W);
+int64_t scan_workspace(const hts_scan_desc &d);
+int64_t scan_states(const hts_scan_desc &d);
+hipError_t launch_linear(hts_seq_ctx &c, int precision, const LinearOp &op);
+hipError_t launch_linear_backward(hts_seq_ctx &c, int precision, const LinearOp &op);
+hipError_t launch_conv(hts_seq_ctx &c, int precision, const ConvOp &op);
+hipError_t launch_conv_backward(hts_seq_ctx &c, int precision, const ConvOp &op);
+hipError_t launch_scan(hts_seq_ctx &c, const ScanOp &op);
+hipError_t launch_scan_backward(hts_seq_ctx &c, const ScanOp &op);
+
+// out = sum over p of part[p][0 .. width), in a fixed order; consecutive entries go to up to three arrays (p NULL: not wanted)
+struct SumTarget { float *p; int64_t n; };
+hipError_t launch_sum_partials(hts_seq_ctx &c, const float *part, int64_t parts, int64_t width, SumTarget a, SumTarget b, SumTarget d);
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+constexpr float LOG2E = 1.44269504088896341f;
+
+// exp, 1 / (1 + exp(-v)): one rounding of the exponent and the matrix unit's neighbours' 1 ulp exp2 and reciprocal; exact limits at both ends
+__device__ __forceinline__ float exp_f(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }
+__device__ __forceinline__ float sigmoid_f(float v) { return __builtin_amdgcn_rcpf(1.0f + exp_f(-v)); }
+// log(1 + e), 0 <= e <= 1, to a few ulp where 1 + e would lose e's bits: 2 artanh(e / (2 + e)), |argument| <= 1/3, eight terms of its series
+__device__ __forceinline__ float log1p_f(float e)
+{
+    const float w = e * __builtin_amdgcn_rcpf(2.0f + e), q = w * w;
+    float p = 1.0f / 17.0f;
+    p = __builtin_fmaf(p, q, 1.0f / 15.0f); p = __builtin_fmaf(p, q, 1.0f / 13.0f); p = __builtin_fmaf(p, q, 1.0f / 11.0f);
+    p = __builtin_fmaf(p, q, 1.0f / 9.0f); p = __builtin_fmaf(p, q, 1.0f / 7.0f); p = __builtin_fmaf(p, q, 1.0f / 5.0f);
+    p = __builtin_fmaf(p, q, 1.0f / 3.0f);
+    return __builtin_fmaf(2.0f * w, q * p, 2.0f * w);
+}
+// softplus and its slope, the logistic function, from one exponential; NaN stays NaN
+__device__ __forceinline__ void softplus_f(float v, float &value, float &slope)
+{
+    const float e = exp_f(-__builtin_fabsf(v)), r = __builtin_amdgcn_rcpf(1.0f + e);
+    value = (v > 0.0f ? v : 0.0f) + log1p_f(e);
+    slope = v >= 0.0f ? r : e * r;
+}
+
+template <int ACT> __device__ __forceinline__ float act_f(float v)
+{
+    if constexpr (ACT == HTS_ACT_RELU) return v < 0.0f ? 0.0f : v;
+    if constexpr (ACT == HTS_ACT_SILU) return v == -__builtin_inff() ? 0.0f : v * sigmoid_f(v);
+    if constexpr (ACT == HTS_ACT_GELU) return v == -__builtin_inff() ? 0.0f : 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    return v;
+}
+template <int ACT> __device__ __forceinline__ float act_slope(float v)
+{
+    if constexpr (ACT == HTS_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == HTS_ACT_SILU) {
+        const float s = sigmoid_f(v);
+        return __builtin_isinf(v) ? (v > 0.0f ? 1.0f : 0.0f) : s * (1.0f + v * (1.0f - s));
+    }
+    if constexpr (ACT == HTS_ACT_GELU)
+        return __builtin_isinf(v) ? (v > 0.0f ? 1.0f : 0.0f) : 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * 0.39894228040143268f * exp_f(-0.5f * v * v);
+    return 1.0f;
+}
+__device__ __forceinline__ float act_of(int act, float v)
+{
+    return act == HTS_ACT_RELU ? act_f<HTS_ACT_RELU>(v) : act == HTS_ACT_SILU ? act_f<HTS_ACT_SILU>(v) : act == HTS_ACT_GELU ? act_f<HTS_ACT_GELU>(v) : v;
+}
+__device__ __forceinline__ float slope_of(int act, float v)
+{
+    return act == HTS_ACT_RELU ? act_slope<HTS_ACT_RELU>(v) : act == HTS_ACT_SILU ? act_slope<HTS_ACT_SILU>(v) : act == HTS_ACT_GELU ? act_slope<HTS_ACT_GELU>(v) : 1.0f;
+}
+
+// V entries from memory, or one at a time where their address is no multiple of their size
+template <typename T, int V> struct Loaded { T e[V]; };
+template <typename T, int V> __device__ __forceinline__ Loaded<T, V> load_v(const T *p)
+{
+    Loaded<T, V> r;
+    __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(T) * V), sizeof r);
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void store_v(T *p, const Loaded<T, V> &v) { __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T) * V), &v, sizeof v); }
+
+}  // namespace hts
