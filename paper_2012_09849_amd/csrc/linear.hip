@@ -4,39 +4,49 @@
 // product, dz of dx) or across (W of dx, both operands of dw).  An operand tile is copied to LDS as it lies in memory, 16 bytes at a time; one along k
 // is read by rows, one across by the transposing LDS read in bfloat16 (four neighbouring k of a column a lane) and word by word in binary32.
 //   bfloat16: v_mfma_f32_32x32x16_bf16, k-tiles of 64;  binary32: v_mfma_f32_32x32x2_f32, k-tiles of 32.
-// The operands go to the instruction in exchanged order, so a lane holds a row of C and four neighbouring columns of it.
+// The operands go to the instruction in exchanged order, so a lane holds a row of C and four neighbouring columns of it; the sums go through LDS
+// once more, so that rows leave as whole lines, with bias, activation and residual on the way.
+// Rows that are whole numbers of 16 bytes, at addresses that are, are copied straight into LDS (buffer_load ... lds), a k-tile ahead; others
+// through registers, entry by entry where a row ends.
+#include "dmagemm.hpp"
 #include "seq.hpp"
 
 namespace hts {
 namespace {
 
 struct Product {
-    const void *a, *b, *a_low;     // a_low: the same operand's low part; the reduction goes over it, with the same b, after a
+    const void *a, *b;
+    int64_t part_stride;           // A may be the sum of `parts` matrices that far apart (entries): the reduction goes over each in turn, with the same b
+    int parts;
     int64_t lda, ldb;
     int M, N, K;                   // C is M x N, reduction over K
-    int klen;                      // reduction of a slice (of both parts of A together), whole k-tiles
+    int klen;                      // reduction of a slice (of all parts of A together), whole k-tiles
     int act;
     const float *bias;
     const void *res;
     void *y, *pre;
     int64_t ldr, ldy, ldp;
-    float *part;                   // slices > 1: [slice][M][N]
+    float *rows;                   // receives A's own sums over the reduction (db), NULL: not wanted.  y NULL: nothing else is wanted
+    float *part;                   // slices > 1: [slice][M][N], then [M] for `rows`
+    int64_t stride;                // entries from slice to slice, a multiple of 4
+    int slices;
+    int words;                     // which of y, pre and res have rows of 16-byte words
 };
+enum { WORDS_Y = 1, WORDS_PRE = 2, WORDS_RES = 4 };
 
 template <typename T> struct Kind { static constexpr int V = 16 / sizeof(T), BK = 128 / sizeof(T); };       // entries of 16 bytes, k-tile
 
 // where the 16 bytes with number s (along the row) of row r of an operand tile are, for operands along k: rows of 128 bytes, the slots exchanged so
 // that the rows of an operand read fall into different banks
-__device__ __forceinline__ int along_at(int r, int s) { return r * 128 + 16 * (s ^ ((r >> 1) & 7)); }
+__host__ __device__ __forceinline__ int along_slot(int r, int s) { return s ^ ((r >> 1) & 7); }
 // ... and for operands across: rows are k, B the tile's width.  bfloat16: 32-byte pieces exchanged by k, so that the four rows of a transposing read
-// fall into different banks; binary32: halves of 128 bytes by k's bit 2, which the two halves of a wavefront differ in
-template <typename T, int B> __device__ __forceinline__ int across_at(int k, int s)
+// fall into different banks (of 32 entries four rows are all of them); binary32: 128-byte halves by k's bit 2, in which the halves of a wavefront differ
+template <typename T, int B> __host__ __device__ __forceinline__ int across_slot(int k, int s)
 {
-    if constexpr (sizeof(T) == 2) {
-        const int f = B >= 128 ? ((k & 3) << 1 | (k >> 2 & 1)) : (k >> 1 & 1) << 1;
-        return k * (B * 2) + ((s ^ f << 1) << 4);
-    } else return k * (B * 4) + ((s ^ (k >> 2 & 1) << 3) << 4);
+    if constexpr (sizeof(T) == 2) return s ^ (B >= 128 ? (k & 3) << 2 | (k >> 2 & 1) << 1 : B >= 64 ? (k >> 1 & 1) << 2 : 0);
+    else return B >= 64 ? s ^ (k >> 2 & 1) << 3 : s;
 }
+template <typename T, bool ACROSS, int B> __device__ __forceinline__ int piece_at(int r, int s) { return ACROSS ? r * (B * (int)sizeof(T)) + 16 * across_slot<T, B>(r, s) : r * 128 + 16 * along_slot(r, s); }
 
 struct Piece { uint32_t w[4]; };
 template <typename T> __device__ __forceinline__ Piece load_piece(const T *p, int64_t count)
@@ -72,7 +82,43 @@ template <typename T, bool ACROSS, int B, int THREADS> struct Staged {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int r = (i * THREADS + tid) / SLOTS, s = (i * THREADS + tid) % SLOTS;
-            *reinterpret_cast<Piece *>(lds + (ACROSS ? across_at<T, B>(r, s) : along_at(r, s))) = v[i];
+            *reinterpret_cast<Piece *>(lds + piece_at<T, ACROSS, B>(r, s)) = v[i];
+        }
+    }
+};
+
+// The same tile copied straight into LDS by WAVES wavefronts: 1 KB an instruction.  The exchange of slots is in the lanes' addresses; a piece that
+// is not there gets an address beyond the matrix, which reads as zero.
+template <typename T, bool ACROSS, int B, int WAVES> struct Copied {
+    static constexpr int V = Kind<T>::V, BK = Kind<T>::BK, COPIES = B / 8 / WAVES, SLOTS = ACROSS ? B / V : BK / V;
+    static_assert(COPIES * 8 * WAVES == B, "tile");
+    uint32_t at[COPIES];           // bytes from the tile's first row (along) or from the k-tile's (across)
+    int col[COPIES];               // along: k within the k-tile
+    const T *p;
+    int64_t ld;
+    int first, edge, K;
+    __device__ __forceinline__ void open(const T *p_, int64_t ld_, int first_, int edge_, int K_, int wave, int lane)
+    {
+        p = p_; ld = ld_; first = first_; edge = edge_; K = K_;
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int piece = (wave * COPIES + i) * 64 + lane, r = piece / SLOTS, phys = piece % SLOTS;
+            const int s = ACROSS ? across_slot<T, B>(r, phys) : along_slot(r, phys);
+            col[i] = s * V;
+            at[i] = (uint32_t)((r * ld + (ACROSS ? first : 0) + s * V) * (int64_t)sizeof(T));
+            if (ACROSS && first + s * V >= edge) at[i] = 0xfffffff0u;
+        }
+    }
+    __device__ __forceinline__ void copy(int k0, char *lds, int wave, int64_t part) const
+    {
+        const int row = ACROSS ? k0 : first, rows = ACROSS ? K : edge;
+        const T *base = p + part + row * ld;
+        const int64_t bytes = ((rows - 1 - row) * ld + (ACROSS ? edge : K)) * (int64_t)sizeof(T);
+        const __amdgpu_buffer_rsrc_t src = dma_source(base, (uint32_t)(bytes < 0xfffffff0ll ? bytes : 0xfffffff0ll));
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const uint32_t off = ACROSS ? at[i] : k0 + col[i] < K ? at[i] + (uint32_t)(k0 * (int)sizeof(T)) : 0xfffffff0u;
+            dma16(src, off, 0, (const bf16_t *)(lds + (wave * COPIES + i) * 1024));
         }
     }
 };
@@ -83,10 +129,10 @@ typedef __attribute__((address_space(3))) i16x4 *lds_quad;
 // operands of a k-tile's kk-th part (16 k in bfloat16, 8 in binary32) for 32 entries from `at`
 template <typename T, bool ACROSS, int B> __device__ __forceinline__ Vec<T, Kind<T>::V> operand(const char *lds, int at, int kk, int lane)
 {
-    if constexpr (!ACROSS) return *reinterpret_cast<const Vec<T, Kind<T>::V> *>(lds + along_at(at + (lane & 31), 2 * kk + (lane >> 5)));
+    if constexpr (!ACROSS) return *reinterpret_cast<const Vec<T, Kind<T>::V> *>(lds + piece_at<T, false, B>(at + (lane & 31), 2 * kk + (lane >> 5)));
     else if constexpr (sizeof(T) == 2) {
         const int k = kk * 16 + (lane >> 5) * 8 + (lane >> 2 & 3), col = at + (lane & 16) + (lane & 3) * 4;
-        const char *q0 = lds + across_at<T, B>(k, col >> 3) + (col & 7) * 2, *q1 = lds + across_at<T, B>(k + 4, col >> 3) + (col & 7) * 2;
+        const char *q0 = lds + piece_at<T, true, B>(k, col >> 3) + (col & 7) * 2, *q1 = lds + piece_at<T, true, B>(k + 4, col >> 3) + (col & 7) * 2;
         const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad)(uintptr_t)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)q0);
         const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad)(uintptr_t)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)q1);
         const short both[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -97,7 +143,7 @@ template <typename T, bool ACROSS, int B> __device__ __forceinline__ Vec<T, Kind
         Vec<T, 4> r;
         const int col = at + (lane & 31);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = *reinterpret_cast<const float *>(lds + across_at<T, B>(kk * 8 + (lane >> 5) * 4 + i, col >> 2) + (col & 3) * 4);
+        for (int i = 0; i < 4; ++i) r[i] = *reinterpret_cast<const float *>(lds + piece_at<T, true, B>(kk * 8 + (lane >> 5) * 4 + i, col >> 2) + (col & 3) * 4);
         return r;
     }
 }
@@ -111,56 +157,177 @@ template <typename T> __device__ __forceinline__ f32x16 multiply(const Vec<T, Ki
     }
 }
 
-// C's entry (m, n), v = sum
-template <typename T, typename OUT> __device__ __forceinline__ void finish(const Product &p, int64_t m, int64_t n, float v)
+// 8 neighbouring entries of a row, as 16-byte words where they may be
+template <typename T> __device__ __forceinline__ void get8(float (&v)[8], const T *p, bool words, int count)
 {
-    if (p.bias) v += p.bias[n];
-    if (p.pre) ((T *)p.pre)[m * p.ldp + n] = from_f32<T>(v);
-    v = act_of(p.act, v);
-    if (p.res) v += to_f32(((const T *)p.res)[m * p.ldr + n]);
-    ((OUT *)p.y)[m * p.ldy + n] = from_f32<OUT>(v);
+    if (words && count >= 8) {
+        const Vec<T, 8> r = *reinterpret_cast<const Vec<T, 8> *>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_f32(r[i]);
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < count ? to_f32(p[i]) : 0.0f;
+}
+template <typename T> __device__ __forceinline__ void put8(T *p, const float (&v)[8], bool words, int count)
+{
+    if (words && count >= 8) {
+        Vec<T, 8> r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = from_f32<T>(v[i]);
+        *reinterpret_cast<Vec<T, 8> *>(p) = r;
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < count) p[i] = from_f32<T>(v[i]);
+}
+template <int ACT> __device__ __forceinline__ void activate(float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = act_f<ACT>(v[i]);
+}
+// C's entries (m, n ..), v their sums
+template <typename T, typename OUT> __device__ __forceinline__ void finish(const Product &p, int m, int n, float (&v)[8], const float (&bias)[8])
+{
+    const int count = p.N - n;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += bias[i];
+    if (p.pre) put8((T *)p.pre + m * p.ldp + n, v, p.words & WORDS_PRE, count);
+    if (p.act == HTS_ACT_RELU) activate<HTS_ACT_RELU>(v);
+    else if (p.act == HTS_ACT_SILU) activate<HTS_ACT_SILU>(v);
+    else if (p.act == HTS_ACT_GELU) activate<HTS_ACT_GELU>(v);
+    if (p.res) {
+        float r[8];
+        get8(r, (const T *)p.res + m * p.ldr + n, p.words & WORDS_RES, count);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    put8((OUT *)p.y + m * p.ldy + n, v, p.words & WORDS_Y, count);
 }
 
-template <typename T, typename OUT, bool AX, bool BX, int BM, int BN>
-__global__ __launch_bounds__(256) void product_kernel(const Product p, const int tiles_n)
+// Workgroups go to the eight dies in turn; a die gets neighbouring tiles, of a slice of the reduction and of a band of C, so that its L2 holds their operands.
+__device__ __forceinline__ bool place(int tiles, int &tile)
 {
-    constexpr int THREADS = 256, BK = Kind<T>::BK, TM = BM / 64, TN = BN / 64;
-    __shared__ __attribute__((aligned(1024))) char tile[(BM + BN) * 128];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
-    const int m0 = (int)(blockIdx.x / tiles_n) * BM, n0 = (int)(blockIdx.x % tiles_n) * BN, z = blockIdx.y;
-    const int half = (p.K + BK - 1) / BK, total = p.a_low ? 2 * half : half, first = z * (p.klen / BK), last = min(total, first + p.klen / BK);
-    f32x16 acc[TM][TN];
+    const int share = (tiles + 7) / 8;
+    tile = (int)(blockIdx.x % 8) * share + (int)(blockIdx.x / 8);
+    return blockIdx.x / 8 < share && tile < tiles;
+}
+
+// A workgroup: WM x WN x KS wavefronts.  A wavefront has BM / WM x BN / WN of the tile and every KS-th part of a k-tile.  DMA: copies straight into
+// LDS, NS stages, one barrier a k-tile; otherwise two stages through registers.
+template <int BM_, int BN_, int WM_, int WN_, int KS_, int NS_> struct Tiling { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KS = KS_, NS = NS_, WAVES = WM_ * WN_ * KS_; };
+
+template <typename T, typename OUT, bool AX, bool BX, class C, bool DMA>
+__global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product p, const int tiles_n, const int tiles)
+{
+    constexpr int WAVES = C::WAVES, THREADS = WAVES * 64, BM = C::BM, BN = C::BN, BK = Kind<T>::BK, TM = BM / C::WM / 32, TN = BN / C::WN / 32, KS = C::KS, NS = DMA ? C::NS : 2;
+    constexpr int STAGE = (BM + BN) * 128, SUMS = KS * BM * BN * 4;
+    static_assert(TM * C::WM * 32 == BM && TN * C::WN * 32 == BN && 4 % KS == 0, "tiling");
+    __shared__ __attribute__((aligned(1024))) char tile[NS * STAGE > SUMS ? NS * STAGE : SUMS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave % C::WM, wn = wave / C::WM % C::WN, ks = wave / (C::WM * C::WN);
+    int which;
+    if (!place(tiles, which)) return;                  // the whole workgroup leaves
+    const int per_slice = p.slices > 1 ? tiles / p.slices : tiles, z = which / per_slice, in_slice = which % per_slice;
+    const int m0 = in_slice / tiles_n * BM, n0 = in_slice % tiles_n * BN;
+    const int each = (p.K + BK - 1) / BK, total = p.parts * each, first = z * (p.klen / BK), nt = min(total, first + p.klen / BK) - first;
+    // db: A times a matrix of ones, which needs no operand from LDS, by the wavefronts of C's first column tile
+    constexpr bool ROW_SUMS = AX && BX;
+    const bool row_sums = ROW_SUMS && p.rows && n0 == 0 && wn == 0;
+    f32x16 acc[TM][TN], sum[ROW_SUMS ? TM : 1];
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int e = 0; e < 16; ++e) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    Staged<T, AX, BM, THREADS> as;
-    Staged<T, BX, BN, THREADS> bs;
-    auto fetch = [&](int t) {
-        const int k0 = (t >= half ? t - half : t) * BK;
-        as.load((const T *)(t >= half ? p.a_low : p.a), p.lda, m0, p.M, k0, p.K, tid);
-        bs.load((const T *)p.b, p.ldb, n0, p.N, k0, p.K, tid);
-    };
-    if (first < last) fetch(first);
-    for (int t = first; t < last; ++t) {
-        __syncthreads();
-        as.put(tile, tid);
-        bs.put(tile + BM * 128, tid);
-        __syncthreads();
-        if (t + 1 < last) fetch(t + 1);
+            for (int j = 0; j < TN; ++j) acc[i][j][e] = 0.0f;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            Vec<T, Kind<T>::V> a[TM], b[TN];
+        for (int i = 0; i < (ROW_SUMS ? TM : 1); ++i) sum[i][e] = 0.0f;
+    }
+    // all of a k-tile's reads are issued before its products
+    auto compute = [&](const char *stage) {
+        Vec<T, Kind<T>::V> a[4 / KS][TM], b[4 / KS][TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = operand<T, AX, BM>(tile, (wm * TM + i) * 32, kk, lane);
+        for (int k = 0; k < 4 / KS; ++k) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = operand<T, BX, BN>(tile + BM * 128, (wn * TN + j) * 32, kk, lane);
+            for (int i = 0; i < TM; ++i) a[k][i] = operand<T, AX, BM>(stage, (wm * TM + i) * 32, k * KS + ks, lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) b[k][j] = operand<T, BX, BN>(stage + BM * 128, (wn * TN + j) * 32, k * KS + ks, lane);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 4 / KS; ++k)
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(a[i], b[j], acc[i][j]);
+                for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(a[k][i], b[k][j], acc[i][j]);
+        if constexpr (ROW_SUMS) if (row_sums) {
+            Vec<T, Kind<T>::V> ones;
+#pragma unroll
+            for (int e = 0; e < Kind<T>::V; ++e) ones[e] = from_f32<T>(1.0f);
+#pragma unroll
+            for (int k = 0; k < 4 / KS; ++k)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) sum[i] = multiply<T>(a[k][i], ones, sum[i]);
+        }
+    };
+    if constexpr (DMA) {
+        Copied<T, AX, BM, WAVES> as;
+        Copied<T, BX, BN, WAVES> bs;
+        as.open((const T *)p.a, p.lda, m0, p.M, p.K, wave, lane);
+        bs.open((const T *)p.b, p.ldb, n0, p.N, p.K, wave, lane);
+        auto fetch = [&](int t, int s) {
+            const int part = p.parts > 1 ? (first + t) / each : 0, k0 = (first + t - part * each) * BK;
+            as.copy(k0, tile + s * STAGE, wave, part * p.part_stride);
+            bs.copy(k0, tile + s * STAGE + BM * 128, wave, 0);
+        };
+#pragma unroll
+        for (int s = 0; s < NS - 1; ++s) if (s < nt) fetch(s, s);
+        auto step = [&](int t, auto u) {
+            constexpr int S = decltype(u)::value;
+            // this wavefront's copies of k-tile t have landed (later ones' may be on their way) and its reads of k-tile t - 1 are done
+            wait_tiles<NS - 2, Copied<T, AX, BM, WAVES>::COPIES + Copied<T, BX, BN, WAVES>::COPIES>(nt - 1 - t);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();              // everybody's
+            asm volatile("" ::: "memory");
+            if (t + NS - 1 < nt) fetch(t + NS - 1, (S + NS - 1) % NS);
+            compute(tile + S * STAGE);
+        };
+        for (int t = 0; t < nt; t += NS) dma_steps(step, t, nt, std::make_integer_sequence<int, NS>{});
+    } else {
+        Staged<T, AX, BM, THREADS> as;
+        Staged<T, BX, BN, THREADS> bs;
+        auto fetch = [&](int t) {
+            const int part = p.parts > 1 ? (first + t) / each : 0, k0 = (first + t - part * each) * BK;
+            as.load((const T *)p.a + part * p.part_stride, p.lda, m0, p.M, k0, p.K, tid);
+            bs.load((const T *)p.b, p.ldb, n0, p.N, k0, p.K, tid);
+        };
+        auto put = [&](int s) { as.put(tile + s * STAGE, tid); bs.put(tile + s * STAGE + BM * 128, tid); };
+        if (nt > 0) { fetch(0); put(0); }
+        __syncthreads();
+        for (int t = 0; t < nt; ++t) {
+            if (t + 1 < nt) fetch(t + 1);
+            compute(tile + (t & 1) * STAGE);
+            if (t + 1 < nt) put((t + 1) & 1);
+            __syncthreads();
+        }
+    }
+    // the sums to LDS, 16 bytes at a time, slots exchanged by row; then a thread finishes 8 neighbouring entries
+    float *sums = reinterpret_cast<float *>(tile);
+    auto at = [](int k, int r, int slot) { return ((k * BM + r) * (BN / 4) + (slot ^ (r & 7))) * 4; };
+    __syncthreads();
+    if constexpr (ROW_SUMS) {
+        if (p.rows && n0 == 0) {
+            if (wn == 0 && lane < 32)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) sums[ks * BM + (wm * TM + i) * 32 + lane] = sum[i][0];
+            __syncthreads();
+            for (int r = tid; r < BM && m0 + r < p.M; r += THREADS) {
+                float v = 0.0f;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) v += sums[s * BM + r];
+                (p.slices > 1 ? p.part + z * p.stride + (int64_t)p.M * p.N : p.rows)[m0 + r] = v;
+            }
+            if (!p.y) return;
+            __syncthreads();
         }
     }
 #pragma unroll
@@ -168,112 +335,186 @@ __global__ __launch_bounds__(256) void product_kernel(const Product p, const int
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int m = m0 + (wm * TM + i) * 32 + (lane & 31), n = n0 + (wn * TN + j) * 32 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-                if (m < p.M && n < p.N) {
-                    if (p.part) p.part[((int64_t)z * p.M + m) * p.N + n] = acc[i][j][e];
-                    else finish<T, OUT>(p, m, n, acc[i][j][e]);
-                }
+            for (int q = 0; q < 4; ++q) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+                *reinterpret_cast<f32x4 *>(sums + at(ks, (wm * TM + i) * 32 + (lane & 31), (wn * TN + j) * 8 + 2 * q + (lane >> 5))) = v;
             }
-}
-
-// g = dy act'(pre) in two parts (binary32: one), and sums of g over a share of the rows for db.  A lane has a column.
-constexpr int COLUMN_ROWS = 64;
-template <typename T>
-__global__ __launch_bounds__(256) void slope_kernel(const LinearOp p, const int groups, T *high, T *low, float *part)
-{
-    __shared__ float sums[4][64];
-    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6, blocks = (p.N + 63) / 64;
-    const int n = (int)(blockIdx.x % blocks) * 64 + lane, group = blockIdx.x / blocks;
-    float s = 0.0f;
-    if (n < p.N)
-        for (int64_t m = group * 4 + row; m < p.M; m += groups * 4) {
-            float g = to_f32(((const T *)p.dy.p)[m * p.dy.ld + n]);
-            if (p.act != HTS_ACT_NONE) {
-                g *= slope_of(p.act, to_f32(((const T *)p.pre.p)[m * p.pre.ld + n]));
-                const T h = from_f32<T>(g);
-                high[m * p.N + n] = h;
-                if (low) low[m * p.N + n] = from_f32<T>(g - to_f32(h));
-            }
-            s += g;
-        }
-    sums[row][lane] = s;
     __syncthreads();
-    if (row == 0 && n < p.N && part) part[(int64_t)group * p.N + n] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    // a thread's entries are in the same columns of its rows
+    constexpr int ROW = BN / 8, ROWS = THREADS / ROW;
+    const int c = tid % ROW, n = n0 + 8 * c;
+    if (n >= p.N) return;
+    float bias[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.0f;
+#pragma unroll 2
+    for (int r = tid / ROW; r < BM; r += ROWS) {
+        const int m = m0 + r;
+        if (m >= p.M) break;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 w = *reinterpret_cast<const f32x4 *>(sums + at(s, r, 2 * c + h));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * h + e] += w[e];
+            }
+        if (p.slices > 1) put8(p.part + z * p.stride + (int64_t)m * p.N + n, v, (p.N & 3) == 0, p.N - n);
+        else finish<T, OUT>(p, m, n, v, bias);
+    }
 }
 
-int column_groups(int64_t M) { const int64_t g = ceil_div(M, COLUMN_ROWS); return (int)(g < 128 ? g : 128); }
+// g = dy act'(pre), in bfloat16 as the sum of three numbers, 24 bits together: V neighbouring entries a thread
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(256) void slope_kernel(const LinearOp p, T *out, const int64_t part)
+{
+    const int across = p.N / V;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / across;
+    if (m >= p.M) return;
+    const int n = (int)(i - m * across) * V;
+    const Loaded<T, V> dy = load_v<T, V>((const T *)p.dy.p + m * p.dy.ld + n), pre = load_v<T, V>((const T *)p.pre.p + m * p.pre.ld + n);
+    constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
+    float g[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) g[e] = to_f32(dy.e[e]) * act_slope<ACT>(to_f32(pre.e[e]));
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+        Loaded<T, V> h;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            h.e[e] = from_f32<T>(g[e]);
+            // (what is left of a number that is not finite would be NaN)
+            g[e] = __builtin_isfinite(g[e]) ? g[e] - to_f32(h.e[e]) : 0.0f;
+        }
+        store_v<T, V>(out + k * part + m * p.N + n, h);
+    }
+}
+
+// dw and db from the slices' sums: 4 neighbouring entries a thread, the slices in order
+__global__ __launch_bounds__(256) void slices_kernel(const float *part, const int slices, const int64_t stride, float *dw, const int64_t n, float *db, const int rows)
+{
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= stride) return;
+    f32x4 s = *reinterpret_cast<const f32x4 *>(part + i);
+#pragma unroll 8
+    for (int k = 1; k < slices; ++k) s += *reinterpret_cast<const f32x4 *>(part + k * stride + i);
+    if (dw && i + 4 <= n && ((uintptr_t)dw & 15) == 0) *reinterpret_cast<f32x4 *>(dw + i) = s;
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (i + e < n) { if (dw) dw[i + e] = s[e]; }
+            else if (db && i + e - n < rows) db[i + e - n] = s[e];
+        }
+}
+
 // dw's reduction over the rows is cut where C has too few tiles for the compute units
 int slices_of(int64_t rows, int64_t N, int64_t K, int bk)
 {
-    const int64_t tiles = ceil_div(N, 128) * ceil_div(K, 128), most = ceil_div(rows, 4 * bk);
+    const int64_t tiles = ceil_div(N, 128) * ceil_div(K, 128), most = ceil_div(rows, 16 * bk);
     int64_t z = 512 / tiles;
     if (z > 16) z = 16;
     if (z > most) z = most;
     return (int)(z < 1 ? 1 : z);
 }
 
-template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq_ctx &c, Product p, int slices)
+template <typename T> bool words(const void *p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * (int64_t)sizeof(T) % 16 == 0; }
+// whether an operand's rows (`cols` entries) can be copied straight into LDS: whole 16-byte words, and a tile's rows within 32 bits
+template <typename T> bool copies(const void *p, int64_t ld, int64_t cols) { return words<T>(p, ld) && cols % Kind<T>::V == 0 && ld < (1ll << 31) / (128 * (int64_t)sizeof(T)); }
+
+template <typename T, typename OUT, bool AX, bool BX, class C> hipError_t product_on(hts_seq_ctx &c, Product p)
 {
-    constexpr int BK = Kind<T>::BK;
-    const int64_t total = ceil_div(p.K, BK) * (p.a_low ? 2 : 1);
-    p.klen = (int)(ceil_div(total, slices) * BK);
-    slices = (int)ceil_div(total * BK, p.klen);
-    const int tn = (int)ceil_div(p.N, 128);
-    hipLaunchKernelGGL((product_kernel<T, OUT, AX, BX, 128, 128>), dim3((uint32_t)(ceil_div(p.M, 128) * tn), slices), dim3(256), 0, c.stream, p, tn);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && p.part) e = launch_sum_partials(c, p.part, slices, (int64_t)p.M * p.N, SumTarget{(float *)p.y, (int64_t)p.M * p.N}, SumTarget{nullptr, 0}, SumTarget{nullptr, 0});
-    return e;
+    const int64_t tn = ceil_div(p.N, C::BN), tiles = ceil_div(p.M, C::BM) * tn * p.slices;
+    const bool dma = copies<T>(p.a, p.lda, AX ? p.M : p.K) && copies<T>(p.b, p.ldb, BX ? p.N : p.K) && p.part_stride % Kind<T>::V == 0;
+    const dim3 grid((uint32_t)(ceil_div(tiles, 8) * 8)), block(C::WAVES * 64);
+    if (dma) hipLaunchKernelGGL((product_kernel<T, OUT, AX, BX, C, true>), grid, block, 0, c.stream, p, (int)tn, (int)tiles);
+    else hipLaunchKernelGGL((product_kernel<T, OUT, AX, BX, C, false>), grid, block, 0, c.stream, p, (int)tn, (int)tiles);
+    return hipGetLastError();
 }
 
-struct Layout { int64_t high, low, columns, dw, total; };       // bytes
+// columns: C's, by which the tiles are chosen
+template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq_ctx &c, Product p, int slices, int columns)
+{
+    constexpr int BK = Kind<T>::BK;
+    const int64_t total = ceil_div(p.K, BK) * p.parts;
+    p.klen = (int)(ceil_div(total, slices) * BK);
+    p.slices = (int)ceil_div(total * BK, p.klen);
+    p.words = (words<OUT>(p.y, p.ldy) ? WORDS_Y : 0) | (words<T>(p.pre, p.ldp) ? WORDS_PRE : 0) | (words<T>(p.res, p.ldr) ? WORDS_RES : 0);
+    p.stride = round_up((int64_t)p.M * p.N + p.M, 4);
+    auto tiles = [&](int m, int n) { return ceil_div(p.M, m) * ceil_div(columns, n) * p.slices; };
+    hipError_t e;
+    if (tiles(128, 128) >= 400) e = product_on<T, OUT, AX, BX, Tiling<128, 128, 2, 2, 1, 2>>(c, p);
+    else if (tiles(64, 64) >= 192) e = product_on<T, OUT, AX, BX, Tiling<64, 64, 2, 2, 1, sizeof(T) == 2 ? 2 : 3>>(c, p);
+    else if (tiles(64, 32) >= 192) e = product_on<T, OUT, AX, BX, Tiling<64, 32, 2, 1, 2, 3>>(c, p);
+    else e = product_on<T, OUT, AX, BX, Tiling<32, 32, 1, 1, 4, 4>>(c, p);
+    if (e != hipSuccess || p.slices == 1) return e;
+    hipLaunchKernelGGL(slices_kernel, dim3((uint32_t)ceil_div(p.stride, 1024)), dim3(256), 0, c.stream, p.part, p.slices, p.stride, (float *)p.y, (int64_t)p.M * p.N, p.rows, p.M);
+    return hipGetLastError();
+}
+
+struct Layout { int64_t slope, stride, part, total; };       // bytes; stride: entries from part to part of an activation's gradient
 Layout layout(int size, int act, int64_t M, int64_t N, int64_t K)
 {
     Layout l;
-    l.high = 0;
-    l.low = l.high + (act == HTS_ACT_NONE ? 0 : round_up(M * N * size, 256));
-    l.columns = l.low + (act == HTS_ACT_NONE || size == 4 ? 0 : round_up(M * N * size, 256));
-    l.dw = l.columns + round_up(4 * column_groups(M) * N, 256);
+    const bool some = act != HTS_ACT_NONE;
+    l.slope = 0;
+    l.stride = some ? round_up(M * N, 128) : 0;
+    l.part = l.stride * size * (size == 2 ? 3 : 1);
     const int z = slices_of(M, N, K, 128 / size);
-    l.total = l.dw + (z > 1 ? 4 * z * N * K : 0);
+    l.total = l.part + (z > 1 ? 4 * z * round_up(N * K + N, 4) : 0);
     return l;
 }
 
 template <typename T> hipError_t forward(hts_seq_ctx &c, const LinearOp &op)
 {
     Product p = {};
+    p.parts = 1;
     p.a = op.x.p; p.lda = op.x.ld; p.b = op.w.p; p.ldb = op.w.ld; p.M = op.M; p.N = op.N; p.K = op.K;
     p.act = op.act; p.bias = op.bias; p.res = op.residual.p; p.ldr = op.residual.ld; p.y = op.y.p; p.ldy = op.y.ld; p.pre = op.pre.p; p.ldp = op.pre.ld;
-    return product<T, T, false, false>(c, p, 1);
+    return product<T, T, false, false>(c, p, 1, p.N);
+}
+
+template <typename T, int V> hipError_t slopes(hts_seq_ctx &c, const LinearOp &op, T *out, int64_t part)
+{
+    const dim3 grid((uint32_t)ceil_div((int64_t)op.M * (op.N / V), 256)), block(256);
+    if (op.act == HTS_ACT_RELU) hipLaunchKernelGGL((slope_kernel<T, V, HTS_ACT_RELU>), grid, block, 0, c.stream, op, out, part);
+    else if (op.act == HTS_ACT_SILU) hipLaunchKernelGGL((slope_kernel<T, V, HTS_ACT_SILU>), grid, block, 0, c.stream, op, out, part);
+    else hipLaunchKernelGGL((slope_kernel<T, V, HTS_ACT_GELU>), grid, block, 0, c.stream, op, out, part);
+    return hipGetLastError();
 }
 
 template <typename T> hipError_t backward(hts_seq_ctx &c, const LinearOp &op)
 {
     const Layout at = layout(sizeof(T), op.act, op.M, op.N, op.K);
     const bool act = op.act != HTS_ACT_NONE;
-    T *high = act ? (T *)(c.ws + at.high) : nullptr, *low = act && sizeof(T) == 2 ? (T *)(c.ws + at.low) : nullptr;
-    float *columns = (float *)(c.ws + at.columns);
+    T *slope = (T *)(c.ws + at.slope);
+    constexpr int V = Kind<T>::V;
     hipError_t e = hipSuccess;
-    if (act || op.db) {
-        const int groups = column_groups(op.M);
-        hipLaunchKernelGGL((slope_kernel<T>), dim3((uint32_t)(groups * ceil_div(op.N, 64))), dim3(256), 0, c.stream, op, groups, high, low, op.db ? columns : nullptr);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        if (op.db && (e = launch_sum_partials(c, columns, groups, op.N, SumTarget{op.db, op.N}, SumTarget{nullptr, 0}, SumTarget{nullptr, 0})) != hipSuccess) return e;
+    if (act) {
+        const bool wide = op.N % V == 0 && words<T>(op.dy.p, op.dy.ld) && words<T>(op.pre.p, op.pre.ld);
+        if ((e = wide ? slopes<T, V>(c, op, slope, at.stride) : slopes<T, 1>(c, op, slope, at.stride)) != hipSuccess) return e;
     }
     Product g = {};
-    g.a = act ? high : op.dy.p; g.lda = act ? op.N : op.dy.ld;
+    g.parts = 1;
+    g.a = act ? slope : op.dy.p; g.lda = act ? op.N : op.dy.ld;
     if (op.dx.p) {
         Product p = g;
         p.b = op.w.p; p.ldb = op.w.ld; p.M = op.M; p.N = op.K; p.K = op.N;
         p.res = op.add.p; p.ldr = op.add.ld; p.y = op.dx.p; p.ldy = op.dx.ld;
-        if ((e = product<T, T, false, true>(c, p, 1)) != hipSuccess) return e;
+        if ((e = product<T, T, false, true>(c, p, 1, p.N)) != hipSuccess) return e;
     }
-    if (op.dw) {
+    if (op.dw || op.db) {
         Product p = g;
         const int z = slices_of(op.M, op.N, op.K, Kind<T>::BK);
-        p.a_low = low; p.b = op.x.p; p.ldb = op.x.ld; p.M = op.N; p.N = op.K; p.K = op.M; p.y = op.dw; p.ldy = op.K;
-        p.part = z > 1 ? (float *)(c.ws + at.dw) : nullptr;
-        e = product<T, float, true, true>(c, p, z);
+        p.parts = act && sizeof(T) == 2 ? 3 : 1; p.part_stride = at.stride; p.b = op.x.p; p.ldb = op.x.ld; p.M = op.N; p.N = op.K; p.K = op.M; p.y = op.dw; p.ldy = op.K; p.rows = op.db;
+        // without dw: one column tile, of any operand with as many rows (x may not be there), whose products go nowhere; the same slices and tiles, hence the same bits
+        if (!op.dw) { p.b = g.a; p.ldb = g.lda; p.N = op.N % V == 0 ? V : 1; }
+        p.part = z > 1 ? (float *)(c.ws + at.part) : nullptr;
+        e = product<T, float, true, true>(c, p, z, op.K);
     }
     return e;
 }
