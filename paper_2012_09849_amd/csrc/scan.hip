@@ -52,46 +52,125 @@ struct Places { int per_group, waves; };          // channels of a group, wavefr
 
 template <typename T> __device__ __forceinline__ float wide_of(T v) { return to_f32(v); }
 __device__ __forceinline__ int length_of(const int32_t *lengths, int n, int T) { return lengths ? max(0, min(T, lengths[n])) : T; }
-// bit k: step t0 + k begins an episode
-template <int L> __device__ __forceinline__ uint32_t starts_of(const uint8_t *starts, int t0, int len, int n, int N, int lane)
+// Loads and stores through buffer descriptors: a base that all lanes share (the chunk's), 32 bits of a lane and 32 bits that all lanes share from it.
+// A lane that has nothing to load or store gets an offset beyond the descriptor's 2 GB: it reads zero and writes nothing, without a branch.
+// (the largest sum of both is below 2^32: the unit does not see a carry)
+constexpr uint32_t REACH = 1u << 31, NOWHERE = REACH;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t reach(const char *base) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, REACH, 0x00020000); }
+// (the bits in a register of its own: two 16-bit values packed into one would have to be waited for where they are loaded)
+template <typename T> __device__ __forceinline__ uint32_t take(__amdgpu_buffer_rsrc_t src, uint32_t lane, uint32_t all)
 {
-    if (!starts) return 0;
-    const int t = t0 + (lane & (L - 1));
-    const bool s = t < len && starts[(int64_t)t * N + n] != 0;
-    return (uint32_t)__ballot(s) & ((1u << L) - 1);
+    if constexpr (sizeof(T) == 2) return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(src, (int)lane, (int)all, 0);
+    else return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, (int)lane, (int)all, 0);
+}
+template <typename T> __device__ __forceinline__ float value_of(uint32_t bits) { return __uint_as_float(sizeof(T) == 2 ? bits << 16 : bits); }
+template <typename T> __device__ __forceinline__ void give(__amdgpu_buffer_rsrc_t dst, uint32_t lane, uint32_t all, float v)
+{
+    const T r = from_f32<T>(v);
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, r), dst, (int)lane, (int)all, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, r), dst, (int)lane, (int)all, 0);
 }
 
-// What a lane loads of a chunk: steps t0 + 4 j + p of its channel.  `full`: all of the chunk's steps exist.
-template <typename T, int NB> struct Strip {
-    T v[NB];
-    __device__ __forceinline__ void load(const T *q, int64_t st, int t, int len)
+// An array's chunk: the base goes from chunk to chunk, so that a chunk's addresses are a few scalar additions
+struct Walk {
+    const char *base;
+    int64_t chunk;                     // bytes to the next chunk
+    uint32_t step;                     // bytes from step to step, at most 2^26
+    __device__ __forceinline__ void open(const void *p, int64_t offset, int64_t step_, int t0, int L)
     {
+        base = (const char *)p + offset + t0 * step_;
+        chunk = L * step_; step = (uint32_t)step_;
+    }
+    __device__ __forceinline__ void forth() { base += chunk; }
+    __device__ __forceinline__ void back() { base -= chunk; }
+};
+// Where a wavefront's 16 channels of a sequence are; the lanes of step q are q steps further
+template <typename T> struct Track : Walk {
+    uint32_t lane;
+    __device__ __forceinline__ void open(const hts_steps &a, int n, int first, int channel, int q, int t0, int L)
+    {
+        Walk::open(a.p, (n * a.sn + first) * (int64_t)sizeof(T), a.st * (int64_t)sizeof(T), t0, L);
+        lane = a.p ? (uint32_t)q * step + (uint32_t)(channel - first) * (uint32_t)sizeof(T) : NOWHERE;
+    }
+    // the lane's channel in steps 4 j + q of the chunk at t0, and the next chunk's turn.  Without a branch, here and below: values that were loaded on
+    // different paths would be waited for where the paths meet
+    template <int NB> __device__ __forceinline__ void load(uint32_t (&v)[NB], int t0, int q, int len) const
+    {
+        const __amdgpu_buffer_rsrc_t src = reach(base);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            if (t + 4 * j < len) v[j] = q[(int64_t)(t + 4 * j) * st];
-            else v[j] = from_f32<T>(0.0f);
-        }
+        for (int j = 0; j < NB; ++j) v[j] = take<T>(src, t0 + 4 * j + q < len ? lane : NOWHERE, 4 * j * step);
+    }
+    template <int NB> __device__ __forceinline__ void store(const float (&v)[NB], int t0, int q, int T_, bool on) const
+    {
+        const __amdgpu_buffer_rsrc_t dst = reach(base);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) give<T>(dst, on && t0 + 4 * j + q < T_ ? lane : NOWHERE, 4 * j * step, v[j]);
     }
 };
-
-// B and C of a chunk: the value with number i = (step, B or C, state) of L * 2 SP
-template <typename T, int SL, int THREADS> struct PairLoad {
-    static constexpr int PAIR = Shape<SL>::PAIR, SP = Shape<SL>::SP, L = Shape<SL>::L, NL = (L * PAIR + THREADS - 1) / THREADS;
-    T v[NL];
-    __device__ __forceinline__ void load(const hts_scan_inputs &in, int64_t S, int g, int n, int t0, int len, int tid)
+// B or C of a chunk, THREADS lanes: value number i THREADS + tid is (step, state)
+template <typename T, int SL, int THREADS> struct Half : Walk {
+    static constexpr int SP = Shape<SL>::SP, L = Shape<SL>::L, NL = (L * SP + THREADS - 1) / THREADS, STEPS = THREADS / SP;
+    static_assert(THREADS % SP == 0, "lanes");
+    uint32_t lane;
+    int first;                         // the lane's step of a load
+    __device__ __forceinline__ void open(const hts_steps &a, int n, int g, int S, int tid, int t0)
     {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int k = i * THREADS + tid, t = t0 + k / PAIR, r = k % PAIR, s = r % SP;
-            const hts_steps &a = r < SP ? in.B : in.C;
-            v[i] = from_f32<T>(0.0f);
-            if (k < L * PAIR && t < len && s < S) v[i] = ((const T *)a.p)[t * a.st + n * a.sn + g * S + s];
-        }
+        const int k = tid % SP;
+        Walk::open(a.p, (n * a.sn + (int64_t)g * S) * (int64_t)sizeof(T), a.st * (int64_t)sizeof(T), t0, L);
+        first = tid / SP;
+        lane = k < S && first < L ? (uint32_t)first * step + k * (uint32_t)sizeof(T) : NOWHERE;
     }
-    __device__ __forceinline__ void put(float *lds, int tid) const
+    __device__ __forceinline__ void load(uint32_t (&v)[NL], int t0, int len) const
+    {
+        const __amdgpu_buffer_rsrc_t src = reach(base);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) v[i] = take<T>(src, t0 + i * STEPS + first < len ? lane : NOWHERE, i * STEPS * step);
+    }
+    __device__ __forceinline__ void put(const uint32_t (&v)[NL], float *lds, int tid) const
     {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) if (i * THREADS + tid < L * PAIR) lds[i * THREADS + tid] = to_f32(v[i]);
+        for (int i = 0; i < NL; ++i)
+            if (L * SP >= THREADS || first < L) lds[(i * STEPS + first) * (2 * SP) + tid % SP] = value_of<T>(v[i]);
+    }
+};
+// which of a chunk's steps begin an episode: a lane loads a step's flag, `mask` collects them (bit k: step t0 + k), as late as it is needed
+template <int L> struct Begins : Walk {
+    uint32_t lane;
+    __device__ __forceinline__ void open(const uint8_t *p, int n, int N, int tid, int t0)
+    {
+        Walk::open(p, n, N, t0, L);
+        lane = p ? (uint32_t)(tid & (L - 1)) * step : NOWHERE;
+    }
+    __device__ __forceinline__ void load(uint32_t &v, int t0, int len, int tid) const
+    {
+        v = (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(reach(base), t0 + (tid & (L - 1)) < len ? (int)lane : (int)NOWHERE, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t mask(uint32_t v) { return (uint32_t)__ballot(v != 0) & ((1u << L) - 1); }
+};
+// the states that a training pass keeps: SL floats of a lane, the same place in every chunk
+template <int SL> struct Kept : Walk {
+    uint32_t lane;
+    __device__ __forceinline__ void open(const float *p, int64_t N, int n, int D, int first, int channel, int q, int chunk)
+    {
+        Walk::open(p, ((int64_t)n * D + first) * Shape<SL>::SP * 4, N * D * Shape<SL>::SP * 4, chunk, 1);
+        lane = (uint32_t)((channel - first) * Shape<SL>::SP + q * SL) * 4u;
+    }
+    __device__ __forceinline__ float *at() const { return (float *)(const_cast<char *>(base) + lane); }
+    // zeros where there is no such chunk
+    __device__ __forceinline__ void load(float (&v)[SL], bool some) const
+    {
+        const __amdgpu_buffer_rsrc_t src = reach(base);
+        const int from = some ? (int)lane : (int)NOWHERE;
+        if constexpr (SL == 2) {
+            const auto r = __builtin_amdgcn_raw_buffer_load_b64(src, from, 0, 0);
+            v[0] = __uint_as_float(r[0]); v[1] = __uint_as_float(r[1]);
+        } else
+#pragma unroll
+            for (int i = 0; i < SL / 4; ++i) {
+                const auto r = __builtin_amdgcn_raw_buffer_load_b128(src, from, 16 * i, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * i + e] = __uint_as_float(r[e]);
+            }
     }
 };
 
@@ -101,97 +180,222 @@ template <int SL> __device__ __forceinline__ void read_states(float (&v)[SL], co
     for (int s = 0; s < SL; ++s) v[s] = p[s];
 }
 
+// B and C of the steps to come, read from LDS two steps ahead
+template <int SL, bool BOTH> struct Ahead {
+    static constexpr int DEPTH = 2, RING = DEPTH + 1, PAIR = Shape<SL>::PAIR, SP = Shape<SL>::SP;
+    const float *lds;
+    float b[RING][SL], c[RING][SL];
+    __device__ __forceinline__ explicit Ahead(const float *at) : lds(at) {}
+    __device__ __forceinline__ void read(int t)
+    {
+        read_states<SL>(b[t % RING], lds + t * PAIR);
+        if (BOTH) read_states<SL>(c[t % RING], lds + t * PAIR + SP);
+    }
+    // before step t of L, in the order of `way`
+    __device__ __forceinline__ void next(int t, int L, int way)
+    {
+        if (t == (way > 0 ? 0 : L - 1))
+#pragma unroll
+            for (int k = 0; k < DEPTH; ++k) read(t + way * k);
+        if (t + way * DEPTH >= 0 && t + way * DEPTH < L) read(t + way * DEPTH);
+    }
+    __device__ __forceinline__ const float *B(int t) const { return b[t % RING]; }
+    __device__ __forceinline__ const float *C(int t) const { return c[t % RING]; }
+};
+
+// A long sequence of few channels is cut into segments that are worked on at the same time: a first pass leaves each segment's last state, begun
+// from nothing (the first one from h_in), and its sum of step sizes; exp(sum A) is then what the state before the segment counts at its end.  The
+// second pass begins every segment from the states that these give, in order, so the result does not depend on who comes first.
+struct Segments {
+    int count, steps;                  // steps: whole chunks
+    float *state, *sum;                // [count - 1][N][D][SP], [count - 1][N][D]: a sum is NaN where an episode begins in the segment and nothing before it counts
+    float *h_in;                       // [N][D][SP]: h_in once more, since h_out may be h_in
+};
+template <int SL> __device__ __forceinline__ int64_t state_at(int64_t row, int d, int D, int q) { return (row * D + d) * Shape<SL>::SP + q * SL; }
+// the state before segment k; NaN: a real sum that is NaN gives NaN states in the segment's last one too
+template <int SL> __device__ __forceinline__ void state_before(float (&h)[SL], const Segments &seg, int k, int n, int N, int d, int D, int q, const float (&A)[SL])
+{
+    read_states<SL>(h, k == 0 ? seg.h_in + state_at<SL>(n, d, D, q) : seg.state + state_at<SL>(n, d, D, q));
+#pragma unroll 4
+    for (int i = 1; i < k; ++i) {
+        const float sum = seg.sum[((int64_t)i * N + n) * D + d];
+        float own[SL];
+        read_states<SL>(own, seg.state + state_at<SL>((int64_t)i * N + n, d, D, q));
+#pragma unroll
+        for (int s = 0; s < SL; ++s) h[s] = sum != sum ? own[s] : __builtin_fmaf(__builtin_amdgcn_exp2f(sum * A[s]), h[s], own[s]);
+    }
+}
+
 constexpr int FWD_WAVES = 4;
 
-template <typename T, int SL>
-__global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, const Places at)
+// STATES: the first pass over segments, which needs neither C nor the gate and writes no output
+template <typename T, int SL, bool STATES>
+__global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, const Places at, const Segments seg)
 {
     typedef Shape<SL> H;
     constexpr int L = H::L, NB = H::NB, SP = H::SP;
     __shared__ __attribute__((aligned(16))) float pairs[FWD_WAVES][L * H::PAIR];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int per = at.waves * p.d.G;                                   // wavefronts of a sequence
-    const int64_t task = (int64_t)blockIdx.x * FWD_WAVES + wave;
-    if (task >= (int64_t)per * p.d.N) return;
-    const int n = (int)(task / per), g = (int)(task % per) / at.waves, c = (int)(task % at.waves) * 16 + (lane >> 2), q = lane & 3;
-    const bool on = c < at.per_group;
-    const int d = g * at.per_group + min(c, at.per_group - 1), len = length_of(p.in.lengths, n, p.d.T), S = p.d.S;
-    const T *x = (const T *)p.in.x.p + n * p.in.x.sn + d, *dt = (const T *)p.in.dt.p + n * p.in.dt.sn + d, *z = (const T *)p.in.z.p + (p.in.z.p ? n * p.in.z.sn + d : 0);
-    T *y = (T *)p.y.p + n * p.y.sn + d;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = p.d.D, S = p.d.S, N = p.d.N;
+    const int per = at.waves * p.d.G;                                   // wavefronts of a sequence's segment
+    const uint32_t task = blockIdx.x * FWD_WAVES + wave, row = task / per, in_row = task % per;        // (their number has 31 bits)
+    if (row >= (uint32_t)(N * (seg.count - STATES))) return;
+    const int k = row / N, n = row % N, g = in_row / at.waves, c = in_row % at.waves * 16, q = lane & 3;
+    const bool on = c + (lane >> 2) < at.per_group;
+    const int d0 = g * at.per_group + c, d = g * at.per_group + min(c + (lane >> 2), at.per_group - 1), len = length_of(p.in.lengths, n, p.d.T);
+    const int first = k * seg.steps, end = min(p.d.T, first + seg.steps);
+    Track<T> xa, da, za, ya;
+    Kept<SL> kept;
+    xa.open(p.in.x, n, d0, d, q, first, L); da.open(p.in.dt, n, d0, d, q, first, L);
+    if (!STATES) { za.open(p.in.z, n, d0, d, q, first, L); ya.open(p.y, n, d0, d, q, first, L); kept.open(p.states_out, N, n, D, d0, d, q, first / L); }
     const float skip = p.in.skip ? p.in.skip[d] : 0.0f, bias = p.in.dt_bias ? p.in.dt_bias[d] : 0.0f;
-    float A[SL], h[SL];
+    float A[SL], h[SL], sum = 0.0f;
+    bool cut = false;
 #pragma unroll
     for (int s = 0; s < SL; ++s) {
-        const int k = q * SL + s;
-        A[s] = k < S ? p.in.A[(int64_t)d * S + k] * LOG2E : 0.0f;
-        h[s] = k < S && p.in.h_in ? p.in.h_in[((int64_t)n * p.d.D + d) * S + k] : 0.0f;
+        const int i = q * SL + s;
+        A[s] = i < S ? p.in.A[(int64_t)d * S + i] * LOG2E : 0.0f;
+        h[s] = i < S && p.in.h_in && (STATES ? k == 0 : seg.count == 1) ? p.in.h_in[((int64_t)n * D + d) * S + i] : 0.0f;
+        if (STATES && k == 0 && on) seg.h_in[state_at<SL>(n, d, D, q) + s] = h[s];
     }
-    Strip<T, NB> xs, ds, zs;
-    PairLoad<T, SL, 64> bc;
-    uint32_t begins;
+    if (!STATES && seg.count > 1) state_before<SL>(h, seg, k, n, N, d, D, q, A);
+    Half<T, SL, 64> bs, cs;
+    Begins<L> begins;
+    bs.open(p.in.B, n, g, S, lane, first);
+    if (!STATES) cs.open(p.in.C, n, g, S, lane, first);
+    begins.open(p.in.starts, n, N, lane, first);
+    struct Loads { uint32_t x[NB], dt[NB], z[NB], b[Half<T, SL, 64>::NL], c[Half<T, SL, 64>::NL], begins; } in;          // what is on its way for the next chunk
+    // (beyond the segment's end nothing is loaded.)  Fenced off: were the loads moved before the last use of what they replace, they would need registers
+    // of their own, and copies from these at the loop's end, which wait for them
     auto fetch = [&](int t0) {
-        xs.load(x, p.in.x.st, t0 + q, len);
-        ds.load(dt, p.in.dt.st, t0 + q, len);
-        if (p.in.z.p) zs.load(z, p.in.z.st, t0 + q, len);
-        bc.load(p.in, S, g, n, t0, len, lane);
-        begins = starts_of<L>(p.in.starts, t0, len, n, p.d.N, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        const int live = min(len, end);
+        begins.load(in.begins, t0, live, lane);
+        xa.load(in.x, t0, q, live);
+        da.load(in.dt, t0, q, live);
+        bs.load(in.b, t0, live);
+        xa.forth(); da.forth(); bs.forth(); begins.forth();
+        if (!STATES) {
+            za.load(in.z, t0, q, live);
+            cs.load(in.c, t0, live);
+            za.forth(); cs.forth();
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    fetch(0);
     float *lds = pairs[wave];
-    for (int t0 = 0, chunk = 0; t0 < p.d.T; t0 += L, ++chunk) {
+    fetch(first);
+    for (int t0 = first; t0 < end; t0 += L) {
         float xv[NB], size[NB], moved[NB], gate[NB];
         wave_order();
-        bc.put(lds, lane);
+        bs.put(in.b, lds, lane);
+        if (!STATES) cs.put(in.c, lds + SP, lane);
         wave_order();
-        const uint32_t fresh = begins;
+        const uint32_t fresh = Begins<L>::mask(in.begins);
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const int t = t0 + 4 * j + q;
-            xv[j] = to_f32(xs.v[j]);
-            float v = to_f32(ds.v[j]) + bias, slope;
-            size[j] = v;
-            if (p.d.softplus) softplus_f(v, size[j], slope);
-            if (t >= len) size[j] = 0.0f;
+            const bool live = t0 + 4 * j + q < len;
+            xv[j] = value_of<T>(in.x[j]);
+            const float v = value_of<T>(in.dt[j]) + bias;
+            float soft, slope;
+            softplus_f(v, soft, slope);
+            size[j] = live ? p.d.softplus ? soft : v : 0.0f;
             moved[j] = size[j] * xv[j];
-            gate[j] = t >= len ? 0.0f : p.in.z.p ? act_f<HTS_ACT_SILU>(to_f32(zs.v[j])) : 1.0f;
+            const float open = act_f<HTS_ACT_SILU>(value_of<T>(in.z[j]));
+            gate[j] = p.in.z.p ? open : 1.0f;
+            sum += size[j];
         }
-        if (t0 + L < p.d.T) fetch(t0 + L);
-        if (p.states_out && on) {
-            float *out = p.states_out + (((int64_t)chunk * p.d.N + n) * p.d.D + d) * SP + q * SL;
+        if (STATES) cut |= fresh != 0;
+        fetch(t0 + L);
+        if (!STATES && p.states_out && on) {
+            float *out = kept.at();
 #pragma unroll
             for (int s = 0; s < SL; ++s) out[s] = h[s];
         }
+        float ys[NB];
+        // twice: chunks in which no episode begins, most of them, reset nothing
+        auto pass = [&](auto has) {
+            Ahead<SL, !STATES> ahead(lds + q * SL);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            float sums[4];
+            for (int j = 0; j < NB; ++j) {
+                float sums[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = 4 * j + i;
-                const float de = quad_from(size[j], i), dx = quad_from(moved[j], i);
-                float B[SL], C[SL];
-                read_states<SL>(B, lds + k * H::PAIR + q * SL);
-                read_states<SL>(C, lds + k * H::PAIR + SP + q * SL);
-                if (fresh >> k & 1)
+                for (int i = 0; i < 4; ++i) {
+                    const int t = 4 * j + i;
+                    const float de = quad_from(size[j], i), dx = quad_from(moved[j], i);
+                    ahead.next(t, L, +1);
+                    if (decltype(has)::value && (fresh >> t & 1))
 #pragma unroll
-                    for (int s = 0; s < SL; ++s) h[s] = 0.0f;
-                float sum = 0.0f;
+                        for (int s = 0; s < SL; ++s) h[s] = 0.0f;
+                    float y = 0.0f;
 #pragma unroll
-                for (int s = 0; s < SL; ++s) {
-                    h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(de * A[s]), h[s], dx * B[s]);
-                    sum = __builtin_fmaf(h[s], C[s], sum);
+                    for (int s = 0; s < SL; ++s) {
+                        h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(de * A[s]), h[s], dx * ahead.B(t)[s]);
+                        if (!STATES) y = __builtin_fmaf(h[s], ahead.C(t)[s], y);
+                    }
+                    sums[i] = y;
                 }
-                sums[i] = sum;
+                if (STATES) continue;
+                const float y = __builtin_fmaf(skip, xv[j], quad_deal(sums, q)) * gate[j];      // (by all lanes of the quad, those of no step too)
+                ys[j] = t0 + 4 * j + q < len ? y : 0.0f;
             }
-            const float sum = quad_deal(sums, q);
-            const int t = t0 + 4 * j + q;
-            // (a gate of 0 and a sum that is not finite beyond the sequence's end, or for a gate of -infinity, give 0)
-            if (on && t < p.d.T) y[(int64_t)t * p.y.st] = from_f32<T>(t < len ? __builtin_fmaf(skip, xv[j], sum) * gate[j] : 0.0f);
-        }
+        };
+        if (fresh) pass(std::true_type()); else pass(std::false_type());
+        if (!STATES) { ya.store(ys, t0, q, p.d.T, on); ya.forth(); kept.forth(); }
     }
-    if (p.h_out && on)
+    if (!on) return;
+    if (STATES) {
+        float *out = seg.state + state_at<SL>((int64_t)k * N + n, d, D, q);
+#pragma unroll
+        for (int s = 0; s < SL; ++s) out[s] = h[s];
+        sum = quad_sum(sum);
+        if (q == 0) seg.sum[((int64_t)k * N + n) * D + d] = cut ? __builtin_nanf("") : sum;
+    } else if (p.h_out && k == seg.count - 1)
 #pragma unroll
         for (int s = 0; s < SL; ++s)
-            if (q * SL + s < S) p.h_out[((int64_t)n * p.d.D + d) * S + q * SL + s] = h[s];
+            if (q * SL + s < S) p.h_out[((int64_t)n * D + d) * S + q * SL + s] = h[s];
+}
+
+// A single step (an actor's, a server's): nothing to share between steps, so B and C come straight to the lanes that hold their states.
+template <typename T, int SL>
+__global__ __launch_bounds__(256) void step_kernel(const ScanOp p)
+{
+    constexpr int SP = Shape<SL>::SP;
+    const int D = p.d.D, S = p.d.S, q = threadIdx.x & 3;
+    const int64_t row = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 2);
+    if (row >= (int64_t)p.d.N * D) return;                              // a quad leaves together
+    const int n = (int)(row / D), d = (int)(row % D), g = d / (D / p.d.G);
+    const bool live = !p.in.lengths || p.in.lengths[n] > 0, fresh = live && p.in.starts && p.in.starts[n];
+    float A[SL], B[SL], C[SL], h[SL];
+#pragma unroll
+    for (int s = 0; s < SL; ++s) {
+        const int i = q * SL + s;
+        A[s] = B[s] = C[s] = h[s] = 0.0f;
+        if (i < S) {
+            A[s] = p.in.A[(int64_t)d * S + i] * LOG2E;
+            if (p.in.h_in) h[s] = p.in.h_in[row * S + i];
+            if (live) { B[s] = to_f32(((const T *)p.in.B.p)[n * p.in.B.sn + (int64_t)g * S + i]); C[s] = to_f32(((const T *)p.in.C.p)[n * p.in.C.sn + (int64_t)g * S + i]); }
+        }
+    }
+    if (p.states_out)
+#pragma unroll
+        for (int s = 0; s < SL; ++s) p.states_out[row * SP + q * SL + s] = h[s];
+    float y = 0.0f;
+    if (live) {
+        const float x = to_f32(((const T *)p.in.x.p)[n * p.in.x.sn + d]), v = to_f32(((const T *)p.in.dt.p)[n * p.in.dt.sn + d]) + (p.in.dt_bias ? p.in.dt_bias[d] : 0.0f);
+        const float z = p.in.z.p ? to_f32(((const T *)p.in.z.p)[n * p.in.z.sn + d]) : 0.0f;
+        float size = v, slope;
+        if (p.d.softplus) softplus_f(v, size, slope);
+        const float dx = size * x;
+#pragma unroll
+        for (int s = 0; s < SL; ++s) {
+            h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(size * A[s]), fresh ? 0.0f : h[s], dx * B[s]);
+            y = __builtin_fmaf(h[s], C[s], y);
+        }
+        y = __builtin_fmaf(p.in.skip ? p.in.skip[d] : 0.0f, x, quad_sum(y)) * (p.in.z.p ? act_f<HTS_ACT_SILU>(z) : 1.0f);
+    }
+    if (p.h_out)
+#pragma unroll
+        for (int s = 0; s < SL; ++s) if (q * SL + s < S) p.h_out[row * S + q * SL + s] = h[s];
+    if (q == 0) ((T *)p.y.p)[n * p.y.sn + d] = from_f32<T>(y);
 }
 
 // Sums over the 16 channels of a wavefront (lane bits 2 .. 5) of NV = 4 K values: after two exchanges of halves a lane has the sums over bits 4
@@ -232,8 +436,13 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
     const int c = (block * BWD_WAVES + wave) * 16 + (lane >> 2);
     const bool on = c < at.per_group;
     const int D = p.d.D, S = p.d.S, TT = p.d.T, d = g * at.per_group + min(c, at.per_group - 1), len = length_of(p.in.lengths, n, TT);
-    const T *x = (const T *)p.in.x.p + n * p.in.x.sn + d, *dt = (const T *)p.in.dt.p + n * p.in.dt.sn + d, *dy = (const T *)p.dy.p + n * p.dy.sn + d;
-    const T *z = (const T *)p.in.z.p + (p.in.z.p ? n * p.in.z.sn + d : 0);
+    Track<T> xa, da, za, ga, dxa, dda, dza;
+    const int d0 = g * at.per_group + min((block * BWD_WAVES + wave) * 16, at.per_group - 1);
+    const int chunks = (TT + L - 1) / L, last = (chunks - 1) * L;
+    xa.open(p.in.x, n, d0, d, q, last, L); da.open(p.in.dt, n, d0, d, q, last, L); za.open(p.in.z, n, d0, d, q, last, L); ga.open(p.dy, n, d0, d, q, last, L);
+    dxa.open(p.g.dx, n, d0, d, q, last, L); dda.open(p.g.ddt, n, d0, d, q, last, L); dza.open(p.g.dz, n, d0, d, q, last, L);
+    Kept<SL> kept;
+    kept.open(p.states, p.d.N, n, D, d0, d, q, chunks - 1);
     const float skip = p.in.skip ? p.in.skip[d] : 0.0f, bias = p.in.dt_bias ? p.in.dt_bias[d] : 0.0f;
     float A[SL], ag[SL], dA[SL], dskip = 0.0f, dbias = 0.0f;
 #pragma unroll
@@ -243,19 +452,28 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
         ag[s] = on && k < S && p.dh_out ? p.dh_out[((int64_t)n * D + d) * S + k] : 0.0f;
         dA[s] = 0.0f;
     }
-    Strip<T, NB> xs, ds, zs, gs;
-    PairLoad<T, SL, THREADS> bc;
+    uint32_t xs[NB], ds[NB], zs[NB], gs[NB];
+    Half<T, SL, THREADS> bs, cs;
+    bs.open(p.in.B, n, g, S, tid, last);
+    cs.open(p.in.C, n, g, S, tid, last);
     float h0[SL];
-    uint32_t begins;
-    auto fetch = [&](int chunk) {
-        const int t0 = chunk * L;
-        xs.load(x, p.in.x.st, t0 + q, len);
-        ds.load(dt, p.in.dt.st, t0 + q, len);
-        gs.load(dy, p.dy.st, t0 + q, len);
-        if (p.in.z.p) zs.load(z, p.in.z.st, t0 + q, len);
-        bc.load(p.in, S, g, n, t0, len, tid);
-        read_states<SL>(h0, p.states + (((int64_t)chunk * p.d.N + n) * D + d) * SP + q * SL);
-        begins = starts_of<L>(p.in.starts, t0, len, n, p.d.N, lane);
+    uint32_t bv[Half<T, SL, THREADS>::NL], cv[Half<T, SL, THREADS>::NL];
+    Begins<L> begins;
+    begins.open(p.in.starts, n, p.d.N, lane, last);
+    uint32_t flag;
+    auto fetch = [&](int chunk) {          // (there is nothing to load before the first chunk)
+        __builtin_amdgcn_sched_barrier(0);
+        const int t0 = chunk * L, live = chunk >= 0 ? len : t0;
+        begins.load(flag, t0, live, lane);
+        xa.load(xs, t0, q, live);
+        da.load(ds, t0, q, live);
+        ga.load(gs, t0, q, live);
+        za.load(zs, t0, q, live);
+        bs.load(bv, t0, live);
+        cs.load(cv, t0, live);
+        kept.load(h0, chunk >= 0);
+        xa.back(); da.back(); za.back(); ga.back(); bs.back(); cs.back(); begins.back(); kept.back();
+        __builtin_amdgcn_sched_barrier(0);
     };
     auto leave = [&](int chunk, int buf) {        // the workgroup's sums of a chunk
         for (int i = tid; i < L * PAIR; i += THREADS) {
@@ -266,75 +484,79 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
             if (t < TT) pair_part[((((int64_t)block * TT + t) * p.d.N + n) * p.d.G + g) * PAIR + i % PAIR] = s;
         }
     };
-    const int chunks = (TT + L - 1) / L;
     fetch(chunks - 1);
     for (int chunk = chunks - 1, buf = 0; chunk >= 0; --chunk, buf ^= 1) {
         const int t0 = chunk * L;
-        bc.put(pairs[buf], tid);
+        bs.put(bv, pairs[buf], tid);
+        cs.put(cv, pairs[buf] + SP, tid);
         float xv[NB], size[NB], moved[NB], slope[NB], r[NB], zf[NB], hb[SL];
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const bool live = t0 + 4 * j + q < len;
-            xv[j] = on ? to_f32(xs.v[j]) : 0.0f;
-            const float v = to_f32(ds.v[j]) + bias;
-            size[j] = v; slope[j] = 1.0f;
-            if (p.d.softplus) softplus_f(v, size[j], slope[j]);
-            if (!live) size[j] = slope[j] = 0.0f;
+            xv[j] = on ? value_of<T>(xs[j]) : 0.0f;
+            const float v = value_of<T>(ds[j]) + bias;
+            float soft, rise;
+            softplus_f(v, soft, rise);
+            size[j] = live ? p.d.softplus ? soft : v : 0.0f;
+            slope[j] = live ? p.d.softplus ? rise : 1.0f : 0.0f;
             moved[j] = size[j] * xv[j];
-            const float dyv = on ? to_f32(gs.v[j]) : 0.0f, zv = p.in.z.p ? to_f32(zs.v[j]) : 0.0f;
-            r[j] = p.in.z.p ? dyv * act_f<HTS_ACT_SILU>(zv) : dyv;
+            const float dyv = on ? value_of<T>(gs[j]) : 0.0f, zv = value_of<T>(zs[j]);
+            const float open = act_f<HTS_ACT_SILU>(zv);
+            r[j] = dyv * (p.in.z.p ? open : 1.0f);
             zf[j] = dyv * act_slope<HTS_ACT_SILU>(zv);
         }
 #pragma unroll
         for (int s = 0; s < SL; ++s) hb[s] = h0[s];
-        const uint32_t fresh = begins;
+        const uint32_t fresh = Begins<L>::mask(flag);
         __syncthreads();
-        if (chunk > 0) fetch(chunk - 1);
+        fetch(chunk - 1);
         if (chunk < chunks - 1) leave(chunk + 1, buf ^ 1);
         const float *lds = pairs[buf];
         // twice: chunks in which no episode begins, most of them, select nothing
         auto pass = [&](auto has) {
             constexpr bool FRESH = decltype(has)::value;
             float a[L][SL], h[L][SL], raw[NB];
-    #pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                float part[4];
-    #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = 4 * j + i;
-                    const float de = quad_from(size[j], i), dx = quad_from(moved[j], i);
-                    float B[SL], C[SL], sum = 0.0f;
-                    read_states<SL>(B, lds + k * PAIR + q * SL);
-                    read_states<SL>(C, lds + k * PAIR + SP + q * SL);
-                    const bool begin = FRESH && (fresh >> k & 1);
-    #pragma unroll
-                    for (int s = 0; s < SL; ++s) {
-                        a[k][s] = __builtin_amdgcn_exp2f(de * A[s]);
-                        h[k][s] = __builtin_fmaf(dx, B[s], (begin ? 0.0f : a[k][s] * (k ? h[k ? k - 1 : 0][s] : hb[s])));
-                        sum = __builtin_fmaf(h[k][s], C[s], sum);
+            {
+                Ahead<SL, true> ahead(lds + q * SL);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    float part[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int k = 4 * j + i;
+                        const float de = quad_from(size[j], i), dx = quad_from(moved[j], i);
+                        ahead.next(k, L, +1);
+                        const bool begin = FRESH && (fresh >> k & 1);
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int s = 0; s < SL; ++s) {
+                            a[k][s] = __builtin_amdgcn_exp2f(de * A[s]);
+                            h[k][s] = __builtin_fmaf(dx, ahead.B(k)[s], begin ? 0.0f : a[k][s] * (k ? h[k ? k - 1 : 0][s] : hb[s]));
+                            sum = __builtin_fmaf(h[k][s], ahead.C(k)[s], sum);
+                        }
+                        part[i] = sum;
                     }
-                    part[i] = sum;
+                    raw[j] = quad_deal(part, q);
                 }
-                raw[j] = quad_deal(part, q);
             }
-    #pragma unroll
+            float outx[NB], outd[NB], outz[NB];
+            Ahead<SL, true> ahead(lds + q * SL);
+#pragma unroll
             for (int j = NB - 1; j >= 0; --j) {
                 float gB[4], dd[4], val[8 * SL];
-    #pragma unroll
+#pragma unroll
                 for (int i = 3; i >= 0; --i) {
                     const int k = 4 * j + i;
                     const float de = quad_from(size[j], i), dx = quad_from(moved[j], i), rk = quad_from(r[j], i);
-                    float B[SL], C[SL];
-                    read_states<SL>(B, lds + k * PAIR + q * SL);
-                    read_states<SL>(C, lds + k * PAIR + SP + q * SL);
+                    ahead.next(k, L, -1);
                     const bool begin = FRESH && (fresh >> k & 1);
                     gB[i] = dd[i] = 0.0f;
-    #pragma unroll
+#pragma unroll
                     for (int s = 0; s < SL; ++s) {
-                        const float gk = __builtin_fmaf(rk, C[s], ag[s]);
+                        const float gk = __builtin_fmaf(rk, ahead.C(k)[s], ag[s]);
                         val[2 * SL * i + s] = gk * dx;
                         val[2 * SL * i + SL + s] = rk * h[k][s];
-                        gB[i] = __builtin_fmaf(gk, B[s], gB[i]);
+                        gB[i] = __builtin_fmaf(gk, ahead.B(k)[s], gB[i]);
                         const float ga = gk * (begin ? 0.0f : a[k][s] * (k ? h[k ? k - 1 : 0][s] : hb[s]));
                         dd[i] = __builtin_fmaf(ga, A[s], dd[i]);
                         dA[s] = __builtin_fmaf(ga, de, dA[s]);
@@ -346,20 +568,21 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
                 // lanes of channel 0 of each row: step 4 j + 2 bit5 + bit4, states q SL ...
                 if ((lane & 12) == 0) {
                     float *to = sums[buf][wave] + (4 * j + 2 * (lane >> 5) + (lane >> 4 & 1)) * PAIR + q * SL;
-    #pragma unroll
+#pragma unroll
                     for (int s = 0; s < SL; ++s) { to[s] = out[s]; to[SP + s] = out[SL + s]; }
                 }
                 const float sB = quad_deal(gB, q), sd = quad_deal(dd, q) * (1.0f / LOG2E);
-                const int t = t0 + 4 * j + q;
-                const float ddt = __builtin_fmaf(sB, xv[j], sd) * slope[j], dx = __builtin_fmaf(sB, size[j], r[j] * skip);
+                const bool live = t0 + 4 * j + q < len;
+                const float ddt = __builtin_fmaf(sB, xv[j], sd) * slope[j];
                 dbias += ddt; dskip = __builtin_fmaf(r[j], xv[j], dskip);
-                if (on && t < TT) {
-                    const bool live = t < len;
-                    ((T *)p.g.dx.p)[t * p.g.dx.st + n * p.g.dx.sn + d] = from_f32<T>(live ? dx : 0.0f);
-                    ((T *)p.g.ddt.p)[t * p.g.ddt.st + n * p.g.ddt.sn + d] = from_f32<T>(live ? ddt : 0.0f);
-                    if (p.g.dz.p) ((T *)p.g.dz.p)[t * p.g.dz.st + n * p.g.dz.sn + d] = from_f32<T>(live ? zf[j] * __builtin_fmaf(skip, xv[j], raw[j]) : 0.0f);
-                }
+                outx[j] = live ? __builtin_fmaf(sB, size[j], r[j] * skip) : 0.0f;
+                outd[j] = live ? ddt : 0.0f;
+                outz[j] = live ? zf[j] * __builtin_fmaf(skip, xv[j], raw[j]) : 0.0f;
             }
+            dxa.store(outx, t0, q, TT, on);
+            dda.store(outd, t0, q, TT, on);
+            if (p.g.dz.p) dza.store(outz, t0, q, TT, on);
+            dxa.back(); dda.back(); dza.back();
         };
         if (fresh) pass(std::true_type()); else pass(std::false_type());
     }
@@ -397,12 +620,42 @@ int blocks_of(const hts_scan_desc &d) { return (int)ceil_div(places(d).waves, BW
 int64_t pair_floats(const hts_scan_desc &d) { return round_up((int64_t)blocks_of(d) * d.T * d.N * d.G * 2 * padded(d.S), 64); }
 int64_t param_floats(const hts_scan_desc &d) { return (int64_t)d.N * d.D * (d.S + 2); }
 
+// Segments of a sequence: where its wavefronts leave most units idle, as many as give two to a SIMD, of 64 steps at least.  The first pass costs
+// four fifths of the second.
+constexpr int MOST_SEGMENTS = 64;
+int segments_of(const hts_scan_desc &d, int cus)
+{
+    const int64_t waves = (int64_t)places(d).waves * d.G * d.N, units = 4ll * cus;
+    if (2 * waves > units) return 1;
+    int64_t count = 2 * units / waves;
+    if (count > d.T / 64) count = d.T / 64;
+    if (count > MOST_SEGMENTS) count = MOST_SEGMENTS;
+    if (count < 3) return 1;           // two passes over halves gain nothing
+    return (int)ceil_div(d.T, round_up(ceil_div(d.T, count), chunk_steps(d.S)));
+}
+int64_t segment_floats(const hts_scan_desc &d, int count) { return count > 1 ? (int64_t)d.N * d.D * (padded(d.S) * (int64_t)count + (count - 1)) : 0; }
+
 template <typename T, int SL> hipError_t run(hts_seq_ctx &c, const ScanOp &op, bool backward)
 {
     const Places at = places(op.d);
     if (!backward) {
-        const int64_t waves = (int64_t)at.waves * op.d.G * op.d.N;
-        hipLaunchKernelGGL((scan_kernel<T, SL>), dim3((uint32_t)ceil_div(waves, FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at);
+        if (op.d.T == 1) {
+            hipLaunchKernelGGL((step_kernel<T, SL>), dim3((uint32_t)ceil_div((int64_t)op.d.N * op.d.D, 64)), dim3(256), 0, c.stream, op);
+            return hipGetLastError();
+        }
+        Segments seg = {};
+        seg.count = segments_of(op.d, c.cus < 256 ? c.cus : 256);
+        seg.steps = (int)round_up(ceil_div(op.d.T, seg.count), Shape<SL>::L);
+        const int64_t states = (int64_t)op.d.N * op.d.D * Shape<SL>::SP, waves = (int64_t)at.waves * op.d.G * op.d.N;
+        if (seg.count > 1) {
+            seg.h_in = (float *)c.ws;
+            seg.state = seg.h_in + states;
+            seg.sum = seg.state + (seg.count - 1) * states;
+            hipLaunchKernelGGL((scan_kernel<T, SL, true>), dim3((uint32_t)ceil_div(waves * (seg.count - 1), FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL((scan_kernel<T, SL, false>), dim3((uint32_t)ceil_div(waves * seg.count, FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
         return hipGetLastError();
     }
     const int blocks = blocks_of(op.d);
@@ -429,7 +682,12 @@ template <typename T> hipError_t by_states(hts_seq_ctx &c, const ScanOp &op, boo
 }  // namespace
 
 int64_t scan_states(const hts_scan_desc &d) { return ceil_div(d.T, chunk_steps(d.S)) * d.N * d.D * padded(d.S); }
-int64_t scan_workspace(const hts_scan_desc &d) { return 4 * (pair_floats(d) + param_floats(d)); }
+int64_t scan_workspace(const hts_scan_desc &d, bool backward)
+{
+    // (on fewer compute units there are fewer segments)
+    if (!backward) return 4 * segment_floats(d, segments_of(d, 256));
+    return 4 * (pair_floats(d) + param_floats(d));
+}
 hipError_t launch_scan(hts_seq_ctx &c, const ScanOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? by_states<bf16_t>(c, op, false) : by_states<float>(c, op, false); }
 hipError_t launch_scan_backward(hts_seq_ctx &c, const ScanOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? by_states<bf16_t>(c, op, true) : by_states<float>(c, op, true); }
 

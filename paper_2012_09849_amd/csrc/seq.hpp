@@ -40,9 +40,9 @@ struct ScanOp {
     hts_scan_grads g;
 };
 
-int64_t linear_workspace(int precision, int act, int64_t M, int64_t N, int64_t K);
+int64_t linear_workspace(int precision, int act, int64_t M, int64_t N, int64_t K);      // of the backward call; the forward call needs none
 int64_t conv_workspace(int64_t T, int64_t N, int64_t D, int W);
-int64_t scan_workspace(const hts_scan_desc &d);
+int64_t scan_workspace(const hts_scan_desc &d, bool backward);
 int64_t scan_states(const hts_scan_desc &d);
 hipError_t launch_linear(hts_seq_ctx &c, int precision, const LinearOp &op);
 hipError_t launch_linear_backward(hts_seq_ctx &c, int precision, const LinearOp &op);

@@ -59,7 +59,8 @@ static int32_t check_rows(const hts_rows &r, int64_t rows, int64_t cols, int siz
 static int32_t check_steps(const hts_steps &s, int64_t T, int64_t N, int64_t cols, int size, bool output)
 {
     if (!s.p || misaligned(s.p, size) || s.st < 0 || s.sn < 0) return HTS_EINVAL;
-    if (s.st > (1ll << 40) || s.sn > (1ll << 40)) return HTS_ESHAPE;
+    // (a few steps' distance is counted in 32 bits)
+    if ((T > 1 && s.st > (1ll << 24)) || s.sn > (1ll << 40)) return HTS_ESHAPE;
     if (!output) return HTS_OK;
     const bool by_step = (N == 1 || s.sn >= cols) && (T == 1 || s.st >= (N == 1 ? cols : s.sn * (N - 1) + cols));
     const bool by_sequence = (T == 1 || s.st >= cols) && (N == 1 || s.sn >= (T == 1 ? cols : s.st * (T - 1) + cols));
@@ -117,7 +118,6 @@ extern "C" int32_t hts_linear(hts_seq_ctx *ctx, const hts_linear_desc *d, hts_ro
     if (residual.p) CHECK(check_rows(residual, d->M, d->N, s, false));
     if (pre.p) CHECK(check_rows(pre, d->M, d->N, s, true));
     if (misaligned(bias, 4)) return HTS_EINVAL;
-    CHECK(check_workspace(ctx, linear_workspace(d->precision, d->act, d->M, d->N, d->K)));
     LinearOp op = {};
     op.M = d->M; op.N = d->N; op.K = d->K; op.act = d->act;
     op.x = x; op.w = w; op.bias = bias; op.residual = residual; op.y = y; op.pre = pre;
@@ -210,7 +210,7 @@ static int32_t check_scan(const hts_scan_desc *d)
 {
     if (!d) return HTS_EINVAL;
     if (d->T <= 0 || d->N <= 0 || d->D <= 0 || d->S <= 0 || d->G <= 0 || (d->softplus != 0 && d->softplus != 1)) return HTS_EINVAL;
-    if (bad_precision(d->precision) || d->S > 64 || d->D % d->G != 0 || d->D > (1 << 20)) return HTS_ESHAPE;
+    if (bad_precision(d->precision) || d->S > 64 || d->D % d->G != 0 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
     // a workgroup per 16 channels and 16 steps at least; their number has 31 bits
     return ceil_div(d->T, 16) * d->N * (ceil_div(d->D / d->G, 16) * d->G) > (1ll << 30) ? HTS_ESHAPE : HTS_OK;
 }
@@ -218,7 +218,8 @@ static int32_t check_scan(const hts_scan_desc *d)
 extern "C" int64_t hts_selective_scan_workspace(const hts_scan_desc *d)
 {
     CHECK(check_scan(d));
-    return scan_workspace(*d);
+    const int64_t forward = scan_workspace(*d, false), backward = scan_workspace(*d, true);
+    return forward > backward ? forward : backward;
 }
 extern "C" int64_t hts_selective_scan_states(const hts_scan_desc *d)
 {
@@ -244,7 +245,7 @@ extern "C" int32_t hts_selective_scan(hts_seq_ctx *ctx, const hts_scan_desc *d, 
     CHECK(check_scan_arrays(d, in));
     CHECK(check_steps(y, d->T, d->N, d->D, size_of(d->precision), true));
     if (misaligned(h_out, 4) || misaligned(states, 16)) return HTS_EINVAL;
-    CHECK(check_workspace(ctx, scan_workspace(*d)));
+    CHECK(check_workspace(ctx, scan_workspace(*d, false)));
     ScanOp op = {};
     op.d = *d; op.in = *in; op.y = y; op.h_out = h_out; op.states_out = states;
     HIP_TRY(launch_scan(*ctx, op));
@@ -266,7 +267,7 @@ extern "C" int32_t hts_selective_scan_backward(hts_seq_ctx *ctx, const hts_scan_
     if (g->dz.p) CHECK(check_steps(g->dz, d->T, d->N, d->D, s, true));
     if (!g->dA || misaligned(g->dA, 4) || misaligned(g->dskip, 4) || misaligned(g->ddt_bias, 4) || misaligned(g->dh_in, 4)) return HTS_EINVAL;
     if (misaligned(states, 16) || misaligned(dh_out, 4) || (dh_out && g->dh_in == dh_out)) return HTS_EINVAL;
-    CHECK(check_workspace(ctx, scan_workspace(*d)));
+    CHECK(check_workspace(ctx, scan_workspace(*d, true)));
     ScanOp op = {};
     op.d = *d; op.in = *in; op.dy = dy; op.dh_out = dh_out; op.states = states; op.g = *g;
     HIP_TRY(launch_scan_backward(*ctx, op));
