@@ -1,10 +1,11 @@
 // Selective state space scan and its gradients (see include/hts.h).
 //
 // h_t = a_t h_{t-1} + delta_t x_t B_t with a_t = exp(delta_t A) for every channel d and state s: time is serial, channels and states are not.
-// Four neighbouring lanes (a quad) hold a channel's states, SL of them a lane, in registers; a wavefront holds 16 channels of one sequence.
-// Steps come in fours: lane p of a quad loads and prepares step 4 j + p (softplus, gate), the quad's other lanes get what they need of it by
-// lane broadcasts, and the sums over the states are dealt out again to the lane that owns the step.  B and C, the same for all channels of a
-// group, are kept for L steps in LDS as binary32.  The work is vector instructions: exp2 (two issue slots) and four others for a state and step.
+// Four neighbouring lanes (a quad) hold a channel's states, SL of them a lane, in registers; a wavefront holds 16 channels of one sequence, L steps
+// (a chunk) at a time.  What belongs to a step and channel (softplus, gate, the outputs) is another lane's work: memory is read and written with a lane
+// for NB neighbouring channels of a step, so that a chunk is one instruction an array, and step sizes, inputs and sums over the states pass between the
+// two orders through LDS, which also holds B and C, the same for all channels of a group, as binary32.  The work is vector instructions: exp2 (two issue
+// slots) and four others for a state and step.
 //
 // Steps that are none (beyond a sequence's length) have delta = x = B = C = 0: a = 1, h stays.
 #include "seq.hpp"
@@ -19,16 +20,6 @@ template <int SL> struct Shape {
 constexpr int chunk_steps(int S) { return S <= 16 ? 16 : S <= 32 ? 8 : 4; }
 constexpr int padded(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : S <= 32 ? 32 : 64; }
 
-__device__ __forceinline__ float quad_from(float v, int q)
-{
-    const int x = __float_as_int(v);
-    switch (q) {
-    case 0: return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x00, 0xf, 0xf, true));
-    case 1: return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x55, 0xf, 0xf, true));
-    case 2: return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0xAA, 0xf, 0xf, true));
-    default: return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0xFF, 0xf, 0xf, true));
-    }
-}
 __device__ __forceinline__ float quad_xor1(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true)); }
 __device__ __forceinline__ float quad_xor2(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true)); }
 template <int CTRL> __device__ __forceinline__ float row_move(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
@@ -52,24 +43,11 @@ struct Places { int per_group, waves; };          // channels of a group, wavefr
 
 template <typename T> __device__ __forceinline__ float wide_of(T v) { return to_f32(v); }
 __device__ __forceinline__ int length_of(const int32_t *lengths, int n, int T) { return lengths ? max(0, min(T, lengths[n])) : T; }
-// Loads and stores through buffer descriptors: a base that all lanes share (the chunk's), 32 bits of a lane and 32 bits that all lanes share from it.
-// A lane that has nothing to load or store gets an offset beyond the descriptor's 2 GB: it reads zero and writes nothing, without a branch.
-// (the largest sum of both is below 2^32: the unit does not see a carry)
+// Loads and stores through buffer descriptors: a base that all lanes share (the chunk's) and 32 bits of a lane from it.  A lane that has nothing to
+// load or store gets an offset beyond the descriptor's 2 GB: it reads zero and writes nothing, without a branch (values that were loaded on different
+// paths would be waited for where the paths meet).
 constexpr uint32_t REACH = 1u << 31, NOWHERE = REACH;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t reach(const char *base) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, REACH, 0x00020000); }
-// (the bits in a register of its own: two 16-bit values packed into one would have to be waited for where they are loaded)
-template <typename T> __device__ __forceinline__ uint32_t take(__amdgpu_buffer_rsrc_t src, uint32_t lane, uint32_t all)
-{
-    if constexpr (sizeof(T) == 2) return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(src, (int)lane, (int)all, 0);
-    else return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, (int)lane, (int)all, 0);
-}
-template <typename T> __device__ __forceinline__ float value_of(uint32_t bits) { return __uint_as_float(sizeof(T) == 2 ? bits << 16 : bits); }
-template <typename T> __device__ __forceinline__ void give(__amdgpu_buffer_rsrc_t dst, uint32_t lane, uint32_t all, float v)
-{
-    const T r = from_f32<T>(v);
-    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, r), dst, (int)lane, (int)all, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, r), dst, (int)lane, (int)all, 0);
-}
 
 // An array's chunk: the base goes from chunk to chunk, so that a chunk's addresses are a few scalar additions
 struct Walk {
@@ -84,53 +62,103 @@ struct Walk {
     __device__ __forceinline__ void forth() { base += chunk; }
     __device__ __forceinline__ void back() { base -= chunk; }
 };
-// Where a wavefront's 16 channels of a sequence are; the lanes of step q are q steps further
-template <typename T> struct Track : Walk {
-    uint32_t lane;
-    __device__ __forceinline__ void open(const hts_steps &a, int n, int first, int channel, int q, int t0, int L)
+
+// V neighbouring entries of a lane: one access where addresses and counts allow it (WIDE), otherwise an entry at a time, `count` of them
+template <typename T, int V, bool WIDE> struct Raw {
+    static constexpr int WORDS = WIDE ? (V * (int)sizeof(T) + 3) / 4 : V;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t src, uint32_t lane, int count)
     {
-        Walk::open(a.p, (n * a.sn + first) * (int64_t)sizeof(T), a.st * (int64_t)sizeof(T), t0, L);
-        lane = a.p ? (uint32_t)q * step + (uint32_t)(channel - first) * (uint32_t)sizeof(T) : NOWHERE;
-    }
-    // the lane's channel in steps 4 j + q of the chunk at t0, and the next chunk's turn.  Without a branch, here and below: values that were loaded on
-    // different paths would be waited for where the paths meet
-    template <int NB> __device__ __forceinline__ void load(uint32_t (&v)[NB], int t0, int q, int len) const
-    {
-        const __amdgpu_buffer_rsrc_t src = reach(base);
+        if constexpr (WIDE && WORDS == 4) {
+            const auto r = __builtin_amdgcn_raw_buffer_load_b128(src, (int)lane, 0, 0);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) v[j] = take<T>(src, t0 + 4 * j + q < len ? lane : NOWHERE, 4 * j * step);
-    }
-    template <int NB> __device__ __forceinline__ void store(const float (&v)[NB], int t0, int q, int T_, bool on) const
-    {
-        const __amdgpu_buffer_rsrc_t dst = reach(base);
+            for (int i = 0; i < 4; ++i) w[i] = r[i];
+        } else if constexpr (WIDE && WORDS == 2) {
+            const auto r = __builtin_amdgcn_raw_buffer_load_b64(src, (int)lane, 0, 0);
+            w[0] = r[0]; w[1] = r[1];
+        } else if constexpr (WIDE && V * sizeof(T) == 4) w[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, (int)lane, 0, 0);
+        else
 #pragma unroll
-        for (int j = 0; j < NB; ++j) give<T>(dst, on && t0 + 4 * j + q < T_ ? lane : NOWHERE, 4 * j * step, v[j]);
+            for (int i = 0; i < V; ++i) {
+                const int at = i < count ? (int)(lane + i * (uint32_t)sizeof(T)) : (int)NOWHERE;
+                if constexpr (sizeof(T) == 2) w[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(src, at, 0, 0);
+                else w[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, at, 0, 0);
+            }
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else if constexpr (!WIDE || V == 1) return __uint_as_float(w[i] << 16);
+        else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
 };
-// B or C of a chunk, THREADS lanes: value number i THREADS + tid is (step, state)
-template <typename T, int SL, int THREADS> struct Half : Walk {
-    static constexpr int SP = Shape<SL>::SP, L = Shape<SL>::L, NL = (L * SP + THREADS - 1) / THREADS, STEPS = THREADS / SP;
-    static_assert(THREADS % SP == 0, "lanes");
+template <typename T> __device__ __forceinline__ uint32_t bits_of(float v)
+{
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(uint16_t, from_f32<T>(v));
+    else return __float_as_uint(v);
+}
+template <typename T, int V, bool WIDE> __device__ __forceinline__ void put_raw(__amdgpu_buffer_rsrc_t dst, uint32_t lane, int count, const float (&v)[V])
+{
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    if constexpr (WIDE && V * sizeof(T) >= 4) {
+        constexpr int WORDS = V * (int)sizeof(T) / 4;
+        uint32_t w[WORDS];
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = sizeof(T) == 4 ? bits_of<T>(v[i]) : bits_of<T>(v[V > 1 ? 2 * i : 0]) | bits_of<T>(v[V > 1 ? 2 * i + 1 : 0]) << 16;
+        if constexpr (WORDS == 1) __builtin_amdgcn_raw_buffer_store_b32(w[0], dst, (int)lane, 0, 0);
+        else if constexpr (WORDS == 2) __builtin_amdgcn_raw_buffer_store_b64(u2{w[0], w[1]}, dst, (int)lane, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b128(u4{w[0], w[1], w[2], w[3]}, dst, (int)lane, 0, 0);
+    } else
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int at = i < count ? (int)(lane + i * (uint32_t)sizeof(T)) : (int)NOWHERE;
+            if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bits_of<T>(v[i]), dst, at, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b32(bits_of<T>(v[i]), dst, at, 0, 0);
+        }
+}
+
+// The order of memory: lane = (step of the chunk, V neighbouring ones of the wavefront's 16 channels)
+template <int SL> struct Cell {
+    static constexpr int V = Shape<SL>::NB, PER = 16 / V;
+    int step, channel, count;          // count: of the V channels that exist
+    __device__ __forceinline__ void open(int lane, int channels)
+    {
+        step = lane / PER; channel = lane % PER * V;
+        count = max(0, min(V, channels - channel));
+    }
+};
+template <typename T, int SL, bool WIDE> struct Track : Walk {
+    static constexpr int V = Shape<SL>::NB;
     uint32_t lane;
-    int first;                         // the lane's step of a load
+    __device__ __forceinline__ void open(const hts_steps &a, int n, int first, const Cell<SL> &c, int t0)
+    {
+        Walk::open(a.p, (n * a.sn + first) * (int64_t)sizeof(T), a.st * (int64_t)sizeof(T), t0, Shape<SL>::L);
+        lane = a.p && c.count > 0 ? (uint32_t)c.step * step + (uint32_t)c.channel * (uint32_t)sizeof(T) : NOWHERE;
+    }
+    __device__ __forceinline__ void load(Raw<T, V, WIDE> &v, bool live, const Cell<SL> &c) const { v.load(reach(base), live ? lane : NOWHERE, live ? c.count : 0); }
+    __device__ __forceinline__ void store(const float (&v)[V], bool some, const Cell<SL> &c) const { put_raw<T, V, WIDE>(reach(base), some ? lane : NOWHERE, some ? c.count : 0, v); }
+};
+// B or C of a chunk: 4 neighbouring states of a step a lane
+template <typename T, int SL, bool WIDE> struct Half : Walk {
+    static constexpr int SP = Shape<SL>::SP, L = Shape<SL>::L;
+    static_assert(L * SP <= 256, "lanes");
+    uint32_t lane;
+    int at, count, row;                // its step, how many of the 4 states exist, its place in LDS
     __device__ __forceinline__ void open(const hts_steps &a, int n, int g, int S, int tid, int t0)
     {
-        const int k = tid % SP;
+        const int s = tid * 4 % SP;
         Walk::open(a.p, (n * a.sn + (int64_t)g * S) * (int64_t)sizeof(T), a.st * (int64_t)sizeof(T), t0, L);
-        first = tid / SP;
-        lane = k < S && first < L ? (uint32_t)first * step + k * (uint32_t)sizeof(T) : NOWHERE;
+        at = tid * 4 / SP;
+        count = at < L ? max(0, min(4, S - s)) : 0;
+        lane = count > 0 ? (uint32_t)at * step + (uint32_t)s * (uint32_t)sizeof(T) : NOWHERE;
+        row = at * Shape<SL>::PAIR + s;
     }
-    __device__ __forceinline__ void load(uint32_t (&v)[NL], int t0, int len) const
+    __device__ __forceinline__ void load(Raw<T, 4, WIDE> &v, int t0, int len) const { v.load(reach(base), t0 + at < len ? lane : NOWHERE, t0 + at < len ? count : 0); }
+    __device__ __forceinline__ void put(const Raw<T, 4, WIDE> &v, float *lds) const
     {
-        const __amdgpu_buffer_rsrc_t src = reach(base);
-#pragma unroll
-        for (int i = 0; i < NL; ++i) v[i] = take<T>(src, t0 + i * STEPS + first < len ? lane : NOWHERE, i * STEPS * step);
-    }
-    __device__ __forceinline__ void put(const uint32_t (&v)[NL], float *lds, int tid) const
-    {
-#pragma unroll
-        for (int i = 0; i < NL; ++i)
-            if (L * SP >= THREADS || first < L) lds[(i * STEPS + first) * (2 * SP) + tid % SP] = value_of<T>(v[i]);
+        if (L * SP < 256 && at >= L) return;
+        *reinterpret_cast<f32x4 *>(lds + row) = f32x4{v[0], v[1], v[2], v[3]};
     }
 };
 // which of a chunk's steps begin an episode: a lane loads a step's flag, `mask` collects them (bit k: step t0 + k), as late as it is needed
@@ -146,6 +174,22 @@ template <int L> struct Begins : Walk {
         v = (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(reach(base), t0 + (tid & (L - 1)) < len ? (int)lane : (int)NOWHERE, 0, 0);
     }
     static __device__ __forceinline__ uint32_t mask(uint32_t v) { return (uint32_t)__ballot(v != 0) & ((1u << L) - 1); }
+};
+// Between the two orders: [16 channels][L steps] of binary32, a row a multiple of 16 bytes long that spreads the channels over the banks
+template <int SL> struct Swap {
+    static constexpr int V = Shape<SL>::NB, L = Shape<SL>::L, PITCH = L + 4, SIZE = 16 * PITCH;
+    static __device__ __forceinline__ void put(float *lds, const Cell<SL> &c, const float (&v)[V])
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) lds[(c.channel + e) * PITCH + c.step] = v[e];
+    }
+    static __device__ __forceinline__ void get(float (&v)[V], const float *lds, const Cell<SL> &c)
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = lds[(c.channel + e) * PITCH + c.step];
+    }
+    // steps 4 j .. 4 j + 3 of a quad's channel
+    static __device__ __forceinline__ f32x4 four(const float *lds, int channel, int j) { return *reinterpret_cast<const f32x4 *>(lds + channel * PITCH + 4 * j); }
 };
 // the states that a training pass keeps: SL floats of a lane, the same place in every chunk
 template <int SL> struct Kept : Walk {
@@ -229,98 +273,109 @@ template <int SL> __device__ __forceinline__ void state_before(float (&h)[SL], c
 constexpr int FWD_WAVES = 4;
 
 // STATES: the first pass over segments, which needs neither C nor the gate and writes no output
-template <typename T, int SL, bool STATES>
+template <typename T, int SL, bool WIDE, bool STATES>
 __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, const Places at, const Segments seg)
 {
     typedef Shape<SL> H;
+    typedef Swap<SL> X;
     constexpr int L = H::L, NB = H::NB, SP = H::SP;
-    __shared__ __attribute__((aligned(16))) float pairs[FWD_WAVES][L * H::PAIR];
+    __shared__ __attribute__((aligned(16))) float shared[FWD_WAVES][L * H::PAIR + 3 * X::SIZE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = p.d.D, S = p.d.S, N = p.d.N;
     const int per = at.waves * p.d.G;                                   // wavefronts of a sequence's segment
     const uint32_t task = blockIdx.x * FWD_WAVES + wave, row = task / per, in_row = task % per;        // (their number has 31 bits)
     if (row >= (uint32_t)(N * (seg.count - STATES))) return;
-    const int k = row / N, n = row % N, g = in_row / at.waves, c = in_row % at.waves * 16, q = lane & 3;
-    const bool on = c + (lane >> 2) < at.per_group;
-    const int d0 = g * at.per_group + c, d = g * at.per_group + min(c + (lane >> 2), at.per_group - 1), len = length_of(p.in.lengths, n, p.d.T);
-    const int first = k * seg.steps, end = min(p.d.T, first + seg.steps);
-    Track<T> xa, da, za, ya;
+    const int k = row / N, n = row % N, g = in_row / at.waves, c = in_row % at.waves * 16, q = lane & 3, own = lane >> 2;
+    const int d0 = g * at.per_group + c, d = d0 + own, len = length_of(p.in.lengths, n, p.d.T);
+    const bool on = c + own < at.per_group;
+    const int first = k * seg.steps, end = min(p.d.T, first + seg.steps), live = min(len, end);
+    Cell<SL> cell;
+    cell.open(lane, at.per_group - c);
+    Track<T, SL, WIDE> xa, da, za, ya;
     Kept<SL> kept;
-    xa.open(p.in.x, n, d0, d, q, first, L); da.open(p.in.dt, n, d0, d, q, first, L);
-    if (!STATES) { za.open(p.in.z, n, d0, d, q, first, L); ya.open(p.y, n, d0, d, q, first, L); kept.open(p.states_out, N, n, D, d0, d, q, first / L); }
-    const float skip = p.in.skip ? p.in.skip[d] : 0.0f, bias = p.in.dt_bias ? p.in.dt_bias[d] : 0.0f;
-    float A[SL], h[SL], sum = 0.0f;
+    xa.open(p.in.x, n, d0, cell, first); da.open(p.in.dt, n, d0, cell, first);
+    if (!STATES) { za.open(p.in.z, n, d0, cell, first); ya.open(p.y, n, d0, cell, first); kept.open(p.states_out, N, n, D, d0, d, q, first / L); }
+    float skip[NB], bias[NB], sum[NB];
+#pragma unroll
+    for (int e = 0; e < NB; ++e) {
+        const bool some = e < cell.count;
+        skip[e] = some && p.in.skip ? p.in.skip[d0 + cell.channel + e] : 0.0f;
+        bias[e] = some && p.in.dt_bias ? p.in.dt_bias[d0 + cell.channel + e] : 0.0f;
+        sum[e] = 0.0f;
+    }
+    float A[SL], h[SL];
     bool cut = false;
 #pragma unroll
     for (int s = 0; s < SL; ++s) {
         const int i = q * SL + s;
-        A[s] = i < S ? p.in.A[(int64_t)d * S + i] * LOG2E : 0.0f;
-        h[s] = i < S && p.in.h_in && (STATES ? k == 0 : seg.count == 1) ? p.in.h_in[((int64_t)n * D + d) * S + i] : 0.0f;
+        A[s] = on && i < S ? p.in.A[(int64_t)d * S + i] * LOG2E : 0.0f;
+        h[s] = on && i < S && p.in.h_in && (STATES ? k == 0 : seg.count == 1) ? p.in.h_in[((int64_t)n * D + d) * S + i] : 0.0f;
         if (STATES && k == 0 && on) seg.h_in[state_at<SL>(n, d, D, q) + s] = h[s];
     }
-    if (!STATES && seg.count > 1) state_before<SL>(h, seg, k, n, N, d, D, q, A);
-    Half<T, SL, 64> bs, cs;
+    if (!STATES && seg.count > 1 && on) state_before<SL>(h, seg, k, n, N, d, D, q, A);
+    Half<T, SL, WIDE> bs, cs;
     Begins<L> begins;
     bs.open(p.in.B, n, g, S, lane, first);
     if (!STATES) cs.open(p.in.C, n, g, S, lane, first);
     begins.open(p.in.starts, n, N, lane, first);
-    struct Loads { uint32_t x[NB], dt[NB], z[NB], b[Half<T, SL, 64>::NL], c[Half<T, SL, 64>::NL], begins; } in;          // what is on its way for the next chunk
+    struct { Raw<T, NB, WIDE> x, dt, z; Raw<T, 4, WIDE> b, c; uint32_t begins; } in;          // what is on its way for the next chunk
     // (beyond the segment's end nothing is loaded.)  Fenced off: were the loads moved before the last use of what they replace, they would need registers
     // of their own, and copies from these at the loop's end, which wait for them
     auto fetch = [&](int t0) {
         __builtin_amdgcn_sched_barrier(0);
-        const int live = min(len, end);
+        const bool some = t0 + cell.step < live;
         begins.load(in.begins, t0, live, lane);
-        xa.load(in.x, t0, q, live);
-        da.load(in.dt, t0, q, live);
+        xa.load(in.x, some, cell);
+        da.load(in.dt, some, cell);
         bs.load(in.b, t0, live);
         xa.forth(); da.forth(); bs.forth(); begins.forth();
         if (!STATES) {
-            za.load(in.z, t0, q, live);
+            za.load(in.z, some, cell);
             cs.load(in.c, t0, live);
             za.forth(); cs.forth();
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    float *lds = pairs[wave];
+    float *pairs = shared[wave], *sizes = pairs + L * H::PAIR, *moves = sizes + X::SIZE, *outs = moves + X::SIZE;
     fetch(first);
     for (int t0 = first; t0 < end; t0 += L) {
+        const bool some = t0 + cell.step < live;
         float xv[NB], size[NB], moved[NB], gate[NB];
         wave_order();
-        bs.put(in.b, lds, lane);
-        if (!STATES) cs.put(in.c, lds + SP, lane);
-        wave_order();
+        bs.put(in.b, pairs);
+        if (!STATES) cs.put(in.c, pairs + SP);
         const uint32_t fresh = Begins<L>::mask(in.begins);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const bool live = t0 + 4 * j + q < len;
-            xv[j] = value_of<T>(in.x[j]);
-            const float v = value_of<T>(in.dt[j]) + bias;
+        for (int e = 0; e < NB; ++e) {
+            xv[e] = in.x[e];
+            const float v = in.dt[e] + bias[e];
             float soft, slope;
             softplus_f(v, soft, slope);
-            size[j] = live ? p.d.softplus ? soft : v : 0.0f;
-            moved[j] = size[j] * xv[j];
-            const float open = act_f<HTS_ACT_SILU>(value_of<T>(in.z[j]));
-            gate[j] = p.in.z.p ? open : 1.0f;
-            sum += size[j];
+            size[e] = some ? p.d.softplus ? soft : v : 0.0f;
+            moved[e] = size[e] * xv[e];
+            const float open = STATES ? 1.0f : act_f<HTS_ACT_SILU>(in.z[e]);
+            gate[e] = p.in.z.p ? open : 1.0f;
+            sum[e] += size[e];
         }
+        X::put(sizes, cell, size);
+        X::put(moves, cell, moved);
         if (STATES) cut |= fresh != 0;
+        wave_order();
         fetch(t0 + L);
         if (!STATES && p.states_out && on) {
             float *out = kept.at();
 #pragma unroll
             for (int s = 0; s < SL; ++s) out[s] = h[s];
         }
-        float ys[NB];
         // twice: chunks in which no episode begins, most of them, reset nothing
         auto pass = [&](auto has) {
-            Ahead<SL, !STATES> ahead(lds + q * SL);
+            Ahead<SL, !STATES> ahead(pairs + q * SL);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
+                const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j);
                 float sums[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = 4 * j + i;
-                    const float de = quad_from(size[j], i), dx = quad_from(moved[j], i);
                     ahead.next(t, L, +1);
                     if (decltype(has)::value && (fresh >> t & 1))
 #pragma unroll
@@ -328,27 +383,40 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
                     float y = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
-                        h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(de * A[s]), h[s], dx * ahead.B(t)[s]);
+                        h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(de[i] * A[s]), h[s], dx[i] * ahead.B(t)[s]);
                         if (!STATES) y = __builtin_fmaf(h[s], ahead.C(t)[s], y);
                     }
                     sums[i] = y;
                 }
-                if (STATES) continue;
-                const float y = __builtin_fmaf(skip, xv[j], quad_deal(sums, q)) * gate[j];      // (by all lanes of the quad, those of no step too)
-                ys[j] = t0 + 4 * j + q < len ? y : 0.0f;
+                if (!STATES) outs[own * X::PITCH + 4 * j + q] = quad_deal(sums, q);
             }
         };
         if (fresh) pass(std::true_type()); else pass(std::false_type());
-        if (!STATES) { ya.store(ys, t0, q, p.d.T, on); ya.forth(); kept.forth(); }
-    }
-    if (!on) return;
-    if (STATES) {
-        float *out = seg.state + state_at<SL>((int64_t)k * N + n, d, D, q);
+        if (!STATES) {
+            wave_order();
+            float y[NB];
+            X::get(y, outs, cell);
+            // (beyond the sequence's end 0 whatever the state)
 #pragma unroll
-        for (int s = 0; s < SL; ++s) out[s] = h[s];
-        sum = quad_sum(sum);
-        if (q == 0) seg.sum[((int64_t)k * N + n) * D + d] = cut ? __builtin_nanf("") : sum;
-    } else if (p.h_out && k == seg.count - 1)
+            for (int e = 0; e < NB; ++e) y[e] = some ? __builtin_fmaf(skip[e], xv[e], y[e]) * gate[e] : 0.0f;
+            ya.store(y, t0 + cell.step < p.d.T, cell);
+            ya.forth(); kept.forth();
+        }
+    }
+    if (STATES) {
+        if (on) {
+            float *out = seg.state + state_at<SL>((int64_t)k * N + n, d, D, q);
+#pragma unroll
+            for (int s = 0; s < SL; ++s) out[s] = h[s];
+        }
+        // over the chunk's steps, which are other lanes
+#pragma unroll
+        for (int e = 0; e < NB; ++e) {
+#pragma unroll
+            for (int m = Cell<SL>::PER; m < 64; m *= 2) sum[e] += __shfl_xor(sum[e], m);
+            if (cell.step == 0 && e < cell.count) seg.sum[((int64_t)k * N + n) * D + d0 + cell.channel + e] = cut ? __builtin_nanf("") : sum[e];
+        }
+    } else if (on && p.h_out && k == seg.count - 1)
 #pragma unroll
         for (int s = 0; s < SL; ++s)
             if (q * SL + s < S) p.h_out[((int64_t)n * D + d) * S + q * SL + s] = h[s];
@@ -398,22 +466,41 @@ __global__ __launch_bounds__(256) void step_kernel(const ScanOp p)
     if (q == 0) ((T *)p.y.p)[n * p.y.sn + d] = from_f32<T>(y);
 }
 
-// Sums over the 16 channels of a wavefront (lane bits 2 .. 5) of NV = 4 K values: after two exchanges of halves a lane has the sums over bits 4
-// and 5 of K values, those of v[(2 bit5 + bit4) K ...], and two rotations add bits 2 and 3.
-template <int K> __device__ __forceinline__ void channel_sums(float (&out)[K], const float (&v)[4 * K])
+// Sums over the 16 channels of a wavefront (lane bits 2 .. 5) of NV values; each step halves the values that a lane keeps.  Within a row of 16 lanes an
+// addition takes its neighbour's value along and writes half the row's banks only, so two of them halve a pair of values: 1 issue slot a value, where an
+// exchange between rows takes 1.5.  A lane ends with the sums of v[(8 bit3 + 4 bit2 + 2 bit4 + bit5) NV / 16 ...].
+// (written out, since the compiler selects with instructions of its own; an instruction that takes a neighbour's value has to be two slots after the one
+// that wrote it, and the exchange that follows one after)
+#define HTS_FOLD(NAME, LOW, HIGH, LOWBANKS, HIGHBANKS)                                                                                                     \
+    __device__ __forceinline__ void NAME(float &a, float &b, float a0, float a1, float b0, float b1)                                                      \
+    {                                                                                                                                                     \
+        asm("s_nop 1\n\t"                                                                                                                                 \
+            "v_add_f32_dpp %0, %2, %2 " LOW " row_mask:0xf bank_mask:" LOWBANKS "\n\t"                                                                    \
+            "v_add_f32_dpp %1, %4, %4 " LOW " row_mask:0xf bank_mask:" LOWBANKS "\n\t"                                                                    \
+            "v_add_f32_dpp %0, %3, %3 " HIGH " row_mask:0xf bank_mask:" HIGHBANKS "\n\t"                                                                  \
+            "v_add_f32_dpp %1, %5, %5 " HIGH " row_mask:0xf bank_mask:" HIGHBANKS "\n\t"                                                                  \
+            "s_nop 1"                                                                                                                                     \
+            : "=&v"(a), "=&v"(b) : "v"(a0), "v"(a1), "v"(b0), "v"(b1));                                                                                   \
+    }
+HTS_FOLD(fold_bit3, "row_ror:8", "row_ror:8", "0x3", "0xc")
+HTS_FOLD(fold_bit2, "row_shl:4", "row_shr:4", "0x5", "0xa")
+#undef HTS_FOLD
+template <int NV> __device__ __forceinline__ void channel_sums(float (&out)[NV / 16], const float (&v)[NV])
 {
-    float a[2 * K];
+    float a[NV / 2], b[NV / 4], c[NV / 8];
 #pragma unroll
-    for (int i = 0; i < 2 * K; ++i) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 2 * K]), false, false);
-        a[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    for (int i = 0; i < NV / 2; i += 2) fold_bit3(a[i], a[i + 1], v[i], v[i + NV / 2], v[i + 1], v[i + 1 + NV / 2]);
+#pragma unroll
+    for (int i = 0; i < NV / 4; i += 2) fold_bit2(b[i], b[i + 1], a[i], a[i + NV / 4], a[i + 1], a[i + 1 + NV / 4]);
+#pragma unroll
+    for (int i = 0; i < NV / 8; ++i) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(b[i]), __float_as_uint(b[i + NV / 8]), false, false);
+        c[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[i]), __float_as_uint(a[i + K]), false, false);
-        float s = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-        s += row_move<0x128>(s);
-        out[i] = s + row_move<0x124>(s);
+    for (int i = 0; i < NV / 16; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(c[i]), __float_as_uint(c[i + NV / 16]), false, false);
+        out[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
 }
 
@@ -424,90 +511,108 @@ constexpr int BWD_WAVES = 4;
 //   g_t = r_t C_t + a_{t+1} g_{t+1},  dB = sum_d g delta x,  dC = sum_d r h,  d(delta) = sum_s g a h_{t-1} A + x sum_s g B,  dA = sum_t g a h_{t-1} delta
 // dB and dC of a workgroup's channels are added in LDS in a fixed order and leave as a partial sum a workgroup; dA, dskip and ddt_bias stay in
 // registers for the whole sequence.  At an episode's first step the products with a are 0, also where the other factor is not finite.
-template <typename T, int SL>
+template <typename T, int SL, bool WIDE>
 __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const ScanOp p, const Places at, const int blocks, float *pair_part, float *param_part)
 {
     typedef Shape<SL> H;
+    typedef Swap<SL> X;
     constexpr int L = H::L, NB = H::NB, SP = H::SP, PAIR = H::PAIR, THREADS = 64 * BWD_WAVES;
     __shared__ __attribute__((aligned(16))) float pairs[2][L * PAIR];
     __shared__ __attribute__((aligned(16))) float sums[2][BWD_WAVES][L * PAIR];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 3;
+    __shared__ __attribute__((aligned(16))) float swaps[BWD_WAVES][6 * X::SIZE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 3, own = lane >> 2;
     const int block = blockIdx.x % blocks, g = blockIdx.x / blocks % p.d.G, n = blockIdx.x / blocks / p.d.G;
-    const int c = (block * BWD_WAVES + wave) * 16 + (lane >> 2);
-    const bool on = c < at.per_group;
-    const int D = p.d.D, S = p.d.S, TT = p.d.T, d = g * at.per_group + min(c, at.per_group - 1), len = length_of(p.in.lengths, n, TT);
-    Track<T> xa, da, za, ga, dxa, dda, dza;
-    const int d0 = g * at.per_group + min((block * BWD_WAVES + wave) * 16, at.per_group - 1);
+    const int c = (block * BWD_WAVES + wave) * 16, D = p.d.D, S = p.d.S, TT = p.d.T, len = length_of(p.in.lengths, n, TT);
+    const bool on = c + own < at.per_group;
+    const int d0 = g * at.per_group + c, d = d0 + own;
     const int chunks = (TT + L - 1) / L, last = (chunks - 1) * L;
-    xa.open(p.in.x, n, d0, d, q, last, L); da.open(p.in.dt, n, d0, d, q, last, L); za.open(p.in.z, n, d0, d, q, last, L); ga.open(p.dy, n, d0, d, q, last, L);
-    dxa.open(p.g.dx, n, d0, d, q, last, L); dda.open(p.g.ddt, n, d0, d, q, last, L); dza.open(p.g.dz, n, d0, d, q, last, L);
+    Cell<SL> cell;
+    cell.open(lane, at.per_group - c);
+    Track<T, SL, WIDE> xa, da, za, ga, dxa, dda, dza;
+    xa.open(p.in.x, n, d0, cell, last); da.open(p.in.dt, n, d0, cell, last); za.open(p.in.z, n, d0, cell, last); ga.open(p.dy, n, d0, cell, last);
+    dxa.open(p.g.dx, n, d0, cell, last); dda.open(p.g.ddt, n, d0, cell, last); dza.open(p.g.dz, n, d0, cell, last);
     Kept<SL> kept;
     kept.open(p.states, p.d.N, n, D, d0, d, q, chunks - 1);
-    const float skip = p.in.skip ? p.in.skip[d] : 0.0f, bias = p.in.dt_bias ? p.in.dt_bias[d] : 0.0f;
-    float A[SL], ag[SL], dA[SL], dskip = 0.0f, dbias = 0.0f;
+    float skip[NB], bias[NB], dskip[NB], dbias[NB];
+#pragma unroll
+    for (int e = 0; e < NB; ++e) {
+        const bool some = e < cell.count;
+        skip[e] = some && p.in.skip ? p.in.skip[d0 + cell.channel + e] : 0.0f;
+        bias[e] = some && p.in.dt_bias ? p.in.dt_bias[d0 + cell.channel + e] : 0.0f;
+        dskip[e] = dbias[e] = 0.0f;
+    }
+    float A[SL], ag[SL], dA[SL];
 #pragma unroll
     for (int s = 0; s < SL; ++s) {
-        const int k = q * SL + s;
-        A[s] = k < S ? p.in.A[(int64_t)d * S + k] * LOG2E : 0.0f;
-        ag[s] = on && k < S && p.dh_out ? p.dh_out[((int64_t)n * D + d) * S + k] : 0.0f;
+        const int i = q * SL + s;
+        A[s] = on && i < S ? p.in.A[(int64_t)d * S + i] * LOG2E : 0.0f;
+        ag[s] = on && i < S && p.dh_out ? p.dh_out[((int64_t)n * D + d) * S + i] : 0.0f;
         dA[s] = 0.0f;
     }
-    uint32_t xs[NB], ds[NB], zs[NB], gs[NB];
-    Half<T, SL, THREADS> bs, cs;
-    bs.open(p.in.B, n, g, S, tid, last);
-    cs.open(p.in.C, n, g, S, tid, last);
-    float h0[SL];
-    uint32_t bv[Half<T, SL, THREADS>::NL], cv[Half<T, SL, THREADS>::NL];
+    // the workgroup's first wavefront brings B, its second C
+    Half<T, SL, WIDE> ps;
+    ps.open(wave == 1 ? p.in.C : p.in.B, n, g, S, lane, last);
+    if (wave > 1) ps.lane = NOWHERE, ps.count = 0;
     Begins<L> begins;
     begins.open(p.in.starts, n, p.d.N, lane, last);
-    uint32_t flag;
+    struct { Raw<T, NB, WIDE> x, dt, z, dy; Raw<T, 4, WIDE> pair; uint32_t begins; float h[SL]; } in;
     auto fetch = [&](int chunk) {          // (there is nothing to load before the first chunk)
         __builtin_amdgcn_sched_barrier(0);
         const int t0 = chunk * L, live = chunk >= 0 ? len : t0;
-        begins.load(flag, t0, live, lane);
-        xa.load(xs, t0, q, live);
-        da.load(ds, t0, q, live);
-        ga.load(gs, t0, q, live);
-        za.load(zs, t0, q, live);
-        bs.load(bv, t0, live);
-        cs.load(cv, t0, live);
-        kept.load(h0, chunk >= 0);
-        xa.back(); da.back(); za.back(); ga.back(); bs.back(); cs.back(); begins.back(); kept.back();
+        const bool some = t0 + cell.step < live;
+        begins.load(in.begins, t0, live, lane);
+        xa.load(in.x, some, cell);
+        da.load(in.dt, some, cell);
+        ga.load(in.dy, some, cell);
+        za.load(in.z, some, cell);
+        ps.load(in.pair, t0, live);
+        kept.load(in.h, on && chunk >= 0);
+        xa.back(); da.back(); za.back(); ga.back(); ps.back(); begins.back(); kept.back();
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto leave = [&](int chunk, int buf) {        // the workgroup's sums of a chunk
-        for (int i = tid; i < L * PAIR; i += THREADS) {
-            float s = 0.0f;
+    // the workgroup's sums of a chunk: a thread has two neighbouring ones of a step
+    static_assert(L * PAIR <= 2 * THREADS, "sums");
+    const int mine = 2 * tid / PAIR;
+    float *leaves = pair_part + ((((int64_t)block * TT + mine) * p.d.N + n) * p.d.G + g) * PAIR + 2 * tid % PAIR;
+    const int64_t row = (int64_t)p.d.N * p.d.G * PAIR;
+    auto leave = [&](int chunk, int buf) {
+        if (mine >= L || chunk * L + mine >= TT) return;
+        float a = 0.0f, b = 0.0f;
 #pragma unroll
-            for (int w = 0; w < BWD_WAVES; ++w) s += sums[buf][w][i];
-            const int t = chunk * L + i / PAIR;
-            if (t < TT) pair_part[((((int64_t)block * TT + t) * p.d.N + n) * p.d.G + g) * PAIR + i % PAIR] = s;
-        }
+        for (int w = 0; w < BWD_WAVES; ++w) { a += sums[buf][w][2 * tid]; b += sums[buf][w][2 * tid + 1]; }
+        float *to = leaves + chunk * (L * row);
+        to[0] = a; to[1] = b;
     };
+    float *sizes = swaps[wave], *moves = sizes + X::SIZE, *rs = moves + X::SIZE, *raws = rs + X::SIZE, *sBs = raws + X::SIZE, *sds = sBs + X::SIZE;
+    const int share = (2 * (lane >> 3 & 1) + (lane >> 2 & 1)) * PAIR + (lane >> 4 & 1) * SP + q * SL + (lane >> 5) * (SL / 2);
     fetch(chunks - 1);
     for (int chunk = chunks - 1, buf = 0; chunk >= 0; --chunk, buf ^= 1) {
         const int t0 = chunk * L;
-        bs.put(bv, pairs[buf], tid);
-        cs.put(cv, pairs[buf] + SP, tid);
-        float xv[NB], size[NB], moved[NB], slope[NB], r[NB], zf[NB], hb[SL];
+        const bool some = t0 + cell.step < len;
+        if (wave < 2) ps.put(in.pair, pairs[buf] + wave * SP);
+        float xv[NB], size[NB], slope[NB], r[NB], zf[NB], hb[SL];
+        {
+            float moved[NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const bool live = t0 + 4 * j + q < len;
-            xv[j] = on ? value_of<T>(xs[j]) : 0.0f;
-            const float v = value_of<T>(ds[j]) + bias;
-            float soft, rise;
-            softplus_f(v, soft, rise);
-            size[j] = live ? p.d.softplus ? soft : v : 0.0f;
-            slope[j] = live ? p.d.softplus ? rise : 1.0f : 0.0f;
-            moved[j] = size[j] * xv[j];
-            const float dyv = on ? value_of<T>(gs[j]) : 0.0f, zv = value_of<T>(zs[j]);
-            const float open = act_f<HTS_ACT_SILU>(zv);
-            r[j] = dyv * (p.in.z.p ? open : 1.0f);
-            zf[j] = dyv * act_slope<HTS_ACT_SILU>(zv);
+            for (int e = 0; e < NB; ++e) {
+                xv[e] = in.x[e];
+                const float v = in.dt[e] + bias[e];
+                float soft, rise;
+                softplus_f(v, soft, rise);
+                size[e] = some ? p.d.softplus ? soft : v : 0.0f;
+                slope[e] = some ? p.d.softplus ? rise : 1.0f : 0.0f;
+                moved[e] = size[e] * xv[e];
+                const float dy = in.dy[e], z = in.z[e], open = act_f<HTS_ACT_SILU>(z);
+                r[e] = dy * (p.in.z.p ? open : 1.0f);
+                zf[e] = dy * act_slope<HTS_ACT_SILU>(z);
+            }
+            X::put(sizes, cell, size);
+            X::put(moves, cell, moved);
+            X::put(rs, cell, r);
         }
 #pragma unroll
-        for (int s = 0; s < SL; ++s) hb[s] = h0[s];
-        const uint32_t fresh = Begins<L>::mask(flag);
+        for (int s = 0; s < SL; ++s) hb[s] = in.h[s];
+        const uint32_t fresh = Begins<L>::mask(in.begins);
         __syncthreads();
         fetch(chunk - 1);
         if (chunk < chunks - 1) leave(chunk + 1, buf ^ 1);
@@ -515,89 +620,102 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
         // twice: chunks in which no episode begins, most of them, select nothing
         auto pass = [&](auto has) {
             constexpr bool FRESH = decltype(has)::value;
-            float a[L][SL], h[L][SL], raw[NB];
+            float a[L][SL], h[L][SL];
             {
                 Ahead<SL, true> ahead(lds + q * SL);
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
+                    const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j);
                     float part[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int k = 4 * j + i;
-                        const float de = quad_from(size[j], i), dx = quad_from(moved[j], i);
                         ahead.next(k, L, +1);
                         const bool begin = FRESH && (fresh >> k & 1);
                         float sum = 0.0f;
 #pragma unroll
                         for (int s = 0; s < SL; ++s) {
-                            a[k][s] = __builtin_amdgcn_exp2f(de * A[s]);
-                            h[k][s] = __builtin_fmaf(dx, ahead.B(k)[s], begin ? 0.0f : a[k][s] * (k ? h[k ? k - 1 : 0][s] : hb[s]));
+                            a[k][s] = __builtin_amdgcn_exp2f(de[i] * A[s]);
+                            h[k][s] = __builtin_fmaf(a[k][s], begin ? 0.0f : k ? h[k ? k - 1 : 0][s] : hb[s], dx[i] * ahead.B(k)[s]);
                             sum = __builtin_fmaf(h[k][s], ahead.C(k)[s], sum);
                         }
                         part[i] = sum;
                     }
-                    raw[j] = quad_deal(part, q);
+                    raws[own * X::PITCH + 4 * j + q] = quad_deal(part, q);
                 }
             }
-            float outx[NB], outd[NB], outz[NB];
             Ahead<SL, true> ahead(lds + q * SL);
 #pragma unroll
             for (int j = NB - 1; j >= 0; --j) {
+                const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j), rk = X::four(rs, own, j);
                 float gB[4], dd[4], val[8 * SL];
 #pragma unroll
                 for (int i = 3; i >= 0; --i) {
                     const int k = 4 * j + i;
-                    const float de = quad_from(size[j], i), dx = quad_from(moved[j], i), rk = quad_from(r[j], i);
                     ahead.next(k, L, -1);
                     const bool begin = FRESH && (fresh >> k & 1);
                     gB[i] = dd[i] = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
-                        const float gk = __builtin_fmaf(rk, ahead.C(k)[s], ag[s]);
-                        val[2 * SL * i + s] = gk * dx;
-                        val[2 * SL * i + SL + s] = rk * h[k][s];
+                        const float gk = __builtin_fmaf(rk[i], ahead.C(k)[s], ag[s]);
+                        val[2 * SL * i + s] = gk * dx[i];
+                        val[2 * SL * i + SL + s] = rk[i] * h[k][s];
                         gB[i] = __builtin_fmaf(gk, ahead.B(k)[s], gB[i]);
-                        const float ga = gk * (begin ? 0.0f : a[k][s] * (k ? h[k ? k - 1 : 0][s] : hb[s]));
-                        dd[i] = __builtin_fmaf(ga, A[s], dd[i]);
-                        dA[s] = __builtin_fmaf(ga, de, dA[s]);
                         ag[s] = begin ? 0.0f : a[k][s] * gk;
+                        const float ga = begin ? 0.0f : ag[s] * (k ? h[k ? k - 1 : 0][s] : hb[s]);
+                        dd[i] = __builtin_fmaf(ga, A[s], dd[i]);
+                        dA[s] = __builtin_fmaf(ga, de[i], dA[s]);
                     }
                 }
-                float out[2 * SL];
-                channel_sums<2 * SL>(out, val);
-                // lanes of channel 0 of each row: step 4 j + 2 bit5 + bit4, states q SL ...
-                if ((lane & 12) == 0) {
-                    float *to = sums[buf][wave] + (4 * j + 2 * (lane >> 5) + (lane >> 4 & 1)) * PAIR + q * SL;
+                // a lane's sums: step 4 j + 2 bit3 + bit2, B or C by bit 4, half of its quad's states by bit 5
+                float out[SL / 2];
+                channel_sums<8 * SL>(out, val);
+                float *to = sums[buf][wave] + 4 * j * PAIR + share;
 #pragma unroll
-                    for (int s = 0; s < SL; ++s) { to[s] = out[s]; to[SP + s] = out[SL + s]; }
-                }
-                const float sB = quad_deal(gB, q), sd = quad_deal(dd, q) * (1.0f / LOG2E);
-                const bool live = t0 + 4 * j + q < len;
-                const float ddt = __builtin_fmaf(sB, xv[j], sd) * slope[j];
-                dbias += ddt; dskip = __builtin_fmaf(r[j], xv[j], dskip);
-                outx[j] = live ? __builtin_fmaf(sB, size[j], r[j] * skip) : 0.0f;
-                outd[j] = live ? ddt : 0.0f;
-                outz[j] = live ? zf[j] * __builtin_fmaf(skip, xv[j], raw[j]) : 0.0f;
+                for (int s = 0; s < SL / 2; ++s) to[s] = out[s];
+                sBs[own * X::PITCH + 4 * j + q] = quad_deal(gB, q);
+                sds[own * X::PITCH + 4 * j + q] = quad_deal(dd, q);
             }
-            dxa.store(outx, t0, q, TT, on);
-            dda.store(outd, t0, q, TT, on);
-            if (p.g.dz.p) dza.store(outz, t0, q, TT, on);
-            dxa.back(); dda.back(); dza.back();
         };
         if (fresh) pass(std::true_type()); else pass(std::false_type());
+        wave_order();
+        float raw[NB], sB[NB], sd[NB], dx[NB], ddt[NB], dz[NB];
+        X::get(raw, raws, cell);
+        X::get(sB, sBs, cell);
+        X::get(sd, sds, cell);
+#pragma unroll
+        for (int e = 0; e < NB; ++e) {
+            ddt[e] = __builtin_fmaf(sB[e], xv[e], sd[e] * (1.0f / LOG2E)) * slope[e];
+            dx[e] = some ? __builtin_fmaf(sB[e], size[e], r[e] * skip[e]) : 0.0f;
+            dz[e] = some ? zf[e] * __builtin_fmaf(skip[e], xv[e], raw[e]) : 0.0f;
+            ddt[e] = some ? ddt[e] : 0.0f;
+            dbias[e] += ddt[e];
+            dskip[e] = __builtin_fmaf(r[e], xv[e], dskip[e]);
+        }
+        const bool there = t0 + cell.step < TT;
+        dxa.store(dx, there, cell);
+        dda.store(ddt, there, cell);
+        dza.store(dz, there, cell);
+        dxa.back(); dda.back(); dza.back();
+        wave_order();
     }
     __syncthreads();
     leave(0, (chunks - 1) & 1);
-    dskip = quad_sum(dskip); dbias = quad_sum(dbias);
-    if (!on) return;
     float *out = param_part + (int64_t)n * D * (S + 2);
+    if (on)
 #pragma unroll
-    for (int s = 0; s < SL; ++s)
-        if (q * SL + s < S) {
-            out[(int64_t)d * S + q * SL + s] = dA[s];
-            if (p.g.dh_in) p.g.dh_in[((int64_t)n * D + d) * S + q * SL + s] = ag[s];
-        }
-    if (q == 0) { out[(int64_t)D * S + d] = dskip; out[(int64_t)D * (S + 1) + d] = dbias; }
+        for (int s = 0; s < SL; ++s)
+            if (q * SL + s < S) {
+                out[(int64_t)d * S + q * SL + s] = dA[s];
+                if (p.g.dh_in) p.g.dh_in[((int64_t)n * D + d) * S + q * SL + s] = ag[s];
+            }
+    // over the chunk's steps, which are other lanes
+#pragma unroll
+    for (int e = 0; e < NB; ++e) {
+#pragma unroll
+        for (int m = Cell<SL>::PER; m < 64; m *= 2) { dskip[e] += __shfl_xor(dskip[e], m); dbias[e] += __shfl_xor(dbias[e], m); }
+        if (cell.step == 0 && e < cell.count) { out[(int64_t)D * S + d0 + cell.channel + e] = dskip[e]; out[(int64_t)D * (S + 1) + d0 + cell.channel + e] = dbias[e]; }
+    }
 }
 
 // dB and dC from the workgroups' sums
@@ -635,32 +753,50 @@ int segments_of(const hts_scan_desc &d, int cus)
 }
 int64_t segment_floats(const hts_scan_desc &d, int count) { return count > 1 ? (int64_t)d.N * d.D * (padded(d.S) * (int64_t)count + (count - 1)) : 0; }
 
+// whether rows of these channels can be read four entries at a time
+template <typename T> bool wide(const hts_steps &s, int64_t N, int64_t cols) { return !s.p || ((uintptr_t)s.p % (4 * sizeof(T)) == 0 && s.st % 4 == 0 && (N == 1 || s.sn % 4 == 0) && cols % 4 == 0); }
+template <typename T> bool wide(const ScanOp &op, bool backward)
+{
+    const hts_scan_desc &d = op.d;
+    bool w = wide<T>(op.in.B, d.N, d.S) && wide<T>(op.in.C, d.N, d.S);
+    for (const hts_steps *s : {&op.in.x, &op.in.dt, &op.in.z}) w = w && wide<T>(*s, d.N, d.D / d.G);
+    if (!backward) return w && wide<T>(op.y, d.N, d.D / d.G);
+    for (const hts_steps *s : {&op.dy, &op.g.dx, &op.g.ddt, &op.g.dz}) w = w && wide<T>(*s, d.N, d.D / d.G);
+    return w;
+}
+
+template <typename T, int SL, bool WIDE> hipError_t scan(hts_seq_ctx &c, const ScanOp &op)
+{
+    const Places at = places(op.d);
+    Segments seg = {};
+    seg.count = segments_of(op.d, c.cus < 256 ? c.cus : 256);
+    seg.steps = (int)round_up(ceil_div(op.d.T, seg.count), Shape<SL>::L);
+    const int64_t states = (int64_t)op.d.N * op.d.D * Shape<SL>::SP, waves = (int64_t)at.waves * op.d.G * op.d.N;
+    if (seg.count > 1) {
+        seg.h_in = (float *)c.ws;
+        seg.state = seg.h_in + states;
+        seg.sum = seg.state + (seg.count - 1) * states;
+        hipLaunchKernelGGL((scan_kernel<T, SL, WIDE, true>), dim3((uint32_t)ceil_div(waves * (seg.count - 1), FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((scan_kernel<T, SL, WIDE, false>), dim3((uint32_t)ceil_div(waves * seg.count, FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
+    return hipGetLastError();
+}
+
 template <typename T, int SL> hipError_t run(hts_seq_ctx &c, const ScanOp &op, bool backward)
 {
     const Places at = places(op.d);
     if (!backward) {
-        if (op.d.T == 1) {
-            hipLaunchKernelGGL((step_kernel<T, SL>), dim3((uint32_t)ceil_div((int64_t)op.d.N * op.d.D, 64)), dim3(256), 0, c.stream, op);
-            return hipGetLastError();
-        }
-        Segments seg = {};
-        seg.count = segments_of(op.d, c.cus < 256 ? c.cus : 256);
-        seg.steps = (int)round_up(ceil_div(op.d.T, seg.count), Shape<SL>::L);
-        const int64_t states = (int64_t)op.d.N * op.d.D * Shape<SL>::SP, waves = (int64_t)at.waves * op.d.G * op.d.N;
-        if (seg.count > 1) {
-            seg.h_in = (float *)c.ws;
-            seg.state = seg.h_in + states;
-            seg.sum = seg.state + (seg.count - 1) * states;
-            hipLaunchKernelGGL((scan_kernel<T, SL, true>), dim3((uint32_t)ceil_div(waves * (seg.count - 1), FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
-        hipLaunchKernelGGL((scan_kernel<T, SL, false>), dim3((uint32_t)ceil_div(waves * seg.count, FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
+        if (op.d.T > 1) return wide<T>(op, false) ? scan<T, SL, true>(c, op) : scan<T, SL, false>(c, op);
+        hipLaunchKernelGGL((step_kernel<T, SL>), dim3((uint32_t)ceil_div((int64_t)op.d.N * op.d.D, 64)), dim3(256), 0, c.stream, op);
         return hipGetLastError();
     }
     const int blocks = blocks_of(op.d);
     float *pairs = (float *)c.ws, *params = pairs + pair_floats(op.d);
-    hipLaunchKernelGGL((scan_backward_kernel<T, SL>), dim3((uint32_t)((int64_t)blocks * op.d.G * op.d.N)), dim3(64 * BWD_WAVES), 0, c.stream, op, at, blocks, pairs, params);
+    const dim3 grid((uint32_t)((int64_t)blocks * op.d.G * op.d.N)), threads(64 * BWD_WAVES);
+    if (wide<T>(op, true)) hipLaunchKernelGGL((scan_backward_kernel<T, SL, true>), grid, threads, 0, c.stream, op, at, blocks, pairs, params);
+    else hipLaunchKernelGGL((scan_backward_kernel<T, SL, false>), grid, threads, 0, c.stream, op, at, blocks, pairs, params);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t width = (int64_t)op.d.T * op.d.N * op.d.G * Shape<SL>::PAIR;

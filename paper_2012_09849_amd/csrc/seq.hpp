@@ -81,33 +81,25 @@ __device__ __forceinline__ void softplus_f(float v, float &value, float &slope)
     slope = v >= 0.0f ? r : e * r;
 }
 
+// (the factors are held within finite bounds, so that infinities give the limits, 0 or 1 times themselves, without a branch; NaN comes through the others)
 template <int ACT> __device__ __forceinline__ float act_f(float v)
 {
     if constexpr (ACT == HTS_ACT_RELU) return v < 0.0f ? 0.0f : v;
-    if constexpr (ACT == HTS_ACT_SILU) return v == -__builtin_inff() ? 0.0f : v * sigmoid_f(v);
-    if constexpr (ACT == HTS_ACT_GELU) return v == -__builtin_inff() ? 0.0f : 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    if constexpr (ACT == HTS_ACT_SILU) return fmaxf(v, -1e4f) * sigmoid_f(v);
+    if constexpr (ACT == HTS_ACT_GELU) return 0.5f * fmaxf(v, -1e4f) * (1.0f + erff(v * 0.70710678118654752f));
     return v;
 }
 template <int ACT> __device__ __forceinline__ float act_slope(float v)
 {
+    const float w = fminf(fmaxf(v, -1e4f), 1e4f);
     if constexpr (ACT == HTS_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
     if constexpr (ACT == HTS_ACT_SILU) {
         const float s = sigmoid_f(v);
-        return __builtin_isinf(v) ? (v > 0.0f ? 1.0f : 0.0f) : s * (1.0f + v * (1.0f - s));
+        return s * __builtin_fmaf(w, 1.0f - s, 1.0f);
     }
-    if constexpr (ACT == HTS_ACT_GELU)
-        return __builtin_isinf(v) ? (v > 0.0f ? 1.0f : 0.0f) : 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * 0.39894228040143268f * exp_f(-0.5f * v * v);
+    if constexpr (ACT == HTS_ACT_GELU) return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + w * 0.39894228040143268f * exp_f(-0.5f * v * v);
     return 1.0f;
 }
-__device__ __forceinline__ float act_of(int act, float v)
-{
-    return act == HTS_ACT_RELU ? act_f<HTS_ACT_RELU>(v) : act == HTS_ACT_SILU ? act_f<HTS_ACT_SILU>(v) : act == HTS_ACT_GELU ? act_f<HTS_ACT_GELU>(v) : v;
-}
-__device__ __forceinline__ float slope_of(int act, float v)
-{
-    return act == HTS_ACT_RELU ? act_slope<HTS_ACT_RELU>(v) : act == HTS_ACT_SILU ? act_slope<HTS_ACT_SILU>(v) : act == HTS_ACT_GELU ? act_slope<HTS_ACT_GELU>(v) : 1.0f;
-}
-
 // V entries from memory, or one at a time where their address is no multiple of their size
 template <typename T, int V> struct Loaded { T e[V]; };
 template <typename T, int V> __device__ __forceinline__ Loaded<T, V> load_v(const T *p)
