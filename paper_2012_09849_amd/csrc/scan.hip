@@ -13,11 +13,12 @@
 namespace hts {
 namespace {
 
-template <int SL> struct Shape {
-    static constexpr int L = SL <= 4 ? 16 : SL == 8 ? 8 : 4;      // steps of a chunk; the backward pass keeps a chunk's states in registers
-    static constexpr int NB = L / 4, SP = 4 * SL, PAIR = 2 * SP;
-};
-constexpr int chunk_steps(int S) { return S <= 16 ? 16 : S <= 32 ? 8 : 4; }
+// L: steps of a chunk.  The backward pass keeps a chunk's states and factors in registers, 2 L SL of them: half as many steps for 16 states, which leaves
+// two wavefronts a SIMD
+template <int SL_, int L_> struct Shape { static constexpr int SL = SL_, L = L_, NB = L / 4, SP = 4 * SL, PAIR = 2 * SP; };
+template <int SL> using Forth = Shape<SL, SL <= 4 ? 16 : SL == 8 ? 8 : 4>;
+template <int SL> using Back = Shape<SL, SL <= 2 ? 16 : SL <= 8 ? 8 : 4>;
+constexpr int back_steps(int S) { return S <= 8 ? 16 : S <= 32 ? 8 : 4; }
 constexpr int padded(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : S <= 32 ? 32 : 64; }
 
 __device__ __forceinline__ float quad_xor1(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true)); }
@@ -37,6 +38,15 @@ __device__ __forceinline__ void wave_order()
 {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+}
+
+// a workgroup's LDS writes are there for its other wavefronts; unlike __syncthreads() it does not wait for what is on its way to or from memory
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);          // vmcnt 63, expcnt 7, lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 struct Places { int per_group, waves; };          // channels of a group, wavefronts (16 channels) of a group
@@ -119,8 +129,8 @@ template <typename T, int V, bool WIDE> __device__ __forceinline__ void put_raw(
 }
 
 // The order of memory: lane = (step of the chunk, V neighbouring ones of the wavefront's 16 channels)
-template <int SL> struct Cell {
-    static constexpr int V = Shape<SL>::NB, PER = 16 / V;
+template <class H> struct Cell {
+    static constexpr int V = H::NB, PER = 16 / V;
     int step, channel, count;          // count: of the V channels that exist
     __device__ __forceinline__ void open(int lane, int channels)
     {
@@ -128,20 +138,20 @@ template <int SL> struct Cell {
         count = max(0, min(V, channels - channel));
     }
 };
-template <typename T, int SL, bool WIDE> struct Track : Walk {
-    static constexpr int V = Shape<SL>::NB;
+template <typename T, class H, bool WIDE> struct Track : Walk {
+    static constexpr int V = H::NB;
     uint32_t lane;
-    __device__ __forceinline__ void open(const hts_steps &a, int n, int first, const Cell<SL> &c, int t0)
+    __device__ __forceinline__ void open(const hts_steps &a, int n, int first, const Cell<H> &c, int t0)
     {
-        Walk::open(a.p, (n * a.sn + first) * (int64_t)sizeof(T), a.st * (int64_t)sizeof(T), t0, Shape<SL>::L);
+        Walk::open(a.p, (n * a.sn + first) * (int64_t)sizeof(T), a.st * (int64_t)sizeof(T), t0, H::L);
         lane = a.p && c.count > 0 ? (uint32_t)c.step * step + (uint32_t)c.channel * (uint32_t)sizeof(T) : NOWHERE;
     }
-    __device__ __forceinline__ void load(Raw<T, V, WIDE> &v, bool live, const Cell<SL> &c) const { v.load(reach(base), live ? lane : NOWHERE, live ? c.count : 0); }
-    __device__ __forceinline__ void store(const float (&v)[V], bool some, const Cell<SL> &c) const { put_raw<T, V, WIDE>(reach(base), some ? lane : NOWHERE, some ? c.count : 0, v); }
+    __device__ __forceinline__ void load(Raw<T, V, WIDE> &v, bool live, const Cell<H> &c) const { v.load(reach(base), live ? lane : NOWHERE, live ? c.count : 0); }
+    __device__ __forceinline__ void store(const float (&v)[V], bool some, const Cell<H> &c) const { put_raw<T, V, WIDE>(reach(base), some ? lane : NOWHERE, some ? c.count : 0, v); }
 };
 // B or C of a chunk: 4 neighbouring states of a step a lane
-template <typename T, int SL, bool WIDE> struct Half : Walk {
-    static constexpr int SP = Shape<SL>::SP, L = Shape<SL>::L;
+template <typename T, class H, bool WIDE> struct Half : Walk {
+    static constexpr int SP = H::SP, L = H::L;
     static_assert(L * SP <= 256, "lanes");
     uint32_t lane;
     int at, count, row;                // its step, how many of the 4 states exist, its place in LDS
@@ -152,7 +162,7 @@ template <typename T, int SL, bool WIDE> struct Half : Walk {
         at = tid * 4 / SP;
         count = at < L ? max(0, min(4, S - s)) : 0;
         lane = count > 0 ? (uint32_t)at * step + (uint32_t)s * (uint32_t)sizeof(T) : NOWHERE;
-        row = at * Shape<SL>::PAIR + s;
+        row = at * H::PAIR + s;
     }
     __device__ __forceinline__ void load(Raw<T, 4, WIDE> &v, int t0, int len) const { v.load(reach(base), t0 + at < len ? lane : NOWHERE, t0 + at < len ? count : 0); }
     __device__ __forceinline__ void put(const Raw<T, 4, WIDE> &v, float *lds) const
@@ -176,14 +186,14 @@ template <int L> struct Begins : Walk {
     static __device__ __forceinline__ uint32_t mask(uint32_t v) { return (uint32_t)__ballot(v != 0) & ((1u << L) - 1); }
 };
 // Between the two orders: [16 channels][L steps] of binary32, a row a multiple of 16 bytes long that spreads the channels over the banks
-template <int SL> struct Swap {
-    static constexpr int V = Shape<SL>::NB, L = Shape<SL>::L, PITCH = L + 4, SIZE = 16 * PITCH;
-    static __device__ __forceinline__ void put(float *lds, const Cell<SL> &c, const float (&v)[V])
+template <class H> struct Swap {
+    static constexpr int V = H::NB, L = H::L, PITCH = L + 4, SIZE = 16 * PITCH;
+    static __device__ __forceinline__ void put(float *lds, const Cell<H> &c, const float (&v)[V])
     {
 #pragma unroll
         for (int e = 0; e < V; ++e) lds[(c.channel + e) * PITCH + c.step] = v[e];
     }
-    static __device__ __forceinline__ void get(float (&v)[V], const float *lds, const Cell<SL> &c)
+    static __device__ __forceinline__ void get(float (&v)[V], const float *lds, const Cell<H> &c)
     {
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = lds[(c.channel + e) * PITCH + c.step];
@@ -196,10 +206,21 @@ template <int SL> struct Kept : Walk {
     uint32_t lane;
     __device__ __forceinline__ void open(const float *p, int64_t N, int n, int D, int first, int channel, int q, int chunk)
     {
-        Walk::open(p, ((int64_t)n * D + first) * Shape<SL>::SP * 4, N * D * Shape<SL>::SP * 4, chunk, 1);
-        lane = (uint32_t)((channel - first) * Shape<SL>::SP + q * SL) * 4u;
+        Walk::open(p, ((int64_t)n * D + first) * 4 * SL * 4, N * D * 4 * SL * 4, chunk, 1);
+        lane = (uint32_t)((channel - first) * 4 * SL + q * SL) * 4u;
     }
-    __device__ __forceinline__ float *at() const { return (float *)(const_cast<char *>(base) + lane); }
+    __device__ __forceinline__ void store(const float (&v)[SL], bool some) const
+    {
+        typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+        typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+        const __amdgpu_buffer_rsrc_t dst = reach(base);
+        const int to = some ? (int)lane : (int)NOWHERE;
+        auto w = [&](int i) { return __float_as_uint(v[i]); };
+        if constexpr (SL == 2) __builtin_amdgcn_raw_buffer_store_b64(u2{w(0), w(1)}, dst, to, 0, 0);
+        else
+#pragma unroll
+            for (int i = 0; i < SL; i += 4) __builtin_amdgcn_raw_buffer_store_b128(u4{w(i), w(i + 1), w(i + 2), w(i + 3)}, dst, to, 4 * i, 0);
+    }
     // zeros where there is no such chunk
     __device__ __forceinline__ void load(float (&v)[SL], bool some) const
     {
@@ -225,8 +246,8 @@ template <int SL> __device__ __forceinline__ void read_states(float (&v)[SL], co
 }
 
 // B and C of the steps to come, read from LDS two steps ahead
-template <int SL, bool BOTH> struct Ahead {
-    static constexpr int DEPTH = 2, RING = DEPTH + 1, PAIR = Shape<SL>::PAIR, SP = Shape<SL>::SP;
+template <class H, bool BOTH> struct Ahead {
+    static constexpr int DEPTH = 2, RING = DEPTH + 1, PAIR = H::PAIR, SP = H::SP, SL = H::SL, L = H::L;
     const float *lds;
     float b[RING][SL], c[RING][SL];
     __device__ __forceinline__ explicit Ahead(const float *at) : lds(at) {}
@@ -235,8 +256,8 @@ template <int SL, bool BOTH> struct Ahead {
         read_states<SL>(b[t % RING], lds + t * PAIR);
         if (BOTH) read_states<SL>(c[t % RING], lds + t * PAIR + SP);
     }
-    // before step t of L, in the order of `way`
-    __device__ __forceinline__ void next(int t, int L, int way)
+    // before step t, in the order of `way`
+    __device__ __forceinline__ void next(int t, int way)
     {
         if (t == (way > 0 ? 0 : L - 1))
 #pragma unroll
@@ -249,19 +270,19 @@ template <int SL, bool BOTH> struct Ahead {
 
 // A long sequence of few channels is cut into segments that are worked on at the same time: a first pass leaves each segment's last state, begun
 // from nothing (the first one from h_in), and its sum of step sizes; exp(sum A) is then what the state before the segment counts at its end.  The
-// second pass begins every segment from the states that these give, in order, so the result does not depend on who comes first.
+// second pass begins every segment from the states that these give, in order, so the result does not depend on who comes first.  Backward the same with
+// the gradient of the state, from the last segment to the first.
 struct Segments {
     int count, steps;                  // steps: whole chunks
-    float *state, *sum;                // [count - 1][N][D][SP], [count - 1][N][D]: a sum is NaN where an episode begins in the segment and nothing before it counts
-    float *h_in;                       // [N][D][SP]: h_in once more, since h_out may be h_in
+    float *state, *sum;                // [segment][N][D][SP], [segment][N][D]: a sum is NaN where an episode begins in the segment and nothing before it counts
+    float *h_in;                       // forward: [N][D][SP]: h_in once more, since h_out may be h_in
 };
-template <int SL> __device__ __forceinline__ int64_t state_at(int64_t row, int d, int D, int q) { return (row * D + d) * Shape<SL>::SP + q * SL; }
-// the state before segment k; NaN: a real sum that is NaN gives NaN states in the segment's last one too
-template <int SL> __device__ __forceinline__ void state_before(float (&h)[SL], const Segments &seg, int k, int n, int N, int d, int D, int q, const float (&A)[SL])
+template <int SL> __device__ __forceinline__ int64_t state_at(int64_t row, int d, int D, int q) { return (row * D + d) * 4 * SL + q * SL; }
+// h over what the segments from `first` to before `last` (in steps of `way`) do to it.  (A real sum that is NaN gives NaN states of its own too.)
+template <int SL> __device__ __forceinline__ void over_segments(float (&h)[SL], const Segments &seg, int first, int last, int way, int n, int N, int d, int D, int q, const float (&A)[SL])
 {
-    read_states<SL>(h, k == 0 ? seg.h_in + state_at<SL>(n, d, D, q) : seg.state + state_at<SL>(n, d, D, q));
 #pragma unroll 4
-    for (int i = 1; i < k; ++i) {
+    for (int i = first; i != last; i += way) {
         const float sum = seg.sum[((int64_t)i * N + n) * D + d];
         float own[SL];
         read_states<SL>(own, seg.state + state_at<SL>((int64_t)i * N + n, d, D, q));
@@ -276,9 +297,9 @@ constexpr int FWD_WAVES = 4;
 template <typename T, int SL, bool WIDE, bool STATES>
 __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, const Places at, const Segments seg)
 {
-    typedef Shape<SL> H;
-    typedef Swap<SL> X;
-    constexpr int L = H::L, NB = H::NB, SP = H::SP;
+    typedef Forth<SL> H;
+    typedef Swap<H> X;
+    constexpr int L = H::L, NB = H::NB, SP = H::SP, KEEP = Back<SL>::L;
     __shared__ __attribute__((aligned(16))) float shared[FWD_WAVES][L * H::PAIR + 3 * X::SIZE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = p.d.D, S = p.d.S, N = p.d.N;
     const int per = at.waves * p.d.G;                                   // wavefronts of a sequence's segment
@@ -288,12 +309,12 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
     const int d0 = g * at.per_group + c, d = d0 + own, len = length_of(p.in.lengths, n, p.d.T);
     const bool on = c + own < at.per_group;
     const int first = k * seg.steps, end = min(p.d.T, first + seg.steps), live = min(len, end);
-    Cell<SL> cell;
+    Cell<H> cell;
     cell.open(lane, at.per_group - c);
-    Track<T, SL, WIDE> xa, da, za, ya;
+    Track<T, H, WIDE> xa, da, za, ya;
     Kept<SL> kept;
     xa.open(p.in.x, n, d0, cell, first); da.open(p.in.dt, n, d0, cell, first);
-    if (!STATES) { za.open(p.in.z, n, d0, cell, first); ya.open(p.y, n, d0, cell, first); kept.open(p.states_out, N, n, D, d0, d, q, first / L); }
+    if (!STATES) { za.open(p.in.z, n, d0, cell, first); ya.open(p.y, n, d0, cell, first); kept.open(p.states_out, N, n, D, d0, d, q, first / KEEP); }
     float skip[NB], bias[NB], sum[NB];
 #pragma unroll
     for (int e = 0; e < NB; ++e) {
@@ -311,8 +332,11 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
         h[s] = on && i < S && p.in.h_in && (STATES ? k == 0 : seg.count == 1) ? p.in.h_in[((int64_t)n * D + d) * S + i] : 0.0f;
         if (STATES && k == 0 && on) seg.h_in[state_at<SL>(n, d, D, q) + s] = h[s];
     }
-    if (!STATES && seg.count > 1 && on) state_before<SL>(h, seg, k, n, N, d, D, q, A);
-    Half<T, SL, WIDE> bs, cs;
+    if (!STATES && seg.count > 1 && on) {
+        read_states<SL>(h, k == 0 ? seg.h_in + state_at<SL>(n, d, D, q) : seg.state + state_at<SL>(n, d, D, q));
+        over_segments<SL>(h, seg, 1, max(k, 1), 1, n, N, d, D, q, A);
+    }
+    Half<T, H, WIDE> bs, cs;
     Begins<L> begins;
     bs.open(p.in.B, n, g, S, lane, first);
     if (!STATES) cs.open(p.in.C, n, g, S, lane, first);
@@ -361,14 +385,10 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
         if (STATES) cut |= fresh != 0;
         wave_order();
         fetch(t0 + L);
-        if (!STATES && p.states_out && on) {
-            float *out = kept.at();
-#pragma unroll
-            for (int s = 0; s < SL; ++s) out[s] = h[s];
-        }
+        const bool keep = !STATES && p.states_out;
         // twice: chunks in which no episode begins, most of them, reset nothing
         auto pass = [&](auto has) {
-            Ahead<SL, !STATES> ahead(pairs + q * SL);
+            Ahead<H, !STATES> ahead(pairs + q * SL);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j);
@@ -376,7 +396,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = 4 * j + i;
-                    ahead.next(t, L, +1);
+                    ahead.next(t, +1);
+                    if (t % KEEP == 0 && keep) { kept.store(h, on && t0 + t < p.d.T); kept.forth(); }
                     if (decltype(has)::value && (fresh >> t & 1))
 #pragma unroll
                         for (int s = 0; s < SL; ++s) h[s] = 0.0f;
@@ -400,7 +421,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
 #pragma unroll
             for (int e = 0; e < NB; ++e) y[e] = some ? __builtin_fmaf(skip[e], xv[e], y[e]) * gate[e] : 0.0f;
             ya.store(y, t0 + cell.step < p.d.T, cell);
-            ya.forth(); kept.forth();
+            ya.forth();
         }
     }
     if (STATES) {
@@ -413,7 +434,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
 #pragma unroll
         for (int e = 0; e < NB; ++e) {
 #pragma unroll
-            for (int m = Cell<SL>::PER; m < 64; m *= 2) sum[e] += __shfl_xor(sum[e], m);
+            for (int m = Cell<H>::PER; m < 64; m *= 2) sum[e] += __shfl_xor(sum[e], m);
             if (cell.step == 0 && e < cell.count) seg.sum[((int64_t)k * N + n) * D + d0 + cell.channel + e] = cut ? __builtin_nanf("") : sum[e];
         }
     } else if (on && p.h_out && k == seg.count - 1)
@@ -426,7 +447,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
 template <typename T, int SL>
 __global__ __launch_bounds__(256) void step_kernel(const ScanOp p)
 {
-    constexpr int SP = Shape<SL>::SP;
+    constexpr int SP = 4 * SL;
     const int D = p.d.D, S = p.d.S, q = threadIdx.x & 3;
     const int64_t row = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 2);
     if (row >= (int64_t)p.d.N * D) return;                              // a quad leaves together
@@ -512,27 +533,27 @@ constexpr int BWD_WAVES = 4;
 // dB and dC of a workgroup's channels are added in LDS in a fixed order and leave as a partial sum a workgroup; dA, dskip and ddt_bias stay in
 // registers for the whole sequence.  At an episode's first step the products with a are 0, also where the other factor is not finite.
 template <typename T, int SL, bool WIDE>
-__global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const ScanOp p, const Places at, const int blocks, float *pair_part, float *param_part)
+__global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const ScanOp p, const Places at, const Segments seg, const int blocks, float *pair_part, float *param_part)
 {
-    typedef Shape<SL> H;
-    typedef Swap<SL> X;
+    typedef Back<SL> H;
+    typedef Swap<H> X;
     constexpr int L = H::L, NB = H::NB, SP = H::SP, PAIR = H::PAIR, THREADS = 64 * BWD_WAVES;
     __shared__ __attribute__((aligned(16))) float pairs[2][L * PAIR];
     __shared__ __attribute__((aligned(16))) float sums[2][BWD_WAVES][L * PAIR];
     __shared__ __attribute__((aligned(16))) float swaps[BWD_WAVES][6 * X::SIZE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 3, own = lane >> 2;
-    const int block = blockIdx.x % blocks, g = blockIdx.x / blocks % p.d.G, n = blockIdx.x / blocks / p.d.G;
+    const int block = blockIdx.x % blocks, g = blockIdx.x / blocks % p.d.G, nk = blockIdx.x / blocks / p.d.G, n = nk % p.d.N, k = nk / p.d.N;
     const int c = (block * BWD_WAVES + wave) * 16, D = p.d.D, S = p.d.S, TT = p.d.T, len = length_of(p.in.lengths, n, TT);
     const bool on = c + own < at.per_group;
     const int d0 = g * at.per_group + c, d = d0 + own;
-    const int chunks = (TT + L - 1) / L, last = (chunks - 1) * L;
-    Cell<SL> cell;
+    const int lowest = k * seg.steps / L, highest = (min(TT, (k + 1) * seg.steps) + L - 1) / L - 1, last = highest * L;      // the segment's chunks
+    Cell<H> cell;
     cell.open(lane, at.per_group - c);
-    Track<T, SL, WIDE> xa, da, za, ga, dxa, dda, dza;
+    Track<T, H, WIDE> xa, da, za, ga, dxa, dda, dza;
     xa.open(p.in.x, n, d0, cell, last); da.open(p.in.dt, n, d0, cell, last); za.open(p.in.z, n, d0, cell, last); ga.open(p.dy, n, d0, cell, last);
     dxa.open(p.g.dx, n, d0, cell, last); dda.open(p.g.ddt, n, d0, cell, last); dza.open(p.g.dz, n, d0, cell, last);
     Kept<SL> kept;
-    kept.open(p.states, p.d.N, n, D, d0, d, q, chunks - 1);
+    kept.open(p.states, p.d.N, n, D, d0, d, q, highest);
     float skip[NB], bias[NB], dskip[NB], dbias[NB];
 #pragma unroll
     for (int e = 0; e < NB; ++e) {
@@ -546,19 +567,23 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
     for (int s = 0; s < SL; ++s) {
         const int i = q * SL + s;
         A[s] = on && i < S ? p.in.A[(int64_t)d * S + i] * LOG2E : 0.0f;
-        ag[s] = on && i < S && p.dh_out ? p.dh_out[((int64_t)n * D + d) * S + i] : 0.0f;
+        ag[s] = on && i < S && p.dh_out && k == seg.count - 1 ? p.dh_out[((int64_t)n * D + d) * S + i] : 0.0f;
         dA[s] = 0.0f;
     }
+    if (on && k < seg.count - 1) {
+        read_states<SL>(ag, seg.state + state_at<SL>((int64_t)(seg.count - 1) * p.d.N + n, d, D, q));
+        over_segments<SL>(ag, seg, seg.count - 2, k, -1, n, p.d.N, d, D, q, A);
+    }
     // the workgroup's first wavefront brings B, its second C
-    Half<T, SL, WIDE> ps;
+    Half<T, H, WIDE> ps;
     ps.open(wave == 1 ? p.in.C : p.in.B, n, g, S, lane, last);
     if (wave > 1) ps.lane = NOWHERE, ps.count = 0;
     Begins<L> begins;
     begins.open(p.in.starts, n, p.d.N, lane, last);
     struct { Raw<T, NB, WIDE> x, dt, z, dy; Raw<T, 4, WIDE> pair; uint32_t begins; float h[SL]; } in;
-    auto fetch = [&](int chunk) {          // (there is nothing to load before the first chunk)
+    auto fetch = [&](int chunk) {          // (there is nothing to load before the segment's first chunk)
         __builtin_amdgcn_sched_barrier(0);
-        const int t0 = chunk * L, live = chunk >= 0 ? len : t0;
+        const int t0 = chunk * L, live = chunk >= lowest ? len : t0;
         const bool some = t0 + cell.step < live;
         begins.load(in.begins, t0, live, lane);
         xa.load(in.x, some, cell);
@@ -566,7 +591,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
         ga.load(in.dy, some, cell);
         za.load(in.z, some, cell);
         ps.load(in.pair, t0, live);
-        kept.load(in.h, on && chunk >= 0);
+        kept.load(in.h, on && chunk >= lowest);
         xa.back(); da.back(); za.back(); ga.back(); ps.back(); begins.back(); kept.back();
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -585,8 +610,8 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
     };
     float *sizes = swaps[wave], *moves = sizes + X::SIZE, *rs = moves + X::SIZE, *raws = rs + X::SIZE, *sBs = raws + X::SIZE, *sds = sBs + X::SIZE;
     const int share = (2 * (lane >> 3 & 1) + (lane >> 2 & 1)) * PAIR + (lane >> 4 & 1) * SP + q * SL + (lane >> 5) * (SL / 2);
-    fetch(chunks - 1);
-    for (int chunk = chunks - 1, buf = 0; chunk >= 0; --chunk, buf ^= 1) {
+    fetch(highest);
+    for (int chunk = highest, buf = 0; chunk >= lowest; --chunk, buf ^= 1) {
         const int t0 = chunk * L;
         const bool some = t0 + cell.step < len;
         if (wave < 2) ps.put(in.pair, pairs[buf] + wave * SP);
@@ -613,56 +638,56 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
 #pragma unroll
         for (int s = 0; s < SL; ++s) hb[s] = in.h[s];
         const uint32_t fresh = Begins<L>::mask(in.begins);
-        __syncthreads();
+        lds_barrier();
         fetch(chunk - 1);
-        if (chunk < chunks - 1) leave(chunk + 1, buf ^ 1);
+        if (chunk < highest) leave(chunk + 1, buf ^ 1);
         const float *lds = pairs[buf];
         // twice: chunks in which no episode begins, most of them, select nothing
         auto pass = [&](auto has) {
             constexpr bool FRESH = decltype(has)::value;
             float a[L][SL], h[L][SL];
             {
-                Ahead<SL, true> ahead(lds + q * SL);
+                Ahead<H, true> ahead(lds + q * SL);
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
                     const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j);
                     float part[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int k = 4 * j + i;
-                        ahead.next(k, L, +1);
-                        const bool begin = FRESH && (fresh >> k & 1);
+                        const int t = 4 * j + i;
+                        ahead.next(t, +1);
+                        const bool begin = FRESH && (fresh >> t & 1);
                         float sum = 0.0f;
 #pragma unroll
                         for (int s = 0; s < SL; ++s) {
-                            a[k][s] = __builtin_amdgcn_exp2f(de[i] * A[s]);
-                            h[k][s] = __builtin_fmaf(a[k][s], begin ? 0.0f : k ? h[k ? k - 1 : 0][s] : hb[s], dx[i] * ahead.B(k)[s]);
-                            sum = __builtin_fmaf(h[k][s], ahead.C(k)[s], sum);
+                            a[t][s] = __builtin_amdgcn_exp2f(de[i] * A[s]);
+                            h[t][s] = __builtin_fmaf(a[t][s], begin ? 0.0f : t ? h[t ? t - 1 : 0][s] : hb[s], dx[i] * ahead.B(t)[s]);
+                            sum = __builtin_fmaf(h[t][s], ahead.C(t)[s], sum);
                         }
                         part[i] = sum;
                     }
                     raws[own * X::PITCH + 4 * j + q] = quad_deal(part, q);
                 }
             }
-            Ahead<SL, true> ahead(lds + q * SL);
+            Ahead<H, true> ahead(lds + q * SL);
 #pragma unroll
             for (int j = NB - 1; j >= 0; --j) {
                 const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j), rk = X::four(rs, own, j);
                 float gB[4], dd[4], val[8 * SL];
 #pragma unroll
                 for (int i = 3; i >= 0; --i) {
-                    const int k = 4 * j + i;
-                    ahead.next(k, L, -1);
-                    const bool begin = FRESH && (fresh >> k & 1);
+                    const int t = 4 * j + i;
+                    ahead.next(t, -1);
+                    const bool begin = FRESH && (fresh >> t & 1);
                     gB[i] = dd[i] = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
-                        const float gk = __builtin_fmaf(rk[i], ahead.C(k)[s], ag[s]);
+                        const float gk = __builtin_fmaf(rk[i], ahead.C(t)[s], ag[s]);
                         val[2 * SL * i + s] = gk * dx[i];
-                        val[2 * SL * i + SL + s] = rk[i] * h[k][s];
-                        gB[i] = __builtin_fmaf(gk, ahead.B(k)[s], gB[i]);
-                        ag[s] = begin ? 0.0f : a[k][s] * gk;
-                        const float ga = begin ? 0.0f : ag[s] * (k ? h[k ? k - 1 : 0][s] : hb[s]);
+                        val[2 * SL * i + SL + s] = rk[i] * h[t][s];
+                        gB[i] = __builtin_fmaf(gk, ahead.B(t)[s], gB[i]);
+                        ag[s] = begin ? 0.0f : a[t][s] * gk;
+                        const float ga = begin ? 0.0f : ag[s] * (t ? h[t ? t - 1 : 0][s] : hb[s]);
                         dd[i] = __builtin_fmaf(ga, A[s], dd[i]);
                         dA[s] = __builtin_fmaf(ga, de[i], dA[s]);
                     }
@@ -699,22 +724,129 @@ __global__ __launch_bounds__(64 * BWD_WAVES) void scan_backward_kernel(const Sca
         dxa.back(); dda.back(); dza.back();
         wave_order();
     }
-    __syncthreads();
-    leave(0, (chunks - 1) & 1);
-    float *out = param_part + (int64_t)n * D * (S + 2);
+    lds_barrier();
+    leave(lowest, (highest - lowest) & 1);
+    float *out = param_part + (int64_t)nk * D * (S + 2);
     if (on)
 #pragma unroll
         for (int s = 0; s < SL; ++s)
             if (q * SL + s < S) {
                 out[(int64_t)d * S + q * SL + s] = dA[s];
-                if (p.g.dh_in) p.g.dh_in[((int64_t)n * D + d) * S + q * SL + s] = ag[s];
+                if (p.g.dh_in && k == 0) p.g.dh_in[((int64_t)n * D + d) * S + q * SL + s] = ag[s];
             }
     // over the chunk's steps, which are other lanes
 #pragma unroll
     for (int e = 0; e < NB; ++e) {
 #pragma unroll
-        for (int m = Cell<SL>::PER; m < 64; m *= 2) { dskip[e] += __shfl_xor(dskip[e], m); dbias[e] += __shfl_xor(dbias[e], m); }
+        for (int m = Cell<H>::PER; m < 64; m *= 2) { dskip[e] += __shfl_xor(dskip[e], m); dbias[e] += __shfl_xor(dbias[e], m); }
         if (cell.step == 0 && e < cell.count) { out[(int64_t)D * S + d0 + cell.channel + e] = dskip[e]; out[(int64_t)D * (S + 1) + d0 + cell.channel + e] = dbias[e]; }
+    }
+}
+
+// The first pass over segments, from the last to the second: the gradient that a segment's own outputs (and, the last one, dh_out) give to the state
+// before it
+template <typename T, int SL, bool WIDE>
+__global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const ScanOp p, const Places at, const Segments seg)
+{
+    typedef Forth<SL> H;
+    typedef Swap<H> X;
+    constexpr int L = H::L, NB = H::NB, SP = H::SP;
+    __shared__ __attribute__((aligned(16))) float shared[FWD_WAVES][L * H::PAIR + 2 * X::SIZE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = p.d.D, S = p.d.S, N = p.d.N;
+    const int per = at.waves * p.d.G;
+    const uint32_t task = blockIdx.x * FWD_WAVES + wave, row = task / per, in_row = task % per;
+    if (row >= (uint32_t)(N * (seg.count - 1))) return;
+    const int k = row / N + 1, n = row % N, g = in_row / at.waves, c = in_row % at.waves * 16, q = lane & 3, own = lane >> 2;
+    const int d0 = g * at.per_group + c, d = d0 + own, len = length_of(p.in.lengths, n, p.d.T);
+    const bool on = c + own < at.per_group;
+    const int first = k * seg.steps, last = (min(p.d.T, first + seg.steps) + L - 1) / L * L - L;
+    Cell<H> cell;
+    cell.open(lane, at.per_group - c);
+    Track<T, H, WIDE> da, za, ga;
+    da.open(p.in.dt, n, d0, cell, last); za.open(p.in.z, n, d0, cell, last); ga.open(p.dy, n, d0, cell, last);
+    float bias[NB], sum[NB];
+#pragma unroll
+    for (int e = 0; e < NB; ++e) {
+        bias[e] = e < cell.count && p.in.dt_bias ? p.in.dt_bias[d0 + cell.channel + e] : 0.0f;
+        sum[e] = 0.0f;
+    }
+    float A[SL], ag[SL];
+    bool cut = false;
+#pragma unroll
+    for (int s = 0; s < SL; ++s) {
+        const int i = q * SL + s;
+        A[s] = on && i < S ? p.in.A[(int64_t)d * S + i] * LOG2E : 0.0f;
+        ag[s] = on && i < S && p.dh_out && k == seg.count - 1 ? p.dh_out[((int64_t)n * D + d) * S + i] : 0.0f;
+    }
+    Half<T, H, WIDE> cs;
+    Begins<L> begins;
+    cs.open(p.in.C, n, g, S, lane, last);
+    begins.open(p.in.starts, n, N, lane, last);
+    struct { Raw<T, NB, WIDE> dt, z, dy; Raw<T, 4, WIDE> c; uint32_t begins; } in;
+    auto fetch = [&](int t0) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int live = t0 >= first ? len : t0;
+        const bool some = t0 + cell.step < live;
+        begins.load(in.begins, t0, live, lane);
+        da.load(in.dt, some, cell);
+        za.load(in.z, some, cell);
+        ga.load(in.dy, some, cell);
+        cs.load(in.c, t0, live);
+        da.back(); za.back(); ga.back(); cs.back(); begins.back();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    float *pairs = shared[wave], *sizes = pairs + L * H::PAIR, *rs = sizes + X::SIZE;
+    fetch(last);
+    for (int t0 = last; t0 >= first; t0 -= L) {
+        const bool some = t0 + cell.step < len;
+        float size[NB], r[NB];
+        wave_order();
+        cs.put(in.c, pairs);
+        const uint32_t fresh = Begins<L>::mask(in.begins);
+#pragma unroll
+        for (int e = 0; e < NB; ++e) {
+            const float v = in.dt[e] + bias[e], open = act_f<HTS_ACT_SILU>(in.z[e]);
+            float soft, slope;
+            softplus_f(v, soft, slope);
+            size[e] = some ? p.d.softplus ? soft : v : 0.0f;
+            r[e] = in.dy[e] * (p.in.z.p ? open : 1.0f);
+            sum[e] += size[e];
+        }
+        X::put(sizes, cell, size);
+        X::put(rs, cell, r);
+        cut |= fresh != 0;
+        wave_order();
+        fetch(t0 - L);
+        auto pass = [&](auto has) {
+            Ahead<H, false> ahead(pairs + q * SL);
+#pragma unroll
+            for (int j = NB - 1; j >= 0; --j) {
+                const f32x4 de = X::four(sizes, own, j), rk = X::four(rs, own, j);
+#pragma unroll
+                for (int i = 3; i >= 0; --i) {
+                    const int t = 4 * j + i;
+                    ahead.next(t, -1);
+                    const bool begin = decltype(has)::value && (fresh >> t & 1);
+#pragma unroll
+                    for (int s = 0; s < SL; ++s) {
+                        const float gk = __builtin_fmaf(rk[i], ahead.B(t)[s], ag[s]);
+                        ag[s] = begin ? 0.0f : __builtin_amdgcn_exp2f(de[i] * A[s]) * gk;
+                    }
+                }
+            }
+        };
+        if (fresh) pass(std::true_type()); else pass(std::false_type());
+    }
+    if (on) {
+        float *out = seg.state + state_at<SL>((int64_t)k * N + n, d, D, q);
+#pragma unroll
+        for (int s = 0; s < SL; ++s) out[s] = ag[s];
+    }
+#pragma unroll
+    for (int e = 0; e < NB; ++e) {
+#pragma unroll
+        for (int m = Cell<H>::PER; m < 64; m *= 2) sum[e] += __shfl_xor(sum[e], m);
+        if (cell.step == 0 && e < cell.count) seg.sum[((int64_t)k * N + n) * D + d0 + cell.channel + e] = cut ? __builtin_nanf("") : sum[e];
     }
 }
 
@@ -735,23 +867,40 @@ __global__ __launch_bounds__(256) void pair_sum_kernel(const ScanOp p, const int
 
 Places places(const hts_scan_desc &d) { const int per = d.D / d.G; return Places{per, (int)ceil_div(per, 16)}; }
 int blocks_of(const hts_scan_desc &d) { return (int)ceil_div(places(d).waves, BWD_WAVES); }
-int64_t pair_floats(const hts_scan_desc &d) { return round_up((int64_t)blocks_of(d) * d.T * d.N * d.G * 2 * padded(d.S), 64); }
-int64_t param_floats(const hts_scan_desc &d) { return (int64_t)d.N * d.D * (d.S + 2); }
 
-// Segments of a sequence: where its wavefronts leave most units idle, as many as give two to a SIMD, of 64 steps at least.  The first pass costs
-// four fifths of the second.
+// Segments of a sequence: where its wavefronts leave units idle, as many as give two to a SIMD, of 64 steps at least, in whole chunks of either direction.
+// Forward the first pass costs two thirds of the second, so that up to three segments gain nothing; backward a fifth, and a lone wavefront waits for itself a third of
+// its time.  (On fewer compute units than 256 there are fewer segments: the workspace is for those.)
 constexpr int MOST_SEGMENTS = 64;
-int segments_of(const hts_scan_desc &d, int cus)
+int segments_of(const hts_scan_desc &d, int cus, bool backward)
 {
-    const int64_t waves = (int64_t)places(d).waves * d.G * d.N, units = 4ll * cus;
-    if (2 * waves > units) return 1;
+    const int64_t waves = (int64_t)places(d).waves * d.G * d.N, units = 4ll * (cus < 256 ? cus : 256);
     int64_t count = 2 * units / waves;
     if (count > d.T / 64) count = d.T / 64;
     if (count > MOST_SEGMENTS) count = MOST_SEGMENTS;
-    if (count < 3) return 1;           // two passes over halves gain nothing
-    return (int)ceil_div(d.T, round_up(ceil_div(d.T, count), chunk_steps(d.S)));
+    if (count < (backward ? 2 : 4)) return 1;
+    return (int)ceil_div(d.T, round_up(ceil_div(d.T, count), 16));
 }
-int64_t segment_floats(const hts_scan_desc &d, int count) { return count > 1 ? (int64_t)d.N * d.D * (padded(d.S) * (int64_t)count + (count - 1)) : 0; }
+Segments segments(const hts_scan_desc &d, int cus, bool backward)
+{
+    Segments seg = {};
+    seg.count = segments_of(d, cus, backward);
+    seg.steps = (int)round_up(ceil_div(d.T, seg.count), 16);
+    return seg;
+}
+struct Layout { int64_t h_in, state, sum, pairs, params, total; };      // floats
+Layout layout(const hts_scan_desc &d, const Segments &seg, bool backward)
+{
+    const int64_t held = (int64_t)d.N * d.D * padded(d.S), some = seg.count > 1;
+    Layout l;
+    l.h_in = 0;
+    l.state = l.h_in + (backward ? 0 : some * held);
+    l.sum = l.state + some * held * seg.count;
+    l.pairs = l.sum + some * round_up((int64_t)seg.count * d.N * d.D, 64);
+    l.params = l.pairs + (backward ? round_up((int64_t)blocks_of(d) * d.T * d.N * d.G * 2 * padded(d.S), 64) : 0);
+    l.total = l.params + (backward ? (int64_t)seg.count * d.N * d.D * (d.S + 2) : 0);
+    return l;
+}
 
 // whether rows of these channels can be read four entries at a time
 template <typename T> bool wide(const hts_steps &s, int64_t N, int64_t cols) { return !s.p || ((uintptr_t)s.p % (4 * sizeof(T)) == 0 && s.st % 4 == 0 && (N == 1 || s.sn % 4 == 0) && cols % 4 == 0); }
@@ -765,45 +914,46 @@ template <typename T> bool wide(const ScanOp &op, bool backward)
     return w;
 }
 
+#define LAUNCH(KERNEL, GRID, THREADS, ...)                                                                                                                 \
+    do {                                                                                                                                                  \
+        hipLaunchKernelGGL(KERNEL, dim3((uint32_t)(GRID)), dim3(THREADS), 0, c.stream, __VA_ARGS__);                                                       \
+        const hipError_t e_ = hipGetLastError();                                                                                                          \
+        if (e_ != hipSuccess) return e_;                                                                                                                  \
+    } while (0)
+
 template <typename T, int SL, bool WIDE> hipError_t scan(hts_seq_ctx &c, const ScanOp &op)
 {
     const Places at = places(op.d);
-    Segments seg = {};
-    seg.count = segments_of(op.d, c.cus < 256 ? c.cus : 256);
-    seg.steps = (int)round_up(ceil_div(op.d.T, seg.count), Shape<SL>::L);
-    const int64_t states = (int64_t)op.d.N * op.d.D * Shape<SL>::SP, waves = (int64_t)at.waves * op.d.G * op.d.N;
-    if (seg.count > 1) {
-        seg.h_in = (float *)c.ws;
-        seg.state = seg.h_in + states;
-        seg.sum = seg.state + (seg.count - 1) * states;
-        hipLaunchKernelGGL((scan_kernel<T, SL, WIDE, true>), dim3((uint32_t)ceil_div(waves * (seg.count - 1), FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((scan_kernel<T, SL, WIDE, false>), dim3((uint32_t)ceil_div(waves * seg.count, FWD_WAVES)), dim3(64 * FWD_WAVES), 0, c.stream, op, at, seg);
-    return hipGetLastError();
+    Segments seg = segments(op.d, c.cus, false);
+    const Layout l = layout(op.d, seg, false);
+    const int64_t waves = (int64_t)at.waves * op.d.G * op.d.N;
+    seg.h_in = (float *)c.ws + l.h_in; seg.state = (float *)c.ws + l.state; seg.sum = (float *)c.ws + l.sum;
+    if (seg.count > 1) LAUNCH((scan_kernel<T, SL, WIDE, true>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
+    LAUNCH((scan_kernel<T, SL, WIDE, false>), ceil_div(waves * seg.count, FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
+    return hipSuccess;
+}
+
+template <typename T, int SL, bool WIDE> hipError_t scan_backward(hts_seq_ctx &c, const ScanOp &op)
+{
+    const Places at = places(op.d);
+    Segments seg = segments(op.d, c.cus, true);
+    const Layout l = layout(op.d, seg, true);
+    const int64_t waves = (int64_t)at.waves * op.d.G * op.d.N, width = (int64_t)op.d.T * op.d.N * op.d.G * 8 * SL, D = op.d.D;
+    const int blocks = blocks_of(op.d);
+    float *pairs = (float *)c.ws + l.pairs, *params = (float *)c.ws + l.params;
+    seg.state = (float *)c.ws + l.state; seg.sum = (float *)c.ws + l.sum;
+    if (seg.count > 1) LAUNCH((scan_adjoint_kernel<T, SL, WIDE>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
+    LAUNCH((scan_backward_kernel<T, SL, WIDE>), (int64_t)blocks * op.d.G * op.d.N * seg.count, 64 * BWD_WAVES, op, at, seg, blocks, pairs, params);
+    LAUNCH((pair_sum_kernel<T>), ceil_div(width, 256), 256, op, blocks, 4 * SL, pairs);
+    return launch_sum_partials(c, params, (int64_t)op.d.N * seg.count, D * (op.d.S + 2), SumTarget{op.g.dA, D * op.d.S}, SumTarget{op.g.dskip, D}, SumTarget{op.g.ddt_bias, D});
 }
 
 template <typename T, int SL> hipError_t run(hts_seq_ctx &c, const ScanOp &op, bool backward)
 {
-    const Places at = places(op.d);
-    if (!backward) {
-        if (op.d.T > 1) return wide<T>(op, false) ? scan<T, SL, true>(c, op) : scan<T, SL, false>(c, op);
-        hipLaunchKernelGGL((step_kernel<T, SL>), dim3((uint32_t)ceil_div((int64_t)op.d.N * op.d.D, 64)), dim3(256), 0, c.stream, op);
-        return hipGetLastError();
-    }
-    const int blocks = blocks_of(op.d);
-    float *pairs = (float *)c.ws, *params = pairs + pair_floats(op.d);
-    const dim3 grid((uint32_t)((int64_t)blocks * op.d.G * op.d.N)), threads(64 * BWD_WAVES);
-    if (wide<T>(op, true)) hipLaunchKernelGGL((scan_backward_kernel<T, SL, true>), grid, threads, 0, c.stream, op, at, blocks, pairs, params);
-    else hipLaunchKernelGGL((scan_backward_kernel<T, SL, false>), grid, threads, 0, c.stream, op, at, blocks, pairs, params);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t width = (int64_t)op.d.T * op.d.N * op.d.G * Shape<SL>::PAIR;
-    hipLaunchKernelGGL((pair_sum_kernel<T>), dim3((uint32_t)ceil_div(width, 256)), dim3(256), 0, c.stream, op, blocks, Shape<SL>::SP, pairs);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int64_t D = op.d.D;
-    return launch_sum_partials(c, params, op.d.N, D * (op.d.S + 2), SumTarget{op.g.dA, D * op.d.S}, SumTarget{op.g.dskip, D}, SumTarget{op.g.ddt_bias, D});
+    if (backward) return wide<T>(op, true) ? scan_backward<T, SL, true>(c, op) : scan_backward<T, SL, false>(c, op);
+    if (op.d.T > 1) return wide<T>(op, false) ? scan<T, SL, true>(c, op) : scan<T, SL, false>(c, op);
+    LAUNCH((step_kernel<T, SL>), ceil_div((int64_t)op.d.N * op.d.D, 64), 256, op);
+    return hipSuccess;
 }
 template <typename T> hipError_t by_states(hts_seq_ctx &c, const ScanOp &op, bool backward)
 {
@@ -817,13 +967,8 @@ template <typename T> hipError_t by_states(hts_seq_ctx &c, const ScanOp &op, boo
 
 }  // namespace
 
-int64_t scan_states(const hts_scan_desc &d) { return ceil_div(d.T, chunk_steps(d.S)) * d.N * d.D * padded(d.S); }
-int64_t scan_workspace(const hts_scan_desc &d, bool backward)
-{
-    // (on fewer compute units there are fewer segments)
-    if (!backward) return 4 * segment_floats(d, segments_of(d, 256));
-    return 4 * (pair_floats(d) + param_floats(d));
-}
+int64_t scan_states(const hts_scan_desc &d) { return ceil_div(d.T, back_steps(d.S)) * d.N * d.D * padded(d.S); }
+int64_t scan_workspace(const hts_scan_desc &d, bool backward) { return 4 * layout(d, segments(d, 256, backward), backward).total; }
 hipError_t launch_scan(hts_seq_ctx &c, const ScanOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? by_states<bf16_t>(c, op, false) : by_states<float>(c, op, false); }
 hipError_t launch_scan_backward(hts_seq_ctx &c, const ScanOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? by_states<bf16_t>(c, op, true) : by_states<float>(c, op, true); }
 

@@ -377,3 +377,41 @@ def test_selective_scan_an_episode_ends_what_is_not_finite(hts):
         assert torch.equal(g[k][19:], g2[k][19:]), k
     assert bool((g2["dh_in"] == 0).all())
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,D,S,G", [(700, 1, 40, 16, 1), (333, 3, 24, 8, 2), (1000, 1, 70, 33, 1), (260, 2, 18, 20, 1), (512, 2, 64, 16, 1), (257, 16, 16, 16, 1)])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_selective_scan_in_segments(hts, dtype, T, N, D, S, G, way):
+    """Few channels and many steps: sequences that are cut into segments, with lengths that end in any of them and episodes that begin in some."""
+    r, ty, way = np.random.default_rng(T + N + D), TYPES[dtype], dict(WAYS[way])
+    d, ref = scan_inputs(r, T, N, D, S, G, way, ty)
+    if way["starts"]:                                           # few, so that states pass through several segments
+        s = (r.random((T, N)) < 1.5 / T).astype(np.uint8)
+        d["starts"], ref["starts"] = put(s, torch.uint8)[0], s
+    for k in ("A",):
+        d[k], ref[k] = put(ref[k] * 0.02)
+    (dy, dy64), (dh, dh64) = put(r.normal(size=(T, N, D)), ty), put(r.normal(size=(N, D, S)))
+    dy = put(spoil(dy64, ref["lengths"]), ty)[0]
+    ctx = hts.SeqContext(hts.selective_scan_workspace(T, N, D, S, G, precision=hts.PRECISION_BF16 if dtype == "bf16" else hts.PRECISION_FP32))
+    y, held, states = torch.empty(T, N, D, dtype=ty, device="cuda"), torch.zeros(N, D, S, device="cuda"), torch.empty(hts.selective_scan_states(T, N, D, S, G), device="cuda")
+    if way["h"]:
+        held.copy_(d["h_in"])
+    forward(hts, ctx, {**d, "h_in": held}, way["softplus"], y, h_out=held, states=states)               # the state in its place
+    torch.cuda.synchronize()
+    want, size = (so.scan(**ref, dy=dy64, dh_out=dh64, size=z) for z in (False, True))
+    chain = 16 * (T + S) + 12 * 40
+    so.near(host(y), want["y"], size["y"], chain, HALF[dtype], "y")
+    so.near(host(held), want["h_out"], size["h_out"], chain, HALF["f32"], "h_out")
+    g = {k: torch.empty(T, N, D, dtype=ty, device="cuda") for k in ("dx", "ddt")}
+    g["dz"] = torch.empty(T, N, D, dtype=ty, device="cuda") if way["z"] else None
+    g.update({k: torch.empty(T, N, G, S, dtype=ty, device="cuda") for k in ("dB", "dC")})
+    g.update(dA=torch.empty(D, S, device="cuda"), dskip=torch.empty(D, device="cuda"), ddt_bias=torch.empty(D, device="cuda"), dh_in=torch.empty(N, D, S, device="cuda"))
+    ctx.hts_selective_scan_backward(d["x"], d["dt"], d["A"], d["B"], d["C"], dy, states, z=d["z"], skip=d["skip"], dt_bias=d["dt_bias"], softplus=way["softplus"], starts=d["starts"],
+                                    lengths=d["lengths"], h_in=d["h_in"], dh_out=dh, **g)
+    torch.cuda.synchronize()
+    for k in g:
+        if g[k] is not None:
+            terms = D if k in ("dB", "dC") else T * N if k in ("dA", "dskip", "ddt_bias") else 0
+            so.near(host(g[k]), want[k], size[k], 2 * chain + terms + 32, HALF[dtype] if k in ("dx", "ddt", "dz", "dB", "dC") else HALF["f32"], k)
+    ctx.close()
