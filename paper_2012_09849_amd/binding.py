@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -382,7 +383,6 @@ class Context:
 
 # ---- sequence memory --------------------------------------------------------------------------------------------------
 _DTYPE = {PRECISION_FP32: torch.float32, PRECISION_BF16: torch.bfloat16}
-_NO_ROWS, _NO_STEPS = _Rows(None, 0), _Steps(None, 0, 0)
 
 
 def _size(what: str, rc: int) -> int:
@@ -409,46 +409,67 @@ def selective_scan_states(T: int, N: int, D: int, S: int, G: int = 1) -> int:
     return _size("hts_selective_scan_states", load_library().hts_selective_scan_states(C.byref(_ScanDesc(T, N, D, S, G, PRECISION_FP32, 1))))
 
 
-def _precision(t, name):
-    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16):
-        raise HtsError(f"{name}: expected a float32 or bfloat16 device tensor")
-    return PRECISION_BF16 if t.dtype == torch.bfloat16 else PRECISION_FP32
+def _precision(t, name, dims=None):
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16) or (dims is not None and t.dim() != dims):
+        raise HtsError(f"{name}: expected a float32 or bfloat16 device tensor" + (f" of {dims} dimensions" if dims else ""))
+    return PRECISION_BF16 if t.dtype is torch.bfloat16 else PRECISION_FP32
+
+
+def _is(t, dtype, shape, name, what=""):
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.shape == shape):
+        raise HtsError(f"{name}: expected a {what}{dtype} device tensor of shape {tuple(shape)}")
 
 
 def _rows(t, dtype, shape, name):
-    """A [M, K] operand whose rows are contiguous, at any distance."""
+    """(address, distance of rows) of a [M, K] operand whose rows are contiguous, at any distance."""
     if t is None:
-        return _NO_ROWS
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape:
-        raise HtsError(f"{name}: expected a {dtype} device tensor of shape {shape}")
+        return 0, 0
+    _is(t, dtype, shape, name)
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         raise HtsError(f"{name}: rows must be contiguous")
-    return _Rows(t.data_ptr(), ld)
+    return t.data_ptr(), ld
 
 
 def _steps(t, dtype, shape, name):
-    """A [T, N, ...] operand whose steps are contiguous, at any distance."""
+    """(address, distances of steps and of sequences) of a [T, N, ...] operand whose steps are contiguous, at any distance."""
     if t is None:
-        return _NO_STEPS
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape:
-        raise HtsError(f"{name}: expected a {dtype} device tensor of shape {shape}")
+        return 0, 0, 0
+    _is(t, dtype, shape, name)
     st = t.stride()
-    inner = 1
-    for size, stride in zip(shape[:1:-1], st[:1:-1]):
-        if stride != inner and size > 1:
-            raise HtsError(f"{name}: steps must be contiguous")
-        inner *= size
-    return _Steps(t.data_ptr(), st[0], st[1])
+    if st[-1] != 1 or len(st) > 3:
+        inner = 1
+        for size, stride in zip(shape[:1:-1], st[:1:-1]):
+            if stride != inner and size > 1:
+                raise HtsError(f"{name}: steps must be contiguous")
+            inner *= size
+    return t.data_ptr(), st[0], st[1]
 
 
 def _array(t, dtype, shape, name):
     """A contiguous array of that shape, or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise HtsError(f"{name}: expected a contiguous {dtype} device tensor of shape {shape}")
+    _is(t, dtype, shape, name, "contiguous ")
+    if not t.is_contiguous():
+        raise HtsError(f"{name}: expected a contiguous {dtype} device tensor of shape {tuple(shape)}")
     return t.data_ptr()
+
+
+class _Arguments:
+    """Structures of a call over one piece of memory that a call fills at once (a small call's time is the host's)."""
+
+    def __init__(self, *kinds):
+        size = sum(C.sizeof(k) for k in kinds)
+        self._memory, self._fill, self.of = bytearray(size), struct.Struct(f"{size // 8}q").pack_into, []
+        at = 0
+        for k in kinds:
+            self.of.append(k.from_buffer(self._memory, at))
+            at += C.sizeof(k)
+
+    def set(self, *words):
+        self._fill(self._memory, 0, *words)
+        return self.of
 
 
 class SeqContext:
@@ -460,6 +481,8 @@ class SeqContext:
         if not torch.cuda.is_available():
             raise HtsError("no GPU visible: the library has no CPU path")
         self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self._linear, self._linear_back, self._conv, self._conv_back = (_Arguments(*[k] * n) for k, n in ((_Rows, 5), (_Rows, 6), (_Steps, 2), (_Steps, 3)))
+        self._scan_in, self._scan_grads, self._one, self._descs = _Arguments(_ScanInputs), _Arguments(_ScanGrads), _Arguments(_Steps), {}
         self._h = C.c_void_p()
         _check(self.lib.hts_seq_create(workspace_bytes, C.c_void_p(self.stream.cuda_stream), C.byref(self._h)), "hts_seq_create")
 
@@ -475,73 +498,104 @@ class SeqContext:
         except Exception:
             pass
 
+    def _desc(self, kind, *sizes):
+        """A call's sizes as the library reads them, made once."""
+        key = kind, sizes
+        d = self._descs.get(key)
+        if d is None:
+            if len(self._descs) > 256:
+                self._descs.clear()
+            d = self._descs[key] = C.byref(kind(*sizes))
+        return d
+
     def hts_linear(self, x, w, y, bias=None, residual=None, pre=None, act=ACT_NONE):
         """y = act(x w^T + bias) + residual; pre receives x w^T + bias."""
-        prec = _precision(x, "x")
+        prec = _precision(x, "x", 2)
+        _precision(w, "w", 2)
         dt, (M, K), N = _DTYPE[prec], x.shape, w.shape[0]
-        _check(self.lib.hts_linear(self._h, C.byref(_LinearDesc(M, N, K, prec, act)), _rows(x, dt, (M, K), "x"), _rows(w, dt, (N, K), "w"),
-                                   _array(bias, torch.float32, (N,), "bias"), _rows(residual, dt, (M, N), "residual"), _rows(y, dt, (M, N), "y"),
-                                   _rows(pre, dt, (M, N), "pre")), "hts_linear")
+        xs, ws, rs, ys, ps = self._linear.set(*_rows(x, dt, (M, K), "x"), *_rows(w, dt, (N, K), "w"), *_rows(residual, dt, (M, N), "residual"), *_rows(y, dt, (M, N), "y"),
+                                              *_rows(pre, dt, (M, N), "pre"))
+        rc = self.lib.hts_linear(self._h, self._desc(_LinearDesc, M, N, K, prec, act), xs, ws, _array(bias, torch.float32, (N,), "bias"), rs, ys, ps)
+        if rc:
+            _check(rc, "hts_linear")
 
     def hts_linear_backward(self, x, w, dy, pre=None, act=ACT_NONE, add=None, dx=None, dw=None, db=None):
         """With g = dy act'(pre): dx = g w + add, dw = g^T x, db = column sums of g; each of the three only where it is given."""
-        prec = _precision(dy, "dy")
-        dt, (M, N), K = _DTYPE[prec], dy.shape, w.shape[1]
-        _check(self.lib.hts_linear_backward(self._h, C.byref(_LinearDesc(M, N, K, prec, act)), _rows(x, dt, (M, K), "x"), _rows(w, dt, (N, K), "w"),
-                                            _rows(pre, dt, (M, N), "pre"), _rows(dy, dt, (M, N), "dy"), _rows(add, dt, (M, K), "add"),
-                                            _rows(dx, dt, (M, K), "dx"), _array(dw, torch.float32, (N, K), "dw"),
-                                            _array(db, torch.float32, (N,), "db")), "hts_linear_backward")
+        prec = _precision(dy, "dy", 2)
+        _precision(w, "w", 2)
+        dt, (M, N), K, f = _DTYPE[prec], dy.shape, w.shape[1], torch.float32
+        a = self._linear_back.set(*_rows(x, dt, (M, K), "x"), *_rows(w, dt, (N, K), "w"), *_rows(pre, dt, (M, N), "pre"), *_rows(dy, dt, (M, N), "dy"),
+                                  *_rows(add, dt, (M, K), "add"), *_rows(dx, dt, (M, K), "dx"))
+        rc = self.lib.hts_linear_backward(self._h, self._desc(_LinearDesc, M, N, K, prec, act), *a, _array(dw, f, (N, K), "dw"), _array(db, f, (N,), "db"))
+        if rc:
+            _check(rc, "hts_linear_backward")
 
     @staticmethod
     def _sequences(starts, lengths, T, N):
         return _array(starts, torch.uint8, (T, N), "starts"), _array(lengths, torch.int32, (N,), "lengths")
 
     def hts_short_conv(self, x, w, y, bias=None, act=ACT_NONE, starts=None, lengths=None, state_in=None, state_out=None):
-        prec, (T, N, D), W, f = _precision(x, "x"), x.shape, w.shape[-1], torch.float32
-        dt, state = _DTYPE[prec], (N, W - 1, D)
-        _check(self.lib.hts_short_conv(self._h, C.byref(_ConvDesc(T, N, D, W, prec, act)), _steps(x, dt, (T, N, D), "x"), _array(w, f, (D, W), "w"),
-                                       _array(bias, f, (D,), "bias"), *self._sequences(starts, lengths, T, N),
-                                       _array(state_in, f, state, "state_in"), _steps(y, dt, (T, N, D), "y"),
-                                       _array(state_out, f, state, "state_out")), "hts_short_conv")
+        """y_t = act(bias + sum_j w[:, j] x_{t-W+1+j}) over the steps of t's episode; state_in and state_out (which may be one) hold the last W - 1 inputs."""
+        prec = _precision(x, "x", 3)
+        cells, W, f = x.shape, w.shape[-1], torch.float32
+        (T, N, D), dt = cells, _DTYPE[prec]
+        state = (N, W - 1, D)
+        xs, ys = self._conv.set(*_steps(x, dt, cells, "x"), *_steps(y, dt, cells, "y"))
+        rc = self.lib.hts_short_conv(self._h, self._desc(_ConvDesc, T, N, D, W, prec, act), xs, _array(w, f, (D, W), "w"), _array(bias, f, (D,), "bias"),
+                                     *self._sequences(starts, lengths, T, N), _array(state_in, f, state, "state_in"), ys, _array(state_out, f, state, "state_out"))
+        if rc:
+            _check(rc, "hts_short_conv")
 
     def hts_short_conv_backward(self, x, w, dy, dx, dw, db=None, bias=None, act=ACT_NONE, starts=None, lengths=None, state_in=None, dstate_out=None,
                                 dstate_in=None):
-        prec, (T, N, D), W, f = _precision(x, "x"), x.shape, w.shape[-1], torch.float32
-        dt, state = _DTYPE[prec], (N, W - 1, D)
-        _check(self.lib.hts_short_conv_backward(self._h, C.byref(_ConvDesc(T, N, D, W, prec, act)), _steps(x, dt, (T, N, D), "x"),
-                                                _array(w, f, (D, W), "w"), _array(bias, f, (D,), "bias"), *self._sequences(starts, lengths, T, N),
-                                                _array(state_in, f, state, "state_in"), _steps(dy, dt, (T, N, D), "dy"),
-                                                _array(dstate_out, f, state, "dstate_out"), _steps(dx, dt, (T, N, D), "dx"),
-                                                _array(dw, f, (D, W), "dw"), _array(db, f, (D,), "db"), _array(dstate_in, f, state, "dstate_in")),
-               "hts_short_conv_backward")
+        """The gradients dx, dw, db and dstate_in of dy and dstate_out."""
+        prec = _precision(x, "x", 3)
+        cells, W, f = x.shape, w.shape[-1], torch.float32
+        (T, N, D), dt = cells, _DTYPE[prec]
+        state = (N, W - 1, D)
+        xs, gs, ds = self._conv_back.set(*_steps(x, dt, cells, "x"), *_steps(dy, dt, cells, "dy"), *_steps(dx, dt, cells, "dx"))
+        rc = self.lib.hts_short_conv_backward(self._h, self._desc(_ConvDesc, T, N, D, W, prec, act), xs, _array(w, f, (D, W), "w"), _array(bias, f, (D,), "bias"),
+                                              *self._sequences(starts, lengths, T, N), _array(state_in, f, state, "state_in"), gs,
+                                              _array(dstate_out, f, state, "dstate_out"), ds, _array(dw, f, (D, W), "dw"), _array(db, f, (D,), "db"),
+                                              _array(dstate_in, f, state, "dstate_in"))
+        if rc:
+            _check(rc, "hts_short_conv_backward")
 
     def _scan(self, x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in):
-        prec, (T, N, D), f = _precision(x, "x"), x.shape, torch.float32
-        S, G, ty = A.shape[-1], B.shape[2] if B.dim() == 4 else 1, _DTYPE[prec]
-        pair = (T, N, G, S) if B.dim() == 4 else (T, N, S)
+        prec, f = _precision(x, "x", 3), torch.float32
+        cells, S, ty = x.shape, A.shape[-1], _DTYPE[prec]
+        T, N, D = cells
+        G = B.shape[2] if B.dim() == 4 else 1
+        pair, held = (T, N, G, S) if B.dim() == 4 else (T, N, S), (N, D, S)
         st, le = self._sequences(starts, lengths, T, N)
-        inputs = _ScanInputs(_steps(x, ty, (T, N, D), "x"), _steps(dt, ty, (T, N, D), "dt"), _steps(B, ty, pair, "B"), _steps(C_, ty, pair, "C"),
-                             _steps(z, ty, (T, N, D), "z"), _array(A, f, (D, S), "A"), _array(skip, f, (D,), "skip"),
-                             _array(dt_bias, f, (D,), "dt_bias"), st, le, _array(h_in, f, (N, D, S), "h_in"))
-        return _ScanDesc(T, N, D, S, G, prec, 1 if softplus else 0), inputs, ty, (T, N, D), pair, (N, D, S)
+        inputs = self._scan_in.set(*_steps(x, ty, cells, "x"), *_steps(dt, ty, cells, "dt"), *_steps(B, ty, pair, "B"), *_steps(C_, ty, pair, "C"), *_steps(z, ty, cells, "z"),
+                                   _array(A, f, (D, S), "A") or 0, _array(skip, f, (D,), "skip") or 0, _array(dt_bias, f, (D,), "dt_bias") or 0, st or 0, le or 0,
+                                   _array(h_in, f, held, "h_in") or 0)
+        return self._desc(_ScanDesc, T, N, D, S, G, prec, 1 if softplus else 0), C.byref(inputs[0]), ty, cells, pair, held, G
 
     def hts_selective_scan(self, x, dt, A, B, C_, y, z=None, skip=None, dt_bias=None, softplus=True, starts=None, lengths=None, h_in=None, h_out=None,
                            states=None):
-        desc, inputs, ty, cells, _, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
-        if states is not None and states.numel() < selective_scan_states(desc.T, desc.N, desc.D, desc.S, desc.G):
+        """h_t = exp(delta A) h_{t-1} + delta x B, y = (C h + skip x) silu(z), delta = softplus(dt + dt_bias).  B, C: [T, N, S] or [T, N, G, S].  h_in and
+        h_out may be one; states (selective_scan_states floats) is for a backward call."""
+        desc, inputs, ty, cells, _, held, G = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
+        if states is not None and states.numel() < selective_scan_states(*cells, held[2], G):
             raise HtsError("states: too few entries (selective_scan_states)")
-        _check(self.lib.hts_selective_scan(self._h, C.byref(desc), C.byref(inputs), _steps(y, ty, cells, "y"),
-                                           _array(h_out, torch.float32, held, "h_out"), _ptr(states, torch.float32, "states")), "hts_selective_scan")
+        rc = self.lib.hts_selective_scan(self._h, desc, inputs, self._one.set(*_steps(y, ty, cells, "y"))[0], _array(h_out, torch.float32, held, "h_out"),
+                                         _ptr(states, torch.float32, "states"))
+        if rc:
+            _check(rc, "hts_selective_scan")
 
     def hts_selective_scan_backward(self, x, dt, A, B, C_, dy, states, dx, ddt, dB, dC, dA, z=None, dz=None, skip=None, dskip=None, dt_bias=None,
                                     ddt_bias=None, softplus=True, starts=None, lengths=None, h_in=None, dh_out=None, dh_in=None):
-        desc, inputs, ty, cells, pair, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
-        if states is None or states.numel() < selective_scan_states(desc.T, desc.N, desc.D, desc.S, desc.G):
+        """The gradients of dy and dh_out; states as the forward call on the same inputs left it."""
+        desc, inputs, ty, cells, pair, held, G = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
+        if states is None or states.numel() < selective_scan_states(*cells, held[2], G):
             raise HtsError("states: too few entries (selective_scan_states)")
-        f, D = torch.float32, desc.D
-        grads = _ScanGrads(_steps(dx, ty, cells, "dx"), _steps(ddt, ty, cells, "ddt"), _steps(dB, ty, pair, "dB"), _steps(dC, ty, pair, "dC"),
-                           _steps(dz, ty, cells, "dz"), _array(dA, f, (D, desc.S), "dA"), _array(dskip, f, (D,), "dskip"),
-                           _array(ddt_bias, f, (D,), "ddt_bias"), _array(dh_in, f, held, "dh_in"))
-        _check(self.lib.hts_selective_scan_backward(self._h, C.byref(desc), C.byref(inputs), _steps(dy, ty, cells, "dy"),
-                                                    _array(dh_out, f, held, "dh_out"), _ptr(states, f, "states"), C.byref(grads)),
-               "hts_selective_scan_backward")
+        f, (_, D, S) = torch.float32, held
+        grads = self._scan_grads.set(*_steps(dx, ty, cells, "dx"), *_steps(ddt, ty, cells, "ddt"), *_steps(dB, ty, pair, "dB"), *_steps(dC, ty, pair, "dC"),
+                                     *_steps(dz, ty, cells, "dz"), _array(dA, f, (D, S), "dA") or 0, _array(dskip, f, (D,), "dskip") or 0,
+                                     _array(ddt_bias, f, (D,), "ddt_bias") or 0, _array(dh_in, f, held, "dh_in") or 0)
+        rc = self.lib.hts_selective_scan_backward(self._h, desc, inputs, self._one.set(*_steps(dy, ty, cells, "dy"))[0], _array(dh_out, f, held, "dh_out"),
+                                                  _ptr(states, f, "states"), C.byref(grads[0]))
+        if rc:
+            _check(rc, "hts_selective_scan_backward")

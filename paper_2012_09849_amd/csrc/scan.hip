@@ -53,12 +53,6 @@ struct Places { int per_group, waves; };          // channels of a group, wavefr
 
 template <typename T> __device__ __forceinline__ float wide_of(T v) { return to_f32(v); }
 __device__ __forceinline__ int length_of(const int32_t *lengths, int n, int T) { return lengths ? max(0, min(T, lengths[n])) : T; }
-// Loads and stores through buffer descriptors: a base that all lanes share (the chunk's) and 32 bits of a lane from it.  A lane that has nothing to
-// load or store gets an offset beyond the descriptor's 2 GB: it reads zero and writes nothing, without a branch (values that were loaded on different
-// paths would be waited for where the paths meet).
-constexpr uint32_t REACH = 1u << 31, NOWHERE = REACH;
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t reach(const char *base) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, REACH, 0x00020000); }
-
 // An array's chunk: the base goes from chunk to chunk, so that a chunk's addresses are a few scalar additions
 struct Walk {
     const char *base;
@@ -72,61 +66,6 @@ struct Walk {
     __device__ __forceinline__ void forth() { base += chunk; }
     __device__ __forceinline__ void back() { base -= chunk; }
 };
-
-// V neighbouring entries of a lane: one access where addresses and counts allow it (WIDE), otherwise an entry at a time, `count` of them
-template <typename T, int V, bool WIDE> struct Raw {
-    static constexpr int WORDS = WIDE ? (V * (int)sizeof(T) + 3) / 4 : V;
-    uint32_t w[WORDS];
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t src, uint32_t lane, int count)
-    {
-        if constexpr (WIDE && WORDS == 4) {
-            const auto r = __builtin_amdgcn_raw_buffer_load_b128(src, (int)lane, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = r[i];
-        } else if constexpr (WIDE && WORDS == 2) {
-            const auto r = __builtin_amdgcn_raw_buffer_load_b64(src, (int)lane, 0, 0);
-            w[0] = r[0]; w[1] = r[1];
-        } else if constexpr (WIDE && V * sizeof(T) == 4) w[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, (int)lane, 0, 0);
-        else
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int at = i < count ? (int)(lane + i * (uint32_t)sizeof(T)) : (int)NOWHERE;
-                if constexpr (sizeof(T) == 2) w[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(src, at, 0, 0);
-                else w[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, at, 0, 0);
-            }
-    }
-    __device__ __forceinline__ float operator[](int i) const
-    {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-        else if constexpr (!WIDE || V == 1) return __uint_as_float(w[i] << 16);
-        else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-    }
-};
-template <typename T> __device__ __forceinline__ uint32_t bits_of(float v)
-{
-    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(uint16_t, from_f32<T>(v));
-    else return __float_as_uint(v);
-}
-template <typename T, int V, bool WIDE> __device__ __forceinline__ void put_raw(__amdgpu_buffer_rsrc_t dst, uint32_t lane, int count, const float (&v)[V])
-{
-    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    if constexpr (WIDE && V * sizeof(T) >= 4) {
-        constexpr int WORDS = V * (int)sizeof(T) / 4;
-        uint32_t w[WORDS];
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) w[i] = sizeof(T) == 4 ? bits_of<T>(v[i]) : bits_of<T>(v[V > 1 ? 2 * i : 0]) | bits_of<T>(v[V > 1 ? 2 * i + 1 : 0]) << 16;
-        if constexpr (WORDS == 1) __builtin_amdgcn_raw_buffer_store_b32(w[0], dst, (int)lane, 0, 0);
-        else if constexpr (WORDS == 2) __builtin_amdgcn_raw_buffer_store_b64(u2{w[0], w[1]}, dst, (int)lane, 0, 0);
-        else __builtin_amdgcn_raw_buffer_store_b128(u4{w[0], w[1], w[2], w[3]}, dst, (int)lane, 0, 0);
-    } else
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int at = i < count ? (int)(lane + i * (uint32_t)sizeof(T)) : (int)NOWHERE;
-            if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bits_of<T>(v[i]), dst, at, 0, 0);
-            else __builtin_amdgcn_raw_buffer_store_b32(bits_of<T>(v[i]), dst, at, 0, 0);
-        }
-}
 
 // The order of memory: lane = (step of the chunk, V neighbouring ones of the wavefront's 16 channels)
 template <class H> struct Cell {
@@ -645,11 +584,13 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
         // twice: chunks in which no episode begins, most of them, select nothing
         auto pass = [&](auto has) {
             constexpr bool FRESH = decltype(has)::value;
+            // (fences between four steps and the next: mixed, they take more registers than two wavefronts a SIMD have; 145 -> 123 us with the shares of dA)
             float a[L][SL], h[L][SL];
             {
                 Ahead<H, true> ahead(lds + q * SL);
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
+                    __builtin_amdgcn_sched_barrier(0);
                     const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j);
                     float part[4];
 #pragma unroll
@@ -672,6 +613,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
             Ahead<H, true> ahead(lds + q * SL);
 #pragma unroll
             for (int j = NB - 1; j >= 0; --j) {
+                __builtin_amdgcn_sched_barrier(0);
                 const f32x4 de = X::four(sizes, own, j), dx = X::four(moves, own, j), rk = X::four(rs, own, j);
                 float gB[4], dd[4], val[8 * SL];
 #pragma unroll
@@ -690,6 +632,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
                         const float ga = begin ? 0.0f : ag[s] * (t ? h[t ? t - 1 : 0][s] : hb[s]);
                         dd[i] = __builtin_fmaf(ga, A[s], dd[i]);
                         dA[s] = __builtin_fmaf(ga, de[i], dA[s]);
+                        asm volatile("" : "+v"(dA[s]));          // (here and now: left to the compiler, a chunk's shares wait for its end, with all their factors)
                     }
                 }
                 // a lane's sums: step 4 j + 2 bit3 + bit2, B or C by bit 4, half of its quad's states by bit 5

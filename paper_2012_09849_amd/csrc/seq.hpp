@@ -110,4 +110,65 @@ template <typename T, int V> __device__ __forceinline__ Loaded<T, V> load_v(cons
 }
 template <typename T, int V> __device__ __forceinline__ void store_v(T *p, const Loaded<T, V> &v) { __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T) * V), &v, sizeof v); }
 
+// Loads and stores through buffer descriptors: a base that all lanes share and 32 bits of a lane (and 32 that all lanes share) from it.  A lane that has nothing to
+// load or store gets an offset beyond the descriptor's 2 GB: it reads zero and writes nothing, without a branch (values that were loaded on different
+// paths would be waited for where the paths meet).
+constexpr uint32_t REACH = 1u << 31, NOWHERE = REACH;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t reach(const char *base) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, REACH, 0x00020000); }
+
+// V neighbouring entries of a lane: one access where addresses and counts allow it (WIDE), otherwise an entry at a time, `count` of them
+template <typename T, int V, bool WIDE> struct Raw {
+    static constexpr int WORDS = WIDE ? (V * (int)sizeof(T) + 3) / 4 : V;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t src, uint32_t lane, int count, uint32_t all = 0)
+    {
+        if constexpr (WIDE && WORDS == 4) {
+            const auto r = __builtin_amdgcn_raw_buffer_load_b128(src, (int)lane, (int)all, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = r[i];
+        } else if constexpr (WIDE && WORDS == 2) {
+            const auto r = __builtin_amdgcn_raw_buffer_load_b64(src, (int)lane, (int)all, 0);
+            w[0] = r[0]; w[1] = r[1];
+        } else if constexpr (WIDE && V * sizeof(T) == 4) w[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, (int)lane, (int)all, 0);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int at = i < count ? (int)(lane + i * (uint32_t)sizeof(T)) : (int)NOWHERE;
+                if constexpr (sizeof(T) == 2) w[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(src, at, (int)all, 0);
+                else w[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(src, at, (int)all, 0);
+            }
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else if constexpr (!WIDE || V == 1) return __uint_as_float(w[i] << 16);
+        else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+template <typename T> __device__ __forceinline__ uint32_t bits_of(float v)
+{
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(uint16_t, from_f32<T>(v));
+    else return __float_as_uint(v);
+}
+template <typename T, int V, bool WIDE> __device__ __forceinline__ void put_raw(__amdgpu_buffer_rsrc_t dst, uint32_t lane, int count, const float (&v)[V], uint32_t all = 0)
+{
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    if constexpr (WIDE && V * sizeof(T) >= 4) {
+        constexpr int WORDS = V * (int)sizeof(T) / 4;
+        uint32_t w[WORDS];
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = sizeof(T) == 4 ? bits_of<T>(v[i]) : bits_of<T>(v[V > 1 ? 2 * i : 0]) | bits_of<T>(v[V > 1 ? 2 * i + 1 : 0]) << 16;
+        if constexpr (WORDS == 1) __builtin_amdgcn_raw_buffer_store_b32(w[0], dst, (int)lane, (int)all, 0);
+        else if constexpr (WORDS == 2) __builtin_amdgcn_raw_buffer_store_b64(u2{w[0], w[1]}, dst, (int)lane, (int)all, 0);
+        else __builtin_amdgcn_raw_buffer_store_b128(u4{w[0], w[1], w[2], w[3]}, dst, (int)lane, (int)all, 0);
+    } else
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int at = i < count ? (int)(lane + i * (uint32_t)sizeof(T)) : (int)NOWHERE;
+            if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bits_of<T>(v[i]), dst, at, (int)all, 0);
+            else __builtin_amdgcn_raw_buffer_store_b32(bits_of<T>(v[i]), dst, at, (int)all, 0);
+        }
+}
+
 }  // namespace hts

@@ -153,7 +153,7 @@ static int32_t check_conv(const hts_short_conv_desc *d)
 {
     if (!d) return HTS_EINVAL;
     if (d->T <= 0 || d->N <= 0 || d->D <= 0 || (d->act != HTS_ACT_NONE && d->act != HTS_ACT_SILU)) return HTS_EINVAL;
-    if (bad_precision(d->precision) || d->W < 2 || d->W > 4 || d->D > (1 << 20)) return HTS_ESHAPE;
+    if (bad_precision(d->precision) || d->W < 2 || d->W > 4 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
     // a workgroup per 64 channels and 64 steps at least; their number has 31 bits
     return ceil_div(d->T, 16) * d->N * ceil_div(d->D, 64) > (1ll << 30) ? HTS_ESHAPE : HTS_OK;
 }
