@@ -1,0 +1,205 @@
+"""A recurrent core for policies that have to remember, from the library's sequence-memory operators (no arithmetic of the core lives here).
+
+The core stands between a trunk's features and the heads:
+
+    u  = x W_in^T + b_in                 [T,N,2I]: what is remembered, and a gate z
+    c  = silu(short convolution of u's first half)
+    p  = c W_proj^T                      [T,N,R+2S]: what the step sizes come from, B, C
+    dt = p[.., :R] W_dt^T
+    h  = selective scan of (c, dt, A, B, C), read out as v, gated by z
+    y  = v W_out^T + b_out + x
+
+A learner runs it over a whole storage (`forward`, `backward`), an actor a step at a time (`step`); both carry the same state (`State`).  `starts` marks the
+steps that begin an episode; rows 1.. of a [T+1,N] array of starts are the `dones` of hts_returns_gae.  Parameters and gradients are flat binary32 vectors of
+the same packing, for hts_adam_apply_static and the like; with bfloat16 operands `sync_params` refreshes the matrices' copies after an update.
+
+    python -m paper_2012_09849_amd.memory        # trains a small core to recall a cue, then acts with it step by step
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as hts
+
+
+class State:
+    """What N sequences carry from call to call: the convolution's last inputs and the scan's states (zeros: nothing remembered)."""
+
+    def __init__(self, core, N):
+        self.conv = torch.zeros(N, core.width - 1, core.inner, device="cuda")
+        self.h = torch.zeros(N, core.inner, core.states, device="cuda")
+
+    def clone(self):
+        other = object.__new__(State)
+        other.conv, other.h = self.conv.clone(), self.h.clone()
+        return other
+
+
+class MemoryCore:
+    """features F, inner I, states S of a channel, filter width W, rank R of the step sizes; up to max_steps x max_rows steps a call."""
+
+    def __init__(self, features=512, inner=1024, states=16, width=4, rank=32, precision=hts.PRECISION_FP32, max_steps=1, max_rows=1, stream=None):
+        self.features, self.inner, self.states, self.width, self.rank = features, inner, states, width, rank
+        self.precision, self.dtype = precision, torch.bfloat16 if precision == hts.PRECISION_BF16 else torch.float32
+        self.max_steps, self.max_rows = max_steps, max_rows
+        F, I, S, R = features, inner, states, rank
+        self.shapes = {"in.w": (2 * I, F), "in.b": (2 * I,), "conv.w": (I, width), "conv.b": (I,), "proj.w": (R + 2 * S, I), "dt.w": (I, R), "dt.b": (I,), "A": (I, S),
+                       "skip": (I,), "out.w": (F, I), "out.b": (F,)}
+        # every array of the packing begins at a multiple of 16 bytes
+        self.offsets, self.P = {}, 0
+        for name, shape in self.shapes.items():
+            self.offsets[name] = self.P
+            self.P += -(-torch.Size(shape).numel() // 4) * 4
+        M, T, N = max_steps * max_rows, max_steps, max_rows
+        need = [hts.linear_workspace(M, n, k, precision=precision) for n, k in (self.shapes[w] for w in ("in.w", "proj.w", "dt.w", "out.w"))]
+        need += [hts.short_conv_workspace(T, N, I, width, precision=precision), hts.selective_scan_workspace(T, N, I, S, precision=precision)]
+        self.ctx = hts.SeqContext(max(need), stream=stream)
+        self.params = torch.zeros(self.P, device="cuda")
+        self.grads = torch.zeros(self.P, device="cuda")
+        self.p, self.g = self.views(self.params), self.views(self.grads)
+        self.m = dict(self.p) if precision == hts.PRECISION_FP32 else {n: torch.zeros(self.shapes[n], dtype=self.dtype, device="cuda") for n in ("in.w", "proj.w", "dt.w", "out.w")}
+        new = lambda *s: torch.empty(*s, dtype=self.dtype, device="cuda")  # noqa: E731
+        self._u, self._c, self._p, self._dt, self._v = new(M, 2 * I), new(M, I), new(M, R + 2 * S), new(M, I), new(M, I)
+        self._states, self._training = None, None
+
+    def views(self, vector):
+        """The packing's arrays, of a vector of P binary32 numbers."""
+        return {n: vector[o:o + torch.Size(s).numel()].view(s) for (n, s), o in zip(self.shapes.items(), self.offsets.values())}
+
+    def init_params(self, seed=0):
+        """Small random projections; decays at -1 .. -S, step sizes between 1e-3 and 0.1."""
+        g = torch.Generator().manual_seed(seed)
+        p = self.views(torch.zeros(self.P))
+        for name in ("in.w", "proj.w", "dt.w", "out.w", "conv.w"):
+            p[name].copy_(torch.randn(p[name].shape, generator=g) / p[name].shape[1] ** 0.5)
+        p["A"].copy_(-torch.arange(1, self.states + 1, dtype=torch.float32).expand(self.inner, -1))
+        size = torch.exp(torch.rand(self.inner, generator=g) * 4.605 - 6.908)
+        p["dt.b"].copy_(size + torch.log(-torch.expm1(-size)))
+        p["skip"].fill_(1.0)
+        for name, t in p.items():
+            self.p[name].copy_(t)
+        self.sync_params()
+
+    def sync_params(self):
+        """After the parameters changed: the matrices in the operands' type, on the context's stream."""
+        if self.precision == hts.PRECISION_BF16:
+            with torch.cuda.stream(self.ctx.stream):
+                for name, t in self.m.items():
+                    t.copy_(self.p[name])
+
+    def _run(self, x, y, starts, lengths, state, states):
+        T, N, F = x.shape
+        I, S, R, M = self.inner, self.states, self.rank, x.shape[0] * x.shape[1]
+        if T > self.max_steps or N > self.max_rows or F != self.features:
+            raise hts.HtsError(f"x: at most [{self.max_steps},{self.max_rows},{self.features}]")
+        c = self.ctx
+        u, conv, p, dt, v = (a[:M] for a in (self._u, self._c, self._p, self._dt, self._v))
+        rows = lambda a: a.reshape(M, -1)  # noqa: E731
+        steps = lambda a: a.view(T, N, a.shape[-1])  # noqa: E731
+        c.hts_linear(rows(x), self.m["in.w"], u, bias=self.p["in.b"])
+        c.hts_short_conv(steps(u)[:, :, :I], self.p["conv.w"], steps(conv), bias=self.p["conv.b"], act=hts.ACT_SILU, starts=starts, lengths=lengths, state_in=state.conv,
+                         state_out=state.conv)
+        c.hts_linear(conv, self.m["proj.w"], p)
+        c.hts_linear(p[:, :R], self.m["dt.w"], dt)
+        c.hts_selective_scan(steps(conv), steps(dt), self.p["A"], steps(p)[:, :, R:R + S], steps(p)[:, :, R + S:], steps(v), z=steps(u)[:, :, I:], skip=self.p["skip"],
+                             dt_bias=self.p["dt.b"], starts=starts, lengths=lengths, h_in=state.h, h_out=state.h, states=states)
+        c.hts_linear(v, self.m["out.w"], rows(y), bias=self.p["out.b"], residual=rows(x))
+
+    def step(self, x, y, state, starts=None):
+        """One step of N sequences: x, y [N,F], starts u8 [N]; the state moves on in its place."""
+        self._run(x[None], y[None], None if starts is None else starts[None], None, state, None)
+
+    def forward(self, x, y, state, starts=None, lengths=None, train=False):
+        """T steps of N sequences: x, y [T,N,F] contiguous, starts u8 [T,N], lengths i32 [N]; the state moves on in its place.  train: what `backward` reads is
+        kept until the next call."""
+        states, self._training = None, None
+        if train:
+            need = hts.selective_scan_states(x.shape[0], x.shape[1], self.inner, self.states)
+            with torch.cuda.stream(self.ctx.stream):          # where they are used
+                if self._states is None or self._states.numel() < need:
+                    self._states = torch.empty(need, device="cuda")
+                begun = state.clone()
+            states = self._states
+        self._run(x, y, starts, lengths, state, states)
+        if train:
+            self._training = (x, starts, lengths, begun)
+
+    def backward(self, dy, dx):
+        """The gradients of dy [T,N,F] at the last forward(train=True): of the parameters into self.grads, of x into dx.  The state that the storage began
+        with is a constant."""
+        if self._training is None:
+            raise hts.HtsError("backward: no forward(train=True) before it")
+        x, starts, lengths, begun = self._training
+        T, N, F = x.shape
+        I, S, R, M, c, g = self.inner, self.states, self.rank, x.shape[0] * x.shape[1], self.ctx, self.g
+        u, conv, p, dt, v = (a[:M] for a in (self._u, self._c, self._p, self._dt, self._v))
+        new = lambda k: torch.empty(M, k, dtype=self.dtype, device="cuda")  # noqa: E731
+        rows = lambda a: a.reshape(M, -1)  # noqa: E731
+        steps = lambda a: a.view(T, N, a.shape[-1])  # noqa: E731
+        with torch.cuda.stream(self.ctx.stream):
+            du, dconv, dp, ddt, dv = new(2 * I), new(I), new(R + 2 * S), new(I), new(I)
+        seq = dict(starts=starts, lengths=lengths)
+        c.hts_linear_backward(v, self.m["out.w"], rows(dy), dx=dv, dw=g["out.w"], db=g["out.b"])
+        c.hts_selective_scan_backward(steps(conv), steps(dt), self.p["A"], steps(p)[:, :, R:R + S], steps(p)[:, :, R + S:], steps(dv), self._states, steps(dconv), steps(ddt),
+                                      steps(dp)[:, :, R:R + S], steps(dp)[:, :, R + S:], g["A"], z=steps(u)[:, :, I:], dz=steps(du)[:, :, I:], skip=self.p["skip"],
+                                      dskip=g["skip"], dt_bias=self.p["dt.b"], ddt_bias=g["dt.b"], h_in=begun.h, **seq)
+        c.hts_linear_backward(p[:, :R], self.m["dt.w"], ddt, dx=dp[:, :R], dw=g["dt.w"])
+        c.hts_linear_backward(conv, self.m["proj.w"], dp, add=dconv, dx=dconv, dw=g["proj.w"])
+        c.hts_short_conv_backward(steps(u)[:, :, :I], self.p["conv.w"], steps(dconv), steps(du)[:, :, :I], g["conv.w"], db=g["conv.b"], bias=self.p["conv.b"],
+                                  act=hts.ACT_SILU, state_in=begun.conv, **seq)
+        c.hts_linear_backward(rows(x), self.m["in.w"], du, add=rows(dy), dx=rows(dx), dw=g["in.w"], db=g["in.b"])
+
+    def close(self):
+        self.ctx.close()
+
+
+def recall_storage(T, N, F, seed):
+    """Episodes of about 12 steps whose first observation carries a cue of +1 or -1 in its first feature (every other feature is noise): observations
+    [T,N,F], the cue of every step's episode [T,N], starts."""
+    g = torch.Generator().manual_seed(seed)
+    starts = (torch.rand(T, N, generator=g) < 1 / 12).to(torch.uint8)
+    starts[0] = 1
+    cue = torch.randint(0, 2, (T, N), generator=g).float() * 2 - 1
+    for t in range(1, T):
+        cue[t] = torch.where(starts[t] != 0, cue[t], cue[t - 1])
+    x = torch.randn(T, N, F, generator=g) * 0.3
+    x[:, :, 0] = torch.where(starts != 0, cue, torch.zeros(()))
+    return x, cue, starts
+
+
+def train_recall(core, updates, T=32, N=16, lr=3e-3, seed=1):
+    """The last feature of y learns to hold the episode's cue: mean squared errors of the updates."""
+    opt, hp, losses = hts.OptState(torch.zeros(core.P, device="cuda"), torch.zeros(core.P, device="cuda")), hts.HParams(lr=lr, max_grad_norm=1.0), []
+    F = core.features
+    for k in range(updates):
+        x, cue, starts = (a.cuda() for a in recall_storage(T, N, F, seed + k))
+        x = x.to(core.dtype)
+        y, dy, dx = torch.empty_like(x), torch.zeros_like(x), torch.empty_like(x)
+        core.forward(x, y, State(core, N), starts=starts, train=True)
+        off = y[:, :, F - 1].float() - cue
+        dy[:, :, F - 1] = (2 / off.numel()) * off
+        losses.append((off * off).mean())
+        core.backward(dy, dx)
+        hts.hts_adam_apply_static(core.params, core.grads, opt, hp, core.ctx.stream)
+        core.sync_params()
+    return [float(v) for v in losses]
+
+
+def main():
+    core = MemoryCore(features=64, inner=128, precision=hts.PRECISION_BF16, max_steps=32, max_rows=16)
+    core.init_params()
+    losses = train_recall(core, 200)
+    print(f"recalling a cue: mean squared error {sum(losses[:5]) / 5:.3f} at first, {sum(losses[-5:]) / 5:.3f} after {len(losses)} updates")
+    x, cue, starts = (a.cuda() for a in recall_storage(32, 16, 64, 12345))
+    x, state = x.to(core.dtype), State(core, 16)
+    y = torch.empty(16, 64, dtype=core.dtype, device="cuda")
+    right = 0
+    for t in range(32):
+        core.step(x[t], y, state, starts[t])
+        right += int((y[:, 63].sign() == cue[t]).sum())
+    print(f"acting step by step on episodes never seen: the cue's sign is right in {right} of {32 * 16} steps")
+    core.close()
+
+
+if __name__ == "__main__":
+    main()
