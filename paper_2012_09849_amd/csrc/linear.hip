@@ -423,13 +423,17 @@ int slices_of(int64_t rows, int64_t N, int64_t K, int bk)
 }
 
 template <typename T> bool words(const void *p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * (int64_t)sizeof(T) % 16 == 0; }
-// whether an operand's rows (`cols` entries) can be copied straight into LDS: whole 16-byte words, and a tile's rows within 32 bits
-template <typename T> bool copies(const void *p, int64_t ld, int64_t cols) { return words<T>(p, ld) && cols % Kind<T>::V == 0 && ld < (1ll << 31) / (128 * (int64_t)sizeof(T)); }
+// whether an operand's rows (`cols` entries) can be copied straight into LDS: whole 16-byte words, and a tile's rows within 32 bits.  Across, rows beyond
+// the reduction's end have to be beyond the matrix, which they are not where its rows overlap or are one.
+template <typename T, bool ACROSS> bool copies(const void *p, int64_t ld, int64_t cols)
+{
+    return words<T>(p, ld) && cols % Kind<T>::V == 0 && ld < (1ll << 31) / (128 * (int64_t)sizeof(T)) && (!ACROSS || ld >= cols);
+}
 
 template <typename T, typename OUT, bool AX, bool BX, class C> hipError_t product_on(hts_seq_ctx &c, Product p)
 {
     const int64_t tn = ceil_div(p.N, C::BN), tiles = ceil_div(p.M, C::BM) * tn * p.slices;
-    const bool dma = copies<T>(p.a, p.lda, AX ? p.M : p.K) && copies<T>(p.b, p.ldb, BX ? p.N : p.K) && p.part_stride % Kind<T>::V == 0;
+    const bool dma = copies<T, AX>(p.a, p.lda, AX ? p.M : p.K) && copies<T, BX>(p.b, p.ldb, BX ? p.N : p.K) && p.part_stride % Kind<T>::V == 0;
     const dim3 grid((uint32_t)(ceil_div(tiles, 8) * 8)), block(C::WAVES * 64);
     if (dma) hipLaunchKernelGGL((product_kernel<T, OUT, AX, BX, C, true>), grid, block, 0, c.stream, p, (int)tn, (int)tiles);
     else hipLaunchKernelGGL((product_kernel<T, OUT, AX, BX, C, false>), grid, block, 0, c.stream, p, (int)tn, (int)tiles);

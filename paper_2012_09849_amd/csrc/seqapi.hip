@@ -49,18 +49,21 @@ static bool bad_precision(int32_t p) { return p != HTS_PRECISION_FP32 && p != HT
 static int size_of(int32_t precision) { return precision == HTS_PRECISION_BF16 ? 2 : 4; }
 static bool misaligned(const void *p, int size) { return (uintptr_t)p % size != 0; }
 
-// Rows of an array: `output` rows must not overlap.  A single row's stride says nothing.
-static int32_t check_rows(const hts_rows &r, int64_t rows, int64_t cols, int size, bool output)
+// Rows of an array: `output` rows must not overlap.  A single row's distance says nothing: it becomes one that suits every kernel.
+static int32_t check_rows(hts_rows &r, int64_t rows, int64_t cols, int size, bool output)
 {
     if (!r.p || misaligned(r.p, size) || r.ld < 0) return HTS_EINVAL;
+    if (rows == 1) r.ld = round_up(cols, 16);
     if (r.ld > (1ll << 40)) return HTS_ESHAPE;
     return output && rows > 1 && r.ld < cols ? HTS_EINVAL : HTS_OK;
 }
-static int32_t check_steps(const hts_steps &s, int64_t T, int64_t N, int64_t cols, int size, bool output)
+static int32_t check_steps(hts_steps &s, int64_t T, int64_t N, int64_t cols, int size, bool output)
 {
     if (!s.p || misaligned(s.p, size) || s.st < 0 || s.sn < 0) return HTS_EINVAL;
+    if (T == 1) s.st = 0;
+    if (N == 1) s.sn = 0;
     // (a few steps' distance is counted in 32 bits)
-    if ((T > 1 && s.st > (1ll << 24)) || s.sn > (1ll << 40)) return HTS_ESHAPE;
+    if (s.st > (1ll << 24) || s.sn > (1ll << 40)) return HTS_ESHAPE;
     if (!output) return HTS_OK;
     const bool by_step = (N == 1 || s.sn >= cols) && (T == 1 || s.st >= (N == 1 ? cols : s.sn * (N - 1) + cols));
     const bool by_sequence = (T == 1 || s.st >= cols) && (N == 1 || s.sn >= (T == 1 ? cols : s.st * (T - 1) + cols));
@@ -164,7 +167,7 @@ extern "C" int64_t hts_short_conv_workspace(const hts_short_conv_desc *d)
     return conv_workspace(d->T, d->N, d->D, d->W);
 }
 
-static int32_t check_conv_arrays(const hts_short_conv_desc *d, const hts_steps &x, const float *w, const float *bias, const int32_t *lengths, const float *state_in)
+static int32_t check_conv_arrays(const hts_short_conv_desc *d, hts_steps &x, const float *w, const float *bias, const int32_t *lengths, const float *state_in)
 {
     CHECK(check_steps(x, d->T, d->N, d->D, size_of(d->precision), false));
     return !w || misaligned(w, 4) || misaligned(bias, 4) || misaligned(lengths, 4) || misaligned(state_in, 4) ? HTS_EINVAL : HTS_OK;
@@ -227,9 +230,10 @@ extern "C" int64_t hts_selective_scan_states(const hts_scan_desc *d)
     return scan_states(*d);
 }
 
-static int32_t check_scan_arrays(const hts_scan_desc *d, const hts_scan_inputs *in)
+static int32_t check_scan_arrays(const hts_scan_desc *d, const hts_scan_inputs *given, hts_scan_inputs *in)
 {
-    if (!in) return HTS_EINVAL;
+    if (!given) return HTS_EINVAL;
+    *in = *given;
     const int s = size_of(d->precision);
     const int64_t pair = (int64_t)d->G * d->S;
     CHECK(check_steps(in->x, d->T, d->N, d->D, s, false)); CHECK(check_steps(in->dt, d->T, d->N, d->D, s, false));
@@ -242,34 +246,38 @@ extern "C" int32_t hts_selective_scan(hts_seq_ctx *ctx, const hts_scan_desc *d, 
 {
     if (!ctx) return HTS_EINVAL;
     CHECK(check_scan(d));
-    CHECK(check_scan_arrays(d, in));
+    ScanOp op = {};
+    op.d = *d;
+    CHECK(check_scan_arrays(d, in, &op.in));
     CHECK(check_steps(y, d->T, d->N, d->D, size_of(d->precision), true));
     if (misaligned(h_out, 4) || misaligned(states, 16)) return HTS_EINVAL;
     CHECK(check_workspace(ctx, scan_workspace(*d, false)));
-    ScanOp op = {};
-    op.d = *d; op.in = *in; op.y = y; op.h_out = h_out; op.states_out = states;
+    op.y = y; op.h_out = h_out; op.states_out = states;
     HIP_TRY(launch_scan(*ctx, op));
     return HTS_OK;
 }
 
 extern "C" int32_t hts_selective_scan_backward(hts_seq_ctx *ctx, const hts_scan_desc *d, const hts_scan_inputs *in, hts_steps dy,
-                                               const float *dh_out, const float *states, const hts_scan_grads *g)
+                                               const float *dh_out, const float *states, const hts_scan_grads *grads)
 {
-    if (!ctx || !g || !states) return HTS_EINVAL;
+    if (!ctx || !grads || !states) return HTS_EINVAL;
     CHECK(check_scan(d));
-    CHECK(check_scan_arrays(d, in));
+    ScanOp op = {};
+    op.d = *d;
+    CHECK(check_scan_arrays(d, in, &op.in));
+    hts_scan_grads *g = &op.g;
+    *g = *grads;
     const int s = size_of(d->precision);
     const int64_t pair = (int64_t)d->G * d->S;
     CHECK(check_steps(dy, d->T, d->N, d->D, s, false));
     CHECK(check_steps(g->dx, d->T, d->N, d->D, s, true)); CHECK(check_steps(g->ddt, d->T, d->N, d->D, s, true));
     CHECK(check_steps(g->dB, d->T, d->N, pair, s, true)); CHECK(check_steps(g->dC, d->T, d->N, pair, s, true));
-    if ((g->dz.p != nullptr) != (in->z.p != nullptr)) return HTS_EINVAL;
+    if ((g->dz.p != nullptr) != (op.in.z.p != nullptr)) return HTS_EINVAL;
     if (g->dz.p) CHECK(check_steps(g->dz, d->T, d->N, d->D, s, true));
     if (!g->dA || misaligned(g->dA, 4) || misaligned(g->dskip, 4) || misaligned(g->ddt_bias, 4) || misaligned(g->dh_in, 4)) return HTS_EINVAL;
     if (misaligned(states, 16) || misaligned(dh_out, 4) || (dh_out && g->dh_in == dh_out)) return HTS_EINVAL;
     CHECK(check_workspace(ctx, scan_workspace(*d, true)));
-    ScanOp op = {};
-    op.d = *d; op.in = *in; op.dy = dy; op.dh_out = dh_out; op.states = states; op.g = *g;
+    op.dy = dy; op.dh_out = dh_out; op.states = states;
     HIP_TRY(launch_scan_backward(*ctx, op));
     return HTS_OK;
 }
