@@ -8,6 +8,8 @@
 // slots) and four others for a state and step.
 //
 // Steps that are none (beyond a sequence's length) have delta = x = B = C = 0: a = 1, h stays.
+#include <algorithm>
+
 #include "seq.hpp"
 
 namespace hts {
@@ -911,7 +913,13 @@ template <typename T> hipError_t by_states(hts_seq_ctx &c, const ScanOp &op, boo
 }  // namespace
 
 int64_t scan_states(const hts_scan_desc &d) { return ceil_div(d.T, back_steps(d.S)) * d.N * d.D * padded(d.S); }
-int64_t scan_workspace(const hts_scan_desc &d, bool backward) { return 4 * layout(d, segments(d, 256, backward), backward).total; }
+// Enough for every shape of no more steps and sequences: fewer sequences are cut into more segments, at most two wavefronts a SIMD in all
+int64_t scan_workspace(const hts_scan_desc &d, bool backward)
+{
+    const int64_t most = std::min<int64_t>(std::min<int64_t>(d.T / 64, MOST_SEGMENTS) * d.N, 2048 / ((int64_t)places(d).waves * d.G)), rows = std::max<int64_t>(d.N, most);
+    const int64_t held = (int64_t)d.D * padded(d.S), cut = most > 1 ? (most + (backward ? 0 : std::min<int64_t>(d.N, most))) * held + round_up(most * d.D, 64) : 0;
+    return 4 * (cut + (backward ? round_up((int64_t)blocks_of(d) * d.T * d.N * d.G * 2 * padded(d.S), 64) + rows * d.D * (d.S + 2) : 0));
+}
 hipError_t launch_scan(hts_seq_ctx &c, const ScanOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? by_states<bf16_t>(c, op, false) : by_states<float>(c, op, false); }
 hipError_t launch_scan_backward(hts_seq_ctx &c, const ScanOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? by_states<bf16_t>(c, op, true) : by_states<float>(c, op, true); }
 

@@ -26,8 +26,9 @@ class State:
     """What N sequences carry from call to call: the convolution's last inputs and the scan's states (zeros: nothing remembered)."""
 
     def __init__(self, core, N):
-        self.conv = torch.zeros(N, core.width - 1, core.inner, device="cuda")
-        self.h = torch.zeros(N, core.inner, core.states, device="cuda")
+        with torch.cuda.stream(core.ctx.stream):               # where it is used
+            self.conv = torch.zeros(N, core.width - 1, core.inner, device="cuda")
+            self.h = torch.zeros(N, core.inner, core.states, device="cuda")
 
     def clone(self):
         other = object.__new__(State)
@@ -54,12 +55,13 @@ class MemoryCore:
         need = [hts.linear_workspace(M, n, k, precision=precision) for n, k in (self.shapes[w] for w in ("in.w", "proj.w", "dt.w", "out.w"))]
         need += [hts.short_conv_workspace(T, N, I, width, precision=precision), hts.selective_scan_workspace(T, N, I, S, precision=precision)]
         self.ctx = hts.SeqContext(max(need), stream=stream)
-        self.params = torch.zeros(self.P, device="cuda")
-        self.grads = torch.zeros(self.P, device="cuda")
-        self.p, self.g = self.views(self.params), self.views(self.grads)
-        self.m = dict(self.p) if precision == hts.PRECISION_FP32 else {n: torch.zeros(self.shapes[n], dtype=self.dtype, device="cuda") for n in ("in.w", "proj.w", "dt.w", "out.w")}
-        new = lambda *s: torch.empty(*s, dtype=self.dtype, device="cuda")  # noqa: E731
-        self._u, self._c, self._p, self._dt, self._v = new(M, 2 * I), new(M, I), new(M, R + 2 * S), new(M, I), new(M, I)
+        with torch.cuda.stream(self.ctx.stream):               # where they are used
+            self.params = torch.zeros(self.P, device="cuda")
+            self.grads = torch.zeros(self.P, device="cuda")
+            self.p, self.g = self.views(self.params), self.views(self.grads)
+            self.m = dict(self.p) if precision == hts.PRECISION_FP32 else {n: torch.zeros(self.shapes[n], dtype=self.dtype, device="cuda") for n in ("in.w", "proj.w", "dt.w", "out.w")}
+            new = lambda *s: torch.empty(*s, dtype=self.dtype, device="cuda")  # noqa: E731
+            self._u, self._c, self._p, self._dt, self._v = new(M, 2 * I), new(M, I), new(M, R + 2 * S), new(M, I), new(M, I)
         self._states, self._training = None, None
 
     def views(self, vector):
@@ -76,8 +78,9 @@ class MemoryCore:
         size = torch.exp(torch.rand(self.inner, generator=g) * 4.605 - 6.908)
         p["dt.b"].copy_(size + torch.log(-torch.expm1(-size)))
         p["skip"].fill_(1.0)
-        for name, t in p.items():
-            self.p[name].copy_(t)
+        with torch.cuda.stream(self.ctx.stream):
+            for name, t in p.items():
+                self.p[name].copy_(t)
         self.sync_params()
 
     def sync_params(self):
@@ -87,32 +90,39 @@ class MemoryCore:
                 for name, t in self.m.items():
                     t.copy_(self.p[name])
 
+    def _rows(self, a, shape, name):
+        """[T,N,F] as [T N, F], in its place."""
+        T, N, _ = shape
+        if not isinstance(a, torch.Tensor) or a.shape != shape or a.dtype is not self.dtype or (T > 1 and N > 1 and a.stride(0) != N * a.stride(1)):
+            raise hts.HtsError(f"{name}: expected a {self.dtype} device tensor of shape {tuple(shape)} whose rows are one distance apart")
+        return a.view(shape[0] * shape[1], shape[2])
+
     def _run(self, x, y, starts, lengths, state, states):
+        self._training = None                                   # what a call before this one kept is overwritten
         T, N, F = x.shape
         I, S, R, M = self.inner, self.states, self.rank, x.shape[0] * x.shape[1]
         if T > self.max_steps or N > self.max_rows or F != self.features:
             raise hts.HtsError(f"x: at most [{self.max_steps},{self.max_rows},{self.features}]")
-        c = self.ctx
+        c, xs, ys = self.ctx, self._rows(x, x.shape, "x"), self._rows(y, x.shape, "y")
         u, conv, p, dt, v = (a[:M] for a in (self._u, self._c, self._p, self._dt, self._v))
-        rows = lambda a: a.reshape(M, -1)  # noqa: E731
         steps = lambda a: a.view(T, N, a.shape[-1])  # noqa: E731
-        c.hts_linear(rows(x), self.m["in.w"], u, bias=self.p["in.b"])
+        c.hts_linear(xs, self.m["in.w"], u, bias=self.p["in.b"])
         c.hts_short_conv(steps(u)[:, :, :I], self.p["conv.w"], steps(conv), bias=self.p["conv.b"], act=hts.ACT_SILU, starts=starts, lengths=lengths, state_in=state.conv,
                          state_out=state.conv)
         c.hts_linear(conv, self.m["proj.w"], p)
         c.hts_linear(p[:, :R], self.m["dt.w"], dt)
         c.hts_selective_scan(steps(conv), steps(dt), self.p["A"], steps(p)[:, :, R:R + S], steps(p)[:, :, R + S:], steps(v), z=steps(u)[:, :, I:], skip=self.p["skip"],
                              dt_bias=self.p["dt.b"], starts=starts, lengths=lengths, h_in=state.h, h_out=state.h, states=states)
-        c.hts_linear(v, self.m["out.w"], rows(y), bias=self.p["out.b"], residual=rows(x))
+        c.hts_linear(v, self.m["out.w"], ys, bias=self.p["out.b"], residual=xs)
 
     def step(self, x, y, state, starts=None):
-        """One step of N sequences: x, y [N,F], starts u8 [N]; the state moves on in its place."""
+        """One step of N sequences: x, y [N,F], starts u8 [N]; the state moves on in its place.  (It takes the place of what a training call kept.)"""
         self._run(x[None], y[None], None if starts is None else starts[None], None, state, None)
 
     def forward(self, x, y, state, starts=None, lengths=None, train=False):
-        """T steps of N sequences: x, y [T,N,F] contiguous, starts u8 [T,N], lengths i32 [N]; the state moves on in its place.  train: what `backward` reads is
+        """T steps of N sequences: x, y [T,N,F], all rows one distance apart, starts u8 [T,N], lengths i32 [N]; the state moves on in its place.  train: what `backward` reads is
         kept until the next call."""
-        states, self._training = None, None
+        states = None
         if train:
             need = hts.selective_scan_states(x.shape[0], x.shape[1], self.inner, self.states)
             with torch.cuda.stream(self.ctx.stream):          # where they are used
@@ -134,12 +144,12 @@ class MemoryCore:
         I, S, R, M, c, g = self.inner, self.states, self.rank, x.shape[0] * x.shape[1], self.ctx, self.g
         u, conv, p, dt, v = (a[:M] for a in (self._u, self._c, self._p, self._dt, self._v))
         new = lambda k: torch.empty(M, k, dtype=self.dtype, device="cuda")  # noqa: E731
-        rows = lambda a: a.reshape(M, -1)  # noqa: E731
+        xs, dys, dxs = (self._rows(a, x.shape, name) for a, name in ((x, "x"), (dy, "dy"), (dx, "dx")))
         steps = lambda a: a.view(T, N, a.shape[-1])  # noqa: E731
         with torch.cuda.stream(self.ctx.stream):
             du, dconv, dp, ddt, dv = new(2 * I), new(I), new(R + 2 * S), new(I), new(I)
         seq = dict(starts=starts, lengths=lengths)
-        c.hts_linear_backward(v, self.m["out.w"], rows(dy), dx=dv, dw=g["out.w"], db=g["out.b"])
+        c.hts_linear_backward(v, self.m["out.w"], dys, dx=dv, dw=g["out.w"], db=g["out.b"])
         c.hts_selective_scan_backward(steps(conv), steps(dt), self.p["A"], steps(p)[:, :, R:R + S], steps(p)[:, :, R + S:], steps(dv), self._states, steps(dconv), steps(ddt),
                                       steps(dp)[:, :, R:R + S], steps(dp)[:, :, R + S:], g["A"], z=steps(u)[:, :, I:], dz=steps(du)[:, :, I:], skip=self.p["skip"],
                                       dskip=g["skip"], dt_bias=self.p["dt.b"], ddt_bias=g["dt.b"], h_in=begun.h, **seq)
@@ -147,7 +157,7 @@ class MemoryCore:
         c.hts_linear_backward(conv, self.m["proj.w"], dp, add=dconv, dx=dconv, dw=g["proj.w"])
         c.hts_short_conv_backward(steps(u)[:, :, :I], self.p["conv.w"], steps(dconv), steps(du)[:, :, :I], g["conv.w"], db=g["conv.b"], bias=self.p["conv.b"],
                                   act=hts.ACT_SILU, state_in=begun.conv, **seq)
-        c.hts_linear_backward(rows(x), self.m["in.w"], du, add=rows(dy), dx=rows(dx), dw=g["in.w"], db=g["in.b"])
+        c.hts_linear_backward(xs, self.m["in.w"], du, add=dys, dx=dxs, dw=g["in.w"], db=g["in.b"])
 
     def close(self):
         self.ctx.close()

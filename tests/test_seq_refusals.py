@@ -117,3 +117,15 @@ def test_binding_names_what_is_wrong():
         b._steps(torch.zeros(2, 2, 2), torch.float32, (2, 2, 2), "y")
     with pytest.raises(hts.HtsError, match="x:"):
         b._precision(torch.zeros(2, dtype=torch.float16), "x")
+
+
+def test_workspace_is_enough_for_less():
+    """A context for T steps of N sequences takes every smaller call: the sizes never fall as T or N grow."""
+    for D, S, G in ((1024, 16, 1), (40, 8, 1), (2048, 33, 2)):
+        size = lambda T, N: hts.selective_scan_workspace(T, N, D, S, G)  # noqa: E731
+        most = size(640, 40)
+        for N in range(1, 41):
+            for T in (1, 63, 64, 128, 200, 512, 639, 640):
+                assert size(T, N) <= size(T + 1, N) and size(T, N) <= size(T, N + 1) and size(T, N) <= most, (D, T, N)
+    for f in (lambda T, N: hts.linear_workspace(T * N, 96, 80, act=hts.ACT_SILU), lambda T, N: hts.short_conv_workspace(T, N, 200, 4)):
+        assert all(f(T, N) <= f(T + 1, N) and f(T, N) <= f(T, N + 1) for T in range(1, 130, 3) for N in (1, 2, 7, 30))
