@@ -813,17 +813,18 @@ __global__ __launch_bounds__(256) void pair_sum_kernel(const ScanOp p, const int
 Places places(const hts_scan_desc &d) { const int per = d.D / d.G; return Places{per, (int)ceil_div(per, 16)}; }
 int blocks_of(const hts_scan_desc &d) { return (int)ceil_div(places(d).waves, BWD_WAVES); }
 
-// Segments of a sequence: where its wavefronts leave units idle, as many as give two to a SIMD, of 64 steps at least, in whole chunks of either direction.
-// Forward the first pass costs two thirds of the second, so that up to three segments gain nothing; backward a fifth, and a lone wavefront waits for itself a third of
-// its time.  (On fewer compute units than 256 there are fewer segments: the workspace is for those.)
-constexpr int MOST_SEGMENTS = 64;
+// Segments of a sequence: where its wavefronts leave units idle, as many as give two to a SIMD, of 32 steps or so at least, in whole chunks of either direction.
+// Forward the first pass costs two thirds of the second and a launch, so that up to three segments gain nothing; backward a fifth, and a lone wavefront
+// waits for itself a third of its time.  129 steps of 5 sequences of 330 channels in binary32, five segments (segments of 64 steps at least: one and
+// two): forward 19.7 us (25.0), backward 28.2 (46.2).  (On fewer compute units than 256 there are fewer segments: the workspace is for those.)
+constexpr int MOST_SEGMENTS = 64, LEAST_STEPS = 24;        // (before they are made whole chunks)
 int segments_of(const hts_scan_desc &d, int cus, bool backward)
 {
     const int64_t waves = (int64_t)places(d).waves * d.G * d.N, units = 4ll * (cus < 256 ? cus : 256);
     int64_t count = 2 * units / waves;
-    if (count > d.T / 64) count = d.T / 64;
+    if (count > d.T / LEAST_STEPS) count = d.T / LEAST_STEPS;
     if (count > MOST_SEGMENTS) count = MOST_SEGMENTS;
-    if (count < (backward ? 2 : 4)) return 1;
+    if (count < (!backward ? 4 : d.T < 128 ? 3 : 2)) return 1;
     return (int)ceil_div(d.T, round_up(ceil_div(d.T, count), 16));
 }
 Segments segments(const hts_scan_desc &d, int cus, bool backward)
@@ -916,7 +917,7 @@ int64_t scan_states(const hts_scan_desc &d) { return ceil_div(d.T, back_steps(d.
 // Enough for every shape of no more steps and sequences: fewer sequences are cut into more segments, at most two wavefronts a SIMD in all
 int64_t scan_workspace(const hts_scan_desc &d, bool backward)
 {
-    const int64_t most = std::min<int64_t>(std::min<int64_t>(d.T / 64, MOST_SEGMENTS) * d.N, 2048 / ((int64_t)places(d).waves * d.G)), rows = std::max<int64_t>(d.N, most);
+    const int64_t most = std::min<int64_t>(std::min<int64_t>(d.T / LEAST_STEPS, MOST_SEGMENTS) * d.N, 2048 / ((int64_t)places(d).waves * d.G)), rows = std::max<int64_t>(d.N, most);
     const int64_t held = (int64_t)d.D * padded(d.S), cut = most > 1 ? (most + (backward ? 0 : std::min<int64_t>(d.N, most))) * held + round_up(most * d.D, 64) : 0;
     return 4 * (cut + (backward ? round_up((int64_t)blocks_of(d) * d.T * d.N * d.G * 2 * padded(d.S), 64) + rows * d.D * (d.S + 2) : 0));
 }
