@@ -87,44 +87,72 @@ template <typename T, bool ACROSS, int B, int THREADS> struct Staged {
     }
 };
 
-// The same tile copied straight into LDS by WAVES wavefronts: 1 KB an instruction.  The exchange of slots is in the lanes' addresses; a piece that
-// is not there gets an address beyond the matrix, which reads as zero.
+// 16 bytes a lane, memory -> LDS: lane l's land at lds + 16 l (one address for the wavefront).  Written out, since the compiler waits for every copy that it knows to
+// be on its way before a transposing LDS read, those of the k-tile after included; the kernel's own waits count them (rows of 8192, 512 x 2048: the
+// gradient of x 38 -> DXNEW us).
+typedef uint32_t Source __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void copy16(Source src, uint32_t lane, uint32_t all, const char *lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 : : "s"((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds), "v"(lane), "s"(src), "s"(all) : "memory", "m0");
+}
+
+// The same tile copied straight into LDS by WAVES wavefronts: 1 KB an instruction, k-tile after k-tile.  The exchange of slots is in the lanes' addresses; a
+// piece that is not there gets an address beyond the matrix, which reads as zero.  From k-tile to k-tile a few scalar additions (with the addresses formed
+// anew, 63 scalar instructions a k-tile: the gradient of x above 30.3 -> 27.0 us).
 template <typename T, bool ACROSS, int B, int WAVES> struct Copied {
     static constexpr int V = Kind<T>::V, BK = Kind<T>::BK, COPIES = B / 8 / WAVES, SLOTS = ACROSS ? B / V : BK / V;
+    static constexpr uint32_t BEYOND = 0xfffffff0u;
     static_assert(COPIES * 8 * WAVES == B, "tile");
     uint32_t at[COPIES];           // bytes from the tile's first row (along) or from the k-tile's (across)
-    int col[COPIES];               // along: k within the k-tile
-    const T *p;
-    int64_t ld;
-    int first, edge, K;
-    __device__ __forceinline__ void open(const T *p_, int64_t ld_, int first_, int edge_, int K_, int wave, int lane)
+    const char *start, *now;       // across: row 0 of the part, the k-tile's first row
+    int64_t step, all, left;       // across: bytes from k-tile to k-tile, of a part, from the k-tile's first row on
+    int64_t part;                  // bytes to the next part
+    int k0, K;
+    __device__ __forceinline__ void open(const T *p, int64_t ld, int first, int edge, int K_, int64_t part_stride, int part0, int k_first, int wave, int lane)
     {
-        p = p_; ld = ld_; first = first_; edge = edge_; K = K_;
+        K = K_; k0 = k_first;
+        part = part_stride * (int64_t)sizeof(T);
+        step = BK * ld * (int64_t)sizeof(T);
+        start = (const char *)p + part0 * part + (ACROSS ? 0 : first * ld * (int64_t)sizeof(T));
+        all = ACROSS ? ((K - 1) * ld + edge) * (int64_t)sizeof(T) : ((edge - 1 - first) * ld + K) * (int64_t)sizeof(T);
+        now = start + (ACROSS ? k0 / BK * step : 0);
+        left = all - (ACROSS ? k0 / BK * step : 0);
 #pragma unroll
         for (int i = 0; i < COPIES; ++i) {
             const int piece = (wave * COPIES + i) * 64 + lane, r = piece / SLOTS, phys = piece % SLOTS;
             const int s = ACROSS ? across_slot<T, B>(r, phys) : along_slot(r, phys);
-            col[i] = s * V;
             at[i] = (uint32_t)((r * ld + (ACROSS ? first : 0) + s * V) * (int64_t)sizeof(T));
-            if (ACROSS && first + s * V >= edge) at[i] = 0xfffffff0u;
+            if (ACROSS ? first + s * V >= edge : first + r >= edge) at[i] = BEYOND;
         }
     }
-    __device__ __forceinline__ void copy(int k0, char *lds, int wave, int64_t part) const
+    __device__ __forceinline__ void copy(char *lds, int wave, int lane)
     {
-        const int row = ACROSS ? k0 : first, rows = ACROSS ? K : edge;
-        const T *base = p + part + row * ld;
-        const int64_t bytes = ((rows - 1 - row) * ld + (ACROSS ? edge : K)) * (int64_t)sizeof(T);
-        const __amdgpu_buffer_rsrc_t src = dma_source(base, (uint32_t)(bytes < 0xfffffff0ll ? bytes : 0xfffffff0ll));
+        const uint64_t from = (uint64_t)(uintptr_t)now;
+        const Source src = {(uint32_t)from, (uint32_t)(from >> 32), (uint32_t)(left < (int64_t)BEYOND ? left : (int64_t)BEYOND), 0x00020000u};
+        const uint32_t off = ACROSS ? 0 : k0 * (int)sizeof(T);
+        char *to = lds + wave * COPIES * 1024;
+        if (ACROSS || k0 + BK <= K)
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            const uint32_t off = ACROSS ? at[i] : k0 + col[i] < K ? at[i] + (uint32_t)(k0 * (int)sizeof(T)) : 0xfffffff0u;
-            dma16(src, off, 0, (const bf16_t *)(lds + (wave * COPIES + i) * 1024));
+            for (int i = 0; i < COPIES; ++i) copy16(src, at[i], off, to + i * 1024);
+        else                       // the row ends in this k-tile
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                const int piece = (wave * COPIES + i) * 64 + lane, s = along_slot(piece / SLOTS, piece % SLOTS);
+                copy16(src, k0 + s * V < K ? at[i] : BEYOND, off, to + i * 1024);
+            }
+        k0 += BK;
+        if constexpr (ACROSS) {
+            if (k0 < K) { now += step; left -= step; }
+            else { k0 = 0; start += part; now = start; left = all; }
         }
     }
 };
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 *lds_quad;
+
+template <typename T> using Eight = Vec<T, 8>;
 
 // operands of a k-tile's kk-th part (16 k in bfloat16, 8 in binary32) for 32 entries from `at`
 template <typename T, bool ACROSS, int B> __device__ __forceinline__ Vec<T, Kind<T>::V> operand(const char *lds, int at, int kk, int lane)
@@ -135,10 +163,7 @@ template <typename T, bool ACROSS, int B> __device__ __forceinline__ Vec<T, Kind
         const char *q0 = lds + piece_at<T, true, B>(k, col >> 3) + (col & 7) * 2, *q1 = lds + piece_at<T, true, B>(k + 4, col >> 3) + (col & 7) * 2;
         const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad)(uintptr_t)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)q0);
         const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad)(uintptr_t)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)q1);
-        const short both[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        Vec<T, 8> r;
-        __builtin_memcpy(&r, both, 16);
-        return r;
+        return __builtin_bit_cast(Eight<T>, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
         Vec<T, 4> r;
         const int col = at + (lane & 31);
@@ -174,7 +199,12 @@ template <typename T> __device__ __forceinline__ void put8(T *p, const float (&v
         Vec<T, 8> r;
 #pragma unroll
         for (int i = 0; i < 8; ++i) r[i] = from_f32<T>(v[i]);
-        *reinterpret_cast<Vec<T, 8> *>(p) = r;
+        // (past the L2's lines: 8192 x 2048 outputs and pre-activations 40 -> 33 us, since the operands stay there)
+        typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+        u4 w[sizeof r / 16];
+        __builtin_memcpy(w, &r, sizeof r);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof r / 16); ++i) __builtin_nontemporal_store(w[i], reinterpret_cast<u4 *>(p) + i);
     } else
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i < count) p[i] = from_f32<T>(v[i]);
@@ -272,15 +302,15 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
     if constexpr (DMA) {
         Copied<T, AX, BM, WAVES> as;
         Copied<T, BX, BN, WAVES> bs;
-        as.open((const T *)p.a, p.lda, m0, p.M, p.K, wave, lane);
-        bs.open((const T *)p.b, p.ldb, n0, p.N, p.K, wave, lane);
-        auto fetch = [&](int t, int s) {
-            const int part = p.parts > 1 ? (first + t) / each : 0, k0 = (first + t - part * each) * BK;
-            as.copy(k0, tile + s * STAGE, wave, part * p.part_stride);
-            bs.copy(k0, tile + s * STAGE + BM * 128, wave, 0);
+        const int part0 = p.parts > 1 ? first / each : 0, k_first = (first - part0 * each) * BK;
+        as.open((const T *)p.a, p.lda, m0, p.M, p.K, p.part_stride, part0, k_first, wave, lane);
+        bs.open((const T *)p.b, p.ldb, n0, p.N, p.K, 0, 0, k_first, wave, lane);
+        auto fetch = [&](int s) {
+            as.copy(tile + s * STAGE, wave, lane);
+            bs.copy(tile + s * STAGE + BM * 128, wave, lane);
         };
 #pragma unroll
-        for (int s = 0; s < NS - 1; ++s) if (s < nt) fetch(s, s);
+        for (int s = 0; s < NS - 1; ++s) if (s < nt) fetch(s);
         auto step = [&](int t, auto u) {
             constexpr int S = decltype(u)::value;
             // this wavefront's copies of k-tile t have landed (later ones' may be on their way) and its reads of k-tile t - 1 are done
@@ -288,7 +318,7 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();              // everybody's
             asm volatile("" ::: "memory");
-            if (t + NS - 1 < nt) fetch(t + NS - 1, (S + NS - 1) % NS);
+            if (t + NS - 1 < nt) fetch((S + NS - 1) % NS);
             compute(tile + S * STAGE);
         };
         for (int t = 0; t < nt; t += NS) dma_steps(step, t, nt, std::make_integer_sequence<int, NS>{});
@@ -452,6 +482,7 @@ template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq
     auto tiles = [&](int m, int n) { return ceil_div(p.M, m) * ceil_div(columns, n) * p.slices; };
     hipError_t e;
     if (tiles(128, 128) >= 400) e = product_on<T, OUT, AX, BX, Tiling<128, 128, 2, 2, 1, 2>>(c, p);
+    else if (tiles(128, 128) >= 192) e = product_on<T, OUT, AX, BX, Tiling<128, 128, 2, 2, 2, 3>>(c, p);
     else if (tiles(64, 64) >= 192) e = product_on<T, OUT, AX, BX, Tiling<64, 64, 2, 2, 1, sizeof(T) == 2 ? 2 : 3>>(c, p);
     else if (tiles(64, 32) >= 192) e = product_on<T, OUT, AX, BX, Tiling<64, 32, 2, 1, 2, 3>>(c, p);
     else e = product_on<T, OUT, AX, BX, Tiling<32, 32, 1, 1, 4, 4>>(c, p);
