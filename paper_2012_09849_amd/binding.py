@@ -383,6 +383,7 @@ class Context:
 
 # ---- sequence memory --------------------------------------------------------------------------------------------------
 _DTYPE = {PRECISION_FP32: torch.float32, PRECISION_BF16: torch.bfloat16}
+_Tensor = torch.Tensor
 
 
 def _size(what: str, rc: int) -> int:
@@ -409,22 +410,23 @@ def selective_scan_states(T: int, N: int, D: int, S: int, G: int = 1) -> int:
     return _size("hts_selective_scan_states", load_library().hts_selective_scan_states(C.byref(_ScanDesc(T, N, D, S, G, PRECISION_FP32, 1))))
 
 
+# A small call's time is the host's, and these run for each of its operands: one look at a tensor's properties, no calls between them.
 def _precision(t, name, dims=None):
     if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16) or (dims is not None and t.dim() != dims):
         raise HtsError(f"{name}: expected a float32 or bfloat16 device tensor" + (f" of {dims} dimensions" if dims else ""))
     return PRECISION_BF16 if t.dtype is torch.bfloat16 else PRECISION_FP32
 
 
-def _is(t, dtype, shape, name, what=""):
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.shape == shape):
-        raise HtsError(f"{name}: expected a {what}{dtype} device tensor of shape {tuple(shape)}")
+def _wrong(dtype, shape, name, what=""):
+    return HtsError(f"{name}: expected a {what}{dtype} device tensor of shape {tuple(shape)}")
 
 
 def _rows(t, dtype, shape, name):
     """(address, distance of rows) of a [M, K] operand whose rows are contiguous, at any distance."""
     if t is None:
         return 0, 0
-    _is(t, dtype, shape, name)
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.is_cuda and t.shape == shape):
+        raise _wrong(dtype, shape, name)
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         raise HtsError(f"{name}: rows must be contiguous")
@@ -435,9 +437,10 @@ def _steps(t, dtype, shape, name):
     """(address, distances of steps and of sequences) of a [T, N, ...] operand whose steps are contiguous, at any distance."""
     if t is None:
         return 0, 0, 0
-    _is(t, dtype, shape, name)
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.is_cuda and t.shape == shape):
+        raise _wrong(dtype, shape, name)
     st = t.stride()
-    if st[-1] != 1 or len(st) > 3:
+    if len(st) > 3 or st[2] != 1:
         inner = 1
         for size, stride in zip(shape[:1:-1], st[:1:-1]):
             if stride != inner and size > 1:
@@ -447,12 +450,11 @@ def _steps(t, dtype, shape, name):
 
 
 def _array(t, dtype, shape, name):
-    """A contiguous array of that shape, or None."""
+    """The address of a contiguous array of that shape, 0 for None."""
     if t is None:
-        return None
-    _is(t, dtype, shape, name, "contiguous ")
-    if not t.is_contiguous():
-        raise HtsError(f"{name}: expected a contiguous {dtype} device tensor of shape {tuple(shape)}")
+        return 0
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous()):
+        raise _wrong(dtype, shape, name, "contiguous ")
     return t.data_ptr()
 
 
@@ -461,11 +463,12 @@ class _Arguments:
 
     def __init__(self, *kinds):
         size = sum(C.sizeof(k) for k in kinds)
-        self._memory, self._fill, self.of = bytearray(size), struct.Struct(f"{size // 8}q").pack_into, []
+        self._memory, self._fill, self.of = bytearray(size), struct.Struct(f"{size // 8}q").pack_into, []      # of: the structures, at: the first one's address
         at = 0
         for k in kinds:
             self.of.append(k.from_buffer(self._memory, at))
             at += C.sizeof(k)
+        self.at = C.byref(self.of[0])
 
     def set(self, *words):
         self._fill(self._memory, 0, *words)
@@ -565,20 +568,22 @@ class SeqContext:
         prec, f = _precision(x, "x", 3), torch.float32
         cells, S, ty = x.shape, A.shape[-1], _DTYPE[prec]
         T, N, D = cells
-        G = B.shape[2] if B.dim() == 4 else 1
-        pair, held = (T, N, G, S) if B.dim() == 4 else (T, N, S), (N, D, S)
+        G, held = 1, (N, D, S)
+        pair = (T, N, S)
+        if B.dim() == 4:
+            G = B.shape[2]
+            pair = (T, N, G, S)
         st, le = self._sequences(starts, lengths, T, N)
-        inputs = self._scan_in.set(*_steps(x, ty, cells, "x"), *_steps(dt, ty, cells, "dt"), *_steps(B, ty, pair, "B"), *_steps(C_, ty, pair, "C"), *_steps(z, ty, cells, "z"),
-                                   _array(A, f, (D, S), "A") or 0, _array(skip, f, (D,), "skip") or 0, _array(dt_bias, f, (D,), "dt_bias") or 0, st or 0, le or 0,
-                                   _array(h_in, f, held, "h_in") or 0)
-        return self._desc(_ScanDesc, T, N, D, S, G, prec, 1 if softplus else 0), C.byref(inputs[0]), ty, cells, pair, held, G
+        self._scan_in.set(*_steps(x, ty, cells, "x"), *_steps(dt, ty, cells, "dt"), *_steps(B, ty, pair, "B"), *_steps(C_, ty, pair, "C"), *_steps(z, ty, cells, "z"),
+                          _array(A, f, (D, S), "A"), _array(skip, f, (D,), "skip"), _array(dt_bias, f, (D,), "dt_bias"), st, le, _array(h_in, f, held, "h_in"))
+        return self._desc(_ScanDesc, T, N, D, S, G, prec, 1 if softplus else 0), self._scan_in.at, ty, cells, pair, held
 
     def hts_selective_scan(self, x, dt, A, B, C_, y, z=None, skip=None, dt_bias=None, softplus=True, starts=None, lengths=None, h_in=None, h_out=None,
                            states=None):
         """h_t = exp(delta A) h_{t-1} + delta x B, y = (C h + skip x) silu(z), delta = softplus(dt + dt_bias).  B, C: [T, N, S] or [T, N, G, S].  h_in and
         h_out may be one; states (selective_scan_states floats) is for a backward call."""
-        desc, inputs, ty, cells, _, held, G = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
-        if states is not None and states.numel() < selective_scan_states(*cells, held[2], G):
+        desc, inputs, ty, cells, _, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
+        if states is not None and states.numel() < self.lib.hts_selective_scan_states(desc):
             raise HtsError("states: too few entries (selective_scan_states)")
         rc = self.lib.hts_selective_scan(self._h, desc, inputs, self._one.set(*_steps(y, ty, cells, "y"))[0], _array(h_out, torch.float32, held, "h_out"),
                                          _ptr(states, torch.float32, "states"))
@@ -588,14 +593,14 @@ class SeqContext:
     def hts_selective_scan_backward(self, x, dt, A, B, C_, dy, states, dx, ddt, dB, dC, dA, z=None, dz=None, skip=None, dskip=None, dt_bias=None,
                                     ddt_bias=None, softplus=True, starts=None, lengths=None, h_in=None, dh_out=None, dh_in=None):
         """The gradients of dy and dh_out; states as the forward call on the same inputs left it."""
-        desc, inputs, ty, cells, pair, held, G = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
-        if states is None or states.numel() < selective_scan_states(*cells, held[2], G):
+        desc, inputs, ty, cells, pair, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
+        if states is None or states.numel() < self.lib.hts_selective_scan_states(desc):
             raise HtsError("states: too few entries (selective_scan_states)")
         f, (_, D, S) = torch.float32, held
-        grads = self._scan_grads.set(*_steps(dx, ty, cells, "dx"), *_steps(ddt, ty, cells, "ddt"), *_steps(dB, ty, pair, "dB"), *_steps(dC, ty, pair, "dC"),
-                                     *_steps(dz, ty, cells, "dz"), _array(dA, f, (D, S), "dA") or 0, _array(dskip, f, (D,), "dskip") or 0,
-                                     _array(ddt_bias, f, (D,), "ddt_bias") or 0, _array(dh_in, f, held, "dh_in") or 0)
+        self._scan_grads.set(*_steps(dx, ty, cells, "dx"), *_steps(ddt, ty, cells, "ddt"), *_steps(dB, ty, pair, "dB"), *_steps(dC, ty, pair, "dC"),
+                             *_steps(dz, ty, cells, "dz"), _array(dA, f, (D, S), "dA"), _array(dskip, f, (D,), "dskip"), _array(ddt_bias, f, (D,), "ddt_bias"),
+                             _array(dh_in, f, held, "dh_in"))
         rc = self.lib.hts_selective_scan_backward(self._h, desc, inputs, self._one.set(*_steps(dy, ty, cells, "dy"))[0], _array(dh_out, f, held, "dh_out"),
-                                                  _ptr(states, f, "states"), C.byref(grads[0]))
+                                                  _ptr(states, f, "states"), self._scan_grads.at)
         if rc:
             _check(rc, "hts_selective_scan_backward")
