@@ -795,13 +795,20 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
     }
 }
 
-// dB and dC from the workgroups' sums
+// dB and dC from the workgroups' sums, and, by the workgroups after those, dA, dskip and ddt_bias from the sequences' (one launch: 2 us less than two)
 template <typename T>
-__global__ __launch_bounds__(256) void pair_sum_kernel(const ScanOp p, const int blocks, const int SP, const float *part)
+__global__ __launch_bounds__(256) void sums_kernel(const ScanOp p, const int blocks, const int SP, const float *part, const int64_t pair_groups, const float *params, const int64_t rows)
 {
+    if (blockIdx.x >= pair_groups) {
+        __shared__ float sums[4][64];
+        const int64_t D = p.d.D, S = p.d.S;
+        sum_partials<4>(sums, blockIdx.x - pair_groups, params, rows, D * (S + 2), SumTarget{p.g.dA, D * S}, SumTarget{p.g.dskip, D}, SumTarget{p.g.ddt_bias, D});
+        return;
+    }
     const int64_t width = (int64_t)p.d.T * p.d.N * p.d.G * 2 * SP, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= width) return;
     float s = 0.0f;
+#pragma unroll 8
     for (int b = 0; b < blocks; ++b) s += part[b * width + i];
     const int r = (int)(i % (2 * SP)), k = r % SP;
     const int64_t at = i / (2 * SP), g = at % p.d.G, n = at / p.d.G % p.d.N, t = at / p.d.G / p.d.N;
@@ -890,8 +897,9 @@ template <typename T, int SL, bool WIDE> hipError_t scan_backward(hts_seq_ctx &c
     seg.state = (float *)c.ws + l.state; seg.sum = (float *)c.ws + l.sum;
     if (seg.count > 1) LAUNCH((scan_adjoint_kernel<T, SL, WIDE>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
     LAUNCH((scan_backward_kernel<T, SL, WIDE>), (int64_t)blocks * op.d.G * op.d.N * seg.count, 64 * BWD_WAVES, op, at, seg, blocks, pairs, params);
-    LAUNCH((pair_sum_kernel<T>), ceil_div(width, 256), 256, op, blocks, 4 * SL, pairs);
-    return launch_sum_partials(c, params, (int64_t)op.d.N * seg.count, D * (op.d.S + 2), SumTarget{op.g.dA, D * op.d.S}, SumTarget{op.g.dskip, D}, SumTarget{op.g.ddt_bias, D});
+    const int64_t pair_groups = ceil_div(width, 256);
+    LAUNCH((sums_kernel<T>), pair_groups + ceil_div(D * (op.d.S + 2), 64), 256, op, blocks, 4 * SL, pairs, pair_groups, params, (int64_t)op.d.N * seg.count);
+    return hipSuccess;
 }
 
 template <typename T, int SL> hipError_t run(hts_seq_ctx &c, const ScanOp &op, bool backward)

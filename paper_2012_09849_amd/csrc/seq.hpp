@@ -54,6 +54,31 @@ hipError_t launch_scan_backward(hts_seq_ctx &c, const ScanOp &op);
 // out = sum over p of part[p][0 .. width), in a fixed order; consecutive entries go to up to three arrays (p NULL: not wanted)
 struct SumTarget { float *p; int64_t n; };
 hipError_t launch_sum_partials(hts_seq_ctx &c, const float *part, int64_t parts, int64_t width, SumTarget a, SumTarget b, SumTarget d);
+// the same by a workgroup of ROWS wavefronts for 64 neighbouring entries: a wavefront takes every ROWS-th partial sum, 4 of them at a time
+template <int ROWS> __device__ __forceinline__ void sum_partials(float (&sums)[ROWS][64], const int64_t block, const float *part, const int64_t parts, const int64_t width, const SumTarget &a, const SumTarget &b, const SumTarget &d)
+{
+    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+    int64_t i = block * 64 + lane;
+    float s = 0.0f;
+    if (i < width) {
+        float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        int64_t k = row;
+        for (; k + 3 * ROWS < parts; k += 4 * ROWS)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) q[u] += part[(k + ROWS * u) * width + i];
+        for (int u = 0; k < parts; k += ROWS, ++u) q[u & 3] += part[k * width + i];
+        s = (q[0] + q[1]) + (q[2] + q[3]);
+    }
+    sums[row][lane] = s;
+    __syncthreads();
+    if (row || i >= width) return;
+    s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) s += sums[r][lane];
+    if (i < a.n) { if (a.p) a.p[i] = s; }
+    else if ((i -= a.n) < b.n) { if (b.p) b.p[i] = s; }
+    else if ((i -= b.n) < d.n) { if (d.p) d.p[i] = s; }
+}
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }

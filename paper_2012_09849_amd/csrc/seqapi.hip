@@ -10,31 +10,10 @@ using namespace hts;
 
 namespace hts {
 namespace {
-// 64 neighbouring entries a workgroup; 16 wavefronts take every sixteenth partial sum, 4 of them at a time
 __global__ __launch_bounds__(1024) void sum_partials_kernel(const float *part, const int64_t parts, const int64_t width, const SumTarget a, const SumTarget b, const SumTarget d)
 {
     __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
-    int64_t i = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (i < width) {
-        float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        int64_t k = row;
-        for (; k + 48 < parts; k += 64)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) q[u] += part[(k + 16 * u) * width + i];
-        for (int u = 0; k < parts; k += 16, ++u) q[u & 3] += part[k * width + i];
-        s = (q[0] + q[1]) + (q[2] + q[3]);
-    }
-    sums[row][lane] = s;
-    __syncthreads();
-    if (row || i >= width) return;
-    s = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s += sums[r][lane];
-    if (i < a.n) { if (a.p) a.p[i] = s; }
-    else if ((i -= a.n) < b.n) { if (b.p) b.p[i] = s; }
-    else if ((i -= b.n) < d.n) { if (d.p) d.p[i] = s; }
+    sum_partials<16>(sums, blockIdx.x, part, parts, width, a, b, d);
 }
 }  // namespace
 
