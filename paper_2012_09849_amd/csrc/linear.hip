@@ -30,9 +30,7 @@ struct Product {
     float *part;                   // slices > 1: [slice][M][N], then [M] for `rows`
     int64_t stride;                // entries from slice to slice, a multiple of 4
     int slices;
-    int words;                     // which of y, pre and res have rows of 16-byte words
 };
-enum { WORDS_Y = 1, WORDS_PRE = 2, WORDS_RES = 4 };
 
 template <typename T> struct Kind { static constexpr int V = 16 / sizeof(T), BK = 128 / sizeof(T); };       // entries of 16 bytes, k-tile
 
@@ -182,29 +180,31 @@ template <typename T> __device__ __forceinline__ f32x16 multiply(const Vec<T, Ki
     }
 }
 
-// 8 neighbouring entries of a row, as 16-byte words where they may be
-template <typename T> __device__ __forceinline__ void get8(float (&v)[8], const T *p, bool words, int count)
+// 8 neighbouring entries of a row, in 16-byte accesses at any address (entry by entry where rows were not whole words, 8192 x 1999 outputs and
+// pre-activations took 86 us, now 60)
+typedef uint32_t AnyWord __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T> __device__ __forceinline__ void get8(float (&v)[8], const T *p, int count)
 {
-    if (words && count >= 8) {
-        const Vec<T, 8> r = *reinterpret_cast<const Vec<T, 8> *>(p);
+    if (count >= 8) {
+        Vec<T, 8> r;
+        __builtin_memcpy(&r, p, sizeof r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = to_f32(r[i]);
     } else
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < count ? to_f32(p[i]) : 0.0f;
 }
-template <typename T> __device__ __forceinline__ void put8(T *p, const float (&v)[8], bool words, int count)
+template <typename T> __device__ __forceinline__ void put8(T *p, const float (&v)[8], int count)
 {
-    if (words && count >= 8) {
+    if (count >= 8) {
         Vec<T, 8> r;
 #pragma unroll
         for (int i = 0; i < 8; ++i) r[i] = from_f32<T>(v[i]);
         // (past the L2's lines: 8192 x 2048 outputs and pre-activations 40 -> 33 us, since the operands stay there)
-        typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-        u4 w[sizeof r / 16];
+        AnyWord w[sizeof r / 16];
         __builtin_memcpy(w, &r, sizeof r);
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof r / 16); ++i) __builtin_nontemporal_store(w[i], reinterpret_cast<u4 *>(p) + i);
+        for (int i = 0; i < (int)(sizeof r / 16); ++i) __builtin_nontemporal_store(w[i], reinterpret_cast<AnyWord *>(p) + i);
     } else
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i < count) p[i] = from_f32<T>(v[i]);
@@ -220,17 +220,17 @@ template <typename T, typename OUT> __device__ __forceinline__ void finish(const
     const int count = p.N - n;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += bias[i];
-    if (p.pre) put8((T *)p.pre + m * p.ldp + n, v, p.words & WORDS_PRE, count);
+    if (p.pre) put8((T *)p.pre + m * p.ldp + n, v, count);
     if (p.act == HTS_ACT_RELU) activate<HTS_ACT_RELU>(v);
     else if (p.act == HTS_ACT_SILU) activate<HTS_ACT_SILU>(v);
     else if (p.act == HTS_ACT_GELU) activate<HTS_ACT_GELU>(v);
     if (p.res) {
         float r[8];
-        get8(r, (const T *)p.res + m * p.ldr + n, p.words & WORDS_RES, count);
+        get8(r, (const T *)p.res + m * p.ldr + n, count);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
-    put8((OUT *)p.y + m * p.ldy + n, v, p.words & WORDS_Y, count);
+    put8((OUT *)p.y + m * p.ldy + n, v, count);
 }
 
 // Workgroups go to the eight dies in turn; a die gets neighbouring tiles, of a slice of the reduction and of a band of C, so that its L2 holds their operands.
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[4 * h + e] += w[e];
             }
-        if (p.slices > 1) put8(p.part + z * p.stride + (int64_t)m * p.N + n, v, (p.N & 3) == 0, p.N - n);
+        if (p.slices > 1) put8(p.part + z * p.stride + (int64_t)m * p.N + n, v, p.N - n);
         else finish<T, OUT>(p, m, n, v, bias);
     }
 }
@@ -479,7 +479,6 @@ template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq
     const int64_t total = ceil_div(p.K, BK) * p.parts;
     p.klen = (int)(ceil_div(total, slices) * BK);
     p.slices = (int)ceil_div(total * BK, p.klen);
-    p.words = (words<OUT>(p.y, p.ldy) ? WORDS_Y : 0) | (words<T>(p.pre, p.ldp) ? WORDS_PRE : 0) | (words<T>(p.res, p.ldr) ? WORDS_RES : 0);
     p.stride = round_up((int64_t)p.M * p.N + p.M, 4);
     auto tiles = [&](int m, int n) { return ceil_div(p.M, m) * ceil_div(columns, n) * p.slices; };
     hipError_t e;
