@@ -8,6 +8,10 @@
 // once more, so that rows leave as whole lines, with bias, activation and residual on the way.
 // Rows that are whole numbers of 16 bytes, at addresses that are, are copied straight into LDS (buffer_load ... lds), a k-tile ahead; others
 // through registers, entry by entry where a row ends.
+// What bounds it: 8192 x 2048 from 512 in bfloat16 with silu and its pre-activation, 30.7 us: 67 MB of outputs (13.5 us at the rate of a large copy), and
+// 268 MB of operands from L2 to LDS at 15 TB/s or so, which two workgroups a compute unit overlap in part; matrix units are busy for a fifth.  The gradient of x there
+// 26 us, of W 29 + 3.6, at the same rate from the L2.  Binary32 gradients of 1024 x 1024 x 512, 45 us: a wavefront alone on its SIMD, whose matrix
+// instructions (a third of its cycles), LDS reads and scalar instructions follow one another.
 #include "dmagemm.hpp"
 #include "seq.hpp"
 
@@ -87,7 +91,7 @@ template <typename T, bool ACROSS, int B, int THREADS> struct Staged {
 
 // 16 bytes a lane, memory -> LDS: lane l's land at lds + 16 l (one address for the wavefront).  Written out, since the compiler waits for every copy that it knows to
 // be on its way before a transposing LDS read, those of the k-tile after included; the kernel's own waits count them (rows of 8192, 512 x 2048: the
-// gradient of x 38 -> DXNEW us).
+// gradient of x 38.7 -> 30.3 us).
 typedef uint32_t Source __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void copy16(Source src, uint32_t lane, uint32_t all, const char *lds)
 {
@@ -481,6 +485,9 @@ template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq
     p.slices = (int)ceil_div(total * BK, p.klen);
     p.stride = round_up((int64_t)p.M * p.N + p.M, 4);
     auto tiles = [&](int m, int n) { return ceil_div(p.M, m) * ceil_div(columns, n) * p.slices; };
+    // The largest tiles that still give most compute units one: operands come from the L2 at a rate of its own, and the smaller the tiles the more of them.
+    // Two workgroups of four wavefronts a unit from 400 tiles on (8192 x 2048 from 512: 33.5 us, eight wavefronts 45, 64 x 64 tiles 55), eight wavefronts on three stages
+    // below (8192 x 512 from 2048 and its other gradient: 66.9, four wavefronts and four stages 76.6, 64 x 64 tiles 74.3).
     hipError_t e;
     if (tiles(128, 128) >= 400) e = product_on<T, OUT, AX, BX, Tiling<128, 128, 2, 2, 1, 2>>(c, p);
     else if (tiles(128, 128) >= 192) e = product_on<T, OUT, AX, BX, Tiling<128, 128, 2, 2, 2, 3>>(c, p);

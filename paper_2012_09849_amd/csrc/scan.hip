@@ -6,6 +6,9 @@
 // for NB neighbouring channels of a step, so that a chunk is one instruction an array, and step sizes, inputs and sums over the states pass between the
 // two orders through LDS, which also holds B and C, the same for all channels of a group, as binary32.  The work is vector instructions: exp2 (two issue
 // slots) and four others for a state and step.
+// What bounds it: issue.  512 x 16 x 1024 channels of 16 states in bfloat16, forward 67 us: a wavefront a SIMD that issues in 73 % of its cycles, 580 instructions for 16
+// steps, 384 slots of them the states'; a prompt of 8192 steps 33 + 53 us, two wavefronts a SIMD and 90 % of their cycles; backward 27 + 129, 72 %.
+// Twice as many segments (four wavefronts a SIMD) leave the prompt at 32 + 61.
 //
 // Steps that are none (beyond a sequence's length) have delta = x = B = C = 0: a = 1, h stays.
 #include <algorithm>
