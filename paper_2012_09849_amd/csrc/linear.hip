@@ -90,7 +90,9 @@ template <typename T, bool ACROSS, int B, int THREADS> struct Staged {
 };
 
 // 16 bytes a lane, memory -> LDS: lane l's land at lds + 16 l (one address for the wavefront).  Written out, since the compiler waits for every copy that it knows to
-// be on its way before a transposing LDS read, those of the k-tile after included; the kernel's own waits count them (rows of 8192, 512 x 2048: the
+// be on its way before a transposing LDS read, those of the k-tile after included; the kernel's own waits count them.  The compiler keeps no distances to
+// what is inside: m0 is written one wait state ahead, and a scalar that a vector instruction writes has to be five ahead, which none is
+// (tests/test_linear_copy_wait_states.py reads it from the built library).  (Rows of 8192, 512 x 2048: the
 // gradient of x 38.7 -> 30.3 us).
 typedef uint32_t Source __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void copy16(Source src, uint32_t lane, uint32_t all, const char *lds)
