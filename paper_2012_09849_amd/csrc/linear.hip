@@ -265,10 +265,15 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
     const int per_slice = p.slices > 1 ? tiles / p.slices : tiles, z = which / per_slice, in_slice = which % per_slice;
     const int m0 = in_slice / tiles_n * BM, n0 = in_slice % tiles_n * BN;
     const int each = (p.K + BK - 1) / BK, total = p.parts * each, first = z * (p.klen / BK), nt = min(total, first + p.klen / BK) - first;
-    // db: A times a matrix of ones, which needs no operand from LDS, by the wavefronts of C's first column tile
-    constexpr bool ROW_SUMS = AX && BX;
+    // db: from the operands of A that the wavefronts of C's first column tile have anyway.  bfloat16: times a matrix of ones (by additions they would take twice as
+    // long to unpack); binary32: added (dw of
+    // 1024 x 512 from 1024 rows 23.0 us with a matrix of ones, whose wavefronts had twice the others' products, now 17.2)
+    constexpr bool ROW_SUMS = AX && BX, BY_ONES = sizeof(T) == 2;
     const bool row_sums = ROW_SUMS && p.rows && n0 == 0 && wn == 0;
-    f32x16 acc[TM][TN], sum[ROW_SUMS ? TM : 1];
+    f32x16 acc[TM][TN], sum[ROW_SUMS && BY_ONES ? TM : 1];
+    float added[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) added[i] = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
 #pragma unroll
@@ -276,7 +281,7 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j][e] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < (ROW_SUMS ? TM : 1); ++i) sum[i][e] = 0.0f;
+        for (int i = 0; i < (ROW_SUMS && BY_ONES ? TM : 1); ++i) sum[i][e] = 0.0f;
     }
     // all of a k-tile's reads are issued before its products
     auto compute = [&](const char *stage) {
@@ -302,7 +307,10 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
 #pragma unroll
             for (int k = 0; k < 4 / KS; ++k)
 #pragma unroll
-                for (int i = 0; i < TM; ++i) sum[i] = multiply<T>(a[k][i], ones, sum[i]);
+                for (int i = 0; i < TM; ++i) {
+                    if constexpr (BY_ONES) sum[i] = multiply<T>(a[k][i], ones, sum[i]);
+                    else added[i] += (a[k][i][0] + a[k][i][1]) + (a[k][i][2] + a[k][i][3]);
+                }
         }
     };
     if constexpr (DMA) {
@@ -352,9 +360,13 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
     __syncthreads();
     if constexpr (ROW_SUMS) {
         if (p.rows && n0 == 0) {
-            if (wn == 0 && lane < 32)
 #pragma unroll
-                for (int i = 0; i < TM; ++i) sums[ks * BM + (wm * TM + i) * 32 + lane] = sum[i][0];
+            for (int i = 0; i < TM; ++i) {
+                float v = added[i];
+                if constexpr (BY_ONES) v = sum[i][0];
+                else v += __shfl_xor(v, 32);           // a lane has half of a row's k
+                if (wn == 0 && lane < 32) sums[ks * BM + (wm * TM + i) * 32 + lane] = v;
+            }
             __syncthreads();
             for (int r = tid; r < BM && m0 + r < p.M; r += THREADS) {
                 float v = 0.0f;
