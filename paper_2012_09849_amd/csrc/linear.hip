@@ -10,7 +10,7 @@
 // through registers, entry by entry where a row ends.
 // What bounds it: 8192 x 2048 from 512 in bfloat16 with silu and its pre-activation, 30.7 us: 67 MB of outputs (13.5 us at the rate of a large copy), and
 // 268 MB of operands from L2 to LDS at 15 TB/s or so, which two workgroups a compute unit overlap in part; matrix units are busy for a fifth.  The gradient of x there
-// 26 us, of W 29 + 3.6, at the same rate from the L2.  Binary32 gradients of 1024 x 1024 x 512, 45 us: a wavefront alone on its SIMD, whose matrix
+// 26 us, of W 29 + 3.6, at the same rate from the L2.  Binary32 gradients of 1024 x 1024 x 512, 39 us: a wavefront alone on its SIMD, whose matrix
 // instructions (a third of its cycles), LDS reads and scalar instructions follow one another.
 #include "dmagemm.hpp"
 #include "seq.hpp"
