@@ -258,7 +258,7 @@ int32_t     hts_stream_destroy(void *hip_stream);
  *
  * Layout: a row or step is contiguous in its last index and starts anywhere, the distance between rows is the caller's: parts of a
  * wider array (one projection that holds several operands) are read and written in place.  Strides count elements.  Strides of
- * inputs may be 0 (one row for all), steps are at most 2^24 entries apart (HTS_ESHAPE beyond); rows of an output must not overlap each other or any input, except where a comment allows it.
+ * inputs may be 0 (one row for all), steps are at most 2^24 entries apart (HTS_ESHAPE beyond); that of a single row, step or sequence is not read; rows of an output must not overlap each other or any input, except where a comment allows it.
  *
  * Sequences: `starts` u8 [T,N] or NULL: 1 = step t begins an episode, nothing from before it is seen.  Rows 1..T of a [T+1,N]
  * array of starts are the `dones` of hts_returns_gae.  `lengths` i32 [N] or NULL: sequence n has steps 0..lengths[n]-1 (less than
@@ -268,7 +268,8 @@ int32_t     hts_stream_destroy(void *hip_stream);
 typedef struct hts_seq_ctx hts_seq_ctx;
 
 /* workspace_bytes >= 0: device memory for the calls' intermediate results (partial sums of split reductions and the like).  A call
- * that needs more than the context has returns HTS_ESHAPE; the hts_*_workspace functions say how much a shape needs. */
+ * that needs more than the context has returns HTS_ESHAPE; the hts_*_workspace functions say how much a shape needs, which is enough for
+ * every shape with fewer rows (M), steps (T) or sequences (N) too. */
 int32_t hts_seq_create(int64_t workspace_bytes, void *hip_stream, hts_seq_ctx **out);
 int32_t hts_seq_destroy(hts_seq_ctx *ctx);
 
