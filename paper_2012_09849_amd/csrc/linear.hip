@@ -13,6 +13,7 @@
 // 26 us, of W 29 + 3.6, at the same rate from the L2.  Binary32 gradients of 1024 x 1024 x 512, 39 us: a wavefront alone on its SIMD, whose matrix
 // instructions (a third of its cycles), LDS reads and scalar instructions follow one another.
 #include "dmagemm.hpp"
+#include "linear_plan.hpp"
 #include "seq.hpp"
 
 namespace hts {
@@ -31,8 +32,8 @@ struct Product {
     void *y, *pre;
     int64_t ldr, ldy, ldp;
     float *rows;                   // receives A's own sums over the reduction (db), NULL: not wanted.  y NULL: nothing else is wanted
-    float *part;                   // slices > 1: [slice][M][N], then [M] for `rows`
-    int64_t stride;                // entries from slice to slice, a multiple of 4
+    float *part;                   // slices > 1: a slice's C, where y is wanted, and at rows_at its `rows`
+    int64_t rows_at, stride;       // entries; stride from slice to slice, a multiple of 4
     int slices;
 };
 
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(C::WAVES * 64, 2) void product_kernel(const Product
                 float v = 0.0f;
 #pragma unroll
                 for (int s = 0; s < KS; ++s) v += sums[s * BM + r];
-                (p.slices > 1 ? p.part + z * p.stride + (int64_t)p.M * p.N : p.rows)[m0 + r] = v;
+                (p.slices > 1 ? p.part + z * p.stride + p.rows_at : p.rows)[m0 + r] = v;
             }
             if (!p.y) return;
             __syncthreads();
@@ -460,18 +461,6 @@ __global__ __launch_bounds__(256) void slices_kernel(const float *part, const in
         }
 }
 
-// dw's reduction over the rows is cut where C has too few tiles for the compute units, into 8 k-tiles at least (16 in binary32, whose k-tiles are half as
-// deep): 8192 rows of 2048 x 512 and the slices' sums 28.9 + 3.6 us in four, 27.6 + 8.1
-// in eight; all gradients of 1024 rows through an activation 36 us with two, 41 with one.
-int slices_of(int64_t rows, int64_t N, int64_t K)
-{
-    const int64_t tiles = ceil_div(N, 128) * ceil_div(K, 128), most = ceil_div(rows, 512);
-    int64_t z = 256 / tiles;
-    if (z > 16) z = 16;
-    if (z > most) z = most;
-    return (int)(z < 1 ? 1 : z);
-}
-
 template <typename T> bool words(const void *p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * (int64_t)sizeof(T) % 16 == 0; }
 // whether an operand's rows (`cols` entries) can be copied straight into LDS: whole 16-byte words, and a tile's rows within 32 bits.  Across, rows beyond
 // the reduction's end have to be beyond the matrix, which they are not where its rows overlap or are one.
@@ -491,13 +480,9 @@ template <typename T, typename OUT, bool AX, bool BX, class C> hipError_t produc
 }
 
 // columns: C's, by which the tiles are chosen
-template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq_ctx &c, Product p, int slices, int columns)
+template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq_ctx &c, Product p, const Slices &slices, int columns)
 {
-    constexpr int BK = Kind<T>::BK;
-    const int64_t total = ceil_div(p.K, BK) * p.parts;
-    p.klen = (int)(ceil_div(total, slices) * BK);
-    p.slices = (int)ceil_div(total * BK, p.klen);
-    p.stride = round_up((int64_t)p.M * p.N + p.M, 4);
+    p.klen = slices.klen; p.slices = slices.count; p.rows_at = slices.rows; p.stride = slices.stride;
     auto tiles = [&](int m, int n) { return ceil_div(p.M, m) * ceil_div(columns, n) * p.slices; };
     // The largest tiles that still give most compute units one: operands come from the L2 at a rate of its own, and the smaller the tiles the more of them.
     // Two workgroups of four wavefronts a unit from 400 tiles on (8192 x 2048 from 512: 33.5 us, eight wavefronts 45, 64 x 64 tiles 55), eight wavefronts on three stages
@@ -509,21 +494,8 @@ template <typename T, typename OUT, bool AX, bool BX> hipError_t product(hts_seq
     else if (tiles(64, 32) >= 192) e = product_on<T, OUT, AX, BX, Tiling<64, 32, 2, 1, 2, 3>>(c, p);
     else e = product_on<T, OUT, AX, BX, Tiling<32, 32, 1, 1, 4, 4>>(c, p);
     if (e != hipSuccess || p.slices == 1) return e;
-    hipLaunchKernelGGL(slices_kernel, dim3((uint32_t)ceil_div(p.stride, 1024)), dim3(256), 0, c.stream, p.part, p.slices, p.stride, (float *)p.y, (int64_t)p.M * p.N, p.rows, p.M);
+    hipLaunchKernelGGL(slices_kernel, dim3((uint32_t)ceil_div(p.stride, 1024)), dim3(256), 0, c.stream, p.part, p.slices, p.stride, (float *)p.y, p.rows_at, p.rows, p.M);
     return hipGetLastError();
-}
-
-struct Layout { int64_t slope, stride, part, total; };       // bytes; stride: entries from part to part of an activation's gradient
-Layout layout(int size, int act, int64_t M, int64_t N, int64_t K)
-{
-    Layout l;
-    const bool some = act != HTS_ACT_NONE;
-    l.slope = 0;
-    l.stride = some ? round_up(M * N, 128) : 0;
-    l.part = l.stride * size * (size == 2 ? 3 : 1);
-    const int z = slices_of(M, N, K);
-    l.total = l.part + (z > 1 ? 4 * z * round_up(N * K + N, 4) : 0);
-    return l;
 }
 
 template <typename T> hipError_t forward(hts_seq_ctx &c, const LinearOp &op)
@@ -532,7 +504,7 @@ template <typename T> hipError_t forward(hts_seq_ctx &c, const LinearOp &op)
     p.parts = 1;
     p.a = op.x.p; p.lda = op.x.ld; p.b = op.w.p; p.ldb = op.w.ld; p.M = op.M; p.N = op.N; p.K = op.K;
     p.act = op.act; p.bias = op.bias; p.res = op.residual.p; p.ldr = op.residual.ld; p.y = op.y.p; p.ldy = op.y.ld; p.pre = op.pre.p; p.ldp = op.pre.ld;
-    return product<T, T, false, false>(c, p, 1, p.N);
+    return product<T, T, false, false>(c, p, cut(p.M, p.N, p.K, Kind<T>::BK, 1, 1, true), p.N);
 }
 
 template <typename T, int V> hipError_t slopes(hts_seq_ctx &c, const LinearOp &op, T *out, int64_t part)
@@ -546,7 +518,7 @@ template <typename T, int V> hipError_t slopes(hts_seq_ctx &c, const LinearOp &o
 
 template <typename T> hipError_t backward(hts_seq_ctx &c, const LinearOp &op)
 {
-    const Layout at = layout(sizeof(T), op.act, op.M, op.N, op.K);
+    const LinearLayout at = linear_layout(sizeof(T), op.act, op.M, op.N, op.K);
     const bool act = op.act != HTS_ACT_NONE;
     T *slope = (T *)(c.ws + at.slope);
     constexpr int V = Kind<T>::V;
@@ -562,23 +534,23 @@ template <typename T> hipError_t backward(hts_seq_ctx &c, const LinearOp &op)
         Product p = g;
         p.b = op.w.p; p.ldb = op.w.ld; p.M = op.M; p.N = op.K; p.K = op.N;
         p.res = op.add.p; p.ldr = op.add.ld; p.y = op.dx.p; p.ldy = op.dx.ld;
-        if ((e = product<T, T, false, true>(c, p, 1, p.N)) != hipSuccess) return e;
+        if ((e = product<T, T, false, true>(c, p, cut(p.M, p.N, p.K, Kind<T>::BK, 1, 1, true), p.N)) != hipSuccess) return e;
     }
     if (op.dw || op.db) {
         Product p = g;
-        const int z = slices_of(op.M, op.N, op.K);
-        p.parts = act && sizeof(T) == 2 ? 3 : 1; p.part_stride = at.stride; p.b = op.x.p; p.ldb = op.x.ld; p.M = op.N; p.N = op.K; p.K = op.M; p.y = op.dw; p.ldy = op.K; p.rows = op.db;
+        const Slices slices = weight_slices(sizeof(T), op.act, op.M, op.N, op.K, op.dw != nullptr);
+        p.parts = parts_of(sizeof(T), op.act); p.part_stride = at.stride; p.b = op.x.p; p.ldb = op.x.ld; p.M = op.N; p.N = weight_columns(sizeof(T), op.dw != nullptr, op.N, op.K); p.K = op.M; p.y = op.dw; p.ldy = op.K; p.rows = op.db;
         // without dw: one column tile, of any operand with as many rows (x may not be there), whose products go nowhere; the same slices and tiles, hence the same bits
-        if (!op.dw) { p.b = g.a; p.ldb = g.lda; p.N = op.N % V == 0 ? V : 1; }
-        p.part = z > 1 ? (float *)(c.ws + at.part) : nullptr;
-        e = product<T, float, true, true>(c, p, z, op.K);
+        if (!op.dw) { p.b = g.a; p.ldb = g.lda; }
+        p.part = slices.count > 1 ? (float *)(c.ws + at.part) : nullptr;
+        e = product<T, float, true, true>(c, p, slices, op.K);
     }
     return e;
 }
 
 }  // namespace
 
-int64_t linear_workspace(int precision, int act, int64_t M, int64_t N, int64_t K) { return layout(precision == HTS_PRECISION_BF16 ? 2 : 4, act, M, N, K).total; }
+int64_t linear_workspace(int precision, int act, int64_t M, int64_t N, int64_t K) { return linear_layout(precision == HTS_PRECISION_BF16 ? 2 : 4, act, M, N, K).total; }
 hipError_t launch_linear(hts_seq_ctx &c, int precision, const LinearOp &op) { return precision == HTS_PRECISION_BF16 ? forward<bf16_t>(c, op) : forward<float>(c, op); }
 hipError_t launch_linear_backward(hts_seq_ctx &c, int precision, const LinearOp &op) { return precision == HTS_PRECISION_BF16 ? backward<bf16_t>(c, op) : backward<float>(c, op); }
 
