@@ -10,7 +10,7 @@
 // steps, 384 slots of them the states'; a prompt of 8192 steps 33 + 53 us, two wavefronts a SIMD and 90 % of their cycles; backward 27 + 129, 72 %.
 // Twice as many segments (four wavefronts a SIMD) leave the prompt at 32 + 61.
 //
-// Steps that are none (beyond a sequence's length) have delta = x = B = C = 0: a = 1, h stays.
+// Steps that are none (beyond a sequence's length) do nothing, whatever the state: 0 times an infinite one would be NaN.  Chunks of them are passed over.
 #include <algorithm>
 
 #include "seq.hpp"
@@ -52,6 +52,16 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);          // vmcnt 63, expcnt 7, lgkmcnt 0
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+}
+
+// A chunk's steps, by what is in it: most chunks have no episode that begins and no end of the sequence, and ask nothing; a sequence ends once.  EACH: a copy for
+// episodes' beginnings alone, otherwise one for both (the gradients' main kernel, whose registers are full: 256 x 16 x 1024 channels of 32 states, both passes, 317 us,
+// with three copies 331; the other kernels three: 512 x 16 of 16 states 206 us, with two 210)
+template <bool EACH, class Pass> __device__ __forceinline__ void by_kind(const Pass &pass, bool fresh, bool ends)
+{
+    if (ends || (!EACH && fresh)) pass(std::integral_constant<int, 2>());
+    else if (EACH && fresh) pass(std::integral_constant<int, 1>());
+    else pass(std::integral_constant<int, 0>());
 }
 
 struct Places { int per_group, waves; };          // channels of a group, wavefronts (16 channels) of a group
@@ -222,7 +232,8 @@ struct Segments {
     float *h_in;                       // forward: [N][D][SP]: h_in once more, since h_out may be h_in
 };
 template <int SL> __device__ __forceinline__ int64_t state_at(int64_t row, int d, int D, int q) { return (row * D + d) * 4 * SL + q * SL; }
-// h over what the segments from `first` to before `last` (in steps of `way`) do to it.  (A real sum that is NaN gives NaN states of its own too.)
+// h over what the segments from `first` to before `last` (in steps of `way`) do to it.  (A real sum that is NaN gives NaN states of its own too; one of 0, of
+// a segment without steps, leaves h whatever A.)
 template <int SL> __device__ __forceinline__ void over_segments(float (&h)[SL], const Segments &seg, int first, int last, int way, int n, int N, int d, int D, int q, const float (&A)[SL])
 {
 #pragma unroll 4
@@ -231,7 +242,7 @@ template <int SL> __device__ __forceinline__ void over_segments(float (&h)[SL], 
         float own[SL];
         read_states<SL>(own, seg.state + state_at<SL>((int64_t)i * N + n, d, D, q));
 #pragma unroll
-        for (int s = 0; s < SL; ++s) h[s] = sum != sum ? own[s] : __builtin_fmaf(__builtin_amdgcn_exp2f(sum * A[s]), h[s], own[s]);
+        for (int s = 0; s < SL; ++s) h[s] = sum != sum ? own[s] : __builtin_fmaf(sum == 0.0f ? 1.0f : __builtin_amdgcn_exp2f(sum * A[s]), h[s], own[s]);
     }
 }
 
@@ -305,7 +316,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
     };
     float *pairs = shared[wave], *sizes = pairs + L * H::PAIR, *moves = sizes + X::SIZE, *outs = moves + X::SIZE;
     fetch(first);
-    for (int t0 = first; t0 < end; t0 += L) {
+    int t0 = first;
+    for (; t0 < live; t0 += L) {
         const bool some = t0 + cell.step < live;
         float xv[NB], size[NB], moved[NB], gate[NB];
         wave_order();
@@ -330,8 +342,9 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
         wave_order();
         fetch(t0 + L);
         const bool keep = !STATES && p.states_out;
-        // twice: chunks in which no episode begins, most of them, reset nothing
-        auto pass = [&](auto has) {
+        const int steps = live - t0;                                    // that there are, of the chunk's
+        auto pass = [&](auto kind) {
+            constexpr bool FRESH = decltype(kind)::value > 0, ENDS = decltype(kind)::value > 1;
             Ahead<H, !STATES> ahead(pairs + q * SL);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
@@ -342,13 +355,15 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
                     const int t = 4 * j + i;
                     ahead.next(t, +1);
                     if (t % KEEP == 0 && keep) { kept.store(h, on && t0 + t < p.d.T); kept.forth(); }
-                    if (decltype(has)::value && (fresh >> t & 1))
+                    if (FRESH && (fresh >> t & 1))
 #pragma unroll
                         for (int s = 0; s < SL; ++s) h[s] = 0.0f;
+                    const bool none = ENDS && t >= steps;
                     float y = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
-                        h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(de[i] * A[s]), h[s], dx[i] * ahead.B(t)[s]);
+                        const float next = __builtin_fmaf(__builtin_amdgcn_exp2f(de[i] * A[s]), h[s], dx[i] * ahead.B(t)[s]);
+                        h[s] = none ? h[s] : next;
                         if (!STATES) y = __builtin_fmaf(h[s], ahead.C(t)[s], y);
                     }
                     sums[i] = y;
@@ -356,7 +371,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
                 if (!STATES) outs[own * X::PITCH + 4 * j + q] = quad_deal(sums, q);
             }
         };
-        if (fresh) pass(std::true_type()); else pass(std::false_type());
+        by_kind<true>(pass, fresh, steps < L);
         if (!STATES) {
             wave_order();
             float y[NB];
@@ -368,6 +383,17 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
             ya.forth();
         }
     }
+    if (!STATES)                                                        // chunks without steps
+        for (; t0 < end; t0 += L) {
+            float y[NB];
+#pragma unroll
+            for (int e = 0; e < NB; ++e) y[e] = 0.0f;
+            ya.store(y, t0 + cell.step < p.d.T, cell);
+            ya.forth();
+            if (p.states_out)
+#pragma unroll
+                for (int t = 0; t < L; t += KEEP) { kept.store(h, on && t0 + t < p.d.T); kept.forth(); }
+        }
     if (STATES) {
         if (on) {
             float *out = seg.state + state_at<SL>((int64_t)k * N + n, d, D, q);
@@ -490,14 +516,15 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
     const int c = (block * BWD_WAVES + wave) * 16, D = p.d.D, S = p.d.S, TT = p.d.T, len = length_of(p.in.lengths, n, TT);
     const bool on = c + own < at.per_group;
     const int d0 = g * at.per_group + c, d = d0 + own;
-    const int lowest = k * seg.steps / L, highest = (min(TT, (k + 1) * seg.steps) + L - 1) / L - 1, last = highest * L;      // the segment's chunks
+    // the segment's chunks; beyond `top` they have no steps
+    const int lowest = k * seg.steps / L, highest = (min(TT, (k + 1) * seg.steps) + L - 1) / L - 1, top = min(highest, len > lowest * L ? (len - 1) / L : lowest - 1), last = top * L;
     Cell<H> cell;
     cell.open(lane, at.per_group - c);
     Track<T, H, WIDE> xa, da, za, ga, dxa, dda, dza;
     xa.open(p.in.x, n, d0, cell, last); da.open(p.in.dt, n, d0, cell, last); za.open(p.in.z, n, d0, cell, last); ga.open(p.dy, n, d0, cell, last);
-    dxa.open(p.g.dx, n, d0, cell, last); dda.open(p.g.ddt, n, d0, cell, last); dza.open(p.g.dz, n, d0, cell, last);
+    dxa.open(p.g.dx, n, d0, cell, highest * L); dda.open(p.g.ddt, n, d0, cell, highest * L); dza.open(p.g.dz, n, d0, cell, highest * L);
     Kept<SL> kept;
-    kept.open(p.states, p.d.N, n, D, d0, d, q, highest);
+    kept.open(p.states, p.d.N, n, D, d0, d, q, top);
     float skip[NB], bias[NB], dskip[NB], dbias[NB];
 #pragma unroll
     for (int e = 0; e < NB; ++e) {
@@ -554,8 +581,22 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
     };
     float *sizes = swaps[wave], *moves = sizes + X::SIZE, *rs = moves + X::SIZE, *raws = rs + X::SIZE, *sBs = raws + X::SIZE, *sds = sBs + X::SIZE;
     const int share = (2 * (lane >> 3 & 1) + (lane >> 2 & 1)) * PAIR + (lane >> 4 & 1) * SP + q * SL + (lane >> 5) * (SL / 2);
-    fetch(highest);
-    for (int chunk = highest, buf = 0; chunk >= lowest; --chunk, buf ^= 1) {
+    for (int chunk = highest; chunk > top; --chunk) {
+        float none[NB];
+#pragma unroll
+        for (int e = 0; e < NB; ++e) none[e] = 0.0f;
+        const bool there = chunk * L + cell.step < TT;
+        dxa.store(none, there, cell);
+        dda.store(none, there, cell);
+        dza.store(none, there, cell);
+        dxa.back(); dda.back(); dza.back();
+        if (mine < L && chunk * L + mine < TT) {
+            float *to = leaves + chunk * (L * row);
+            to[0] = to[1] = 0.0f;
+        }
+    }
+    fetch(top);
+    for (int chunk = top, buf = 0; chunk >= lowest; --chunk, buf ^= 1) {
         const int t0 = chunk * L;
         const bool some = t0 + cell.step < len;
         if (wave < 2) ps.put(in.pair, pairs[buf] + wave * SP);
@@ -584,11 +625,11 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
         const uint32_t fresh = Begins<L>::mask(in.begins);
         lds_barrier();
         fetch(chunk - 1);
-        if (chunk < highest) leave(chunk + 1, buf ^ 1);
+        if (chunk < top) leave(chunk + 1, buf ^ 1);
         const float *lds = pairs[buf];
-        // twice: chunks in which no episode begins, most of them, select nothing
-        auto pass = [&](auto has) {
-            constexpr bool FRESH = decltype(has)::value;
+        const int steps = len - t0;                                     // that there are, of the chunk's
+        auto pass = [&](auto kind) {
+            constexpr bool FRESH = decltype(kind)::value > 0, ENDS = decltype(kind)::value > 1;
             // (fences between four steps and the next: mixed, they take more registers than two wavefronts a SIMD have; 145 -> 123 us with the shares of dA)
             float a[L][SL], h[L][SL];
             {
@@ -625,16 +666,16 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
                 for (int i = 3; i >= 0; --i) {
                     const int t = 4 * j + i;
                     ahead.next(t, -1);
-                    const bool begin = FRESH && (fresh >> t & 1);
+                    const bool begin = FRESH && (fresh >> t & 1), none = ENDS && t >= steps;          // (of h only the steps before are read)
                     gB[i] = dd[i] = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
                         const float gk = __builtin_fmaf(rk[i], ahead.C(t)[s], ag[s]);
-                        val[2 * SL * i + s] = gk * dx[i];
-                        val[2 * SL * i + SL + s] = rk[i] * h[t][s];
+                        val[2 * SL * i + s] = none ? 0.0f : gk * dx[i];
+                        val[2 * SL * i + SL + s] = none ? 0.0f : rk[i] * h[t][s];
                         gB[i] = __builtin_fmaf(gk, ahead.B(t)[s], gB[i]);
-                        ag[s] = begin ? 0.0f : a[t][s] * gk;
-                        const float ga = begin ? 0.0f : ag[s] * (t ? h[t ? t - 1 : 0][s] : hb[s]);
+                        const float back = begin ? 0.0f : a[t][s] * gk, ga = begin || none ? 0.0f : back * (t ? h[t ? t - 1 : 0][s] : hb[s]);
+                        ag[s] = none ? ag[s] : back;
                         dd[i] = __builtin_fmaf(ga, A[s], dd[i]);
                         dA[s] = __builtin_fmaf(ga, de[i], dA[s]);
                         asm volatile("" : "+v"(dA[s]));          // (here and now: left to the compiler, a chunk's shares wait for its end, with all their factors)
@@ -650,7 +691,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
                 sds[own * X::PITCH + 4 * j + q] = quad_deal(dd, q);
             }
         };
-        if (fresh) pass(std::true_type()); else pass(std::false_type());
+        by_kind<false>(pass, fresh, steps < L);
         wave_order();
         float raw[NB], sB[NB], sd[NB], dx[NB], ddt[NB], dz[NB];
         X::get(raw, raws, cell);
@@ -673,7 +714,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
         wave_order();
     }
     lds_barrier();
-    leave(lowest, (highest - lowest) & 1);
+    if (top >= lowest) leave(lowest, (top - lowest) & 1);
     float *out = param_part + (int64_t)nk * D * (S + 2);
     if (on)
 #pragma unroll
@@ -707,7 +748,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
     const int k = row / N + 1, n = row % N, g = in_row / at.waves, c = in_row % at.waves * 16, q = lane & 3, own = lane >> 2;
     const int d0 = g * at.per_group + c, d = d0 + own, len = length_of(p.in.lengths, n, p.d.T);
     const bool on = c + own < at.per_group;
-    const int first = k * seg.steps, last = (min(p.d.T, first + seg.steps) + L - 1) / L * L - L;
+    const int first = k * seg.steps, last = len > first ? (min(len, first + seg.steps) + L - 1) / L * L - L : first - L;          // the last chunk with steps
     Cell<H> cell;
     cell.open(lane, at.per_group - c);
     Track<T, H, WIDE> da, za, ga;
@@ -765,7 +806,9 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
         cut |= fresh != 0;
         wave_order();
         fetch(t0 - L);
-        auto pass = [&](auto has) {
+        const int steps = len - t0;
+        auto pass = [&](auto kind) {
+            constexpr bool FRESH = decltype(kind)::value > 0, ENDS = decltype(kind)::value > 1;
             Ahead<H, false> ahead(pairs + q * SL);
 #pragma unroll
             for (int j = NB - 1; j >= 0; --j) {
@@ -774,16 +817,16 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
                 for (int i = 3; i >= 0; --i) {
                     const int t = 4 * j + i;
                     ahead.next(t, -1);
-                    const bool begin = decltype(has)::value && (fresh >> t & 1);
+                    const bool begin = FRESH && (fresh >> t & 1), none = ENDS && t >= steps;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
-                        const float gk = __builtin_fmaf(rk[i], ahead.B(t)[s], ag[s]);
-                        ag[s] = begin ? 0.0f : __builtin_amdgcn_exp2f(de[i] * A[s]) * gk;
+                        const float gk = __builtin_fmaf(rk[i], ahead.B(t)[s], ag[s]), back = begin ? 0.0f : __builtin_amdgcn_exp2f(de[i] * A[s]) * gk;
+                        ag[s] = none ? ag[s] : back;
                     }
                 }
             }
         };
-        if (fresh) pass(std::true_type()); else pass(std::false_type());
+        by_kind<true>(pass, fresh, steps < L);
     }
     if (on) {
         float *out = seg.state + state_at<SL>((int64_t)k * N + n, d, D, q);
