@@ -103,3 +103,54 @@ def test_scan_state_stays_whatever_its_decay(hts, T):
     torch.cuda.synchronize()
     assert torch.equal(h[1:], d["h_in"][1:]) and bool(torch.isfinite(y).all()) and bool(torch.isfinite(h).all())
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("T,N,D,W", [(40, 4, 20, 4), (1, 3, 72, 4), (17, 5, 33, 3), (8, 3, 64, 2), (3, 4, 128, 4)])
+def test_convolution_of_sequences_without_steps(hts, dtype, silu, T, N, D, W):
+    g = torch.Generator(device="cuda").manual_seed(T + D)
+    normal = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    x, dy, w, b, state, dstate = normal(T, N, D).to(dtype), normal(T, N, D).to(dtype), normal(D, W), normal(D), normal(N, W - 1, D), normal(N, W - 1, D)
+    lengths = torch.tensor([T, 0, max(1, T // 3), 0, T][:N], dtype=torch.int32, device="cuda")
+    idle, live = [n for n in range(N) if int(lengths[n]) == 0], [n for n in range(N) if int(lengths[n])]
+    ctx = hts.SeqContext(hts.short_conv_workspace(T, N, D, W))
+
+    def both(state, dstate):
+        like = lambda t: torch.full(t.shape, 7.0, dtype=t.dtype, device="cuda")  # noqa: E731
+        o = dict(y=like(x), state_out=like(state), dx=like(x), dw=like(w), db=like(b), dstate_in=like(state))
+        more = dict(bias=b, act=hts.ACT_SILU if silu else hts.ACT_NONE, lengths=lengths, state_in=state)
+        ctx.hts_short_conv(x, w, o["y"], state_out=o["state_out"], **more)
+        ctx.hts_short_conv_backward(x, w, dy, o["dx"], o["dw"], db=o["db"], dstate_out=dstate, dstate_in=o["dstate_in"], **more)
+        torch.cuda.synchronize()
+        return o
+    clean, bad, dbad = both(state, dstate), state.clone(), dstate.clone()
+    for k, n in enumerate(idle):
+        bad[n], dbad[n] = (INF, NAN) if k % 2 else (NAN, INF)
+    bad[1, :, ::2] = -INF
+    got = both(bad, dbad)
+    for k, v in got.items():
+        if k in ("state_out", "dstate_in"):
+            assert same(v[idle], (bad if k == "state_out" else dbad)[idle]) and torch.equal(v[live], clean[k][live]), k
+        else:
+            assert torch.equal(v, clean[k]), k
+    ctx.close()
+
+
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("W", [2, 3, 4])
+def test_convolution_beyond_an_end_that_is_not_finite(hts, silu, W):
+    """The last inputs of a sequence are NaN: the gradients of the steps beyond it are 0."""
+    T, N, D = 29, 3, 40
+    x, dy, w, state = (torch.randn(*s, device="cuda") for s in ((T, N, D), (T, N, D), (D, W), (N, W - 1, D)))
+    ends = [T, 11, 16]
+    x[ends[1] - 2:ends[1], 1], x[ends[2] - 1, 2] = NAN, INF
+    dx, dw = torch.full((T, N, D), 7.0, device="cuda"), torch.empty(D, W, device="cuda")
+    ctx = hts.SeqContext(hts.short_conv_workspace(T, N, D, W))
+    ctx.hts_short_conv_backward(x, w, dy, dx, dw, act=hts.ACT_SILU if silu else hts.ACT_NONE, lengths=torch.tensor(ends, dtype=torch.int32, device="cuda"), state_in=state,
+                                dstate_out=torch.randn(N, W - 1, D, device="cuda"))
+    torch.cuda.synchronize()
+    for n in range(N):
+        assert bool((dx[ends[n]:, n] == 0).all()), n
+    assert bool(torch.isfinite(dx[:, 0]).all())
+    ctx.close()
