@@ -10,6 +10,7 @@
 // steps, 384 slots of them the states'; a prompt of 8192 steps 33 + 53 us, two wavefronts a SIMD and 90 % of their cycles; backward 27 + 129, 72 %.
 // Twice as many segments (four wavefronts a SIMD) leave the prompt at 32 + 61.
 //
+// States beyond S and channels beyond the last are zeros all through; where infinities come, whose products with those would be NaN, a chunk selects.
 // Steps that are none (beyond a sequence's length) do nothing, whatever the state: 0 times an infinite one would be NaN.  Chunks of them are passed over.
 #include <algorithm>
 
@@ -54,15 +55,25 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-// A chunk's steps, by what is in it: most chunks have no episode that begins and no end of the sequence, and ask nothing; a sequence ends once.  EACH: a copy for
-// episodes' beginnings alone, otherwise one for both (the gradients' main kernel, whose registers are full: 256 x 16 x 1024 channels of 32 states, both passes, 317 us,
+// A chunk's steps, by what is in it: most chunks have no episode that begins, no end of the sequence and no infinities, and ask nothing; a sequence ends once.  EACH: a
+// copy for episodes' beginnings alone, otherwise one for all (the gradients' main kernel, whose registers are full: 256 x 16 x 1024 channels of 32 states, both passes, 317 us,
 // with three copies 331; the other kernels three: 512 x 16 of 16 states 206 us, with two 210)
-template <bool EACH, class Pass> __device__ __forceinline__ void by_kind(const Pass &pass, bool fresh, bool ends)
+template <bool EACH, class Pass> __device__ __forceinline__ void by_kind(const Pass &pass, bool fresh, bool odd)
 {
-    if (ends || (!EACH && fresh)) pass(std::integral_constant<int, 2>());
+    if (odd || (!EACH && fresh)) pass(std::integral_constant<int, 2>());
     else if (EACH && fresh) pass(std::integral_constant<int, 1>());
     else pass(std::integral_constant<int, 0>());
 }
+
+// how many of a lane's states exist, counted anew where it is asked for (kept, the comparisons with it would take scalar registers all through)
+template <int SL> __device__ __forceinline__ int states_of(int S, int q, bool on)
+{
+    int n = on ? S - q * SL : 0;
+    asm volatile("" : "+v"(n));
+    return n;
+}
+// zero, or NaN from the first value on that is not finite
+__device__ __forceinline__ void look(float &zero, float v) { zero = __builtin_fmaf(v, 0.0f, zero); }
 
 struct Places { int per_group, waves; };          // channels of a group, wavefronts (16 channels) of a group
 
@@ -233,7 +244,7 @@ struct Segments {
 };
 template <int SL> __device__ __forceinline__ int64_t state_at(int64_t row, int d, int D, int q) { return (row * D + d) * 4 * SL + q * SL; }
 // h over what the segments from `first` to before `last` (in steps of `way`) do to it.  (A real sum that is NaN gives NaN states of its own too; one of 0, of
-// a segment without steps, leaves h whatever A.)
+// a segment without steps, leaves h whatever A; a state of 0, as those beyond S are, is what the segment began from anyway, whatever its factors.)
 template <int SL> __device__ __forceinline__ void over_segments(float (&h)[SL], const Segments &seg, int first, int last, int way, int n, int N, int d, int D, int q, const float (&A)[SL])
 {
 #pragma unroll 4
@@ -242,14 +253,14 @@ template <int SL> __device__ __forceinline__ void over_segments(float (&h)[SL], 
         float own[SL];
         read_states<SL>(own, seg.state + state_at<SL>((int64_t)i * N + n, d, D, q));
 #pragma unroll
-        for (int s = 0; s < SL; ++s) h[s] = sum != sum ? own[s] : __builtin_fmaf(sum == 0.0f ? 1.0f : __builtin_amdgcn_exp2f(sum * A[s]), h[s], own[s]);
+        for (int s = 0; s < SL; ++s) h[s] = sum != sum || h[s] == 0.0f ? own[s] : __builtin_fmaf(sum == 0.0f ? 1.0f : __builtin_amdgcn_exp2f(sum * A[s]), h[s], own[s]);
     }
 }
 
 constexpr int FWD_WAVES = 4;
 
-// STATES: the first pass over segments, which needs neither C nor the gate and writes no output
-template <typename T, int SL, bool WIDE, bool STATES>
+// STATES: the first pass over segments, which needs neither C nor the gate and writes no output.  ABSENT: there are states beyond S
+template <typename T, int SL, bool WIDE, bool ABSENT, bool STATES>
 __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, const Places at, const Segments seg)
 {
     typedef Forth<SL> H;
@@ -319,7 +330,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
     int t0 = first;
     for (; t0 < live; t0 += L) {
         const bool some = t0 + cell.step < live;
-        float xv[NB], size[NB], moved[NB], gate[NB];
+        float xv[NB], size[NB], moved[NB], gate[NB], zero = 0.0f;
         wave_order();
         bs.put(in.b, pairs);
         if (!STATES) cs.put(in.c, pairs + SP);
@@ -332,6 +343,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
             softplus_f(v, soft, slope);
             size[e] = some ? p.d.softplus ? soft : v : 0.0f;
             moved[e] = size[e] * xv[e];
+            if (ABSENT) look(zero, moved[e]);
             const float open = STATES ? 1.0f : act_f<HTS_ACT_SILU>(in.z[e]);
             gate[e] = p.in.z.p ? open : 1.0f;
             sum[e] += size[e];
@@ -344,7 +356,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
         const bool keep = !STATES && p.states_out;
         const int steps = live - t0;                                    // that there are, of the chunk's
         auto pass = [&](auto kind) {
-            constexpr bool FRESH = decltype(kind)::value > 0, ENDS = decltype(kind)::value > 1;
+            constexpr bool FRESH = decltype(kind)::value > 0, ODD = decltype(kind)::value > 1;
+            const int exist = ABSENT && ODD ? states_of<SL>(S, q, on) : SL;
             Ahead<H, !STATES> ahead(pairs + q * SL);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
@@ -358,10 +371,10 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
                     if (FRESH && (fresh >> t & 1))
 #pragma unroll
                         for (int s = 0; s < SL; ++s) h[s] = 0.0f;
-                    const bool none = ENDS && t >= steps;
                     float y = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
+                        const bool none = ODD && (t >= steps || s >= exist);
                         const float next = __builtin_fmaf(__builtin_amdgcn_exp2f(de[i] * A[s]), h[s], dx[i] * ahead.B(t)[s]);
                         h[s] = none ? h[s] : next;
                         if (!STATES) y = __builtin_fmaf(h[s], ahead.C(t)[s], y);
@@ -371,7 +384,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_kernel(const ScanOp p, co
                 if (!STATES) outs[own * X::PITCH + 4 * j + q] = quad_deal(sums, q);
             }
         };
-        by_kind<true>(pass, fresh, steps < L);
+        by_kind<true>(pass, fresh, steps < L || (ABSENT && __ballot(zero != zero)));
         if (!STATES) {
             wave_order();
             float y[NB];
@@ -446,6 +459,7 @@ __global__ __launch_bounds__(256) void step_kernel(const ScanOp p)
         const float dx = size * x;
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
+            if (q * SL + s >= S) continue;
             h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(size * A[s]), fresh ? 0.0f : h[s], dx * B[s]);
             y = __builtin_fmaf(h[s], C[s], y);
         }
@@ -502,7 +516,8 @@ constexpr int BWD_WAVES = 4;
 //   g_t = r_t C_t + a_{t+1} g_{t+1},  dB = sum_d g delta x,  dC = sum_d r h,  d(delta) = sum_s g a h_{t-1} A + x sum_s g B,  dA = sum_t g a h_{t-1} delta
 // dB and dC of a workgroup's channels are added in LDS in a fixed order and leave as a partial sum a workgroup; dA, dskip and ddt_bias stay in
 // registers for the whole sequence.  At an episode's first step the products with a are 0, also where the other factor is not finite.
-template <typename T, int SL, bool WIDE>
+// ABSENT: there are states beyond S or channels beyond a group's last
+template <typename T, int SL, bool WIDE, bool ABSENT>
 __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const ScanOp p, const Places at, const Segments seg, const int blocks, float *pair_part, float *param_part)
 {
     typedef Back<SL> H;
@@ -600,6 +615,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
         const int t0 = chunk * L;
         const bool some = t0 + cell.step < len;
         if (wave < 2) ps.put(in.pair, pairs[buf] + wave * SP);
+        float zero = 0.0f;
         float xv[NB], size[NB], slope[NB], r[NB], zf[NB], hb[SL];
         {
             float moved[NB];
@@ -614,6 +630,10 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
                 moved[e] = size[e] * xv[e];
                 const float dy = in.dy[e], z = in.z[e], open = act_f<HTS_ACT_SILU>(z);
                 r[e] = dy * (p.in.z.p ? open : 1.0f);
+                if (ABSENT) {
+                    look(zero, moved[e]);
+                    look(zero, r[e]);
+                }
                 zf[e] = dy * act_slope<HTS_ACT_SILU>(z);
             }
             X::put(sizes, cell, size);
@@ -627,9 +647,14 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
         fetch(chunk - 1);
         if (chunk < top) leave(chunk + 1, buf ^ 1);
         const float *lds = pairs[buf];
+        // states beyond S meet what is their channel's, absent channels B and C, which are every channel's
+        if (ABSENT && c + 16 > at.per_group)
+#pragma unroll
+            for (int i = 0; i < L * PAIR; i += 64) look(zero, lds[i + lane]);
         const int steps = len - t0;                                     // that there are, of the chunk's
         auto pass = [&](auto kind) {
-            constexpr bool FRESH = decltype(kind)::value > 0, ENDS = decltype(kind)::value > 1;
+            constexpr bool FRESH = decltype(kind)::value > 0, ODD = decltype(kind)::value > 1;
+            const int exist = ABSENT && ODD ? states_of<SL>(S, q, on) : SL;
             // (fences between four steps and the next: mixed, they take more registers than two wavefronts a SIMD have; 145 -> 123 us with the shares of dA)
             float a[L][SL], h[L][SL];
             {
@@ -649,6 +674,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
                         for (int s = 0; s < SL; ++s) {
                             a[t][s] = __builtin_amdgcn_exp2f(de[i] * A[s]);
                             h[t][s] = __builtin_fmaf(a[t][s], begin ? 0.0f : t ? h[t ? t - 1 : 0][s] : hb[s], dx[i] * ahead.B(t)[s]);
+                            if (ODD && s >= exist) h[t][s] = 0.0f;
                             sum = __builtin_fmaf(h[t][s], ahead.C(t)[s], sum);
                         }
                         part[i] = sum;
@@ -666,18 +692,20 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
                 for (int i = 3; i >= 0; --i) {
                     const int t = 4 * j + i;
                     ahead.next(t, -1);
-                    const bool begin = FRESH && (fresh >> t & 1), none = ENDS && t >= steps;          // (of h only the steps before are read)
+                    const bool begin = FRESH && (fresh >> t & 1);
                     gB[i] = dd[i] = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
+                        // (of h only the steps before are read)
+                        const bool no = ODD && s >= exist, none = no || (ODD && t >= steps);
                         const float gk = __builtin_fmaf(rk[i], ahead.C(t)[s], ag[s]);
                         val[2 * SL * i + s] = none ? 0.0f : gk * dx[i];
                         val[2 * SL * i + SL + s] = none ? 0.0f : rk[i] * h[t][s];
-                        gB[i] = __builtin_fmaf(gk, ahead.B(t)[s], gB[i]);
+                        gB[i] = no ? gB[i] : __builtin_fmaf(gk, ahead.B(t)[s], gB[i]);
                         const float back = begin ? 0.0f : a[t][s] * gk, ga = begin || none ? 0.0f : back * (t ? h[t ? t - 1 : 0][s] : hb[s]);
                         ag[s] = none ? ag[s] : back;
-                        dd[i] = __builtin_fmaf(ga, A[s], dd[i]);
-                        dA[s] = __builtin_fmaf(ga, de[i], dA[s]);
+                        dd[i] = no ? dd[i] : __builtin_fmaf(ga, A[s], dd[i]);
+                        dA[s] = no ? dA[s] : __builtin_fmaf(ga, de[i], dA[s]);
                         asm volatile("" : "+v"(dA[s]));          // (here and now: left to the compiler, a chunk's shares wait for its end, with all their factors)
                     }
                 }
@@ -691,7 +719,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
                 sds[own * X::PITCH + 4 * j + q] = quad_deal(dd, q);
             }
         };
-        by_kind<false>(pass, fresh, steps < L);
+        by_kind<false>(pass, fresh, steps < L || (ABSENT && __ballot(zero != zero)));
         wave_order();
         float raw[NB], sB[NB], sd[NB], dx[NB], ddt[NB], dz[NB];
         X::get(raw, raws, cell);
@@ -734,7 +762,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_backward_kernel(const 
 
 // The first pass over segments, from the last to the second: the gradient that a segment's own outputs (and, the last one, dh_out) give to the state
 // before it
-template <typename T, int SL, bool WIDE>
+template <typename T, int SL, bool WIDE, bool ABSENT>
 __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const ScanOp p, const Places at, const Segments seg)
 {
     typedef Forth<SL> H;
@@ -788,7 +816,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
     fetch(last);
     for (int t0 = last; t0 >= first; t0 -= L) {
         const bool some = t0 + cell.step < len;
-        float size[NB], r[NB];
+        float size[NB], r[NB], zero = 0.0f;
         wave_order();
         cs.put(in.c, pairs);
         const uint32_t fresh = Begins<L>::mask(in.begins);
@@ -799,6 +827,10 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
             softplus_f(v, soft, slope);
             size[e] = some ? p.d.softplus ? soft : v : 0.0f;
             r[e] = in.dy[e] * (p.in.z.p ? open : 1.0f);
+            if (ABSENT) {
+                look(zero, r[e]);
+                look(zero, size[e]);
+            }
             sum[e] += size[e];
         }
         X::put(sizes, cell, size);
@@ -808,7 +840,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
         fetch(t0 - L);
         const int steps = len - t0;
         auto pass = [&](auto kind) {
-            constexpr bool FRESH = decltype(kind)::value > 0, ENDS = decltype(kind)::value > 1;
+            constexpr bool FRESH = decltype(kind)::value > 0, ODD = decltype(kind)::value > 1;
+            const int exist = ABSENT && ODD ? states_of<SL>(S, q, on) : SL;
             Ahead<H, false> ahead(pairs + q * SL);
 #pragma unroll
             for (int j = NB - 1; j >= 0; --j) {
@@ -817,16 +850,17 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void scan_adjoint_kernel(const Scan
                 for (int i = 3; i >= 0; --i) {
                     const int t = 4 * j + i;
                     ahead.next(t, -1);
-                    const bool begin = FRESH && (fresh >> t & 1), none = ENDS && t >= steps;
+                    const bool begin = FRESH && (fresh >> t & 1);
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
+                        const bool none = ODD && (t >= steps || s >= exist);
                         const float gk = __builtin_fmaf(rk[i], ahead.B(t)[s], ag[s]), back = begin ? 0.0f : __builtin_amdgcn_exp2f(de[i] * A[s]) * gk;
                         ag[s] = none ? ag[s] : back;
                     }
                 }
             }
         };
-        by_kind<true>(pass, fresh, steps < L);
+        by_kind<true>(pass, fresh, steps < L || (ABSENT && __ballot(zero != zero)));
     }
     if (on) {
         float *out = seg.state + state_at<SL>((int64_t)k * N + n, d, D, q);
@@ -920,19 +954,19 @@ template <typename T> bool wide(const ScanOp &op, bool backward)
         if (e_ != hipSuccess) return e_;                                                                                                                  \
     } while (0)
 
-template <typename T, int SL, bool WIDE> hipError_t scan(hts_seq_ctx &c, const ScanOp &op)
+template <typename T, int SL, bool WIDE, bool ABSENT> hipError_t scan(hts_seq_ctx &c, const ScanOp &op)
 {
     const Places at = places(op.d);
     Segments seg = segments(op.d, c.cus, false);
     const Layout l = layout(op.d, seg, false);
     const int64_t waves = (int64_t)at.waves * op.d.G * op.d.N;
     seg.h_in = (float *)c.ws + l.h_in; seg.state = (float *)c.ws + l.state; seg.sum = (float *)c.ws + l.sum;
-    if (seg.count > 1) LAUNCH((scan_kernel<T, SL, WIDE, true>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
-    LAUNCH((scan_kernel<T, SL, WIDE, false>), ceil_div(waves * seg.count, FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
+    if (seg.count > 1) LAUNCH((scan_kernel<T, SL, WIDE, ABSENT, true>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
+    LAUNCH((scan_kernel<T, SL, WIDE, ABSENT, false>), ceil_div(waves * seg.count, FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
     return hipSuccess;
 }
 
-template <typename T, int SL, bool WIDE> hipError_t scan_backward(hts_seq_ctx &c, const ScanOp &op)
+template <typename T, int SL, bool WIDE, bool ABSENT> hipError_t scan_backward(hts_seq_ctx &c, const ScanOp &op)
 {
     const Places at = places(op.d);
     Segments seg = segments(op.d, c.cus, true);
@@ -941,8 +975,8 @@ template <typename T, int SL, bool WIDE> hipError_t scan_backward(hts_seq_ctx &c
     const int blocks = blocks_of(op.d);
     float *pairs = (float *)c.ws + l.pairs, *params = (float *)c.ws + l.params;
     seg.state = (float *)c.ws + l.state; seg.sum = (float *)c.ws + l.sum;
-    if (seg.count > 1) LAUNCH((scan_adjoint_kernel<T, SL, WIDE>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
-    LAUNCH((scan_backward_kernel<T, SL, WIDE>), (int64_t)blocks * op.d.G * op.d.N * seg.count, 64 * BWD_WAVES, op, at, seg, blocks, pairs, params);
+    if (seg.count > 1) LAUNCH((scan_adjoint_kernel<T, SL, WIDE, ABSENT>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
+    LAUNCH((scan_backward_kernel<T, SL, WIDE, ABSENT>), (int64_t)blocks * op.d.G * op.d.N * seg.count, 64 * BWD_WAVES, op, at, seg, blocks, pairs, params);
     const int64_t pair_groups = ceil_div(width, 256);
     LAUNCH((sums_kernel<T>), pair_groups + ceil_div(D * (op.d.S + 2), 64), 256, op, blocks, 4 * SL, pairs, pair_groups, params, (int64_t)op.d.N * seg.count);
     return hipSuccess;
@@ -950,8 +984,17 @@ template <typename T, int SL, bool WIDE> hipError_t scan_backward(hts_seq_ctx &c
 
 template <typename T, int SL> hipError_t run(hts_seq_ctx &c, const ScanOp &op, bool backward)
 {
-    if (backward) return wide<T>(op, true) ? scan_backward<T, SL, true>(c, op) : scan_backward<T, SL, false>(c, op);
-    if (op.d.T > 1) return wide<T>(op, false) ? scan<T, SL, true>(c, op) : scan<T, SL, false>(c, op);
+    // kernels that look for infinities where there are states or channels that do not exist: others have no use for it (512 x 16 both ways 206 us, looking 214; of
+    // more than 32 states there are these alone)
+    const bool states = SL == 16 || op.d.S < 4 * SL, absent = states || places(op.d).per_group % (16 * BWD_WAVES) != 0;
+    if (backward) {
+        if (absent) return wide<T>(op, true) ? scan_backward<T, SL, true, true>(c, op) : scan_backward<T, SL, false, true>(c, op);
+        return wide<T>(op, true) ? scan_backward<T, SL, true, SL == 16>(c, op) : scan_backward<T, SL, false, SL == 16>(c, op);
+    }
+    if (op.d.T > 1) {
+        if (states) return wide<T>(op, false) ? scan<T, SL, true, true>(c, op) : scan<T, SL, false, true>(c, op);
+        return wide<T>(op, false) ? scan<T, SL, true, SL == 16>(c, op) : scan<T, SL, false, SL == 16>(c, op);
+    }
     LAUNCH((step_kernel<T, SL>), ceil_div((int64_t)op.d.N * op.d.D, 64), 256, op);
     return hipSuccess;
 }
