@@ -244,16 +244,22 @@ struct Segments {
 };
 template <int SL> __device__ __forceinline__ int64_t state_at(int64_t row, int d, int D, int q) { return (row * D + d) * 4 * SL + q * SL; }
 // h over what the segments from `first` to before `last` (in steps of `way`) do to it.  (A real sum that is NaN gives NaN states of its own too; one of 0, of
-// a segment without steps, leaves h whatever A; a state of 0, as those beyond S are, is what the segment began from anyway, whatever its factors.)
+// a segment without steps, leaves h whatever A.)
 template <int SL> __device__ __forceinline__ void over_segments(float (&h)[SL], const Segments &seg, int first, int last, int way, int n, int N, int d, int D, int q, const float (&A)[SL])
 {
 #pragma unroll 4
     for (int i = first; i != last; i += way) {
         const float sum = seg.sum[((int64_t)i * N + n) * D + d];
+        // exp(sum A) in two factors, since it may be beyond binary32's range where the state times it is not.  Finite, for the sake of states of 0 (those beyond S, too), and
+        // not 0 for infinite ones, which no finite step size takes away
+        const float least = sum == 0.0f ? 1.0f : __builtin_fabsf(sum) < __builtin_inff() ? 0x1p-126f : 0.0f;
         float own[SL];
         read_states<SL>(own, seg.state + state_at<SL>((int64_t)i * N + n, d, D, q));
 #pragma unroll
-        for (int s = 0; s < SL; ++s) h[s] = sum != sum || h[s] == 0.0f ? own[s] : __builtin_fmaf(sum == 0.0f ? 1.0f : __builtin_amdgcn_exp2f(sum * A[s]), h[s], own[s]);
+        for (int s = 0; s < SL; ++s) {
+            const float half = fminf(fmaxf(__builtin_amdgcn_exp2f(0.5f * sum * A[s]), least), 0x1.fffffep+127f);
+            h[s] = sum != sum ? own[s] : __builtin_fmaf(h[s] * half, half, own[s]);
+        }
     }
 }
 

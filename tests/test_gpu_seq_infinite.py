@@ -1,8 +1,10 @@
 """Infinities within the scan's sequences, where every number is positive so that the formula gives infinities and never NaN: what only the kernels have (states
 beyond S, channels beyond the last, segments) must not turn them into NaN."""
+import numpy as np
 import pytest
 import torch
 
+import seq_oracle as so
 from test_gpu_seq_empty import scan
 
 pytestmark = pytest.mark.gpu
@@ -75,4 +77,46 @@ def test_an_infinite_entry_of_B_or_C(hts, T, N, D, S, which):
         if k[1] != which:
             want[slice(at, T) if which == "B" else slice(0, at + 1), 0, S - 1] = True
         assert torch.equal(got[k] == INF, want) and not bool(torch.isnan(got[k]).any()), k
+    ctx.close()
+
+
+@pytest.mark.parametrize("S", [5, 16])
+@pytest.mark.parametrize("T", [60, 700])
+def test_decays_over_one(hts, T, S):
+    """Negative step sizes grow a state: from nothing it stays nothing, however large the factors' product, and a small one that a segment's factors take beyond
+    binary32's range and the next ones back is what it is step by step."""
+    N, D = 1, 24
+    d = positive(T, N, D, S)
+    d["dt_bias"] = None
+    d["A"] = -torch.ones(D, S, device="cuda")
+    d["dt"].fill_(-3.5)
+    d["x"].zero_()
+    ctx = hts.SeqContext(hts.selective_scan_workspace(T, N, D, S))
+    y, h = torch.empty(T, N, D, device="cuda"), torch.empty(N, D, S, device="cuda")
+    ctx.hts_selective_scan(d["x"], d["dt"], d["A"], d["B"], d["C"], y, z=d["z"], skip=d["skip"], softplus=False, h_out=h)
+    torch.cuda.synchronize()
+    assert bool((y == 0).all()) and bool((h == 0).all())
+    d["dt"][32:] = 3.5
+    small = torch.full((N, D, S), 1e-30, device="cuda")
+    ctx.hts_selective_scan(d["x"], d["dt"], d["A"], d["B"], d["C"], y, z=d["z"], skip=d["skip"], softplus=False, h_in=small, h_out=h)
+    torch.cuda.synchronize()
+    wide = {k: v.double().cpu().numpy() for k, v in d.items() if k not in ("dy", "dh_out", "h_in", "dt_bias")}
+    wide["B"], wide["C"] = wide["B"][:, :, None], wide["C"][:, :, None]
+    want = so.scan(**wide, softplus=False, h_in=small.double().cpu().numpy())
+    # a step's roundings and its exponent's; a segment's product is of one exponent, at most 112 / log 2 of it, rounded once and to 2^-24 of itself
+    so.near(y.double().cpu().numpy(), want["y"], np.abs(want["y"]), 16 * (min(T, 64) + S) + 12 * 112, 2.0 ** -24, "y")
+    ctx.close()
+
+
+def test_an_infinite_state_stays(hts):
+    """A state that is infinite decays by less than everything at every step, so it stays infinite, however many steps a segment has."""
+    T, N, D, S = 700, 1, 24, 8
+    d = positive(T, N, D, S)
+    d["A"], d["dt_bias"] = torch.full((D, S), -5.0, device="cuda"), torch.zeros(D, device="cuda")
+    d["h_in"][0, 5] = INF
+    ctx = hts.SeqContext(hts.selective_scan_workspace(T, N, D, S))
+    got = scan(hts, ctx, d, None)
+    assert bool((got["y"][:, 0, 5] == INF).all()) and bool((got["h_out"][0, 5] == INF).all())
+    rest = [k for k in range(D) if k != 5]
+    assert bool(torch.isfinite(got["y"][:, :, rest]).all()) and bool(torch.isfinite(got["h_out"][:, rest]).all())
     ctx.close()
