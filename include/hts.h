@@ -294,8 +294,8 @@ int32_t hts_linear(hts_seq_ctx *ctx, const hts_linear_desc *desc, hts_rows x, ht
                    hts_rows y, hts_rows pre);
 /* With g = dy act'(pre):  dx = g W + add [M,K],  dw = g^T x f32 [N,K] contiguous,  db = column sums of g f32 [N].
  * dx.p, dw, db: any may be NULL, not all.  add [M,K], p NULL: none; dx may take its place.  (A residual's own gradient is dy: a
- * block with a skip hands it over as `add`.)  pre is read for an activation only.  In bfloat16 an activation's g goes to dw and db
- * as the sum of three bfloat16 numbers, which lose nothing that counts in binary32, and rounded once to dx. */
+ * block with a skip hands it over as `add`.)  pre is read for an activation only.  In bfloat16 an activation's g goes on
+ * as the sum of three bfloat16 numbers, which lose nothing that counts in binary32: three products in place of one. */
 int32_t hts_linear_backward(hts_seq_ctx *ctx, const hts_linear_desc *desc, hts_rows x, hts_rows w, hts_rows pre, hts_rows dy,
                             hts_rows add, hts_rows dx, float *dw, float *db);
 

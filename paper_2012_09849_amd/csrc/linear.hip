@@ -150,7 +150,7 @@ template <typename T, bool ACROSS, int B, int WAVES> struct Copied {
         if constexpr (ACROSS) {
             if (k0 < K) { now += step; left -= step; }
             else { k0 = 0; start += part; now = start; left = all; }
-        }
+        } else if (k0 >= K) { k0 = 0; now += part; }
     }
 };
 
@@ -534,7 +534,8 @@ template <typename T> hipError_t backward(hts_seq_ctx &c, const LinearOp &op)
         Product p = g;
         p.b = op.w.p; p.ldb = op.w.ld; p.M = op.M; p.N = op.K; p.K = op.N;
         p.res = op.add.p; p.ldr = op.add.ld; p.y = op.dx.p; p.ldy = op.dx.ld;
-        if ((e = product<T, T, false, true>(c, p, cut(p.M, p.N, p.K, Kind<T>::BK, 1, 1, true), p.N)) != hipSuccess) return e;
+        p.parts = parts_of(sizeof(T), op.act); p.part_stride = at.stride;
+        if ((e = product<T, T, false, true>(c, p, cut(p.M, p.N, p.K, Kind<T>::BK, p.parts, 1, true), p.N)) != hipSuccess) return e;
     }
     if (op.dw || op.db) {
         Product p = g;
