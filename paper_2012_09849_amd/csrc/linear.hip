@@ -436,9 +436,10 @@ __global__ __launch_bounds__(256) void slope_kernel(const LinearOp p, T *out, co
         Loaded<T, V> h;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            h.e[e] = from_f32<T>(g[e]);
-            // (what is left of a number that is not finite would be NaN)
-            g[e] = __builtin_isfinite(g[e]) ? g[e] - to_f32(h.e[e]) : 0.0f;
+            // (what is left of a number that is not finite would be NaN, and of one that bfloat16 rounds to infinity infinite)
+            const bool finite = __builtin_isfinite(g[e]);
+            h.e[e] = from_f32<T>(PARTS > 1 && finite ? fminf(fmaxf(g[e], -0x1.fep+127f), 0x1.fep+127f) : g[e]);
+            g[e] = finite ? g[e] - to_f32(h.e[e]) : 0.0f;
         }
         store_v<T, V>(out + k * part + m * p.N + n, h);
     }

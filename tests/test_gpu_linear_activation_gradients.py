@@ -64,3 +64,24 @@ def test_three_numbers_and_no_fewer(hts, M):
     so.near(host(db), g, np.abs(g), 4 + 16 + 12 * 0.25, 0, "db")
     so.near(host(dw), g[:, None] * x64[M // 2], np.abs(g[:, None] * x64[M // 2]), 4 + 16 + 12 * 0.25, 0, "dw")
     ctx.close()
+
+
+def test_a_gradient_beyond_bfloat16(hts):
+    """dy is bfloat16's largest number and the slope a little over 1: g is within binary32 and beyond bfloat16, which would round it to infinity."""
+    largest = float(torch.finfo(torch.bfloat16).max)
+    pre64 = np.array([[p for p in np.arange(0.5, 3, 1 / 128) if 1.0020 < so.slope(np.array(p), "silu") < 1.0038]])
+    N, K = pre64.shape[1], 8
+    assert N > 0
+    pre, dy = torch.from_numpy(pre64).bfloat16().cuda(), torch.full((1, N), largest, dtype=torch.bfloat16, device="cuda")
+    dy[0, ::2] = -largest
+    x, w = (torch.full(s, 2.0 ** -100, dtype=torch.bfloat16, device="cuda") for s in ((1, K), (N, K)))
+    ctx = context(hts, 1, N, K, hts.ACT_SILU)
+    dx, dw, db = torch.empty(1, K, dtype=torch.bfloat16, device="cuda"), torch.empty(N, K, device="cuda"), torch.empty(N, device="cuda")
+    ctx.hts_linear_backward(x, w, dy, pre=pre, act=hts.ACT_SILU, dx=dx, dw=dw, db=db)
+    torch.cuda.synchronize()
+    g = host(dy)[0] * so.slope(host(pre)[0], "silu")
+    assert bool((np.abs(g) > largest).all())
+    so.near(host(db), g, np.abs(g), 4 + 16 + 12 * 2.25, 0, "db")
+    so.near(host(dw), g[:, None] * host(x), np.abs(g[:, None] * host(x)), 4 + 16 + 12 * 2.25, 0, "dw")
+    so.near(host(dx), g[None] @ host(w), np.abs(g)[None] @ host(w), 6 * N + 24 + 12 * 2.25, HALF["bf16"], "dx")
+    ctx.close()
