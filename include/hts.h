@@ -284,7 +284,7 @@ typedef struct { void *p; int64_t ld; } hts_rows;
 typedef struct { void *p; int64_t st, sn; } hts_steps;
 
 /* ---- y = act(x W^T + bias) + residual ----
- *   x [M,K]   w [N,K]   bias f32 [N] or NULL   residual [M,N], p NULL: none; y may take its place
+ *   x [M,K]   w [N,K]   bias f32 [N] or NULL   residual [M,N], p NULL: none; y may take its place, unless it is x
  *   pre [M,N], p NULL: not wanted; receives x W^T + bias, which the backward call of an activation reads
  * M, N, K 1 .. 2^24. */
 typedef struct { int32_t M, N, K; int32_t precision, act; } hts_linear_desc;
@@ -293,8 +293,8 @@ int64_t hts_linear_workspace(const hts_linear_desc *desc);
 int32_t hts_linear(hts_seq_ctx *ctx, const hts_linear_desc *desc, hts_rows x, hts_rows w, const float *bias, hts_rows residual,
                    hts_rows y, hts_rows pre);
 /* With g = dy act'(pre):  dx = g W + add [M,K],  dw = g^T x f32 [N,K] contiguous,  db = column sums of g f32 [N].
- * dx.p, dw, db: any may be NULL, not all.  add [M,K], p NULL: none; dx may take its place.  (A residual's own gradient is dy: a
- * block with a skip hands it over as `add`.)  pre is read for an activation only.  In bfloat16 an activation's g goes on
+ * dx.p, dw, db: any may be NULL, not all.  add [M,K], p NULL: none; dx may take its place, unless it is
+ * dy.  (A residual's own gradient is dy: a block with a skip hands it over as `add`.)  Both calls return HTS_EINVAL for outputs that share memory with anything else.  pre is read for an activation only.  In bfloat16 an activation's g goes on
  * as the sum of three bfloat16 numbers, which lose nothing that counts in binary32: three products in place of one. */
 int32_t hts_linear_backward(hts_seq_ctx *ctx, const hts_linear_desc *desc, hts_rows x, hts_rows w, hts_rows pre, hts_rows dy,
                             hts_rows add, hts_rows dx, float *dw, float *db);

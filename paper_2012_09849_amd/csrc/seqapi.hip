@@ -1,8 +1,10 @@
 // C ABI of the sequence memory: argument checks, the context, and sums of partial results (see include/hts.h).
+#include <initializer_list>
 #include <new>
 
 #include "internal.hpp"
 #include "seq.hpp"
+#include "spans.hpp"
 
 using namespace hts;
 
@@ -49,6 +51,12 @@ static int32_t check_steps(hts_steps &s, int64_t T, int64_t N, int64_t cols, int
     return by_step || by_sequence ? HTS_OK : HTS_EINVAL;
 }
 #define CHECK(x) do { const int32_t rc_ = (x); if (rc_ != HTS_OK) return rc_; } while (0)
+// What a call writes shares nothing with the other arrays, but for `place`, whose rows it may take (p 0: none)
+static int32_t check_apart(const Span &out, std::initializer_list<Span> others, const Span &place)
+{
+    for (const Span &o : others) if (meet(out, o)) return HTS_EINVAL;
+    return meet(out, place) && !same(out, place) ? HTS_EINVAL : HTS_OK;
+}
 static int32_t check_workspace(const hts_seq_ctx *ctx, int64_t need) { return need > ctx->bytes ? HTS_ESHAPE : HTS_OK; }
 
 extern "C" int32_t hts_seq_create(int64_t workspace_bytes, void *hip_stream, hts_seq_ctx **out)
@@ -100,6 +108,9 @@ extern "C" int32_t hts_linear(hts_seq_ctx *ctx, const hts_linear_desc *d, hts_ro
     if (residual.p) CHECK(check_rows(residual, d->M, d->N, s, false));
     if (pre.p) CHECK(check_rows(pre, d->M, d->N, s, true));
     if (misaligned(bias, 4)) return HTS_EINVAL;
+    const Span xs = span(x.p, x.ld, d->M, d->K, s), ws = span(w.p, w.ld, d->N, d->K, s), bs = span(bias, 0, 1, d->N, 4), rs = span(residual.p, residual.ld, d->M, d->N, s);
+    const Span ys = span(y.p, y.ld, d->M, d->N, s), ps = span(pre.p, pre.ld, d->M, d->N, s);
+    CHECK(check_apart(ys, {xs, ws, bs, ps}, rs)); CHECK(check_apart(ps, {xs, ws, bs, rs}, Span{}));
     LinearOp op = {};
     op.M = d->M; op.N = d->N; op.K = d->K; op.act = d->act;
     op.x = x; op.w = w; op.bias = bias; op.residual = residual; op.y = y; op.pre = pre;
@@ -123,6 +134,11 @@ extern "C" int32_t hts_linear_backward(hts_seq_ctx *ctx, const hts_linear_desc *
     }
     if (misaligned(dw, 4) || misaligned(db, 4)) return HTS_EINVAL;
     CHECK(check_workspace(ctx, linear_workspace(d->precision, d->act, d->M, d->N, d->K)));
+    // what is read: x for dw, w and add for dx, pre for an activation
+    const Span xs = span(dw ? x.p : nullptr, x.ld, d->M, d->K, s), ws = span(dx.p ? w.p : nullptr, w.ld, d->N, d->K, s), as = span(dx.p ? add.p : nullptr, add.ld, d->M, d->K, s);
+    const Span ps = span(d->act != HTS_ACT_NONE ? pre.p : nullptr, pre.ld, d->M, d->N, s), gs = span(dy.p, dy.ld, d->M, d->N, s);
+    const Span dxs = span(dx.p, dx.ld, d->M, d->K, s), dws = span(dw, 0, 1, (int64_t)d->N * d->K, 4), dbs = span(db, 0, 1, d->N, 4);
+    CHECK(check_apart(dxs, {xs, ws, ps, gs, dws, dbs}, as)); CHECK(check_apart(dws, {xs, ws, as, ps, gs, dbs}, Span{})); CHECK(check_apart(dbs, {xs, ws, as, ps, gs}, Span{}));
     LinearOp op = {};
     op.M = d->M; op.N = d->N; op.K = d->K; op.act = d->act;
     op.x = x; op.w = w; op.pre = pre; op.dy = dy; op.add = add; op.dx = dx; op.dw = dw; op.db = db;
