@@ -22,6 +22,18 @@ import torch
 from . import binding as hts
 
 
+def _meet(a, b):
+    """Whether rows [M,F] of two tensors share memory."""
+    (p, ld, m, size), (q, to, n, other) = ((t.data_ptr(), t.stride(0) * t.element_size(), t.shape[0], t.shape[1] * t.element_size()) for t in (a, b))
+    if p + (m - 1) * ld + size <= q or q + (n - 1) * to + other <= p:
+        return False
+    # of the second one's rows the first that ends beyond a row's beginning begins before that row's end
+    rows, theirs = p + torch.arange(m) * ld, q + torch.arange(n) * to
+    first = torch.searchsorted(theirs + other, rows, right=True)
+    there = first < n
+    return bool((theirs[first[there]] < rows[there] + size).any())
+
+
 class State:
     """What N sequences carry from call to call: the convolution's last inputs and the scan's states (zeros: nothing remembered)."""
 
@@ -120,10 +132,12 @@ class MemoryCore:
         self._run(x[None], y[None], None if starts is None else starts[None], None, state, None)
 
     def forward(self, x, y, state, starts=None, lengths=None, train=False):
-        """T steps of N sequences: x, y [T,N,F], all rows one distance apart, starts u8 [T,N], lengths i32 [N]; the state moves on in its place.  train: what `backward` reads is
-        kept until the next call."""
+        """T steps of N sequences: x, y [T,N,F], all rows one distance apart, starts u8 [T,N], lengths i32 [N]; the state moves on in its place; y may take x's place.  train: what
+        `backward` reads is kept until the next call, but for x, starts and lengths, which it reads where they are: they stay as they are until then, and y is not in x's place."""
         states = None
         if train:
+            if _meet(self._rows(x, x.shape, "x"), self._rows(y, x.shape, "y")):
+                raise hts.HtsError("forward: y shares memory with x, which backward reads")
             need = hts.selective_scan_states(x.shape[0], x.shape[1], self.inner, self.states)
             with torch.cuda.stream(self.ctx.stream):          # where they are used
                 if self._states is None or self._states.numel() < need:
@@ -135,8 +149,8 @@ class MemoryCore:
             self._training = (x, starts, lengths, begun)
 
     def backward(self, dy, dx):
-        """The gradients of dy [T,N,F] at the last forward(train=True): of the parameters into self.grads, of x into dx.  The state that the storage began
-        with is a constant."""
+        """The gradients of dy [T,N,F] at the last forward(train=True): of the parameters into self.grads, of x into dx, which shares no memory with dy and x.  The state that
+        the storage began with is a constant."""
         if self._training is None:
             raise hts.HtsError("backward: no forward(train=True) before it")
         x, starts, lengths, begun = self._training
@@ -145,6 +159,8 @@ class MemoryCore:
         u, conv, p, dt, v = (a[:M] for a in (self._u, self._c, self._p, self._dt, self._v))
         new = lambda k: torch.empty(M, k, dtype=self.dtype, device="cuda")  # noqa: E731
         xs, dys, dxs = (self._rows(a, x.shape, name) for a, name in ((x, "x"), (dy, "dy"), (dx, "dx")))
+        if _meet(dxs, dys) or _meet(dxs, xs):
+            raise hts.HtsError("backward: dx shares memory with dy or x")
         steps = lambda a: a.view(T, N, a.shape[-1])  # noqa: E731
         with torch.cuda.stream(self.ctx.stream):
             du, dconv, dp, ddt, dv = new(2 * I), new(I), new(R + 2 * S), new(I), new(I)
