@@ -195,24 +195,28 @@ def recall_storage(T, N, F, seed):
 
 def train_recall(core, updates, T=32, N=16, lr=3e-3, seed=1):
     """The last feature of y learns to hold the episode's cue: mean squared errors of the updates."""
-    opt, hp, losses = hts.OptState(torch.zeros(core.P, device="cuda"), torch.zeros(core.P, device="cuda")), hts.HParams(lr=lr, max_grad_norm=1.0), []
-    F = core.features
-    for k in range(updates):
-        x, cue, starts = (a.cuda() for a in recall_storage(T, N, F, seed + k))
-        x = x.to(core.dtype)
-        y, dy, dx = torch.empty_like(x), torch.zeros_like(x), torch.empty_like(x)
-        core.forward(x, y, State(core, N), starts=starts, train=True)
-        off = y[:, :, F - 1].float() - cue
-        dy[:, :, F - 1] = (2 / off.numel()) * off
-        losses.append((off * off).mean())
-        core.backward(dy, dx)
-        hts.hts_adam_apply_static(core.params, core.grads, opt, hp, core.ctx.stream)
-        core.sync_params()
-    return [float(v) for v in losses]
+    F, losses, caller = core.features, [], torch.cuda.current_stream()
+    core.ctx.stream.wait_stream(caller)
+    with torch.cuda.stream(core.ctx.stream):                   # the storages and what is computed from them, where the core's calls read and write them
+        opt, hp = hts.OptState(torch.zeros(core.P, device="cuda"), torch.zeros(core.P, device="cuda")), hts.HParams(lr=lr, max_grad_norm=1.0)
+        for k in range(updates):
+            x, cue, starts = (a.cuda() for a in recall_storage(T, N, F, seed + k))
+            x = x.to(core.dtype)
+            y, dy, dx = torch.empty_like(x), torch.zeros_like(x), torch.empty_like(x)
+            core.forward(x, y, State(core, N), starts=starts, train=True)
+            off = y[:, :, F - 1].float() - cue
+            dy[:, :, F - 1] = (2 / off.numel()) * off
+            losses.append((off * off).mean())
+            core.backward(dy, dx)
+            hts.hts_adam_apply_static(core.params, core.grads, opt, hp, core.ctx.stream)
+            core.sync_params()
+        losses = [float(v) for v in losses]
+    caller.wait_stream(core.ctx.stream)
+    return losses
 
 
 def main():
-    core = MemoryCore(features=64, inner=128, precision=hts.PRECISION_BF16, max_steps=32, max_rows=16)
+    core = MemoryCore(features=64, inner=128, precision=hts.PRECISION_BF16, max_steps=32, max_rows=16)         # on the current stream, as is all of the below
     core.init_params()
     losses = train_recall(core, 200)
     print(f"recalling a cue: mean squared error {sum(losses[:5]) / 5:.3f} at first, {sum(losses[-5:]) / 5:.3f} after {len(losses)} updates")
