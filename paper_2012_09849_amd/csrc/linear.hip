@@ -474,6 +474,7 @@ template <typename T, typename OUT, bool AX, bool BX, class C> hipError_t produc
 {
     const int64_t tn = ceil_div(p.N, C::BN), tiles = ceil_div(p.M, C::BM) * tn * p.slices;
     const bool dma = copies<T, AX>(p.a, p.lda, AX ? p.M : p.K) && copies<T, BX>(p.b, p.ldb, BX ? p.N : p.K) && p.part_stride % Kind<T>::V == 0;
+    if (tiles > INT32_MAX - 8 || !launchable(ceil_div(tiles, 8) * 8, C::WAVES * 64)) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)(ceil_div(tiles, 8) * 8)), block(C::WAVES * 64);
     if (dma) hipLaunchKernelGGL((product_kernel<T, OUT, AX, BX, C, true>), grid, block, 0, c.stream, p, (int)tn, (int)tiles);
     else hipLaunchKernelGGL((product_kernel<T, OUT, AX, BX, C, false>), grid, block, 0, c.stream, p, (int)tn, (int)tiles);
@@ -510,7 +511,9 @@ template <typename T> hipError_t forward(hts_seq_ctx &c, const LinearOp &op)
 
 template <typename T, int V> hipError_t slopes(hts_seq_ctx &c, const LinearOp &op, T *out, int64_t part)
 {
-    const dim3 grid((uint32_t)ceil_div((int64_t)op.M * (op.N / V), 256)), block(256);
+    const int64_t workgroups = ceil_div((int64_t)op.M * (op.N / V), 256);
+    if (!launchable(workgroups, 256)) return hipErrorInvalidConfiguration;
+    const dim3 grid((uint32_t)workgroups), block(256);
     if (op.act == HTS_ACT_RELU) hipLaunchKernelGGL((slope_kernel<T, V, HTS_ACT_RELU>), grid, block, 0, c.stream, op, out, part);
     else if (op.act == HTS_ACT_SILU) hipLaunchKernelGGL((slope_kernel<T, V, HTS_ACT_SILU>), grid, block, 0, c.stream, op, out, part);
     else hipLaunchKernelGGL((slope_kernel<T, V, HTS_ACT_GELU>), grid, block, 0, c.stream, op, out, part);

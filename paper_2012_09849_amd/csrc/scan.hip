@@ -967,6 +967,7 @@ template <typename T, int SL, bool WIDE, bool ABSENT> hipError_t scan(hts_seq_ct
     const Layout l = layout(op.d, seg, false);
     const int64_t waves = (int64_t)at.waves * op.d.G * op.d.N;
     seg.h_in = (float *)c.ws + l.h_in; seg.state = (float *)c.ws + l.state; seg.sum = (float *)c.ws + l.sum;
+    if (!launchable(ceil_div(waves * seg.count, FWD_WAVES), 64 * FWD_WAVES)) return hipErrorInvalidConfiguration;
     if (seg.count > 1) LAUNCH((scan_kernel<T, SL, WIDE, ABSENT, true>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
     LAUNCH((scan_kernel<T, SL, WIDE, ABSENT, false>), ceil_div(waves * seg.count, FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
     return hipSuccess;
@@ -981,10 +982,11 @@ template <typename T, int SL, bool WIDE, bool ABSENT> hipError_t scan_backward(h
     const int blocks = blocks_of(op.d);
     float *pairs = (float *)c.ws + l.pairs, *params = (float *)c.ws + l.params;
     seg.state = (float *)c.ws + l.state; seg.sum = (float *)c.ws + l.sum;
+    const int64_t pair_groups = ceil_div(width, 256), sum_groups = pair_groups + ceil_div(D * (op.d.S + 2), 64), workgroups = (int64_t)blocks * op.d.G * op.d.N * seg.count;
+    if (!launchable(workgroups, 64 * BWD_WAVES) || !launchable(sum_groups, 256)) return hipErrorInvalidConfiguration;
     if (seg.count > 1) LAUNCH((scan_adjoint_kernel<T, SL, WIDE, ABSENT>), ceil_div(waves * (seg.count - 1), FWD_WAVES), 64 * FWD_WAVES, op, at, seg);
-    LAUNCH((scan_backward_kernel<T, SL, WIDE, ABSENT>), (int64_t)blocks * op.d.G * op.d.N * seg.count, 64 * BWD_WAVES, op, at, seg, blocks, pairs, params);
-    const int64_t pair_groups = ceil_div(width, 256);
-    LAUNCH((sums_kernel<T>), pair_groups + ceil_div(D * (op.d.S + 2), 64), 256, op, blocks, 4 * SL, pairs, pair_groups, params, (int64_t)op.d.N * seg.count);
+    LAUNCH((scan_backward_kernel<T, SL, WIDE, ABSENT>), workgroups, 64 * BWD_WAVES, op, at, seg, blocks, pairs, params);
+    LAUNCH((sums_kernel<T>), sum_groups, 256, op, blocks, 4 * SL, pairs, pair_groups, params, (int64_t)op.d.N * seg.count);
     return hipSuccess;
 }
 
@@ -1001,6 +1003,7 @@ template <typename T, int SL> hipError_t run(hts_seq_ctx &c, const ScanOp &op, b
         if (states) return wide<T>(op, false) ? scan<T, SL, true, true>(c, op) : scan<T, SL, false, true>(c, op);
         return wide<T>(op, false) ? scan<T, SL, true, SL == 16>(c, op) : scan<T, SL, false, SL == 16>(c, op);
     }
+    if (!launchable(ceil_div((int64_t)op.d.N * op.d.D, 64), 256)) return hipErrorInvalidConfiguration;
     LAUNCH((step_kernel<T, SL>), ceil_div((int64_t)op.d.N * op.d.D, 64), 256, op);
     return hipSuccess;
 }

@@ -80,6 +80,9 @@ template <int ROWS> __device__ __forceinline__ void sum_partials(float (&sums)[R
     else if ((i -= b.n) < d.n) { if (d.p) d.p[i] = s; }
 }
 
+// whether a launch of that many workgroups is within what the runtime takes (the grid's threads have 32 bits); hipErrorInvalidConfiguration says that a shape is not
+inline bool launchable(int64_t groups, int threads) { return groups * threads < (1ll << 32); }
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 

@@ -8,6 +8,8 @@
 
 using namespace hts;
 
+// a launch that no grid is large enough for is a shape's fault
+#define LAUNCH_TRY(x) do { const hipError_t l_ = (x); if (l_ == hipErrorInvalidConfiguration) return HTS_ESHAPE; HIP_TRY(l_); } while (0)
 #define HIP_TRY(x) do { const hipError_t e_ = (x); if (e_ != hipSuccess) { note_hip_error(e_); return HTS_EHIP; } } while (0)
 
 namespace hts {
@@ -114,7 +116,7 @@ extern "C" int32_t hts_linear(hts_seq_ctx *ctx, const hts_linear_desc *d, hts_ro
     LinearOp op = {};
     op.M = d->M; op.N = d->N; op.K = d->K; op.act = d->act;
     op.x = x; op.w = w; op.bias = bias; op.residual = residual; op.y = y; op.pre = pre;
-    HIP_TRY(launch_linear(*ctx, d->precision, op));
+    LAUNCH_TRY(launch_linear(*ctx, d->precision, op));
     return HTS_OK;
 }
 
@@ -142,7 +144,7 @@ extern "C" int32_t hts_linear_backward(hts_seq_ctx *ctx, const hts_linear_desc *
     LinearOp op = {};
     op.M = d->M; op.N = d->N; op.K = d->K; op.act = d->act;
     op.x = x; op.w = w; op.pre = pre; op.dy = dy; op.add = add; op.dx = dx; op.dw = dw; op.db = db;
-    HIP_TRY(launch_linear_backward(*ctx, d->precision, op));
+    LAUNCH_TRY(launch_linear_backward(*ctx, d->precision, op));
     return HTS_OK;
 }
 
@@ -152,8 +154,8 @@ static int32_t check_conv(const hts_short_conv_desc *d)
     if (!d) return HTS_EINVAL;
     if (d->T <= 0 || d->N <= 0 || d->D <= 0 || (d->act != HTS_ACT_NONE && d->act != HTS_ACT_SILU)) return HTS_EINVAL;
     if (bad_precision(d->precision) || d->W < 2 || d->W > 4 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
-    // a workgroup per 64 channels and 64 steps at least; their number has 31 bits
-    return ceil_div(d->T, 16) * d->N * ceil_div(d->D, 64) > (1ll << 30) ? HTS_ESHAPE : HTS_OK;
+    // (tasks of 8 steps of a sequence, 64 channels each or more, are counted in 32 bits)
+    return ceil_div(d->T, 8) * d->N * ceil_div(d->D, 64) > (1ll << 31) ? HTS_ESHAPE : HTS_OK;
 }
 
 extern "C" int64_t hts_short_conv_workspace(const hts_short_conv_desc *d)
@@ -179,7 +181,7 @@ extern "C" int32_t hts_short_conv(hts_seq_ctx *ctx, const hts_short_conv_desc *d
     ConvOp op = {};
     op.T = d->T; op.N = d->N; op.D = d->D; op.W = d->W; op.act = d->act;
     op.x = x; op.y = y; op.w = w; op.bias = bias; op.starts = starts; op.lengths = lengths; op.state_in = state_in; op.state_out = state_out;
-    HIP_TRY(launch_conv(*ctx, d->precision, op));
+    LAUNCH_TRY(launch_conv(*ctx, d->precision, op));
     return HTS_OK;
 }
 
@@ -199,7 +201,7 @@ extern "C" int32_t hts_short_conv_backward(hts_seq_ctx *ctx, const hts_short_con
     op.T = d->T; op.N = d->N; op.D = d->D; op.W = d->W; op.act = d->act;
     op.x = x; op.dy = dy; op.dx = dx; op.w = w; op.bias = bias; op.starts = starts; op.lengths = lengths; op.state_in = state_in;
     op.dstate_out = dstate_out; op.dw = dw; op.db = db; op.dstate_in = dstate_in;
-    HIP_TRY(launch_conv_backward(*ctx, d->precision, op));
+    LAUNCH_TRY(launch_conv_backward(*ctx, d->precision, op));
     return HTS_OK;
 }
 
@@ -209,7 +211,7 @@ static int32_t check_scan(const hts_scan_desc *d)
     if (!d) return HTS_EINVAL;
     if (d->T <= 0 || d->N <= 0 || d->D <= 0 || d->S <= 0 || d->G <= 0 || (d->softplus != 0 && d->softplus != 1)) return HTS_EINVAL;
     if (bad_precision(d->precision) || d->S > 64 || d->D % d->G != 0 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
-    // a workgroup per 16 channels and 16 steps at least; their number has 31 bits
+    // (a wavefront for 16 channels of a group and 16 steps at least; they are counted in 32 bits)
     return ceil_div(d->T, 16) * d->N * (ceil_div(d->D / d->G, 16) * d->G) > (1ll << 30) ? HTS_ESHAPE : HTS_OK;
 }
 
@@ -248,7 +250,7 @@ extern "C" int32_t hts_selective_scan(hts_seq_ctx *ctx, const hts_scan_desc *d, 
     if (misaligned(h_out, 4) || misaligned(states, 16)) return HTS_EINVAL;
     CHECK(check_workspace(ctx, scan_workspace(*d, false)));
     op.y = y; op.h_out = h_out; op.states_out = states;
-    HIP_TRY(launch_scan(*ctx, op));
+    LAUNCH_TRY(launch_scan(*ctx, op));
     return HTS_OK;
 }
 
@@ -273,6 +275,6 @@ extern "C" int32_t hts_selective_scan_backward(hts_seq_ctx *ctx, const hts_scan_
     if (misaligned(states, 16) || misaligned(dh_out, 4) || (dh_out && g->dh_in == dh_out)) return HTS_EINVAL;
     CHECK(check_workspace(ctx, scan_workspace(*d, true)));
     op.dy = dy; op.dh_out = dh_out; op.states = states;
-    HIP_TRY(launch_scan_backward(*ctx, op));
+    LAUNCH_TRY(launch_scan_backward(*ctx, op));
     return HTS_OK;
 }

@@ -351,7 +351,9 @@ template <bool BACKWARD_CALL, typename T, int V, int W, int ACT> hipError_t run(
     const int dv = (int)ceil_div(ceil_div(op.D, V), 64);
     if constexpr (!BACKWARD_CALL) {
         const int chunks = (int)ceil_div(op.T, FORWARD);
-        const dim3 grid((uint32_t)(ceil_div((int64_t)op.N * chunks, ROWS) * dv)), block(64 * ROWS);
+        const int64_t workgroups = ceil_div((int64_t)op.N * chunks, ROWS) * dv;
+        if (!launchable(workgroups, 64 * ROWS)) return hipErrorInvalidConfiguration;
+        const dim3 grid((uint32_t)workgroups), block(64 * ROWS);
         if (op.T == 1) hipLaunchKernelGGL((conv_kernel<T, V, W, ACT, 1>), grid, block, 0, c.stream, op, dv, chunks);
         else hipLaunchKernelGGL((conv_kernel<T, V, W, ACT, FORWARD>), grid, block, 0, c.stream, op, dv, chunks);
         return hipGetLastError();
