@@ -4,9 +4,9 @@
 
 namespace hts {
 
-// dw's reduction over the rows is cut where C has too few tiles for the compute units, into 8 k-tiles at least (16 in binary32, whose k-tiles are half as
-// deep): 8192 rows of 2048 x 512 and the slices' sums 28.9 + 3.6 us in four, 27.6 + 8.1
-// in eight; all gradients of 1024 rows through an activation 36 us with two, 41 with one.
+// dw's reduction over the rows is cut where C has too few tiles for the compute units, into a slice for every 512 rows (8 k-tiles, 16 in binary32) or part of them
+// at most, so that one has more than 256 of them: 8192 rows of 2048 x 512 and the slices' sums 28.9 + 3.6 us in four, 27.6 + 8.1 in eight; dw and db of 1024 rows through
+// an activation 5 us less with two than with one.
 inline int slices_of(int64_t rows, int64_t N, int64_t K)
 {
     const int64_t tiles = ceil_div(N, 128) * ceil_div(K, 128), most = ceil_div(rows, 512);

@@ -29,7 +29,6 @@ constexpr int padded(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : S <= 32 ? 32 : 
 
 __device__ __forceinline__ float quad_xor1(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true)); }
 __device__ __forceinline__ float quad_xor2(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true)); }
-template <int CTRL> __device__ __forceinline__ float row_move(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
 // lane p of a quad gets the quad's sum of v[p]
 __device__ __forceinline__ float quad_deal(const float (&v)[4], int p)
 {
@@ -77,7 +76,6 @@ __device__ __forceinline__ void look(float &zero, float v) { zero = __builtin_fm
 
 struct Places { int per_group, waves; };          // channels of a group, wavefronts (16 channels) of a group
 
-template <typename T> __device__ __forceinline__ float wide_of(T v) { return to_f32(v); }
 __device__ __forceinline__ int length_of(const int32_t *lengths, int n, int T) { return lengths ? max(0, min(T, lengths[n])) : T; }
 // An array's chunk: the base goes from chunk to chunk, so that a chunk's addresses are a few scalar additions
 struct Walk {
