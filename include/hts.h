@@ -258,7 +258,7 @@ int32_t     hts_stream_destroy(void *hip_stream);
  *
  * Layout: a row or step is contiguous in its last index and starts anywhere, the distance between rows is the caller's: parts of a
  * wider array (one projection that holds several operands) are read and written in place.  Strides count elements.  Strides of
- * inputs may be 0 (one row for all), steps are at most 2^24 entries apart (HTS_ESHAPE beyond); that of a single row, step or sequence is not read; rows of an output must not overlap each other or any input, except where a comment allows it.
+ * inputs may be 0 (one row for all), T is at most 2^30 and steps are at most 2^24 entries apart (HTS_ESHAPE beyond); that of a single row, step or sequence is not read; rows of an output must not overlap each other or any input, except where a comment allows it.
  *
  * Sequences: `starts` u8 [T,N] or NULL: 1 = step t begins an episode, nothing from before it is seen.  Rows 1..T of a [T+1,N]
  * array of starts are the `dones` of hts_returns_gae.  `lengths` i32 [N] or NULL: sequence n has steps 0..lengths[n]-1 (less than

@@ -29,6 +29,7 @@ hipError_t launch_sum_partials(hts_seq_ctx &c, const float *part, int64_t parts,
 }  // namespace hts
 
 static bool bad_precision(int32_t p) { return p != HTS_PRECISION_FP32 && p != HTS_PRECISION_BF16; }
+constexpr int32_t MOST_STEPS = 1 << 30;       // the kernels count steps in 32 bits, and go beyond the last one by up to a few chunks
 static int size_of(int32_t precision) { return precision == HTS_PRECISION_BF16 ? 2 : 4; }
 static bool misaligned(const void *p, int size) { return (uintptr_t)p % size != 0; }
 
@@ -153,7 +154,7 @@ static int32_t check_conv(const hts_short_conv_desc *d)
 {
     if (!d) return HTS_EINVAL;
     if (d->T <= 0 || d->N <= 0 || d->D <= 0 || (d->act != HTS_ACT_NONE && d->act != HTS_ACT_SILU)) return HTS_EINVAL;
-    if (bad_precision(d->precision) || d->W < 2 || d->W > 4 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
+    if (bad_precision(d->precision) || d->T > MOST_STEPS || d->W < 2 || d->W > 4 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
     // (tasks of 8 steps of a sequence, 64 channels each or more, are counted in 32 bits)
     return ceil_div(d->T, 8) * d->N * ceil_div(d->D, 64) > (1ll << 31) ? HTS_ESHAPE : HTS_OK;
 }
@@ -210,7 +211,7 @@ static int32_t check_scan(const hts_scan_desc *d)
 {
     if (!d) return HTS_EINVAL;
     if (d->T <= 0 || d->N <= 0 || d->D <= 0 || d->S <= 0 || d->G <= 0 || (d->softplus != 0 && d->softplus != 1)) return HTS_EINVAL;
-    if (bad_precision(d->precision) || d->S > 64 || d->D % d->G != 0 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
+    if (bad_precision(d->precision) || d->T > MOST_STEPS || d->S > 64 || d->D % d->G != 0 || d->D > (1 << 20) || d->N > (1 << 24)) return HTS_ESHAPE;
     // (a wavefront for 16 channels of a group and 16 steps at least; they are counted in 32 bits)
     return ceil_div(d->T, 16) * d->N * (ceil_div(d->D / d->G, 16) * d->G) > (1ll << 30) ? HTS_ESHAPE : HTS_OK;
 }

@@ -30,3 +30,14 @@ def test_selective_scan(ctx, T, N, D, S):
     d, s, pair, none = b._ScanDesc(T, N, D, S, 1, 0, 1), STEPS(HERE, D, T * D), STEPS(HERE, S, T * S), STEPS(None, 0, 0)
     inputs = b._ScanInputs(s, s, pair, pair, none, HERE, None, None, None, None, None)
     assert b.load_library().hts_selective_scan(ctx, C.byref(d), C.byref(inputs), s, None, None) == ESHAPE
+
+
+def test_steps_are_counted_in_32_bits():
+    """Chunks go beyond the last step, so that steps near 2^31 would count into the sign: refused."""
+    import paper_2012_09849_amd as hts
+    most = 1 << 30
+    assert hts.short_conv_workspace(most, 1, 1, 2) > 0 and hts.selective_scan_workspace(most, 1, 1, 1) > 0 and hts.selective_scan_states(most, 1, 1, 1) > 0
+    for T in (most + 1, (1 << 31) - 1):
+        for size in (lambda: hts.short_conv_workspace(T, 1, 1, 2), lambda: hts.selective_scan_workspace(T, 1, 1, 1), lambda: hts.selective_scan_states(T, 1, 1, 1)):
+            with pytest.raises(hts.HtsError):
+                size()
