@@ -417,6 +417,13 @@ def _precision(t, name, dims=None):
     return PRECISION_BF16 if t.dtype is torch.bfloat16 else PRECISION_FP32
 
 
+def _last(t, name):
+    """The length of a tensor's last dimension, from which a call takes a size."""
+    if not isinstance(t, _Tensor) or t.dim() < 2:
+        raise HtsError(f"{name}: expected a device tensor of two dimensions or more")
+    return t.shape[-1]
+
+
 def _wrong(dtype, shape, name, what=""):
     return HtsError(f"{name}: expected a {what}{dtype} device tensor of shape {tuple(shape)}")
 
@@ -540,7 +547,7 @@ class SeqContext:
     def hts_short_conv(self, x, w, y, bias=None, act=ACT_NONE, starts=None, lengths=None, state_in=None, state_out=None):
         """y_t = act(bias + sum_j w[:, j] x_{t-W+1+j}) over the steps of t's episode; state_in and state_out (which may be one) hold the last W - 1 inputs."""
         prec = _precision(x, "x", 3)
-        cells, W, f = x.shape, w.shape[-1], torch.float32
+        cells, W, f = x.shape, _last(w, "w"), torch.float32
         (T, N, D), dt = cells, _DTYPE[prec]
         state = (N, W - 1, D)
         xs, ys = self._conv.set(*_steps(x, dt, cells, "x"), *_steps(y, dt, cells, "y"))
@@ -553,7 +560,7 @@ class SeqContext:
                                 dstate_in=None):
         """The gradients dx, dw, db and dstate_in of dy and dstate_out."""
         prec = _precision(x, "x", 3)
-        cells, W, f = x.shape, w.shape[-1], torch.float32
+        cells, W, f = x.shape, _last(w, "w"), torch.float32
         (T, N, D), dt = cells, _DTYPE[prec]
         state = (N, W - 1, D)
         xs, gs, ds = self._conv_back.set(*_steps(x, dt, cells, "x"), *_steps(dy, dt, cells, "dy"), *_steps(dx, dt, cells, "dx"))
@@ -566,10 +573,11 @@ class SeqContext:
 
     def _scan(self, x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in):
         prec, f = _precision(x, "x", 3), torch.float32
-        cells, S, ty = x.shape, A.shape[-1], _DTYPE[prec]
+        cells, S, ty = x.shape, _last(A, "A"), _DTYPE[prec]
         T, N, D = cells
         G, held = 1, (N, D, S)
         pair = (T, N, S)
+        _last(B, "B")
         if B.dim() == 4:
             G = B.shape[2]
             pair = (T, N, G, S)
@@ -583,7 +591,7 @@ class SeqContext:
         """h_t = exp(delta A) h_{t-1} + delta x B, y = (C h + skip x) silu(z), delta = softplus(dt + dt_bias).  B, C: [T, N, S] or [T, N, G, S].  h_in and
         h_out may be one; states (selective_scan_states floats) is for a backward call."""
         desc, inputs, ty, cells, _, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
-        if states is not None and states.numel() < self.lib.hts_selective_scan_states(desc):
+        if states is not None and (not isinstance(states, _Tensor) or states.numel() < self.lib.hts_selective_scan_states(desc)):
             raise HtsError("states: too few entries (selective_scan_states)")
         rc = self.lib.hts_selective_scan(self._h, desc, inputs, self._one.set(*_steps(y, ty, cells, "y"))[0], _array(h_out, torch.float32, held, "h_out"),
                                          _ptr(states, torch.float32, "states"))
@@ -594,7 +602,7 @@ class SeqContext:
                                     ddt_bias=None, softplus=True, starts=None, lengths=None, h_in=None, dh_out=None, dh_in=None):
         """The gradients of dy and dh_out; states as the forward call on the same inputs left it."""
         desc, inputs, ty, cells, pair, held = self._scan(x, dt, A, B, C_, z, skip, dt_bias, softplus, starts, lengths, h_in)
-        if states is None or states.numel() < self.lib.hts_selective_scan_states(desc):
+        if not isinstance(states, _Tensor) or states.numel() < self.lib.hts_selective_scan_states(desc):
             raise HtsError("states: too few entries (selective_scan_states)")
         f, (_, D, S) = torch.float32, held
         self._scan_grads.set(*_steps(dx, ty, cells, "dx"), *_steps(ddt, ty, cells, "ddt"), *_steps(dB, ty, pair, "dB"), *_steps(dC, ty, pair, "dC"),
