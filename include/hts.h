@@ -247,8 +247,9 @@ int32_t     hts_stream_create_cu_range(int32_t first_cu, int32_t n_cus, void **h
 int32_t     hts_stream_destroy(void *hip_stream);
 
 /* ---- Sequence memory ---------------------------------------------------------------------------------------------
- * Operators of a recurrent core between a trunk's features and the heads, for policies that have to remember: matrix products with
- * bias, activation and residual, a short causal convolution along time, and a selective state space scan, each with its gradients.
+ * Operators of a recurrent core, for policies that have to remember: matrix products with bias, activation and residual, a short
+ * causal convolution along time, and a selective state space scan, each with its gradients.  They work on features that the program
+ * has: hts_act and hts_learner_step go from frames to logits and to an update in one call, and neither hand out their trunk's nor take others.
  * A learner runs them over a whole storage, an actor one step at a time (T = 1, the state handed from call to call), a server over
  * prompts of any length.
  *
@@ -262,7 +263,8 @@ int32_t     hts_stream_destroy(void *hip_stream);
  *
  * Sequences: `starts` u8 [T,N] or NULL: 1 = step t begins an episode, nothing from before it is seen.  Rows 1..T of a [T+1,N]
  * array of starts are the `dones` of hts_returns_gae.  `lengths` i32 [N] or NULL: sequence n has steps 0..lengths[n]-1 (less than
- * 0 counts as 0, more than T as T); beyond them nothing is read, outputs are 0, and states stay what they were.
+ * 0 counts as 0, more than T as T); beyond them nothing is read, outputs are 0, and states stay what they were,
+ * also where they are not finite: nothing of them reaches another sequence or the parameters' gradients.
  *
  * Conventions are those above; the context is of its own type, since these calls need no network: */
 typedef struct hts_seq_ctx hts_seq_ctx;
@@ -288,7 +290,7 @@ typedef struct { void *p; int64_t st, sn; } hts_steps;
  *   pre [M,N], p NULL: not wanted; receives x W^T + bias, which the backward call of an activation reads
  * M, N, K 1 .. 2^24. */
 typedef struct { int32_t M, N, K; int32_t precision, act; } hts_linear_desc;
-/* Bytes of workspace of the call and its backward call; negative error code for an unsupported shape.  Host only. */
+/* Bytes of workspace of the backward call (hts_linear needs none); negative error code for an unsupported shape.  Host only. */
 int64_t hts_linear_workspace(const hts_linear_desc *desc);
 int32_t hts_linear(hts_seq_ctx *ctx, const hts_linear_desc *desc, hts_rows x, hts_rows w, const float *bias, hts_rows residual,
                    hts_rows y, hts_rows pre);

@@ -393,7 +393,7 @@ def _size(what: str, rc: int) -> int:
 
 
 def linear_workspace(M: int, N: int, K: int, precision: int = PRECISION_FP32, act: int = ACT_NONE) -> int:
-    """Bytes of workspace that hts_linear and hts_linear_backward need for M rows, N outputs and K inputs."""
+    """Bytes of workspace that hts_linear_backward needs for M rows, N outputs and K inputs (hts_linear needs none)."""
     return _size("hts_linear_workspace", load_library().hts_linear_workspace(C.byref(_LinearDesc(M, N, K, precision, act))))
 
 

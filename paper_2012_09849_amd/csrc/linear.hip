@@ -8,9 +8,11 @@
 // once more, so that rows leave as whole lines, with bias, activation and residual on the way.
 // Rows that are whole numbers of 16 bytes, at addresses that are, are copied straight into LDS (buffer_load ... lds), a k-tile ahead; others
 // through registers, entry by entry where a row ends.
-// What bounds it: 8192 x 2048 from 512 in bfloat16 with silu and its pre-activation, 30.7 us: 67 MB of outputs (13.5 us at the rate of a large copy), and
-// 268 MB of operands from L2 to LDS at 15 TB/s or so, which two workgroups a compute unit overlap in part; matrix units are busy for a fifth.  The gradient of x there
-// 26 us, of W 29 + 3.6, at the same rate from the L2.  Binary32 gradients of 1024 x 1024 x 512, 39 us: a wavefront alone on its SIMD, whose matrix
+// An activation's gradient in bfloat16 is the sum of three matrices, which a reduction goes over one after the other: 8192 x 2048 x 512 with silu, dx 69 us, dw 87, forming
+// them 32 (in a trace; the call 170).
+// What bounds it: 8192 x 2048 from 512 in bfloat16 with silu and its pre-activation, 32.2 us: 67 MB of outputs (13.5 us at the rate of a large copy), and
+// 268 MB of operands from L2 to LDS at 15 TB/s or so, which two workgroups a compute unit overlap in part; matrix units are busy for a fifth.  The gradient of x there,
+// without an activation, 25 us, of W 29 + 5.4, at the same rate from the L2.  Binary32 gradients of 1024 x 1024 x 512, 39 us: a wavefront alone on its SIMD, whose matrix
 // instructions (a third of its cycles), LDS reads and scalar instructions follow one another.
 #include "dmagemm.hpp"
 #include "linear_plan.hpp"

@@ -6,9 +6,9 @@
 // for NB neighbouring channels of a step, so that a chunk is one instruction an array, and step sizes, inputs and sums over the states pass between the
 // two orders through LDS, which also holds B and C, the same for all channels of a group, as binary32.  The work is vector instructions: exp2 (two issue
 // slots) and four others for a state and step.
-// What bounds it: issue.  512 x 16 x 1024 channels of 16 states in bfloat16, forward 67 us: a wavefront a SIMD that issues in 73 % of its cycles, 580 instructions for 16
-// steps, 384 slots of them the states'; a prompt of 8192 steps 33 + 53 us, two wavefronts a SIMD and 90 % of their cycles; backward 27 + 129, 72 %.
-// Twice as many segments (four wavefronts a SIMD) leave the prompt at 32 + 61.
+// What bounds it: issue.  512 x 16 x 1024 channels of 16 states in bfloat16, forward 68 us: a wavefront a SIMD that issues in 72 % of its cycles, 555 vector instructions
+// for 16 steps, 384 slots of them the states'; a prompt of 8192 steps 33 + 56 us, two wavefronts a SIMD, whose vector instructions take 89 % of the cycles; backward 27
+// (a wavefront a SIMD, 71 %) + 124 (two, 97 %).  Twice as many segments (four wavefronts a SIMD) left the prompt at 32 + 61 where these took 33 + 53.
 //
 // States beyond S and channels beyond the last are zeros all through; where infinities come, whose products with those would be NaN, a chunk selects.
 // Steps that are none (beyond a sequence's length) do nothing, whatever the state: 0 times an infinite one would be NaN.  Chunks of them are passed over.
@@ -907,7 +907,7 @@ int blocks_of(const hts_scan_desc &d) { return (int)ceil_div(places(d).waves, BW
 // Segments of a sequence: where its wavefronts leave units idle, as many as give two to a SIMD, of 32 steps or so at least, in whole chunks of either direction.
 // Forward the first pass costs two thirds of the second and a launch, so that up to three segments gain nothing; backward a fifth, and a lone wavefront
 // waits for itself a third of its time.  129 steps of 5 sequences of 330 channels in binary32, five segments (segments of 64 steps at least: one and
-// two): forward 19.7 us (25.0), backward 28.2 (46.2).  (On fewer compute units than 256 there are fewer segments: the workspace is for those.)
+// two): forward 18.9 us, backward 30.9 (before these kernels looked for infinities 19.7 and 28.2, with one and two segments 25.0 and 46.2).  (On fewer compute units than 256 there are fewer segments: the workspace is for those.)
 constexpr int MOST_SEGMENTS = 64, LEAST_STEPS = 24;        // (before they are made whole chunks)
 int segments_of(const hts_scan_desc &d, int cus, bool backward)
 {

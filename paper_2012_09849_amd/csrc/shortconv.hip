@@ -338,8 +338,8 @@ __global__ __launch_bounds__(64 * ROWS, 4) void conv_backward_kernel(const ConvO
 
 template <typename T> bool wide(const hts_steps &s, int V) { return ((uintptr_t)s.p % (sizeof(T) * V)) == 0 && s.st % V == 0 && s.sn % V == 0; }
 
-// workgroups over the tasks, each with a partial sum of the filter gradients: about four a compute unit (512 x 16 x 1024 in bfloat16: 17.0 us, with twice as
-// many 19.2)
+// workgroups over the tasks, each with a partial sum of the filter gradients: about four a compute unit (512 x 16 x 1024 in bfloat16: 18.2 us; 17.0 before tasks at a
+// sequence's end looked at what they have, and with twice as many workgroups 19.2 then)
 int groups_of(int64_t T, int64_t N, int64_t dv)
 {
     const int64_t g = ceil_div(N * ceil_div(T, BACKWARD), ROWS), most = ceil_div(1024, dv);

@@ -1,6 +1,6 @@
 """A recurrent core for policies that have to remember, from the library's sequence-memory operators (no arithmetic of the core lives here).
 
-The core stands between a trunk's features and the heads:
+The core turns features that a program has into features that remember (the library's own policies go from frames to logits in one call, without it):
 
     u  = x W_in^T + b_in                 [T,N,2I]: what is remembered, and a gate z
     c  = silu(short convolution of u's first half)
