@@ -107,7 +107,10 @@ template <int W, int V> struct Filter {
 #pragma unroll
         for (int j = 0; j < W; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(w[j][i], !CUT || W - 1 - j <= vis ? win[j][i] : 0.0f, v[i]);
+            for (int i = 0; i < V; ++i) {
+                const float more = __builtin_fmaf(w[j][i], win[j][i], v[i]);
+                v[i] = !CUT || W - 1 - j <= vis ? more : v[i];
+            }
     }
 };
 
@@ -254,9 +257,12 @@ __global__ __launch_bounds__(64 * ROWS, 4) void conv_backward_kernel(const ConvO
                 const bool sees = !CUT || W - 1 - j <= vis;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float share = sees ? g[i] : 0.0f;
-                    pend[W - 1 - j][i] = __builtin_fmaf(ENDS && !sees ? 0.0f : f.w[j][i], share, pend[W - 1 - j][i]);
-                    if (k < TC) dw[j][i] = __builtin_fmaf(sees ? win[j][i] : 0.0f, share, dw[j][i]);
+                    const float given = __builtin_fmaf(f.w[j][i], g[i], pend[W - 1 - j][i]);
+                    pend[W - 1 - j][i] = sees ? given : pend[W - 1 - j][i];
+                    if (k < TC) {
+                        const float more = __builtin_fmaf(win[j][i], g[i], dw[j][i]);
+                        dw[j][i] = sees ? more : dw[j][i];
+                    }
                 }
             }
             if (k < TC)

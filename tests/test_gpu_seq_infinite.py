@@ -120,3 +120,38 @@ def test_an_infinite_state_stays(hts):
     rest = [k for k in range(D) if k != 5]
     assert bool(torch.isfinite(got["y"][:, :, rest]).all()) and bool(torch.isfinite(got["h_out"][:, rest]).all())
     ctx.close()
+
+
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("W", [2, 4])
+def test_an_infinite_filter_weight(hts, silu, W):
+    """The weight of the oldest input, infinite for one channel: steps that do not see that input, at an episode's beginning, are what they are without it, and so are the
+    other channels; forward and backward."""
+    T, N, D = 21, 2, 40
+    g = torch.Generator(device="cuda").manual_seed(W)
+    normal = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    x, dy, w, b, state = normal(T, N, D), normal(T, N, D), normal(D, W), normal(D), normal(N, W - 1, D)
+    starts = torch.zeros(T, N, dtype=torch.uint8, device="cuda")
+    starts[0], starts[9, 0], starts[20, 1] = 1, 1, 1
+    ctx = hts.SeqContext(hts.short_conv_workspace(T, N, D, W))
+    unseen = torch.zeros(T, N, dtype=torch.bool, device="cuda")
+    for t, n in ((0, 0), (0, 1), (9, 0), (20, 1)):
+        unseen[t:t + W - 1, n] = True
+    more = dict(bias=b, act=hts.ACT_SILU if silu else hts.ACT_NONE, starts=starts, state_in=state)
+    results = []
+    for weight in (0.5, INF):
+        w[7, 0] = weight
+        y, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty_like(w)
+        ctx.hts_short_conv(x, w, y, **more)
+        # only steps that do not see the oldest input have a gradient
+        ctx.hts_short_conv_backward(x, w, dy * unseen[:, :, None], dx, dw, **more)
+        torch.cuda.synchronize()
+        results.append((y, dx, dw))
+    (y, dx, dw), (y2, dx2, dw2) = results
+    rest = [d for d in range(D) if d != 7]
+    assert torch.equal(y[unseen], y2[unseen]) and torch.equal(y[:, :, rest], y2[:, :, rest])
+    assert silu or not bool(torch.isfinite(y2[~unseen][:, 7]).any())          # (silu of -inf is 0)
+    assert torch.equal(dx[:, :, rest], dx2[:, :, rest]) and torch.equal(dw[rest], dw2[rest])
+    # channel 7: what no step beyond the beginnings reaches, whose gradients are 0 times an infinite weight or slope
+    assert torch.equal(dx[20, 1, 7], dx2[20, 1, 7])
+    ctx.close()
