@@ -208,6 +208,36 @@ int32_t hts_adam_apply(hts_ctx *ctx, float *params, const float *grads, hts_opt_
 int32_t hts_adam_apply_static(float *params, const float *grads, hts_opt_state *opt, const hts_hparams *hp, int64_t P,
                               void *hip_stream);
 
+/* AdamW over many tensors at once: decay that does not pass through the moments, for each tensor its own, and bfloat16 copies of what matrix
+ * products read, in one launch (two with the gradients' norm).
+ *   g <- g min(1, max_grad_norm / (|g| + 1e-6)) (all tensors' norm; max_grad_norm <= 0: as they are);  m <- beta1 m + (1 - beta1) g;
+ *   v <- beta2 v + (1 - beta2) g^2;  p <- p (1 - lr_i weight_decay) - lr_i (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),  lr_i = lr lr_scale
+ * States in 32 bits (bits = 32: m, v f32 [n]) or in 8 (bits = 8: m, v u8 [n], m_scale, v_scale f32 [ceil(n / 256)]): m holds the first moment and v the
+ * root of the second as e4m3 numbers times a power of two for every 256 entries, which the entries of the largest size set to less than 256.  A number is
+ * rounded up with the probability that makes its expectation exact (by 16 random bits, so what is less than 2^-16 of a step counts as nothing), so averages
+ * that move by less than a step an update still move; a root above zero stays above.  The bits are Philox4x32-10's (key = seed lo/hi, counter = (entry / 4,
+ * tensor, t lo, t hi), word entry % 4: the lower half for m, the upper for v): the same on every run.  States that are all zeros (bytes and scales) are a beginning.
+ *   p f32 [n]   g [n] of grad_precision (HTS_PRECISION_*)   copy bf16 [n] or NULL: receives p rounded   n 1 .. 2^34
+ * The plan keeps the arrays' addresses (host structs are read once): they have to live as long as it does.  HTS_EINVAL where two arrays share memory, gradients
+ * among themselves excepted.  Creating and destroying a plan wait for the device; steps do not, on the stream of creation, and do not overlap each other. */
+typedef struct {
+    float *p;
+    const void *g;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void *copy;
+    int64_t n;
+    float weight_decay, lr_scale;      /* >= 0 */
+    int32_t grad_precision, bits;
+} hts_adamw_tensor;
+typedef struct { float lr, beta1, beta2, eps, max_grad_norm; int32_t reserved; uint64_t seed; } hts_adamw_hparams;
+typedef struct hts_adamw hts_adamw;
+int32_t hts_adamw_create(const hts_adamw_tensor *tensors, int32_t count, void *hip_stream, hts_adamw **out);
+int32_t hts_adamw_destroy(hts_adamw *opt);
+/* *step: host counter of completed updates (the call uses t = *step + 1 and increments it; a captured call repeats its own t).
+ * grad_norm_or_null: device f32 [1], receives the norm before clipping. */
+int32_t hts_adamw_step(hts_adamw *opt, const hts_adamw_hparams *hp, int64_t *step, float *grad_norm_or_null);
+
 /* Test hook for the tiled matrix-multiply core every layer is built on: C[M,N] = A[M,K] * B[N,K]^T, all f32
  * row-major device arrays; operands are rounded to bf16 first when precision = HTS_PRECISION_BF16.  K % 8 == 0. */
 int32_t hts_test_gemm(hts_ctx *ctx, int32_t precision, const float *A, const float *B, float *Cout, int32_t M,
@@ -343,6 +373,52 @@ typedef struct {
 } hts_scan_grads;
 int32_t hts_selective_scan_backward(hts_seq_ctx *ctx, const hts_scan_desc *desc, const hts_scan_inputs *in, hts_steps dy,
                                     const float *dh_out, const float *states, const hts_scan_grads *grads);
+
+/* ---- layer norm of rows ----
+ *   mean and var (the mean square of x - mean) over a row's F entries;  y = (x - mean) / sqrt(var + eps) w + b
+ *   x, y [M,F]; y may take x's place   w, b f32 [F] or NULL (ones, zeros)   eps >= 0
+ * M 1 .. 2^24, F 1 .. 16384 (HTS_ESHAPE beyond). */
+typedef struct { int32_t M, F; int32_t precision; float eps; } hts_layer_norm_desc;
+/* Bytes of workspace of the backward call (hts_layer_norm needs none). */
+int64_t hts_layer_norm_workspace(const hts_layer_norm_desc *desc);
+int32_t hts_layer_norm(hts_seq_ctx *ctx, const hts_layer_norm_desc *desc, hts_rows x, const float *w, const float *b, hts_rows y);
+/* With h = (x - mean) r, r = 1 / sqrt(var + eps), g = dy w:  dx = r (g - mean(g) - h mean(g h)) + add [M,F],  dw = sum over rows of dy h f32 [F],
+ * db = sum over rows of dy f32 [F].  dx.p, dw, db: any may be NULL, not all.  add [M,F], p NULL: none.  dx may take the place of dy, of add or of
+ * x.  Nothing of the forward call is needed but x.  Both calls return HTS_EINVAL for outputs that share memory with anything else. */
+int32_t hts_layer_norm_backward(hts_seq_ctx *ctx, const hts_layer_norm_desc *desc, hts_rows x, const float *w, hts_rows dy, hts_rows add,
+                                hts_rows dx, float *dw, float *db);
+
+/* ---- gated delta rule: a memory that is written by what it had wrong ----
+ *   delta = softplus(a + a_bias) (softplus = 1) or a + a_bias (0);  alpha = exp(delta A[h]) (0 where a step begins an episode);  beta = 1 / (1 + exp(-b))
+ *   for every head h, of group g = h / (H / G), a state S_t [K,V]:
+ *   z_t = v_t - alpha_t S_{t-1}^T k_t;  S_t = alpha_t S_{t-1} + beta_t k_t z_t^T;  y_t = scale S_t^T q_t
+ *   normalize = 1: q and k are divided by sqrt(their square + 1e-6) first (with keys of length one and A delta <= 0 the state stays bounded).
+ *   q, k [T,N,G*K]   v, y [T,N,H*V]   a, b [T,N,H]   K 1..128, V 1..65536, G divides H, H 1..65536   A f32 [H]   a_bias f32 [H] or NULL (zeros)
+ *   h_in f32 [N,H,K,V] or NULL (zeros); h_out or NULL: the state after the last step.  h_out may be h_in.
+ *   states f32 or NULL: receives what the backward call needs, hts_delta_rule_states(desc) floats.
+ * Values that are not finite (queries and keys: or whose squares' sum is not) make NaN of what sees them: outputs from their step on to the episode's end,
+ * gradients of their episode.  Nothing of them reaches other episodes, sequences or, of q, k, a and b, other groups' heads (but for the sums dA and
+ * da_bias).  The same holds for a state that leaves binary32, within 64 steps of where it does. */
+typedef struct { int32_t T, N, H, G, K, V; int32_t precision, normalize, softplus; float scale; } hts_delta_rule_desc;
+typedef struct {
+    hts_steps q, k, v, a, b;
+    const float *A, *a_bias;
+    const uint8_t *starts;
+    const int32_t *lengths;
+    const float *h_in;
+} hts_delta_rule_inputs;
+int64_t hts_delta_rule_workspace(const hts_delta_rule_desc *desc);
+int64_t hts_delta_rule_states(const hts_delta_rule_desc *desc);
+int32_t hts_delta_rule(hts_seq_ctx *ctx, const hts_delta_rule_desc *desc, const hts_delta_rule_inputs *in, hts_steps y, float *h_out,
+                       float *states);
+/* Gradients of dy and dh_out (f32 [N,H,K,V], NULL: zeros), `states` as the forward call on the same inputs left it.  dq and dk are sums over a group's
+ * heads.  dA f32 [H]; da_bias f32 [H] and dh_in f32 [N,H,K,V] may be NULL. */
+typedef struct {
+    hts_steps dq, dk, dv, da, db;
+    float *dA, *da_bias, *dh_in;
+} hts_delta_rule_grads;
+int32_t hts_delta_rule_backward(hts_seq_ctx *ctx, const hts_delta_rule_desc *desc, const hts_delta_rule_inputs *in, hts_steps dy,
+                                const float *dh_out, const float *states, const hts_delta_rule_grads *grads);
 
 int32_t     hts_last_hip_error(void);
 const char *hts_strerror(int32_t code);

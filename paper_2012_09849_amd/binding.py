@@ -21,7 +21,9 @@ EXPORTS = ["hts_param_count", "hts_create", "hts_destroy", "hts_act", "hts_sync_
            "hts_profile_end", "hts_profile_overhead", "hts_profile_begin_sampled", "hts_adam_apply_static", "hts_track_params",
            "hts_stream_create_cu_range", "hts_stream_destroy", "hts_seq_create", "hts_seq_destroy", "hts_linear_workspace", "hts_linear",
            "hts_linear_backward", "hts_short_conv_workspace", "hts_short_conv", "hts_short_conv_backward", "hts_selective_scan_workspace",
-           "hts_selective_scan_states", "hts_selective_scan", "hts_selective_scan_backward"]
+           "hts_selective_scan_states", "hts_selective_scan", "hts_selective_scan_backward", "hts_layer_norm_workspace", "hts_layer_norm",
+           "hts_layer_norm_backward", "hts_delta_rule_workspace", "hts_delta_rule_states", "hts_delta_rule", "hts_delta_rule_backward", "hts_adamw_create",
+           "hts_adamw_destroy", "hts_adamw_step"]
 
 
 class HtsError(RuntimeError):
@@ -92,6 +94,36 @@ class _ScanGrads(C.Structure):
                 ("ddt_bias", C.c_void_p), ("dh_in", C.c_void_p)]
 
 
+class _NormDesc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("F", C.c_int32), ("precision", C.c_int32), ("eps", C.c_float)]
+
+
+class _DeltaDesc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("T", "N", "H", "G", "K", "V", "precision", "normalize", "softplus")] + [("scale", C.c_float)]
+
+
+class _DeltaInputs(C.Structure):
+    _fields_ = [("q", _Steps), ("k", _Steps), ("v", _Steps), ("a", _Steps), ("b", _Steps), ("A", C.c_void_p), ("a_bias", C.c_void_p), ("starts", C.c_void_p),
+                ("lengths", C.c_void_p), ("h_in", C.c_void_p)]
+
+
+class _DeltaGrads(C.Structure):
+    _fields_ = [("dq", _Steps), ("dk", _Steps), ("dv", _Steps), ("da", _Steps), ("db", _Steps), ("dA", C.c_void_p), ("da_bias", C.c_void_p), ("dh_in", C.c_void_p)]
+
+
+class _AdamWTensorC(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("p", "g", "m", "v", "m_scale", "v_scale", "copy")] + [("n", C.c_int64), ("weight_decay", C.c_float), ("lr_scale", C.c_float),
+                                                                                                 ("grad_precision", C.c_int32), ("bits", C.c_int32)]
+
+
+class AdamWHParams(C.Structure):
+    """hts_adamw_hparams."""
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float), ("max_grad_norm", C.c_float), ("reserved", C.c_int32), ("seed", C.c_uint64)]
+
+    def __init__(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, max_grad_norm=0.0, seed=0):
+        super().__init__(lr, beta1, beta2, eps, max_grad_norm, 0, seed)
+
+
 STATS_FIELDS = ("policy_loss", "value_loss", "entropy", "grad_norm", "clip_frac", "approx_kl", "nonfinite")
 
 _lib = None
@@ -152,6 +184,16 @@ def load_library():
         lib.hts_short_conv_backward.argtypes = [vp, C.POINTER(_ConvDesc), steps, vp, vp, vp, vp, vp, steps, vp, steps, vp, vp, vp]
         lib.hts_selective_scan.argtypes = [vp, C.POINTER(_ScanDesc), C.POINTER(_ScanInputs), steps, vp, vp]
         lib.hts_selective_scan_backward.argtypes = [vp, C.POINTER(_ScanDesc), C.POINTER(_ScanInputs), steps, vp, vp, C.POINTER(_ScanGrads)]
+        for f, desc in (("hts_layer_norm_workspace", _NormDesc), ("hts_delta_rule_workspace", _DeltaDesc), ("hts_delta_rule_states", _DeltaDesc)):
+            getattr(lib, f).restype = C.c_int64
+            getattr(lib, f).argtypes = [C.POINTER(desc)]
+        lib.hts_layer_norm.argtypes = [vp, C.POINTER(_NormDesc), rows, vp, vp, rows]
+        lib.hts_layer_norm_backward.argtypes = [vp, C.POINTER(_NormDesc), rows, vp, rows, rows, rows, vp, vp]
+        lib.hts_delta_rule.argtypes = [vp, C.POINTER(_DeltaDesc), C.POINTER(_DeltaInputs), steps, vp, vp]
+        lib.hts_delta_rule_backward.argtypes = [vp, C.POINTER(_DeltaDesc), C.POINTER(_DeltaInputs), steps, vp, vp, C.POINTER(_DeltaGrads)]
+        lib.hts_adamw_create.argtypes = [C.POINTER(_AdamWTensorC), C.c_int32, vp, C.POINTER(vp)]
+        lib.hts_adamw_destroy.argtypes = [vp]
+        lib.hts_adamw_step.argtypes = [vp, C.POINTER(AdamWHParams), C.POINTER(C.c_int64), vp]
         _lib = lib
     return _lib
 
@@ -187,6 +229,71 @@ def hts_adam_apply_static(params, grads, opt: OptState, hp: HParams, stream=None
                                      C.byref(oc), C.byref(hp), params.numel(), C.c_void_p(stream.cuda_stream)),
            "hts_adam_apply_static")
     opt.step = oc.step
+
+
+class AdamWTensor:
+    """A tensor of an AdamW plan: p float32, g float32 or bfloat16, m and v float32, or uint8 with m_scale and v_scale (adamw_scales(n) float32 each), copy
+    bfloat16 or None; all contiguous device tensors of p's number of entries."""
+
+    def __init__(self, p, g, m, v, m_scale=None, v_scale=None, copy=None, weight_decay=0.0, lr_scale=1.0):
+        self.p, self.g, self.m, self.v, self.m_scale, self.v_scale, self.copy, self.weight_decay, self.lr_scale = p, g, m, v, m_scale, v_scale, copy, weight_decay, lr_scale
+
+
+def adamw_scales(n: int) -> int:
+    """Scales of a moment of n entries that is held in 8 bits: one for every 256 of them."""
+    return -(-n // 256)
+
+
+class AdamW:
+    """Owns an hts_adamw plan over AdamWTensors, bound to a torch stream (default: the current stream at construction); keeps the tensors alive.
+    step: updates done."""
+
+    def __init__(self, tensors, stream=None):
+        self.lib = load_library()
+        self._h = C.c_void_p()
+        if not torch.cuda.is_available():
+            raise HtsError("no GPU visible: the library has no CPU path")
+        self.tensors, self.step = list(tensors), 0
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        table = (_AdamWTensorC * max(1, len(self.tensors)))()
+        for i, t in enumerate(self.tensors):
+            table[i] = self._entry(t, f"tensor {i}: ")
+        self.stream.synchronize()                              # (the tensors' contents may still be on their way; the plan's tables are there when create returns)
+        _check(self.lib.hts_adamw_create(table, len(self.tensors), C.c_void_p(self.stream.cuda_stream), C.byref(self._h)), "hts_adamw_create")
+
+    @staticmethod
+    def _entry(t, name):
+        if not isinstance(t.p, torch.Tensor) or t.p.numel() == 0:
+            raise HtsError(name + "p: expected a contiguous torch.float32 device tensor")
+        n, f = t.p.numel(), torch.float32
+        eight = isinstance(t.m, torch.Tensor) and t.m.dtype is torch.uint8
+        state, half = torch.uint8 if eight else f, isinstance(t.g, torch.Tensor) and t.g.dtype is torch.bfloat16
+        given = [(t.p, f, n, "p"), (t.g, torch.bfloat16 if half else f, n, "g"), (t.m, state, n, "m"), (t.v, state, n, "v")]
+        given += [(t.m_scale, f, adamw_scales(n), "m_scale"), (t.v_scale, f, adamw_scales(n), "v_scale")] if eight else []
+        for x, dtype, count, what in given + ([(t.copy, torch.bfloat16, n, "copy")] if t.copy is not None else []):
+            if x is None or _ptr(x, dtype, name + what) is None or x.numel() != count:
+                raise HtsError(f"{name}{what}: expected {count} entries of {dtype}")
+        scales = (t.m_scale.data_ptr(), t.v_scale.data_ptr()) if eight else (None, None)
+        return _AdamWTensorC(t.p.data_ptr(), t.g.data_ptr(), t.m.data_ptr(), t.v.data_ptr(), *scales, t.copy.data_ptr() if t.copy is not None else None, n, t.weight_decay,
+                             t.lr_scale, PRECISION_BF16 if half else PRECISION_FP32, 8 if eight else 32)
+
+    def hts_adamw_step(self, hp: AdamWHParams, grad_norm=None):
+        """One update of all tensors; grad_norm (float32 [1]) receives the gradients' norm before clipping."""
+        step = C.c_int64(self.step)
+        _check(self.lib.hts_adamw_step(self._h, C.byref(hp), C.byref(step), _array(grad_norm, torch.float32, (1,), "grad_norm") or None), "hts_adamw_step")
+        self.step = step.value
+
+    def close(self):
+        if getattr(self, "_h", None) and self._h.value:
+            self.stream.synchronize()
+            self.lib.hts_adamw_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class CuRangeStream:
@@ -410,6 +517,20 @@ def selective_scan_states(T: int, N: int, D: int, S: int, G: int = 1) -> int:
     return _size("hts_selective_scan_states", load_library().hts_selective_scan_states(C.byref(_ScanDesc(T, N, D, S, G, PRECISION_FP32, 1))))
 
 
+def layer_norm_workspace(M: int, F: int, precision: int = PRECISION_FP32) -> int:
+    """Bytes of workspace that hts_layer_norm_backward needs for M rows of F entries (hts_layer_norm needs none)."""
+    return _size("hts_layer_norm_workspace", load_library().hts_layer_norm_workspace(C.byref(_NormDesc(M, F, precision, 0.0))))
+
+
+def delta_rule_workspace(T: int, N: int, H: int, G: int, K: int, V: int, precision: int = PRECISION_FP32) -> int:
+    return _size("hts_delta_rule_workspace", load_library().hts_delta_rule_workspace(C.byref(_DeltaDesc(T, N, H, G, K, V, precision, 1, 1, 1.0))))
+
+
+def delta_rule_states(T: int, N: int, H: int, K: int, V: int) -> int:
+    """Floats of the `states` that a training forward call hands to its backward call."""
+    return _size("hts_delta_rule_states", load_library().hts_delta_rule_states(C.byref(_DeltaDesc(T, N, H, H, K, V, PRECISION_FP32, 1, 1, 1.0))))
+
+
 # A small call's time is the host's, and these run for each of its operands: one look at a tensor's properties, no calls between them.
 def _precision(t, name, dims=None):
     if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16) or (dims is not None and t.dim() != dims):
@@ -484,7 +605,7 @@ class _Arguments:
 
 class SeqContext:
     """Owns an hts_seq_ctx bound to a torch stream (default: the current stream at construction): the operators of a sequence memory.
-    workspace_bytes: the most that any of its calls needs (linear_workspace, short_conv_workspace, selective_scan_workspace)."""
+    workspace_bytes: the most that any of its calls needs (linear_workspace, short_conv_workspace, selective_scan_workspace, layer_norm_workspace, delta_rule_workspace)."""
 
     def __init__(self, workspace_bytes=0, stream=None):
         self.lib = load_library()
@@ -492,6 +613,8 @@ class SeqContext:
             raise HtsError("no GPU visible: the library has no CPU path")
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self._linear, self._linear_back, self._conv, self._conv_back = (_Arguments(*[k] * n) for k, n in ((_Rows, 5), (_Rows, 6), (_Steps, 2), (_Steps, 3)))
+        self._norm, self._norm_back = _Arguments(*[_Rows] * 2), _Arguments(*[_Rows] * 4)
+        self._delta_in, self._delta_grads = _Arguments(_DeltaInputs), _Arguments(_DeltaGrads)
         self._scan_in, self._scan_grads, self._one, self._descs = _Arguments(_ScanInputs), _Arguments(_ScanGrads), _Arguments(_Steps), {}
         self._h = C.c_void_p()
         _check(self.lib.hts_seq_create(workspace_bytes, C.c_void_p(self.stream.cuda_stream), C.byref(self._h)), "hts_seq_create")
@@ -612,3 +735,59 @@ class SeqContext:
                                                   _ptr(states, f, "states"), self._scan_grads.at)
         if rc:
             _check(rc, "hts_selective_scan_backward")
+
+    def hts_layer_norm(self, x, y, w=None, b=None, eps=1e-5):
+        """y = (x - mean) / sqrt(var + eps) w + b over the rows of x [M, F]; y may be x."""
+        prec = _precision(x, "x", 2)
+        shape, dt, f = x.shape, _DTYPE[prec], torch.float32
+        xs, ys = self._norm.set(*_rows(x, dt, shape, "x"), *_rows(y, dt, shape, "y"))
+        rc = self.lib.hts_layer_norm(self._h, self._desc(_NormDesc, *shape, prec, eps), xs, _array(w, f, shape[1:], "w"), _array(b, f, shape[1:], "b"), ys)
+        if rc:
+            _check(rc, "hts_layer_norm")
+
+    def hts_layer_norm_backward(self, x, dy, w=None, add=None, dx=None, dw=None, db=None, eps=1e-5):
+        """The gradients of dy: dx (and add), dw, db; each of the three only where it is given.  dx may be dy, add or x."""
+        prec = _precision(x, "x", 2)
+        shape, dt, f = x.shape, _DTYPE[prec], torch.float32
+        xs, gs, adds, ds = self._norm_back.set(*_rows(x, dt, shape, "x"), *_rows(dy, dt, shape, "dy"), *_rows(add, dt, shape, "add"), *_rows(dx, dt, shape, "dx"))
+        rc = self.lib.hts_layer_norm_backward(self._h, self._desc(_NormDesc, *shape, prec, eps), xs, _array(w, f, shape[1:], "w"), gs, adds, ds, _array(dw, f, shape[1:], "dw"),
+                                              _array(db, f, shape[1:], "db"))
+        if rc:
+            _check(rc, "hts_layer_norm_backward")
+
+    def _delta(self, q, k, v, a, b, A, a_bias, scale, normalize, softplus, starts, lengths, h_in):
+        prec, f = _precision(q, "q", 4), torch.float32
+        _precision(v, "v", 4)
+        keys, values, ty = q.shape, v.shape, _DTYPE[prec]
+        T, N, G, K = keys
+        H, V = values[2:]
+        gates, held = (T, N, H), (N, H, K, V)
+        st, le = self._sequences(starts, lengths, T, N)
+        self._delta_in.set(*_steps(q, ty, keys, "q"), *_steps(k, ty, keys, "k"), *_steps(v, ty, (T, N, H, V), "v"), *_steps(a, ty, gates, "a"), *_steps(b, ty, gates, "b"),
+                           _array(A, f, (H,), "A"), _array(a_bias, f, (H,), "a_bias"), st, le, _array(h_in, f, held, "h_in"))
+        return self._desc(_DeltaDesc, T, N, H, G, K, V, prec, 1 if normalize else 0, 1 if softplus else 0, scale), self._delta_in.at, ty, keys, values, gates, held
+
+    def hts_delta_rule(self, q, k, v, a, b, A, y, a_bias=None, scale=1.0, normalize=True, softplus=True, starts=None, lengths=None, h_in=None, h_out=None, states=None):
+        """z = v - alpha S^T k, S = alpha S + beta k z^T, y = scale S^T q; alpha = exp(A softplus(a + a_bias)), beta = sigmoid(b).  q, k [T, N, G, K], v, y [T, N, H, V],
+        a, b [T, N, H].  h_in and h_out (float32 [N, H, K, V]) may be one; states (delta_rule_states floats) is for a backward call."""
+        desc, inputs, ty, _, values, _, held = self._delta(q, k, v, a, b, A, a_bias, scale, normalize, softplus, starts, lengths, h_in)
+        if states is not None and (not isinstance(states, _Tensor) or states.numel() < _size("hts_delta_rule_states", self.lib.hts_delta_rule_states(desc))):
+            raise HtsError("states: too few entries (delta_rule_states)")
+        rc = self.lib.hts_delta_rule(self._h, desc, inputs, self._one.set(*_steps(y, ty, values, "y"))[0], _array(h_out, torch.float32, held, "h_out"),
+                                     _ptr(states, torch.float32, "states"))
+        if rc:
+            _check(rc, "hts_delta_rule")
+
+    def hts_delta_rule_backward(self, q, k, v, a, b, A, dy, states, dq, dk, dv, da, db, dA, a_bias=None, da_bias=None, scale=1.0, normalize=True, softplus=True, starts=None,
+                                lengths=None, h_in=None, dh_out=None, dh_in=None):
+        """The gradients of dy and dh_out; states as the forward call on the same inputs left it."""
+        desc, inputs, ty, keys, values, gates, held = self._delta(q, k, v, a, b, A, a_bias, scale, normalize, softplus, starts, lengths, h_in)
+        if not isinstance(states, _Tensor) or states.numel() < _size("hts_delta_rule_states", self.lib.hts_delta_rule_states(desc)):
+            raise HtsError("states: too few entries (delta_rule_states)")
+        f, heads = torch.float32, held[1:2]
+        self._delta_grads.set(*_steps(dq, ty, keys, "dq"), *_steps(dk, ty, keys, "dk"), *_steps(dv, ty, values, "dv"), *_steps(da, ty, gates, "da"), *_steps(db, ty, gates, "db"),
+                              _array(dA, f, heads, "dA"), _array(da_bias, f, heads, "da_bias"), _array(dh_in, f, held, "dh_in"))
+        rc = self.lib.hts_delta_rule_backward(self._h, desc, inputs, self._one.set(*_steps(dy, ty, values, "dy"))[0], _array(dh_out, f, held, "dh_out"), _ptr(states, f, "states"),
+                                              self._delta_grads.at)
+        if rc:
+            _check(rc, "hts_delta_rule_backward")

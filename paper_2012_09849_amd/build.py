@@ -8,10 +8,10 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhts.so")
-SOURCES = ["api.hip", "fwd.hip", "bwd.hip", "misc.hip", "seqapi.hip", "linear.hip", "shortconv.hip", "scan.hip"]
+SOURCES = ["api.hip", "fwd.hip", "bwd.hip", "misc.hip", "seqapi.hip", "linear.hip", "shortconv.hip", "scan.hip", "layernorm.hip", "delta.hip", "adamw.hip"]
 COMMON = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-PER_FILE = {"misc.hip": ["-ffp-contract=off"]}
+PER_FILE = {"misc.hip": ["-ffp-contract=off"], "adamw.hip": ["-ffp-contract=off"]}
 
 
 def _compile(src: str) -> str:

@@ -1,0 +1,1158 @@
+// The gated delta rule and its gradients (see include/hts.h).
+//
+// Step by step, with al = exp(delta A), be = 1 / (1 + exp(-b)), k and q of length one (or as they are):
+//   z = v - al S^T k,  S <- al S + be k z^T,  y = scale S^T q.
+// Up to 64 steps of a chunk at a time, S the state before it, G[i][j] = the product of the decays of steps j + 1 .. i (0 where an episode begins among them),
+// kept[i] that of steps 0 .. i, left[j] that of steps j + 1 .. to the end, M = (k_i . k_j) G[i][j] below the diagonal:
+//   Z = (I + M diag(be))^-1 (V - kept K S),  U = be Z,  Y = scale (kept Q S + (Q K^T G) U),  S' = kept[end] S + K^T (left U).
+// The gradients, dS' being the state's at the chunk's end, W the inverse above:
+//   dU = (Q K^T G)^T dY + left K dS',  dV = W^T (be dU),  dS = kept[end] dS' + Q^T (kept dY) - K^T (kept dV)
+//   dQ = kept dY S^T + (dY U^T G) K,  dK = left U dS'^T - kept dV S^T + (dY U^T G)^T Q - X K - X^T K,  X = dV U^T G below the diagonal
+//   db = (1 - be) Z . dV,  and the logarithm of a step's decay has what passes it: all that goes from before it (earlier steps, S) to it and what is after.
+//
+// Three kinds of kernels: what needs the chunk's own steps only (prep: every chunk at a time), what goes from chunk to chunk (forward, reverse: 32 of the values'
+// entries of a head at a time, whose states never meet), and the gradients that sum over the values (grads: every chunk at a time again).
+#include "delta.hpp"
+
+namespace hts {
+namespace {
+
+constexpr int TILE = 32;                  // the values' entries of a workgroup
+
+__device__ __forceinline__ float wave_add(float x)
+{
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+
+struct Decay { float delta, slope, exponent; };       // exponent: of 2
+__device__ __forceinline__ Decay decay_of(float x, float bias, float A, int softplus)
+{
+    Decay r;
+    x += bias;
+    r.delta = x; r.slope = 1.0f;
+    if (softplus) softplus_f(x, r.delta, r.slope);
+    r.exponent = r.delta * A;
+    return r;
+}
+// below this (in exponents of 2) nothing of binary32 is left: the step forgets
+constexpr double FORGETS = -150.0;
+constexpr double LOG2E_64 = 1.4426950408889634074;
+
+// ---- what needs the chunk's steps only --------------------------------------------------------------------------------
+template <typename T, int KP> struct PrepLds {
+    static constexpr int PITCH = Num<T>::exact_pitch(KP), LINE = 65;
+    static constexpr int FAR = 0, EPISODE = FAR + 8 * CHUNK, STRENGTH = EPISODE + 4 * CHUNK, Q = STRENGTH + 4 * CHUNK, K = Q + 4 * CHUNK, BAD = K + 4 * CHUNK;
+    static constexpr int KEYS = BAD + 64, QUERIES = KEYS + CHUNK * PITCH, BELOW = QUERIES + CHUNK * PITCH, INVERSE = BELOW + 4 * CHUNK * LINE, HALF = INVERSE + 4 * CHUNK * LINE;
+    static constexpr int BYTES = HALF + 4 * 32 * 33 + 64;
+};
+
+// C (16x16) = sum over n of A[row][k] B[k][col], binary32 from LDS
+__device__ __forceinline__ f32x4 tile_product(const float *a, int lda, const float *b, int ldb, int n, int col, int quad)
+{
+    f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < n; k += 4) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[col * lda + k + quad], b[(k + quad) * ldb + col], c, 0, 0, 0);
+    return c;
+}
+
+template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void prep_kernel(const DeltaArgs a)
+{
+    typedef PrepLds<T, KP> L;
+    typedef Num<T> N_;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const hts_delta_rule_desc &d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
+    const int64_t unit = blockIdx.x;
+    const int h = (int)(unit % d.H), n = (int)(unit / d.H % d.N), c = (int)(unit / d.H / d.N), t0 = c * CHUNK, len = length_of(a, n);
+    if (t0 >= len) return;
+    const int K = d.K, group = h / (d.H / d.G);
+    double *far = (double *)(lds + L::FAR);
+    int *episode = (int *)(lds + L::EPISODE);
+    float *strength = (float *)(lds + L::STRENGTH), *q_unit = (float *)(lds + L::Q), *k_unit = (float *)(lds + L::K);
+    uint32_t *bad = (uint32_t *)(lds + L::BAD);                     // [4] keys by wavefront, [4] queries, [2] rows of the matrix
+    float *below = (float *)(lds + L::BELOW), *inverse = (float *)(lds + L::INVERSE), *half = (float *)(lds + L::HALF);
+    Gates &gates = a.gates[unit];
+
+    uint64_t gates_bad = 0, resets = 0;
+    if (wave == 0) {
+        const int t = t0 + lane;
+        const bool live = t < len;
+        float be = 0.0f;
+        double e = 0.0;
+        bool reset = false, wrong = false;
+        if (live) {
+            const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
+            be = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
+            e = (double)dc.exponent * LOG2E_64;
+            wrong = !finite(be) || !(e < 1e30);
+            reset = (a.in.starts && a.in.starts[(int64_t)t * d.N + n]) || e < FORGETS || wrong;
+            if (wrong) be = 0.0f;
+            if (reset) e = 0.0;
+        }
+        resets = __ballot(reset);
+        gates_bad = __ballot(wrong);
+        const uint64_t upto = resets & (~0ull >> (63 - lane));
+        const int ep = __popcll(upto), last = __popcll(resets), first = upto ? 63 - __clzll(upto) : 0;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const double x = __shfl_up(e, o, 64);
+            if (lane >= o) e += x;
+        }
+        const double end = __shfl(e, 63, 64);
+        far[lane] = e; episode[lane] = ep; strength[lane] = be;
+        gates.far[lane] = e; gates.strength[lane] = be; gates.episode[lane] = ep; gates.first[lane] = first;
+        gates.keep[lane] = ep == 0 ? exp2_wide(e) : -1.0f;
+        gates.left[lane] = ep == last ? exp2_wide(end - e) : -1.0f;
+    }
+    // rows of keys and queries, zeros for those that are not finite, and their lengths
+    uint32_t bad_k = 0, bad_q = 0;
+    char *keys = lds + L::KEYS, *queries = lds + L::QUERIES;
+#pragma unroll 4
+    for (int rr = 0; rr < 16; ++rr) {
+        const int row = wave * 16 + rr, t = t0 + row;
+        const bool live = t < len;
+        const T *kr = live ? step_of<T>(a.in.k, t, n) + (int64_t)group * K : nullptr, *qr = live ? step_of<T>(a.in.q, t, n) + (int64_t)group * K : nullptr;
+        T kx[2], qx[2];
+        float ks = 0.0f, qs = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = lane + 64 * i;
+            kx[i] = live && at < K ? kr[at] : from_f32<T>(0.0f);
+            qx[i] = live && at < K ? qr[at] : from_f32<T>(0.0f);
+            ks = __builtin_fmaf(to_f32(kx[i]), to_f32(kx[i]), ks);
+            qs = __builtin_fmaf(to_f32(qx[i]), to_f32(qx[i]), qs);
+        }
+        ks = wave_add(ks); qs = wave_add(qs);
+        const bool k_wrong = !finite(ks), q_wrong = !finite(qs);
+        bad_k |= (uint32_t)k_wrong << rr; bad_q |= (uint32_t)q_wrong << rr;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = lane + 64 * i;
+            if (at >= KP) continue;
+            *(T *)(keys + row * L::PITCH + at * sizeof(T)) = k_wrong ? from_f32<T>(0.0f) : kx[i];
+            *(T *)(queries + row * L::PITCH + at * sizeof(T)) = q_wrong ? from_f32<T>(0.0f) : qx[i];
+        }
+        if (lane == 0) {
+            k_unit[row] = gates.k_unit[row] = d.normalize && !k_wrong ? 1.0f / __builtin_sqrtf(ks + 1e-6f) : 1.0f;
+            q_unit[row] = gates.q_unit[row] = q_wrong ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(qs + 1e-6f) : 1.0f;
+        }
+    }
+    if (lane == 0) { bad[wave] = bad_k; bad[4 + wave] = bad_q; }
+    if (tid < 2) bad[8 + tid] = 0;
+    __syncthreads();
+
+    // M diag(be) below the diagonal; Q K^T G.  Wavefront w has rows 16 w .. of the steps that look back
+    {
+        float far_unit[4];
+        double far_i[4];
+        int ep_i[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * wave + 4 * quad + r;
+            far_i[r] = far[i]; ep_i[r] = episode[i]; far_unit[r] = k_unit[i];
+        }
+        for (int jt = 0; jt < 4; ++jt) {
+            f32x4 kk = {0.0f, 0.0f, 0.0f, 0.0f}, qk = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (jt <= wave)
+#pragma unroll
+                for (int s = 0; s < KP / 32; ++s) {
+                    const int at = (4 * s + quad) * N_::EXACT;
+                    const Exact<T> ki = get_exact<T>(keys + (16 * wave + col) * L::PITCH + at, 16), kj = get_exact<T>(keys + (16 * jt + col) * L::PITCH + at, 16);
+                    const Exact<T> qi = get_exact<T>(queries + (16 * wave + col) * L::PITCH + at, 16);
+                    mma(kk, ki, kj);
+                    if constexpr (BACK) mma(qk, qi, kj);       // rows of steps that look back: handed on along them
+                    else mma(qk, kj, qi);                      // ... along the steps that they look at
+                }
+            const int j = 16 * jt + col;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * wave + 4 * quad + r;
+                float x = 0.0f;
+                if (j < i && episode[j] == ep_i[r]) {
+                    x = kk[r] * (far_unit[r] * k_unit[j]) * exp2_wide(far_i[r] - far[j]) * strength[j];
+                    if (!finite(x)) { atomicOr(&bad[8 + (i >> 5)], 1u << (i & 31)); x = 0.0f; }
+                }
+                below[i * L::LINE + j] = x;
+            }
+            float p[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = BACK ? 16 * wave + 4 * quad + r : 16 * wave + col, m = BACK ? j : 16 * jt + 4 * quad + r;
+                p[r] = m <= i && episode[m] == episode[i] ? qk[r] * (q_unit[i] * d.scale * k_unit[m]) * exp2_wide(far[i] - far[m]) : 0.0f;
+            }
+            // fragments of 16 rows and 32 entries: rows are the steps that look back (forward), those that are looked at (back)
+            const int row = BACK ? 16 * jt + col : 16 * wave + col, at = BACK ? 16 * wave + 4 * quad : 16 * jt + 4 * quad;
+            char *f = a.read + (unit * 8 + (row >> 4) * 2 + (at >> 5)) * N_::WIDE_FRAGMENT + ((at & 31) >> 3) * 256 + (row & 15) * 16;
+            put_wide4<T>(f, 1024, (at >> 2) & 1, p);
+        }
+    }
+    // keys (and queries) with the steps along a row
+    for (int f = wave; f < KP / 16 * 2; f += 4) {
+        const int row = 16 * (f >> 1) + col, at = 32 * (f & 1) + 8 * quad;
+        T x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = *(const T *)(keys + (at + i) * L::PITCH + row * sizeof(T));
+        put_exact<T>(a.keys + (unit * (KP / 8) + f) * N_::EXACT_FRAGMENT + lane * 16, 1024, make_exact<T>(x));
+        if constexpr (BACK) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = *(const T *)(queries + (at + i) * L::PITCH + row * sizeof(T));
+            put_exact<T>(a.queries + (unit * (KP / 8) + f) * N_::EXACT_FRAGMENT + lane * 16, 1024, make_exact<T>(x));
+        }
+    }
+    __syncthreads();
+    // the inverse: blocks of 16 on the diagonal by substitution, a column a lane; then those of 32 and the whole, W10 = -W11 M10 W00
+    if (lane < 16) {
+        const float *m = below + 16 * wave * (L::LINE + 1);
+        float x[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            x[r] = r == lane ? 1.0f : 0.0f;
+#pragma unroll
+            for (int k = 0; k < r; ++k) x[r] = __builtin_fmaf(-m[r * L::LINE + k], x[k], x[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) inverse[(16 * wave + r) * L::LINE + 16 * wave + lane] = x[r];
+    }
+    // zeros above the diagonal's blocks
+#pragma unroll
+    for (int jt = 1; jt < 4; ++jt)
+        if (jt > wave)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) inverse[(16 * wave + 4 * quad + r) * L::LINE + 16 * jt + col] = 0.0f;
+    __syncthreads();
+    const int block = 32 * wave;              // wavefronts 0, 1: block rows 16 .. 31 and 48 .. 63
+    f32x4 x;
+    if (wave < 2) {
+        x = tile_product(below + (block + 16) * L::LINE + block, L::LINE, inverse + block * (L::LINE + 1), L::LINE, 16, col, quad);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) half[(16 * wave + 4 * quad + r) * 33 + col] = x[r];
+    }
+    __syncthreads();
+    if (wave < 2) {
+        x = tile_product(inverse + (block + 16) * (L::LINE + 1), L::LINE, half + 16 * wave * 33, 33, 16, col, quad);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) inverse[(block + 16 + 4 * quad + r) * L::LINE + block + col] = -x[r];
+    }
+    __syncthreads();
+    const int tr = 16 * (wave >> 1), tc = 16 * (wave & 1);
+    x = tile_product(below + (32 + tr) * L::LINE, L::LINE, inverse + tc, L::LINE, 32, col, quad);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) half[(tr + 4 * quad + r) * 33 + tc + col] = x[r];
+    __syncthreads();
+    x = tile_product(inverse + (32 + tr) * L::LINE + 32, L::LINE, half + tc, 33, 32, col, quad);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) inverse[(32 + tr + 4 * quad + r) * L::LINE + tc + col] = -x[r];
+    __syncthreads();
+    for (int p = tid; p < CHUNK * CHUNK / 4; p += 256) {
+        const int row = p >> 4, at = 4 * (p & 15);
+        float v[4];
+        const int64_t f = (unit * 8 + (row >> 4) * 2 + (at >> 5)) * N_::WIDE_FRAGMENT + ((at & 31) >> 3) * 256 + (row & 15) * 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = BACK ? inverse[(at + i) * L::LINE + row] : inverse[row * L::LINE + at + i];
+        put_wide4<T>((BACK ? a.inverse_t : a.inverse) + f, 1024, (at >> 2) & 1, v);
+    }
+    if (tid == 0) {
+        const auto rows = [&](int at) { return (uint64_t)bad[at] | (uint64_t)bad[at + 1] << 16 | (uint64_t)bad[at + 2] << 32 | (uint64_t)bad[at + 3] << 48; };
+        gates.bad_k = rows(0) | gates_bad | bad[8] | (uint64_t)bad[9] << 32;
+        gates.bad_q = rows(4);
+        gates.resets = resets;
+    }
+}
+
+// ---- from chunk to chunk ------------------------------------------------------------------------------------------------
+// Columns of values that are not finite: what they were at which step.  They are taken out of the products, which would spread them, and put back where the rule has them.
+struct Marks {
+    uint32_t any, pad[3];                 // the chunk (+ 1) that has some
+    uint32_t steps[TILE][2];
+    __device__ __forceinline__ uint64_t of(int column) const { return (uint64_t)steps[column][0] | (uint64_t)steps[column][1] << 32; }
+};
+__device__ __forceinline__ void mark(Marks &m, int column, int step, int chunk)
+{
+    atomicOr(&m.steps[column][step >> 5], 1u << (step & 31));
+    m.any = chunk + 1;
+}
+__device__ __forceinline__ uint64_t steps_between(int from, int to) { return (~0ull >> (63 - to)) & (~0ull << from); }
+
+template <typename T> __device__ __forceinline__ void store4(T *p, const float (&v)[4], int count)
+{
+    T x[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = from_f32<T>(v[r]);
+    if (count >= 4) __builtin_memcpy(p, x, sizeof x);
+    else
+#pragma unroll
+        for (int r = 0; r < 4; ++r) if (r < count) p[r] = x[r];
+}
+
+template <typename T, int KP> struct RunLds {
+    typedef Num<T> N_;
+    static constexpr int STATE_PITCH = N_::pitch(KP), ROW_PITCH = N_::pitch(CHUNK), EXACT_PITCH = N_::exact_pitch(CHUNK);
+    static constexpr int STATE = 0, ONE = STATE + TILE * STATE_PITCH, TWO = ONE + TILE * ROW_PITCH, THREE = TWO + TILE * ROW_PITCH, MARKS = THREE + TILE * ROW_PITCH;
+    static constexpr int BYTES = MARKS + (int)sizeof(Marks);
+};
+// tiles of 16 keys' entries of a wavefront
+template <int KP> constexpr int key_tiles() { return KP / 64 > 0 ? KP / 64 : 1; }
+
+template <typename T, int KP> __global__ __launch_bounds__(256) void forward_kernel(const DeltaArgs a)
+{
+    typedef RunLds<T, KP> L;
+    typedef Num<T> N_;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const hts_delta_rule_desc &d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
+    const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % d.H, n = blockIdx.x / a.tiles / d.H;
+    const int K = d.K, V = d.V, v0 = tile * TILE, group = h / (d.H / d.G), len = length_of(a, n);
+    constexpr int MT = key_tiles<KP>();
+    const bool has_keys = wave * MT * 16 < KP;
+    char *state = lds + L::STATE, *left_over = lds + L::ONE, *writes = lds + L::TWO, *late = lds + L::THREE;
+    Marks &marks = *(Marks *)(lds + L::MARKS);
+    if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
+    if (tid == TILE) marks.any = 0;
+
+    f32x4 S[MT][2];
+    const int64_t held = ((int64_t)n * d.H + h) * K * V;
+    const auto each_state = [&](auto f) {
+        if (!has_keys) return;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int k = 16 * (wave * MT + m) + 4 * quad + r, v = v0 + 16 * nt + col;
+                    S[m][nt][r] = f(S[m][nt][r], k < K && v < V, (int64_t)k * V + v);
+                }
+    };
+    const auto share_state = [&]() {
+        if (!has_keys) return;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                const float x[4] = {S[m][nt][0], S[m][nt][1], S[m][nt][2], S[m][nt][3]};
+                put_wide4<T>(state + (16 * nt + col) * L::STATE_PITCH + (2 * (wave * MT + m) + (quad >> 1)) * N_::WIDE, 16, quad & 1, x);
+            }
+    };
+    each_state([&](float, bool there, int64_t at) { return there && a.in.h_in ? a.in.h_in[held + at] : 0.0f; });
+    share_state();
+    __syncthreads();
+
+    const int used = (len + CHUNK - 1) / CHUNK;
+    for (int c = 0; c < used; ++c) {
+        const int64_t unit = ((int64_t)c * d.N + n) * d.H + h;
+        const Gates &gates = a.gates[unit];
+        const int t0 = c * CHUNK;
+        if (a.states) each_state([&](float s, bool there, int64_t at) { if (there) a.states[unit * K * V + at] = s; return s; });
+        // what the state has for the keys, and for the queries
+        f32x4 ks[2] = {}, qs[2] = {};
+        const int mine = t0 + 16 * wave + col;
+        const T *k_row = mine < len ? step_of<T>(a.in.k, mine, n) + (int64_t)group * K : nullptr, *q_row = mine < len ? step_of<T>(a.in.q, mine, n) + (int64_t)group * K : nullptr;
+#pragma unroll
+        for (int s = 0; s < KP / 32; ++s) {
+            const Exact<T> kf = exact_row(k_row, 32 * s + 8 * quad, K), qf = exact_row(q_row, 32 * s + 8 * quad, K);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                const Wide<T> sf = get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * s + quad) * N_::WIDE, 16);
+                mma(ks[nt], kf, sf);
+                mma(qs[nt], sf, qf);
+            }
+        }
+        const int row = 16 * wave + 4 * quad;             // of 4 steps, one after the other
+        float keep[4], k_unit[4], strength[4], left[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { keep[r] = gates.keep[row + r]; k_unit[r] = gates.k_unit[row + r]; strength[r] = gates.strength[row + r]; left[r] = gates.left[row + r]; }
+        const uint64_t bad_k = gates.bad_k;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const int v = v0 + 16 * nt + col;
+            float e[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool live = t0 + row + r < len && v < V;
+                e[r] = 0.0f;
+                if (live) {
+                    e[r] = to_f32(step_of<T>(a.in.v, t0 + row + r, n)[(int64_t)h * V + v]);
+                    if (keep[r] >= 0.0f) e[r] -= keep[r] * k_unit[r] * ks[nt][r];
+                    if (!finite(e[r]) || (bad_k >> (row + r) & 1)) { e[r] = 0.0f; mark(marks, 16 * nt + col, row + r, c); }
+                }
+            }
+            put_wide4<T>(left_over + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, e);
+        }
+        __syncthreads();
+        const bool some = marks.any == (uint32_t)c + 1;
+        // Z, and what it writes
+        f32x4 z[2] = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s == 1 && wave < 2) continue;              // zeros
+            const Wide<T> w = get_wide<T>(a.inverse + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) mma(z[nt], w, get_wide<T>(left_over + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16));
+        }
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            float u[4], l[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                u[r] = strength[r] * z[nt][r];
+                l[r] = left[r] >= 0.0f ? left[r] * k_unit[r] * u[r] : 0.0f;
+            }
+            put_wide4<T>(writes + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, u);
+            put_wide4<T>(late + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, l);
+            if (a.z) {
+                const int v = v0 + 16 * nt + col;
+                if (v < V)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const bool wrong = some && (marks.of(16 * nt + col) & steps_between(gates.first[row + r], row + r));
+                        if (t0 + row + r < len) a.z[unit * CHUNK * V + (int64_t)(row + r) * V + v] = wrong ? __builtin_nanf("") : z[nt][r];
+                    }
+            }
+        }
+        __syncthreads();
+        // outputs, the values along a row
+        const int i = 16 * wave + col;
+        const float asked = gates.keep[i] >= 0.0f ? gates.keep[i] * gates.q_unit[i] * d.scale : -1.0f;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) qs[nt][r] = gates.keep[i] >= 0.0f ? asked * qs[nt][r] : 0.0f;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s == 1 && wave < 2) continue;
+            const Wide<T> p = get_wide<T>(a.read + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) mma(qs[nt], get_wide<T>(writes + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16), p);
+        }
+        if (t0 + i < len) {
+            const uint64_t seen = steps_between(gates.first[i], i);
+            T *y = step_of<T>(a.y, t0 + i, n) + (int64_t)h * V;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                const int v = v0 + 16 * nt + 4 * quad;
+                float o[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = some && (marks.of(16 * nt + 4 * quad + r) & seen) ? __builtin_nanf("") : qs[nt][r];
+                store4(y + v, o, V - v);
+            }
+        }
+        // the state at the end
+        const float all = gates.keep[CHUNK - 1];
+        if (has_keys) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[m][nt][r] = all >= 0.0f ? all * S[m][nt][r] : 0.0f;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                Wide<T> l[2];
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) l[nt] = get_wide<T>(late + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const Exact<T> kf = get_exact<T>(a.keys + (unit * (KP / 8) + (wave * MT + m) * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024);
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) mma(S[m][nt], kf, l[nt]);
+                }
+            }
+            if (some) {
+                const uint64_t last = steps_between(gates.first[CHUNK - 1], CHUNK - 1);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+                        if (marks.of(16 * nt + col) & last)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) S[m][nt][r] = __builtin_nanf("");
+            }
+            share_state();
+        }
+        __syncthreads();
+        if (some) {
+            if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
+            __syncthreads();
+        }
+    }
+    if (a.h_out) each_state([&](float s, bool there, int64_t at) { if (there) a.h_out[held + at] = s; return s; });
+    for (int64_t p = tid; p < (int64_t)(d.T - len) * TILE; p += 256) {
+        const int v = v0 + (int)(p % TILE);
+        if (v < V) step_of<T>(a.y, len + p / TILE, n)[(int64_t)h * V + v] = from_f32<T>(0.0f);
+    }
+}
+
+// A few steps: the state in registers, 64 of the values' entries a workgroup, 4 to a thread, every 16th of the keys'.  One sum over the keys a step: of the state before it
+// with the key and with the query, y = scale (al q . S + (q . k) be z).
+constexpr int STEP_TILE = 64, STEP_ROWS = 8;
+template <typename T> __global__ __launch_bounds__(256) void step_kernel(const DeltaArgs a)
+{
+    const hts_delta_rule_desc &d = a.d;
+    __shared__ float kq[2][128], lengths[2][4], sums[4][2][STEP_TILE];
+    const int tid = threadIdx.x, wave = tid >> 6, four = tid & 15, rg = tid >> 4;
+    const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % d.H, n = blockIdx.x / a.tiles / d.H;
+    const int K = d.K, V = d.V, v0 = tile * STEP_TILE + 4 * four, group = h / (d.H / d.G), len = length_of(a, n), count = V - v0;
+    const int64_t held = ((int64_t)n * d.H + h) * K * V;
+    float S[STEP_ROWS][4];
+#pragma unroll
+    for (int m = 0; m < STEP_ROWS; ++m) {
+        const int k = rg + 16 * m;
+        const float *p = a.in.h_in + held + (int64_t)k * V + v0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[m][i] = 0.0f;
+        if (a.in.h_in && k < K) {
+            if (count >= 4) __builtin_memcpy(S[m], p, 16);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (i < count) S[m][i] = p[i];
+        }
+    }
+    const auto put_state = [&](float *to) {
+#pragma unroll
+        for (int m = 0; m < STEP_ROWS; ++m) {
+            const int k = rg + 16 * m;
+            if (k < K) store4(to + (int64_t)k * V + v0, S[m], count);
+        }
+    };
+    if (a.states && len > 0) put_state(a.states + held);
+    for (int t = 0; t < len; ++t) {
+        if (tid < 128) {
+            const float kv = tid < K ? to_f32(step_of<T>(a.in.k, t, n)[(int64_t)group * K + tid]) : 0.0f, qv = tid < K ? to_f32(step_of<T>(a.in.q, t, n)[(int64_t)group * K + tid]) : 0.0f;
+            kq[0][tid] = kv; kq[1][tid] = qv;
+            const float kk = wave_add(kv * kv), qq = wave_add(qv * qv), qk = wave_add(qv * kv);
+            if ((tid & 63) == 0) { lengths[wave][0] = kk; lengths[wave][1] = qq; lengths[wave][2] = qk; }
+        }
+        float val[4];
+        const T *v_row = step_of<T>(a.in.v, t, n) + (int64_t)h * V + v0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) val[i] = i < count ? to_f32(v_row[i]) : 0.0f;
+        const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
+        const double e = (double)dc.exponent * LOG2E_64;
+        const bool reset = (a.in.starts && a.in.starts[(int64_t)t * d.N + n]) || e < FORGETS;
+        const float decay = reset ? 0.0f : e < 1e30 ? exp2_wide(e) : __builtin_nanf(""), strength = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
+        if (reset)
+#pragma unroll
+            for (int m = 0; m < STEP_ROWS; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) S[m][i] = 0.0f;
+        __syncthreads();
+        float has[2][4] = {};
+#pragma unroll
+        for (int m = 0; m < STEP_ROWS; ++m) {
+            const float kv = kq[0][rg + 16 * m], qv = kq[1][rg + 16 * m];
+            if (rg + 16 * m < K)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    has[0][i] = __builtin_fmaf(kv, S[m][i], has[0][i]);
+                    has[1][i] = __builtin_fmaf(qv, S[m][i], has[1][i]);
+                }
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                has[w][i] += __shfl_xor(has[w][i], 16, 64);
+                has[w][i] += __shfl_xor(has[w][i], 32, 64);
+            }
+        if ((rg & 3) == 0)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) __builtin_memcpy(&sums[wave][w][4 * four], has[w], 16);
+        __syncthreads();
+        const float k_unit = d.normalize ? 1.0f / __builtin_sqrtf(lengths[0][0] + lengths[1][0] + 1e-6f) : 1.0f;
+        const float q_unit = d.scale * (d.normalize ? 1.0f / __builtin_sqrtf(lengths[0][1] + lengths[1][1] + 1e-6f) : 1.0f);
+        const float along = (lengths[0][2] + lengths[1][2]) * k_unit;
+        float u[4], y[4], z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float ks = (sums[0][0][4 * four + i] + sums[1][0][4 * four + i]) + (sums[2][0][4 * four + i] + sums[3][0][4 * four + i]);
+            const float qs = (sums[0][1][4 * four + i] + sums[1][1][4 * four + i]) + (sums[2][1][4 * four + i] + sums[3][1][4 * four + i]);
+            z[i] = reset ? val[i] : val[i] - decay * k_unit * ks;
+            u[i] = strength * z[i];
+            y[i] = q_unit * (reset ? along * u[i] : __builtin_fmaf(decay, qs, along * u[i]));
+        }
+#pragma unroll
+        for (int m = 0; m < STEP_ROWS; ++m) {
+            const float kv = kq[0][rg + 16 * m] * k_unit;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[m][i] = reset ? kv * u[i] : __builtin_fmaf(decay, S[m][i], kv * u[i]);
+        }
+        if (rg == 0 && count > 0) {
+            store4(step_of<T>(a.y, t, n) + (int64_t)h * V + v0, y, count);
+            if (a.z) store4(a.z + ((int64_t)n * d.H + h) * CHUNK * V + (int64_t)t * V + v0, z, count);
+        }
+        __syncthreads();
+    }
+    if (a.h_out) put_state(a.h_out + held);
+    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (rg == 0)
+        for (int t = len; t < d.T; ++t) store4(step_of<T>(a.y, t, n) + (int64_t)h * V + v0, none, count);
+}
+
+// The state's gradient from chunk to chunk, from the last one
+template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_kernel(const DeltaArgs a)
+{
+    typedef RunLds<T, KP> L;
+    typedef Num<T> N_;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const hts_delta_rule_desc &d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
+    const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % d.H, n = blockIdx.x / a.tiles / d.H;
+    const int K = d.K, V = d.V, v0 = tile * TILE, group = h / (d.H / d.G), len = length_of(a, n);
+    constexpr int MT = key_tiles<KP>();
+    const bool has_keys = wave * MT * 16 < KP;
+    // ONE: the output's gradient (Exact), TWO: that of what is written, times its strength, then minus that of the values, kept; THREE: the output's, kept
+    char *state = lds + L::STATE, *given = lds + L::ONE, *sent = lds + L::TWO, *asked = lds + L::THREE;
+    Marks &marks = *(Marks *)(lds + L::MARKS);
+    if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
+    if (tid == TILE) marks.any = 0;
+
+    f32x4 S[MT][2];
+    const int64_t held = ((int64_t)n * d.H + h) * K * V;
+    const auto each_state = [&](auto f) {
+        if (!has_keys) return;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int k = 16 * (wave * MT + m) + 4 * quad + r, v = v0 + 16 * nt + col;
+                    S[m][nt][r] = f(S[m][nt][r], k < K && v < V, (int64_t)k * V + v);
+                }
+    };
+    each_state([&](float, bool there, int64_t at) { return there && a.dh_out ? a.dh_out[held + at] : 0.0f; });
+
+    for (int c = (len + CHUNK - 1) / CHUNK - 1; c >= 0; --c) {
+        const int64_t unit = ((int64_t)c * d.N + n) * d.H + h;
+        const Gates &gates = a.gates[unit];
+        const int t0 = c * CHUNK;
+        each_state([&](float s, bool there, int64_t at) { if (there) a.late[unit * K * V + at] = s; return s; });
+        __syncthreads();                                       // (the arrays of the chunk after this one have been read)
+        if (has_keys)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    const float x[4] = {S[m][nt][0], S[m][nt][1], S[m][nt][2], S[m][nt][3]};
+                    put_wide4<T>(state + (16 * nt + col) * L::STATE_PITCH + (2 * (wave * MT + m) + (quad >> 1)) * N_::WIDE, 16, quad & 1, x);
+                }
+        {
+            // 8 steps of one of the values' entries: a thread's
+            const int v = tid & 31, i0 = 8 * (tid >> 5);
+            const uint64_t bad_q = gates.bad_q;
+            T x[8];
+            float w[2][4];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = t0 + i0 + i;
+                const bool live = t < len && v0 + v < V;
+                x[i] = live ? step_of<T>(a.dy, t, n)[(int64_t)h * V + v0 + v] : from_f32<T>(0.0f);
+                if (live && (!finite(to_f32(x[i])) || (bad_q >> (i0 + i) & 1))) { x[i] = from_f32<T>(0.0f); mark(marks, v, i0 + i, c); }
+                const float keep = gates.keep[i0 + i];
+                w[i >> 2][i & 3] = live && keep >= 0.0f && !(bad_q >> (i0 + i) & 1) ? keep * gates.q_unit[i0 + i] * d.scale * to_f32(x[i]) : 0.0f;
+            }
+            put_exact<T>(given + v * L::EXACT_PITCH + (i0 >> 3) * N_::EXACT, 16, make_exact<T>(x));
+            put_wide4<T>(asked + v * L::ROW_PITCH + (i0 >> 3) * N_::WIDE, 16, 0, w[0]);
+            put_wide4<T>(asked + v * L::ROW_PITCH + (i0 >> 3) * N_::WIDE, 16, 1, w[1]);
+        }
+        __syncthreads();
+        // dU: by the outputs of this chunk, by the state at its end
+        f32x4 du[2] = {}, ks[2] = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s == 0 && wave >= 2) continue;                 // (steps before: zeros)
+            const Wide<T> p = get_wide<T>(a.read + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) mma(du[nt], p, get_exact<T>(given + (16 * nt + col) * L::EXACT_PITCH + (4 * s + quad) * N_::EXACT, 16));
+        }
+        const int mine = t0 + 16 * wave + col;
+        const T *k_row = mine < len ? step_of<T>(a.in.k, mine, n) + (int64_t)group * K : nullptr;
+#pragma unroll
+        for (int s = 0; s < KP / 32; ++s) {
+            const Exact<T> kf = exact_row(k_row, 32 * s + 8 * quad, K);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) mma(ks[nt], kf, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * s + quad) * N_::WIDE, 16));
+        }
+        const int row = 16 * wave + 4 * quad;
+        float keep[4], k_unit[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { keep[r] = gates.keep[row + r]; k_unit[r] = gates.k_unit[row + r]; }
+        const uint64_t bad_k = gates.bad_k;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            float x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float left = gates.left[row + r];
+                x[r] = du[nt][r];
+                if (left >= 0.0f) x[r] += left * k_unit[r] * ks[nt][r];
+                x[r] *= gates.strength[row + r];
+                if (!finite(x[r]) || (bad_k >> (row + r) & 1)) { x[r] = 0.0f; if (v0 + 16 * nt + col < V) mark(marks, 16 * nt + col, row + r, c); }
+            }
+            put_wide4<T>(sent + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, x);
+        }
+        __syncthreads();
+        const bool some = marks.any == (uint32_t)c + 1;
+        f32x4 dv[2] = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s == 0 && wave >= 2) continue;
+            const Wide<T> w = get_wide<T>(a.inverse_t + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) mma(dv[nt], w, get_wide<T>(sent + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const int v = v0 + 16 * nt + col;
+            float x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] = keep[r] >= 0.0f ? -(keep[r] * k_unit[r] * dv[nt][r]) : 0.0f;
+                if (v < V && t0 + row + r < len) {
+                    // a step's gradient has what the later ones of its episode have
+                    bool wrong = false;
+                    if (some) {
+                        const uint64_t later = row + r == 63 ? 0 : gates.resets & (~0ull << (row + r + 1));
+                        wrong = marks.of(16 * nt + col) & steps_between(row + r, later ? __builtin_ctzll(later) - 1 : 63);
+                    }
+                    a.write[unit * CHUNK * V + (int64_t)(row + r) * V + v] = wrong ? __builtin_nanf("") : dv[nt][r];
+                }
+            }
+            put_wide4<T>(sent + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, x);
+        }
+        __syncthreads();
+        const float all = gates.keep[CHUNK - 1];
+        if (has_keys) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[m][nt][r] = all >= 0.0f ? all * S[m][nt][r] : 0.0f;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                Wide<T> w[2], y[2];
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    w[nt] = get_wide<T>(sent + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16);
+                    y[nt] = get_wide<T>(asked + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16);
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const int64_t f = (unit * (KP / 8) + (wave * MT + m) * 2 + s) * N_::EXACT_FRAGMENT + lane * 16;
+                    const Exact<T> kf = get_exact<T>(a.keys + f, 1024), qf = get_exact<T>(a.queries + f, 1024);
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) { mma(S[m][nt], kf, w[nt]); mma(S[m][nt], qf, y[nt]); }
+                }
+            }
+            if (some) {
+                const uint64_t before = gates.resets ? (gates.resets & 1 ? 0 : steps_between(0, __builtin_ctzll(gates.resets) - 1)) : ~0ull;
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+                        if (marks.of(16 * nt + col) & before)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) S[m][nt][r] = __builtin_nanf("");
+            }
+        }
+        if (some) {
+            __syncthreads();
+            if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
+        }
+    }
+    if (a.g.dh_in) each_state([&](float s, bool there, int64_t at) { if (there) a.g.dh_in[held + at] = s; return s; });
+}
+
+// ---- gradients that sum over the values -----------------------------------------------------------------------------------
+template <typename T, int KP> struct GradLds {
+    typedef Num<T> N_;
+    static constexpr int PITCH = N_::pitch(TILE), LINE = 68, MATRIX = 4 * CHUNK * LINE;
+    static constexpr int STATES = KP * PITCH, AREA = 2 * STATES > 3 * MATRIX ? 2 * STATES : 3 * MATRIX;
+    static constexpr int WRITES = 0, VALUES = WRITES + CHUNK * PITCH, BEFORE = VALUES + CHUNK * PITCH, LATE = BEFORE + STATES;
+    static constexpr int PARALLEL = BEFORE, CROSS = PARALLEL + MATRIX, PASSING = CROSS + MATRIX;           // (when the states have been read)
+    static constexpr int SUMS = BEFORE + AREA, BYTES = SUMS + 4 * (8 * CHUNK + 8);
+};
+
+// A workgroup for a chunk of a group's heads; SHARED: more than one, one after the other.
+//
+// The gradient of the logarithm of a step's decay is the sum of what passes the step: C[i][j], the part of the gradient that goes through G[i][j], of all pairs j < step <= i, and of the
+// state before the chunk and its end.  (Those are also a difference of sums, q . dq - v . dv of the steps from it on, in which what does not pass it cancels, and with
+// strong decays all digits: 1.7e-4 of dA's values against 64 bits, 512 x 16 steps of 8 heads, now 4e-7.)
+template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(256) void grads_kernel(const DeltaArgs a)
+{
+    typedef GradLds<T, KP> L;
+    typedef Num<T> N_;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int KT = KP / 16;
+    const hts_delta_rule_desc &d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
+    const int group = blockIdx.x % d.G, n = blockIdx.x / d.G % d.N, c = blockIdx.x / d.G / d.N, per = d.H / d.G, t0 = c * CHUNK, len = length_of(a, n);
+    const int K = d.K, V = d.V, row = 16 * wave + 4 * quad, steps = d.T - t0 < CHUNK ? d.T - t0 : CHUNK;
+    float *part = a.part + ((int64_t)c * d.N + n) * 2 * d.H;
+    if (t0 >= len) {
+        for (int i = wave; i < steps; i += 4) {
+            for (int k = lane; k < K; k += 64) step_of<T>(a.g.dq, t0 + i, n)[(int64_t)group * K + k] = step_of<T>(a.g.dk, t0 + i, n)[(int64_t)group * K + k] = from_f32<T>(0.0f);
+            for (int v = lane; v < per * V; v += 64) step_of<T>(a.g.dv, t0 + i, n)[(int64_t)group * per * V + v] = from_f32<T>(0.0f);
+            for (int h = lane; h < per; h += 64) step_of<T>(a.g.da, t0 + i, n)[group * per + h] = step_of<T>(a.g.db, t0 + i, n)[group * per + h] = from_f32<T>(0.0f);
+        }
+        for (int h = tid; h < per; h += 256) part[group * per + h] = part[d.H + group * per + h] = 0.0f;
+        return;
+    }
+    char *writes = lds + L::WRITES, *values = lds + L::VALUES, *before = lds + L::BEFORE, *late = lds + L::LATE;
+    float *parallel = (float *)(lds + L::PARALLEL), *cross = (float *)(lds + L::CROSS), *passing = (float *)(lds + L::PASSING);
+    // [64] each: q . dq by the state before the chunk less the same of k; k . dk by the state's at the end; z . dv; 4 parts of C's sums.  [8]: <dS', S> by wavefront
+    float *sums = (float *)(lds + L::SUMS);
+    const int mine = t0 + 16 * wave + col;
+    const T *q_mine = mine < len ? step_of<T>(a.in.q, mine, n) + (int64_t)group * K : nullptr, *k_mine = mine < len ? step_of<T>(a.in.k, mine, n) + (int64_t)group * K : nullptr;
+    const auto key_at = [&](const hts_steps &s, int r, int k) { return t0 + row + r < len && k < K ? to_f32(step_of<T>(s, t0 + row + r, n)[(int64_t)group * K + k]) : 0.0f; };
+    f32x4 dq[SHARED ? KT : 1] = {}, dk[SHARED ? KT : 1] = {};      // of the queries (scaled) and keys of length one, of the heads so far
+    // back through the lengths, and out
+    const auto finish = [&](const f32x4 *gq, const f32x4 *gk, const Gates &gates) {
+        float q_dq[4] = {}, k_dk[4] = {}, q_unit[4], k_unit[4];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                q_dq[r] = __builtin_fmaf(key_at(a.in.q, r, 16 * kt + col), gq[kt][r], q_dq[r]);
+                k_dk[r] = __builtin_fmaf(key_at(a.in.k, r, 16 * kt + col), gk[kt][r], k_dk[r]);
+            }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            q_unit[r] = gates.q_unit[row + r]; k_unit[r] = gates.k_unit[row + r];
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) { q_dq[r] += __shfl_xor(q_dq[r], o, 64); k_dk[r] += __shfl_xor(k_dk[r], o, 64); }
+            q_dq[r] *= q_unit[r] * d.scale;
+            k_dk[r] *= k_unit[r];
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int k = 16 * kt + col, t = t0 + row + r;
+                if (k >= K || t >= d.T) continue;
+                float x = 0.0f, y = 0.0f;
+                if (t < len) {
+                    x = d.scale * gq[kt][r];
+                    y = gk[kt][r];
+                    if (d.normalize) {
+                        x = q_unit[r] * (x - q_unit[r] * key_at(a.in.q, r, k) * q_dq[r]);
+                        y = k_unit[r] * (y - k_unit[r] * key_at(a.in.k, r, k) * k_dk[r]);
+                    }
+                }
+                step_of<T>(a.g.dq, t, n)[(int64_t)group * K + k] = from_f32<T>(x);
+                step_of<T>(a.g.dk, t, n)[(int64_t)group * K + k] = from_f32<T>(y);
+            }
+    };
+    for (int hh = 0; hh < (SHARED ? per : 1); ++hh) {
+        const int h = group * per + hh;
+        const int64_t unit = ((int64_t)c * d.N + n) * d.H + h;
+        const Gates &gates = a.gates[unit];
+        const float all = gates.keep[CHUNK - 1];
+        f32x4 par[4] = {}, cro[4] = {}, q_state[KT] = {}, k_late[KT] = {}, k_state[KT] = {};
+        float z_dv = 0.0f, end = 0.0f;
+        const int my_row = tid >> 2, my_part = tid & 3;
+        const bool my_live = t0 + my_row < len;
+        const float my_strength = gates.strength[my_row];
+        for (int v0 = 0; v0 < V; v0 += TILE) {
+            __syncthreads();
+            {
+                const int v = v0 + 8 * my_part;
+                float z[8], g[8], u[8];
+                const int64_t at = unit * CHUNK * V + (int64_t)my_row * V;
+                row8(z, my_live ? a.z + at : nullptr, v, V);
+                row8(g, my_live ? a.write + at : nullptr, v, V);
+                T *out = my_row < steps ? step_of<T>(a.g.dv, t0 + my_row, n) + (int64_t)h * V + v : nullptr;
+                T o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    z_dv = __builtin_fmaf(z[i], g[i], z_dv);
+                    u[i] = my_strength * z[i];
+                    o[i] = from_f32<T>(g[i]);
+                }
+                if (out) {
+                    if (v + 8 <= V) __builtin_memcpy(out, o, sizeof o);
+                    else
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) if (v + i < V) out[i] = o[i];
+                }
+                const int p = my_row * L::PITCH + my_part * N_::WIDE;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float ua[4] = {u[4 * half], u[4 * half + 1], u[4 * half + 2], u[4 * half + 3]}, ga[4] = {g[4 * half], g[4 * half + 1], g[4 * half + 2], g[4 * half + 3]};
+                    put_wide4<T>(writes + p, 16, half, ua);
+                    put_wide4<T>(values + p, 16, half, ga);
+                }
+            }
+            for (int p = tid; p < KP * 4; p += 256) {
+                const int k = p >> 2, v = v0 + 8 * (p & 3);
+                float s[8], g[8];
+                row8(s, k < K ? a.states + (unit * K + k) * V : nullptr, v, V);
+                row8(g, k < K ? a.late + (unit * K + k) * V : nullptr, v, V);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) end = __builtin_fmaf(s[i], g[i], end);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float sa[4] = {s[4 * half], s[4 * half + 1], s[4 * half + 2], s[4 * half + 3]}, ga[4] = {g[4 * half], g[4 * half + 1], g[4 * half + 2], g[4 * half + 3]};
+                    put_wide4<T>(before + k * L::PITCH + (p & 3) * N_::WIDE, 16, half, sa);
+                    put_wide4<T>(late + k * L::PITCH + (p & 3) * N_::WIDE, 16, half, ga);
+                }
+            }
+            __syncthreads();
+            const Exact<T> y = exact_row(mine < len ? step_of<T>(a.dy, mine, n) + (int64_t)h * V : nullptr, v0 + 8 * quad, V);
+            const Wide<T> u = get_wide<T>(writes + (16 * wave + col) * L::PITCH + quad * N_::WIDE, 16), g = get_wide<T>(values + (16 * wave + col) * L::PITCH + quad * N_::WIDE, 16);
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt)
+                if (jt <= wave) {
+                    const Wide<T> b = get_wide<T>(writes + (16 * jt + col) * L::PITCH + quad * N_::WIDE, 16);
+                    mma(par[jt], y, b);
+                    mma(cro[jt], g, b);
+                }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const Wide<T> s = get_wide<T>(before + (16 * kt + col) * L::PITCH + quad * N_::WIDE, 16), l = get_wide<T>(late + (16 * kt + col) * L::PITCH + quad * N_::WIDE, 16);
+                mma(q_state[kt], y, s);
+                mma(k_state[kt], g, s);
+                mma(k_late[kt], u, l);
+            }
+        }
+        __syncthreads();
+        // the steps' own: dY U^T G, -dV U^T G, and what passes from step to step
+        float keep[4], left[4], q_unit[4], k_unit[4];
+        double far_i[4];
+        int ep_i[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            keep[r] = gates.keep[row + r]; left[r] = gates.left[row + r]; far_i[r] = gates.far[row + r]; ep_i[r] = gates.episode[row + r];
+            k_unit[r] = gates.k_unit[row + r]; q_unit[r] = gates.q_unit[row + r];
+        }
+        const uint64_t bad_q = gates.bad_q, bad_k = gates.bad_k;
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            const int j = 16 * jt + col;
+            f32x4 qk = {0.0f, 0.0f, 0.0f, 0.0f}, kk = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (jt <= wave) {
+                const T *k_row = t0 + j < len ? step_of<T>(a.in.k, t0 + j, n) + (int64_t)group * K : nullptr;
+#pragma unroll
+                for (int s = 0; s < KP / 32; ++s) {
+                    const Exact<T> kj = exact_row(k_row, 32 * s + 8 * quad, K);
+                    mma(qk, exact_row(q_mine, 32 * s + 8 * quad, K), kj);
+                    mma(kk, exact_row(k_mine, 32 * s + 8 * quad, K), kj);
+                }
+            }
+            const double far_j = gates.far[j];
+            const float unit_j = gates.k_unit[j];
+            const int ep_j = gates.episode[j];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = row + r;
+                const bool sees = j <= i && ep_j == ep_i[r];
+                const float ratio = sees ? exp2_wide(far_i[r] - far_j) : 0.0f;
+                const float p = sees ? par[jt][r] * ratio : 0.0f, x = sees && j < i ? -(cro[jt][r] * ratio) : 0.0f;
+                parallel[i * L::LINE + j] = p;
+                cross[i * L::LINE + j] = x;
+                passing[i * L::LINE + j] = sees && j < i ? unit_j * (p * (q_unit[r] * d.scale * qk[r]) + x * (k_unit[r] * kk[r])) : 0.0f;
+            }
+        }
+        float from_late[4] = {}, from_state[4] = {};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float kv = key_at(a.in.k, r, 16 * kt + col) * k_unit[r], qv = key_at(a.in.q, r, 16 * kt + col) * (q_unit[r] * d.scale);
+                if (keep[r] >= 0.0f) {
+                    q_state[kt][r] *= keep[r];
+                    const float x = keep[r] * k_state[kt][r];
+                    from_state[r] = __builtin_fmaf(qv, q_state[kt][r], __builtin_fmaf(-kv, x, from_state[r]));
+                    k_state[kt][r] = x;
+                } else q_state[kt][r] = k_state[kt][r] = 0.0f;
+                k_late[kt][r] = left[r] >= 0.0f ? left[r] * k_late[kt][r] : 0.0f;
+                if (left[r] >= 0.0f) from_late[r] = __builtin_fmaf(kv, k_late[kt][r], from_late[r]);
+                k_late[kt][r] -= k_state[kt][r];
+            }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) { from_state[r] += __shfl_xor(from_state[r], o, 64); from_late[r] += __shfl_xor(from_late[r], o, 64); }
+            if (col == 0) { sums[row + r] = from_state[r]; sums[CHUNK + row + r] = from_late[r]; }
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) z_dv += __shfl_xor(z_dv, o, 64);
+        if (my_part == 0) sums[2 * CHUNK + my_row] = z_dv;
+        end = wave_add(end);
+        if (lane == 0) sums[8 * CHUNK + wave] = end;
+        __syncthreads();
+        {
+            // C's sums along each row up to a column: 16 columns a thread, and those of the threads before it
+            float *line = passing + my_row * L::LINE + 16 * my_part, x = 0.0f;
+            float below[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) { below[j] = x; x += line[j]; }
+            float before_mine = 0.0f;
+#pragma unroll
+            for (int o = 1; o < 4; ++o) {
+                const float other = __shfl(x, (lane & ~3) + o - 1, 64);
+                if (o <= my_part) before_mine += other;
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) line[j] = before_mine + below[j];
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            // rows 16 w + col: of dQ, of dK by the queries that look at them, of dK by the keys on both sides
+            const int i = 16 * wave + col, at = 32 * s + 8 * quad;
+            float m1[8], m2[8], m3[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const float unit_j = gates.k_unit[at + x];
+                m1[x] = parallel[i * L::LINE + at + x] * unit_j;
+                const bool ok = !(bad_q >> (at + x) & 1);
+                m2[x] = ok ? parallel[(at + x) * L::LINE + i] * gates.q_unit[at + x] * d.scale : 0.0f;
+                m3[x] = (cross[i * L::LINE + at + x] + cross[(at + x) * L::LINE + i]) * unit_j;
+            }
+            const Wide<T> w1 = make_wide<T>(m1), w2 = make_wide<T>(m2), w3 = make_wide<T>(m3);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const int64_t f = (unit * (KP / 8) + kt * 2 + s) * N_::EXACT_FRAGMENT + lane * 16;
+                const Exact<T> kf = get_exact<T>(a.keys + f, 1024), qf = get_exact<T>(a.queries + f, 1024);
+                mma(q_state[kt], w1, kf);
+                mma(k_late[kt], w2, qf);
+                mma(k_late[kt], w3, kf);
+            }
+        }
+        if constexpr (SHARED)
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) { dq[kt] += q_state[kt]; dk[kt] += k_late[kt]; }
+        else finish(q_state, k_late, gates);
+        __syncthreads();
+        {
+            // ... and down a column from its row on
+            float x = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int at = 16 * wave + i;
+                if (at >= lane) x += passing[at * L::LINE + lane];
+            }
+            sums[(3 + wave) * CHUNK + lane] = x;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            // the gates
+            const int t = t0 + lane;
+            const bool live = t < len;
+            float after = sums[lane], earlier = sums[CHUNK + lane];         // of the state before the chunk: this step and later ones'; at its end: earlier ones'
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const float x = __shfl_down(after, o, 64), y = __shfl_up(earlier, o, 64);
+                if (lane + o < 64) after += x;
+                if (lane >= o) earlier += y;
+            }
+            earlier = __shfl_up(earlier, 1, 64);
+            float g = after + (lane > 0 ? earlier : 0.0f) + ((sums[3 * CHUNK + lane] + sums[4 * CHUNK + lane]) + (sums[5 * CHUNK + lane] + sums[6 * CHUNK + lane]));
+            if (all >= 0.0f) g += all * ((sums[8 * CHUNK] + sums[8 * CHUNK + 1]) + (sums[8 * CHUNK + 2] + sums[8 * CHUNK + 3]));
+            float da = 0.0f, dA = 0.0f;
+            if (live) {
+                const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
+                if (!(gates.resets >> lane & 1)) { da = g * a.in.A[h] * dc.slope; dA = g * dc.delta; }
+                if (bad_k >> lane & 1) da = dA = __builtin_nanf("");
+                step_of<T>(a.g.da, t, n)[h] = from_f32<T>(da);
+                step_of<T>(a.g.db, t, n)[h] = from_f32<T>((1.0f - gates.strength[lane]) * sums[2 * CHUNK + lane]);
+            } else if (t < d.T) step_of<T>(a.g.da, t, n)[h] = step_of<T>(a.g.db, t, n)[h] = from_f32<T>(0.0f);
+            dA = wave_add(dA); da = wave_add(da);
+            if (lane == 0) { part[h] = dA; part[d.H + h] = da; }
+        }
+        if constexpr (SHARED) if (hh == per - 1) finish(dq, dk, gates);
+    }
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------------
+// (more LDS than 64 KB has to be asked for)
+template <class F> hipError_t launch(F kernel, int64_t groups, int lds, hipStream_t stream, const DeltaArgs &a)
+{
+    if (groups == 0) return hipSuccess;
+    if (!launchable(groups, 256) || groups > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(256), (uint32_t)lds, stream, a);
+    return hipGetLastError();
+}
+template <typename F> hipError_t by_keys(int K, F f)
+{
+    if (K <= 32) return f(std::integral_constant<int, 32>{});
+    if (K <= 64) return f(std::integral_constant<int, 64>{});
+    return f(std::integral_constant<int, 128>{});
+}
+int keys_padded(int K) { return K <= 32 ? 32 : K <= 64 ? 64 : 128; }
+
+constexpr int MOST_STEPS = 16;            // calls of so many steps or fewer go step by step
+
+struct Layout { int64_t inverse, read, keys, queries, gates, late, write, part, total; };
+Layout layout(const hts_delta_rule_desc &d, bool back)
+{
+    const int64_t units = ceil_div(d.T, CHUNK) * d.N * d.H, wide = d.precision == HTS_PRECISION_BF16 ? 3072 : 2048, exact = d.precision == HTS_PRECISION_BF16 ? 1024 : 2048;
+    Layout l;
+    l.inverse = 0;
+    l.read = l.inverse + units * 8 * wide;
+    l.keys = l.read + units * 8 * wide;
+    l.queries = l.keys + units * (keys_padded(d.K) / 8) * exact;
+    l.gates = l.queries + (back ? units * (keys_padded(d.K) / 8) * exact : 0);
+    l.late = l.gates + round_up(units * (int64_t)sizeof(Gates), 256);
+    l.write = l.late + (back ? round_up(units * d.K * d.V * 4, 256) : 0);
+    l.part = l.write + (back ? round_up(units * CHUNK * d.V * 4, 256) : 0);
+    l.total = l.part + (back ? round_up(ceil_div(d.T, CHUNK) * d.N * 2 * d.H * 4, 256) : 0);
+    return l;
+}
+DeltaArgs arguments(hts_seq_ctx &c, const DeltaOp &op, bool back)
+{
+    const Layout l = layout(op.d, back);
+    DeltaArgs a = {};
+    a.d = op.d; a.in = op.in; a.y = op.y; a.dy = op.dy; a.h_out = op.h_out; a.states = op.states; a.dh_out = op.dh_out; a.g = op.g;
+    a.chunks = (int)ceil_div(op.d.T, CHUNK);
+    a.tiles = (int)ceil_div(op.d.V, TILE);
+    if (op.states) a.z = op.states + delta_state_floats(op.d);
+    a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates);
+    a.late = (float *)(c.ws + l.late); a.write = (float *)(c.ws + l.write); a.part = (float *)(c.ws + l.part);
+    return a;
+}
+template <typename T> hipError_t forward(hts_seq_ctx &c, const DeltaOp &op)
+{
+    const hts_delta_rule_desc &d = op.d;
+    DeltaArgs a = arguments(c, op, false);
+    if (d.T <= MOST_STEPS) {
+        a.tiles = (int)ceil_div(d.V, STEP_TILE);
+        return launch(step_kernel<T>, (int64_t)d.N * d.H * a.tiles, 0, c.stream, a);
+    }
+    return by_keys(d.K, [&](auto kp) {
+        constexpr int KP = decltype(kp)::value;
+        const hipError_t e = launch(prep_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
+        return e != hipSuccess ? e : launch(forward_kernel<T, KP>, (int64_t)d.N * d.H * a.tiles, RunLds<T, KP>::BYTES, c.stream, a);
+    });
+}
+template <typename T> hipError_t backward(hts_seq_ctx &c, const DeltaOp &op)
+{
+    const hts_delta_rule_desc &d = op.d;
+    const DeltaArgs a = arguments(c, op, true);
+    const hipError_t e = by_keys(d.K, [&](auto kp) {
+        constexpr int KP = decltype(kp)::value;
+        hipError_t e = launch(prep_kernel<T, KP, true>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
+        if (e == hipSuccess) e = launch(reverse_kernel<T, KP>, (int64_t)d.N * d.H * a.tiles, RunLds<T, KP>::BYTES, c.stream, a);
+        if (e == hipSuccess) e = launch(d.H > d.G ? grads_kernel<T, KP, true> : grads_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.G, GradLds<T, KP>::BYTES, c.stream, a);
+        return e;
+    });
+    if (e != hipSuccess) return e;
+    return launch_sum_partials(c, a.part, (int64_t)a.chunks * d.N, 2 * (int64_t)d.H, SumTarget{op.g.dA, d.H}, SumTarget{op.g.da_bias, d.H}, SumTarget{nullptr, 0});
+}
+}  // namespace
+
+int64_t delta_workspace(const hts_delta_rule_desc &d, bool back) { return !back && d.T <= MOST_STEPS ? 0 : layout(d, back).total; }
+int64_t delta_state_floats(const hts_delta_rule_desc &d) { return round_up(ceil_div(d.T, CHUNK) * d.N * d.H * d.K * d.V, 4); }
+int64_t delta_states(const hts_delta_rule_desc &d) { return delta_state_floats(d) + ceil_div(d.T, CHUNK) * CHUNK * d.N * d.H * d.V; }
+
+hipError_t launch_delta(hts_seq_ctx &c, const DeltaOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? forward<bf16_t>(c, op) : forward<float>(c, op); }
+hipError_t launch_delta_backward(hts_seq_ctx &c, const DeltaOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? backward<bf16_t>(c, op) : backward<float>(c, op); }
+
+}  // namespace hts

@@ -1,0 +1,282 @@
+// Layer norm of rows and its gradients (see include/hts.h).
+//
+//   y = (x - mean) r w + b,  r = 1 / sqrt(var + eps);   with h = (x - mean) r, g = dy w:  dx = r (g - mean(g) - h mean(g h)) + add,  dw = sum dy h,  db = sum dy
+//
+// Bound by bytes: a row is read once, into the registers of a wavefront (up to 2048 entries), of four or of sixteen, its variance is the mean square of what is left
+// after the mean is taken off, so that nothing cancels, and it is written once.  The backward call keeps nothing of the forward call: the mean and r of a row
+// that is in registers cost two reductions and no bytes.
+#include "seq.hpp"
+
+namespace hts {
+namespace {
+
+struct NormArgs {
+    const void *x, *dy, *add;
+    void *y, *dx;
+    int64_t x_ld, dy_ld, add_ld, y_ld, dx_ld;
+    const float *w, *b;
+    float *part;              // [workgroups][2 F]: dw, db
+    float eps;
+    int M, F;
+    bool sums;                // dw or db is wanted
+};
+
+// What a thread holds of a row: PER times VEC neighbouring entries, 16 bytes, of which `count` exist.  16-byte accesses at any address: the hardware takes them.
+template <typename T> struct Piece {
+    static constexpr int V = 16 / (int)sizeof(T);
+    T e[V];
+    __device__ __forceinline__ void load(const T *p, int count)
+    {
+        if (count >= V) __builtin_memcpy(this, p, 16);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) e[i] = i < count ? p[i] : from_f32<T>(0.0f);
+    }
+    __device__ __forceinline__ void store(T *p, int count) const
+    {
+        if (count >= V) __builtin_memcpy(p, this, 16);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) if (i < count) p[i] = e[i];
+    }
+};
+template <int V> __device__ __forceinline__ void load_params(float (&v)[V], const float *p, int count, float none)
+{
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = none;
+    } else if (count >= V) __builtin_memcpy(v, p, sizeof v);
+    else
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = i < count ? p[i] : 0.0f;
+}
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+// The sums of N values over the ROW threads of a row.  Every wavefront adds the others' sums in the same order.
+template <int ROW, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float *shared)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (ROW > 64) {
+        constexpr int W = ROW / 64;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) shared[(threadIdx.x >> 6) * N + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.0f;
+            for (int k = 0; k < W; ++k) v[i] += shared[k * N + i];
+        }
+    }
+}
+
+// (x - mean) of a row that is in registers (0 where there is no entry), and r
+template <typename T, int ROW, int PER> __device__ __forceinline__ float centre(const Piece<T> (&x)[PER], float (&h)[PER][Piece<T>::V], const int first, const int F, const float eps, float *shared)
+{
+    constexpr int V = Piece<T>::V;
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[0] += h[p][i] = to_f32(x[p].e[i]);
+    row_sums<ROW>(s, shared);
+    const float mean = s[0] / (float)F;
+    s[0] = 0.0f;
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            h[p][i] = first + p * ROW * V + i < F ? h[p][i] - mean : 0.0f;
+            s[0] = __builtin_fmaf(h[p][i], h[p][i], s[0]);
+        }
+    row_sums<ROW>(s, shared);
+    return 1.0f / __builtin_sqrtf(s[0] / (float)F + eps);
+}
+
+template <typename T, int ROW, int PER> __global__ __launch_bounds__(ROW > 256 ? ROW : 256) void norm_kernel(const NormArgs a)
+{
+    constexpr int V = Piece<T>::V, ROWS = ROW > 256 ? 1 : 256 / ROW;
+    __shared__ float shared[16];
+    const int in_row = ROW == 64 ? threadIdx.x & 63 : threadIdx.x, first = in_row * V;
+    float w[PER][V], b[PER][V];
+    bool have = false;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / ROW; row < a.M; row += (int64_t)gridDim.x * ROWS) {
+        Piece<T> x[PER];
+#pragma unroll
+        for (int p = 0; p < PER; ++p) x[p].load((const T *)a.x + row * a.x_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+        if (!have)
+#pragma unroll
+            for (int p = 0; p < PER; ++p) {
+                const int at = first + p * ROW * V;
+                load_params<V>(w[p], a.w ? a.w + at : nullptr, a.F - at, 1.0f);
+                load_params<V>(b[p], a.b ? a.b + at : nullptr, a.F - at, 0.0f);
+            }
+        have = true;
+        float h[PER][V];
+        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, shared);
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            Piece<T> y;
+#pragma unroll
+            for (int i = 0; i < V; ++i) y.e[i] = from_f32<T>(__builtin_fmaf(h[p][i] * r, w[p][i], b[p][i]));
+            y.store((T *)a.y + row * a.y_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+        }
+    }
+}
+
+constexpr int BACK_ROWS = 8;           // rows that a workgroup's wavefronts work on at a time, where a row is a wavefront's
+template <int ROW> constexpr int back_threads() { return ROW == 64 ? 64 * BACK_ROWS : ROW; }
+
+template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_threads<ROW>()) void norm_backward_kernel(const NormArgs a)
+{
+    constexpr int V = Piece<T>::V, ROWS = back_threads<ROW>() / ROW, COLS = ROW * PER * V;
+    __shared__ float shared[ROWS > 1 ? ROWS * COLS : 32];
+    const int in_row = ROW == 64 ? threadIdx.x & 63 : threadIdx.x, first = in_row * V, wave = threadIdx.x / ROW;
+    float w[PER][V], dw[PER][V], db[PER][V];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const int at = first + p * ROW * V;
+        load_params<V>(w[p], a.w ? a.w + at : nullptr, a.F - at, 1.0f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) dw[p][i] = db[p][i] = 0.0f;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + wave; row < a.M; row += (int64_t)gridDim.x * ROWS) {
+        Piece<T> x[PER], dy[PER], add[PER];
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int at = first + p * ROW * V;
+            x[p].load((const T *)a.x + row * a.x_ld + at, a.F - at);
+            dy[p].load((const T *)a.dy + row * a.dy_ld + at, a.F - at);
+        }
+        if (a.dx && a.add)
+#pragma unroll
+            for (int p = 0; p < PER; ++p) add[p].load((const T *)a.add + row * a.add_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+        float h[PER][V];
+        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, shared);
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int p = 0; p < PER; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = to_f32(dy[p].e[i]), g = d * w[p][i];
+                h[p][i] *= r;
+                dw[p][i] = __builtin_fmaf(d, h[p][i], dw[p][i]);
+                db[p][i] += d;
+                s[0] += g;
+                s[1] = __builtin_fmaf(g, h[p][i], s[1]);
+            }
+        if (!a.dx) continue;
+        row_sums<ROW>(s, shared);
+        const float mean = s[0] / (float)a.F, along = s[1] / (float)a.F;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            Piece<T> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float g = to_f32(dy[p].e[i]) * w[p][i] - mean;
+                float v = r * __builtin_fmaf(-h[p][i], along, g);
+                if (a.add) v += to_f32(add[p].e[i]);
+                o.e[i] = from_f32<T>(v);
+            }
+            o.store((T *)a.dx + row * a.dx_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+        }
+    }
+    if (!a.sums) return;
+    // a workgroup's sums: its rows in the order of its wavefronts
+    float *part = a.part + (int64_t)blockIdx.x * 2 * a.F;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if constexpr (ROWS > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < PER; ++p)
+#pragma unroll
+                for (int i = 0; i < V; ++i) shared[wave * COLS + first + p * ROW * V + i] = which ? db[p][i] : dw[p][i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.F; c += back_threads<ROW>()) {
+                float s = 0.0f;
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) s += shared[k * COLS + c];
+                part[which * a.F + c] = s;
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < PER; ++p)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int c = first + p * ROW * V + i;
+                    if (c < a.F) part[which * a.F + c] = which ? db[p][i] : dw[p][i];
+                }
+        }
+    }
+}
+
+// Entries of a row that a thread holds, and threads of a row: a wavefront up to 2048 entries, four up to 8192, sixteen up to 16384
+template <int V, typename F> hipError_t by_width(int width, F f)
+{
+    const int64_t per = ceil_div(width, 64 * V);
+    const auto with = [&](auto row, auto entries) { return f(std::integral_constant<int, decltype(row)::value>{}, std::integral_constant<int, decltype(entries)::value / V>{}); };
+    typedef std::integral_constant<int, 64> wave;
+    typedef std::integral_constant<int, 256> four;
+    typedef std::integral_constant<int, 1024> sixteen;
+    if (per * V <= 8) return with(wave{}, std::integral_constant<int, 8>{});
+    if (per * V <= 16) return with(wave{}, std::integral_constant<int, 16>{});
+    if (per * V <= 32) return with(wave{}, std::integral_constant<int, 32>{});
+    if (per * V <= 64) return with(four{}, std::integral_constant<int, 16>{});
+    if (per * V <= 128) return with(four{}, std::integral_constant<int, 32>{});
+    return with(sixteen{}, std::integral_constant<int, 16>{});
+}
+
+constexpr int MOST_PARTS = 256;        // workgroups of a backward call whose sums are added up afterwards
+int back_parts(int64_t M, int64_t F)
+{
+    const int64_t rows = F <= 2048 ? BACK_ROWS : 1, groups = ceil_div(M, rows);
+    return (int)(groups < MOST_PARTS ? groups : MOST_PARTS);
+}
+
+template <typename T> hipError_t norm(hts_seq_ctx &c, const NormArgs &a)
+{
+    return by_width<Piece<T>::V>(a.F, [&](auto row, auto per) {
+        constexpr int ROW = decltype(row)::value, PER = decltype(per)::value, ROWS = ROW > 256 ? 1 : 256 / ROW;
+        const int64_t groups = ceil_div(a.M, ROWS), most = (int64_t)c.cus * (ROW > 256 ? 2 : 8);
+        hipLaunchKernelGGL((norm_kernel<T, ROW, PER>), dim3((uint32_t)(groups < most ? groups : most)), dim3(ROW > 256 ? ROW : 256), 0, c.stream, a);
+        return hipGetLastError();
+    });
+}
+template <typename T> hipError_t norm_backward(hts_seq_ctx &c, const NormArgs &a, float *dw, float *db)
+{
+    const int parts = back_parts(a.M, a.F);
+    const hipError_t e = by_width<Piece<T>::V>(a.F, [&](auto row, auto per) {
+        constexpr int ROW = decltype(row)::value, PER = decltype(per)::value;
+        hipLaunchKernelGGL((norm_backward_kernel<T, ROW, PER>), dim3((uint32_t)parts), dim3(back_threads<ROW>()), 0, c.stream, a);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || !a.sums) return e;
+    return launch_sum_partials(c, a.part, parts, 2 * (int64_t)a.F, SumTarget{dw, a.F}, SumTarget{db, a.F}, SumTarget{nullptr, 0});
+}
+}  // namespace
+
+int64_t norm_workspace(int64_t M, int64_t F) { return 8 * back_parts(M, F) * F; }
+
+hipError_t launch_norm(hts_seq_ctx &c, int precision, const NormOp &op)
+{
+    NormArgs a = {};
+    a.x = op.x.p; a.x_ld = op.x.ld; a.y = op.y.p; a.y_ld = op.y.ld; a.w = op.w; a.b = op.b; a.eps = op.eps; a.M = op.M; a.F = op.F;
+    return precision == HTS_PRECISION_BF16 ? norm<bf16_t>(c, a) : norm<float>(c, a);
+}
+hipError_t launch_norm_backward(hts_seq_ctx &c, int precision, const NormOp &op)
+{
+    NormArgs a = {};
+    a.x = op.x.p; a.x_ld = op.x.ld; a.dy = op.dy.p; a.dy_ld = op.dy.ld; a.add = op.add.p; a.add_ld = op.add.ld; a.dx = op.dx.p; a.dx_ld = op.dx.ld;
+    a.w = op.w; a.eps = op.eps; a.M = op.M; a.F = op.F; a.sums = op.dw || op.db; a.part = (float *)c.ws;
+    return precision == HTS_PRECISION_BF16 ? norm_backward<bf16_t>(c, a, op.dw, op.db) : norm_backward<float>(c, a, op.dw, op.db);
+}
+
+}  // namespace hts

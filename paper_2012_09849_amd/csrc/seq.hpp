@@ -1,4 +1,4 @@
-// Sequence memory: declarations and device helpers shared by linear.hip, shortconv.hip, scan.hip and seqapi.hip (not part of the C ABI).
+// Sequence memory: declarations and device helpers shared by linear.hip, shortconv.hip, scan.hip, layernorm.hip, delta.hip and seqapi.hip (not part of the C ABI).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -40,16 +40,40 @@ struct ScanOp {
     hts_scan_grads g;
 };
 
+struct NormOp {
+    int M, F;
+    float eps;
+    hts_rows x, y, dy, add, dx;
+    const float *w, *b;
+    float *dw, *db;
+};
+struct DeltaOp {
+    hts_delta_rule_desc d;
+    hts_delta_rule_inputs in;
+    hts_steps y, dy;
+    float *h_out, *states;                  // states: written by the forward call, read by the backward call
+    const float *dh_out;
+    hts_delta_rule_grads g;
+};
+
 int64_t linear_workspace(int precision, int act, int64_t M, int64_t N, int64_t K);      // of the backward call; the forward call needs none
 int64_t conv_workspace(int64_t T, int64_t N, int64_t D, int W);
 int64_t scan_workspace(const hts_scan_desc &d, bool backward);
 int64_t scan_states(const hts_scan_desc &d);
+int64_t norm_workspace(int64_t M, int64_t F);
+int64_t delta_workspace(const hts_delta_rule_desc &d, bool backward);
+int64_t delta_states(const hts_delta_rule_desc &d);
+int64_t delta_state_floats(const hts_delta_rule_desc &d);        // of them the chunks' states
 hipError_t launch_linear(hts_seq_ctx &c, int precision, const LinearOp &op);
 hipError_t launch_linear_backward(hts_seq_ctx &c, int precision, const LinearOp &op);
 hipError_t launch_conv(hts_seq_ctx &c, int precision, const ConvOp &op);
 hipError_t launch_conv_backward(hts_seq_ctx &c, int precision, const ConvOp &op);
 hipError_t launch_scan(hts_seq_ctx &c, const ScanOp &op);
 hipError_t launch_scan_backward(hts_seq_ctx &c, const ScanOp &op);
+hipError_t launch_norm(hts_seq_ctx &c, int precision, const NormOp &op);
+hipError_t launch_norm_backward(hts_seq_ctx &c, int precision, const NormOp &op);
+hipError_t launch_delta(hts_seq_ctx &c, const DeltaOp &op);
+hipError_t launch_delta_backward(hts_seq_ctx &c, const DeltaOp &op);
 
 // out = sum over p of part[p][0 .. width), in a fixed order; consecutive entries go to up to three arrays (p NULL: not wanted)
 struct SumTarget { float *p; int64_t n; };

@@ -279,3 +279,136 @@ extern "C" int32_t hts_selective_scan_backward(hts_seq_ctx *ctx, const hts_scan_
     LAUNCH_TRY(launch_scan_backward(*ctx, op));
     return HTS_OK;
 }
+
+// ---- layer norm ---------------------------------------------------------------------------------------------------
+static int32_t check_norm(const hts_layer_norm_desc *d)
+{
+    if (!d) return HTS_EINVAL;
+    if (d->M <= 0 || d->F <= 0 || !(d->eps >= 0.0f && d->eps <= 3.402823466e38f)) return HTS_EINVAL;
+    return bad_precision(d->precision) || d->M > (1 << 24) || d->F > 16384 ? HTS_ESHAPE : HTS_OK;
+}
+
+extern "C" int64_t hts_layer_norm_workspace(const hts_layer_norm_desc *d)
+{
+    CHECK(check_norm(d));
+    return norm_workspace(d->M, d->F);
+}
+
+extern "C" int32_t hts_layer_norm(hts_seq_ctx *ctx, const hts_layer_norm_desc *d, hts_rows x, const float *w, const float *b, hts_rows y)
+{
+    if (!ctx) return HTS_EINVAL;
+    CHECK(check_norm(d));
+    const int s = size_of(d->precision);
+    CHECK(check_rows(x, d->M, d->F, s, false)); CHECK(check_rows(y, d->M, d->F, s, true));
+    if (misaligned(w, 4) || misaligned(b, 4)) return HTS_EINVAL;
+    CHECK(check_apart(span(y.p, y.ld, d->M, d->F, s), {span(w, 0, 1, d->F, 4), span(b, 0, 1, d->F, 4)}, span(x.p, x.ld, d->M, d->F, s)));
+    NormOp op = {};
+    op.M = d->M; op.F = d->F; op.eps = d->eps; op.x = x; op.y = y; op.w = w; op.b = b;
+    LAUNCH_TRY(launch_norm(*ctx, d->precision, op));
+    return HTS_OK;
+}
+
+extern "C" int32_t hts_layer_norm_backward(hts_seq_ctx *ctx, const hts_layer_norm_desc *d, hts_rows x, const float *w, hts_rows dy, hts_rows add,
+                                           hts_rows dx, float *dw, float *db)
+{
+    if (!ctx) return HTS_EINVAL;
+    CHECK(check_norm(d));
+    if (!dx.p && !dw && !db) return HTS_EINVAL;
+    const int s = size_of(d->precision);
+    CHECK(check_rows(x, d->M, d->F, s, false)); CHECK(check_rows(dy, d->M, d->F, s, false));
+    if (dx.p) {
+        CHECK(check_rows(dx, d->M, d->F, s, true));
+        if (add.p) CHECK(check_rows(add, d->M, d->F, s, false));
+    } else add.p = nullptr;
+    if (misaligned(w, 4) || misaligned(dw, 4) || misaligned(db, 4)) return HTS_EINVAL;
+    const Span xs = span(x.p, x.ld, d->M, d->F, s), gs = span(dy.p, dy.ld, d->M, d->F, s), as = span(add.p, add.ld, d->M, d->F, s), ws = span(w, 0, 1, d->F, 4);
+    const Span dxs = span(dx.p, dx.ld, d->M, d->F, s), dws = span(dw, 0, 1, d->F, 4), dbs = span(db, 0, 1, d->F, 4);
+    // a row's gradient takes its place in any of what it comes from, which may be one another
+    for (const Span &place : {xs, gs, as}) if (meet(dxs, place) && !same(dxs, place)) return HTS_EINVAL;
+    CHECK(check_apart(dxs, {ws, dws, dbs}, Span{})); CHECK(check_apart(dws, {xs, gs, as, ws, dbs}, Span{})); CHECK(check_apart(dbs, {xs, gs, as, ws}, Span{}));
+    if (dw || db) CHECK(check_workspace(ctx, norm_workspace(d->M, d->F)));
+    NormOp op = {};
+    op.M = d->M; op.F = d->F; op.eps = d->eps; op.x = x; op.w = w; op.dy = dy; op.add = add; op.dx = dx; op.dw = dw; op.db = db;
+    LAUNCH_TRY(launch_norm_backward(*ctx, d->precision, op));
+    return HTS_OK;
+}
+
+// ---- gated delta rule ---------------------------------------------------------------------------------------------
+static int32_t check_delta(const hts_delta_rule_desc *d)
+{
+    if (!d) return HTS_EINVAL;
+    if (d->T <= 0 || d->N <= 0 || d->H <= 0 || d->G <= 0 || d->K <= 0 || d->V <= 0 || (d->normalize != 0 && d->normalize != 1) || (d->softplus != 0 && d->softplus != 1) ||
+        !(d->scale >= -3.402823466e38f && d->scale <= 3.402823466e38f)) return HTS_EINVAL;
+    if (bad_precision(d->precision) || d->T > MOST_STEPS || d->N > (1 << 24) || d->H > (1 << 16) || d->H % d->G != 0 || d->K > 128 || d->V > (1 << 16)) return HTS_ESHAPE;
+    // (workgroups for a chunk of 64 steps of a head, and for 32 values of a head, are counted in 31 bits)
+    const int64_t heads = (int64_t)d->N * d->H, most = (1ll << 31) - 1;
+    return heads > most || ceil_div(d->T, 64) > most / heads || ceil_div(d->V, 32) > most / heads ? HTS_ESHAPE : HTS_OK;
+}
+
+extern "C" int64_t hts_delta_rule_workspace(const hts_delta_rule_desc *d)
+{
+    CHECK(check_delta(d));
+    const int64_t forward = delta_workspace(*d, false), backward = delta_workspace(*d, true);
+    return forward > backward ? forward : backward;
+}
+extern "C" int64_t hts_delta_rule_states(const hts_delta_rule_desc *d)
+{
+    CHECK(check_delta(d));
+    return delta_states(*d);
+}
+
+static int32_t check_delta_arrays(const hts_delta_rule_desc *d, const hts_delta_rule_inputs *given, hts_delta_rule_inputs *in)
+{
+    if (!given) return HTS_EINVAL;
+    *in = *given;
+    const int s = size_of(d->precision);
+    const int64_t keys = (int64_t)d->G * d->K, values = (int64_t)d->H * d->V;
+    CHECK(check_steps(in->q, d->T, d->N, keys, s, false)); CHECK(check_steps(in->k, d->T, d->N, keys, s, false)); CHECK(check_steps(in->v, d->T, d->N, values, s, false));
+    CHECK(check_steps(in->a, d->T, d->N, d->H, s, false)); CHECK(check_steps(in->b, d->T, d->N, d->H, s, false));
+    return !in->A || misaligned(in->A, 4) || misaligned(in->a_bias, 4) || misaligned(in->lengths, 4) || misaligned(in->h_in, 4) ? HTS_EINVAL : HTS_OK;
+}
+// an output in an input's place (outputs beside inputs in a wider array are the caller's)
+static bool takes_place(const hts_steps &out, const hts_delta_rule_inputs &in) { return out.p == in.q.p || out.p == in.k.p || out.p == in.v.p || out.p == in.a.p || out.p == in.b.p; }
+
+extern "C" int32_t hts_delta_rule(hts_seq_ctx *ctx, const hts_delta_rule_desc *d, const hts_delta_rule_inputs *in, hts_steps y, float *h_out, float *states)
+{
+    if (!ctx) return HTS_EINVAL;
+    CHECK(check_delta(d));
+    DeltaOp op = {};
+    op.d = *d;
+    CHECK(check_delta_arrays(d, in, &op.in));
+    CHECK(check_steps(y, d->T, d->N, (int64_t)d->H * d->V, size_of(d->precision), true));
+    if (misaligned(h_out, 4) || misaligned(states, 16) || takes_place(y, op.in) || (states && (states == h_out || states == op.in.h_in))) return HTS_EINVAL;
+    CHECK(check_workspace(ctx, delta_workspace(*d, false)));
+    op.y = y; op.h_out = h_out; op.states = states;
+    LAUNCH_TRY(launch_delta(*ctx, op));
+    return HTS_OK;
+}
+
+extern "C" int32_t hts_delta_rule_backward(hts_seq_ctx *ctx, const hts_delta_rule_desc *d, const hts_delta_rule_inputs *in, hts_steps dy,
+                                           const float *dh_out, const float *states, const hts_delta_rule_grads *grads)
+{
+    if (!ctx || !grads || !states) return HTS_EINVAL;
+    CHECK(check_delta(d));
+    DeltaOp op = {};
+    op.d = *d;
+    CHECK(check_delta_arrays(d, in, &op.in));
+    hts_delta_rule_grads *g = &op.g;
+    *g = *grads;
+    const int s = size_of(d->precision);
+    const int64_t keys = (int64_t)d->G * d->K, values = (int64_t)d->H * d->V;
+    CHECK(check_steps(dy, d->T, d->N, values, s, false));
+    CHECK(check_steps(g->dq, d->T, d->N, keys, s, true)); CHECK(check_steps(g->dk, d->T, d->N, keys, s, true)); CHECK(check_steps(g->dv, d->T, d->N, values, s, true));
+    CHECK(check_steps(g->da, d->T, d->N, d->H, s, true)); CHECK(check_steps(g->db, d->T, d->N, d->H, s, true));
+    if (!g->dA || misaligned(g->dA, 4) || misaligned(g->da_bias, 4) || misaligned(g->dh_in, 4) || misaligned(states, 16) || misaligned(dh_out, 4)) return HTS_EINVAL;
+    const hts_steps *outs[] = {&g->dq, &g->dk, &g->dv, &g->da, &g->db};
+    for (int i = 0; i < 5; ++i) {
+        if (takes_place(*outs[i], op.in) || outs[i]->p == dy.p) return HTS_EINVAL;
+        for (int k = 0; k < i; ++k) if (outs[i]->p == outs[k]->p) return HTS_EINVAL;
+    }
+    if (g->dA == g->da_bias || (g->dh_in && (g->dh_in == dh_out || g->dh_in == op.in.h_in || g->dh_in == states))) return HTS_EINVAL;
+    CHECK(check_workspace(ctx, delta_workspace(*d, true)));
+    op.dy = dy; op.dh_out = dh_out; op.states = const_cast<float *>(states);
+    LAUNCH_TRY(launch_delta_backward(*ctx, op));
+    return HTS_OK;
+}
