@@ -589,7 +589,13 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
         for (int t = len; t < d.T; ++t) store4(step_of<T>(a.y, t, n) + (int64_t)h * V + v0, none, count);
 }
 
-// The state's gradient from chunk to chunk, from the last one
+__device__ __forceinline__ float sign_of(int chunk, int n) { return (chunk + n) & 1 ? -1.0f : 1.0f; }
+
+// The state's gradient from chunk to chunk, from the last one.
+//
+// What a matrix instruction drops of its products goes towards minus infinity.  Gradients have either sign, but keys, queries, values and states may be mostly positive, and then
+// the sums of the decays' gradients over thousands of steps add up what was dropped (da_bias 4.6e-6 of its values off, 512 x 16 steps).  So every second chunk has all gradients
+// with the other sign, here and in the sums after it.
 template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_kernel(const DeltaArgs a)
 {
     typedef RunLds<T, KP> L;
@@ -623,11 +629,19 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
     };
     each_state([&](float, bool there, int64_t at) { return there && a.dh_out ? a.dh_out[held + at] : 0.0f; });
 
+    float held_sign = 1.0f;
     for (int c = (len + CHUNK - 1) / CHUNK - 1; c >= 0; --c) {
         const int64_t unit = ((int64_t)c * d.N + n) * d.H + h;
         const Gates &gates = a.gates[unit];
         const int t0 = c * CHUNK;
-        each_state([&](float s, bool there, int64_t at) { if (there) a.late[unit * K * V + at] = s; return s; });
+        const float sign = sign_of(c, n);
+        if (sign != held_sign)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) S[m][nt] = -S[m][nt];
+        held_sign = sign;
+        each_state([&](float s, bool there, int64_t at) { if (there) a.late[unit * K * V + at] = sign * s; return s; });
         __syncthreads();                                       // (the arrays of the chunk after this one have been read)
         if (has_keys)
 #pragma unroll
@@ -647,7 +661,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
             for (int i = 0; i < 8; ++i) {
                 const int t = t0 + i0 + i;
                 const bool live = t < len && v0 + v < V;
-                x[i] = live ? step_of<T>(a.dy, t, n)[(int64_t)h * V + v0 + v] : from_f32<T>(0.0f);
+                x[i] = from_f32<T>(live ? sign * to_f32(step_of<T>(a.dy, t, n)[(int64_t)h * V + v0 + v]) : 0.0f);
                 if (live && (!finite(to_f32(x[i])) || (bad_q >> (i0 + i) & 1))) { x[i] = from_f32<T>(0.0f); mark(marks, v, i0 + i, c); }
                 const float keep = gates.keep[i0 + i];
                 w[i >> 2][i & 3] = live && keep >= 0.0f && !(bad_q >> (i0 + i) & 1) ? keep * gates.q_unit[i0 + i] * d.scale * to_f32(x[i]) : 0.0f;
@@ -717,7 +731,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
                         const uint64_t later = row + r == 63 ? 0 : gates.resets & (~0ull << (row + r + 1));
                         wrong = marks.of(16 * nt + col) & steps_between(row + r, later ? __builtin_ctzll(later) - 1 : 63);
                     }
-                    a.write[unit * CHUNK * V + (int64_t)(row + r) * V + v] = wrong ? __builtin_nanf("") : dv[nt][r];
+                    a.write[unit * CHUNK * V + (int64_t)(row + r) * V + v] = wrong ? __builtin_nanf("") : sign * dv[nt][r];
                 }
             }
             put_wide4<T>(sent + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, x);
@@ -763,321 +777,447 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
             if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
         }
     }
-    if (a.g.dh_in) each_state([&](float s, bool there, int64_t at) { if (there) a.g.dh_in[held + at] = s; return s; });
+    if (a.g.dh_in) each_state([&](float s, bool there, int64_t at) { if (there) a.g.dh_in[held + at] = held_sign * s; return s; });
 }
 
 // ---- gradients that sum over the values -----------------------------------------------------------------------------------
+// Eight wavefronts.  Products with the states: a wavefront has 16 of the keys' entries and up to four tiles of 16 steps, so a state's entry is read and cut into parts by
+// one wavefront (two or four where keys are short), straight from memory.  A tile's rows are steps 32 (t / 2) + 8 (row / 4) + 4 (t % 2) + row % 4, so that the 8 steps of a
+// lane's two tiles are those of a fragment of the keys: their values are there for sums along them.
 template <typename T, int KP> struct GradLds {
     typedef Num<T> N_;
-    static constexpr int PITCH = N_::pitch(TILE), LINE = 68, MATRIX = 4 * CHUNK * LINE;
-    static constexpr int STATES = KP * PITCH, AREA = 2 * STATES > 3 * MATRIX ? 2 * STATES : 3 * MATRIX;
-    static constexpr int WRITES = 0, VALUES = WRITES + CHUNK * PITCH, BEFORE = VALUES + CHUNK * PITCH, LATE = BEFORE + STATES;
-    static constexpr int PARALLEL = BEFORE, CROSS = PARALLEL + MATRIX, PASSING = CROSS + MATRIX;           // (when the states have been read)
-    static constexpr int SUMS = BEFORE + AREA, BYTES = SUMS + 4 * (8 * CHUNK + 8);
+    static constexpr int PITCH = N_::pitch(TILE), Y_PITCH = N_::exact_pitch(TILE), LINE = 68;
+    static constexpr int WRITES = 0, VALUES = WRITES + CHUNK * PITCH, GIVEN = VALUES + CHUNK * PITCH, STAGE = GIVEN + CHUNK * Y_PITCH;      // two of these, in turn
+    // after the values: a matrix of 64 x 64, what passes from step to step; at last the rows that leave
+    static constexpr int MATRIX = 0, MATRIX_PITCH = N_::pitch(CHUNK), PASSING = MATRIX + CHUNK * MATRIX_PITCH, AFTER = PASSING + 4 * CHUNK * LINE;
+    static constexpr int OUT_PITCH = KP * (int)sizeof(T) + 16, OUT = 2 * CHUNK * OUT_PITCH;
+    static constexpr int AREA = (2 * STAGE > AFTER ? 2 * STAGE : AFTER) > OUT ? (2 * STAGE > AFTER ? 2 * STAGE : AFTER) : OUT;
+    static constexpr int ROWS = AREA, SUMS = ROWS + 4 * 2 * 8 * CHUNK, BYTES = SUMS + 4 * (5 * CHUNK + 8);
 };
 
-// A workgroup for a chunk of a group's heads; SHARED: more than one, one after the other.
+template <int CONTROL> __device__ __forceinline__ float add_moved(float x) { return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xf, 0xf, true)); }
+// over 16 neighbouring lanes: pairs, fours, eights (mirrored), sixteen
+__device__ __forceinline__ float add16(float x) { return add_moved<0x140>(add_moved<0x141>(add_moved<0x4E>(add_moved<0xB1>(x)))); }
+template <typename T> __device__ __forceinline__ void row4(T (&x)[4], const T *row, int at, int K)
+{
+    if (row && at + 4 <= K) __builtin_memcpy(x, row + at, sizeof x);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = row && at + i < K ? row[at + i] : from_f32<T>(0.0f);
+}
+__device__ __forceinline__ float entry(const Exact<float> &x, int i) { return x.e[i]; }
+__device__ __forceinline__ float entry(const Exact<bf16_t> &x, int i) { return (float)x.v[i]; }
+
+// the entry of the fragments that row 4 q + r of a lane's tile t is
+template <typename T> __device__ __forceinline__ float entry(const Exact<T> (&f)[2], int t, int r) { return t & 1 ? (t & 2 ? entry(f[1], 4 + r) : entry(f[0], 4 + r)) : t & 2 ? entry(f[1], r) : entry(f[0], r); }
+
+// A workgroup for a chunk of a head.  SHARED: other heads have the same queries and keys, whose gradients leave in binary32, to be added up.
 //
 // The gradient of the logarithm of a step's decay is the sum of what passes the step: C[i][j], the part of the gradient that goes through G[i][j], of all pairs j < step <= i, and of the
 // state before the chunk and its end.  (Those are also a difference of sums, q . dq - v . dv of the steps from it on, in which what does not pass it cancels, and with
-// strong decays all digits: 1.7e-4 of dA's values against 64 bits, 512 x 16 steps of 8 heads, now 4e-7.)
-template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(256) void grads_kernel(const DeltaArgs a)
+// strong decays all digits: 1.7e-4 of dA's values against 64 bits, 512 x 16 steps of 8 heads.)
+template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) void grads_kernel(const DeltaArgs a)
 {
     typedef GradLds<T, KP> L;
     typedef Num<T> N_;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    constexpr int KT = KP / 16;
+    constexpr int KT = KP / 16, IT = KT / 2;
     const hts_delta_rule_desc &d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
-    const int group = blockIdx.x % d.G, n = blockIdx.x / d.G % d.N, c = blockIdx.x / d.G / d.N, per = d.H / d.G, t0 = c * CHUNK, len = length_of(a, n);
-    const int K = d.K, V = d.V, row = 16 * wave + 4 * quad, steps = d.T - t0 < CHUNK ? d.T - t0 : CHUNK;
+    const int64_t unit = blockIdx.x;
+    const int h = (int)(unit % d.H), n = (int)(unit / d.H % d.N), c = (int)(unit / d.H / d.N), group = h / (d.H / d.G), t0 = c * CHUNK, len = length_of(a, n);
+    const int K = d.K, V = d.V, steps = d.T - t0 < CHUNK ? d.T - t0 : CHUNK;
     float *part = a.part + ((int64_t)c * d.N + n) * 2 * d.H;
     if (t0 >= len) {
-        for (int i = wave; i < steps; i += 4) {
-            for (int k = lane; k < K; k += 64) step_of<T>(a.g.dq, t0 + i, n)[(int64_t)group * K + k] = step_of<T>(a.g.dk, t0 + i, n)[(int64_t)group * K + k] = from_f32<T>(0.0f);
-            for (int v = lane; v < per * V; v += 64) step_of<T>(a.g.dv, t0 + i, n)[(int64_t)group * per * V + v] = from_f32<T>(0.0f);
-            for (int h = lane; h < per; h += 64) step_of<T>(a.g.da, t0 + i, n)[group * per + h] = step_of<T>(a.g.db, t0 + i, n)[group * per + h] = from_f32<T>(0.0f);
+        for (int i = wave; i < steps; i += 8) {
+            if constexpr (!SHARED)
+                for (int k = lane; k < K; k += 64) step_of<T>(a.g.dq, t0 + i, n)[(int64_t)group * K + k] = step_of<T>(a.g.dk, t0 + i, n)[(int64_t)group * K + k] = from_f32<T>(0.0f);
+            for (int v = lane; v < V; v += 64) step_of<T>(a.g.dv, t0 + i, n)[(int64_t)h * V + v] = from_f32<T>(0.0f);
+            if (lane == 0) step_of<T>(a.g.da, t0 + i, n)[h] = step_of<T>(a.g.db, t0 + i, n)[h] = from_f32<T>(0.0f);
         }
-        for (int h = tid; h < per; h += 256) part[group * per + h] = part[d.H + group * per + h] = 0.0f;
+        if (tid == 0) part[h] = part[d.H + h] = 0.0f;
         return;
     }
-    char *writes = lds + L::WRITES, *values = lds + L::VALUES, *before = lds + L::BEFORE, *late = lds + L::LATE;
-    float *parallel = (float *)(lds + L::PARALLEL), *cross = (float *)(lds + L::CROSS), *passing = (float *)(lds + L::PASSING);
-    // [64] each: q . dq by the state before the chunk less the same of k; k . dk by the state's at the end; z . dv; 4 parts of C's sums.  [8]: <dS', S> by wavefront
-    float *sums = (float *)(lds + L::SUMS);
-    const int mine = t0 + 16 * wave + col;
-    const T *q_mine = mine < len ? step_of<T>(a.in.q, mine, n) + (int64_t)group * K : nullptr, *k_mine = mine < len ? step_of<T>(a.in.k, mine, n) + (int64_t)group * K : nullptr;
-    const auto key_at = [&](const hts_steps &s, int r, int k) { return t0 + row + r < len && k < K ? to_f32(step_of<T>(s, t0 + row + r, n)[(int64_t)group * K + k]) : 0.0f; };
-    f32x4 dq[SHARED ? KT : 1] = {}, dk[SHARED ? KT : 1] = {};      // of the queries (scaled) and keys of length one, of the heads so far
-    // back through the lengths, and out
-    const auto finish = [&](const f32x4 *gq, const f32x4 *gk, const Gates &gates) {
-        float q_dq[4] = {}, k_dk[4] = {}, q_unit[4], k_unit[4];
+    // with the states: keys 16 kt .. and tiles first_tile ..; of the steps among themselves: rows 16 ti .., by the outputs' gradients (wavefronts 0 .. 3) or by the values' (4 .. 7)
+    const int kt = wave % KT, first_tile = wave / KT * IT, ti = wave & 3;
+    const bool by_values = wave >= 4;
+    const float sign = sign_of(c, n);
+    const auto tile_row = [](int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); };
+    char *matrix = lds + L::MATRIX;
+    float *passing = (float *)(lds + L::PASSING), *rows = (float *)(lds + L::ROWS);       // rows: [2][KT][64] sums along the keys
+    float *sums = (float *)(lds + L::SUMS);                                               // [64]: z . dv; 4 x what passes; [8]: <dS', S>
+    Exact<T> kf[2], qf[2];
+    const int my_row = tid >> 3, my_part = tid & 7;
+    const bool my_live = t0 + my_row < len;
+    const Gates &gates = a.gates[unit];
+    f32x4 by_step[4] = {}, by_seen[4] = {};                  // rows 16 ti .. with columns 16 jt .., and the same the other way round
+    f32x4 q_state[IT] = {}, k_late[IT] = {}, k_state[IT] = {};
+    float z_dv = 0.0f, end = 0.0f;
+    const float my_strength = gates.strength[my_row];
+    float z[4], g[4], s8[8], l8[8];
+    T y[4];
+    const int64_t at_row = unit * CHUNK * V + (int64_t)my_row * V, at_state = (unit * K + 16 * kt + col) * V;
+    const bool has_key = 16 * kt + col < K;
+    const auto load = [&](int v0) {
+        row4(z, my_live ? a.z + at_row : nullptr, v0 + 4 * my_part, V);
+        row4(g, my_live ? a.write + at_row : nullptr, v0 + 4 * my_part, V);
+        row4(y, my_live ? step_of<T>(a.dy, t0 + my_row, n) + (int64_t)h * V : nullptr, v0 + 4 * my_part, V);
+        row8(s8, has_key ? a.states + at_state : nullptr, v0 + 8 * quad, V);
+        row8(l8, has_key ? a.late + at_state : nullptr, v0 + 8 * quad, V);
+    };
+    load(0);
+    for (int v0 = 0, turn = 0; v0 < V; v0 += TILE, turn ^= 1) {
+        char *writes = lds + turn * L::STAGE + L::WRITES, *values = lds + turn * L::STAGE + L::VALUES, *given = lds + turn * L::STAGE + L::GIVEN;
+        {
+            const int p = my_row * L::PITCH + (my_part >> 1) * N_::WIDE;
+            float u[4];
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                q_dq[r] = __builtin_fmaf(key_at(a.in.q, r, 16 * kt + col), gq[kt][r], q_dq[r]);
-                k_dk[r] = __builtin_fmaf(key_at(a.in.k, r, 16 * kt + col), gk[kt][r], k_dk[r]);
+            for (int i = 0; i < 4; ++i) { z_dv = __builtin_fmaf(z[i], g[i], z_dv); u[i] = sign * my_strength * z[i]; }
+            put_wide4<T>(writes + p, 16, my_part & 1, u);
+            put_wide4<T>(values + p, 16, my_part & 1, g);
+            __builtin_memcpy(given + my_row * L::Y_PITCH + 4 * my_part * sizeof(T), y, sizeof y);
+            if (my_row < steps) {
+                const int v = v0 + 4 * my_part;
+                store4(step_of<T>(a.g.dv, t0 + my_row, n) + (int64_t)h * V + v, g, V - v);
             }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { end = __builtin_fmaf(s8[i], l8[i], end); s8[i] *= sign; }
+        const Wide<T> sf = make_wide<T>(s8), lf = make_wide<T>(l8);
+        if (v0 + TILE < V) load(v0 + TILE);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < IT; ++t) {
+            const int row = tile_row(first_tile + t, col);
+            mma(q_state[t], get_exact<T>(given + row * L::Y_PITCH + quad * N_::EXACT, 16), sf);
+            mma(k_state[t], get_wide<T>(values + row * L::PITCH + quad * N_::WIDE, 16), sf);
+            mma(k_late[t], get_wide<T>(writes + row * L::PITCH + quad * N_::WIDE, 16), lf);
+        }
+        const Exact<T> yf = get_exact<T>(given + (16 * ti + col) * L::Y_PITCH + quad * N_::EXACT, 16);
+        const Wide<T> gf = get_wide<T>(values + (16 * ti + col) * L::PITCH + quad * N_::WIDE, 16);
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt)
+            if (jt <= ti) {
+                const Wide<T> u = get_wide<T>(writes + (16 * jt + col) * L::PITCH + quad * N_::WIDE, 16);
+                if (by_values) { mma(by_step[jt], gf, u); mma(by_seen[jt], u, gf); }
+                else { mma(by_step[jt], yf, u); mma(by_seen[jt], u, yf); }
+            }
+    }
+    // sums along the keys of what goes through the state before the chunk, and through the one at its end
+    const auto fragment = [&](const char *base, int s) { return get_exact<T>(base + (unit * (KP / 8) + kt * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024); };
+#pragma unroll
+    for (int s = 0; s < 2; ++s) { kf[s] = fragment(a.keys, s); qf[s] = fragment(a.queries, s); }
+#pragma unroll
+    for (int t = 0; t < IT; ++t) {
+        const int tt = first_tile + t, step = tile_row(tt, 4 * quad);
+        float keep[4], left[4], q_unit[4], k_unit[4];
+        __builtin_memcpy(keep, gates.keep + step, 16); __builtin_memcpy(left, gates.left + step, 16);
+        __builtin_memcpy(q_unit, gates.q_unit + step, 16); __builtin_memcpy(k_unit, gates.k_unit + step, 16);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            q_unit[r] = gates.q_unit[row + r]; k_unit[r] = gates.k_unit[row + r];
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) { q_dq[r] += __shfl_xor(q_dq[r], o, 64); k_dk[r] += __shfl_xor(k_dk[r], o, 64); }
-            q_dq[r] *= q_unit[r] * d.scale;
-            k_dk[r] *= k_unit[r];
+            const float kv = entry(kf, tt, r) * k_unit[r];
+            const float qv = entry(qf, tt, r) * (q_unit[r] * d.scale);
+            float from_state = 0.0f, from_late = 0.0f;
+            if (keep[r] >= 0.0f) {
+                q_state[t][r] *= sign * keep[r];
+                k_state[t][r] *= sign * keep[r];
+                from_state = __builtin_fmaf(qv, q_state[t][r], -kv * k_state[t][r]);
+            } else q_state[t][r] = k_state[t][r] = 0.0f;
+            if (left[r] >= 0.0f) {
+                k_late[t][r] *= sign * left[r];
+                from_late = kv * k_late[t][r];
+            } else k_late[t][r] = 0.0f;
+            k_late[t][r] -= k_state[t][r];
+            from_state = add16(from_state); from_late = add16(from_late);
+            if (col == 0) { rows[kt * CHUNK + step + r] = from_state; rows[(KT + kt) * CHUNK + step + r] = from_late; }
         }
+    }
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int k = 16 * kt + col, t = t0 + row + r;
-                if (k >= K || t >= d.T) continue;
-                float x = 0.0f, y = 0.0f;
-                if (t < len) {
-                    x = d.scale * gq[kt][r];
-                    y = gk[kt][r];
-                    if (d.normalize) {
-                        x = q_unit[r] * (x - q_unit[r] * key_at(a.in.q, r, k) * q_dq[r]);
-                        y = k_unit[r] * (y - k_unit[r] * key_at(a.in.k, r, k) * k_dk[r]);
-                    }
-                }
-                step_of<T>(a.g.dq, t, n)[(int64_t)group * K + k] = from_f32<T>(x);
-                step_of<T>(a.g.dk, t, n)[(int64_t)group * K + k] = from_f32<T>(y);
-            }
-    };
-    for (int hh = 0; hh < (SHARED ? per : 1); ++hh) {
-        const int h = group * per + hh;
-        const int64_t unit = ((int64_t)c * d.N + n) * d.H + h;
-        const Gates &gates = a.gates[unit];
-        const float all = gates.keep[CHUNK - 1];
-        f32x4 par[4] = {}, cro[4] = {}, q_state[KT] = {}, k_late[KT] = {}, k_state[KT] = {};
-        float z_dv = 0.0f, end = 0.0f;
-        const int my_row = tid >> 2, my_part = tid & 3;
-        const bool my_live = t0 + my_row < len;
-        const float my_strength = gates.strength[my_row];
-        for (int v0 = 0; v0 < V; v0 += TILE) {
-            __syncthreads();
-            {
-                const int v = v0 + 8 * my_part;
-                float z[8], g[8], u[8];
-                const int64_t at = unit * CHUNK * V + (int64_t)my_row * V;
-                row8(z, my_live ? a.z + at : nullptr, v, V);
-                row8(g, my_live ? a.write + at : nullptr, v, V);
-                T *out = my_row < steps ? step_of<T>(a.g.dv, t0 + my_row, n) + (int64_t)h * V + v : nullptr;
-                T o[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    z_dv = __builtin_fmaf(z[i], g[i], z_dv);
-                    u[i] = my_strength * z[i];
-                    o[i] = from_f32<T>(g[i]);
-                }
-                if (out) {
-                    if (v + 8 <= V) __builtin_memcpy(out, o, sizeof o);
-                    else
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) if (v + i < V) out[i] = o[i];
-                }
-                const int p = my_row * L::PITCH + my_part * N_::WIDE;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float ua[4] = {u[4 * half], u[4 * half + 1], u[4 * half + 2], u[4 * half + 3]}, ga[4] = {g[4 * half], g[4 * half + 1], g[4 * half + 2], g[4 * half + 3]};
-                    put_wide4<T>(writes + p, 16, half, ua);
-                    put_wide4<T>(values + p, 16, half, ga);
-                }
-            }
-            for (int p = tid; p < KP * 4; p += 256) {
-                const int k = p >> 2, v = v0 + 8 * (p & 3);
-                float s[8], g[8];
-                row8(s, k < K ? a.states + (unit * K + k) * V : nullptr, v, V);
-                row8(g, k < K ? a.late + (unit * K + k) * V : nullptr, v, V);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) end = __builtin_fmaf(s[i], g[i], end);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float sa[4] = {s[4 * half], s[4 * half + 1], s[4 * half + 2], s[4 * half + 3]}, ga[4] = {g[4 * half], g[4 * half + 1], g[4 * half + 2], g[4 * half + 3]};
-                    put_wide4<T>(before + k * L::PITCH + (p & 3) * N_::WIDE, 16, half, sa);
-                    put_wide4<T>(late + k * L::PITCH + (p & 3) * N_::WIDE, 16, half, ga);
-                }
-            }
-            __syncthreads();
-            const Exact<T> y = exact_row(mine < len ? step_of<T>(a.dy, mine, n) + (int64_t)h * V : nullptr, v0 + 8 * quad, V);
-            const Wide<T> u = get_wide<T>(writes + (16 * wave + col) * L::PITCH + quad * N_::WIDE, 16), g = get_wide<T>(values + (16 * wave + col) * L::PITCH + quad * N_::WIDE, 16);
-#pragma unroll
-            for (int jt = 0; jt < 4; ++jt)
-                if (jt <= wave) {
-                    const Wide<T> b = get_wide<T>(writes + (16 * jt + col) * L::PITCH + quad * N_::WIDE, 16);
-                    mma(par[jt], y, b);
-                    mma(cro[jt], g, b);
-                }
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const Wide<T> s = get_wide<T>(before + (16 * kt + col) * L::PITCH + quad * N_::WIDE, 16), l = get_wide<T>(late + (16 * kt + col) * L::PITCH + quad * N_::WIDE, 16);
-                mma(q_state[kt], y, s);
-                mma(k_state[kt], g, s);
-                mma(k_late[kt], u, l);
-            }
-        }
-        __syncthreads();
-        // the steps' own: dY U^T G, -dV U^T G, and what passes from step to step
-        float keep[4], left[4], q_unit[4], k_unit[4];
+    for (int o = 1; o < 8; o <<= 1) z_dv += __shfl_xor(z_dv, o, 64);
+    if (my_part == 0) sums[my_row] = z_dv;
+    end = wave_add(first_tile == 0 ? end : 0.0f);
+    if (lane == 0) sums[5 * CHUNK + wave] = end;
+    // the steps among themselves, each pair's decay on it
+    const int row = 16 * ti + 4 * quad, i_seen = 16 * ti + col;
+    const T *mine = t0 + i_seen < len ? step_of<T>(by_values ? a.in.k : a.in.q, t0 + i_seen, n) + (int64_t)group * K : nullptr;
+    f32x4 pass[4] = {};
+    {
         double far_i[4];
         int ep_i[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            keep[r] = gates.keep[row + r]; left[r] = gates.left[row + r]; far_i[r] = gates.far[row + r]; ep_i[r] = gates.episode[row + r];
-            k_unit[r] = gates.k_unit[row + r]; q_unit[r] = gates.q_unit[row + r];
-        }
-        const uint64_t bad_q = gates.bad_q, bad_k = gates.bad_k;
+        float unit_i[4];
+        __builtin_memcpy(far_i, gates.far + row, 32); __builtin_memcpy(ep_i, gates.episode + row, 16);
+        __builtin_memcpy(unit_i, (by_values ? gates.k_unit : gates.q_unit) + row, 16);
+        const double far_seen = gates.far[i_seen];
+        const int ep_seen = gates.episode[i_seen];
 #pragma unroll
         for (int jt = 0; jt < 4; ++jt) {
+            if (jt > ti) continue;
             const int j = 16 * jt + col;
-            f32x4 qk = {0.0f, 0.0f, 0.0f, 0.0f}, kk = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (jt <= wave) {
-                const T *k_row = t0 + j < len ? step_of<T>(a.in.k, t0 + j, n) + (int64_t)group * K : nullptr;
+            const T *k_row = t0 + j < len ? step_of<T>(a.in.k, t0 + j, n) + (int64_t)group * K : nullptr;
 #pragma unroll
-                for (int s = 0; s < KP / 32; ++s) {
-                    const Exact<T> kj = exact_row(k_row, 32 * s + 8 * quad, K);
-                    mma(qk, exact_row(q_mine, 32 * s + 8 * quad, K), kj);
-                    mma(kk, exact_row(k_mine, 32 * s + 8 * quad, K), kj);
-                }
-            }
+            for (int s = 0; s < KP / 32; ++s) mma(pass[jt], exact_row(mine, 32 * s + 8 * quad, K), exact_row(k_row, 32 * s + 8 * quad, K));
             const double far_j = gates.far[j];
             const float unit_j = gates.k_unit[j];
             const int ep_j = gates.episode[j];
+            double far_s[4];
+            int ep_s[4];
+            __builtin_memcpy(far_s, gates.far + 16 * jt + 4 * quad, 32); __builtin_memcpy(ep_s, gates.episode + 16 * jt + 4 * quad, 16);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = row + r;
-                const bool sees = j <= i && ep_j == ep_i[r];
-                const float ratio = sees ? exp2_wide(far_i[r] - far_j) : 0.0f;
-                const float p = sees ? par[jt][r] * ratio : 0.0f, x = sees && j < i ? -(cro[jt][r] * ratio) : 0.0f;
-                parallel[i * L::LINE + j] = p;
-                cross[i * L::LINE + j] = x;
-                passing[i * L::LINE + j] = sees && j < i ? unit_j * (p * (q_unit[r] * d.scale * qk[r]) + x * (k_unit[r] * kk[r])) : 0.0f;
+                const int i = row + r, js = 16 * jt + 4 * quad + r;
+                const bool sees = (by_values ? j < i : j <= i) && ep_j == ep_i[r], seen = (by_values ? js < i_seen : js <= i_seen) && ep_s[r] == ep_seen;
+                const float x = sees ? by_step[jt][r] * exp2_wide(far_i[r] - far_j) : 0.0f, w = seen ? by_seen[jt][r] * exp2_wide(far_seen - far_s[r]) : 0.0f;
+                by_step[jt][r] = by_values ? -sign * x : sign * x;
+                by_seen[jt][r] = by_values ? -sign * w : sign * w;
+                pass[jt][r] = sees && j < i ? by_step[jt][r] * (unit_j * unit_i[r] * (by_values ? 1.0f : d.scale) * pass[jt][r]) : 0.0f;
             }
         }
-        float from_late[4] = {}, from_state[4] = {};
+    }
+    const uint64_t bad_q = gates.bad_q, bad_k = gates.bad_k;
+    const auto product = [&](f32x4 (&out)[IT], const Exact<T> (&f)[2]) {
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+        for (int t = 0; t < IT; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) mma(out[t], get_wide<T>(matrix + tile_row(first_tile + t, col) * L::MATRIX_PITCH + (4 * s + quad) * N_::WIDE, 16), f[s]);
+    };
+    const auto put_matrix = [&](int r, int at, const float (&x)[4]) { put_wide4<T>(matrix + r * L::MATRIX_PITCH + (at >> 3) * N_::WIDE, 16, (at >> 2) & 1, x); };
+    __syncthreads();
+    // dQ: rows are the steps that look back
+    if (!by_values) {
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            float unit_j[4], x[4];
+            __builtin_memcpy(unit_j, gates.k_unit + 16 * jt + 4 * quad, 16);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = jt <= ti ? by_seen[jt][r] * unit_j[r] : 0.0f;
+            put_matrix(i_seen, 16 * jt + 4 * quad, x);
+        }
+    } else {
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) passing[(row + r) * L::LINE + 16 * jt + col] = jt <= ti ? pass[jt][r] : 0.0f;
+    }
+    __syncthreads();
+    product(q_state, kf);
+    __syncthreads();
+    // dK by the queries: rows are the steps that are looked at
+    if (!by_values) {
+        float unit_i[4];
+        __builtin_memcpy(unit_i, gates.q_unit + row, 16);
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            float x[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float kv = key_at(a.in.k, r, 16 * kt + col) * k_unit[r], qv = key_at(a.in.q, r, 16 * kt + col) * (q_unit[r] * d.scale);
-                if (keep[r] >= 0.0f) {
-                    q_state[kt][r] *= keep[r];
-                    const float x = keep[r] * k_state[kt][r];
-                    from_state[r] = __builtin_fmaf(qv, q_state[kt][r], __builtin_fmaf(-kv, x, from_state[r]));
-                    k_state[kt][r] = x;
-                } else q_state[kt][r] = k_state[kt][r] = 0.0f;
-                k_late[kt][r] = left[r] >= 0.0f ? left[r] * k_late[kt][r] : 0.0f;
-                if (left[r] >= 0.0f) from_late[r] = __builtin_fmaf(kv, k_late[kt][r], from_late[r]);
-                k_late[kt][r] -= k_state[kt][r];
+                x[r] = jt <= ti && !(bad_q >> (row + r) & 1) ? by_step[jt][r] * (unit_i[r] * d.scale) : 0.0f;
+                if (jt <= ti) passing[(row + r) * L::LINE + 16 * jt + col] += pass[jt][r];
             }
+            put_matrix(16 * jt + col, row, x);
+        }
+    }
+    __syncthreads();
+    product(k_late, qf);
+    __syncthreads();
+    // dK by the keys, on both sides: X + X^T
+    if (by_values) {
+        float unit_i[4];
+        __builtin_memcpy(unit_i, gates.k_unit + row, 16);
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            if (jt > ti) continue;
+            float unit_j[4], x[4];
+            __builtin_memcpy(unit_j, gates.k_unit + 16 * jt + 4 * quad, 16);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = (jt == ti && 4 * quad + r > col ? by_step[jt][r] : by_seen[jt][r]) * unit_j[r];
+            put_matrix(i_seen, 16 * jt + 4 * quad, x);
+            if (jt < ti) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = by_step[jt][r] * unit_i[r];
+                put_matrix(16 * jt + col, row, x);
+            }
+        }
+    } else {
+        // what passes, along each row up to a column: 16 columns a thread, and those of the threads before it
+        const int r = tid >> 2, p = tid & 3;
+        float *line = passing + r * L::LINE + 16 * p, x = 0.0f, below[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) { below[j] = x; x += line[j]; }
+        float before = 0.0f;
+#pragma unroll
+        for (int o = 0; o < 3; ++o) {
+            const float other = __shfl(x, (lane & ~3) + o, 64);
+            if (o < p) before += other;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) line[j] = before + below[j];
+    }
+    __syncthreads();
+    product(k_late, kf);
+    if (wave < 4) {
+        // ... and down a column from its row on
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = 16 * wave + i;
+            if (at >= lane) x += passing[at * L::LINE + lane];
+        }
+        sums[(1 + wave) * CHUNK + lane] = x;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        // the gates
+        const int t = t0 + lane;
+        const bool live = t < len;
+        float after = 0.0f, earlier = 0.0f;                  // of the state before the chunk: this step's and later ones; at its end: earlier ones
+#pragma unroll
+        for (int k = 0; k < KT; ++k) { after += rows[k * CHUNK + lane]; earlier += rows[(KT + k) * CHUNK + lane]; }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const float x = __shfl_down(after, o, 64), w = __shfl_up(earlier, o, 64);
+            if (lane + o < 64) after += x;
+            if (lane >= o) earlier += w;
+        }
+        earlier = __shfl_up(earlier, 1, 64);
+        float grad = after + (lane > 0 ? earlier : 0.0f) + ((sums[CHUNK + lane] + sums[2 * CHUNK + lane]) + (sums[3 * CHUNK + lane] + sums[4 * CHUNK + lane]));
+        const float all = gates.keep[CHUNK - 1];
+        if (all >= 0.0f) {
+            float held = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) held += sums[5 * CHUNK + w];
+            grad += all * held;
+        }
+        float da = 0.0f, dA = 0.0f;
+        if (live) {
+            const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
+            if (!(gates.resets >> lane & 1)) { da = grad * a.in.A[h] * dc.slope; dA = grad * dc.delta; }
+            if (bad_k >> lane & 1) da = dA = __builtin_nanf("");
+            step_of<T>(a.g.da, t, n)[h] = from_f32<T>(da);
+            step_of<T>(a.g.db, t, n)[h] = from_f32<T>((1.0f - gates.strength[lane]) * sums[lane]);
+        } else if (t < d.T) step_of<T>(a.g.da, t, n)[h] = step_of<T>(a.g.db, t, n)[h] = from_f32<T>(0.0f);
+        dA = wave_add(dA); da = wave_add(da);
+        if (lane == 0) { part[h] = dA; part[d.H + h] = da; }
+    }
+    __syncthreads();                                         // (the sums have been read, and the matrix)
+    if constexpr (SHARED) {
+#pragma unroll
+        for (int t = 0; t < IT; ++t) {
+            const int step = tile_row(first_tile + t, 4 * quad), k = 16 * kt + col;
+            if (k < K)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    a.heads[((2 * unit + 0) * CHUNK + step + r) * K + k] = q_state[t][r];
+                    a.heads[((2 * unit + 1) * CHUNK + step + r) * K + k] = k_late[t][r];
+                }
+        }
+        return;
+    }
+    // back through the lengths, and out
+    if (d.normalize) {
+#pragma unroll
+        for (int t = 0; t < IT; ++t) {
+            const int tt = first_tile + t, step = tile_row(tt, 4 * quad);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float q_dq = add16(entry(qf, tt, r) * q_state[t][r]);
+                const float k_dk = add16(entry(kf, tt, r) * k_late[t][r]);
+                if (col == 0) { rows[kt * CHUNK + step + r] = q_dq; rows[(KT + kt) * CHUNK + step + r] = k_dk; }
+            }
+        }
+        __syncthreads();
+    }
+    char *out_q = lds, *out_k = lds + CHUNK * L::OUT_PITCH;
+#pragma unroll
+    for (int t = 0; t < IT; ++t) {
+        const int tt = first_tile + t, step = tile_row(tt, 4 * quad);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+            float x = d.scale * q_state[t][r], w = k_late[t][r];
+            if (d.normalize) {
+                const float q_unit = gates.q_unit[step + r], k_unit = gates.k_unit[step + r];
+                float q_dq = 0.0f, k_dk = 0.0f;
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) { from_state[r] += __shfl_xor(from_state[r], o, 64); from_late[r] += __shfl_xor(from_late[r], o, 64); }
-            if (col == 0) { sums[row + r] = from_state[r]; sums[CHUNK + row + r] = from_late[r]; }
-        }
-#pragma unroll
-        for (int o = 1; o < 4; o <<= 1) z_dv += __shfl_xor(z_dv, o, 64);
-        if (my_part == 0) sums[2 * CHUNK + my_row] = z_dv;
-        end = wave_add(end);
-        if (lane == 0) sums[8 * CHUNK + wave] = end;
-        __syncthreads();
-        {
-            // C's sums along each row up to a column: 16 columns a thread, and those of the threads before it
-            float *line = passing + my_row * L::LINE + 16 * my_part, x = 0.0f;
-            float below[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) { below[j] = x; x += line[j]; }
-            float before_mine = 0.0f;
-#pragma unroll
-            for (int o = 1; o < 4; ++o) {
-                const float other = __shfl(x, (lane & ~3) + o - 1, 64);
-                if (o <= my_part) before_mine += other;
+                for (int k = 0; k < KT; ++k) { q_dq += rows[k * CHUNK + step + r]; k_dk += rows[(KT + k) * CHUNK + step + r]; }
+                const float qv = entry(qf, tt, r), kv = entry(kf, tt, r);
+                x = q_unit * (x - q_unit * qv * (q_unit * d.scale * q_dq));
+                w = k_unit * (w - k_unit * kv * (k_unit * k_dk));
+                if (bad_k >> (step + r) & 1) w = __builtin_nanf("");
             }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) line[j] = before_mine + below[j];
+            *(T *)(out_q + (step + r) * L::OUT_PITCH + (16 * kt + col) * sizeof(T)) = from_f32<T>(x);
+            *(T *)(out_k + (step + r) * L::OUT_PITCH + (16 * kt + col) * sizeof(T)) = from_f32<T>(w);
         }
+    }
+    __syncthreads();
+    constexpr int PIECE = 16 / (int)sizeof(T), PIECES = KP / PIECE;
+    for (int p = tid; p < 2 * CHUNK * PIECES; p += 512) {
+        const int which = p / (CHUNK * PIECES), i = p / PIECES % CHUNK, at = p % PIECES * PIECE, count = K - at;
+        if (i >= steps || count <= 0) continue;
+        T *to = step_of<T>(which ? a.g.dk : a.g.dq, t0 + i, n) + (int64_t)group * K + at, x[PIECE];
+        __builtin_memcpy(x, __builtin_assume_aligned((which ? out_k : out_q) + i * L::OUT_PITCH + at * sizeof(T), 16), 16);
+        if (t0 + i >= len)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            // rows 16 w + col: of dQ, of dK by the queries that look at them, of dK by the keys on both sides
-            const int i = 16 * wave + col, at = 32 * s + 8 * quad;
-            float m1[8], m2[8], m3[8];
+            for (int e = 0; e < PIECE; ++e) x[e] = from_f32<T>(0.0f);
+        if (count >= PIECE) __builtin_memcpy(to, x, 16);
+        else
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const float unit_j = gates.k_unit[at + x];
-                m1[x] = parallel[i * L::LINE + at + x] * unit_j;
-                const bool ok = !(bad_q >> (at + x) & 1);
-                m2[x] = ok ? parallel[(at + x) * L::LINE + i] * gates.q_unit[at + x] * d.scale : 0.0f;
-                m3[x] = (cross[i * L::LINE + at + x] + cross[(at + x) * L::LINE + i]) * unit_j;
+            for (int e = 0; e < PIECE; ++e) if (e < count) to[e] = x[e];
+    }
+}
+
+// Queries and keys of several heads: their gradients added up, back through the lengths, and out.  A wavefront for a step of a group.
+template <typename T> __global__ __launch_bounds__(256) void join_kernel(const DeltaArgs a)
+{
+    const hts_delta_rule_desc &d = a.d;
+    const int lane = threadIdx.x & 63, i = (int)(blockIdx.x % (CHUNK / 4)) * 4 + (threadIdx.x >> 6), per = d.H / d.G, K = d.K;
+    const int64_t of = blockIdx.x / (CHUNK / 4);
+    const int group = (int)(of % d.G), n = (int)(of / d.G % d.N), c = (int)(of / d.G / d.N), t = c * CHUNK + i;
+    if (t >= d.T) return;
+    const bool live = t < length_of(a, n);
+    const int64_t unit = ((int64_t)c * d.N + n) * d.H + group * per;
+    float q[2] = {}, k[2] = {}, dq[2] = {}, dk[2] = {}, q_dq = 0.0f, k_dk = 0.0f;
+    if (live) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int at = lane + 64 * e;
+            if (at >= K) continue;
+            q[e] = to_f32(step_of<T>(a.in.q, t, n)[(int64_t)group * K + at]);
+            k[e] = to_f32(step_of<T>(a.in.k, t, n)[(int64_t)group * K + at]);
+            for (int h = 0; h < per; ++h) {
+                dq[e] += a.heads[((2 * (unit + h) + 0) * CHUNK + i) * K + at];
+                dk[e] += a.heads[((2 * (unit + h) + 1) * CHUNK + i) * K + at];
             }
-            const Wide<T> w1 = make_wide<T>(m1), w2 = make_wide<T>(m2), w3 = make_wide<T>(m3);
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const int64_t f = (unit * (KP / 8) + kt * 2 + s) * N_::EXACT_FRAGMENT + lane * 16;
-                const Exact<T> kf = get_exact<T>(a.keys + f, 1024), qf = get_exact<T>(a.queries + f, 1024);
-                mma(q_state[kt], w1, kf);
-                mma(k_late[kt], w2, qf);
-                mma(k_late[kt], w3, kf);
-            }
+            q_dq = __builtin_fmaf(q[e], dq[e], q_dq);
+            k_dk = __builtin_fmaf(k[e], dk[e], k_dk);
         }
-        if constexpr (SHARED)
+        if (d.normalize) {
+            const float q_unit = a.gates[unit].q_unit[i], k_unit = a.gates[unit].k_unit[i];
+            q_dq = wave_add(q_dq); k_dk = wave_add(k_dk);
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) { dq[kt] += q_state[kt]; dk[kt] += k_late[kt]; }
-        else finish(q_state, k_late, gates);
-        __syncthreads();
-        {
-            // ... and down a column from its row on
-            float x = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int at = 16 * wave + i;
-                if (at >= lane) x += passing[at * L::LINE + lane];
+            for (int e = 0; e < 2; ++e) {
+                dq[e] = q_unit * (d.scale * dq[e] - q_unit * q[e] * (q_unit * d.scale * q_dq));
+                dk[e] = k_unit * (dk[e] - k_unit * k[e] * (k_unit * k_dk));
             }
-            sums[(3 + wave) * CHUNK + lane] = x;
-        }
-        __syncthreads();
-        if (wave == 0) {
-            // the gates
-            const int t = t0 + lane;
-            const bool live = t < len;
-            float after = sums[lane], earlier = sums[CHUNK + lane];         // of the state before the chunk: this step and later ones'; at its end: earlier ones'
+        } else { dq[0] *= d.scale; dq[1] *= d.scale; }
+    }
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const float x = __shfl_down(after, o, 64), y = __shfl_up(earlier, o, 64);
-                if (lane + o < 64) after += x;
-                if (lane >= o) earlier += y;
-            }
-            earlier = __shfl_up(earlier, 1, 64);
-            float g = after + (lane > 0 ? earlier : 0.0f) + ((sums[3 * CHUNK + lane] + sums[4 * CHUNK + lane]) + (sums[5 * CHUNK + lane] + sums[6 * CHUNK + lane]));
-            if (all >= 0.0f) g += all * ((sums[8 * CHUNK] + sums[8 * CHUNK + 1]) + (sums[8 * CHUNK + 2] + sums[8 * CHUNK + 3]));
-            float da = 0.0f, dA = 0.0f;
-            if (live) {
-                const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
-                if (!(gates.resets >> lane & 1)) { da = g * a.in.A[h] * dc.slope; dA = g * dc.delta; }
-                if (bad_k >> lane & 1) da = dA = __builtin_nanf("");
-                step_of<T>(a.g.da, t, n)[h] = from_f32<T>(da);
-                step_of<T>(a.g.db, t, n)[h] = from_f32<T>((1.0f - gates.strength[lane]) * sums[2 * CHUNK + lane]);
-            } else if (t < d.T) step_of<T>(a.g.da, t, n)[h] = step_of<T>(a.g.db, t, n)[h] = from_f32<T>(0.0f);
-            dA = wave_add(dA); da = wave_add(da);
-            if (lane == 0) { part[h] = dA; part[d.H + h] = da; }
-        }
-        if constexpr (SHARED) if (hh == per - 1) finish(dq, dk, gates);
+    for (int e = 0; e < 2; ++e) {
+        const int at = lane + 64 * e;
+        if (at >= K) continue;
+        step_of<T>(a.g.dq, t, n)[(int64_t)group * K + at] = from_f32<T>(dq[e]);
+        step_of<T>(a.g.dk, t, n)[(int64_t)group * K + at] = from_f32<T>(dk[e]);
     }
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
 // (more LDS than 64 KB has to be asked for)
-template <class F> hipError_t launch(F kernel, int64_t groups, int lds, hipStream_t stream, const DeltaArgs &a)
+template <class F> hipError_t launch(F kernel, int64_t groups, int lds, hipStream_t stream, const DeltaArgs &a, int threads = 256)
 {
-    if (groups == 0) return hipSuccess;
-    if (!launchable(groups, 256) || groups > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (!launchable(groups, threads) || groups > 0x7fffffff) return hipErrorInvalidConfiguration;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(256), (uint32_t)lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(threads), (uint32_t)lds, stream, a);
     return hipGetLastError();
 }
 template <typename F> hipError_t by_keys(int K, F f)
@@ -1090,7 +1230,7 @@ int keys_padded(int K) { return K <= 32 ? 32 : K <= 64 ? 64 : 128; }
 
 constexpr int MOST_STEPS = 16;            // calls of so many steps or fewer go step by step
 
-struct Layout { int64_t inverse, read, keys, queries, gates, late, write, part, total; };
+struct Layout { int64_t inverse, read, keys, queries, gates, late, write, part, heads, total; };
 Layout layout(const hts_delta_rule_desc &d, bool back)
 {
     const int64_t units = ceil_div(d.T, CHUNK) * d.N * d.H, wide = d.precision == HTS_PRECISION_BF16 ? 3072 : 2048, exact = d.precision == HTS_PRECISION_BF16 ? 1024 : 2048;
@@ -1103,7 +1243,8 @@ Layout layout(const hts_delta_rule_desc &d, bool back)
     l.late = l.gates + round_up(units * (int64_t)sizeof(Gates), 256);
     l.write = l.late + (back ? round_up(units * d.K * d.V * 4, 256) : 0);
     l.part = l.write + (back ? round_up(units * CHUNK * d.V * 4, 256) : 0);
-    l.total = l.part + (back ? round_up(ceil_div(d.T, CHUNK) * d.N * 2 * d.H * 4, 256) : 0);
+    l.heads = l.part + (back ? round_up(ceil_div(d.T, CHUNK) * d.N * 2 * d.H * 4, 256) : 0);
+    l.total = l.heads + (back && d.H > d.G ? units * 2 * CHUNK * d.K * 4 : 0);
     return l;
 }
 DeltaArgs arguments(hts_seq_ctx &c, const DeltaOp &op, bool back)
@@ -1115,7 +1256,7 @@ DeltaArgs arguments(hts_seq_ctx &c, const DeltaOp &op, bool back)
     a.tiles = (int)ceil_div(op.d.V, TILE);
     if (op.states) a.z = op.states + delta_state_floats(op.d);
     a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates);
-    a.late = (float *)(c.ws + l.late); a.write = (float *)(c.ws + l.write); a.part = (float *)(c.ws + l.part);
+    a.late = (float *)(c.ws + l.late); a.write = (float *)(c.ws + l.write); a.part = (float *)(c.ws + l.part); a.heads = (float *)(c.ws + l.heads);
     return a;
 }
 template <typename T> hipError_t forward(hts_seq_ctx &c, const DeltaOp &op)
@@ -1140,7 +1281,8 @@ template <typename T> hipError_t backward(hts_seq_ctx &c, const DeltaOp &op)
         constexpr int KP = decltype(kp)::value;
         hipError_t e = launch(prep_kernel<T, KP, true>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
         if (e == hipSuccess) e = launch(reverse_kernel<T, KP>, (int64_t)d.N * d.H * a.tiles, RunLds<T, KP>::BYTES, c.stream, a);
-        if (e == hipSuccess) e = launch(d.H > d.G ? grads_kernel<T, KP, true> : grads_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.G, GradLds<T, KP>::BYTES, c.stream, a);
+        if (e == hipSuccess) e = launch(d.H > d.G ? grads_kernel<T, KP, true> : grads_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, GradLds<T, KP>::BYTES, c.stream, a, 512);
+        if (e == hipSuccess && d.H > d.G) e = launch(join_kernel<T>, (int64_t)a.chunks * d.N * d.G * (CHUNK / 4), 0, c.stream, a);
         return e;
     });
     if (e != hipSuccess) return e;

@@ -45,23 +45,17 @@ __device__ __forceinline__ void mma(f32x4 &c, const Exact<bf16_t> &a, const Exac
 // a last digit on average where products are 2^-15 of C, measured), which a sum over thousands of steps adds up: dA 2.3e-6 of its values off, now 4e-7.
 __device__ __forceinline__ void mma(f32x4 &c, const Exact<bf16_t> &a, const Wide<bf16_t> &b)
 {
-    f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
-    mma1(t, a.v, b.p[2]); mma1(t, a.v, b.p[1]); mma1(t, a.v, b.p[0]);
-    c += t;
+    mma1(c, a.v, b.p[2]); mma1(c, a.v, b.p[1]); mma1(c, a.v, b.p[0]);
 }
 __device__ __forceinline__ void mma(f32x4 &c, const Wide<bf16_t> &a, const Exact<bf16_t> &b)
 {
-    f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
-    mma1(t, a.p[2], b.v); mma1(t, a.p[1], b.v); mma1(t, a.p[0], b.v);
-    c += t;
+    mma1(c, a.p[2], b.v); mma1(c, a.p[1], b.v); mma1(c, a.p[0], b.v);
 }
 __device__ __forceinline__ void mma(f32x4 &c, const Wide<bf16_t> &a, const Wide<bf16_t> &b)
 {
-    f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
-    mma1(t, a.p[2], b.p[0]); mma1(t, a.p[1], b.p[1]); mma1(t, a.p[0], b.p[2]);
-    mma1(t, a.p[1], b.p[0]); mma1(t, a.p[0], b.p[1]);
-    mma1(t, a.p[0], b.p[0]);
-    c += t;
+    mma1(c, a.p[2], b.p[0]); mma1(c, a.p[1], b.p[1]); mma1(c, a.p[0], b.p[2]);
+    mma1(c, a.p[1], b.p[0]); mma1(c, a.p[0], b.p[1]);
+    mma1(c, a.p[0], b.p[0]);
 }
 
 template <typename T> __device__ __forceinline__ Exact<T> get_exact(const char *p, int plane)
@@ -176,7 +170,7 @@ struct DeltaArgs {
     int chunks, tiles;                            // tiles of the values
     char *inverse, *inverse_t, *read, *keys, *queries;     // fragments of each chunk, sequence and head
     Gates *gates;
-    float *late, *write, *part;                   // gradients of the states at the chunks' ends; of the values; sums of the decays' parameters
+    float *late, *write, *part, *heads;           // gradients of the states at the chunks' ends; of the values; sums of the decays' parameters; of shared queries and keys
 };
 __device__ __forceinline__ int length_of(const DeltaArgs &a, int n)
 {
