@@ -18,6 +18,7 @@ namespace hts {
 namespace {
 
 constexpr int TILE = 32;                  // the values' entries of a workgroup
+__host__ __device__ __forceinline__ int keys_padded(int K) { return K <= 32 ? 32 : K <= 64 ? 64 : 128; }
 
 __device__ __forceinline__ float wave_add(float x)
 {
@@ -187,6 +188,14 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
             put_wide4<T>(f, 1024, (at >> 2) & 1, p);
         }
     }
+    if (a.rows)
+        for (int p = tid; p < CHUNK * KP / 8; p += 256) {
+            const int row = p / (KP / 8), at = p % (KP / 8);
+            T *to = (T *)a.rows + unit * 2 * CHUNK * KP + row * KP + 8 * at;
+            const Exact<T> kx = get_exact<T>(keys + row * L::PITCH + at * N_::EXACT, 16), qx = get_exact<T>(queries + row * L::PITCH + at * N_::EXACT, 16);
+            __builtin_memcpy(to, &kx, sizeof kx);
+            __builtin_memcpy(to + CHUNK * KP, &qx, sizeof qx);
+        }
     // keys (and queries) with the steps along a row
     for (int f = wave; f < KP / 16 * 2; f += 4) {
         const int row = 16 * (f >> 1) + col, at = 32 * (f & 1) + 8 * quad;
@@ -285,23 +294,35 @@ template <typename T> __device__ __forceinline__ void store4(T *p, const float (
         for (int r = 0; r < 4; ++r) if (r < count) p[r] = x[r];
 }
 
+// A head's tiles on one die (workgroups go to the dies in turn), whose L2 then has the chunks' fragments for all of them
+constexpr int DIES = 8;
+struct Part { int tile, h, n; };
+__device__ __forceinline__ Part part_of(const DeltaArgs &a)
+{
+    const uint32_t die = blockIdx.x % DIES, i = blockIdx.x / DIES, head = i / a.tiles * DIES + die;
+    return Part{(int)(i % a.tiles), (int)(head % a.d.H), (int)(head / a.d.H)};
+}
+inline int64_t parts(const DeltaArgs &a) { return round_up((int64_t)a.d.N * a.d.H, DIES) * a.tiles; }
+
 template <typename T, int KP> struct RunLds {
     typedef Num<T> N_;
     static constexpr int STATE_PITCH = N_::pitch(KP), ROW_PITCH = N_::pitch(CHUNK), EXACT_PITCH = N_::exact_pitch(CHUNK);
     static constexpr int STATE = 0, ONE = STATE + TILE * STATE_PITCH, TWO = ONE + TILE * ROW_PITCH, THREE = TWO + TILE * ROW_PITCH, MARKS = THREE + TILE * ROW_PITCH;
-    static constexpr int BYTES = MARKS + (int)sizeof(Marks);
+    static constexpr int FOUR = MARKS + (int)sizeof(Marks), BYTES = FOUR, BACK_BYTES = FOUR + TILE * EXACT_PITCH;
 };
 // tiles of 16 keys' entries of a wavefront
 template <int KP> constexpr int key_tiles() { return KP / 64 > 0 ? KP / 64 : 1; }
 
-template <typename T, int KP> __global__ __launch_bounds__(256) void forward_kernel(const DeltaArgs a)
+template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_kernel(const DeltaArgs a)
 {
     typedef RunLds<T, KP> L;
     typedef Num<T> N_;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const hts_delta_rule_desc &d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
-    const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % d.H, n = blockIdx.x / a.tiles / d.H;
+    const Part at = part_of(a);
+    if (at.n >= d.N) return;
+    const int tile = at.tile, h = at.h, n = at.n;
     const int K = d.K, V = d.V, v0 = tile * TILE, group = h / (d.H / d.G), len = length_of(a, n);
     constexpr int MT = key_tiles<KP>();
     const bool has_keys = wave * MT * 16 < KP;
@@ -314,13 +335,14 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void forward_ker
     const int64_t held = ((int64_t)n * d.H + h) * K * V;
     const auto each_state = [&](auto f) {
         if (!has_keys) return;
+        const int row4 = again(4 * quad), column = again(col);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int k = 16 * (wave * MT + m) + 4 * quad + r, v = v0 + 16 * nt + col;
+                    const int k = 16 * (wave * MT + m) + row4 + r, v = v0 + 16 * nt + column;
                     S[m][nt][r] = f(S[m][nt][r], k < K && v < V, (int64_t)k * V + v);
                 }
     };
@@ -336,60 +358,115 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void forward_ker
     };
     each_state([&](float, bool there, int64_t at) { return there && a.in.h_in ? a.in.h_in[held + at] : 0.0f; });
     share_state();
-    __syncthreads();
+    const int VP = a.VP;
+    const uint32_t state_at = row_at<float>(16 * wave * MT + 4 * quad, VP, col), z_at = row_at<float>(16 * wave + 4 * quad, VP, col);
 
-    const int used = (len + CHUNK - 1) / CHUNK;
-    for (int c = 0; c < used; ++c) {
-        const int64_t unit = ((int64_t)c * d.N + n) * d.H + h;
-        const Gates &gates = a.gates[unit];
-        const int t0 = c * CHUNK;
-        if (a.states) each_state([&](float s, bool there, int64_t at) { if (there) a.states[unit * K * V + at] = s; return s; });
-        // what the state has for the keys, and for the queries
-        f32x4 ks[2] = {}, qs[2] = {};
-        const int mine = t0 + 16 * wave + col;
-        const T *k_row = mine < len ? step_of<T>(a.in.k, mine, n) + (int64_t)group * K : nullptr, *q_row = mine < len ? step_of<T>(a.in.q, mine, n) + (int64_t)group * K : nullptr;
+    // A chunk's operands are requested when the chunk's before it have been used, and arrive while it is worked on (the barriers wait for LDS only)
+    const int used = (len + CHUNK - 1) / CHUNK, row = 16 * wave + 4 * quad, i = 16 * wave + col;     // of 4 steps, one after the other; of a step
+    Exact<T> kf[KP / 32], qf[KP / 32], tf[MT][2];
+    Wide<T> wf[2], pf[2];
+    T val[2][4];
+    float keep[4], k_unit[4], strength[4], left[4], keep_i = 0.0f, q_unit_i = 0.0f, all = 0.0f;
+    uint64_t bad_k = 0;
+    const auto unit_of = [&](int c) { return ((int64_t)c * d.N + n) * d.H + h; };
+    // rows behind the end: the last one again, whose products go nowhere; keys' entries behind K, where the state has zeros: the first ones
+    const auto load_rows = [&](int c) {
+        const int t = c * CHUNK + i < len ? i : len - 1 - c * CHUNK;
+        const T *k = a.rows ? (const T *)a.rows + unit_of(c) * 2 * CHUNK * KP : step_of<T>(a.in.k, c * CHUNK, n) + (int64_t)group * K;
+        const T *q = a.rows ? k + CHUNK * KP : step_of<T>(a.in.q, c * CHUNK, n) + (int64_t)group * K;
+        const uint32_t k_at = row_at<T>(t, a.rows ? KP : a.in.k.st, 0), q_at = row_at<T>(t, a.rows ? KP : a.in.q.st, 0);
 #pragma unroll
         for (int s = 0; s < KP / 32; ++s) {
-            const Exact<T> kf = exact_row(k_row, 32 * s + 8 * quad, K), qf = exact_row(q_row, 32 * s + 8 * quad, K);
+            const uint32_t at = (K < KP && 32 * s + 8 * quad >= K ? 0 : 32 * s + 8 * quad) * (uint32_t)sizeof(T);
+            kf[s] = load_at<Exact<T>>(k, k_at + at); qf[s] = load_at<Exact<T>>(q, q_at + at);
+        }
+    };
+    const auto load_values = [&](int c) {
+        const T *v = step_of<T>(a.in.v, c * CHUNK, n) + (int64_t)h * V;
+        const int last = len - 1 - c * CHUNK;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t at = row_at<T>(row + r < last ? row + r : last, a.in.v.st, 0);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                const int column = v0 + 16 * nt + col;
+                val[nt][r] = load_at<T>(v, at + (column < V ? column : V - 1) * (uint32_t)sizeof(T));
+            }
+        }
+    };
+    const auto load_gates = [&](int c) {
+        const Gates &g = a.gates[unit_of(c)];
+        __builtin_memcpy(keep, g.keep + row, 16); __builtin_memcpy(k_unit, g.k_unit + row, 16);
+        __builtin_memcpy(strength, g.strength + row, 16); __builtin_memcpy(left, g.left + row, 16);
+        keep_i = g.keep[i]; q_unit_i = g.q_unit[i]; all = g.keep[CHUNK - 1]; bad_k = g.bad_k;
+    };
+    const auto load_pair = [&](Wide<T> (&f)[2], const char *base, int c) {      // (the second one of rows 0 .. 31 is zeros)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s == 0 || wave >= 2) f[s] = get_wide<T>(base + (unit_of(c) * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+    };
+    const auto load_keys = [&](int c) {
+        if (!has_keys) return;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) tf[m][s] = get_exact<T>(a.keys + (unit_of(c) * (KP / 8) + (wave * MT + m) * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024);
+    };
+    if (used > 0) { load_rows(0); load_gates(0); load_values(0); }
+    lds_barrier();
+    for (int c = 0; c < used; ++c) {
+        const int64_t unit = unit_of(c);
+        const int t0 = c * CHUNK;
+        const bool more = c + 1 < used;
+        load_pair(wf, a.inverse, c);
+        if (a.states && has_keys) {
+            float *to = a.states + unit * KP * VP + v0;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) store_at(to + (16 * m + r) * (int64_t)VP + 16 * nt, state_at, S[m][nt][r]);
+        }
+        // what the state has for the keys, and for the queries
+        f32x4 ks[2] = {}, qs[2] = {};
+#pragma unroll
+        for (int s = 0; s < KP / 32; ++s) {
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) {
                 const Wide<T> sf = get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * s + quad) * N_::WIDE, 16);
-                mma(ks[nt], kf, sf);
-                mma(qs[nt], sf, qf);
+                mma(ks[nt], kf[s], sf);
+                mma(qs[nt], sf, qf[s]);
             }
+            __builtin_amdgcn_sched_barrier(0);                 // (operands of every s at once are more than there are registers)
         }
-        const int row = 16 * wave + 4 * quad;             // of 4 steps, one after the other
-        float keep[4], k_unit[4], strength[4], left[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { keep[r] = gates.keep[row + r]; k_unit[r] = gates.k_unit[row + r]; strength[r] = gates.strength[row + r]; left[r] = gates.left[row + r]; }
-        const uint64_t bad_k = gates.bad_k;
+        load_pair(pf, a.read, c);
+        if (more) load_rows(c + 1);
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-            const int v = v0 + 16 * nt + col;
             float e[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bool live = t0 + row + r < len && v < V;
-                e[r] = 0.0f;
-                if (live) {
-                    e[r] = to_f32(step_of<T>(a.in.v, t0 + row + r, n)[(int64_t)h * V + v]);
-                    if (keep[r] >= 0.0f) e[r] -= keep[r] * k_unit[r] * ks[nt][r];
-                    if (!finite(e[r]) || (bad_k >> (row + r) & 1)) { e[r] = 0.0f; mark(marks, 16 * nt + col, row + r, c); }
-                }
+                const bool live = t0 + row + r < len && v0 + 16 * nt + col < V;
+                e[r] = to_f32(val[nt][r]);
+                if (keep[r] >= 0.0f) e[r] -= keep[r] * k_unit[r] * ks[nt][r];
+                if (!live) e[r] = 0.0f;
+                else if (!finite(e[r]) || (bad_k >> (row + r) & 1)) { e[r] = 0.0f; mark(marks, 16 * nt + col, row + r, c); }
             }
             put_wide4<T>(left_over + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, e);
         }
-        __syncthreads();
+        if (more) load_values(c + 1);
+        lds_barrier();
         const bool some = marks.any == (uint32_t)c + 1;
         // Z, and what it writes
         f32x4 z[2] = {};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            if (s == 1 && wave < 2) continue;              // zeros
-            const Wide<T> w = get_wide<T>(a.inverse + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+            if (s == 1 && wave < 2) continue;
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) mma(z[nt], w, get_wide<T>(left_over + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16));
+            for (int nt = 0; nt < 2; ++nt) mma(z[nt], wf[s], get_wide<T>(left_over + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16));
         }
+        load_keys(c);
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             float u[4], l[4];
@@ -401,44 +478,43 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void forward_ker
             put_wide4<T>(writes + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, u);
             put_wide4<T>(late + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, l);
             if (a.z) {
-                const int v = v0 + 16 * nt + col;
-                if (v < V)
+                float *to = a.z + unit * CHUNK * VP + v0 + 16 * nt;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const bool wrong = some && (marks.of(16 * nt + col) & steps_between(gates.first[row + r], row + r));
-                        if (t0 + row + r < len) a.z[unit * CHUNK * V + (int64_t)(row + r) * V + v] = wrong ? __builtin_nanf("") : z[nt][r];
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    const bool wrong = some && t0 + row + r < len && (marks.of(16 * nt + col) & steps_between(a.gates[unit].first[row + r], row + r));
+                    store_at(to + r * (int64_t)VP, z_at, wrong ? __builtin_nanf("") : z[nt][r]);
+                }
             }
         }
-        __syncthreads();
+        lds_barrier();
         // outputs, the values along a row
-        const int i = 16 * wave + col;
-        const float asked = gates.keep[i] >= 0.0f ? gates.keep[i] * gates.q_unit[i] * d.scale : -1.0f;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) qs[nt][r] = gates.keep[i] >= 0.0f ? asked * qs[nt][r] : 0.0f;
+            for (int r = 0; r < 4; ++r) qs[nt][r] = keep_i >= 0.0f ? keep_i * q_unit_i * d.scale * qs[nt][r] : 0.0f;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             if (s == 1 && wave < 2) continue;
-            const Wide<T> p = get_wide<T>(a.read + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) mma(qs[nt], get_wide<T>(writes + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16), p);
+            for (int nt = 0; nt < 2; ++nt) mma(qs[nt], get_wide<T>(writes + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16), pf[s]);
         }
         if (t0 + i < len) {
-            const uint64_t seen = steps_between(gates.first[i], i);
-            T *y = step_of<T>(a.y, t0 + i, n) + (int64_t)h * V;
+            const uint64_t seen = some ? steps_between(a.gates[unit].first[i], i) : 0;
+            T *y = step_of<T>(a.y, t0, n) + (int64_t)h * V + v0;
+            const uint32_t y_at = row_at<T>(i, a.y.st, 4 * quad);
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) {
-                const int v = v0 + 16 * nt + 4 * quad;
-                float o[4];
+                Four<T> o;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = some && (marks.of(16 * nt + 4 * quad + r) & seen) ? __builtin_nanf("") : qs[nt][r];
-                store4(y + v, o, V - v);
+                for (int r = 0; r < 4; ++r) o.e[r] = from_f32<T>(some && (marks.of(16 * nt + 4 * quad + r) & seen) ? __builtin_nanf("") : qs[nt][r]);
+                const int count = V - (v0 + 16 * nt + 4 * quad);
+                if (count >= 4) store_at(y + 16 * nt, y_at, o);
+                else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) if (r < count) store_at(y + 16 * nt + r, y_at, o.e[r]);
             }
         }
         // the state at the end
-        const float all = gates.keep[CHUNK - 1];
         if (has_keys) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -452,14 +528,13 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void forward_ker
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt) l[nt] = get_wide<T>(late + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const Exact<T> kf = get_exact<T>(a.keys + (unit * (KP / 8) + (wave * MT + m) * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024);
+                for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int nt = 0; nt < 2; ++nt) mma(S[m][nt], kf, l[nt]);
-                }
+                    for (int nt = 0; nt < 2; ++nt) mma(S[m][nt], tf[m][s], l[nt]);
+                __builtin_amdgcn_sched_barrier(0);
             }
             if (some) {
-                const uint64_t last = steps_between(gates.first[CHUNK - 1], CHUNK - 1);
+                const uint64_t last = steps_between(a.gates[unit].first[CHUNK - 1], CHUNK - 1);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -470,10 +545,11 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void forward_ker
             }
             share_state();
         }
-        __syncthreads();
+        if (more) load_gates(c + 1);
+        lds_barrier();
         if (some) {
             if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
-            __syncthreads();
+            lds_barrier();
         }
     }
     if (a.h_out) each_state([&](float s, bool there, int64_t at) { if (there) a.h_out[held + at] = s; return s; });
@@ -508,14 +584,19 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
                 for (int i = 0; i < 4; ++i) if (i < count) S[m][i] = p[i];
         }
     }
-    const auto put_state = [&](float *to) {
+    const auto put_state = [&](float *to, int keys, int values) {
 #pragma unroll
         for (int m = 0; m < STEP_ROWS; ++m) {
             const int k = rg + 16 * m;
-            if (k < K) store4(to + (int64_t)k * V + v0, S[m], count);
+            if (k < keys) store4(to + (int64_t)k * values + v0, S[m], values - v0);
         }
     };
-    if (a.states && len > 0) put_state(a.states + held);
+    const int64_t unit = (int64_t)n * d.H + h;
+    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (a.states && len > 0) {
+        put_state(a.states + unit * keys_padded(K) * a.VP, keys_padded(K), a.VP);
+        for (int t = len + rg; t < CHUNK; t += 16) store4(a.z + (unit * CHUNK + t) * a.VP + v0, none, a.VP - v0);
+    }
     for (int t = 0; t < len; ++t) {
         if (tid < 128) {
             const float kv = tid < K ? to_f32(step_of<T>(a.in.k, t, n)[(int64_t)group * K + tid]) : 0.0f, qv = tid < K ? to_f32(step_of<T>(a.in.q, t, n)[(int64_t)group * K + tid]) : 0.0f;
@@ -577,14 +658,13 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
 #pragma unroll
             for (int i = 0; i < 4; ++i) S[m][i] = reset ? kv * u[i] : __builtin_fmaf(decay, S[m][i], kv * u[i]);
         }
-        if (rg == 0 && count > 0) {
+        if (rg == 0) {
             store4(step_of<T>(a.y, t, n) + (int64_t)h * V + v0, y, count);
-            if (a.z) store4(a.z + ((int64_t)n * d.H + h) * CHUNK * V + (int64_t)t * V + v0, z, count);
+            if (a.z) store4(a.z + (unit * CHUNK + t) * a.VP + v0, z, a.VP - v0);
         }
         __syncthreads();
     }
-    if (a.h_out) put_state(a.h_out + held);
-    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (a.h_out) put_state(a.h_out + held, K, V);
     if (rg == 0)
         for (int t = len; t < d.T; ++t) store4(step_of<T>(a.y, t, n) + (int64_t)h * V + v0, none, count);
 }
@@ -596,19 +676,21 @@ __device__ __forceinline__ float sign_of(int chunk, int n) { return (chunk + n) 
 // What a matrix instruction drops of its products goes towards minus infinity.  Gradients have either sign, but keys, queries, values and states may be mostly positive, and then
 // the sums of the decays' gradients over thousands of steps add up what was dropped (da_bias 4.6e-6 of its values off, 512 x 16 steps).  So every second chunk has all gradients
 // with the other sign, here and in the sums after it.
-template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_kernel(const DeltaArgs a)
+template <typename T, int KP> __global__ __launch_bounds__(256, 2) void reverse_kernel(const DeltaArgs a)
 {
     typedef RunLds<T, KP> L;
     typedef Num<T> N_;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const hts_delta_rule_desc &d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
-    const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % d.H, n = blockIdx.x / a.tiles / d.H;
+    const Part at = part_of(a);
+    if (at.n >= d.N) return;
+    const int tile = at.tile, h = at.h, n = at.n;
     const int K = d.K, V = d.V, v0 = tile * TILE, group = h / (d.H / d.G), len = length_of(a, n);
     constexpr int MT = key_tiles<KP>();
     const bool has_keys = wave * MT * 16 < KP;
-    // ONE: the output's gradient (Exact), TWO: that of what is written, times its strength, then minus that of the values, kept; THREE: the output's, kept
-    char *state = lds + L::STATE, *given = lds + L::ONE, *sent = lds + L::TWO, *asked = lds + L::THREE;
+    // the output's gradient (Exact); that of what is written, times its strength; minus that of the values, kept; the output's, kept
+    char *state = lds + L::STATE, *given = lds + L::FOUR, *sent = lds + L::ONE, *kept = lds + L::TWO, *asked = lds + L::THREE;
     Marks &marks = *(Marks *)(lds + L::MARKS);
     if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
     if (tid == TILE) marks.any = 0;
@@ -617,23 +699,79 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
     const int64_t held = ((int64_t)n * d.H + h) * K * V;
     const auto each_state = [&](auto f) {
         if (!has_keys) return;
+        const int row4 = again(4 * quad), column = again(col);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int k = 16 * (wave * MT + m) + 4 * quad + r, v = v0 + 16 * nt + col;
+                    const int k = 16 * (wave * MT + m) + row4 + r, v = v0 + 16 * nt + column;
                     S[m][nt][r] = f(S[m][nt][r], k < K && v < V, (int64_t)k * V + v);
                 }
     };
     each_state([&](float, bool there, int64_t at) { return there && a.dh_out ? a.dh_out[held + at] : 0.0f; });
 
+    const int used = (len + CHUNK - 1) / CHUNK, row = 16 * wave + 4 * quad, i = 16 * wave + col;
+    const int VP = a.VP;
+    const uint32_t state_at = row_at<float>(16 * wave * MT + 4 * quad, VP, col), dv_at = row_at<float>(row, VP, col);
+    const int my_v = tid & 31, my_i = 8 * (tid >> 5);                  // 8 steps of one of the values' entries
+    Exact<T> kf[KP / 32], tf[MT][2], gf[MT][2];
+    Wide<T> wf[2], pf[2];
+    T given_y[8];
+    float asked_by[8], keep[4], k_unit[4], strength[4], left[4], all = 0.0f;
+    uint64_t bad_k = 0, bad_q = 0;
+    const auto unit_of = [&](int c) { return ((int64_t)c * d.N + n) * d.H + h; };
+    const auto load_outputs = [&](int c) {
+        const Gates &g = a.gates[unit_of(c)];
+        float q_unit[8];
+        __builtin_memcpy(asked_by, g.keep + my_i, 32); __builtin_memcpy(q_unit, g.q_unit + my_i, 32);
+        bad_q = g.bad_q;
+        const T *y = step_of<T>(a.dy, c * CHUNK, n) + (int64_t)h * V;
+        const int last = len - 1 - c * CHUNK;
+        const uint32_t column = (v0 + my_v < V ? v0 + my_v : V - 1) * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) given_y[x] = load_at<T>(y, row_at<T>(my_i + x < last ? my_i + x : last, a.dy.st, 0) + column);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            asked_by[x] = asked_by[x] >= 0.0f && !(bad_q >> (my_i + x) & 1) ? asked_by[x] * q_unit[x] * d.scale : 0.0f;
+        }
+    };
+    const auto load_rows = [&](int c) {                                // (as in the forward kernel)
+        const int t = c * CHUNK + i < len ? i : len - 1 - c * CHUNK;
+        const T *k = a.rows ? (const T *)a.rows + unit_of(c) * 2 * CHUNK * KP : step_of<T>(a.in.k, c * CHUNK, n) + (int64_t)group * K;
+        const uint32_t k_at = row_at<T>(t, a.rows ? KP : a.in.k.st, 0);
+#pragma unroll
+        for (int s = 0; s < KP / 32; ++s) kf[s] = load_at<Exact<T>>(k, k_at + (K < KP && 32 * s + 8 * quad >= K ? 0 : 32 * s + 8 * quad) * (uint32_t)sizeof(T));
+    };
+    const auto load_gates = [&](int c) {
+        const Gates &g = a.gates[unit_of(c)];
+        __builtin_memcpy(keep, g.keep + row, 16); __builtin_memcpy(k_unit, g.k_unit + row, 16);
+        __builtin_memcpy(strength, g.strength + row, 16); __builtin_memcpy(left, g.left + row, 16);
+        all = g.keep[CHUNK - 1]; bad_k = g.bad_k;
+    };
+    const auto load_pair = [&](Wide<T> (&f)[2], const char *base, int c) {      // (the first one of rows 32 .. 63 is zeros)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s == 1 || wave < 2) f[s] = get_wide<T>(base + (unit_of(c) * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+    };
+    const auto load_keys = [&](int c) {
+        if (!has_keys) return;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int64_t f = (unit_of(c) * (KP / 8) + (wave * MT + m) * 2 + s) * N_::EXACT_FRAGMENT + lane * 16;
+                tf[m][s] = get_exact<T>(a.keys + f, 1024); gf[m][s] = get_exact<T>(a.queries + f, 1024);
+            }
+    };
+    if (used > 0) { const int c = used - 1; load_outputs(c); load_rows(c); load_gates(c); }
     float held_sign = 1.0f;
-    for (int c = (len + CHUNK - 1) / CHUNK - 1; c >= 0; --c) {
-        const int64_t unit = ((int64_t)c * d.N + n) * d.H + h;
-        const Gates &gates = a.gates[unit];
+    for (int c = used - 1; c >= 0; --c) {
+        const int64_t unit = unit_of(c);
         const int t0 = c * CHUNK;
+        const bool more = c > 0;
+        load_pair(pf, a.read, c);
         const float sign = sign_of(c, n);
         if (sign != held_sign)
 #pragma unroll
@@ -641,8 +779,16 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt) S[m][nt] = -S[m][nt];
         held_sign = sign;
-        each_state([&](float s, bool there, int64_t at) { if (there) a.late[unit * K * V + at] = sign * s; return s; });
-        __syncthreads();                                       // (the arrays of the chunk after this one have been read)
+        if (has_keys) {
+            float *to = a.late + unit * KP * VP + v0;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) store_at(to + (16 * m + r) * (int64_t)VP + 16 * nt, state_at, sign * S[m][nt][r]);
+        }
+        lds_barrier();                                         // (the arrays of the chunk after this one have been read)
         if (has_keys)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -652,117 +798,104 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
                     put_wide4<T>(state + (16 * nt + col) * L::STATE_PITCH + (2 * (wave * MT + m) + (quad >> 1)) * N_::WIDE, 16, quad & 1, x);
                 }
         {
-            // 8 steps of one of the values' entries: a thread's
-            const int v = tid & 31, i0 = 8 * (tid >> 5);
-            const uint64_t bad_q = gates.bad_q;
             T x[8];
             float w[2][4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = t0 + i0 + i;
-                const bool live = t < len && v0 + v < V;
-                x[i] = from_f32<T>(live ? sign * to_f32(step_of<T>(a.dy, t, n)[(int64_t)h * V + v0 + v]) : 0.0f);
-                if (live && (!finite(to_f32(x[i])) || (bad_q >> (i0 + i) & 1))) { x[i] = from_f32<T>(0.0f); mark(marks, v, i0 + i, c); }
-                const float keep = gates.keep[i0 + i];
-                w[i >> 2][i & 3] = live && keep >= 0.0f && !(bad_q >> (i0 + i) & 1) ? keep * gates.q_unit[i0 + i] * d.scale * to_f32(x[i]) : 0.0f;
+            for (int e = 0; e < 8; ++e) {
+                const bool live = t0 + my_i + e < len && v0 + my_v < V;
+                x[e] = from_f32<T>(live ? sign * to_f32(given_y[e]) : 0.0f);
+                if (!finite(to_f32(x[e])) || (bad_q >> (my_i + e) & 1)) {
+                    x[e] = from_f32<T>(0.0f);
+                    if (live) mark(marks, my_v, my_i + e, c);
+                }
+                w[e >> 2][e & 3] = asked_by[e] * to_f32(x[e]);
             }
-            put_exact<T>(given + v * L::EXACT_PITCH + (i0 >> 3) * N_::EXACT, 16, make_exact<T>(x));
-            put_wide4<T>(asked + v * L::ROW_PITCH + (i0 >> 3) * N_::WIDE, 16, 0, w[0]);
-            put_wide4<T>(asked + v * L::ROW_PITCH + (i0 >> 3) * N_::WIDE, 16, 1, w[1]);
+            put_exact<T>(given + my_v * L::EXACT_PITCH + (my_i >> 3) * N_::EXACT, 16, make_exact<T>(x));
+            put_wide4<T>(asked + my_v * L::ROW_PITCH + (my_i >> 3) * N_::WIDE, 16, 0, w[0]);
+            put_wide4<T>(asked + my_v * L::ROW_PITCH + (my_i >> 3) * N_::WIDE, 16, 1, w[1]);
         }
-        __syncthreads();
+        if (more) load_outputs(c - 1);
+        lds_barrier();
         // dU: by the outputs of this chunk, by the state at its end
         f32x4 du[2] = {}, ks[2] = {};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            if (s == 0 && wave >= 2) continue;                 // (steps before: zeros)
-            const Wide<T> p = get_wide<T>(a.read + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
+            if (s == 0 && wave >= 2) continue;
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) mma(du[nt], p, get_exact<T>(given + (16 * nt + col) * L::EXACT_PITCH + (4 * s + quad) * N_::EXACT, 16));
+            for (int nt = 0; nt < 2; ++nt) mma(du[nt], pf[s], get_exact<T>(given + (16 * nt + col) * L::EXACT_PITCH + (4 * s + quad) * N_::EXACT, 16));
         }
-        const int mine = t0 + 16 * wave + col;
-        const T *k_row = mine < len ? step_of<T>(a.in.k, mine, n) + (int64_t)group * K : nullptr;
+        load_pair(wf, a.inverse_t, c);
 #pragma unroll
         for (int s = 0; s < KP / 32; ++s) {
-            const Exact<T> kf = exact_row(k_row, 32 * s + 8 * quad, K);
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) mma(ks[nt], kf, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * s + quad) * N_::WIDE, 16));
+            for (int nt = 0; nt < 2; ++nt) mma(ks[nt], kf[s], get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * s + quad) * N_::WIDE, 16));
+            __builtin_amdgcn_sched_barrier(0);
         }
-        const int row = 16 * wave + 4 * quad;
-        float keep[4], k_unit[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { keep[r] = gates.keep[row + r]; k_unit[r] = gates.k_unit[row + r]; }
-        const uint64_t bad_k = gates.bad_k;
+        if (more) load_rows(c - 1);
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             float x[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float left = gates.left[row + r];
                 x[r] = du[nt][r];
-                if (left >= 0.0f) x[r] += left * k_unit[r] * ks[nt][r];
-                x[r] *= gates.strength[row + r];
+                if (left[r] >= 0.0f) x[r] += left[r] * k_unit[r] * ks[nt][r];
+                x[r] = t0 + row + r < len ? x[r] * strength[r] : 0.0f;
                 if (!finite(x[r]) || (bad_k >> (row + r) & 1)) { x[r] = 0.0f; if (v0 + 16 * nt + col < V) mark(marks, 16 * nt + col, row + r, c); }
             }
             put_wide4<T>(sent + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, x);
         }
-        __syncthreads();
+        lds_barrier();
         const bool some = marks.any == (uint32_t)c + 1;
         f32x4 dv[2] = {};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             if (s == 0 && wave >= 2) continue;
-            const Wide<T> w = get_wide<T>(a.inverse_t + (unit * 8 + wave * 2 + s) * N_::WIDE_FRAGMENT + lane * 16, 1024);
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) mma(dv[nt], w, get_wide<T>(sent + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16));
+            for (int nt = 0; nt < 2; ++nt) mma(dv[nt], wf[s], get_wide<T>(sent + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16));
         }
-        __syncthreads();
+        load_keys(c);
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-            const int v = v0 + 16 * nt + col;
-            float x[4];
+            float x[4], *to = a.write + unit * CHUNK * VP + v0 + 16 * nt;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 x[r] = keep[r] >= 0.0f ? -(keep[r] * k_unit[r] * dv[nt][r]) : 0.0f;
-                if (v < V && t0 + row + r < len) {
-                    // a step's gradient has what the later ones of its episode have
-                    bool wrong = false;
-                    if (some) {
-                        const uint64_t later = row + r == 63 ? 0 : gates.resets & (~0ull << (row + r + 1));
-                        wrong = marks.of(16 * nt + col) & steps_between(row + r, later ? __builtin_ctzll(later) - 1 : 63);
-                    }
-                    a.write[unit * CHUNK * V + (int64_t)(row + r) * V + v] = wrong ? __builtin_nanf("") : sign * dv[nt][r];
+                // a step's gradient has what the later ones of its episode have
+                bool wrong = false;
+                if (some && t0 + row + r < len) {
+                    const uint64_t later = row + r == 63 ? 0 : a.gates[unit].resets & (~0ull << (row + r + 1));
+                    wrong = marks.of(16 * nt + col) & steps_between(row + r, later ? __builtin_ctzll(later) - 1 : 63);
                 }
+                store_at(to + r * (int64_t)VP, dv_at, wrong ? __builtin_nanf("") : sign * dv[nt][r]);
             }
-            put_wide4<T>(sent + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, x);
+            put_wide4<T>(kept + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, x);
         }
-        __syncthreads();
-        const float all = gates.keep[CHUNK - 1];
+        const float all_of = all;
+        if (more) load_gates(c - 1);
+        lds_barrier();
         if (has_keys) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[m][nt][r] = all >= 0.0f ? all * S[m][nt][r] : 0.0f;
+                    for (int r = 0; r < 4; ++r) S[m][nt][r] = all_of >= 0.0f ? all_of * S[m][nt][r] : 0.0f;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 Wide<T> w[2], y[2];
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt) {
-                    w[nt] = get_wide<T>(sent + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16);
+                    w[nt] = get_wide<T>(kept + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16);
                     y[nt] = get_wide<T>(asked + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16);
                 }
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const int64_t f = (unit * (KP / 8) + (wave * MT + m) * 2 + s) * N_::EXACT_FRAGMENT + lane * 16;
-                    const Exact<T> kf = get_exact<T>(a.keys + f, 1024), qf = get_exact<T>(a.queries + f, 1024);
+                for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int nt = 0; nt < 2; ++nt) { mma(S[m][nt], kf, w[nt]); mma(S[m][nt], qf, y[nt]); }
-                }
+                    for (int nt = 0; nt < 2; ++nt) { mma(S[m][nt], tf[m][s], w[nt]); mma(S[m][nt], gf[m][s], y[nt]); }
+                __builtin_amdgcn_sched_barrier(0);
             }
             if (some) {
-                const uint64_t before = gates.resets ? (gates.resets & 1 ? 0 : steps_between(0, __builtin_ctzll(gates.resets) - 1)) : ~0ull;
+                const uint64_t resets = a.gates[unit].resets, before = resets ? (resets & 1 ? 0 : steps_between(0, __builtin_ctzll(resets) - 1)) : ~0ull;
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -773,7 +906,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void reverse_ker
             }
         }
         if (some) {
-            __syncthreads();
+            lds_barrier();
             if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
         }
     }
@@ -856,14 +989,16 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
     const float my_strength = gates.strength[my_row];
     float z[4], g[4], s8[8], l8[8];
     T y[4];
-    const int64_t at_row = unit * CHUNK * V + (int64_t)my_row * V, at_state = (unit * K + 16 * kt + col) * V;
-    const bool has_key = 16 * kt + col < K;
+    const bool whole = t0 + CHUNK <= len;
+    const uint32_t my_at = row_at<float>(my_row, a.VP, 4 * my_part), my_y = row_at<T>(my_row, a.dy.st, 4 * my_part), my_dv = row_at<T>(my_row, a.g.dv.st, 4 * my_part);
+    const uint32_t state_at = row_at<float>(16 * kt + col, a.VP, 8 * quad);
     const auto load = [&](int v0) {
-        row4(z, my_live ? a.z + at_row : nullptr, v0 + 4 * my_part, V);
-        row4(g, my_live ? a.write + at_row : nullptr, v0 + 4 * my_part, V);
-        row4(y, my_live ? step_of<T>(a.dy, t0 + my_row, n) + (int64_t)h * V : nullptr, v0 + 4 * my_part, V);
-        row8(s8, has_key ? a.states + at_state : nullptr, v0 + 8 * quad, V);
-        row8(l8, has_key ? a.late + at_state : nullptr, v0 + 8 * quad, V);
+        __builtin_memcpy(z, (const char *)(a.z + unit * CHUNK * a.VP + v0) + my_at, 16);
+        __builtin_memcpy(g, (const char *)(a.write + unit * CHUNK * a.VP + v0) + my_at, 16);
+        __builtin_memcpy(s8, (const char *)(a.states + unit * KP * a.VP + v0) + state_at, 32);
+        __builtin_memcpy(l8, (const char *)(a.late + unit * KP * a.VP + v0) + state_at, 32);
+        if (whole && v0 + TILE <= V) __builtin_memcpy(y, (const char *)(step_of<T>(a.dy, t0, n) + (int64_t)h * V + v0) + my_y, sizeof y);
+        else row4(y, my_live ? step_of<T>(a.dy, t0 + my_row, n) + (int64_t)h * V : nullptr, v0 + 4 * my_part, V);
     };
     load(0);
     for (int v0 = 0, turn = 0; v0 < V; v0 += TILE, turn ^= 1) {
@@ -876,7 +1011,12 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
             put_wide4<T>(writes + p, 16, my_part & 1, u);
             put_wide4<T>(values + p, 16, my_part & 1, g);
             __builtin_memcpy(given + my_row * L::Y_PITCH + 4 * my_part * sizeof(T), y, sizeof y);
-            if (my_row < steps) {
+            if (whole && v0 + TILE <= V) {
+                Four<T> o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o.e[i] = from_f32<T>(g[i]);
+                store_at(step_of<T>(a.g.dv, t0, n) + (int64_t)h * V + v0, my_dv, o);
+            } else if (my_row < steps) {
                 const int v = v0 + 4 * my_part;
                 store4(step_of<T>(a.g.dv, t0 + my_row, n) + (int64_t)h * V + v, g, V - v);
             }
@@ -1226,11 +1366,10 @@ template <typename F> hipError_t by_keys(int K, F f)
     if (K <= 64) return f(std::integral_constant<int, 64>{});
     return f(std::integral_constant<int, 128>{});
 }
-int keys_padded(int K) { return K <= 32 ? 32 : K <= 64 ? 64 : 128; }
 
 constexpr int MOST_STEPS = 16;            // calls of so many steps or fewer go step by step
 
-struct Layout { int64_t inverse, read, keys, queries, gates, late, write, part, heads, total; };
+struct Layout { int64_t inverse, read, keys, queries, rows, gates, late, write, part, heads, total; };
 Layout layout(const hts_delta_rule_desc &d, bool back)
 {
     const int64_t units = ceil_div(d.T, CHUNK) * d.N * d.H, wide = d.precision == HTS_PRECISION_BF16 ? 3072 : 2048, exact = d.precision == HTS_PRECISION_BF16 ? 1024 : 2048;
@@ -1239,10 +1378,11 @@ Layout layout(const hts_delta_rule_desc &d, bool back)
     l.read = l.inverse + units * 8 * wide;
     l.keys = l.read + units * 8 * wide;
     l.queries = l.keys + units * (keys_padded(d.K) / 8) * exact;
-    l.gates = l.queries + (back ? units * (keys_padded(d.K) / 8) * exact : 0);
+    l.rows = l.queries + (back ? units * (keys_padded(d.K) / 8) * exact : 0);
+    l.gates = l.rows + (d.K % 8 ? units * 2 * (keys_padded(d.K) / 8) * exact : 0);
     l.late = l.gates + round_up(units * (int64_t)sizeof(Gates), 256);
-    l.write = l.late + (back ? round_up(units * d.K * d.V * 4, 256) : 0);
-    l.part = l.write + (back ? round_up(units * CHUNK * d.V * 4, 256) : 0);
+    l.write = l.late + (back ? units * keys_padded(d.K) * round_up(d.V, TILE) * 4 : 0);
+    l.part = l.write + (back ? units * CHUNK * round_up(d.V, TILE) * 4 : 0);
     l.heads = l.part + (back ? round_up(ceil_div(d.T, CHUNK) * d.N * 2 * d.H * 4, 256) : 0);
     l.total = l.heads + (back && d.H > d.G ? units * 2 * CHUNK * d.K * 4 : 0);
     return l;
@@ -1253,9 +1393,9 @@ DeltaArgs arguments(hts_seq_ctx &c, const DeltaOp &op, bool back)
     DeltaArgs a = {};
     a.d = op.d; a.in = op.in; a.y = op.y; a.dy = op.dy; a.h_out = op.h_out; a.states = op.states; a.dh_out = op.dh_out; a.g = op.g;
     a.chunks = (int)ceil_div(op.d.T, CHUNK);
-    a.tiles = (int)ceil_div(op.d.V, TILE);
+    a.tiles = (int)ceil_div(op.d.V, TILE); a.VP = a.tiles * TILE;
     if (op.states) a.z = op.states + delta_state_floats(op.d);
-    a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates);
+    a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates); a.rows = op.d.K % 8 ? c.ws + l.rows : nullptr;
     a.late = (float *)(c.ws + l.late); a.write = (float *)(c.ws + l.write); a.part = (float *)(c.ws + l.part); a.heads = (float *)(c.ws + l.heads);
     return a;
 }
@@ -1270,7 +1410,7 @@ template <typename T> hipError_t forward(hts_seq_ctx &c, const DeltaOp &op)
     return by_keys(d.K, [&](auto kp) {
         constexpr int KP = decltype(kp)::value;
         const hipError_t e = launch(prep_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
-        return e != hipSuccess ? e : launch(forward_kernel<T, KP>, (int64_t)d.N * d.H * a.tiles, RunLds<T, KP>::BYTES, c.stream, a);
+        return e != hipSuccess ? e : launch(forward_kernel<T, KP>, parts(a), RunLds<T, KP>::BYTES, c.stream, a);
     });
 }
 template <typename T> hipError_t backward(hts_seq_ctx &c, const DeltaOp &op)
@@ -1280,7 +1420,7 @@ template <typename T> hipError_t backward(hts_seq_ctx &c, const DeltaOp &op)
     const hipError_t e = by_keys(d.K, [&](auto kp) {
         constexpr int KP = decltype(kp)::value;
         hipError_t e = launch(prep_kernel<T, KP, true>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
-        if (e == hipSuccess) e = launch(reverse_kernel<T, KP>, (int64_t)d.N * d.H * a.tiles, RunLds<T, KP>::BYTES, c.stream, a);
+        if (e == hipSuccess) e = launch(reverse_kernel<T, KP>, parts(a), RunLds<T, KP>::BACK_BYTES, c.stream, a);
         if (e == hipSuccess) e = launch(d.H > d.G ? grads_kernel<T, KP, true> : grads_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, GradLds<T, KP>::BYTES, c.stream, a, 512);
         if (e == hipSuccess && d.H > d.G) e = launch(join_kernel<T>, (int64_t)a.chunks * d.N * d.G * (CHUNK / 4), 0, c.stream, a);
         return e;
@@ -1291,8 +1431,8 @@ template <typename T> hipError_t backward(hts_seq_ctx &c, const DeltaOp &op)
 }  // namespace
 
 int64_t delta_workspace(const hts_delta_rule_desc &d, bool back) { return !back && d.T <= MOST_STEPS ? 0 : layout(d, back).total; }
-int64_t delta_state_floats(const hts_delta_rule_desc &d) { return round_up(ceil_div(d.T, CHUNK) * d.N * d.H * d.K * d.V, 4); }
-int64_t delta_states(const hts_delta_rule_desc &d) { return delta_state_floats(d) + ceil_div(d.T, CHUNK) * CHUNK * d.N * d.H * d.V; }
+int64_t delta_state_floats(const hts_delta_rule_desc &d) { return ceil_div(d.T, CHUNK) * d.N * d.H * keys_padded(d.K) * round_up(d.V, TILE); }
+int64_t delta_states(const hts_delta_rule_desc &d) { return delta_state_floats(d) + ceil_div(d.T, CHUNK) * CHUNK * d.N * d.H * round_up(d.V, TILE); }
 
 hipError_t launch_delta(hts_seq_ctx &c, const DeltaOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? forward<bf16_t>(c, op) : forward<float>(c, op); }
 hipError_t launch_delta_backward(hts_seq_ctx &c, const DeltaOp &op) { return op.d.precision == HTS_PRECISION_BF16 ? backward<bf16_t>(c, op) : backward<float>(c, op); }

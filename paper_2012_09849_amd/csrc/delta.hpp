@@ -142,6 +142,24 @@ template <typename T> __device__ __forceinline__ Exact<T> exact_row(const T *row
     return make_exact<T>(x);
 }
 
+// An address as a base that all lanes share and 32 bits of a lane, which an access takes as they are: no arithmetic in vector registers.  (Steps are at most 2^24 entries
+// apart, so a chunk's lie within 4 GB of its first one.)
+template <typename P> __device__ __forceinline__ P load_at(const void *base, uint32_t at)
+{
+    P r;
+    __builtin_memcpy(&r, (const char *)base + at, sizeof r);
+    return r;
+}
+template <typename P> __device__ __forceinline__ void store_at(void *base, uint32_t at, const P &x) { __builtin_memcpy((char *)base + at, &x, sizeof x); }
+template <typename T> __device__ __forceinline__ uint32_t row_at(int64_t row, int64_t distance, int entry) { return (uint32_t)((row * distance + entry) * (int64_t)sizeof(T)); }
+template <typename P> struct Four { P e[4]; };
+// the same value, which the compiler takes for another: addresses of paths that are hardly ever taken are formed on them, not kept in registers for them
+__device__ __forceinline__ int again(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) <= 3.402823466e38f; }
 // 2^x for exponents that are sums of many steps': what is left after the whole part is taken off has binary32's precision
 __device__ __forceinline__ float exp2_wide(double x)
@@ -164,11 +182,12 @@ struct DeltaArgs {
     hts_delta_rule_desc d;
     hts_delta_rule_inputs in;
     hts_steps y, dy;
-    float *h_out, *states, *z;                    // states [chunk][N][H][K][V]; z [chunk][N][H][64][V]: v minus what the state had for the key
+    float *h_out, *states, *z;                    // states [chunk][N][H][KP][VP]; z [chunk][N][H][64][VP]: v minus what the state had for the key
     const float *dh_out;
     hts_delta_rule_grads g;
-    int chunks, tiles;                            // tiles of the values
+    int chunks, tiles, VP;                        // tiles of the values; V in whole tiles (KP: K in whole fragments; zeros in what K, V and a sequence's end leave over)
     char *inverse, *inverse_t, *read, *keys, *queries;     // fragments of each chunk, sequence and head
+    char *rows;                                   // K no multiple of 8: keys [unit][64][KP], then queries, that rows are read from in eights
     Gates *gates;
     float *late, *write, *part, *heads;           // gradients of the states at the chunks' ends; of the values; sums of the decays' parameters; of shared queries and keys
 };

@@ -45,15 +45,6 @@ __device__ __forceinline__ void wave_order()
     __builtin_amdgcn_wave_barrier();
 }
 
-// a workgroup's LDS writes are there for its other wavefronts; unlike __syncthreads() it does not wait for what is on its way to or from memory
-__device__ __forceinline__ void lds_barrier()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);          // vmcnt 63, expcnt 7, lgkmcnt 0
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // A chunk's steps, by what is in it: most chunks have no episode that begins, no end of the sequence and no infinities, and ask nothing; a sequence ends once.  EACH: a
 // copy for episodes' beginnings alone, otherwise one for all (the gradients' main kernel, whose registers are full: 256 x 16 x 1024 channels of 32 states, both passes, 317 us,
 // with three copies 331; the other kernels three: 512 x 16 of 16 states 206 us, with two 210)

@@ -152,6 +152,15 @@ template <int ACT> __device__ __forceinline__ float act_slope(float v)
     if constexpr (ACT == HTS_ACT_GELU) return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + w * 0.39894228040143268f * exp_f(-0.5f * v * v);
     return 1.0f;
 }
+// a workgroup's LDS writes are there for its other wavefronts; unlike __syncthreads() it does not wait for what is on its way to or from memory
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);          // vmcnt 63, expcnt 7, lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // V entries from memory, or one at a time where their address is no multiple of their size
 template <typename T, int V> struct Loaded { T e[V]; };
 template <typename T, int V> __device__ __forceinline__ Loaded<T, V> load_v(const T *p)
