@@ -27,6 +27,18 @@ __device__ __forceinline__ float wave_add(float x)
     return x;
 }
 
+template <int CONTROL> __device__ __forceinline__ float add_moved(float x) { return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xf, 0xf, true)); }
+// over 16 neighbouring lanes: pairs, fours, eights (mirrored), sixteen
+__device__ __forceinline__ float add16(float x) { return add_moved<0x140>(add_moved<0x141>(add_moved<0x4E>(add_moved<0xB1>(x)))); }
+// ... over as many lanes as a row of eights has
+template <int LANES> __device__ __forceinline__ float add_row(float x)
+{
+    x = add_moved<0x4E>(add_moved<0xB1>(x));
+    if constexpr (LANES >= 8) x = add_moved<0x141>(x);
+    if constexpr (LANES >= 16) x = add_moved<0x140>(x);
+    return x;
+}
+
 struct Decay { float delta, slope, exponent; };       // exponent: of 2
 __device__ __forceinline__ Decay decay_of(float x, float bias, float A, int softplus)
 {
@@ -45,8 +57,8 @@ constexpr double LOG2E_64 = 1.4426950408889634074;
 template <typename T, int KP> struct PrepLds {
     static constexpr int PITCH = Num<T>::exact_pitch(KP), LINE = 65;
     static constexpr int FAR = 0, EPISODE = FAR + 8 * CHUNK, STRENGTH = EPISODE + 4 * CHUNK, Q = STRENGTH + 4 * CHUNK, K = Q + 4 * CHUNK, BAD = K + 4 * CHUNK;
-    static constexpr int KEYS = BAD + 64, QUERIES = KEYS + CHUNK * PITCH, BELOW = QUERIES + CHUNK * PITCH, INVERSE = BELOW + 4 * CHUNK * LINE, HALF = INVERSE + 4 * CHUNK * LINE;
-    static constexpr int BYTES = HALF + 4 * 32 * 33 + 64;
+    static constexpr int BELOW = BAD + 64, KEYS = BELOW + 4 * CHUNK * LINE, QUERIES = KEYS + CHUNK * PITCH, INVERSE = KEYS, HALF = INVERSE + 4 * CHUNK * LINE;  // (the keys have left by then)
+    static constexpr int BYTES = KEYS + (2 * CHUNK * PITCH > 4 * (CHUNK * LINE + 32 * 33) ? 2 * CHUNK * PITCH : 4 * (CHUNK * LINE + 32 * 33));
 };
 
 // C (16x16) = sum over n of A[row][k] B[k][col], binary32 from LDS
@@ -71,7 +83,7 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
     double *far = (double *)(lds + L::FAR);
     int *episode = (int *)(lds + L::EPISODE);
     float *strength = (float *)(lds + L::STRENGTH), *q_unit = (float *)(lds + L::Q), *k_unit = (float *)(lds + L::K);
-    uint32_t *bad = (uint32_t *)(lds + L::BAD);                     // [4] keys by wavefront, [4] queries, [2] rows of the matrix
+    uint32_t *bad = (uint32_t *)(lds + L::BAD);                     // [2] keys, and rows of the matrix; [2] queries
     float *below = (float *)(lds + L::BELOW), *inverse = (float *)(lds + L::INVERSE), *half = (float *)(lds + L::HALF);
     Gates &gates = a.gates[unit];
 
@@ -86,7 +98,7 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
             const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
             be = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
             e = (double)dc.exponent * LOG2E_64;
-            wrong = !finite(be) || !(e < 1e30);
+            wrong = !finite(be) || !(e < MOST_EXPONENT);
             reset = (a.in.starts && a.in.starts[(int64_t)t * d.N + n]) || e < FORGETS || wrong;
             if (wrong) be = 0.0f;
             if (reset) e = 0.0;
@@ -106,41 +118,44 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
         gates.keep[lane] = ep == 0 ? exp2_wide(e) : -1.0f;
         gates.left[lane] = ep == last ? exp2_wide(end - e) : -1.0f;
     }
-    // rows of keys and queries, zeros for those that are not finite, and their lengths
-    uint32_t bad_k = 0, bad_q = 0;
+    // rows of keys and queries, zeros for those that are not finite, and their lengths: a thread has 8 entries of a row at a time
     char *keys = lds + L::KEYS, *queries = lds + L::QUERIES;
-#pragma unroll 4
-    for (int rr = 0; rr < 16; ++rr) {
-        const int row = wave * 16 + rr, t = t0 + row;
-        const bool live = t < len;
-        const T *kr = live ? step_of<T>(a.in.k, t, n) + (int64_t)group * K : nullptr, *qr = live ? step_of<T>(a.in.q, t, n) + (int64_t)group * K : nullptr;
-        T kx[2], qx[2];
+    constexpr int EIGHTS = KP / 8, TIMES = CHUNK * EIGHTS / 256, ROWS = 256 / EIGHTS;
+    T kx[TIMES][8], qx[TIMES][8];
+    const int my_at = 8 * (tid % EIGHTS);
+#pragma unroll
+    for (int i = 0; i < TIMES; ++i) {
+        const int t = t0 + i * ROWS + tid / EIGHTS;
+        row8(kx[i], t < len ? step_of<T>(a.in.k, t, n) + (int64_t)group * K : nullptr, my_at, K);
+        row8(qx[i], t < len ? step_of<T>(a.in.q, t, n) + (int64_t)group * K : nullptr, my_at, K);
+    }
+    if (tid < 16) bad[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TIMES; ++i) {
+        const int row = i * ROWS + tid / EIGHTS;
         float ks = 0.0f, qs = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = lane + 64 * i;
-            kx[i] = live && at < K ? kr[at] : from_f32<T>(0.0f);
-            qx[i] = live && at < K ? qr[at] : from_f32<T>(0.0f);
-            ks = __builtin_fmaf(to_f32(kx[i]), to_f32(kx[i]), ks);
-            qs = __builtin_fmaf(to_f32(qx[i]), to_f32(qx[i]), qs);
+        for (int e = 0; e < 8; ++e) {
+            ks = __builtin_fmaf(to_f32(kx[i][e]), to_f32(kx[i][e]), ks);
+            qs = __builtin_fmaf(to_f32(qx[i][e]), to_f32(qx[i][e]), qs);
         }
-        ks = wave_add(ks); qs = wave_add(qs);
+        ks = add_row<EIGHTS>(ks); qs = add_row<EIGHTS>(qs);
         const bool k_wrong = !finite(ks), q_wrong = !finite(qs);
-        bad_k |= (uint32_t)k_wrong << rr; bad_q |= (uint32_t)q_wrong << rr;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = lane + 64 * i;
-            if (at >= KP) continue;
-            *(T *)(keys + row * L::PITCH + at * sizeof(T)) = k_wrong ? from_f32<T>(0.0f) : kx[i];
-            *(T *)(queries + row * L::PITCH + at * sizeof(T)) = q_wrong ? from_f32<T>(0.0f) : qx[i];
+        for (int e = 0; e < 8; ++e) {
+            if (k_wrong) kx[i][e] = from_f32<T>(0.0f);
+            if (q_wrong) qx[i][e] = from_f32<T>(0.0f);
         }
-        if (lane == 0) {
+        put_exact<T>(keys + row * L::PITCH + my_at / 8 * N_::EXACT, 16, make_exact<T>(kx[i]));
+        put_exact<T>(queries + row * L::PITCH + my_at / 8 * N_::EXACT, 16, make_exact<T>(qx[i]));
+        if (my_at == 0) {
             k_unit[row] = gates.k_unit[row] = d.normalize && !k_wrong ? 1.0f / __builtin_sqrtf(ks + 1e-6f) : 1.0f;
             q_unit[row] = gates.q_unit[row] = q_wrong ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(qs + 1e-6f) : 1.0f;
+            if (k_wrong) atomicOr(&bad[row >> 5], 1u << (row & 31));
+            if (q_wrong) atomicOr(&bad[2 + (row >> 5)], 1u << (row & 31));
         }
     }
-    if (lane == 0) { bad[wave] = bad_k; bad[4 + wave] = bad_q; }
-    if (tid < 2) bad[8 + tid] = 0;
     __syncthreads();
 
     // M diag(be) below the diagonal; Q K^T G.  Wavefront w has rows 16 w .. of the steps that look back
@@ -172,7 +187,7 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
                 float x = 0.0f;
                 if (j < i && episode[j] == ep_i[r]) {
                     x = kk[r] * (far_unit[r] * k_unit[j]) * exp2_wide(far_i[r] - far[j]) * strength[j];
-                    if (!finite(x)) { atomicOr(&bad[8 + (i >> 5)], 1u << (i & 31)); x = 0.0f; }
+                    if (!finite(x)) { atomicOr(&bad[i >> 5], 1u << (i & 31)); x = 0.0f; }
                 }
                 below[i * L::LINE + j] = x;
             }
@@ -262,9 +277,8 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
         put_wide4<T>((BACK ? a.inverse_t : a.inverse) + f, 1024, (at >> 2) & 1, v);
     }
     if (tid == 0) {
-        const auto rows = [&](int at) { return (uint64_t)bad[at] | (uint64_t)bad[at + 1] << 16 | (uint64_t)bad[at + 2] << 32 | (uint64_t)bad[at + 3] << 48; };
-        gates.bad_k = rows(0) | gates_bad | bad[8] | (uint64_t)bad[9] << 32;
-        gates.bad_q = rows(4);
+        gates.bad_k = gates_bad | bad[0] | (uint64_t)bad[1] << 32;
+        gates.bad_q = bad[2] | (uint64_t)bad[3] << 32;
         gates.resets = resets;
     }
 }
@@ -611,7 +625,7 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
         const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
         const double e = (double)dc.exponent * LOG2E_64;
         const bool reset = (a.in.starts && a.in.starts[(int64_t)t * d.N + n]) || e < FORGETS;
-        const float decay = reset ? 0.0f : e < 1e30 ? exp2_wide(e) : __builtin_nanf(""), strength = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
+        const float decay = reset ? 0.0f : e < MOST_EXPONENT ? exp2_wide(e) : __builtin_nanf(""), strength = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
         if (reset)
 #pragma unroll
             for (int m = 0; m < STEP_ROWS; ++m)
@@ -928,9 +942,6 @@ template <typename T, int KP> struct GradLds {
     static constexpr int ROWS = AREA, SUMS = ROWS + 4 * 2 * 8 * CHUNK, BYTES = SUMS + 4 * (5 * CHUNK + 8);
 };
 
-template <int CONTROL> __device__ __forceinline__ float add_moved(float x) { return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xf, 0xf, true)); }
-// over 16 neighbouring lanes: pairs, fours, eights (mirrored), sixteen
-__device__ __forceinline__ float add16(float x) { return add_moved<0x140>(add_moved<0x141>(add_moved<0x4E>(add_moved<0xB1>(x)))); }
 template <typename T> __device__ __forceinline__ void row4(T (&x)[4], const T *row, int at, int K)
 {
     if (row && at + 4 <= K) __builtin_memcpy(x, row + at, sizeof x);

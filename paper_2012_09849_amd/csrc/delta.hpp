@@ -161,10 +161,11 @@ __device__ __forceinline__ int again(int x)
 }
 
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) <= 3.402823466e38f; }
-// 2^x for exponents that are sums of many steps': what is left after the whole part is taken off has binary32's precision
+// 2^x for exponents that are sums of up to 64 steps' (each below MOST_EXPONENT in size, or forgets): what is left after the whole part is taken off has binary32's precision
+constexpr double MOST_EXPONENT = 4096.0;
 __device__ __forceinline__ float exp2_wide(double x)
 {
-    const double whole = __builtin_rint(x < -1000.0 ? -1000.0 : x > 1000.0 ? 1000.0 : x);
+    const double whole = __builtin_rint(x);
     return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(x - whole)), (int)whole);
 }
 
