@@ -311,12 +311,12 @@ template <typename T> __device__ __forceinline__ void store4(T *p, const float (
 // A head's tiles on one die (workgroups go to the dies in turn), whose L2 then has the chunks' fragments for all of them
 constexpr int DIES = 8;
 struct Part { int tile, h, n; };
-__device__ __forceinline__ Part part_of(const DeltaArgs &a)
+__device__ __forceinline__ Part part_of(const DeltaArgs &a, int tiles)
 {
-    const uint32_t die = blockIdx.x % DIES, i = blockIdx.x / DIES, head = i / a.tiles * DIES + die;
-    return Part{(int)(i % a.tiles), (int)(head % a.d.H), (int)(head / a.d.H)};
+    const uint32_t die = blockIdx.x % DIES, i = blockIdx.x / DIES, head = i / tiles * DIES + die;
+    return Part{(int)(i % tiles), (int)(head % a.d.H), (int)(head / a.d.H)};
 }
-inline int64_t parts(const DeltaArgs &a) { return round_up((int64_t)a.d.N * a.d.H, DIES) * a.tiles; }
+inline int64_t parts(const DeltaArgs &a, int tiles) { return round_up((int64_t)a.d.N * a.d.H, DIES) * tiles; }
 
 template <typename T, int KP> struct RunLds {
     typedef Num<T> N_;
@@ -327,17 +327,22 @@ template <typename T, int KP> struct RunLds {
 // tiles of 16 keys' entries of a wavefront
 template <int KP> constexpr int key_tiles() { return KP / 64 > 0 ? KP / 64 : 1; }
 
-template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_kernel(const DeltaArgs a)
+// ENDS: a segment's part of the states after it, of its own steps and, in tiles behind the values', of the state before it: that of a one for each key, and no values
+template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) void forward_kernel(const DeltaArgs a)
 {
     typedef RunLds<T, KP> L;
     typedef Num<T> N_;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const hts_delta_rule_desc &d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
-    const Part at = part_of(a);
+    const Part at = part_of(a, a.tiles + (ENDS ? KP / TILE : 0));
     if (at.n >= d.N) return;
-    const int tile = at.tile, h = at.h, n = at.n;
+    const bool ones = ENDS && at.tile >= a.tiles;
+    const int tile = ones ? at.tile - a.tiles : at.tile, h = at.h, n = at.n, segment = blockIdx.y;
     const int K = d.K, V = d.V, v0 = tile * TILE, group = h / (d.H / d.G), len = length_of(a, n);
+    const int begin = segment * a.per_segment, all_chunks = (len + CHUNK - 1) / CHUNK, used = begin + a.per_segment < all_chunks ? begin + a.per_segment : all_chunks;
+    if (begin >= used && segment > 0) return;
+    const int64_t place = ((int64_t)segment * d.N + n) * d.H + h;
     constexpr int MT = key_tiles<KP>();
     const bool has_keys = wave * MT * 16 < KP;
     char *state = lds + L::STATE, *left_over = lds + L::ONE, *writes = lds + L::TWO, *late = lds + L::THREE;
@@ -370,13 +375,28 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
                 put_wide4<T>(state + (16 * nt + col) * L::STATE_PITCH + (2 * (wave * MT + m) + (quad >> 1)) * N_::WIDE, 16, quad & 1, x);
             }
     };
-    each_state([&](float, bool there, int64_t at) { return there && a.in.h_in ? a.in.h_in[held + at] : 0.0f; });
-    share_state();
     const int VP = a.VP;
+    if constexpr (ENDS) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[m][nt][r] = ones && 16 * (wave * MT + m) + 4 * quad + r == v0 + 16 * nt + col ? 1.0f : 0.0f;
+    } else if (segment > 0) {
+        if (has_keys)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) S[m][nt][r] = a.begins[(place * KP + 16 * (wave * MT + m) + 4 * quad + r) * VP + v0 + 16 * nt + col];
+    } else each_state([&](float, bool there, int64_t at) { return there && a.in.h_in ? a.in.h_in[held + at] : 0.0f; });
+    share_state();
     const uint32_t state_at = row_at<float>(16 * wave * MT + 4 * quad, VP, col), z_at = row_at<float>(16 * wave + 4 * quad, VP, col);
 
     // A chunk's operands are requested when the chunk's before it have been used, and arrive while it is worked on (the barriers wait for LDS only)
-    const int used = (len + CHUNK - 1) / CHUNK, row = 16 * wave + 4 * quad, i = 16 * wave + col;     // of 4 steps, one after the other; of a step
+    const int row = 16 * wave + 4 * quad, i = 16 * wave + col;     // of 4 steps, one after the other; of a step
     Exact<T> kf[KP / 32], qf[KP / 32], tf[MT][2];
     Wide<T> wf[2], pf[2];
     T val[2][4];
@@ -392,7 +412,8 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
 #pragma unroll
         for (int s = 0; s < KP / 32; ++s) {
             const uint32_t at = (K < KP && 32 * s + 8 * quad >= K ? 0 : 32 * s + 8 * quad) * (uint32_t)sizeof(T);
-            kf[s] = load_at<Exact<T>>(k, k_at + at); qf[s] = load_at<Exact<T>>(q, q_at + at);
+            kf[s] = load_at<Exact<T>>(k, k_at + at);
+            if constexpr (!ENDS) qf[s] = load_at<Exact<T>>(q, q_at + at);
         }
     };
     const auto load_values = [&](int c) {
@@ -405,6 +426,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
             for (int nt = 0; nt < 2; ++nt) {
                 const int column = v0 + 16 * nt + col;
                 val[nt][r] = load_at<T>(v, at + (column < V ? column : V - 1) * (uint32_t)sizeof(T));
+                if (ones) val[nt][r] = from_f32<T>(0.0f);
             }
         }
     };
@@ -426,14 +448,14 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
 #pragma unroll
             for (int s = 0; s < 2; ++s) tf[m][s] = get_exact<T>(a.keys + (unit_of(c) * (KP / 8) + (wave * MT + m) * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024);
     };
-    if (used > 0) { load_rows(0); load_gates(0); load_values(0); }
+    if (begin < used) { load_rows(begin); load_gates(begin); load_values(begin); }
     lds_barrier();
-    for (int c = 0; c < used; ++c) {
+    for (int c = begin; c < used; ++c) {
         const int64_t unit = unit_of(c);
         const int t0 = c * CHUNK;
         const bool more = c + 1 < used;
         load_pair(wf, a.inverse, c);
-        if (a.states && has_keys) {
+        if (!ENDS && a.states && has_keys) {
             float *to = a.states + unit * KP * VP + v0;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -450,18 +472,18 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
             for (int nt = 0; nt < 2; ++nt) {
                 const Wide<T> sf = get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * s + quad) * N_::WIDE, 16);
                 mma(ks[nt], kf[s], sf);
-                mma(qs[nt], sf, qf[s]);
+                if constexpr (!ENDS) mma(qs[nt], sf, qf[s]);
             }
             __builtin_amdgcn_sched_barrier(0);                 // (operands of every s at once are more than there are registers)
         }
-        load_pair(pf, a.read, c);
+        if constexpr (!ENDS) load_pair(pf, a.read, c);
         if (more) load_rows(c + 1);
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             float e[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bool live = t0 + row + r < len && v0 + 16 * nt + col < V;
+                const bool live = t0 + row + r < len && (ones || v0 + 16 * nt + col < V);
                 e[r] = to_f32(val[nt][r]);
                 if (keep[r] >= 0.0f) e[r] -= keep[r] * k_unit[r] * ks[nt][r];
                 if (!live) e[r] = 0.0f;
@@ -489,9 +511,9 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
                 u[r] = strength[r] * z[nt][r];
                 l[r] = left[r] >= 0.0f ? left[r] * k_unit[r] * u[r] : 0.0f;
             }
-            put_wide4<T>(writes + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, u);
+            if constexpr (!ENDS) put_wide4<T>(writes + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, u);
             put_wide4<T>(late + (16 * nt + col) * L::ROW_PITCH + (row >> 3) * N_::WIDE, 16, quad & 1, l);
-            if (a.z) {
+            if (!ENDS && a.z) {
                 float *to = a.z + unit * CHUNK * VP + v0 + 16 * nt;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -502,6 +524,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
         }
         lds_barrier();
         // outputs, the values along a row
+        if constexpr (!ENDS) {
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
@@ -527,6 +550,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
 #pragma unroll
                     for (int r = 0; r < 4; ++r) if (r < count) store_at(y + 16 * nt + r, y_at, o.e[r]);
             }
+        }
         }
         // the state at the end
         if (has_keys) {
@@ -566,10 +590,90 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void forward_
             lds_barrier();
         }
     }
-    if (a.h_out) each_state([&](float s, bool there, int64_t at) { if (there) a.h_out[held + at] = s; return s; });
+    if constexpr (ENDS) {
+        const int width = VP + KP, first = ones ? VP + v0 : v0;
+        if (has_keys)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) a.ends[(place * KP + 16 * (wave * MT + m) + 4 * quad + r) * width + first + 16 * nt + col] = S[m][nt][r];
+        return;
+    }
+    if (a.h_out && used == all_chunks) each_state([&](float s, bool there, int64_t at) { if (there) a.h_out[held + at] = s; return s; });
+    if (segment > 0) return;
     for (int64_t p = tid; p < (int64_t)(d.T - len) * TILE; p += 256) {
         const int v = v0 + (int)(p % TILE);
         if (v < V) step_of<T>(a.y, len + p / TILE, n)[(int64_t)h * V + v] = from_f32<T>(0.0f);
+    }
+}
+
+// The states that the segments begin with: from one to the next, what its steps make of the state before it and what they add.  A segment in which an episode begins leaves
+// nothing of it (not 0 times it, which would be NaN of what is not finite).
+template <typename T, int KP> __global__ __launch_bounds__(256) void begin_kernel(const DeltaArgs a)
+{
+    typedef RunLds<T, KP> L;
+    typedef Num<T> N_;
+    __shared__ __attribute__((aligned(16))) char state[TILE * L::STATE_PITCH];
+    const hts_delta_rule_desc &d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
+    const Part at = part_of(a, a.tiles);
+    if (at.n >= d.N) return;
+    const int h = at.h, n = at.n, v0 = at.tile * TILE, VP = a.VP, width = VP + KP, chunks = (length_of(a, n) + CHUNK - 1) / CHUNK;
+    constexpr int MT = key_tiles<KP>();
+    const bool has_keys = wave * MT * 16 < KP;
+    f32x4 S[MT][2] = {};
+    if (has_keys && a.in.h_in)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int k = 16 * (wave * MT + m) + 4 * quad + r, v = v0 + 16 * nt + col;
+                    if (k < d.K && v < d.V) S[m][nt][r] = a.in.h_in[(((int64_t)n * d.H + h) * d.K + k) * d.V + v];
+                }
+    for (int s = 0; s + 1 < a.segments && (s + 1) * a.per_segment < chunks; ++s) {
+        const int64_t place = ((int64_t)s * d.N + n) * d.H + h;
+        float move[KP / 32][MT][8];
+        if (has_keys)
+#pragma unroll
+            for (int k = 0; k < KP / 32; ++k)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    __builtin_memcpy(move[k][m], __builtin_assume_aligned(a.ends + (place * KP + 16 * (wave * MT + m) + col) * width + VP + 32 * k + 8 * quad, 16), 32);
+        bool passes = true;
+        for (int c = lane; c < a.per_segment; c += 64) passes = passes && a.gates[((int64_t)(s * a.per_segment + c) * d.N + n) * d.H + h].keep[CHUNK - 1] >= 0.0f;
+        passes = __all(passes);
+        if (has_keys)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    const float x[4] = {S[m][nt][0], S[m][nt][1], S[m][nt][2], S[m][nt][3]};
+                    put_wide4<T>(state + (16 * nt + col) * L::STATE_PITCH + (2 * (wave * MT + m) + (quad >> 1)) * N_::WIDE, 16, quad & 1, x);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[m][nt][r] = a.ends[(place * KP + 16 * (wave * MT + m) + 4 * quad + r) * width + v0 + 16 * nt + col];
+                }
+        __syncthreads();
+        if (has_keys && passes)
+#pragma unroll
+            for (int k = 0; k < KP / 32; ++k)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const Wide<T> moved = make_wide<T>(move[k][m]);
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) mma(S[m][nt], moved, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * k + quad) * N_::WIDE, 16));
+                }
+        if (has_keys)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) a.begins[((place + (int64_t)d.N * d.H) * KP + 16 * (wave * MT + m) + 4 * quad + r) * VP + v0 + 16 * nt + col] = S[m][nt][r];
+        __syncthreads();
     }
 }
 
@@ -697,7 +801,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void reverse_
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const hts_delta_rule_desc &d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
-    const Part at = part_of(a);
+    const Part at = part_of(a, a.tiles);
     if (at.n >= d.N) return;
     const int tile = at.tile, h = at.h, n = at.n;
     const int K = d.K, V = d.V, v0 = tile * TILE, group = h / (d.H / d.G), len = length_of(a, n);
@@ -1361,14 +1465,14 @@ template <typename T> __global__ __launch_bounds__(256) void join_kernel(const D
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
 // (more LDS than 64 KB has to be asked for)
-template <class F> hipError_t launch(F kernel, int64_t groups, int lds, hipStream_t stream, const DeltaArgs &a, int threads = 256)
+template <class F> hipError_t launch(F kernel, int64_t groups, int lds, hipStream_t stream, const DeltaArgs &a, int threads = 256, int segments = 1)
 {
-    if (!launchable(groups, threads) || groups > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (!launchable(groups, threads)) return hipErrorInvalidConfiguration;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(threads), (uint32_t)lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)groups, (uint32_t)segments), dim3(threads), (uint32_t)lds, stream, a);
     return hipGetLastError();
 }
 template <typename F> hipError_t by_keys(int K, F f)
@@ -1380,12 +1484,35 @@ template <typename F> hipError_t by_keys(int K, F f)
 
 constexpr int MOST_STEPS = 16;            // calls of so many steps or fewer go step by step
 
-struct Layout { int64_t inverse, read, keys, queries, rows, gates, late, write, part, heads, total; };
+// Segments: as many as a device of 256 units has room for beside each other, of 4 chunks or more, where there are three of them at least (with two the passes over the segments'
+// ends cost what they save).  The same on every device and range of units: results do not depend on where they are computed.
+struct Segments { int count, chunks; };
+constexpr int ROOM = 256;
+Segments segments_of(const hts_delta_rule_desc &d)
+{
+    const int64_t chunks = ceil_div(d.T, CHUNK), groups = (int64_t)d.N * d.H * ceil_div(d.V, TILE);
+    int64_t count = ROOM / groups;
+    if (count > chunks / 4) count = chunks / 4;
+    if (count < 3) return Segments{1, (int)chunks};
+    const int64_t each = ceil_div(chunks, count);
+    return Segments{(int)ceil_div(chunks, each), (int)each};
+}
+// ... their arrays, for the most that any number of sequences has
+int64_t most_places(const hts_delta_rule_desc &d)
+{
+    if (ceil_div(d.T, CHUNK) < 12) return 0;
+    return ROOM / ceil_div(d.V, TILE);
+}
+
+struct Layout { int64_t ends, begins,  inverse, read, keys, queries, rows, gates, late, write, part, heads, total; };
 Layout layout(const hts_delta_rule_desc &d, bool back)
 {
     const int64_t units = ceil_div(d.T, CHUNK) * d.N * d.H, wide = d.precision == HTS_PRECISION_BF16 ? 3072 : 2048, exact = d.precision == HTS_PRECISION_BF16 ? 1024 : 2048;
     Layout l;
-    l.inverse = 0;
+    const int64_t KP = keys_padded(d.K), VP = round_up(d.V, TILE), places = back ? 0 : most_places(d);
+    l.ends = 0;
+    l.begins = l.ends + 4 * places * KP * (VP + KP);
+    l.inverse = l.begins + 4 * places * KP * VP;
     l.read = l.inverse + units * 8 * wide;
     l.keys = l.read + units * 8 * wide;
     l.queries = l.keys + units * (keys_padded(d.K) / 8) * exact;
@@ -1404,11 +1531,21 @@ DeltaArgs arguments(hts_seq_ctx &c, const DeltaOp &op, bool back)
     DeltaArgs a = {};
     a.d = op.d; a.in = op.in; a.y = op.y; a.dy = op.dy; a.h_out = op.h_out; a.states = op.states; a.dh_out = op.dh_out; a.g = op.g;
     a.chunks = (int)ceil_div(op.d.T, CHUNK);
+    const Segments seg = segments_of(op.d);
+    a.segments = back ? 1 : seg.count; a.per_segment = back ? a.chunks : seg.chunks;
+    a.ends = (float *)(c.ws + l.ends); a.begins = (float *)(c.ws + l.begins);
     a.tiles = (int)ceil_div(op.d.V, TILE); a.VP = a.tiles * TILE;
     if (op.states) a.z = op.states + delta_state_floats(op.d);
     a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates); a.rows = op.d.K % 8 ? c.ws + l.rows : nullptr;
     a.late = (float *)(c.ws + l.late); a.write = (float *)(c.ws + l.write); a.part = (float *)(c.ws + l.part); a.heads = (float *)(c.ws + l.heads);
     return a;
+}
+// whether every launch of a call is within what the runtime takes: none is made otherwise
+bool fits(const DeltaArgs &a, bool back)
+{
+    const int64_t units = (int64_t)a.chunks * a.d.N * a.d.H;
+    if (!launchable(units, back ? 512 : 256) || !launchable(parts(a, a.tiles), 256)) return false;
+    return !back || a.d.H == a.d.G || launchable((int64_t)a.chunks * a.d.N * a.d.G * (CHUNK / 4), 256);
 }
 template <typename T> hipError_t forward(hts_seq_ctx &c, const DeltaOp &op)
 {
@@ -1418,20 +1555,26 @@ template <typename T> hipError_t forward(hts_seq_ctx &c, const DeltaOp &op)
         a.tiles = (int)ceil_div(d.V, STEP_TILE);
         return launch(step_kernel<T>, (int64_t)d.N * d.H * a.tiles, 0, c.stream, a);
     }
+    if (!fits(a, false)) return hipErrorInvalidConfiguration;
     return by_keys(d.K, [&](auto kp) {
         constexpr int KP = decltype(kp)::value;
-        const hipError_t e = launch(prep_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
-        return e != hipSuccess ? e : launch(forward_kernel<T, KP>, parts(a), RunLds<T, KP>::BYTES, c.stream, a);
+        hipError_t e = launch(prep_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
+        if (e == hipSuccess && a.segments > 1) {
+            e = launch(forward_kernel<T, KP, true>, parts(a, a.tiles + KP / TILE), RunLds<T, KP>::BYTES, c.stream, a, 256, a.segments - 1);
+            if (e == hipSuccess) e = launch(begin_kernel<T, KP>, parts(a, a.tiles), 0, c.stream, a);
+        }
+        return e != hipSuccess ? e : launch(forward_kernel<T, KP, false>, parts(a, a.tiles), RunLds<T, KP>::BYTES, c.stream, a, 256, a.segments);
     });
 }
 template <typename T> hipError_t backward(hts_seq_ctx &c, const DeltaOp &op)
 {
     const hts_delta_rule_desc &d = op.d;
     const DeltaArgs a = arguments(c, op, true);
+    if (!fits(a, true)) return hipErrorInvalidConfiguration;
     const hipError_t e = by_keys(d.K, [&](auto kp) {
         constexpr int KP = decltype(kp)::value;
         hipError_t e = launch(prep_kernel<T, KP, true>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
-        if (e == hipSuccess) e = launch(reverse_kernel<T, KP>, parts(a), RunLds<T, KP>::BACK_BYTES, c.stream, a);
+        if (e == hipSuccess) e = launch(reverse_kernel<T, KP>, parts(a, a.tiles), RunLds<T, KP>::BACK_BYTES, c.stream, a);
         if (e == hipSuccess) e = launch(d.H > d.G ? grads_kernel<T, KP, true> : grads_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, GradLds<T, KP>::BYTES, c.stream, a, 512);
         if (e == hipSuccess && d.H > d.G) e = launch(join_kernel<T>, (int64_t)a.chunks * d.N * d.G * (CHUNK / 4), 0, c.stream, a);
         return e;

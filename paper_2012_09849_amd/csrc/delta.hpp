@@ -190,6 +190,10 @@ struct DeltaArgs {
     char *inverse, *inverse_t, *read, *keys, *queries;     // fragments of each chunk, sequence and head
     char *rows;                                   // K no multiple of 8: keys [unit][64][KP], then queries, that rows are read from in eights
     Gates *gates;
+    // long sequences of few heads, in segments of so many chunks that are worked on at the same time: what each makes of nothing and of a state of ones on the diagonal,
+    // [segment][N][H][KP][VP + KP], and the states that they begin with, [segment][N][H][KP][VP]
+    int segments, per_segment;
+    float *ends, *begins;
     float *late, *write, *part, *heads;           // gradients of the states at the chunks' ends; of the values; sums of the decays' parameters; of shared queries and keys
 };
 __device__ __forceinline__ int length_of(const DeltaArgs &a, int n)

@@ -101,6 +101,20 @@ def test_values_and_gradients(hts, dtype, T, N, G, H, K, V, pad, shift, starts):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,G,H,K,V,starts", [(800, 1, 1, 1, 16, 24, 0.0), (1100, 2, 1, 2, 40, 40, 0.002), (1600, 1, 1, 1, 128, 128, 0.0), (900, 1, 1, 1, 64, 33, 0.01)])
+def test_long(hts, dtype, T, N, G, H, K, V, starts):  # noqa: F811
+    """Long sequences of few heads are worked on in segments at the same time: sequences that end in the first one, in a later one and at one's end among them; states of chunks."""
+    for lengths in (None, [T // 2 + 3] * N, [130] * N, [0] * N, [768] * N):
+        c = Case(hts, dtype, T, N, G, H, K, V, starts=starts, lengths=lengths)
+        got, plain = c.run(), c.run(False)
+        want, off = c.oracle()
+        for name in got:
+            so.near(host(got[name]), want[name], off[name] / so.U, 1, HALF["f32" if got[name].dtype is torch.float32 else dtype], name)
+        assert torch.equal(got["y"], plain["y"]) and torch.equal(got["h_out"], plain["h_out"])
+        c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [4, 140])
 def test_lengths(hts, dtype, T):  # noqa: F811
     """Sequences of no steps, of one, up to and past a chunk's end, fewer than none and more than all; what lies behind is not read, outputs there are zeros, states stay."""
