@@ -22,7 +22,7 @@ struct hts_adamw {
 namespace hts {
 namespace {
 
-constexpr int PIECE = 2048, GROUP = 256, NORM_GROUPS = 256;        // entries of a workgroup; that share a scale; partial sums of the norm
+constexpr int PIECE = 2048, GROUP = 256, NORM_GROUPS = 1024;       // entries of a workgroup; that share a scale; partial sums of the norm
 
 struct Tensor {
     float *p;
@@ -85,28 +85,30 @@ template <int THREADS> __device__ __forceinline__ double group_sum(double x, dou
     return s;
 }
 
-// Sums of squares, in 64 bits: the factor on the gradients is then the same however the sum is formed
-__global__ __launch_bounds__(1024) void norm_kernel(const StepArgs a)
+// Sums of squares, in 64 bits: the factor on the gradients is then the same however the sum is formed.  A workgroup takes two pieces at a time, 8 neighbours a thread of each
+__global__ __launch_bounds__(256) void norm_kernel(const StepArgs a)
 {
-    __shared__ double shared[16];
+    __shared__ double shared[4];
     double s = 0.0;
-    const int wave = threadIdx.x >> 8, lane = threadIdx.x & 255;
-    for (int64_t i = (int64_t)blockIdx.x * 4 + wave; i < a.count; i += NORM_GROUPS * 4) {
-        const Piece piece = a.pieces[i];
-        const Tensor t = a.tensors[piece.tensor];
-        const int64_t first = (int64_t)piece.part * PIECE + 4 * lane;
-        float g[PIECE / 1024][4];
+    for (int64_t i = blockIdx.x; i < a.count; i += 2 * NORM_GROUPS) {
+        float g[2][2][4] = {};
 #pragma unroll
-        for (int k = 0; k < PIECE / 1024; ++k) {
-            const int64_t at = first + 1024 * k, left = t.n - at;
-            take_grads(g[k], t, at, left > 4 ? 4 : left > 0 ? (int)left : 0);
+        for (int k = 0; k < 2; ++k) {
+            if (i + k * NORM_GROUPS >= a.count) continue;
+            const Piece piece = a.pieces[i + k * NORM_GROUPS];
+            const Tensor t = a.tensors[piece.tensor];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int64_t at = (int64_t)piece.part * PIECE + 8 * (int)threadIdx.x + 4 * e, left = t.n - at;
+                take_grads(g[k][e], t, at, left > 4 ? 4 : left > 0 ? (int)left : 0);
+            }
         }
 #pragma unroll
-        for (int k = 0; k < PIECE / 1024; ++k)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s += (double)g[k][e] * (double)g[k][e];
+            for (int e = 0; e < 8; ++e) s += (double)g[k][e >> 2][e & 3] * (double)g[k][e >> 2][e & 3];
     }
-    s = group_sum<1024>(s, shared);
+    s = group_sum<256>(s, shared);
     if (threadIdx.x == 0) a.norm[blockIdx.x] = s;
 }
 
@@ -115,8 +117,9 @@ __device__ __forceinline__ void philox(uint32_t (&c)[4], uint32_t k0, uint32_t k
 {
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
-        const uint32_t h0 = __umulhi(0xD2511F53u, c[0]), l0 = 0xD2511F53u * c[0], h1 = __umulhi(0xCD9E8D57u, c[2]), l1 = 0xCD9E8D57u * c[2];
-        c[0] = h1 ^ c[1] ^ k0; c[1] = l1; c[2] = h0 ^ c[3] ^ k1; c[3] = l0;
+        // (both halves of a product by one instruction)
+        const uint64_t p0 = (uint64_t)0xD2511F53u * c[0], p1 = (uint64_t)0xCD9E8D57u * c[2];
+        c[0] = (uint32_t)(p1 >> 32) ^ c[1] ^ k0; c[1] = (uint32_t)p1; c[2] = (uint32_t)(p0 >> 32) ^ c[3] ^ k1; c[3] = (uint32_t)p0;
         k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
     }
 }
@@ -125,7 +128,11 @@ __device__ __forceinline__ float power_of_2(int e) { return __uint_as_float((uin
 __device__ __forceinline__ float wave_max(float x)
 {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+    for (int o = 32; o >= 16; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+    // over 16 neighbouring lanes: pairs, fours, eights (mirrored), sixteen
+#define MOVED(control) x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), control, 0xf, 0xf, true)))
+    MOVED(0xB1); MOVED(0x4E); MOVED(0x141); MOVED(0x140);
+#undef MOVED
     return x;
 }
 __device__ __forceinline__ float size_of_finite(float x)
@@ -137,9 +144,10 @@ __device__ __forceinline__ float size_of_finite(float x)
 template <bool POSITIVE> __device__ __forceinline__ uint32_t held(float x, float by, uint32_t part)
 {
     const float y = x * by, s = __builtin_fabsf(y);
-    int e = exponent(s);
-    if (e < -6) e = -6;
-    int code = (e + 7) * 8 + (int)__builtin_floorf(s * power_of_2(3 - e) + (float)part * (1.0f / 65536.0f)) - 8;
+    // from 2^-6 on the exponent's digits go on above the number's: the random part is added to the 20 that are dropped, and a carry is the next power of two
+    const int normal = (int)((__float_as_uint(s) + (part << 4)) >> 20) - (120 << 3);
+    const int small = (int)__builtin_floorf(s * 512.0f + (float)part * (1.0f / 65536.0f));
+    int code = s >= 0.015625f ? normal : small;
     if (POSITIVE && code == 0 && s > 0.0f) code = 1;
     if (!(__builtin_fabsf(x) <= 3.402823466e38f)) return 0x7f;       // NaN
     return (uint32_t)code | (y < 0.0f ? 0x80u : 0u);
@@ -189,7 +197,10 @@ __global__ __launch_bounds__(256) void step_kernel(const StepArgs a)
     }
     float by = 1.0f;
     if (a.normed) {
-        const float norm = (float)__builtin_sqrt(group_sum<256>(a.norm[threadIdx.x], shared));
+        double part = 0.0;
+#pragma unroll
+        for (int k = 0; k < NORM_GROUPS / 256; ++k) part += a.norm[256 * k + threadIdx.x];
+        const float norm = (float)__builtin_sqrt(group_sum<256>(part, shared));
         if (a.clip > 0.0f) {
             by = a.clip / (norm + 1e-6f);
             by = by >= 1.0f ? 1.0f : by;            // (NaN stays)
@@ -355,7 +366,7 @@ extern "C" int32_t hts_adamw_step(hts_adamw *opt, const hts_adamw_hparams *hp, i
     a.eps = hp->eps; a.clip = hp->max_grad_norm;
     a.normed = hp->max_grad_norm > 0.0f || grad_norm_or_null;
     if (a.normed) {
-        hipLaunchKernelGGL(norm_kernel, dim3(NORM_GROUPS), dim3(1024), 0, opt->stream, a);
+        hipLaunchKernelGGL(norm_kernel, dim3(NORM_GROUPS), dim3(256), 0, opt->stream, a);
         HIP_TRY(hipGetLastError());
     }
     hipLaunchKernelGGL(step_kernel, dim3((uint32_t)opt->pieces), dim3(256), 0, opt->stream, a);

@@ -20,17 +20,7 @@ namespace {
 constexpr int TILE = 32;                  // the values' entries of a workgroup
 __host__ __device__ __forceinline__ int keys_padded(int K) { return K <= 32 ? 32 : K <= 64 ? 64 : 128; }
 
-__device__ __forceinline__ float wave_add(float x)
-{
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
-    return x;
-}
-
-template <int CONTROL> __device__ __forceinline__ float add_moved(float x) { return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xf, 0xf, true)); }
-// over 16 neighbouring lanes: pairs, fours, eights (mirrored), sixteen
-__device__ __forceinline__ float add16(float x) { return add_moved<0x140>(add_moved<0x141>(add_moved<0x4E>(add_moved<0xB1>(x)))); }
-// ... over as many lanes as a row of eights has
+// sums over as many neighbouring lanes as a row of eights has
 template <int LANES> __device__ __forceinline__ float add_row(float x)
 {
     x = add_moved<0x4E>(add_moved<0xB1>(x));

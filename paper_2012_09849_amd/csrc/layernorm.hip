@@ -2,7 +2,7 @@
 //
 //   y = (x - mean) r w + b,  r = 1 / sqrt(var + eps);   with h = (x - mean) r, g = dy w:  dx = r (g - mean(g) - h mean(g h)) + add,  dw = sum dy h,  db = sum dy
 //
-// Bound by bytes: a row is read once, into the registers of a wavefront (up to 2048 entries), of four or of sixteen, its variance is the mean square of what is left
+// Bound by bytes: a row is read once, into the registers of a wavefront (up to 1024 entries), of four or of sixteen, its variance is the mean square of what is left
 // after the mean is taken off, so that nothing cancels, and it is written once.  The backward call keeps nothing of the forward call: the mean and r of a row
 // that is in registers cost two reductions and no bytes.
 #include "seq.hpp"
@@ -51,34 +51,33 @@ template <int V> __device__ __forceinline__ void load_params(float (&v)[V], cons
         for (int i = 0; i < V; ++i) v[i] = i < count ? p[i] : 0.0f;
 }
 
-__device__ __forceinline__ float wave_sum(float x)
+// The sums of N values over the ROW threads of a row, by all of them, in the same order.  `turn`: the array that the next sums take, of two (whoever is still reading the other one
+// has not passed the barrier of this one).
+constexpr int SUMS = 16 * 2;
+template <int ROW, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float *shared, int &turn)
 {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
-    return x;
-}
-// The sums of N values over the ROW threads of a row.  Every wavefront adds the others' sums in the same order.
-template <int ROW, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float *shared)
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = wave_add(v[i]);
     if constexpr (ROW > 64) {
         constexpr int W = ROW / 64;
-        __syncthreads();
+        float *to = shared + turn * SUMS;
+        turn ^= 1;
+        const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int i = 0; i < N; ++i) shared[(threadIdx.x >> 6) * N + i] = v[i];
+            for (int i = 0; i < N; ++i) to[wave * N + i] = v[i];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             v[i] = 0.0f;
-            for (int k = 0; k < W; ++k) v[i] += shared[k * N + i];
+#pragma unroll
+            for (int k = 0; k < W; ++k) v[i] += to[(wave / W * W + k) * N + i];
         }
     }
 }
 
 // (x - mean) of a row that is in registers (0 where there is no entry), and r
-template <typename T, int ROW, int PER> __device__ __forceinline__ float centre(const Piece<T> (&x)[PER], float (&h)[PER][Piece<T>::V], const int first, const int F, const float eps, float *shared)
+template <typename T, int ROW, int PER> __device__ __forceinline__ float centre(const Piece<T> (&x)[PER], float (&h)[PER][Piece<T>::V], const int first, const int F, const float eps, float *shared, int &turn)
 {
     constexpr int V = Piece<T>::V;
     float s[1] = {0.0f};
@@ -86,60 +85,87 @@ template <typename T, int ROW, int PER> __device__ __forceinline__ float centre(
     for (int p = 0; p < PER; ++p)
 #pragma unroll
         for (int i = 0; i < V; ++i) s[0] += h[p][i] = to_f32(x[p].e[i]);
-    row_sums<ROW>(s, shared);
+    row_sums<ROW>(s, shared, turn);
     const float mean = s[0] / (float)F;
     s[0] = 0.0f;
 #pragma unroll
-    for (int p = 0; p < PER; ++p)
+    for (int p = 0; p < PER; ++p) {
+        const int count = F - first - p * ROW * V;
+        if (count >= V)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            h[p][i] = first + p * ROW * V + i < F ? h[p][i] - mean : 0.0f;
-            s[0] = __builtin_fmaf(h[p][i], h[p][i], s[0]);
-        }
-    row_sums<ROW>(s, shared);
+            for (int i = 0; i < V; ++i) h[p][i] -= mean;
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[p][i] = i < count ? h[p][i] - mean : 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[0] = __builtin_fmaf(h[p][i], h[p][i], s[0]);
+    }
+    row_sums<ROW>(s, shared, turn);
     return 1.0f / __builtin_sqrtf(s[0] / (float)F + eps);
 }
 
-template <typename T, int ROW, int PER> __global__ __launch_bounds__(ROW > 256 ? ROW : 256) void norm_kernel(const NormArgs a)
+template <int ROW> constexpr int threads() { return ROW > 256 ? ROW : 256; }
+template <typename T, int ROW, int PER> __global__ __launch_bounds__(threads<ROW>()) void norm_kernel(const NormArgs a)
 {
-    constexpr int V = Piece<T>::V, ROWS = ROW > 256 ? 1 : 256 / ROW;
-    __shared__ float shared[16];
-    const int in_row = ROW == 64 ? threadIdx.x & 63 : threadIdx.x, first = in_row * V;
+    constexpr int V = Piece<T>::V, ROWS = threads<ROW>() / ROW;
+    __shared__ float shared[2 * SUMS];
+    const int in_row = threadIdx.x % ROW, first = in_row * V;
+    const int64_t rows = (int64_t)gridDim.x * ROWS, begin = (int64_t)blockIdx.x * ROWS + threadIdx.x / ROW;
+    int turn = 0;
     float w[PER][V], b[PER][V];
-    bool have = false;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / ROW; row < a.M; row += (int64_t)gridDim.x * ROWS) {
-        Piece<T> x[PER];
+    Piece<T> x[PER], next[PER];
+    const auto load = [&](Piece<T> (&to)[PER], int64_t row) {
 #pragma unroll
-        for (int p = 0; p < PER; ++p) x[p].load((const T *)a.x + row * a.x_ld + first + p * ROW * V, a.F - first - p * ROW * V);
-        if (!have)
+        for (int p = 0; p < PER; ++p) to[p].load((const T *)a.x + row * a.x_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+    };
+    if (begin < a.M) load(x, begin);
 #pragma unroll
-            for (int p = 0; p < PER; ++p) {
-                const int at = first + p * ROW * V;
-                load_params<V>(w[p], a.w ? a.w + at : nullptr, a.F - at, 1.0f);
-                load_params<V>(b[p], a.b ? a.b + at : nullptr, a.F - at, 0.0f);
-            }
-        have = true;
+    for (int p = 0; p < PER; ++p) {
+        const int at = first + p * ROW * V;
+        load_params<V>(w[p], a.w ? a.w + at : nullptr, a.F - at, 1.0f);
+        load_params<V>(b[p], a.b ? a.b + at : nullptr, a.F - at, 0.0f);
+    }
+    for (int64_t row = begin; row < a.M; row += rows) {
+        if (row + rows < a.M) load(next, row + rows);          // on its way while this one is worked on
         float h[PER][V];
-        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, shared);
+        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, shared, turn);
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             Piece<T> y;
 #pragma unroll
             for (int i = 0; i < V; ++i) y.e[i] = from_f32<T>(__builtin_fmaf(h[p][i] * r, w[p][i], b[p][i]));
             y.store((T *)a.y + row * a.y_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+            x[p] = next[p];
         }
     }
 }
 
-constexpr int BACK_ROWS = 8;           // rows that a workgroup's wavefronts work on at a time, where a row is a wavefront's
-template <int ROW> constexpr int back_threads() { return ROW == 64 ? 64 * BACK_ROWS : ROW; }
+// Rows that a workgroup works on at a time: eight of a wavefront each, two of four, one of sixteen; and all of its threads go round together
+template <int ROW> constexpr int back_threads() { return ROW > 256 ? ROW : 512; }
 
 template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_threads<ROW>()) void norm_backward_kernel(const NormArgs a)
 {
     constexpr int V = Piece<T>::V, ROWS = back_threads<ROW>() / ROW, COLS = ROW * PER * V;
-    __shared__ float shared[ROWS > 1 ? ROWS * COLS : 32];
-    const int in_row = ROW == 64 ? threadIdx.x & 63 : threadIdx.x, first = in_row * V, wave = threadIdx.x / ROW;
+    __shared__ float shared[(ROWS > 1 ? ROWS * COLS : 0) + 2 * SUMS];
+    float *sums = shared + (ROWS > 1 ? ROWS * COLS : 0);
+    constexpr bool AHEAD = ROW <= 256;           // the next row's entries are requested before this one's are worked on (sixteen wavefronts have no registers for them)
+    const int in_row = threadIdx.x % ROW, first = in_row * V, mine = threadIdx.x / ROW;
+    const int64_t rows = (int64_t)gridDim.x * ROWS;
+    int turn = 0;
     float w[PER][V], dw[PER][V], db[PER][V];
+    Piece<T> x[PER], dy[PER], add[PER], next_x[PER] = {}, next_dy[PER] = {}, next_add[PER] = {};
+    const auto load = [&](Piece<T> (&to)[PER], const void *from, int64_t ld, int64_t row) {
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int at = first + p * ROW * V;
+            to[p].load((const T *)from + row * ld + at, row < a.M ? a.F - at : 0);
+        }
+    };
+    const bool adds = a.dx && a.add;
+    int64_t row = (int64_t)blockIdx.x * ROWS;
+    load(x, a.x, a.x_ld, row + mine);
+    load(dy, a.dy, a.dy_ld, row + mine);
+    if (adds) load(add, a.add, a.add_ld, row + mine);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
         const int at = first + p * ROW * V;
@@ -147,49 +173,54 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[p][i] = db[p][i] = 0.0f;
     }
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + wave; row < a.M; row += (int64_t)gridDim.x * ROWS) {
-        Piece<T> x[PER], dy[PER], add[PER];
-#pragma unroll
-        for (int p = 0; p < PER; ++p) {
-            const int at = first + p * ROW * V;
-            x[p].load((const T *)a.x + row * a.x_ld + at, a.F - at);
-            dy[p].load((const T *)a.dy + row * a.dy_ld + at, a.F - at);
+    for (; row < a.M; row += rows) {
+        const int64_t to = row + mine;
+        if (AHEAD && row + rows < a.M) {
+            load(next_x, a.x, a.x_ld, to + rows);
+            load(next_dy, a.dy, a.dy_ld, to + rows);
+            if (adds) load(next_add, a.add, a.add_ld, to + rows);
         }
-        if (a.dx && a.add)
-#pragma unroll
-            for (int p = 0; p < PER; ++p) add[p].load((const T *)a.add + row * a.add_ld + first + p * ROW * V, a.F - first - p * ROW * V);
         float h[PER][V];
-        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, shared);
+        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, sums, turn);
+        const float own = to < a.M ? r : 0.0f;                   // (of rows behind the last one r is that of zeros, which eps = 0 makes infinite)
         float s[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int p = 0; p < PER; ++p)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float d = to_f32(dy[p].e[i]), g = d * w[p][i];
-                h[p][i] *= r;
-                dw[p][i] = __builtin_fmaf(d, h[p][i], dw[p][i]);
+                h[p][i] *= own;
+                dw[p][i] = __builtin_fmaf(d, h[p][i], dw[p][i]);          // (of rows behind the last one: zeros)
                 db[p][i] += d;
                 s[0] += g;
                 s[1] = __builtin_fmaf(g, h[p][i], s[1]);
             }
-        if (!a.dx) continue;
-        row_sums<ROW>(s, shared);
-        const float mean = s[0] / (float)a.F, along = s[1] / (float)a.F;
+        if (a.dx) {
+            row_sums<ROW>(s, sums, turn);
+            const float mean = s[0] / (float)a.F, along = s[1] / (float)a.F;
+            if (to < a.M)
 #pragma unroll
-        for (int p = 0; p < PER; ++p) {
-            Piece<T> o;
+                for (int p = 0; p < PER; ++p) {
+                    Piece<T> o;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float g = to_f32(dy[p].e[i]) * w[p][i] - mean;
-                float v = r * __builtin_fmaf(-h[p][i], along, g);
-                if (a.add) v += to_f32(add[p].e[i]);
-                o.e[i] = from_f32<T>(v);
-            }
-            o.store((T *)a.dx + row * a.dx_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+                    for (int i = 0; i < V; ++i) {
+                        float v = r * __builtin_fmaf(-h[p][i], along, to_f32(dy[p].e[i]) * w[p][i] - mean);
+                        if (a.add) v += to_f32(add[p].e[i]);
+                        o.e[i] = from_f32<T>(v);
+                    }
+                    o.store((T *)a.dx + to * a.dx_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+                }
+        }
+#pragma unroll
+        for (int p = 0; p < PER; ++p) { x[p] = next_x[p]; dy[p] = next_dy[p]; add[p] = next_add[p]; }
+        if (!AHEAD && row + rows < a.M) {
+            load(x, a.x, a.x_ld, to + rows);
+            load(dy, a.dy, a.dy_ld, to + rows);
+            if (adds) load(add, a.add, a.add_ld, to + rows);
         }
     }
     if (!a.sums) return;
-    // a workgroup's sums: its rows in the order of its wavefronts
+    // a workgroup's sums: its rows in order
     float *part = a.part + (int64_t)blockIdx.x * 2 * a.F;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
@@ -198,7 +229,7 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
 #pragma unroll
             for (int p = 0; p < PER; ++p)
 #pragma unroll
-                for (int i = 0; i < V; ++i) shared[wave * COLS + first + p * ROW * V + i] = which ? db[p][i] : dw[p][i];
+                for (int i = 0; i < V; ++i) shared[mine * COLS + first + p * ROW * V + i] = which ? db[p][i] : dw[p][i];
             __syncthreads();
             for (int c = threadIdx.x; c < a.F; c += back_threads<ROW>()) {
                 float s = 0.0f;
@@ -218,35 +249,37 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
     }
 }
 
-// Entries of a row that a thread holds, and threads of a row: a wavefront up to 2048 entries, four up to 8192, sixteen up to 16384
+// Threads of a row, and entries that each holds: 8 or 16 of a wavefront's, of four or of sixteen wavefronts'.  (32 of a wavefront's left one or two of them to a SIMD: gradients of
+// 8192 x 2048 in bf16 38 us, with four wavefronts a row 30.)
 template <int V, typename F> hipError_t by_width(int width, F f)
 {
-    const int64_t per = ceil_div(width, 64 * V);
     const auto with = [&](auto row, auto entries) { return f(std::integral_constant<int, decltype(row)::value>{}, std::integral_constant<int, decltype(entries)::value / V>{}); };
     typedef std::integral_constant<int, 64> wave;
     typedef std::integral_constant<int, 256> four;
     typedef std::integral_constant<int, 1024> sixteen;
-    if (per * V <= 8) return with(wave{}, std::integral_constant<int, 8>{});
-    if (per * V <= 16) return with(wave{}, std::integral_constant<int, 16>{});
-    if (per * V <= 32) return with(wave{}, std::integral_constant<int, 32>{});
-    if (per * V <= 64) return with(four{}, std::integral_constant<int, 16>{});
-    if (per * V <= 128) return with(four{}, std::integral_constant<int, 32>{});
-    return with(sixteen{}, std::integral_constant<int, 16>{});
+    const std::integral_constant<int, 8> eight;
+    const std::integral_constant<int, 16> more;
+    if (width <= 512) return with(wave{}, eight);
+    if (width <= 1024) return with(wave{}, more);
+    if (width <= 2048) return with(four{}, eight);
+    if (width <= 4096) return with(four{}, more);
+    if (width <= 8192) return with(sixteen{}, eight);
+    return with(sixteen{}, more);
 }
 
-constexpr int MOST_PARTS = 256;        // workgroups of a backward call whose sums are added up afterwards
+// workgroups of a backward call, whose sums are added up afterwards: two a unit, one of sixteen wavefronts
 int back_parts(int64_t M, int64_t F)
 {
-    const int64_t rows = F <= 2048 ? BACK_ROWS : 1, groups = ceil_div(M, rows);
-    return (int)(groups < MOST_PARTS ? groups : MOST_PARTS);
+    const int64_t rows = F <= 1024 ? 8 : F <= 4096 ? 2 : 1, most = F <= 4096 ? 512 : 256, groups = ceil_div(M, rows);
+    return (int)(groups < most ? groups : most);
 }
 
 template <typename T> hipError_t norm(hts_seq_ctx &c, const NormArgs &a)
 {
     return by_width<Piece<T>::V>(a.F, [&](auto row, auto per) {
-        constexpr int ROW = decltype(row)::value, PER = decltype(per)::value, ROWS = ROW > 256 ? 1 : 256 / ROW;
-        const int64_t groups = ceil_div(a.M, ROWS), most = (int64_t)c.cus * (ROW > 256 ? 2 : 8);
-        hipLaunchKernelGGL((norm_kernel<T, ROW, PER>), dim3((uint32_t)(groups < most ? groups : most)), dim3(ROW > 256 ? ROW : 256), 0, c.stream, a);
+        constexpr int ROW = decltype(row)::value, PER = decltype(per)::value, ROWS = threads<ROW>() / ROW;
+        const int64_t groups = ceil_div(a.M, ROWS), most = (int64_t)c.cus * (ROW > 256 ? 2 : 4);
+        hipLaunchKernelGGL((norm_kernel<T, ROW, PER>), dim3((uint32_t)(groups < most ? groups : most)), dim3(threads<ROW>()), 0, c.stream, a);
         return hipGetLastError();
     });
 }

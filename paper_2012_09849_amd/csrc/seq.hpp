@@ -161,6 +161,16 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
+// Sums over 16 neighbouring lanes by moves between vector registers: pairs, fours, eights (mirrored), sixteen; over a wavefront
+template <int CONTROL> __device__ __forceinline__ float add_moved(float x) { return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float add16(float x) { return add_moved<0x140>(add_moved<0x141>(add_moved<0x4E>(add_moved<0xB1>(x)))); }
+__device__ __forceinline__ float wave_add(float x)
+{
+    x = add16(x);
+    x += __shfl_xor(x, 16, 64);
+    return x + __shfl_xor(x, 32, 64);
+}
+
 // V entries from memory, or one at a time where their address is no multiple of their size
 template <typename T, int V> struct Loaded { T e[V]; };
 template <typename T, int V> __device__ __forceinline__ Loaded<T, V> load_v(const T *p)

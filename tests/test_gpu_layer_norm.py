@@ -83,3 +83,17 @@ def test_no_noise(hts):  # noqa: F811
     want, off = do.norm(x64, None, None, 0.0)
     so.near(host(y), want["y"], off["y"] / so.U, 1, HALF["f32"], "y")
     ctx.close()
+
+
+@pytest.mark.parametrize("M,F", [(3, 100), (9, 1500), (1, 6000)])
+def test_no_eps(hts, M, F):  # noqa: F811
+    """Rows that are not there have no deviations, and without eps no inverse of them: nothing of it reaches the sums."""
+    ctx = hts.SeqContext(hts.layer_norm_workspace(M, F))
+    r = np.random.default_rng(6)
+    (x, x64), (dy, dy64) = put(r.normal(size=(M, F))), put(r.normal(size=(M, F)))
+    dx, dw, db = torch.empty_like(x), torch.empty(F, device="cuda"), torch.empty(F, device="cuda")
+    ctx.hts_layer_norm_backward(x, dy, dx=dx, dw=dw, db=db, eps=0.0)
+    want, off = do.norm(x64, None, None, 0.0, dy64)
+    for name, got in (("dx", dx), ("dw", dw), ("db", db)):
+        so.near(host(got), want[name], off[name] / so.U, 1, HALF["f32"], name)
+    ctx.close()
