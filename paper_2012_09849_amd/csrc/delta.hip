@@ -43,6 +43,10 @@ __device__ __forceinline__ Decay decay_of(float x, float bias, float A, int soft
 constexpr double FORGETS = -150.0;
 constexpr double LOG2E_64 = 1.4426950408889634074;
 
+// tiles of 16 x 16 steps on and below the diagonal
+constexpr int PAIRS = 10;
+__device__ __forceinline__ int pair_of(int back, int seen) { return back * (back + 1) / 2 + seen; }
+
 // ---- what needs the chunk's steps only --------------------------------------------------------------------------------
 template <typename T, int KP> struct PrepLds {
     static constexpr int PITCH = Num<T>::exact_pitch(KP), LINE = 65;
@@ -181,6 +185,18 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
                 }
                 below[i * L::LINE + j] = x;
             }
+            if constexpr (BACK)
+                if (jt <= wave) {
+                    Four<float> by_q, by_k;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        by_q.e[r] = qk[r] * (q_unit[16 * wave + 4 * quad + r] * d.scale * k_unit[j]);
+                        by_k.e[r] = kk[r] * (far_unit[r] * k_unit[j]);
+                    }
+                    float *to = a.pairs + (unit * 2 * PAIRS + pair_of(wave, jt)) * 256;
+                    store_at(to, lane * 16, by_q);
+                    store_at(to + PAIRS * 256, lane * 16, by_k);
+                }
             float p[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -1033,7 +1049,7 @@ template <typename T, int KP> struct GradLds {
     static constexpr int MATRIX = 0, MATRIX_PITCH = N_::pitch(CHUNK), PASSING = MATRIX + CHUNK * MATRIX_PITCH, AFTER = PASSING + 4 * CHUNK * LINE;
     static constexpr int OUT_PITCH = KP * (int)sizeof(T) + 16, OUT = 2 * CHUNK * OUT_PITCH;
     static constexpr int AREA = (2 * STAGE > AFTER ? 2 * STAGE : AFTER) > OUT ? (2 * STAGE > AFTER ? 2 * STAGE : AFTER) : OUT;
-    static constexpr int ROWS = AREA, SUMS = ROWS + 4 * 2 * 8 * CHUNK, BYTES = SUMS + 4 * (5 * CHUNK + 8);
+    static constexpr int ROWS = AREA, SUMS = ROWS + 4 * 2 * 8 * CHUNK, GATES = SUMS + 4 * (5 * CHUNK + 8), BYTES = GATES + (int)sizeof(Gates);
 };
 
 template <typename T> __device__ __forceinline__ void row4(T (&x)[4], const T *row, int at, int K)
@@ -1087,11 +1103,13 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
     Exact<T> kf[2], qf[2];
     const int my_row = tid >> 3, my_part = tid & 7;
     const bool my_live = t0 + my_row < len;
-    const Gates &gates = a.gates[unit];
-    f32x4 by_step[4] = {}, by_seen[4] = {};                  // rows 16 ti .. with columns 16 jt .., and the same the other way round
+    static_assert(sizeof(Gates) % 16 == 0, "whole pieces");
+    if (tid < (int)sizeof(Gates) / 16) *(u32x4 *)(lds + L::GATES + 16 * tid) = ((const u32x4 *)(a.gates + unit))[tid];       // read by every part from here on
+    const Gates &gates = *(const Gates *)(lds + L::GATES);
+    f32x4 by_step[4] = {};                                   // rows 16 ti .. with columns 16 jt ..
     f32x4 q_state[IT] = {}, k_late[IT] = {}, k_state[IT] = {};
     float z_dv = 0.0f, end = 0.0f;
-    const float my_strength = gates.strength[my_row];
+    const float my_strength = a.gates[unit].strength[my_row];
     float z[4], g[4], s8[8], l8[8];
     T y[4];
     const bool whole = t0 + CHUNK <= len;
@@ -1105,6 +1123,8 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
         if (whole && v0 + TILE <= V) __builtin_memcpy(y, (const char *)(step_of<T>(a.dy, t0, n) + (int64_t)h * V + v0) + my_y, sizeof y);
         else row4(y, my_live ? step_of<T>(a.dy, t0 + my_row, n) + (int64_t)h * V : nullptr, v0 + 4 * my_part, V);
     };
+    const auto fragment = [&](const char *base, int s) { return get_exact<T>(base + (unit * (KP / 8) + kt * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024); };
+    f32x4 pass[4] = {};
     load(0);
     for (int v0 = 0, turn = 0; v0 < V; v0 += TILE, turn ^= 1) {
         char *writes = lds + turn * L::STAGE + L::WRITES, *values = lds + turn * L::STAGE + L::VALUES, *given = lds + turn * L::STAGE + L::GIVEN;
@@ -1130,6 +1150,13 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
         for (int i = 0; i < 8; ++i) { end = __builtin_fmaf(s8[i], l8[i], end); s8[i] *= sign; }
         const Wide<T> sf = make_wide<T>(s8), lf = make_wide<T>(l8);
         if (v0 + TILE < V) load(v0 + TILE);
+        else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) { kf[s] = fragment(a.keys, s); qf[s] = fragment(a.queries, s); }
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt)
+                if (jt <= ti) pass[jt] = load_at<f32x4>(a.pairs + ((unit * 2 + by_values) * PAIRS + pair_of(ti, jt)) * 256, lane * 16);
+        }
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < IT; ++t) {
@@ -1144,14 +1171,11 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
         for (int jt = 0; jt < 4; ++jt)
             if (jt <= ti) {
                 const Wide<T> u = get_wide<T>(writes + (16 * jt + col) * L::PITCH + quad * N_::WIDE, 16);
-                if (by_values) { mma(by_step[jt], gf, u); mma(by_seen[jt], u, gf); }
-                else { mma(by_step[jt], yf, u); mma(by_seen[jt], u, yf); }
+                if (by_values) mma(by_step[jt], gf, u);
+                else mma(by_step[jt], yf, u);
             }
     }
     // sums along the keys of what goes through the state before the chunk, and through the one at its end
-    const auto fragment = [&](const char *base, int s) { return get_exact<T>(base + (unit * (KP / 8) + kt * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024); };
-#pragma unroll
-    for (int s = 0; s < 2; ++s) { kf[s] = fragment(a.keys, s); qf[s] = fragment(a.queries, s); }
 #pragma unroll
     for (int t = 0; t < IT; ++t) {
         const int tt = first_tile + t, step = tile_row(tt, 4 * quad);
@@ -1184,37 +1208,23 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
     if (lane == 0) sums[5 * CHUNK + wave] = end;
     // the steps among themselves, each pair's decay on it
     const int row = 16 * ti + 4 * quad, i_seen = 16 * ti + col;
-    const T *mine = t0 + i_seen < len ? step_of<T>(by_values ? a.in.k : a.in.q, t0 + i_seen, n) + (int64_t)group * K : nullptr;
-    f32x4 pass[4] = {};
     {
         double far_i[4];
         int ep_i[4];
-        float unit_i[4];
         __builtin_memcpy(far_i, gates.far + row, 32); __builtin_memcpy(ep_i, gates.episode + row, 16);
-        __builtin_memcpy(unit_i, (by_values ? gates.k_unit : gates.q_unit) + row, 16);
-        const double far_seen = gates.far[i_seen];
-        const int ep_seen = gates.episode[i_seen];
 #pragma unroll
         for (int jt = 0; jt < 4; ++jt) {
             if (jt > ti) continue;
             const int j = 16 * jt + col;
-            const T *k_row = t0 + j < len ? step_of<T>(a.in.k, t0 + j, n) + (int64_t)group * K : nullptr;
-#pragma unroll
-            for (int s = 0; s < KP / 32; ++s) mma(pass[jt], exact_row(mine, 32 * s + 8 * quad, K), exact_row(k_row, 32 * s + 8 * quad, K));
             const double far_j = gates.far[j];
-            const float unit_j = gates.k_unit[j];
             const int ep_j = gates.episode[j];
-            double far_s[4];
-            int ep_s[4];
-            __builtin_memcpy(far_s, gates.far + 16 * jt + 4 * quad, 32); __builtin_memcpy(ep_s, gates.episode + 16 * jt + 4 * quad, 16);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = row + r, js = 16 * jt + 4 * quad + r;
-                const bool sees = (by_values ? j < i : j <= i) && ep_j == ep_i[r], seen = (by_values ? js < i_seen : js <= i_seen) && ep_s[r] == ep_seen;
-                const float x = sees ? by_step[jt][r] * exp2_wide(far_i[r] - far_j) : 0.0f, w = seen ? by_seen[jt][r] * exp2_wide(far_seen - far_s[r]) : 0.0f;
+                const int i = row + r;
+                const bool sees = (by_values ? j < i : j <= i) && ep_j == ep_i[r];
+                const float x = sees ? by_step[jt][r] * exp2_wide(far_i[r] - far_j) : 0.0f;
                 by_step[jt][r] = by_values ? -sign * x : sign * x;
-                by_seen[jt][r] = by_values ? -sign * w : sign * w;
-                pass[jt][r] = sees && j < i ? by_step[jt][r] * (unit_j * unit_i[r] * (by_values ? 1.0f : d.scale) * pass[jt][r]) : 0.0f;
+                pass[jt][r] = sees && j < i ? by_step[jt][r] * pass[jt][r] : 0.0f;
             }
         }
     }
@@ -1226,16 +1236,17 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
             for (int s = 0; s < 2; ++s) mma(out[t], get_wide<T>(matrix + tile_row(first_tile + t, col) * L::MATRIX_PITCH + (4 * s + quad) * N_::WIDE, 16), f[s]);
     };
     const auto put_matrix = [&](int r, int at, const float (&x)[4]) { put_wide4<T>(matrix + r * L::MATRIX_PITCH + (at >> 3) * N_::WIDE, 16, (at >> 2) & 1, x); };
+    const auto put_one = [&](int r, int at, float x) { put_wide1<T>(matrix + r * L::MATRIX_PITCH + (at >> 3) * N_::WIDE, 16, at & 7, x); };
+    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     __syncthreads();
     // dQ: rows are the steps that look back
     if (!by_values) {
 #pragma unroll
         for (int jt = 0; jt < 4; ++jt) {
-            float unit_j[4], x[4];
-            __builtin_memcpy(unit_j, gates.k_unit + 16 * jt + 4 * quad, 16);
+            if (jt > ti) { put_matrix(i_seen, 16 * jt + 4 * quad, none); continue; }
+            const float unit_j = gates.k_unit[16 * jt + col];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = jt <= ti ? by_seen[jt][r] * unit_j[r] : 0.0f;
-            put_matrix(i_seen, 16 * jt + 4 * quad, x);
+            for (int r = 0; r < 4; ++r) put_one(row + r, 16 * jt + col, by_step[jt][r] * unit_j);
         }
     } else {
 #pragma unroll
@@ -1271,16 +1282,17 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
 #pragma unroll
         for (int jt = 0; jt < 4; ++jt) {
             if (jt > ti) continue;
-            float unit_j[4], x[4];
-            __builtin_memcpy(unit_j, gates.k_unit + 16 * jt + 4 * quad, 16);
+            const int j = 16 * jt + col;
+            const float unit_j = gates.k_unit[j];
+            float x[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = (jt == ti && 4 * quad + r > col ? by_step[jt][r] : by_seen[jt][r]) * unit_j[r];
-            put_matrix(i_seen, 16 * jt + 4 * quad, x);
-            if (jt < ti) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = by_step[jt][r] * unit_i[r];
-                put_matrix(16 * jt + col, row, x);
+            for (int r = 0; r < 4; ++r) {
+                x[r] = by_step[jt][r] * unit_i[r];
+                if (jt < ti || j < row + r) put_one(row + r, j, by_step[jt][r] * unit_j);
+                if (jt == ti && j < row + r) put_one(j, row + r, x[r]);
+                if (jt == ti && j == row + r) put_one(j, j, 0.0f);
             }
+            if (jt < ti) put_matrix(j, row, x);
         }
     } else {
         // what passes, along each row up to a column: 16 columns a thread, and those of the threads before it
@@ -1370,6 +1382,13 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
             }
         }
         __syncthreads();
+        if (tid < 2 * CHUNK) {
+            float x = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KT; ++k) x += rows[(tid / CHUNK * KT + k) * CHUNK + tid % CHUNK];
+            sums[tid] = x;
+        }
+        __syncthreads();
     }
     char *out_q = lds, *out_k = lds + CHUNK * L::OUT_PITCH;
 #pragma unroll
@@ -1380,9 +1399,7 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
             float x = d.scale * q_state[t][r], w = k_late[t][r];
             if (d.normalize) {
                 const float q_unit = gates.q_unit[step + r], k_unit = gates.k_unit[step + r];
-                float q_dq = 0.0f, k_dk = 0.0f;
-#pragma unroll
-                for (int k = 0; k < KT; ++k) { q_dq += rows[k * CHUNK + step + r]; k_dk += rows[(KT + k) * CHUNK + step + r]; }
+                const float q_dq = sums[step + r], k_dk = sums[CHUNK + step + r];
                 const float qv = entry(qf, tt, r), kv = entry(kf, tt, r);
                 x = q_unit * (x - q_unit * qv * (q_unit * d.scale * q_dq));
                 w = k_unit * (w - k_unit * kv * (k_unit * k_dk));
@@ -1494,7 +1511,7 @@ int64_t most_places(const hts_delta_rule_desc &d)
     return ROOM / ceil_div(d.V, TILE);
 }
 
-struct Layout { int64_t ends, begins,  inverse, read, keys, queries, rows, gates, late, write, part, heads, total; };
+struct Layout { int64_t ends, begins, inverse, read, keys, queries, pairs, rows, gates, late, write, part, heads, total; };
 Layout layout(const hts_delta_rule_desc &d, bool back)
 {
     const int64_t units = ceil_div(d.T, CHUNK) * d.N * d.H, wide = d.precision == HTS_PRECISION_BF16 ? 3072 : 2048, exact = d.precision == HTS_PRECISION_BF16 ? 1024 : 2048;
@@ -1506,7 +1523,8 @@ Layout layout(const hts_delta_rule_desc &d, bool back)
     l.read = l.inverse + units * 8 * wide;
     l.keys = l.read + units * 8 * wide;
     l.queries = l.keys + units * (keys_padded(d.K) / 8) * exact;
-    l.rows = l.queries + (back ? units * (keys_padded(d.K) / 8) * exact : 0);
+    l.pairs = l.queries + (back ? units * (keys_padded(d.K) / 8) * exact : 0);
+    l.rows = l.pairs + (back ? units * 2 * PAIRS * 1024 : 0);
     l.gates = l.rows + (d.K % 8 ? units * 2 * (keys_padded(d.K) / 8) * exact : 0);
     l.late = l.gates + round_up(units * (int64_t)sizeof(Gates), 256);
     l.write = l.late + (back ? units * keys_padded(d.K) * round_up(d.V, TILE) * 4 : 0);
@@ -1526,7 +1544,7 @@ DeltaArgs arguments(hts_seq_ctx &c, const DeltaOp &op, bool back)
     a.ends = (float *)(c.ws + l.ends); a.begins = (float *)(c.ws + l.begins);
     a.tiles = (int)ceil_div(op.d.V, TILE); a.VP = a.tiles * TILE;
     if (op.states) a.z = op.states + delta_state_floats(op.d);
-    a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates); a.rows = op.d.K % 8 ? c.ws + l.rows : nullptr;
+    a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates); a.pairs = (float *)(c.ws + l.pairs); a.rows = op.d.K % 8 ? c.ws + l.rows : nullptr;
     a.late = (float *)(c.ws + l.late); a.write = (float *)(c.ws + l.write); a.part = (float *)(c.ws + l.part); a.heads = (float *)(c.ws + l.heads);
     return a;
 }

@@ -103,6 +103,18 @@ template <typename T> __device__ __forceinline__ void put_wide4(char *p, int pla
         }
     }
 }
+// one number, the i-th of 8
+template <typename T> __device__ __forceinline__ void put_wide1(char *p, int plane, int i, float x)
+{
+    if constexpr (sizeof(T) == 4) *(float *)(p + (i >> 2) * plane + 4 * (i & 3)) = x;
+    else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            *(uint16_t *)(p + k * plane + 2 * i) = (uint16_t)(__float_as_uint(x) >> 16);
+            x -= cut8(x);
+        }
+    }
+}
 template <typename T> __device__ __forceinline__ Wide<T> make_wide(const float (&x)[8])
 {
     Wide<T> r;
@@ -188,6 +200,7 @@ struct DeltaArgs {
     hts_delta_rule_grads g;
     int chunks, tiles, VP;                        // tiles of the values; V in whole tiles (KP: K in whole fragments; zeros in what K, V and a sequence's end leave over)
     char *inverse, *inverse_t, *read, *keys, *queries;     // fragments of each chunk, sequence and head
+    float *pairs;                                 // [unit][20][64 lanes][4]: products of queries or keys that look back with keys, all of length one (and scaled), tiles on and below the diagonal
     char *rows;                                   // K no multiple of 8: keys [unit][64][KP], then queries, that rows are read from in eights
     Gates *gates;
     // long sequences of few heads, in segments of so many chunks that are worked on at the same time: what each makes of nothing and of a state of ones on the diagonal,
