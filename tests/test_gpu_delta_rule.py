@@ -264,6 +264,59 @@ def test_not_finite(hts, T):  # noqa: F811
     clean.ctx.close()
 
 
+def test_not_finite_in_segments(hts):  # noqa: F811
+    """A long sequence in segments: what one makes of the state before it is not multiplied by what is not finite where an episode begins in it."""
+    c = Case(hts, "f32", 900, 1, 1, 1, 16, 40, starts=0.5)
+    s = np.zeros((900, 1), dtype=np.uint8)
+    s[[0, 500, 700]] = 1
+    c.at["starts"] = torch.from_numpy(s).cuda()
+    c.at["h_in"][:] = float("inf")
+    base = c.run(False)
+    assert bool(base["y"].isfinite().all()) and bool(base["h_out"].isfinite().all())
+    for name in ("v", "k", "a"):
+        kept = c.at[name].clone()
+        c.at[name][130] = float("nan")
+        got = c.run(False)
+        c.at[name].copy_(kept)
+        assert bool(got["y"][:130].isfinite().all()) and bool(got["y"][130:500].isnan().all()) and bool(got["y"][500:].isfinite().all()), name
+        assert np.allclose(host(got["y"][500:]), host(base["y"][500:]), atol=1e-5) and bool(got["h_out"].isfinite().all())
+    s[0] = 0
+    c.at["starts"] = torch.from_numpy(s).cuda()
+    got = c.run(False)
+    assert not bool(got["y"][:500].isfinite().any()) and bool(got["y"][500:].isfinite().all())
+    c.ctx.close()
+
+
+def test_streams_of_some_units(hts):  # noqa: F811
+    """The same bits on a range of compute units, in segments and not."""
+    for T, N in ((900, 1), (100, 3)):
+        c = Case(hts, "bf16", T, N, 1, 2, 32, 32)
+        want = c.run()
+        part = hts.CuRangeStream(0, 64)
+        ctx = hts.SeqContext(hts.delta_rule_workspace(T, N, 2, 1, 32, 32, precision=hts.PRECISION_BF16), stream=part.stream)
+        torch.cuda.synchronize()
+        got = c.run(ctx=ctx)
+        assert all(torch.equal(want[n], got[n]) for n in want)
+        ctx.close()
+        part.close()
+        c.ctx.close()
+
+
+def test_one_row_for_all_and_far_apart(hts):  # noqa: F811
+    """Strides of nothing (the same queries, keys and gates at every step of every sequence), and sequences that lie between another array's."""
+    T, N, G, H, K, V = 70, 3, 1, 2, 24, 20
+    c = Case(hts, "f32", T, N, G, H, K, V)
+    for name in ("q", "k", "a", "b"):
+        one = c.at[name][:1, :1].clone()
+        c.at[name] = one.expand(T, N, *one.shape[2:])
+        c.wide[name] = c.at[name].double().cpu().numpy()
+    by_sequence = torch.randn(N, T, 2, H, V, device="cuda")
+    c.at["v"] = by_sequence[:, :, 1].transpose(0, 1)
+    c.wide["v"] = c.at["v"].double().cpu().numpy()
+    c.check()
+    c.ctx.close()
+
+
 def test_bits(hts):  # noqa: F811
     """The same bits again, in a context with more workspace than needed, and whatever the workspace held."""
     c = Case(hts, "bf16", 150, 2, 1, 2, 64, 64, starts=0.05)
