@@ -389,7 +389,7 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[m][nt][r] = ones && 16 * (wave * MT + m) + 4 * quad + r == v0 + 16 * nt + col ? 1.0f : 0.0f;
-    } else if (segment > 0) {
+    } else if (a.segments > 1) {                             // (the first one's too: the last one may be writing h_out into h_in's place by now)
         if (has_keys)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -630,6 +630,15 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void begin_kerne
     constexpr int MT = key_tiles<KP>();
     const bool has_keys = wave * MT * 16 < KP;
     f32x4 S[MT][2] = {};
+    const auto put_begin = [&](int64_t place) {
+        if (has_keys)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) a.begins[(place * KP + 16 * (wave * MT + m) + 4 * quad + r) * VP + v0 + 16 * nt + col] = S[m][nt][r];
+    };
     if (has_keys && a.in.h_in)
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -640,6 +649,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void begin_kerne
                     const int k = 16 * (wave * MT + m) + 4 * quad + r, v = v0 + 16 * nt + col;
                     if (k < d.K && v < d.V) S[m][nt][r] = a.in.h_in[(((int64_t)n * d.H + h) * d.K + k) * d.V + v];
                 }
+    put_begin((int64_t)n * d.H + h);
     for (int s = 0; s + 1 < a.segments && (s + 1) * a.per_segment < chunks; ++s) {
         const int64_t place = ((int64_t)s * d.N + n) * d.H + h;
         float move[KP / 32][MT][8];
@@ -672,13 +682,7 @@ template <typename T, int KP> __global__ __launch_bounds__(256) void begin_kerne
 #pragma unroll
                     for (int nt = 0; nt < 2; ++nt) mma(S[m][nt], moved, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * k + quad) * N_::WIDE, 16));
                 }
-        if (has_keys)
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) a.begins[((place + (int64_t)d.N * d.H) * KP + 16 * (wave * MT + m) + 4 * quad + r) * VP + v0 + 16 * nt + col] = S[m][nt][r];
+        put_begin(place + (int64_t)d.N * d.H);
         __syncthreads();
     }
 }

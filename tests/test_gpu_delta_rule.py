@@ -111,6 +111,12 @@ def test_long(hts, dtype, T, N, G, H, K, V, starts):  # noqa: F811
         for name in got:
             so.near(host(got[name]), want[name], off[name] / so.U, 1, HALF["f32" if got[name].dtype is torch.float32 else dtype], name)
         assert torch.equal(got["y"], plain["y"]) and torch.equal(got["h_out"], plain["h_out"])
+        # ... and the state at the end in the place of the one at the beginning, which every segment's is made of
+        state, y = c.at["h_in"].clone(), torch.empty(T, N, H, V, dtype=c.ty, device="cuda")
+        at = c.at
+        c.ctx.hts_delta_rule(*(at[n] for n in ("q", "k", "v", "a", "b", "A")), y, a_bias=at["a_bias"], starts=at["starts"], lengths=at["lengths"], h_in=state, h_out=state, **c.more)
+        torch.cuda.synchronize()
+        assert torch.equal(got["y"], y) and torch.equal(got["h_out"], state)
         c.ctx.close()
 
 
