@@ -768,8 +768,10 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
 #pragma unroll
             for (int w = 0; w < 2; ++w) __builtin_memcpy(&sums[wave][w][4 * four], has[w], 16);
         __syncthreads();
-        const float k_unit = d.normalize ? 1.0f / __builtin_sqrtf(lengths[0][0] + lengths[1][0] + 1e-6f) : 1.0f;
-        const float q_unit = d.scale * (d.normalize ? 1.0f / __builtin_sqrtf(lengths[0][1] + lengths[1][1] + 1e-6f) : 1.0f);
+        // (a key or query whose square is not finite is none, also where its entries are)
+        const float k_square = lengths[0][0] + lengths[1][0], q_square = lengths[0][1] + lengths[1][1];
+        const float k_unit = !finite(k_square) ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(k_square + 1e-6f) : 1.0f;
+        const float q_unit = d.scale * (!finite(q_square) ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(q_square + 1e-6f) : 1.0f);
         const float along = (lengths[0][2] + lengths[1][2]) * k_unit;
         float u[4], y[4], z[4];
 #pragma unroll

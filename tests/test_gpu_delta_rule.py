@@ -270,6 +270,25 @@ def test_not_finite(hts, T):  # noqa: F811
     clean.ctx.close()
 
 
+@pytest.mark.parametrize("T", [1, 16, 20])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_squares_that_are_not_finite(hts, T, normalize):  # noqa: F811
+    """A key or query of finite entries whose square is beyond binary32 is none: the same of a few steps as of many."""
+    c = Case(hts, "bf16", T, 2, 1, 2, 16, 40, normalize=normalize)
+    for name in ("k", "q"):
+        kept = c.at[name].clone()
+        c.at[name][T // 2, 0] = 1e20
+        got = c.run()
+        c.at[name].copy_(kept)
+        assert bool(got["y"][:T // 2].isfinite().all()) and bool(got["y"][:, 1].isfinite().all()) and bool(got["h_out"][1].isfinite().all()), name
+        assert bool(got["y"][T // 2, 0].isnan().all()), name
+        if name == "k":
+            assert bool(got["y"][T // 2:, 0].isnan().all()) and bool(got["h_out"][0].isnan().all())
+        else:
+            assert bool(got["y"][T // 2 + 1:].isfinite().all()) and bool(got["h_out"].isfinite().all())
+    c.ctx.close()
+
+
 def test_not_finite_in_segments(hts):  # noqa: F811
     """A long sequence in segments: what one makes of the state before it is not multiplied by what is not finite where an episode begins in it."""
     c = Case(hts, "f32", 900, 1, 1, 1, 16, 40, starts=0.5)
