@@ -18,6 +18,7 @@ namespace hts {
 namespace {
 
 constexpr int TILE = 32;                  // the values' entries of a workgroup
+constexpr int ROOM = 256;                 // workgroups that segments are made for, and the most of them
 __host__ __device__ __forceinline__ int keys_padded(int K) { return K <= 32 ? 32 : K <= 64 ? 64 : 128; }
 
 // sums over as many neighbouring lanes as a row of eights has
@@ -616,74 +617,74 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
 }
 
 // The states that the segments begin with: from one to the next, what its steps make of the state before it and what they add.  A segment in which an episode begins leaves
-// nothing of it (not 0 times it, which would be NaN of what is not finite).
-template <typename T, int KP> __global__ __launch_bounds__(256) void begin_kernel(const DeltaArgs a)
+// nothing of it (not 0 times it, which would be NaN of what is not finite).  A step's latency is all that counts: a wavefront for 16 of the keys' entries (with two such parts
+// each a prompt of 8192 and 8 heads of 128 keys took 31 us, and 35 with operands requested where they are used; now 25, seven steps).
+template <typename T, int KP> __global__ __launch_bounds__(4 * KP) void begin_kernel(const DeltaArgs a)
 {
     typedef RunLds<T, KP> L;
     typedef Num<T> N_;
     __shared__ __attribute__((aligned(16))) char state[TILE * L::STATE_PITCH];
+    __shared__ int forgets[ROOM];
     const hts_delta_rule_desc &d = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
     const Part at = part_of(a, a.tiles);
     if (at.n >= d.N) return;
-    const int h = at.h, n = at.n, v0 = at.tile * TILE, VP = a.VP, width = VP + KP, chunks = (length_of(a, n) + CHUNK - 1) / CHUNK;
-    constexpr int MT = key_tiles<KP>();
-    const bool has_keys = wave * MT * 16 < KP;
-    f32x4 S[MT][2] = {};
-    const auto put_begin = [&](int64_t place) {
-        if (has_keys)
+    const int h = at.h, n = at.n, v0 = at.tile * TILE, VP = a.VP, width = VP + KP, chunks = (length_of(a, n) + CHUNK - 1) / CHUNK, row = 16 * wave + 4 * quad;
+    f32x4 S[2] = {};
+    if (a.in.h_in)
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+        for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
+            for (int r = 0; r < 4; ++r) {
+                const int k = row + r, v = v0 + 16 * nt + col;
+                if (k < d.K && v < d.V) S[nt][r] = a.in.h_in[(((int64_t)n * d.H + h) * d.K + k) * d.V + v];
+            }
+    const auto place_of = [&](int s) { return (((int64_t)s * d.N + n) * d.H + h) * KP; };
+    const auto put_begin = [&](int s) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) a.begins[(place * KP + 16 * (wave * MT + m) + 4 * quad + r) * VP + v0 + 16 * nt + col] = S[m][nt][r];
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) a.begins[(place_of(s) + row + r) * VP + v0 + 16 * nt + col] = S[nt][r];
     };
-    if (has_keys && a.in.h_in)
+    put_begin(0);
+    // a segment's operands arrive while the one before it is worked on
+    float next_move[KP / 32][8], next_own[2][4];
+    const auto more = [&](int s) { return s + 1 < a.segments && (s + 1) * a.per_segment < chunks; };
+    const auto load = [&](int s) {
+        const float *from = a.ends + (place_of(s) + 16 * wave) * width;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int k = 0; k < KP / 32; ++k) __builtin_memcpy(next_move[k], __builtin_assume_aligned(from + (int64_t)col * width + VP + 32 * k + 8 * quad, 16), 32);
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+        for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int k = 16 * (wave * MT + m) + 4 * quad + r, v = v0 + 16 * nt + col;
-                    if (k < d.K && v < d.V) S[m][nt][r] = a.in.h_in[(((int64_t)n * d.H + h) * d.K + k) * d.V + v];
-                }
-    put_begin((int64_t)n * d.H + h);
-    for (int s = 0; s + 1 < a.segments && (s + 1) * a.per_segment < chunks; ++s) {
-        const int64_t place = ((int64_t)s * d.N + n) * d.H + h;
-        float move[KP / 32][MT][8];
-        if (has_keys)
+            for (int r = 0; r < 4; ++r) next_own[nt][r] = from[(int64_t)(4 * quad + r) * width + v0 + 16 * nt + col];
+    };
+    if (more(0)) load(0);
+    for (int i = tid; i < ROOM; i += 4 * KP) forgets[i] = 0;
+    lds_barrier();
+    for (int c = tid; c < chunks; c += 4 * KP)
+        if (a.gates[((int64_t)c * d.N + n) * d.H + h].keep[CHUNK - 1] < 0.0f) forgets[c / a.per_segment] = 1;
+    for (int s = 0; more(s); ++s) {
+        float move[KP / 32][8];
 #pragma unroll
-            for (int k = 0; k < KP / 32; ++k)
+        for (int nt = 0; nt < 2; ++nt) {
+            const float x[4] = {S[nt][0], S[nt][1], S[nt][2], S[nt][3]};
+            put_wide4<T>(state + (16 * nt + col) * L::STATE_PITCH + (2 * wave + (quad >> 1)) * N_::WIDE, 16, quad & 1, x);
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-                    __builtin_memcpy(move[k][m], __builtin_assume_aligned(a.ends + (place * KP + 16 * (wave * MT + m) + col) * width + VP + 32 * k + 8 * quad, 16), 32);
-        bool passes = true;
-        for (int c = lane; c < a.per_segment; c += 64) passes = passes && a.gates[((int64_t)(s * a.per_segment + c) * d.N + n) * d.H + h].keep[CHUNK - 1] >= 0.0f;
-        passes = __all(passes);
-        if (has_keys)
+            for (int r = 0; r < 4; ++r) S[nt][r] = next_own[nt][r];
+        }
+        __builtin_memcpy(move, next_move, sizeof move);
+        if (more(s + 1)) load(s + 1);
+        lds_barrier();
+        if (!forgets[s])
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int k = 0; k < KP / 32; ++k) {
+                const Wide<T> moved = make_wide<T>(move[k]);
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    const float x[4] = {S[m][nt][0], S[m][nt][1], S[m][nt][2], S[m][nt][3]};
-                    put_wide4<T>(state + (16 * nt + col) * L::STATE_PITCH + (2 * (wave * MT + m) + (quad >> 1)) * N_::WIDE, 16, quad & 1, x);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) S[m][nt][r] = a.ends[(place * KP + 16 * (wave * MT + m) + 4 * quad + r) * width + v0 + 16 * nt + col];
-                }
-        __syncthreads();
-        if (has_keys && passes)
-#pragma unroll
-            for (int k = 0; k < KP / 32; ++k)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const Wide<T> moved = make_wide<T>(move[k][m]);
-#pragma unroll
-                    for (int nt = 0; nt < 2; ++nt) mma(S[m][nt], moved, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * k + quad) * N_::WIDE, 16));
-                }
-        put_begin(place + (int64_t)d.N * d.H);
-        __syncthreads();
+                for (int nt = 0; nt < 2; ++nt) mma(S[nt], moved, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * k + quad) * N_::WIDE, 16));
+            }
+        put_begin(s + 1);
+        lds_barrier();
     }
 }
 
@@ -1500,7 +1501,6 @@ constexpr int MOST_STEPS = 16;            // calls of so many steps or fewer go 
 // Segments: as many as a device of 256 units has room for beside each other, of 4 chunks or more, where there are three of them at least (with two the passes over the segments'
 // ends cost what they save).  The same on every device and range of units: results do not depend on where they are computed.
 struct Segments { int count, chunks; };
-constexpr int ROOM = 256;
 Segments segments_of(const hts_delta_rule_desc &d)
 {
     const int64_t chunks = ceil_div(d.T, CHUNK), groups = (int64_t)d.N * d.H * ceil_div(d.V, TILE);
@@ -1575,7 +1575,7 @@ template <typename T> hipError_t forward(hts_seq_ctx &c, const DeltaOp &op)
         hipError_t e = launch(prep_kernel<T, KP, false>, (int64_t)a.chunks * d.N * d.H, PrepLds<T, KP>::BYTES, c.stream, a);
         if (e == hipSuccess && a.segments > 1) {
             e = launch(forward_kernel<T, KP, true>, parts(a, a.tiles + KP / TILE), RunLds<T, KP>::BYTES, c.stream, a, 256, a.segments - 1);
-            if (e == hipSuccess) e = launch(begin_kernel<T, KP>, parts(a, a.tiles), 0, c.stream, a);
+            if (e == hipSuccess) e = launch(begin_kernel<T, KP>, parts(a, a.tiles), 0, c.stream, a, 4 * KP);
         }
         return e != hipSuccess ? e : launch(forward_kernel<T, KP, false>, parts(a, a.tiles), RunLds<T, KP>::BYTES, c.stream, a, 256, a.segments);
     });
