@@ -1051,9 +1051,12 @@ template <typename T, int KP> __global__ __launch_bounds__(256, 2) void reverse_
 template <typename T, int KP> struct GradLds {
     typedef Num<T> N_;
     static constexpr int PITCH = N_::pitch(TILE), Y_PITCH = N_::exact_pitch(TILE), LINE = 68;
-    static constexpr int WRITES = 0, VALUES = WRITES + CHUNK * PITCH, GIVEN = VALUES + CHUNK * PITCH, STAGE = GIVEN + CHUNK * Y_PITCH;      // two of these, in turn
+    // a tile's 16 rows are fours of every eight: with 64 bytes more between sixteens they begin in 16 places of four banks, without in 8
+    static __device__ __forceinline__ int row_of(int row, int pitch) { return row * pitch + (row >> 4) * 64; }
+    static constexpr int MORE = CHUNK / 16 * 64;
+    static constexpr int WRITES = 0, VALUES = WRITES + CHUNK * PITCH + MORE, GIVEN = VALUES + CHUNK * PITCH + MORE, STAGE = GIVEN + CHUNK * Y_PITCH + MORE;      // two of these, in turn
     // after the values: a matrix of 64 x 64, what passes from step to step; at last the rows that leave
-    static constexpr int MATRIX = 0, MATRIX_PITCH = N_::pitch(CHUNK), PASSING = MATRIX + CHUNK * MATRIX_PITCH, AFTER = PASSING + 4 * CHUNK * LINE;
+    static constexpr int MATRIX = 0, MATRIX_PITCH = N_::pitch(CHUNK), PASSING = MATRIX + CHUNK * MATRIX_PITCH + MORE, AFTER = PASSING + 4 * CHUNK * LINE;
     static constexpr int OUT_PITCH = KP * (int)sizeof(T) + 16, OUT = 2 * CHUNK * OUT_PITCH;
     static constexpr int AREA = (2 * STAGE > AFTER ? 2 * STAGE : AFTER) > OUT ? (2 * STAGE > AFTER ? 2 * STAGE : AFTER) : OUT;
     static constexpr int ROWS = AREA, SUMS = ROWS + 4 * 2 * 8 * CHUNK, GATES = SUMS + 4 * (5 * CHUNK + 8), BYTES = GATES + (int)sizeof(Gates);
@@ -1117,7 +1120,7 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
     f32x4 q_state[IT] = {}, k_late[IT] = {}, k_state[IT] = {};
     float z_dv = 0.0f, end = 0.0f;
     const float my_strength = a.gates[unit].strength[my_row];
-    float z[4], g[4], s8[8], l8[8];
+    float z[4], g[4], s8[8], l8[8], next_s[8], next_l[8];
     T y[4];
     const bool whole = t0 + CHUNK <= len;
     const uint32_t my_at = row_at<float>(my_row, a.VP, 4 * my_part), my_y = row_at<T>(my_row, a.dy.st, 4 * my_part), my_dv = row_at<T>(my_row, a.g.dv.st, 4 * my_part);
@@ -1125,24 +1128,30 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
     const auto load = [&](int v0) {
         __builtin_memcpy(z, (const char *)(a.z + unit * CHUNK * a.VP + v0) + my_at, 16);
         __builtin_memcpy(g, (const char *)(a.write + unit * CHUNK * a.VP + v0) + my_at, 16);
-        __builtin_memcpy(s8, (const char *)(a.states + unit * KP * a.VP + v0) + state_at, 32);
-        __builtin_memcpy(l8, (const char *)(a.late + unit * KP * a.VP + v0) + state_at, 32);
         if (whole && v0 + TILE <= V) __builtin_memcpy(y, (const char *)(step_of<T>(a.dy, t0, n) + (int64_t)h * V + v0) + my_y, sizeof y);
         else row4(y, my_live ? step_of<T>(a.dy, t0 + my_row, n) + (int64_t)h * V : nullptr, v0 + 4 * my_part, V);
     };
+    const auto load_states = [&](int v0) {
+        __builtin_memcpy(next_s, (const char *)(a.states + unit * KP * a.VP + v0) + state_at, 32);
+        __builtin_memcpy(next_l, (const char *)(a.late + unit * KP * a.VP + v0) + state_at, 32);
+    };
     const auto fragment = [&](const char *base, int s) { return get_exact<T>(base + (unit * (KP / 8) + kt * 2 + s) * N_::EXACT_FRAGMENT + lane * 16, 1024); };
     f32x4 pass[4] = {};
+    // the states, most of what is read, come two tiles ahead, the rest one (there are no registers for more, nor, meanwhile, for what the products after the loop take)
+    load_states(0);
+    __builtin_memcpy(s8, next_s, 32); __builtin_memcpy(l8, next_l, 32);
     load(0);
+    if (TILE < V) load_states(TILE);
     for (int v0 = 0, turn = 0; v0 < V; v0 += TILE, turn ^= 1) {
         char *writes = lds + turn * L::STAGE + L::WRITES, *values = lds + turn * L::STAGE + L::VALUES, *given = lds + turn * L::STAGE + L::GIVEN;
         {
-            const int p = my_row * L::PITCH + (my_part >> 1) * N_::WIDE;
+            const int p = L::row_of(my_row, L::PITCH) + (my_part >> 1) * N_::WIDE;
             float u[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) { z_dv = __builtin_fmaf(z[i], g[i], z_dv); u[i] = sign * my_strength * z[i]; }
             put_wide4<T>(writes + p, 16, my_part & 1, u);
             put_wide4<T>(values + p, 16, my_part & 1, g);
-            __builtin_memcpy(given + my_row * L::Y_PITCH + 4 * my_part * sizeof(T), y, sizeof y);
+            __builtin_memcpy(given + L::row_of(my_row, L::Y_PITCH) + 4 * my_part * sizeof(T), y, sizeof y);
             if (whole && v0 + TILE <= V) {
                 Four<T> o;
 #pragma unroll
@@ -1156,32 +1165,32 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
 #pragma unroll
         for (int i = 0; i < 8; ++i) { end = __builtin_fmaf(s8[i], l8[i], end); s8[i] *= sign; }
         const Wide<T> sf = make_wide<T>(s8), lf = make_wide<T>(l8);
+        __builtin_memcpy(s8, next_s, 32); __builtin_memcpy(l8, next_l, 32);
         if (v0 + TILE < V) load(v0 + TILE);
-        else {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) { kf[s] = fragment(a.keys, s); qf[s] = fragment(a.queries, s); }
-#pragma unroll
-            for (int jt = 0; jt < 4; ++jt)
-                if (jt <= ti) pass[jt] = load_at<f32x4>(a.pairs + ((unit * 2 + by_values) * PAIRS + pair_of(ti, jt)) * 256, lane * 16);
-        }
+        if (v0 + 2 * TILE < V) load_states(v0 + 2 * TILE);
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < IT; ++t) {
             const int row = tile_row(first_tile + t, col);
-            mma(q_state[t], get_exact<T>(given + row * L::Y_PITCH + quad * N_::EXACT, 16), sf);
-            mma(k_state[t], get_wide<T>(values + row * L::PITCH + quad * N_::WIDE, 16), sf);
-            mma(k_late[t], get_wide<T>(writes + row * L::PITCH + quad * N_::WIDE, 16), lf);
+            mma(q_state[t], get_exact<T>(given + L::row_of(row, L::Y_PITCH) + quad * N_::EXACT, 16), sf);
+            mma(k_state[t], get_wide<T>(values + L::row_of(row, L::PITCH) + quad * N_::WIDE, 16), sf);
+            mma(k_late[t], get_wide<T>(writes + L::row_of(row, L::PITCH) + quad * N_::WIDE, 16), lf);
         }
-        const Exact<T> yf = get_exact<T>(given + (16 * ti + col) * L::Y_PITCH + quad * N_::EXACT, 16);
-        const Wide<T> gf = get_wide<T>(values + (16 * ti + col) * L::PITCH + quad * N_::WIDE, 16);
+        const Exact<T> yf = get_exact<T>(given + L::row_of(16 * ti + col, L::Y_PITCH) + quad * N_::EXACT, 16);
+        const Wide<T> gf = get_wide<T>(values + L::row_of(16 * ti + col, L::PITCH) + quad * N_::WIDE, 16);
 #pragma unroll
         for (int jt = 0; jt < 4; ++jt)
             if (jt <= ti) {
-                const Wide<T> u = get_wide<T>(writes + (16 * jt + col) * L::PITCH + quad * N_::WIDE, 16);
+                const Wide<T> u = get_wide<T>(writes + L::row_of(16 * jt + col, L::PITCH) + quad * N_::WIDE, 16);
                 if (by_values) mma(by_step[jt], gf, u);
                 else mma(by_step[jt], yf, u);
             }
     }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) { kf[s] = fragment(a.keys, s); qf[s] = fragment(a.queries, s); }
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt)
+        if (jt <= ti) pass[jt] = load_at<f32x4>(a.pairs + ((unit * 2 + by_values) * PAIRS + pair_of(ti, jt)) * 256, lane * 16);
     // sums along the keys of what goes through the state before the chunk, and through the one at its end
 #pragma unroll
     for (int t = 0; t < IT; ++t) {
@@ -1240,10 +1249,10 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
 #pragma unroll
         for (int t = 0; t < IT; ++t)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) mma(out[t], get_wide<T>(matrix + tile_row(first_tile + t, col) * L::MATRIX_PITCH + (4 * s + quad) * N_::WIDE, 16), f[s]);
+            for (int s = 0; s < 2; ++s) mma(out[t], get_wide<T>(matrix + L::row_of(tile_row(first_tile + t, col), L::MATRIX_PITCH) + (4 * s + quad) * N_::WIDE, 16), f[s]);
     };
-    const auto put_matrix = [&](int r, int at, const float (&x)[4]) { put_wide4<T>(matrix + r * L::MATRIX_PITCH + (at >> 3) * N_::WIDE, 16, (at >> 2) & 1, x); };
-    const auto put_one = [&](int r, int at, float x) { put_wide1<T>(matrix + r * L::MATRIX_PITCH + (at >> 3) * N_::WIDE, 16, at & 7, x); };
+    const auto put_matrix = [&](int r, int at, const float (&x)[4]) { put_wide4<T>(matrix + L::row_of(r, L::MATRIX_PITCH) + (at >> 3) * N_::WIDE, 16, (at >> 2) & 1, x); };
+    const auto put_one = [&](int r, int at, float x) { put_wide1<T>(matrix + L::row_of(r, L::MATRIX_PITCH) + (at >> 3) * N_::WIDE, 16, at & 7, x); };
     const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     __syncthreads();
     // dQ: rows are the steps that look back
