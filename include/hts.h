@@ -407,6 +407,7 @@ typedef struct {
     const int32_t *lengths;
     const float *h_in;
 } hts_delta_rule_inputs;
+/* (enough for fewer steps and fewer sequences too) */
 int64_t hts_delta_rule_workspace(const hts_delta_rule_desc *desc);
 int64_t hts_delta_rule_states(const hts_delta_rule_desc *desc);
 int32_t hts_delta_rule(hts_seq_ctx *ctx, const hts_delta_rule_desc *desc, const hts_delta_rule_inputs *in, hts_steps y, float *h_out,

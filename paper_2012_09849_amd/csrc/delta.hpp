@@ -41,8 +41,8 @@ __device__ __forceinline__ void mma(f32x4 &c, const Exact<float> &a, const Wide<
 __device__ __forceinline__ void mma(f32x4 &c, const Wide<float> &a, const Exact<float> &b) { mma_f32(c, a, b); }
 __device__ __forceinline__ void mma(f32x4 &c, const Wide<float> &a, const Wide<float> &b) { mma_f32(c, a, b); }
 __device__ __forceinline__ void mma(f32x4 &c, const Exact<bf16_t> &a, const Exact<bf16_t> &b) { mma1(c, a.v, b.v); }
-// Added to C when they are together, smallest parts first: the instruction drops what lies below C's last digits towards minus infinity (by a few guard digits; 1.4% of
-// a last digit on average where products are 2^-15 of C, measured), which a sum over thousands of steps adds up: dA 2.3e-6 of its values off, now 4e-7.
+// Smallest parts first.  (The instruction drops what lies below C's last digits towards minus infinity, by a few guard digits: 1.4% of a last digit on average where
+// products are 2^-15 of C, measured.  Where sums over thousands of steps would add that up, every second chunk has the other sign.)
 __device__ __forceinline__ void mma(f32x4 &c, const Exact<bf16_t> &a, const Wide<bf16_t> &b)
 {
     mma1(c, a.v, b.p[2]); mma1(c, a.v, b.p[1]); mma1(c, a.v, b.p[0]);
