@@ -101,6 +101,15 @@ def test_values_and_gradients(hts, dtype, T, N, G, H, K, V, pad, shift, starts):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,G,H,K,V", [(70, 1, 1, 1, 16, 1100), (20, 1000, 1, 1, 8, 8), (3, 3000, 1, 2, 4, 4), (66, 2, 1, 40, 12, 8)])
+def test_many(hts, dtype, T, N, G, H, K, V):  # noqa: F811
+    """Many tiles of values, many sequences, many heads of one group."""
+    c = Case(hts, dtype, T, N, G, H, K, V, starts=0.05)
+    c.check()
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,N,G,H,K,V,starts", [(800, 1, 1, 1, 16, 24, 0.0), (1100, 2, 1, 2, 40, 40, 0.002), (1600, 1, 1, 1, 128, 128, 0.0), (900, 1, 1, 1, 64, 33, 0.01)])
 def test_long(hts, dtype, T, N, G, H, K, V, starts):  # noqa: F811
     """Long sequences of few heads are worked on in segments at the same time: sequences that end in the first one, in a later one and at one's end among them; states of chunks."""
