@@ -696,17 +696,51 @@ template <typename T, int KP> __global__ __launch_bounds__(4 * KP) void begin_ke
 }
 
 // A few steps: the state in registers, 64 of the values' entries a workgroup, 4 to a thread, every 16th of the keys'.  One sum over the keys a step: of the state before it
-// with the key and with the query, y = scale (al q . S + (q . k) be z).  A step reads and writes the state once: 32 rows of 8 heads of 128 x 128 12.5 us, 33.5 MB (2.7 TB/s; all of it is on its
-// way at once, in and then out).  Five steps of 16 rows of 4 heads of 64 x 64 14.5: two barriers and a reduction a step.
+// with the key and with the query, y = scale (al q . S + (q . k) be z).  A step reads and writes the state once: 32 rows of 8 heads of 128 x 128 11.7 us, 33.5 MB (2.9 TB/s; all of it is on its
+// way at once, in and then out).  Five steps of 16 rows of 4 heads of 64 x 64 10.5: a reduction
+// and a barrier a step (14.6 with each step's gates and lengths made in it, of which the exponentials are most).
+// Calls of so many steps or fewer go step by step: 16 steps of 32 x 8 heads of 128 x 128 in bf16 31 us, in a chunk 40; of 1 x 8 heads 26 and 26; of 16 x 4 heads of 64 x 64 in binary32
+// 23 and 24.  (24 steps of the smaller ones would cost more than a chunk.)
+constexpr int MOST_STEPS = 16;
 constexpr int STEP_TILE = 64, STEP_ROWS = 8;
 template <typename T> __global__ __launch_bounds__(256) void step_kernel(const DeltaArgs a)
 {
     const hts_delta_rule_desc &d = a.d;
-    __shared__ float kq[2][128], lengths[2][4], sums[4][2][STEP_TILE];
-    const int tid = threadIdx.x, wave = tid >> 6, four = tid & 15, rg = tid >> 4;
+    // what the steps have by themselves is made for all of them before the first one: keys and queries, [16 m + r] at 8 r + m; what a step takes of each
+    struct Step { float decay, strength, k_unit, q_unit, along; int reset; };
+    __shared__ __attribute__((aligned(16))) float kq[MOST_STEPS][2][128], sums[2][4][2][STEP_TILE];
+    __shared__ Step steps[MOST_STEPS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, four = tid & 15, rg = tid >> 4;
     const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % d.H, n = blockIdx.x / a.tiles / d.H;
     const int K = d.K, V = d.V, v0 = tile * STEP_TILE + 4 * four, group = h / (d.H / d.G), len = length_of(a, n), count = V - v0;
     const int64_t held = ((int64_t)n * d.H + h) * K * V;
+    // a wavefront for every fourth step's key and query, lanes of the last one for the gates; the state arrives meanwhile
+    T k_in[MOST_STEPS / 4][2], q_in[MOST_STEPS / 4][2], a_in = from_f32<T>(0.0f), b_in = a_in, v_in[4];
+    uint8_t start = 0;
+#pragma unroll
+    for (int i = 0; i < MOST_STEPS / 4; ++i) {
+        const int t = 4 * i + wave;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const bool there = t < len && lane + 64 * e < K;
+            k_in[i][e] = there ? step_of<T>(a.in.k, t, n)[(int64_t)group * K + lane + 64 * e] : from_f32<T>(0.0f);
+            q_in[i][e] = there ? step_of<T>(a.in.q, t, n)[(int64_t)group * K + lane + 64 * e] : from_f32<T>(0.0f);
+        }
+    }
+    const bool gated = wave == 3 && lane < len;
+    if (gated) {
+        a_in = step_of<T>(a.in.a, lane, n)[h];
+        b_in = step_of<T>(a.in.b, lane, n)[h];
+        if (a.in.starts) start = a.in.starts[(int64_t)lane * d.N + n];
+    }
+    const auto load_values = [&](int t) {
+        const T *v = step_of<T>(a.in.v, t, n) + (int64_t)h * V + v0;
+        if (count >= 4) __builtin_memcpy(v_in, v, sizeof v_in);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v_in[i] = i < count ? v[i] : from_f32<T>(0.0f);
+    };
+    if (len > 0) load_values(0);
     float S[STEP_ROWS][4];
 #pragma unroll
     for (int m = 0; m < STEP_ROWS; ++m) {
@@ -721,6 +755,32 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
                 for (int i = 0; i < 4; ++i) if (i < count) S[m][i] = p[i];
         }
     }
+#pragma unroll
+    for (int i = 0; i < MOST_STEPS / 4; ++i) {
+        const int t = 4 * i + wave;
+        if (t >= len) break;
+        float k_square = 0.0f, q_square = 0.0f, both = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float kv = to_f32(k_in[i][e]), qv = to_f32(q_in[i][e]);
+            const int at = 8 * (lane & 15) + (lane >> 4) + 4 * e;
+            kq[t][0][at] = kv; kq[t][1][at] = qv;
+            k_square = __builtin_fmaf(kv, kv, k_square); q_square = __builtin_fmaf(qv, qv, q_square); both = __builtin_fmaf(qv, kv, both);
+        }
+        k_square = wave_add(k_square); q_square = wave_add(q_square); both = wave_add(both);
+        // (a key or query whose square is not finite is none, also where its entries are)
+        const float k_unit = !finite(k_square) ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(k_square + 1e-6f) : 1.0f;
+        const float q_unit = d.scale * (!finite(q_square) ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(q_square + 1e-6f) : 1.0f);
+        if (lane == 0) { steps[t].k_unit = k_unit; steps[t].q_unit = q_unit; steps[t].along = both * k_unit; }
+    }
+    if (gated) {
+        const Decay dc = decay_of(to_f32(a_in), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
+        const double e = (double)dc.exponent * LOG2E_64;
+        const bool reset = start || e < FORGETS;
+        steps[lane].reset = reset;
+        steps[lane].decay = reset ? 0.0f : e < MOST_EXPONENT ? exp2_wide(e) : __builtin_nanf("");
+        steps[lane].strength = sigmoid_f(to_f32(b_in));
+    }
     const auto put_state = [&](float *to, int keys, int values) {
 #pragma unroll
         for (int m = 0; m < STEP_ROWS; ++m) {
@@ -734,38 +794,29 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
         put_state(a.states + unit * keys_padded(K) * a.VP, keys_padded(K), a.VP);
         for (int t = len + rg; t < CHUNK; t += 16) store4(a.z + (unit * CHUNK + t) * a.VP + v0, none, a.VP - v0);
     }
+    lds_barrier();
     for (int t = 0; t < len; ++t) {
-        if (tid < 128) {
-            const float kv = tid < K ? to_f32(step_of<T>(a.in.k, t, n)[(int64_t)group * K + tid]) : 0.0f, qv = tid < K ? to_f32(step_of<T>(a.in.q, t, n)[(int64_t)group * K + tid]) : 0.0f;
-            kq[0][tid] = kv; kq[1][tid] = qv;
-            const float kk = wave_add(kv * kv), qq = wave_add(qv * qv), qk = wave_add(qv * kv);
-            if ((tid & 63) == 0) { lengths[wave][0] = kk; lengths[wave][1] = qq; lengths[wave][2] = qk; }
-        }
-        float val[4];
-        const T *v_row = step_of<T>(a.in.v, t, n) + (int64_t)h * V + v0;
+        const Step step = steps[t];
+        float val[4], kv[STEP_ROWS], qv[STEP_ROWS];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) val[i] = i < count ? to_f32(v_row[i]) : 0.0f;
-        const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
-        const double e = (double)dc.exponent * LOG2E_64;
-        const bool reset = (a.in.starts && a.in.starts[(int64_t)t * d.N + n]) || e < FORGETS;
-        const float decay = reset ? 0.0f : e < MOST_EXPONENT ? exp2_wide(e) : __builtin_nanf(""), strength = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
-        if (reset)
+        for (int i = 0; i < 4; ++i) val[i] = to_f32(v_in[i]);
+        if (t + 1 < len) load_values(t + 1);
+        __builtin_memcpy(kv, __builtin_assume_aligned(&kq[t][0][8 * rg], 16), sizeof kv);
+        __builtin_memcpy(qv, __builtin_assume_aligned(&kq[t][1][8 * rg], 16), sizeof qv);
+        if (step.reset)
 #pragma unroll
             for (int m = 0; m < STEP_ROWS; ++m)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) S[m][i] = 0.0f;
-        __syncthreads();
         float has[2][4] = {};
 #pragma unroll
-        for (int m = 0; m < STEP_ROWS; ++m) {
-            const float kv = kq[0][rg + 16 * m], qv = kq[1][rg + 16 * m];
+        for (int m = 0; m < STEP_ROWS; ++m)
             if (rg + 16 * m < K)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    has[0][i] = __builtin_fmaf(kv, S[m][i], has[0][i]);
-                    has[1][i] = __builtin_fmaf(qv, S[m][i], has[1][i]);
+                    has[0][i] = __builtin_fmaf(kv[m], S[m][i], has[0][i]);
+                    has[1][i] = __builtin_fmaf(qv[m], S[m][i], has[1][i]);
                 }
-        }
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -773,35 +824,30 @@ template <typename T> __global__ __launch_bounds__(256) void step_kernel(const D
                 has[w][i] += __shfl_xor(has[w][i], 16, 64);
                 has[w][i] += __shfl_xor(has[w][i], 32, 64);
             }
+        float (&all)[4][2][STEP_TILE] = sums[t & 1];             // (whoever reads those of the step before has not passed this step's barrier)
         if ((rg & 3) == 0)
 #pragma unroll
-            for (int w = 0; w < 2; ++w) __builtin_memcpy(&sums[wave][w][4 * four], has[w], 16);
-        __syncthreads();
-        // (a key or query whose square is not finite is none, also where its entries are)
-        const float k_square = lengths[0][0] + lengths[1][0], q_square = lengths[0][1] + lengths[1][1];
-        const float k_unit = !finite(k_square) ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(k_square + 1e-6f) : 1.0f;
-        const float q_unit = d.scale * (!finite(q_square) ? __builtin_nanf("") : d.normalize ? 1.0f / __builtin_sqrtf(q_square + 1e-6f) : 1.0f);
-        const float along = (lengths[0][2] + lengths[1][2]) * k_unit;
+            for (int w = 0; w < 2; ++w) __builtin_memcpy(&all[wave][w][4 * four], has[w], 16);
+        lds_barrier();
         float u[4], y[4], z[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float ks = (sums[0][0][4 * four + i] + sums[1][0][4 * four + i]) + (sums[2][0][4 * four + i] + sums[3][0][4 * four + i]);
-            const float qs = (sums[0][1][4 * four + i] + sums[1][1][4 * four + i]) + (sums[2][1][4 * four + i] + sums[3][1][4 * four + i]);
-            z[i] = reset ? val[i] : val[i] - decay * k_unit * ks;
-            u[i] = strength * z[i];
-            y[i] = q_unit * (reset ? along * u[i] : __builtin_fmaf(decay, qs, along * u[i]));
+            const float ks = (all[0][0][4 * four + i] + all[1][0][4 * four + i]) + (all[2][0][4 * four + i] + all[3][0][4 * four + i]);
+            const float qs = (all[0][1][4 * four + i] + all[1][1][4 * four + i]) + (all[2][1][4 * four + i] + all[3][1][4 * four + i]);
+            z[i] = step.reset ? val[i] : val[i] - step.decay * step.k_unit * ks;
+            u[i] = step.strength * z[i];
+            y[i] = step.q_unit * (step.reset ? step.along * u[i] : __builtin_fmaf(step.decay, qs, step.along * u[i]));
         }
 #pragma unroll
         for (int m = 0; m < STEP_ROWS; ++m) {
-            const float kv = kq[0][rg + 16 * m] * k_unit;
+            const float by = kv[m] * step.k_unit;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[m][i] = reset ? kv * u[i] : __builtin_fmaf(decay, S[m][i], kv * u[i]);
+            for (int i = 0; i < 4; ++i) S[m][i] = step.reset ? by * u[i] : __builtin_fmaf(step.decay, S[m][i], by * u[i]);
         }
         if (rg == 0) {
             store4(step_of<T>(a.y, t, n) + (int64_t)h * V + v0, y, count);
             if (a.z) store4(a.z + (unit * CHUNK + t) * a.VP + v0, z, a.VP - v0);
         }
-        __syncthreads();
     }
     if (a.h_out) put_state(a.h_out + held, K, V);
     if (rg == 0)
@@ -1518,7 +1564,6 @@ template <typename F> hipError_t by_keys(int K, F f)
     return f(std::integral_constant<int, 128>{});
 }
 
-constexpr int MOST_STEPS = 16;            // calls of so many steps or fewer go step by step
 
 // Segments: as many as a device of 256 units has room for beside each other, of 4 chunks or more, where there are three of them at least (with two the passes over the segments'
 // ends cost what they save).  The same on every device and range of units: results do not depend on where they are computed.
