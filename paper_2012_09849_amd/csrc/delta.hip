@@ -156,59 +156,48 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
     }
     __syncthreads();
 
-    // M diag(be) below the diagonal; Q K^T G.  Wavefront w has rows 16 w .. of the steps that look back
+    // M diag(be) below the diagonal; Q K^T G
     {
-        float far_unit[4];
-        double far_i[4];
-        int ep_i[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * wave + 4 * quad + r;
-            far_i[r] = far[i]; ep_i[r] = episode[i]; far_unit[r] = k_unit[i];
-        }
-        for (int jt = 0; jt < 4; ++jt) {
+        // A wavefront takes three of the ten tiles on and below the diagonal and of the two above it that fragments reach over.  i looks back at m: results are handed on along the
+        // steps that are looked at (forward) or that look back (back).
+        for (int tile = wave; tile < PAIRS + 2; tile += 4) {
+            const int it = tile < 4 ? 3 : tile < 7 ? 2 : tile < 9 ? 1 : tile < 11 ? 0 : 2, jt = tile < 4 ? tile : tile < 7 ? tile - 4 : tile < 9 ? tile - 7 : tile == 9 ? 0 : tile == 10 ? 1 : 3;
             f32x4 kk = {0.0f, 0.0f, 0.0f, 0.0f}, qk = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (jt <= wave)
+            if (jt <= it)
 #pragma unroll
                 for (int s = 0; s < KP / 32; ++s) {
                     const int at = (4 * s + quad) * N_::EXACT;
-                    const Exact<T> ki = get_exact<T>(keys + (16 * wave + col) * L::PITCH + at, 16), kj = get_exact<T>(keys + (16 * jt + col) * L::PITCH + at, 16);
-                    const Exact<T> qi = get_exact<T>(queries + (16 * wave + col) * L::PITCH + at, 16);
-                    mma(kk, ki, kj);
-                    if constexpr (BACK) mma(qk, qi, kj);       // rows of steps that look back: handed on along them
-                    else mma(qk, kj, qi);                      // ... along the steps that they look at
+                    const Exact<T> ki = get_exact<T>(keys + (16 * it + col) * L::PITCH + at, 16), kj = get_exact<T>(keys + (16 * jt + col) * L::PITCH + at, 16);
+                    const Exact<T> qi = get_exact<T>(queries + (16 * it + col) * L::PITCH + at, 16);
+                    if constexpr (BACK) { mma(kk, ki, kj); mma(qk, qi, kj); }
+                    else { mma(kk, kj, ki); mma(qk, kj, qi); }
                 }
-            const int j = 16 * jt + col;
+            float p[4];
+            Four<float> by_q, by_k;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * wave + 4 * quad + r;
+                const int i = BACK ? 16 * it + 4 * quad + r : 16 * it + col, m = BACK ? 16 * jt + col : 16 * jt + 4 * quad + r;
+                const bool sees = m <= i && episode[m] == episode[i];
                 float x = 0.0f;
-                if (j < i && episode[j] == ep_i[r]) {
-                    x = kk[r] * (far_unit[r] * k_unit[j]) * exp2_wide(far_i[r] - far[j]) * strength[j];
+                p[r] = 0.0f;
+                by_q.e[r] = qk[r] * (q_unit[i] * d.scale * k_unit[m]);
+                by_k.e[r] = kk[r] * (k_unit[i] * k_unit[m]);
+                if (sees) {
+                    const float decay = exp2_wide(far[i] - far[m]);
+                    p[r] = by_q.e[r] * decay;
+                    if (m < i) x = by_k.e[r] * decay * strength[m];
                     if (!finite(x)) { atomicOr(&bad[i >> 5], 1u << (i & 31)); x = 0.0f; }
                 }
-                below[i * L::LINE + j] = x;
+                if (jt <= it) below[i * L::LINE + m] = x;
             }
             if constexpr (BACK)
-                if (jt <= wave) {
-                    Four<float> by_q, by_k;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        by_q.e[r] = qk[r] * (q_unit[16 * wave + 4 * quad + r] * d.scale * k_unit[j]);
-                        by_k.e[r] = kk[r] * (far_unit[r] * k_unit[j]);
-                    }
-                    float *to = a.pairs + (unit * 2 * PAIRS + pair_of(wave, jt)) * 256;
+                if (jt <= it) {
+                    float *to = a.pairs + (unit * 2 * PAIRS + pair_of(it, jt)) * 256;
                     store_at(to, lane * 16, by_q);
                     store_at(to + PAIRS * 256, lane * 16, by_k);
                 }
-            float p[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = BACK ? 16 * wave + 4 * quad + r : 16 * wave + col, m = BACK ? j : 16 * jt + 4 * quad + r;
-                p[r] = m <= i && episode[m] == episode[i] ? qk[r] * (q_unit[i] * d.scale * k_unit[m]) * exp2_wide(far[i] - far[m]) : 0.0f;
-            }
             // fragments of 16 rows and 32 entries: rows are the steps that look back (forward), those that are looked at (back)
-            const int row = BACK ? 16 * jt + col : 16 * wave + col, at = BACK ? 16 * wave + 4 * quad : 16 * jt + 4 * quad;
+            const int row = BACK ? 16 * jt + col : 16 * it + col, at = BACK ? 16 * it + 4 * quad : 16 * jt + 4 * quad;
             char *f = a.read + (unit * 8 + (row >> 4) * 2 + (at >> 5)) * N_::WIDE_FRAGMENT + ((at & 31) >> 3) * 256 + (row & 15) * 16;
             put_wide4<T>(f, 1024, (at >> 2) & 1, p);
         }
