@@ -51,7 +51,7 @@ __device__ __forceinline__ int pair_of(int back, int seen) { return back * (back
 // ---- what needs the chunk's steps only --------------------------------------------------------------------------------
 // A workgroup for a chunk of a head.  What leaves is in the order that the kernels after it take it in (fragments in lane order, read in whole lines).  Bound by the latency of its
 // dependent phases (gates, lengths, products, substitution in blocks of 16, two levels of products), with three workgroups a unit to overlap them: 1024 chunks of 128 keys in bf16
-// 40 us, 18 MB read and 68 MB written (105 MB for the backward call); 90 chunks of 37 in binary32 18.
+// 38 us, 18 MB read and 68 MB written (105 MB for the backward call); 90 chunks of 37 in binary32 17 to 18.
 template <typename T, int KP> struct PrepLds {
     static constexpr int PITCH = Num<T>::exact_pitch(KP), LINE = 65;
     static constexpr int FAR = 0, EPISODE = FAR + 8 * CHUNK, STRENGTH = EPISODE + 4 * CHUNK, Q = STRENGTH + 4 * CHUNK, K = Q + 4 * CHUNK, BAD = K + 4 * CHUNK;
