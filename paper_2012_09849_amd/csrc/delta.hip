@@ -285,7 +285,7 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
 // ---- from chunk to chunk ------------------------------------------------------------------------------------------------
 // Columns of values that are not finite: what they were at which step.  They are taken out of the products, which would spread them, and put back where the rule has them.
 struct Marks {
-    uint32_t any, pad[3];                 // the chunk (+ 1) that has some
+    uint32_t any, most[3];                // the chunk (+ 1) that has some; the largest of the state's entries after a chunk, of three in turn (see lift_of)
     uint32_t steps[TILE][2];
     __device__ __forceinline__ uint64_t of(int column) const { return (uint64_t)steps[column][0] | (uint64_t)steps[column][1] << 32; }
 };
@@ -295,6 +295,17 @@ __device__ __forceinline__ void mark(Marks &m, int column, int step, int chunk)
     m.any = chunk + 1;
 }
 __device__ __forceinline__ uint64_t steps_between(int from, int to) { return (~0ull >> (63 - to)) & (~0ull << from); }
+
+// What a segment makes of ones on the diagonal may leave binary32 where no state does: growing steps make more of them than there is, also of a state of nothing, and strong decays less,
+// which later steps may bring back.  So it is held as numbers between 2^-40 and 2^-10 at each chunk's beginning (a chunk may lengthen by 2^127) and a power of two, which joins them when
+// they have met the state.  Powers of two round nothing.  (A prompt of 8192, 8 heads of 128 x 128, bf16: 209 us, without 208; lifted in every chunk 214.)
+__device__ __forceinline__ int lift_of(uint32_t most)
+{
+    const int e = (int)(most >> 23);
+    return e == 0 || e == 255 || (e >= 127 - 40 && e <= 127 - 10) ? 0 : 127 - e - 20;
+}
+// ... the part of the power that the numbers take before they meet the state: up to 2^60, so that a small state's products are not the smallest numbers, and no less than there is
+__device__ __forceinline__ int early_part(int power) { return power < 0 ? 0 : power < 60 ? power : 60; }
 
 template <typename T> __device__ __forceinline__ void store4(T *p, const float (&v)[4], int count)
 {
@@ -352,6 +363,7 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
     Marks &marks = *(Marks *)(lds + L::MARKS);
     if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
     if (tid == TILE) marks.any = 0;
+    if (ENDS && tid < 3) marks.most[tid] = tid == 2 ? __float_as_uint(1.0f) : 0u;
 
     f32x4 S[MT][2];
     const int64_t held = ((int64_t)n * d.H + h) * K * V;
@@ -368,6 +380,15 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
                     S[m][nt][r] = f(S[m][nt][r], k < K && v < V, (int64_t)k * V + v);
                 }
     };
+    const auto lift_state = [&](int by) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[m][nt][r] = __builtin_ldexpf(S[m][nt][r], by);
+    };
+    int power = 0, turn = 2;                                   // turn: which of the three holds what is largest now
     const auto share_state = [&]() {
         if (!has_keys) return;
 #pragma unroll
@@ -402,7 +423,7 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
     const int row = 16 * wave + 4 * quad, i = 16 * wave + col;     // of 4 steps, one after the other; of a step
     Exact<T> kf[KP / 32], qf[KP / 32], tf[MT][2];
     Wide<T> wf[2], pf[2];
-    T val[2][4];
+    T val[2][4] = {};
     float keep[4], k_unit[4], strength[4], left[4], keep_i = 0.0f, q_unit_i = 0.0f, all = 0.0f;
     uint64_t bad_k = 0;
     const auto unit_of = [&](int c) { return ((int64_t)c * d.N + n) * d.H + h; };
@@ -420,6 +441,7 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
         }
     };
     const auto load_values = [&](int c) {
+        if (ones) return;                                      // (zeros)
         const T *v = step_of<T>(a.in.v, c * CHUNK, n) + (int64_t)h * V;
         const int last = len - 1 - c * CHUNK;
 #pragma unroll
@@ -429,7 +451,6 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
             for (int nt = 0; nt < 2; ++nt) {
                 const int column = v0 + 16 * nt + col;
                 val[nt][r] = load_at<T>(v, at + (column < V ? column : V - 1) * (uint32_t)sizeof(T));
-                if (ones) val[nt][r] = from_f32<T>(0.0f);
             }
         }
     };
@@ -458,6 +479,7 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
         const int t0 = c * CHUNK;
         const bool more = c + 1 < used;
         load_pair(wf, a.inverse, c);
+        const uint32_t largest = ENDS ? marks.most[turn] : 0u;
         if (!ENDS && a.states && has_keys) {
             float *to = a.states + unit * KP * VP + v0;
 #pragma unroll
@@ -481,6 +503,19 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
         }
         if constexpr (!ENDS) load_pair(pf, a.read, c);
         if (more) load_rows(c + 1);
+        int lift = 0;
+        if (ENDS && ones) {
+            lift = __builtin_amdgcn_readfirstlane(lift_of(largest));
+            power -= lift;
+            turn = turn == 2 ? 0 : turn + 1;
+            if (lift != 0) {                                   // (the rows in LDS are still as they were: their products take the same)
+                lift_state(lift);
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) ks[nt][r] = __builtin_ldexpf(ks[nt][r], lift);
+            }
+        }
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             float e[4];
@@ -584,10 +619,22 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
 #pragma unroll
                             for (int r = 0; r < 4; ++r) S[m][nt][r] = __builtin_nanf("");
             }
+            if (ENDS && ones) {
+                float most = 0.0f;
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) most = fmaxf(most, __builtin_fabsf(S[m][nt][r]));
+                most = most16(most);
+                if (col == 0) atomicMax(&marks.most[turn], __float_as_uint(most));       // (sizes are in their bits' order)
+            }
             share_state();
         }
         if (more) load_gates(c + 1);
         lds_barrier();
+        if (ENDS && ones && tid == 0) marks.most[turn == 2 ? 0 : turn + 1] = 0;      // (read in the chunk before this one, and written in the next one, two barriers on)
         if (some) {
             if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
             lds_barrier();
@@ -595,6 +642,11 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
     }
     if constexpr (ENDS) {
         const int width = VP + KP, first = ones ? VP + v0 : v0;
+        if (ones) {
+            const int lift = lift_of(marks.most[turn]), early = early_part(power - lift);
+            lift_state(lift + early);
+            if (tid == 0) a.powers[place * (KP / TILE) + tile] = power - lift - early;
+        }
         if (has_keys)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -644,12 +696,17 @@ template <typename T, int KP> __global__ __launch_bounds__(4 * KP) void begin_ke
     };
     put_begin(0);
     // a segment's operands arrive while the one before it is worked on
+    static_assert(TILE == 32, "a tile's power is that of 32 of the entries that a product sums over");
     float next_move[KP / 32][8], next_own[2][4];
+    int next_power[KP / 32];
     const auto more = [&](int s) { return s + 1 < a.segments && (s + 1) * a.per_segment < chunks; };
     const auto load = [&](int s) {
         const float *from = a.ends + (place_of(s) + 16 * wave) * width;
 #pragma unroll
-        for (int k = 0; k < KP / 32; ++k) __builtin_memcpy(next_move[k], __builtin_assume_aligned(from + (int64_t)col * width + VP + 32 * k + 8 * quad, 16), 32);
+        for (int k = 0; k < KP / 32; ++k) {
+            __builtin_memcpy(next_move[k], __builtin_assume_aligned(from + (int64_t)col * width + VP + 32 * k + 8 * quad, 16), 32);
+            next_power[k] = a.powers[place_of(s) / KP * (KP / TILE) + k];
+        }
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
@@ -662,6 +719,7 @@ template <typename T, int KP> __global__ __launch_bounds__(4 * KP) void begin_ke
         if (a.gates[((int64_t)c * d.N + n) * d.H + h].keep[CHUNK - 1] < 0.0f) forgets[c / a.per_segment] = 1;
     for (int s = 0; more(s); ++s) {
         float move[KP / 32][8];
+        int power[KP / 32];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const float x[4] = {S[nt][0], S[nt][1], S[nt][2], S[nt][3]};
@@ -670,14 +728,24 @@ template <typename T, int KP> __global__ __launch_bounds__(4 * KP) void begin_ke
             for (int r = 0; r < 4; ++r) S[nt][r] = next_own[nt][r];
         }
         __builtin_memcpy(move, next_move, sizeof move);
+        __builtin_memcpy(power, next_power, sizeof power);
         if (more(s + 1)) load(s + 1);
         lds_barrier();
         if (!forgets[s])
 #pragma unroll
             for (int k = 0; k < KP / 32; ++k) {
                 const Wide<T> moved = make_wide<T>(move[k]);
+                if (power[k] == 0)
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) mma(S[nt], moved, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * k + quad) * N_::WIDE, 16));
+                    for (int nt = 0; nt < 2; ++nt) mma(S[nt], moved, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * k + quad) * N_::WIDE, 16));
+                else
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) {
+                        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+                        mma(x, moved, get_wide<T>(state + (16 * nt + col) * L::STATE_PITCH + (4 * k + quad) * N_::WIDE, 16));
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) S[nt][r] += __builtin_ldexpf(x[r], power[k]);
+                    }
             }
         put_begin(s + 1);
         lds_barrier();
@@ -1573,7 +1641,7 @@ int64_t most_places(const hts_delta_rule_desc &d)
     return ROOM / ceil_div(d.V, TILE);
 }
 
-struct Layout { int64_t ends, begins, inverse, read, keys, queries, pairs, rows, gates, late, write, part, heads, total; };
+struct Layout { int64_t ends, begins, powers, inverse, read, keys, queries, pairs, rows, gates, late, write, part, heads, total; };
 Layout layout(const hts_delta_rule_desc &d, bool back)
 {
     const int64_t units = ceil_div(d.T, CHUNK) * d.N * d.H, wide = d.precision == HTS_PRECISION_BF16 ? Num<bf16_t>::WIDE_FRAGMENT : Num<float>::WIDE_FRAGMENT, exact = d.precision == HTS_PRECISION_BF16 ? Num<bf16_t>::EXACT_FRAGMENT : Num<float>::EXACT_FRAGMENT;
@@ -1581,7 +1649,8 @@ Layout layout(const hts_delta_rule_desc &d, bool back)
     const int64_t KP = keys_padded(d.K), VP = round_up(d.V, TILE), places = back ? 0 : most_places(d);
     l.ends = 0;
     l.begins = l.ends + 4 * places * KP * (VP + KP);
-    l.inverse = l.begins + 4 * places * KP * VP;
+    l.powers = l.begins + 4 * places * KP * VP;
+    l.inverse = l.powers + round_up(4 * places * (KP / TILE), 256);
     l.read = l.inverse + units * 8 * wide;
     l.keys = l.read + units * 8 * wide;
     l.queries = l.keys + units * (keys_padded(d.K) / 8) * exact;
@@ -1603,7 +1672,7 @@ DeltaArgs arguments(hts_seq_ctx &c, const DeltaOp &op, bool back)
     a.chunks = (int)ceil_div(op.d.T, CHUNK);
     const Segments seg = segments_of(op.d);
     a.segments = back ? 1 : seg.count; a.per_segment = back ? a.chunks : seg.chunks;
-    a.ends = (float *)(c.ws + l.ends); a.begins = (float *)(c.ws + l.begins);
+    a.ends = (float *)(c.ws + l.ends); a.begins = (float *)(c.ws + l.begins); a.powers = (int32_t *)(c.ws + l.powers);
     a.tiles = (int)ceil_div(op.d.V, TILE); a.VP = a.tiles * TILE;
     if (op.states) a.z = op.states + delta_state_floats(op.d);
     a.inverse = a.inverse_t = c.ws + l.inverse; a.read = c.ws + l.read; a.keys = c.ws + l.keys; a.queries = c.ws + l.queries; a.gates = (Gates *)(c.ws + l.gates); a.pairs = (float *)(c.ws + l.pairs); a.rows = op.d.K % 8 ? c.ws + l.rows : nullptr;

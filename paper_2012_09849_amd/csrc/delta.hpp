@@ -207,6 +207,7 @@ struct DeltaArgs {
     // [segment][N][H][KP][VP + KP], and the states that they begin with, [segment][N][H][KP][VP]
     int segments, per_segment;
     float *ends, *begins;
+    int32_t *powers;                              // of two, that products with the ends of ones are to be multiplied by: [segment][N][H][KP / 32]
     float *late, *write, *part, *heads;           // gradients of the states at the chunks' ends; of the values; sums of the decays' parameters; of shared queries and keys
 };
 __device__ __forceinline__ int length_of(const DeltaArgs &a, int n)

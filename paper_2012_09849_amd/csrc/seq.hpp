@@ -171,6 +171,10 @@ __device__ __forceinline__ float wave_add(float x)
     return x + __shfl_xor(x, 32, 64);
 }
 
+// ... and the largest of 16 neighbouring lanes' sizes (0 or more; NaN is passed over)
+template <int CONTROL> __device__ __forceinline__ float most_moved(float x) { return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xf, 0xf, true))); }
+__device__ __forceinline__ float most16(float x) { return most_moved<0x140>(most_moved<0x141>(most_moved<0x4E>(most_moved<0xB1>(x)))); }
+
 // V entries from memory, or one at a time where their address is no multiple of their size
 template <typename T, int V> struct Loaded { T e[V]; };
 template <typename T, int V> __device__ __forceinline__ Loaded<T, V> load_v(const T *p)
