@@ -96,8 +96,9 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
             const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
             be = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
             e = (double)dc.exponent * LOG2E_64;
-            wrong = !finite(be) || !(e < MOST_EXPONENT);
-            reset = (a.in.starts && a.in.starts[(int64_t)t * d.N + n]) || e < FORGETS || wrong;
+            const bool start = a.in.starts && a.in.starts[(int64_t)t * d.N + n];          // (has no decay, whatever its input)
+            wrong = !finite(be) || (!start && !(e < MOST_EXPONENT));
+            reset = start || e < FORGETS || wrong;
             if (wrong) be = 0.0f;
             if (reset) e = 0.0;
         }

@@ -1,0 +1,30 @@
+"""The gated delta rule's gates where they are at their limits."""
+import numpy as np
+import pytest
+import torch
+
+import seq_oracle as so
+from test_gpu_delta_rule import Case
+from test_gpu_seq import HALF, hts, host, put  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 16, 17, 130])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf"), -1e4, 1e38])
+def test_a_first_step_has_no_decay(hts, dtype, T, value):  # noqa: F811
+    """alpha is 0 where a step begins an episode, whatever its input: of calls of a few steps as of long ones, of outputs as of gradients."""
+    c = Case(hts, dtype, T, 2, 1, 2, 16, 40, starts=0.5, softplus=False)
+    s = np.zeros((T, 2), dtype=np.uint8)
+    for t in {0, T // 2, T - 1}:
+        s[t, 0] = 1
+        c.at["a"][t, 0] = value                        # (A is -1: a growth that no number holds, or a step that forgets)
+        c.wide["a"][t, 0] = 0.0                        # the oracle's factor is 0 there, and times infinity no number
+    c.wide["starts"], c.at["starts"] = s, torch.from_numpy(s).cuda()
+    got = c.run()
+    want, off = c.oracle()
+    for name in got:
+        so.near(host(got[name]), want[name], off[name] / so.U, 1, HALF["f32" if got[name].dtype is torch.float32 else dtype], name)
+    assert bool((got["da"][torch.from_numpy(s).cuda() != 0] == 0).all())
+    c.ctx.close()
