@@ -98,9 +98,9 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
             e = (double)dc.exponent * LOG2E_64;
             const bool start = a.in.starts && a.in.starts[(int64_t)t * d.N + n];          // (has no decay, whatever its input)
             wrong = !finite(be) || (!start && !(e < MOST_EXPONENT));
-            reset = start || e < FORGETS || wrong;
+            reset = start || (e < FORGETS && !wrong);          // (a step that is wrong is marked, also for the ones before it, which its state's gradient goes to)
             if (wrong) be = 0.0f;
-            if (reset) e = 0.0;
+            if (reset || wrong) e = 0.0;
         }
         resets = __ballot(reset);
         gates_bad = __ballot(wrong);

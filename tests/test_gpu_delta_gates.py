@@ -28,3 +28,25 @@ def test_a_first_step_has_no_decay(hts, dtype, T, value):  # noqa: F811
         so.near(host(got[name]), want[name], off[name] / so.U, 1, HALF["f32" if got[name].dtype is torch.float32 else dtype], name)
     assert bool((got["da"][torch.from_numpy(s).cuda() != 0] == 0).all())
     c.ctx.close()
+
+
+@pytest.mark.parametrize("T", [12, 130])
+@pytest.mark.parametrize("name,value", [("a", float("nan")), ("a", -1e4), ("b", float("nan"))])
+def test_gradients_before_a_gate_that_is_no_number(hts, T, name, value):  # noqa: F811
+    """A decay that is no number is a factor of the state's gradient on its way to the steps before it, and to the state that the sequence began with; a strength is one of what a
+    step takes away.  The episode before has nothing of it."""
+    c = Case(hts, "f32", T, 2, 1, 2, 16, 40, starts=0.5, softplus=False)
+    s = np.zeros((T, 2), dtype=np.uint8)
+    s[T // 4, 1] = 1                                  # the second sequence: an episode begins a quarter into it
+    c.wide["starts"], c.at["starts"] = s, torch.from_numpy(s).cuda()
+    at = T // 2
+    c.at[name][at] = value
+    got = c.run()
+    for n, first in ((0, 0), (1, T // 4)):
+        for g in ("dk", "dv"):
+            assert bool(got[g][first:at + 1, n].isnan().all()), (g, n)
+        assert bool(got["y"][at:, n].isnan().all()) and bool(got["h_out"][n].isnan().all()) and bool(got["y"][:at, n].isfinite().all())
+    for g in ("dq", "dk", "dv", "da", "db"):
+        assert bool(got[g][:T // 4, 1].isfinite().all()), g
+    assert bool(got["dh_in"][0].isnan().all()) and bool(got["dh_in"][1].isfinite().all())
+    c.ctx.close()
