@@ -89,12 +89,14 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
     if (wave == 0) {
         const int t = t0 + lane;
         const bool live = t < len;
-        float be = 0.0f;
+        float be = 0.0f, rest = 0.0f;
         double e = 0.0;
         bool reset = false, wrong = false;
         if (live) {
             const Decay dc = decay_of(to_f32(step_of<T>(a.in.a, t, n)[h]), a.in.a_bias ? a.in.a_bias[h] : 0.0f, a.in.A[h], d.softplus);
-            be = sigmoid_f(to_f32(step_of<T>(a.in.b, t, n)[h]));
+            const float b = to_f32(step_of<T>(a.in.b, t, n)[h]);
+            be = sigmoid_f(b);
+            if constexpr (BACK) rest = sigmoid_f(-b);
             e = (double)dc.exponent * LOG2E_64;
             const bool start = a.in.starts && a.in.starts[(int64_t)t * d.N + n];          // (has no decay, whatever its input)
             wrong = !finite(be) || (!start && !(e < MOST_EXPONENT));
@@ -114,6 +116,7 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
         const double end = __shfl(e, 63, 64);
         far[lane] = e; episode[lane] = ep; strength[lane] = be;
         gates.far[lane] = e; gates.strength[lane] = be; gates.episode[lane] = ep; gates.first[lane] = first;
+        if constexpr (BACK) gates.rest[lane] = rest;
         gates.keep[lane] = ep == 0 ? exp2_wide(e) : -1.0f;
         gates.left[lane] = ep == last ? exp2_wide(end - e) : -1.0f;
     }
@@ -1482,7 +1485,7 @@ template <typename T, int KP, bool SHARED> __global__ __launch_bounds__(512) voi
             if (!(gates.resets >> lane & 1)) { da = grad * a.in.A[h] * dc.slope; dA = grad * dc.delta; }
             if (bad_k >> lane & 1) da = dA = __builtin_nanf("");
             step_of<T>(a.g.da, t, n)[h] = from_f32<T>(da);
-            step_of<T>(a.g.db, t, n)[h] = from_f32<T>((1.0f - gates.strength[lane]) * sums[lane]);
+            step_of<T>(a.g.db, t, n)[h] = from_f32<T>(gates.rest[lane] * sums[lane]);
         } else if (t < d.T) step_of<T>(a.g.da, t, n)[h] = step_of<T>(a.g.db, t, n)[h] = from_f32<T>(0.0f);
         dA = wave_add(dA); da = wave_add(da);
         if (lane == 0) { part[h] = dA; part[d.H + h] = da; }

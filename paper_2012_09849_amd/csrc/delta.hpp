@@ -185,6 +185,7 @@ __device__ __forceinline__ float exp2_wide(double x)
 // -1: nothing, an episode began in between (a factor of 0 would make NaN of what is not finite).
 struct Gates {
     double far[CHUNK];                    // sums of the decays' exponents (base 2) from the chunk's beginning
+    float rest[CHUNK];                    // 1 - strength, by itself: of a strength next to one the difference has no digits left (for the backward call)
     float keep[CHUNK], left[CHUNK], strength[CHUNK], q_unit[CHUNK], k_unit[CHUNK];
     int32_t episode[CHUNK], first[CHUNK]; // episodes that began in the chunk up to a step; the first step of its own
     uint64_t bad_k, bad_q, resets;        // steps whose key or gates, whose query, are not finite; steps that see nothing of what was before

@@ -50,3 +50,27 @@ def test_gradients_before_a_gate_that_is_no_number(hts, T, name, value):  # noqa
         assert bool(got[g][:T // 4, 1].isfinite().all()), g
     assert bool(got["dh_in"][0].isnan().all()) and bool(got["dh_in"][1].isfinite().all())
     c.ctx.close()
+
+
+@pytest.mark.parametrize("T", [5, 90])
+def test_strengths_next_to_one(hts, T):  # noqa: F811
+    """db has a factor 1 - beta, which has digits where beta has none left of them.  The logistic function's own roundings: |b| for the product with log2(e), |b| for that number and
+    eight more, on what the products of the two columns are off by."""
+    c = Case(hts, "f32", T, 1, 1, 2, 16, 16)
+    b = np.linspace(-20.0, 40.0, 2 * T).reshape(T, 1, 2)
+    c.at["b"], c.wide["b"] = put(b)
+    got = c.run()
+    want, off = c.oracle()
+    rest, share = so.sigmoid(-c.wide["b"]), so.sigmoid(c.wide["b"])
+    # the oracle's db has 1 - beta as a difference, which is nothing in binary64 either from b = 37 on: from its dv = beta dz / d(beta z), and z step by step
+    S, unit = c.wide["h_in"][0].copy(), lambda x: x / np.sqrt((x * x).sum() + 1e-6)
+    for t in range(T):
+        k = unit(c.wide["k"][t, 0, 0])
+        al = np.exp(np.logaddexp(0, c.wide["a"][t, 0] + c.wide["a_bias"]) * c.wide["A"])[:, None, None]
+        z = c.wide["v"][t, 0] - (k[:, None] * al * S).sum(1)
+        S = al * S + share[t, 0][:, None, None] * k[:, None] * z[:, None]
+        want["db"][t, 0] = (want["dv"][t, 0] * z).sum(1) * rest[t, 0]
+    room = off["db"] / so.U * rest * share + np.abs(want["db"]) * (2 * np.abs(c.wide["b"]) + 8)
+    so.near(host(got["db"]), want["db"], room, 1, HALF["f32"], "db")
+    assert bool((got["db"] != 0).all())
+    c.ctx.close()
