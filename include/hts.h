@@ -394,7 +394,8 @@ int32_t hts_layer_norm_backward(hts_seq_ctx *ctx, const hts_layer_norm_desc *des
  *   z_t = v_t - alpha_t S_{t-1}^T k_t;  S_t = alpha_t S_{t-1} + beta_t k_t z_t^T;  y_t = scale S_t^T q_t
  *   normalize = 1: q and k are divided by sqrt(their square + 1e-6) first (with keys of length one and A delta <= 0 the state stays bounded).
  *   q, k [T,N,G*K]   v, y [T,N,H*V]   a, b [T,N,H]   K 1..128, V 1..65536, G divides H, H 1..65536   A f32 [H]   a_bias f32 [H] or NULL (zeros)
- *   h_in f32 [N,H,K,V] or NULL (zeros); h_out or NULL: the state after the last step.  h_out may be h_in.
+ *   h_in f32 [N,H,K,V] or NULL (zeros); h_out or NULL: the state after the last step.  h_out may be h_in; other outputs that share memory with
+ *   anything else, of the backward call too, are HTS_EINVAL (they may lie between an array's rows).
  *   states f32 or NULL: receives what the backward call needs, hts_delta_rule_states(desc) floats.
  * Values that are not finite (queries and keys: or whose squares' sum is not) make NaN of what sees them: outputs from their step on to the episode's end,
  * gradients of their episode.  Nothing of them reaches other episodes, sequences or, of q, k, a and b, other groups' heads (but for the sums dA and

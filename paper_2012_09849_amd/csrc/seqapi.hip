@@ -367,8 +367,29 @@ static int32_t check_delta_arrays(const hts_delta_rule_desc *d, const hts_delta_
     CHECK(check_steps(in->a, d->T, d->N, d->H, s, false)); CHECK(check_steps(in->b, d->T, d->N, d->H, s, false));
     return !in->A || misaligned(in->A, 4) || misaligned(in->a_bias, 4) || misaligned(in->lengths, 4) || misaligned(in->h_in, 4) ? HTS_EINVAL : HTS_OK;
 }
-// an output in an input's place (outputs beside inputs in a wider array are the caller's)
-static bool takes_place(const hts_steps &out, const hts_delta_rule_inputs &in) { return out.p == in.q.p || out.p == in.k.p || out.p == in.v.p || out.p == in.a.p || out.p == in.b.p; }
+// Where a call's arrays lie: what it reads, then what it writes, which shares memory with nothing else
+struct DeltaAreas {
+    const hts_delta_rule_desc &d;
+    Area of[24];
+    int read = 0, count = 0;
+    void steps(const hts_steps &s, int64_t cols) { of[count++] = area(s.p, s.st, s.sn, d.T, d.N, cols, size_of(d.precision)); }
+    void dense(const void *p, int64_t n, int size) { of[count++] = area(p, n, size); }
+    int64_t keys() const { return (int64_t)d.G * d.K; }
+    int64_t values() const { return (int64_t)d.H * d.V; }
+    int64_t held() const { return (int64_t)d.N * d.H * d.K * d.V; }
+    // h_in: not where an output takes its place
+    void inputs(const hts_delta_rule_inputs &in, bool h_in)
+    {
+        steps(in.q, keys()); steps(in.k, keys()); steps(in.v, values()); steps(in.a, d.H); steps(in.b, d.H);
+        dense(in.A, d.H, 4); dense(in.a_bias, d.H, 4); dense(in.starts, (int64_t)d.T * d.N, 1); dense(in.lengths, d.N, 4);
+        if (h_in) dense(in.h_in, held(), 4);
+    }
+    bool apart() const
+    {
+        for (int i = read; i < count; ++i) for (int k = 0; k < i; ++k) if (meet(of[i], of[k])) return false;
+        return true;
+    }
+};
 
 extern "C" int32_t hts_delta_rule(hts_seq_ctx *ctx, const hts_delta_rule_desc *d, const hts_delta_rule_inputs *in, hts_steps y, float *h_out, float *states)
 {
@@ -378,7 +399,12 @@ extern "C" int32_t hts_delta_rule(hts_seq_ctx *ctx, const hts_delta_rule_desc *d
     op.d = *d;
     CHECK(check_delta_arrays(d, in, &op.in));
     CHECK(check_steps(y, d->T, d->N, (int64_t)d->H * d->V, size_of(d->precision), true));
-    if (misaligned(h_out, 4) || misaligned(states, 16) || takes_place(y, op.in) || (states && (states == h_out || states == op.in.h_in))) return HTS_EINVAL;
+    if (misaligned(h_out, 4) || misaligned(states, 16)) return HTS_EINVAL;
+    DeltaAreas all{*d};
+    all.inputs(op.in, h_out != op.in.h_in);
+    all.read = all.count;
+    all.steps(y, all.values()); all.dense(h_out, all.held(), 4); all.dense(states, delta_states(*d), 4);
+    if (!all.apart()) return HTS_EINVAL;
     CHECK(check_workspace(ctx, delta_workspace(*d, false)));
     op.y = y; op.h_out = h_out; op.states = states;
     LAUNCH_TRY(launch_delta(*ctx, op));
@@ -401,12 +427,13 @@ extern "C" int32_t hts_delta_rule_backward(hts_seq_ctx *ctx, const hts_delta_rul
     CHECK(check_steps(g->dq, d->T, d->N, keys, s, true)); CHECK(check_steps(g->dk, d->T, d->N, keys, s, true)); CHECK(check_steps(g->dv, d->T, d->N, values, s, true));
     CHECK(check_steps(g->da, d->T, d->N, d->H, s, true)); CHECK(check_steps(g->db, d->T, d->N, d->H, s, true));
     if (!g->dA || misaligned(g->dA, 4) || misaligned(g->da_bias, 4) || misaligned(g->dh_in, 4) || misaligned(states, 16) || misaligned(dh_out, 4)) return HTS_EINVAL;
-    const hts_steps *outs[] = {&g->dq, &g->dk, &g->dv, &g->da, &g->db};
-    for (int i = 0; i < 5; ++i) {
-        if (takes_place(*outs[i], op.in) || outs[i]->p == dy.p) return HTS_EINVAL;
-        for (int k = 0; k < i; ++k) if (outs[i]->p == outs[k]->p) return HTS_EINVAL;
-    }
-    if (g->dA == g->da_bias || (g->dh_in && (g->dh_in == dh_out || g->dh_in == op.in.h_in || g->dh_in == states))) return HTS_EINVAL;
+    DeltaAreas all{*d};
+    all.inputs(op.in, true);
+    all.steps(dy, values); all.dense(dh_out, all.held(), 4); all.dense(states, delta_states(*d), 4);
+    all.read = all.count;
+    all.steps(g->dq, keys); all.steps(g->dk, keys); all.steps(g->dv, values); all.steps(g->da, d->H); all.steps(g->db, d->H);
+    all.dense(g->dA, d->H, 4); all.dense(g->da_bias, d->H, 4); all.dense(g->dh_in, all.held(), 4);
+    if (!all.apart()) return HTS_EINVAL;
     CHECK(check_workspace(ctx, delta_workspace(*d, true)));
     op.dy = dy; op.dh_out = dh_out; op.states = const_cast<float *>(states);
     LAUNCH_TRY(launch_delta_backward(*ctx, op));
