@@ -30,6 +30,7 @@ template <int LANES> __device__ __forceinline__ float add_row(float x)
     return x;
 }
 
+__device__ __forceinline__ float sizes_of(const f32x4 &x) { return (__builtin_fabsf(x[0]) + __builtin_fabsf(x[1])) + (__builtin_fabsf(x[2]) + __builtin_fabsf(x[3])); }
 struct Decay { float delta, slope, exponent; };       // exponent: of 2
 __device__ __forceinline__ Decay decay_of(float x, float bias, float A, int softplus)
 {
@@ -228,16 +229,39 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
         }
     }
     __syncthreads();
-    // the inverse: blocks of 16 on the diagonal by substitution, a column a lane; then those of 32 and the whole, W10 = -W11 M10 W00
+    // the inverse: blocks of 16 on the diagonal by substitution, a column a lane; then those of 32 and the whole, W10 = -W11 M10 W00.  A step whose row leaves binary32 (by keys that lengthen
+    // the state) is one that is not finite, and leaves nothing in the products: 0 times it would be NaN of other episodes
+    const auto keep_finite = [&](float &x, int step) {
+        if (finite(x)) return;
+        atomicOr(&bad[step >> 5], 1u << (step & 31));
+        x = 0.0f;
+    };
+    const auto keep_finite4 = [&](f32x4 &x, int step) {
+        if (!finite(sizes_of(x)))
+            for (int r = 0; r < 4; ++r) {
+                float v = x[r];
+                keep_finite(v, step + r);
+                x[r] = v;
+            }
+    };
     if (lane < 16) {
         const float *m = below + 16 * wave * (L::LINE + 1);
-        float x[16];
+        float x[16], sizes = 0.0f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             x[r] = r == lane ? 1.0f : 0.0f;
 #pragma unroll
             for (int k = 0; k < r; ++k) x[r] = __builtin_fmaf(-m[r * L::LINE + k], x[k], x[r]);
+            sizes += __builtin_fabsf(x[r]);
         }
+        if (!finite(sizes))                                    // again, row by row
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                x[r] = r == lane ? 1.0f : 0.0f;
+#pragma unroll
+                for (int k = 0; k < r; ++k) x[r] = __builtin_fmaf(-m[r * L::LINE + k], x[k], x[r]);
+                keep_finite(x[r], 16 * wave + r);
+            }
 #pragma unroll
         for (int r = 0; r < 16; ++r) inverse[(16 * wave + r) * L::LINE + 16 * wave + lane] = x[r];
     }
@@ -252,22 +276,26 @@ template <typename T, int KP, bool BACK> __global__ __launch_bounds__(256) void 
     f32x4 x;
     if (wave < 2) {
         x = tile_product(below + (block + 16) * L::LINE + block, L::LINE, inverse + block * (L::LINE + 1), L::LINE, 16, col, quad);
+        keep_finite4(x, block + 16 + 4 * quad);
 #pragma unroll
         for (int r = 0; r < 4; ++r) half[(16 * wave + 4 * quad + r) * 33 + col] = x[r];
     }
     __syncthreads();
     if (wave < 2) {
         x = tile_product(inverse + (block + 16) * (L::LINE + 1), L::LINE, half + 16 * wave * 33, 33, 16, col, quad);
+        keep_finite4(x, block + 16 + 4 * quad);
 #pragma unroll
         for (int r = 0; r < 4; ++r) inverse[(block + 16 + 4 * quad + r) * L::LINE + block + col] = -x[r];
     }
     __syncthreads();
     const int tr = 16 * (wave >> 1), tc = 16 * (wave & 1);
     x = tile_product(below + (32 + tr) * L::LINE, L::LINE, inverse + tc, L::LINE, 32, col, quad);
+    keep_finite4(x, 32 + tr + 4 * quad);
 #pragma unroll
     for (int r = 0; r < 4; ++r) half[(tr + 4 * quad + r) * 33 + tc + col] = x[r];
     __syncthreads();
     x = tile_product(inverse + (32 + tr) * L::LINE + 32, L::LINE, half + tc, 33, 32, col, quad);
+    keep_finite4(x, 32 + tr + 4 * quad);
 #pragma unroll
     for (int r = 0; r < 4; ++r) inverse[(32 + tr + 4 * quad + r) * L::LINE + tc + col] = -x[r];
     __syncthreads();
@@ -535,7 +563,6 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
         }
         if (more) load_values(c + 1);
         lds_barrier();
-        const bool some = marks.any == (uint32_t)c + 1;
         // Z, and what it writes
         f32x4 z[2] = {};
 #pragma unroll
@@ -545,6 +572,12 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
             for (int nt = 0; nt < 2; ++nt) mma(z[nt], wf[s], get_wide<T>(left_over + (16 * nt + col) * L::ROW_PITCH + (4 * s + quad) * N_::WIDE, 16));
         }
         load_keys(c);
+        if (!finite(sizes_of(z[0]) + sizes_of(z[1])))          // (the state leaves binary32 at such a step)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (!finite(z[nt][r])) { z[nt][r] = 0.0f; mark(marks, again(16 * nt + col), again(row) + r, c); }
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             float u[4], l[4];
@@ -558,13 +591,11 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
             if (!ENDS && a.z) {
                 float *to = a.z + unit * CHUNK * VP + v0 + 16 * nt;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const bool wrong = some && t0 + row + r < len && (marks.of(16 * nt + col) & steps_between(a.gates[unit].first[row + r], row + r));
-                    store_at(to + r * (int64_t)VP, z_at, wrong ? __builtin_nanf("") : z[nt][r]);
-                }
+                for (int r = 0; r < 4; ++r) store_at(to + r * (int64_t)VP, z_at, z[nt][r]);
             }
         }
         lds_barrier();
+        const bool some = marks.any == (uint32_t)c + 1;
         // outputs, the values along a row
         if constexpr (!ENDS) {
 #pragma unroll
@@ -640,6 +671,12 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
         lds_barrier();
         if (ENDS && ones && tid == 0) marks.most[turn == 2 ? 0 : turn + 1] = 0;      // (read in the chunk before this one, and written in the next one, two barriers on)
         if (some) {
+            if (!ENDS && a.z)
+                for (int p = again(0); p < 8; ++p) {               // (a lane's own, after what it has written there)
+                    const int step = row + (p & 3), column = 16 * (p >> 2) + col;
+                    if (t0 + step < len && (marks.of(column) & steps_between(a.gates[unit].first[step], step))) a.z[(unit * CHUNK + step) * VP + v0 + column] = __builtin_nanf("");
+                }
+            lds_barrier();
             if (tid < TILE) marks.steps[tid][0] = marks.steps[tid][1] = 0;
             lds_barrier();
         }
@@ -732,7 +769,8 @@ template <typename T, int KP> __global__ __launch_bounds__(4 * KP) void begin_ke
             for (int r = 0; r < 4; ++r) S[nt][r] = next_own[nt][r];
         }
         __builtin_memcpy(move, next_move, sizeof move);
-        __builtin_memcpy(power, next_power, sizeof power);
+#pragma unroll
+        for (int k = 0; k < KP / 32; ++k) power[k] = __builtin_amdgcn_readfirstlane(next_power[k]);
         if (more(s + 1)) load(s + 1);
         lds_barrier();
         if (!forgets[s])
