@@ -21,25 +21,39 @@ struct NormArgs {
     bool sums;                // dw or db is wanted
 };
 
-// What a thread holds of a row: PER times VEC neighbouring entries, 16 bytes, of which `count` exist.  16-byte accesses at any address: the hardware takes them.
+// What a thread holds of a row: PER times V neighbouring entries, 16 bytes, of which `count` exist.  16-byte accesses at any address: the hardware takes them.  As words, so that a
+// load is not waited for where it is taken apart into entries.
 template <typename T> struct Piece {
-    static constexpr int V = 16 / (int)sizeof(T);
-    T e[V];
+    static constexpr int V = 16 / (int)sizeof(T), IN_WORD = 4 / (int)sizeof(T);
+    uint32_t w[4];
     __device__ __forceinline__ void load(const T *p, int count)
     {
-        if (count >= V) __builtin_memcpy(this, p, 16);
+        if (count >= V) __builtin_memcpy(w, p, 16);
         else
 #pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = i < count ? p[i] : from_f32<T>(0.0f);
+            for (int i = 0; i < 4; ++i) {
+                w[i] = 0;
+#pragma unroll
+                for (int k = 0; k < IN_WORD; ++k) if (i * IN_WORD + k < count) w[i] |= bits_of<T>(to_f32(p[i * IN_WORD + k])) << (16 * k);
+            }
     }
-    __device__ __forceinline__ void store(T *p, int count) const
+    __device__ __forceinline__ float operator[](int i) const
     {
-        if (count >= V) __builtin_memcpy(p, this, 16);
-        else
-#pragma unroll
-            for (int i = 0; i < V; ++i) if (i < count) p[i] = e[i];
+        if constexpr (IN_WORD == 1) return __uint_as_float(w[i]);
+        else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
 };
+template <typename T> __device__ __forceinline__ void store(T *p, const float (&v)[16 / sizeof(T)], int count)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    T e[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = from_f32<T>(v[i]);
+    if (count >= V) __builtin_memcpy(p, e, 16);
+    else
+#pragma unroll
+        for (int i = 0; i < V; ++i) if (i < count) p[i] = e[i];
+}
 template <int V> __device__ __forceinline__ void load_params(float (&v)[V], const float *p, int count, float none)
 {
     if (!p) {
@@ -66,7 +80,7 @@ template <int ROW, int N> __device__ __forceinline__ void row_sums(float (&v)[N]
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) to[wave * N + i] = v[i];
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             v[i] = 0.0f;
@@ -76,15 +90,38 @@ template <int ROW, int N> __device__ __forceinline__ void row_sums(float (&v)[N]
     }
 }
 
-// (x - mean) of a row that is in registers (0 where there is no entry), and r
-template <typename T, int ROW, int PER> __device__ __forceinline__ float centre(const Piece<T> (&x)[PER], float (&h)[PER][Piece<T>::V], const int first, const int F, const float eps, float *shared, int &turn)
+// ... and the largest of a row's values (0 or more)
+template <int ROW> __device__ __forceinline__ float row_most(float v, float *shared, int &turn)
+{
+    v = most16(v);
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    v = fmaxf(v, __shfl_xor(v, 32, 64));
+    if constexpr (ROW > 64) {
+        constexpr int W = ROW / 64;
+        float *to = shared + turn * SUMS;
+        turn ^= 1;
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) to[wave] = v;
+        lds_barrier();
+#pragma unroll
+        for (int k = 0; k < W; ++k) v = fmaxf(v, to[wave / W * W + k]);
+    }
+    return v;
+}
+
+// (x 2^by - mean) of a row that is in registers (0 where there is no entry), and the sum of its squares
+template <typename T, int ROW, int PER, bool SCALED> __device__ __forceinline__ float deviations(const Piece<T> (&x)[PER], float (&h)[PER][Piece<T>::V], const int by, const int first, const int F, float *shared, int &turn)
 {
     constexpr int V = Piece<T>::V;
     float s[1] = {0.0f};
 #pragma unroll
     for (int p = 0; p < PER; ++p)
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[0] += h[p][i] = to_f32(x[p].e[i]);
+        for (int i = 0; i < V; ++i) {
+            h[p][i] = x[p][i];
+            if constexpr (SCALED) h[p][i] = __builtin_ldexpf(h[p][i], by);
+            s[0] += h[p][i];
+        }
     row_sums<ROW>(s, shared, turn);
     const float mean = s[0] / (float)F;
     s[0] = 0.0f;
@@ -101,7 +138,36 @@ template <typename T, int ROW, int PER> __device__ __forceinline__ float centre(
         for (int i = 0; i < V; ++i) s[0] = __builtin_fmaf(h[p][i], h[p][i], s[0]);
     }
     row_sums<ROW>(s, shared, turn);
-    return 1.0f / __builtin_sqrtf(s[0] / (float)F + eps);
+    return s[0];
+}
+
+// A row whose squares leave binary32, or are so small that they have no digits left (without eps), is worked on again with its largest entry between 1 and 2
+__device__ __forceinline__ bool ordinary(float sum, int F, float eps)
+{
+    const float v = sum / (float)F + eps;
+    return v >= 0x1p-100f && v <= 3.402823466e38f;
+}
+__device__ __forceinline__ float inverse_root(float sum, int F, float eps) { return 1.0f / __builtin_sqrtf(sum / (float)F + eps); }
+// h as such deviations, of a row that is read again; what makes them of length one, and that of the row's own.  Rows that are ordinary come out as they were (in a workgroup whose rows meet at barriers).
+struct Roots { float of_h, of_row; };
+template <typename T, int ROW, int PER> __device__ __forceinline__ Roots again_scaled(const T *from, const bool there, float (&h)[PER][Piece<T>::V], const bool as_it_is, const int first, const int F, const float eps, float *shared,
+                                                                                     int &turn)
+{
+    Piece<T> x[PER];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const int at = first + p * ROW * Piece<T>::V;
+        x[p].load(from + at, there ? F - at : 0);
+    }
+    float most = 0.0f;
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+#pragma unroll
+        for (int i = 0; i < Piece<T>::V; ++i) most = fmaxf(most, __builtin_fabsf(x[p][i]));
+    most = fmaxf(row_most<ROW>(most, shared, turn), __builtin_sqrtf(eps));
+    const int e = (int)(__float_as_uint(most) >> 23), by = as_it_is || e == 0 || e == 255 ? 0 : 127 - e;
+    const float r = inverse_root(deviations<T, ROW, PER, true>(x, h, by, first, F, shared, turn), F, __builtin_ldexpf(eps, 2 * by));
+    return Roots{r, __builtin_ldexpf(r, by)};
 }
 
 // Rows in turn, by four workgroups a unit: 8192 x 512 in bf16 5.9 us (2.8 TB/s of 16.8 MB; the launch, a row's arrival and two reductions are most of it), 16 rows 2.5.
@@ -129,13 +195,15 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(threads<ROW
     for (int64_t row = begin; row < a.M; row += rows) {
         if (row + rows < a.M) load(next, row + rows);          // on its way while this one is worked on
         float h[PER][V];
-        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, shared, turn);
+        const float sum = deviations<T, ROW, PER, false>(x, h, 0, first, a.F, shared, turn);
+        float r = inverse_root(sum, a.F, a.eps);
+        if (!ordinary(sum, a.F, a.eps)) r = again_scaled<T, ROW, PER>((const T *)a.x + row * a.x_ld, true, h, false, first, a.F, a.eps, shared, turn).of_h;      // (a workgroup's threads have one row here, or no barriers)
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            Piece<T> y;
+            float y[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) y.e[i] = from_f32<T>(__builtin_fmaf(h[p][i] * r, w[p][i], b[p][i]));
-            y.store((T *)a.y + row * a.y_ld + first + p * ROW * V, a.F - first - p * ROW * V);
+            for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(h[p][i] * r, w[p][i], b[p][i]);
+            store((T *)a.y + row * a.y_ld + first + p * ROW * V, y, a.F - first - p * ROW * V);
             x[p] = next[p];
         }
     }
@@ -146,9 +214,15 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(threads<ROW
 // Rows that a workgroup works on at a time: eight of a wavefront each, two of four, one of sixteen; and all of its threads go round together
 template <int ROW> constexpr int back_threads() { return ROW > 256 ? ROW : 512; }
 
+// workgroups of a backward call, whose sums are added up afterwards, at the most: two a unit, one of sixteen wavefronts
+template <int ROW> constexpr int back_most() { return ROW > 256 ? 256 : 512; }
+
 template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_threads<ROW>()) void norm_backward_kernel(const NormArgs a)
 {
     constexpr int V = Piece<T>::V, ROWS = back_threads<ROW>() / ROW, COLS = ROW * PER * V;
+    // Rows that are to be worked on again, a bit for each of the workgroup's: after the others, so that the loop has nothing of it
+    constexpr int MOST_ROWS = (1 << 24) / back_most<ROW>();
+    __shared__ uint32_t seldom[MOST_ROWS / 32], some;
     __shared__ float shared[(ROWS > 1 ? ROWS * COLS : 0) + 2 * SUMS];
     float *sums = shared + (ROWS > 1 ? ROWS * COLS : 0);
     constexpr bool AHEAD = ROW <= 256;           // the next row's entries are requested before this one's are worked on (sixteen wavefronts have no registers for them)
@@ -165,7 +239,39 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
         }
     };
     const bool adds = a.dx && a.add;
+    const auto along_row = [&](float (&h)[PER][V], const Piece<T> (&dy)[PER], float (&s)[2], float own, bool take) {
+#pragma unroll
+        for (int p = 0; p < PER; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = dy[p][i], g = d * w[p][i];
+                h[p][i] *= own;
+                if (take) {
+                    dw[p][i] = __builtin_fmaf(d, h[p][i], dw[p][i]);          // (of rows behind the last one: zeros)
+                    db[p][i] += d;
+                }
+                s[0] += g;
+                s[1] = __builtin_fmaf(g, h[p][i], s[1]);
+            }
+    };
+    const auto give = [&](const float (&h)[PER][V], const Piece<T> (&dy)[PER], const Piece<T> (&add)[PER], const float (&s)[2], float r, int64_t to) {
+        const float mean = s[0] / (float)a.F, along = s[1] / (float)a.F;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            float o[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                o[i] = r * __builtin_fmaf(-h[p][i], along, dy[p][i] * w[p][i] - mean);
+                if (a.add) o[i] += add[p][i];
+            }
+            store((T *)a.dx + to * a.dx_ld + first + p * ROW * V, o, a.F - first - p * ROW * V);
+        }
+    };
+    for (int i = threadIdx.x; i < MOST_ROWS / 32 && i * 32ll * gridDim.x < a.M; i += back_threads<ROW>()) seldom[i] = 0;
+    if (threadIdx.x == 0) some = 0;
+    __syncthreads();
     int64_t row = (int64_t)blockIdx.x * ROWS;
+    int at_row = mine;                                       // of the workgroup's
     load(x, a.x, a.x_ld, row + mine);
     load(dy, a.dy, a.dy_ld, row + mine);
     if (adds) load(add, a.add, a.add_ld, row + mine);
@@ -176,7 +282,7 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[p][i] = db[p][i] = 0.0f;
     }
-    for (; row < a.M; row += rows) {
+    for (; row < a.M; row += rows, at_row += ROWS) {
         const int64_t to = row + mine;
         if (AHEAD && row + rows < a.M) {
             load(next_x, a.x, a.x_ld, to + rows);
@@ -184,35 +290,16 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
             if (adds) load(next_add, a.add, a.add_ld, to + rows);
         }
         float h[PER][V];
-        const float r = centre<T, ROW, PER>(x, h, first, a.F, a.eps, sums, turn);
-        const float own = to < a.M ? r : 0.0f;                   // (of rows behind the last one r is that of zeros, which eps = 0 makes infinite)
+        const float sum = deviations<T, ROW, PER, false>(x, h, 0, first, a.F, sums, turn);
+        float r = inverse_root(sum, a.F, a.eps);
+        const bool rare = to < a.M && !ordinary(sum, a.F, a.eps);          // (of rows behind the last one r is that of zeros, which eps = 0 makes infinite)
         float s[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int p = 0; p < PER; ++p)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = to_f32(dy[p].e[i]), g = d * w[p][i];
-                h[p][i] *= own;
-                dw[p][i] = __builtin_fmaf(d, h[p][i], dw[p][i]);          // (of rows behind the last one: zeros)
-                db[p][i] += d;
-                s[0] += g;
-                s[1] = __builtin_fmaf(g, h[p][i], s[1]);
-            }
+        if (rare) {
+            if (in_row == 0) { atomicOr(&seldom[at_row >> 5], 1u << (at_row & 31)); some = 1; }
+        } else along_row(h, dy, s, to < a.M ? r : 0.0f, true);
         if (a.dx) {
             row_sums<ROW>(s, sums, turn);
-            const float mean = s[0] / (float)a.F, along = s[1] / (float)a.F;
-            if (to < a.M)
-#pragma unroll
-                for (int p = 0; p < PER; ++p) {
-                    Piece<T> o;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        float v = r * __builtin_fmaf(-h[p][i], along, to_f32(dy[p].e[i]) * w[p][i] - mean);
-                        if (a.add) v += to_f32(add[p].e[i]);
-                        o.e[i] = from_f32<T>(v);
-                    }
-                    o.store((T *)a.dx + to * a.dx_ld + first + p * ROW * V, a.F - first - p * ROW * V);
-                }
+            if (to < a.M && !rare) give(h, dy, add, s, r, to);
         }
 #pragma unroll
         for (int p = 0; p < PER; ++p) { x[p] = next_x[p]; dy[p] = next_dy[p]; add[p] = next_add[p]; }
@@ -222,6 +309,22 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
             if (adds) load(add, a.add, a.add_ld, to + rows);
         }
     }
+    __syncthreads();
+    if (some)
+        for (row = (int64_t)blockIdx.x * ROWS, at_row = 0; row < a.M; row += rows, at_row += ROWS) {
+            const uint32_t which = seldom[at_row >> 5] >> (at_row & 31) & ((1u << ROWS) - 1);
+            if (!which) continue;
+            const bool rare = which >> mine & 1;             // (the others' threads meet these at barriers)
+            const int64_t to = row + mine;
+            load(dy, a.dy, a.dy_ld, to);
+            if (adds) load(add, a.add, a.add_ld, to);
+            float h[PER][V], s[2] = {0.0f, 0.0f};
+            const Roots roots = again_scaled<T, ROW, PER>((const T *)a.x + to * a.x_ld, to < a.M, h, !rare, first, a.F, a.eps, sums, turn);
+            along_row(h, dy, s, roots.of_h, rare);
+            if (!a.dx) continue;
+            row_sums<ROW>(s, sums, turn);
+            if (rare) give(h, dy, add, s, roots.of_row, to);
+        }
     if (!a.sums) return;
     // a workgroup's sums: its rows in order
     float *part = a.part + (int64_t)blockIdx.x * 2 * a.F;
@@ -270,10 +373,9 @@ template <int V, typename F> hipError_t by_width(int width, F f)
     return with(sixteen{}, more);
 }
 
-// workgroups of a backward call, whose sums are added up afterwards: two a unit, one of sixteen wavefronts
 int back_parts(int64_t M, int64_t F)
 {
-    const int64_t rows = F <= 1024 ? 8 : F <= 4096 ? 2 : 1, most = F <= 4096 ? 512 : 256, groups = ceil_div(M, rows);
+    const int64_t rows = F <= 1024 ? 8 : F <= 4096 ? 2 : 1, most = F <= 4096 ? back_most<64>() : back_most<1024>(), groups = ceil_div(M, rows);
     return (int)(groups < most ? groups : most);
 }
 
