@@ -122,7 +122,9 @@ class MemoryCore:
         return State(self, N)
 
     def optimizer(self, bits=32, weight_decay=0.0):
-        """hts.AdamW over the core's arrays and their gradients, on the core's stream: matrices decay, nothing else does; their copies are written with them."""
+        """hts.AdamW over the core's arrays and their gradients, on the core's stream: matrices decay, nothing else does; their copies are written with them.  bits: 32 or 8."""
+        if bits not in (8, 32):
+            raise hts.HtsError("optimizer: states have 32 or 8 bits")
         tensors = []
         with torch.cuda.stream(self.ctx.stream):
             for name, p in self.p.items():
