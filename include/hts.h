@@ -400,7 +400,7 @@ int32_t hts_layer_norm_backward(hts_seq_ctx *ctx, const hts_layer_norm_desc *des
  * Values that are not finite (queries and keys: or whose squares' sum is not) make NaN of what sees them: outputs from their step on to the episode's end,
  * gradients of their episode.  Nothing of them reaches other episodes, sequences or, of q, k, a and b, other groups' heads (but for the sums dA and
  * da_bias).  The same holds for a state that leaves binary32, within 64 steps of where it does, and in calls of more than 16
- * steps for one of which up to 64 steps would make 2^128 of 1 (growing decays, long keys), whatever the state is. */
+ * steps and backward calls where up to 64 steps would make 2^128 of 1 (growing decays, long keys), whatever the state is. */
 typedef struct { int32_t T, N, H, G, K, V; int32_t precision, normalize, softplus; float scale; } hts_delta_rule_desc;
 typedef struct {
     hts_steps q, k, v, a, b;

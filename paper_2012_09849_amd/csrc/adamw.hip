@@ -3,8 +3,8 @@
 //   g <- g min(1, c / (|g| + 1e-6));  m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2;  p <- p (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // Bound by bytes: every entry's numbers are read once and written once, by one launch for all tensors (and one before it for the norm, where it is asked for).
-// 41 M entries with states in 8 bits: norm 31 us of 82 MB, update 180 to 190 of 653 MB (3.5 TB/s), 130 of them issue of vector instructions, those of the random bits
-// and the rounding first of all; 1.7 M in 32 bits, which stay in the cache between updates, 4.2 and 11.6; 49 thousand 2.7 and 5.0.
+// 41 M entries with states in 8 bits: a call among others 196 us, under a trace 31 for the norm (82 MB; its wavefronts wait for 80% of their cycles) and 175 to 191 for the update, which untraced
+// leaves about 165 for 653 MB (4.0 TB/s): issue of vector instructions, 99 million of a wavefront's, 161 us at 2.4 GHz, those of the random bits and the rounding first of all; 1.7 M in 32 bits, which stay in the cache between updates, 4.2 and 11.7; 49 thousand 2.7 and 4.9.
 //
 // A workgroup takes 2048 entries of one tensor, which a table of the plan names; a wavefront 256 of them at a time, 4 neighbours a lane.  Without contraction of
 // products and sums (a build flag of this file) the arithmetic is that of its terms one by one, so states in 8 bits have the same bits wherever these rules are followed.

@@ -12,6 +12,8 @@
 //
 // Three kinds of kernels: what needs the chunk's own steps only (prep: every chunk at a time), what goes from chunk to chunk (forward, reverse: 32 of the values'
 // entries of a head at a time, whose states never meet), and the gradients that sum over the values (grads: every chunk at a time again).
+// (The chunked form is the published one of Yang, Wang, Zhang, Shen and Kim, "Parallelizing Linear Transformers with the Delta Rule over Sequence Length", 2024, the decays those of
+// Yang, Kautz and Hatamizadeh, "Gated Delta Networks", 2024; the derivations here are from the rule above.)
 #include "delta.hpp"
 
 namespace hts {
@@ -52,7 +54,7 @@ __device__ __forceinline__ int pair_of(int back, int seen) { return back * (back
 // ---- what needs the chunk's steps only --------------------------------------------------------------------------------
 // A workgroup for a chunk of a head.  What leaves is in the order that the kernels after it take it in (fragments in lane order, read in whole lines).  Bound by the latency of its
 // dependent phases (gates, lengths, products, substitution in blocks of 16, two levels of products), with three workgroups a unit to overlap them: 1024 chunks of 128 keys in bf16
-// 38 us, 18 MB read and 68 MB written (105 MB for the backward call); 90 chunks of 37 in binary32 17 to 18.
+// 38 us, 18 MB read and 63 MB written (101 MB for the backward call); 90 chunks of 37 in binary32 17.
 template <typename T, int KP> struct PrepLds {
     static constexpr int PITCH = Num<T>::exact_pitch(KP), LINE = 65;
     static constexpr int FAR = 0, EPISODE = FAR + 8 * CHUNK, STRENGTH = EPISODE + 4 * CHUNK, Q = STRENGTH + 4 * CHUNK, K = Q + 4 * CHUNK, BAD = K + 4 * CHUNK;
@@ -330,7 +332,7 @@ __device__ __forceinline__ uint64_t steps_between(int from, int to) { return (~0
 
 // What a segment makes of ones on the diagonal may leave binary32 where no state does: growing steps make more of them than there is, also of a state of nothing, and strong decays less,
 // which later steps may bring back.  So it is held as numbers between 2^-40 and 2^-10 at each chunk's beginning (a chunk may lengthen by 2^127) and a power of two, which joins them when
-// they have met the state.  Powers of two round nothing.  (A prompt of 8192, 8 heads of 128 x 128, bf16: 209 us, without 208; lifted in every chunk 214.)
+// they have met the state.  Powers of two round nothing.  (A prompt of 8192, 8 heads of 128 x 128, bf16, in turn: 209 us, without 208; lifted in every chunk 214.)
 __device__ __forceinline__ int lift_of(uint32_t most)
 {
     const int e = (int)(most >> 23);
@@ -370,8 +372,8 @@ template <typename T, int KP> struct RunLds {
 template <int KP> constexpr int key_tiles() { return KP / 64 > 0 ? KP / 64 : 1; }
 
 // A workgroup for 32 of a head's values (a column of the state meets no other one), its state in registers; rows of LDS hand on what another wavefront takes.  A chunk is a chain of four
-// phases (left over, Z, outputs and state), and a prompt or storage a chain of chunks: bound by latency, with two workgroups a unit.  512 x 16 steps, 8 heads of 128 x 128, bf16: 79 us,
-// 3 us a chunk of the chain where memory is near, the rest the states for the backward call (127 MB written).  The matrix units work for 11 us of it, the vector units for 22.  129 x 5 in binary32 20.
+// phases (left over, Z, outputs and state), and a prompt or storage a chain of chunks: bound by latency, with two workgroups a unit.  512 x 16 steps, 8 heads of 128 x 128, bf16: 76 us,
+// 3 us a chunk of the chain where memory is near, the rest the states for the backward call (126 MB written).  The matrix units work for 12 us of it, the vector units for 18.  129 x 5 in binary32 19.
 //
 // ENDS: a segment's part of the states after it, of its own steps and, in tiles behind the values', of the state before it: that of a one for each key, and no values
 template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) void forward_kernel(const DeltaArgs a)
@@ -707,7 +709,7 @@ template <typename T, int KP, bool ENDS> __global__ __launch_bounds__(256, 2) vo
 
 // The states that the segments begin with: from one to the next, what its steps make of the state before it and what they add.  A segment in which an episode begins leaves
 // nothing of it (not 0 times it, which would be NaN of what is not finite).  A step's latency is all that counts: a wavefront for 16 of the keys' entries (with two such parts
-// each a prompt of 8192 and 8 heads of 128 keys took 31 us, and 35 with operands requested where they are used; now 25, seven steps).
+// each a prompt of 8192 and 8 heads of 128 keys took 31 us, and 35 with operands requested where they are used; now 25, with the powers of two 27, seven steps).
 template <typename T, int KP> __global__ __launch_bounds__(4 * KP) void begin_kernel(const DeltaArgs a)
 {
     typedef RunLds<T, KP> L;
@@ -960,7 +962,7 @@ __device__ __forceinline__ float sign_of(int chunk, int n) { return (chunk + n) 
 // What a matrix instruction drops of its products goes towards minus infinity.  Gradients have either sign, but keys, queries, values and states may be mostly positive, and then
 // the sums of the decays' gradients over thousands of steps add up what was dropped (da_bias 4.6e-6 of its values off, 512 x 16 steps).  So every second chunk has all gradients
 // with the other sign, here and in the sums after it.
-// The same shape as the forward kernel's, with one phase more: 512 x 16 steps, 8 heads of 128 x 128, bf16 105 us, 129 x 5 in binary32 21.
+// The same shape as the forward kernel's, with one phase more: 512 x 16 steps, 8 heads of 128 x 128, bf16 104 us, 129 x 5 in binary32 21.
 template <typename T, int KP> __global__ __launch_bounds__(256, 2) void reverse_kernel(const DeltaArgs a)
 {
     typedef RunLds<T, KP> L;
@@ -1229,7 +1231,7 @@ __device__ __forceinline__ float entry(const Exact<bf16_t> &x, int i) { return (
 // the entry of the fragments that row 4 q + r of a lane's tile t is
 template <typename T> __device__ __forceinline__ float entry(const Exact<T> (&f)[2], int t, int r) { return t & 1 ? (t & 2 ? entry(f[1], 4 + r) : entry(f[0], 4 + r)) : t & 2 ? entry(f[1], r) : entry(f[0], r); }
 
-// One workgroup a unit, by its registers: 1024 chunks of 128 x 128 in bf16 150 us, four one after the other on a unit.  190 MB come and go (37 us at a copy's rate) and the matrix units work
+// One workgroup a unit, by its registers: 1024 chunks of 128 x 128 in bf16 149 us, four one after the other on a unit.  193 MB come and go (38 us at a copy's rate) and the matrix units work
 // for 19 us; two wavefronts a SIMD do not hide more of each other's waiting.  90 chunks of 37 x 53 in binary32 22.
 //
 // A workgroup for a chunk of a head.  SHARED: other heads have the same queries and keys, whose gradients leave in binary32, to be added up.

@@ -3,7 +3,7 @@
 //   y = (x - mean) r w + b,  r = 1 / sqrt(var + eps);   with h = (x - mean) r, g = dy w:  dx = r (g - mean(g) - h mean(g h)) + add,  dw = sum dy h,  db = sum dy
 //
 // Bound by bytes: a row is read once, into the registers of a wavefront (up to 1024 entries), of four or of sixteen, its variance is the mean square of what is left
-// after the mean is taken off, so that nothing cancels, and it is written once.  The backward call keeps nothing of the forward call: the mean and r of a row
+// after the mean is taken off, so that nothing cancels, and it is written once.  (Rows whose squares leave binary32 are read again.)  The backward call keeps nothing of the forward call: the mean and r of a row
 // that is in registers cost two reductions and no bytes.
 #include "seq.hpp"
 
@@ -170,7 +170,7 @@ template <typename T, int ROW, int PER> __device__ __forceinline__ Roots again_s
     return Roots{r, __builtin_ldexpf(r, by)};
 }
 
-// Rows in turn, by four workgroups a unit: 8192 x 512 in bf16 5.9 us (2.8 TB/s of 16.8 MB; the launch, a row's arrival and two reductions are most of it), 16 rows 2.5.
+// Rows in turn, by four workgroups a unit: 8192 x 512 in bf16 6.4 us (2.6 TB/s of 16.8 MB; the launch, a row's arrival and two reductions are most of it), 16 rows 2.6.
 template <int ROW> constexpr int threads() { return ROW > 256 ? ROW : 256; }
 template <typename T, int ROW, int PER> __global__ __launch_bounds__(threads<ROW>()) void norm_kernel(const NormArgs a)
 {
@@ -209,8 +209,9 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(threads<ROW
     }
 }
 
-// Registers hold the sums of dw and db of all rows that a thread sees, and rows come while others are worked on: 8192 x 2048 in bf16 with a residual's gradient, 134 MB, 37.8 us
-// (3.6 TB/s), 1021 x 777 in binary32 6.4, and 3 to 5 for the workgroups' sums (the call 41 us, without the next rows on their way 43).
+// Registers hold the sums of dw and db of all rows that a thread sees, and rows come while others are worked on: 8192 x 2048 in bf16 with a residual's gradient, 134 MB, 36.2 us
+// (3.7 TB/s: wavefronts wait for 56% of their cycles, for rows and at the three reductions of each, and the vector units work for 18 us), 1021 x 777 in binary32 6.8 (128 workgroups of eight rows on 256
+// units), and 3 to 5 for the workgroups' sums (the call 39 us).
 // Rows that a workgroup works on at a time: eight of a wavefront each, two of four, one of sixteen; and all of its threads go round together
 template <int ROW> constexpr int back_threads() { return ROW > 256 ? ROW : 512; }
 
