@@ -148,8 +148,9 @@ __device__ __forceinline__ bool ordinary(float sum, int F, float eps)
     return v >= 0x1p-100f && v <= 3.402823466e38f;
 }
 __device__ __forceinline__ float inverse_root(float sum, int F, float eps) { return 1.0f / __builtin_sqrtf(sum / (float)F + eps); }
-// h as such deviations, of a row that is read again; what makes them of length one, and that of the row's own.  Rows that are ordinary come out as they were (in a workgroup whose rows meet at barriers).
-struct Roots { float of_h, of_row; };
+// h as such deviations, of a row that is read again; what makes them of length one, and the power of two in them.  Rows that are ordinary come out as they were (in a workgroup whose rows meet
+// at barriers).
+struct Roots { float of_h; int power; };
 template <typename T, int ROW, int PER> __device__ __forceinline__ Roots again_scaled(const T *from, const bool there, float (&h)[PER][Piece<T>::V], const bool as_it_is, const int first, const int F, const float eps, float *shared,
                                                                                      int &turn)
 {
@@ -165,9 +166,9 @@ template <typename T, int ROW, int PER> __device__ __forceinline__ Roots again_s
 #pragma unroll
         for (int i = 0; i < Piece<T>::V; ++i) most = fmaxf(most, __builtin_fabsf(x[p][i]));
     most = fmaxf(row_most<ROW>(most, shared, turn), __builtin_sqrtf(eps));
-    const int e = (int)(__float_as_uint(most) >> 23), by = as_it_is || e == 0 || e == 255 ? 0 : 127 - e;
+    const int e = (int)(__float_as_uint(most) >> 23), by = as_it_is || e == 255 ? 0 : 127 - e;         // (the smallest numbers: by 2^127)
     const float r = inverse_root(deviations<T, ROW, PER, true>(x, h, by, first, F, shared, turn), F, __builtin_ldexpf(eps, 2 * by));
-    return Roots{r, __builtin_ldexpf(r, by)};
+    return Roots{r, by};
 }
 
 // Rows in turn, by four workgroups a unit: 8192 x 512 in bf16 6.4 us (2.6 TB/s of 16.8 MB; the launch, a row's arrival and two reductions are most of it), 16 rows 2.6.
@@ -255,14 +256,14 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
                 s[1] = __builtin_fmaf(g, h[p][i], s[1]);
             }
     };
-    const auto give = [&](const float (&h)[PER][V], const Piece<T> (&dy)[PER], const Piece<T> (&add)[PER], const float (&s)[2], float r, int64_t to) {
+    const auto give = [&](const float (&h)[PER][V], const Piece<T> (&dy)[PER], const Piece<T> (&add)[PER], const float (&s)[2], float r, auto finish, int64_t to) {
         const float mean = s[0] / (float)a.F, along = s[1] / (float)a.F;
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             float o[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                o[i] = r * __builtin_fmaf(-h[p][i], along, dy[p][i] * w[p][i] - mean);
+                o[i] = finish(r * __builtin_fmaf(-h[p][i], along, dy[p][i] * w[p][i] - mean));
                 if (a.add) o[i] += add[p][i];
             }
             store((T *)a.dx + to * a.dx_ld + first + p * ROW * V, o, a.F - first - p * ROW * V);
@@ -300,7 +301,7 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
         } else along_row(h, dy, s, to < a.M ? r : 0.0f, true);
         if (a.dx) {
             row_sums<ROW>(s, sums, turn);
-            if (to < a.M && !rare) give(h, dy, add, s, r, to);
+            if (to < a.M && !rare) give(h, dy, add, s, r, [](float x) { return x; }, to);
         }
 #pragma unroll
         for (int p = 0; p < PER; ++p) { x[p] = next_x[p]; dy[p] = next_dy[p]; add[p] = next_add[p]; }
@@ -324,7 +325,7 @@ template <typename T, int ROW, int PER> __global__ __launch_bounds__(back_thread
             along_row(h, dy, s, roots.of_h, rare);
             if (!a.dx) continue;
             row_sums<ROW>(s, sums, turn);
-            if (rare) give(h, dy, add, s, roots.of_row, to);
+            if (rare) give(h, dy, add, s, roots.of_h, [&](float x) { return __builtin_ldexpf(x, roots.power); }, to);
         }
     if (!a.sums) return;
     // a workgroup's sums: its rows in order
