@@ -171,7 +171,7 @@ template <typename T, int ROW, int PER> __device__ __forceinline__ Roots again_s
     return Roots{r, by};
 }
 
-// Rows in turn, by four workgroups a unit: 8192 x 512 in bf16 6.4 us (2.6 TB/s of 16.8 MB; the launch, a row's arrival and two reductions are most of it), 16 rows 2.6.
+// Rows in turn, by four workgroups a unit: 8192 x 512 in bf16 6.0 to 6.4 us (2.6 to 2.8 TB/s of 16.8 MB; the launch, a row's arrival and two reductions are most of it), 16 rows 2.6.
 template <int ROW> constexpr int threads() { return ROW > 256 ? ROW : 256; }
 template <typename T, int ROW, int PER> __global__ __launch_bounds__(threads<ROW>()) void norm_kernel(const NormArgs a)
 {
