@@ -160,7 +160,7 @@ def _user(case, s):
     new = lambda *shape: torch.empty(*shape, dtype=dt, device="cuda")  # noqa: E731
     if kind in ("norm", "norm_grad"):
         m, f = case["m"], case["f"]
-        need = hts.layer_norm_workspace(m, f, precision=precision)
+        need = hts.layer_norm_workspace(m, f, precision=precision) if kind == "norm_grad" else 0        # (a forward call needs none)
         s["out"] = {"y": new(m, f)} if kind == "norm" else {"dx": new(m, f), "dw": new32(f), "db": new32(f)}
     else:
         t, n, h, gr, k, v = (case[c] for c in "tnhgkv")
